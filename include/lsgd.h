@@ -426,6 +426,50 @@ lsgd_status lsgd_conv3x3_bn_bf16(const uint16_t* x, const uint16_t* W, float* y,
 lsgd_status lsgd_batchnorm_stats_noalloc(const float* y, int64_t P, int C, int G, float* mean,
                                          float* rstd, void* stream);
 
+/* Group normalisation with an activation, channels last: the normalisation to put in BatchNorm's
+ * place where workers should keep no statistics of their own (per-worker BatchNorm, Sec. A.4,
+ * keeps running ones that the model average leaves out).  Stand-alone; no counterpart in the paper.
+ * x [G][B][P][C] (G workers, B images each, P positions, channel fastest) is split into `groups`
+ * groups of D = C / groups neighbouring channels; for each image and group
+ *   mean = sum x / (P D),  rstd = 1 / sqrt(sum (x - mean)^2 / (P D) + eps),
+ *   y = act(gamma (x - mean) rstd + beta),
+ * act(z) = z, max(z, 0) or z / (1 + exp(-z)).  gamma and beta are worker g's C values at gamma + g
+ * par_gs and beta + g par_gs (par_gs >= C: they may stand in a replica-major parameter buffer).
+ * x and y are each LSGD_FP32 or LSGD_BF16 (lsgd_precision); mean and rstd [G][B][groups] fp32 are
+ * written too.  Statistics and arithmetic are fp32 (the deviations are taken from the mean, so a
+ * mean far above the deviation loses nothing more than x itself has); a bf16 y is rounded once.
+ * Deterministic.  Non-finite values of x make their own image's group NaN and no other.
+ *
+ * `workspace` is device memory of at least the bytes that lsgd_groupnorm_workspace reports, 16-byte
+ * aligned, whose contents do not matter before or after; calls (or captured graphs) that may run at
+ * the same time need one each.  No allocation: the calls may be captured into a CUDA graph.
+ * G <= 65535, G B <= 2^24, P <= 2^24, C <= 65536, sizes >= 1, C a multiple of groups, eps > 0.  Any C
+ * and any alignment of at least the element's are taken; vectors of up to 16 bytes are used where C
+ * and the pointers allow.  LSGD_EINVAL on anything else and for tensors that overlap.  Device pointers,
+ * asynchronous on `stream`, which belongs to the current device. */
+typedef enum { LSGD_ACT_NONE = 0, LSGD_ACT_RELU = 1, LSGD_ACT_SILU = 2 } lsgd_activation;
+lsgd_status lsgd_groupnorm_workspace(int G, int B, int64_t P, int C, int groups, int backward,
+                                     size_t* bytes);
+lsgd_status lsgd_groupnorm_forward(const void* x, int x_type, const float* gamma, const float* beta,
+                                   int64_t par_gs, void* y, int y_type, float* mean, float* rstd,
+                                   int G, int B, int64_t P, int C, int groups, float eps, int act,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* The gradients of lsgd_groupnorm_forward: with dz = dy act'(.), xh = (x - mean) rstd, m1 and m2 the
+ * means of gamma dz and of gamma dz xh over the image's group,
+ *   dx = rstd (gamma dz - m1 - xh m2),  dgamma = sum dz xh,  dbeta = sum dz,
+ * the sums over worker g's images and positions, written (not added) at dgamma + g par_gs and dbeta
+ * + g par_gs.  x, gamma, beta, mean and rstd as in the forward; dx has x's type, y and dy y's.
+ * ReLU's derivative is taken from the stored output (y > 0), as in the training step; the other
+ * activations do not read y (NULL is fine).  Sums are fp32 in a fixed order: deterministic.
+ * Workspace, limits and errors as for the forward (backward = 1). */
+lsgd_status lsgd_groupnorm_backward(const void* x, int x_type, const void* y, const void* dy,
+                                    int y_type, const float* gamma, const float* beta,
+                                    int64_t par_gs, const float* mean, const float* rstd, void* dx,
+                                    float* dgamma, float* dbeta, int G, int B, int64_t P, int C,
+                                    int groups, int act, void* workspace, size_t workspace_bytes,
+                                    void* stream);
+
 /* Worker mini-batch indices for one step into dst [K][B] int32 (device), as lsgd_local_step. */
 lsgd_status lsgd_sample_indices(int32_t* dst, uint64_t seed, int64_t step, int K, int B, int64_t N,
                                 void* stream);

@@ -25,6 +25,7 @@ COMPRESS_NONE, COMPRESS_SIGN, COMPRESS_EF_SIGN = 0, 1, 2
 STATE_WREF, STATE_ERROR, STATE_GLOBAL_MOMENTUM = 0, 1, 2
 HWARM_NONE, HWARM_LINEAR, HWARM_EXPONENTIAL, HWARM_CONSTANT = 0, 1, 2, 3
 SAMPLE_SHARDS, SAMPLE_RESHUFFLE = 0, 1
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 
 OK, EINVAL, ENOMEM, ECUDA, ESTATE, ENONFINITE, ETIMEOUT, EUNSUPPORTED, EIO = range(9)
 _STATUS = {0: "OK", 1: "EINVAL", 2: "ENOMEM", 3: "ECUDA", 4: "ESTATE", 5: "ENONFINITE",
@@ -43,6 +44,7 @@ EXPORTS = [
     "lsgd_sync_state", "lsgd_set_sync_state", "lsgd_schedule", "lsgd_device_status",
     "lsgd_bounded_wait_selftest", "lsgd_losses_async", "lsgd_synchronize", "lsgd_set_step",
     "lsgd_conv_wgrad_bf16", "lsgd_conv3x3_bf16", "lsgd_conv3x3_bn_bf16", "lsgd_run_batch",
+    "lsgd_groupnorm_workspace", "lsgd_groupnorm_forward", "lsgd_groupnorm_backward",
 ]
 PHASES = ["input", "forward", "loss", "backward", "update", "average"]
 
@@ -189,6 +191,14 @@ def lib():
             "lsgd_grouped_gemm_bf16": ([vp, ctypes.c_int, vp, ctypes.c_int, vp, ctypes.c_int,
                                         ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, vp], st),
             "lsgd_profile_read": ([vp, P(Profile)], st),
+            "lsgd_groupnorm_workspace": ([ctypes.c_int, ctypes.c_int, i64, ctypes.c_int, ctypes.c_int,
+                                          ctypes.c_int, P(ctypes.c_size_t)], st),
+            "lsgd_groupnorm_forward": ([vp, ctypes.c_int, vp, vp, i64, vp, ctypes.c_int, vp, vp, ctypes.c_int,
+                                        ctypes.c_int, i64, ctypes.c_int, ctypes.c_int, ctypes.c_float,
+                                        ctypes.c_int, vp, ctypes.c_size_t, vp], st),
+            "lsgd_groupnorm_backward": ([vp, ctypes.c_int, vp, vp, ctypes.c_int, vp, vp, i64, vp, vp, vp, vp, vp,
+                                         ctypes.c_int, ctypes.c_int, i64, ctypes.c_int, ctypes.c_int,
+                                         ctypes.c_int, vp, ctypes.c_size_t, vp], st),
         }
         for name, (args, res) in sig.items():
             f = getattr(L, name)
@@ -552,3 +562,94 @@ def lsgd_batchnorm_stats_noalloc(y, P: int, C: int, G: int, mean, rstd, stream=N
     stream = _current_stream() if stream is None else stream
     _check(lib().lsgd_batchnorm_stats_noalloc(_ptr(y), int(P), int(C), int(G), _ptr(mean),
                                               _ptr(rstd), ctypes.c_void_p(stream)))
+
+
+def _type_of(t):
+    """FP32 or BF16: how a tensor's values are held."""
+    name = str(t.dtype)
+    if name == "torch.float32":
+        return FP32
+    if name == "torch.bfloat16":
+        return BF16
+    raise LsgdError(EINVAL, f"a float32 or bfloat16 tensor is wanted, got {name}")
+
+
+def _checked(tensors):
+    """Checks (name, tensor or None, number of elements, types) rows: CUDA tensors of one device, contiguous
+    and large enough, so that no kernel leaves them.  Returns the device."""
+    dev = None
+    for name, t, n, types in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise LsgdError(EINVAL, f"{name}: a CUDA tensor is wanted")
+        if _type_of(t) not in types:
+            raise LsgdError(EINVAL, f"{name}: type {t.dtype} is not taken here")
+        if not t.is_contiguous() or t.numel() < n:
+            raise LsgdError(EINVAL, f"{name}: a contiguous tensor of at least {n} elements is wanted")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise LsgdError(EINVAL, f"{name}: on {t.device}, others on {dev}")
+    return dev
+
+
+def _on_device(dev, stream, workspace, nbytes, call):
+    """call(workspace pointer, its bytes, stream) with `dev` current.  Without a workspace one comes from
+    PyTorch's allocator for this call; on a stream other than the current one its memory is kept until
+    that stream has passed the call."""
+    import torch
+
+    with torch.cuda.device(dev):
+        cur = torch.cuda.current_stream()
+        st = cur.cuda_stream if stream is None else int(stream)
+        ws = workspace
+        if ws is None:
+            ws = torch.empty(max(1, nbytes), dtype=torch.uint8, device=dev)
+            if st != cur.cuda_stream:
+                ws.record_stream(torch.cuda.ExternalStream(st))
+        elif not ws.is_cuda or ws.device != dev or not ws.is_contiguous():
+            raise LsgdError(EINVAL, f"workspace: a contiguous CUDA tensor on {dev} is wanted")
+        _check(call(ctypes.c_void_p(ws.data_ptr()), ws.numel() * ws.element_size(), ctypes.c_void_p(st)))
+
+
+def lsgd_groupnorm_workspace(G: int, B: int, P: int, C: int, groups: int, backward: bool = False) -> int:
+    """Bytes of workspace that lsgd_groupnorm_forward (or _backward) needs for these sizes."""
+    n = ctypes.c_size_t()
+    _check(lib().lsgd_groupnorm_workspace(int(G), int(B), int(P), int(C), int(groups), int(bool(backward)),
+                                          ctypes.byref(n)))
+    return int(n.value)
+
+
+def lsgd_groupnorm_forward(x, gamma, beta, y, mean, rstd, G: int, B: int, P: int, C: int, groups: int,
+                           act: int = ACT_NONE, eps: float = 1e-5, par_gs: int = 0, workspace=None, stream=None):
+    """y = act(gamma (x - mean) rstd + beta) over groups of C / groups channels of each image: x, y
+    [G, B, P, C] float32 or bfloat16, mean and rstd [G, B, groups] float32, gamma and beta float32 at
+    worker stride par_gs (0: C)."""
+    nbytes = lsgd_groupnorm_workspace(G, B, P, C, groups)
+    par_gs = int(par_gs) or int(C)
+    n, ng, npar = G * B * P * C, G * B * groups, (G - 1) * par_gs + C
+    both, f = (FP32, BF16), (FP32,)
+    dev = _checked((("x", x, n, both), ("y", y, n, both), ("gamma", gamma, npar, f), ("beta", beta, npar, f),
+                    ("mean", mean, ng, f), ("rstd", rstd, ng, f)))
+    _on_device(dev, stream, workspace, nbytes, lambda ws, wn, st: lib().lsgd_groupnorm_forward(
+        _ptr(x), _type_of(x), _ptr(gamma), _ptr(beta), par_gs, _ptr(y), _type_of(y), _ptr(mean), _ptr(rstd),
+        int(G), int(B), int(P), int(C), int(groups), float(eps), int(act), ws, wn, st))
+
+
+def lsgd_groupnorm_backward(x, y, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, G: int, B: int, P: int, C: int,
+                            groups: int, act: int = ACT_NONE, par_gs: int = 0, workspace=None, stream=None):
+    """The gradients of lsgd_groupnorm_forward: dx (x's type) and, written at worker stride par_gs, dgamma and
+    dbeta (float32), from dy (y's type).  y, the stored output, is read for ReLU only (None otherwise)."""
+    nbytes = lsgd_groupnorm_workspace(G, B, P, C, groups, True)
+    par_gs = int(par_gs) or int(C)
+    n, ng, npar = G * B * P * C, G * B * groups, (G - 1) * par_gs + C
+    both, f = (FP32, BF16), (FP32,)
+    dev = _checked((("x", x, n, both), ("dx", dx, n, (_type_of(x),)), ("dy", dy, n, both),
+                    ("y", y, n, (_type_of(dy),)), ("gamma", gamma, npar, f), ("beta", beta, npar, f),
+                    ("dgamma", dgamma, npar, f), ("dbeta", dbeta, npar, f), ("mean", mean, ng, f),
+                    ("rstd", rstd, ng, f)))
+    _on_device(dev, stream, workspace, nbytes, lambda ws, wn, st: lib().lsgd_groupnorm_backward(
+        _ptr(x), _type_of(x), _ptr(y), _ptr(dy), _type_of(dy), _ptr(gamma), _ptr(beta), par_gs, _ptr(mean),
+        _ptr(rstd), _ptr(dx), _ptr(dgamma), _ptr(dbeta), int(G), int(B), int(P), int(C), int(groups), int(act),
+        ws, wn, st))

@@ -1,0 +1,597 @@
+// Group normalisation with an activation over channels-last tensors, forward and backward, for G workers of B
+// images each.  Unlike the per-worker BatchNorm of Sec. A.4 it keeps no statistics that differ from worker to worker.
+//
+// For image n, group q (D = C / groups channels) and its P x D values x:
+//   mean = sum x / (P D),  rstd = 1 / sqrt(sum (x - mean)^2 / (P D) + eps),  xh = (x - mean) rstd,
+//   y = act(gamma xh + beta).
+// Backward, with dz = dy act'(.), m1 and m2 the group's means of gamma dz and gamma dz xh:
+//   dgamma = sum dz xh,  dbeta = sum dz (over the worker's images and positions),
+//   dx = rstd (gamma dz - m1 - xh m2).
+//
+// Both are bound by memory.  A thread owns V neighbouring channels (a vector of up to 16 bytes) and walks down the
+// positions, so that its parameters and channel sums stay in registers whatever the group width.
+#include <algorithm>
+#include <string>
+
+#include "../../include/lsgd.h"
+#include "common.cuh"
+#include "lsgd_internal.h"
+
+namespace lsgd {
+namespace {
+
+template <int BYTES>
+struct RawOf;
+template <>
+struct RawOf<16> {
+  using type = uint4;
+};
+template <>
+struct RawOf<8> {
+  using type = uint2;
+};
+template <>
+struct RawOf<4> {
+  using type = uint32_t;
+};
+template <>
+struct RawOf<2> {
+  using type = uint16_t;
+};
+
+// V values of T as loaded, and as floats.
+template <typename T, int V>
+struct Vec {
+  using Raw = typename RawOf<V * (int)sizeof(T) <= 16 ? V * (int)sizeof(T) : 16>::type;
+  static constexpr int kN = V * (int)sizeof(T) <= 16 ? 1 : V * (int)sizeof(T) / 16;
+  Raw r[kN];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) r[i] = __ldg(reinterpret_cast<const Raw*>(p) + i);
+  }
+  __device__ __forceinline__ void floats(float (&v)[V]) const {
+    if constexpr (sizeof(T) == 4) {
+      const float* f = reinterpret_cast<const float*>(r);
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[j] = f[j];
+    } else if constexpr (V == 1) {
+      v[0] = bf2f((uint16_t)r[0]);
+    } else {
+      const uint32_t* w = reinterpret_cast<const uint32_t*>(r);
+#pragma unroll
+      for (int j = 0; j < V / 2; ++j) {
+        v[2 * j] = __uint_as_float(w[j] << 16);
+        v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+      }
+    }
+  }
+  __device__ __forceinline__ void set(const float (&v)[V]) {
+    if constexpr (sizeof(T) == 4) {
+      float* f = reinterpret_cast<float*>(r);
+#pragma unroll
+      for (int j = 0; j < V; ++j) f[j] = v[j];
+    } else if constexpr (V == 1) {
+      r[0] = f2bf(v[0]);
+    } else {
+      uint32_t* w = reinterpret_cast<uint32_t*>(r);
+#pragma unroll
+      for (int j = 0; j < V / 2; ++j) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+        w[j] = *reinterpret_cast<const uint32_t*>(&b);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(T* p) const {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) reinterpret_cast<Raw*>(p)[i] = r[i];
+  }
+};
+
+struct GnArgs {
+  const void *x, *y, *dy;
+  void* out;  // y (forward), dx (backward)
+  const float *gamma, *beta;
+  int64_t par_gs;
+  float *mean, *rstd;
+  float* part;    // split form: per (image, split, channel) pairs; backward's channel sums
+  float* sums;    // split backward: per (image, channel) pairs
+  float* m12;     // split backward: per (image, group) pairs (m1, m2)
+  float *dgamma, *dbeta;
+  int B, P, C, groups, D, act;
+  int S;          // position ranges of an image
+  int rows;       // positions of a range
+  int64_t N;
+  float eps;
+};
+
+// 1 / (1 + exp(-z)): the exponential's overflow gives 0.
+template <bool EXACT>
+__device__ __forceinline__ float sigmoid(float z) {
+  if constexpr (EXACT) return 1.f / (1.f + expf(-z));
+  return __fdividef(1.f, 1.f + __expf(-z));
+}
+
+// act(z).  EXACT (fp32 results): the accurate exponential and division; a bf16 result's rounding hides the fast ones'.
+// __fdividef gives 0 for divisors above 2^126, which is what 1 / (1 + exp(-z)) rounds to there.
+template <bool EXACT>
+__device__ __forceinline__ float activate(float z, int act) {
+  if (act == LSGD_ACT_RELU) return z < 0.f ? 0.f : z;  // NaN stays
+  if (act == LSGD_ACT_SILU) return z * sigmoid<EXACT>(z);
+  return z;
+}
+
+// ---- split form: any size, three launches ----
+
+constexpr int kSplitThreads = 256;
+
+// Per range and channel: forward (mean, sum of squared deviations), backward (sum dz, sum dz xh).
+template <typename XT, typename YT, int V, bool BWD>
+__global__ void __launch_bounds__(kSplitThreads) gn_partial_kernel(const GnArgs a, int tx_n, int ty_n) {
+  pdl_begin();
+  const int tx = threadIdx.x % tx_n, ty = threadIdx.x / tx_n;
+  const int c0 = (blockIdx.y * tx_n + tx) * V;
+  const bool on = ty < ty_n && c0 < a.C;
+  const int64_t n = blockIdx.x / a.S;
+  const int s = blockIdx.x % a.S;
+  const int p0 = s * a.rows, p1 = min(a.P, p0 + a.rows);
+  constexpr int U = 4;
+  float s0[V], s1[V];
+  float cnt = 0.f;
+#pragma unroll
+  for (int j = 0; j < V; ++j) s0[j] = s1[j] = 0.f;
+  if (on) {
+    const int64_t base = n * a.P * (int64_t)a.C + c0;
+    const XT* x = static_cast<const XT*>(a.x) + base;
+    if constexpr (!BWD) {
+      // batches of U positions: their mean and squared deviations, merged by Chan et al.'s formula
+      int p = p0 + ty;
+      for (; p + (U - 1) * ty_n < p1; p += U * ty_n) {
+        Vec<XT, V> r[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) r[i].load(x + (int64_t)(p + i * ty_n) * a.C);
+        float v[U][V];
+#pragma unroll
+        for (int i = 0; i < U; ++i) r[i].floats(v[i]);
+        const float w = U / (cnt + U), cw = cnt * w;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float m = (v[0][j] + v[1][j] + v[2][j] + v[3][j]) * (1.f / U);
+          float q = 0.f;
+#pragma unroll
+          for (int i = 0; i < U; ++i) q = fmaf(v[i][j] - m, v[i][j] - m, q);
+          const float d = m - s0[j];
+          s0[j] = fmaf(d, w, s0[j]);
+          s1[j] += fmaf(d * d, cw, q);
+        }
+        cnt += U;
+      }
+      for (; p < p1; p += ty_n) {
+        Vec<XT, V> r;
+        r.load(x + (int64_t)p * a.C);
+        float v[V];
+        r.floats(v);
+        const float w = 1.f / (cnt + 1.f), cw = cnt * w;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float d = v[j] - s0[j];
+          s0[j] = fmaf(d, w, s0[j]);
+          s1[j] = fmaf(d * d, cw, s1[j]);
+        }
+        cnt += 1.f;
+      }
+    } else {
+      const YT* dy = static_cast<const YT*>(a.dy) + base;
+      const YT* y = static_cast<const YT*>(a.y) + base;
+      float ga[V], be[V], mu[V], rs[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int64_t pc = (n / a.B) * a.par_gs + c0 + j;
+        ga[j] = a.gamma[pc];
+        be[j] = a.beta[pc];
+        mu[j] = a.mean[n * a.groups + (c0 + j) / a.D];
+        rs[j] = a.rstd[n * a.groups + (c0 + j) / a.D];
+      }
+#pragma unroll 2
+      for (int p = p0 + ty; p < p1; p += ty_n) {
+        Vec<XT, V> rx;
+        Vec<YT, V> rd, ry;
+        rx.load(x + (int64_t)p * a.C);
+        rd.load(dy + (int64_t)p * a.C);
+        if (a.act == LSGD_ACT_RELU) ry.load(y + (int64_t)p * a.C);
+        float xv[V], dv[V], yv[V];
+        rx.floats(xv);
+        rd.floats(dv);
+        if (a.act == LSGD_ACT_RELU) ry.floats(yv);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float xh = (xv[j] - mu[j]) * rs[j];
+          float dz = dv[j];
+          if (a.act == LSGD_ACT_RELU) dz = yv[j] > 0.f ? dz : 0.f;
+          if (a.act == LSGD_ACT_SILU) {
+            const float z = fmaf(xh, ga[j], be[j]), sg = sigmoid<sizeof(XT) == 4>(z);
+            dz *= sg * fmaf(z, 1.f - sg, 1.f);
+          }
+          s0[j] += dz;
+          s1[j] = fmaf(dz, xh, s1[j]);
+        }
+      }
+    }
+  }
+  // the rows of threads, one after another in thread 0's row
+  __shared__ float red[kSplitThreads * V * 2];
+  __shared__ float rc[kSplitThreads];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    red[(threadIdx.x * V + j) * 2] = s0[j];
+    red[(threadIdx.x * V + j) * 2 + 1] = s1[j];
+  }
+  rc[threadIdx.x] = cnt;
+  __syncthreads();
+  if (on && ty == 0) {
+    for (int t = 1; t < ty_n; ++t) {
+      const int o = threadIdx.x + t * tx_n;
+      const float oc = rc[o];
+      const float w = BWD || oc == 0.f ? 0.f : oc / (cnt + oc), cw = cnt * w;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float b0 = red[(o * V + j) * 2], b1 = red[(o * V + j) * 2 + 1];
+        if constexpr (BWD) {
+          s0[j] += b0;
+          s1[j] += b1;
+        } else if (oc > 0.f) {
+          const float d = b0 - s0[j];
+          s0[j] = fmaf(d, w, s0[j]);
+          s1[j] += fmaf(d * d, cw, b1);
+        }
+      }
+      cnt += oc;
+    }
+    float* out = a.part + ((n * a.S + s) * a.C + c0) * 2;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      out[2 * j] = s0[j];
+      out[2 * j + 1] = s1[j];
+    }
+  }
+}
+
+// (count, mean, M2) <- merged with (nb, mb, qb)
+__device__ __forceinline__ void chan(float& n, float& m, float& q, float nb, float mb, float qb) {
+  if (nb == 0.f) return;
+  const float t = n + nb, w = nb / t, d = mb - m;
+  m = fmaf(d, w, m);
+  q += fmaf(d * d, n * w, qb);
+  n = t;
+}
+
+// Forward: a warp per (image, group) merges its ranges' channels into mean and rstd.
+__global__ void __launch_bounds__(128) gn_stats_merge_kernel(const GnArgs a) {
+  pdl_begin();
+  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (w >= a.N * a.groups) return;
+  const int64_t n = w / a.groups;
+  const int q = (int)(w % a.groups);
+  float cn = 0.f, cm = 0.f, cq = 0.f;
+  for (int i = lane; i < a.S * a.D; i += 32) {
+    const int s = i / a.D, c = q * a.D + i % a.D;
+    const float2 v = *reinterpret_cast<const float2*>(a.part + ((n * a.S + s) * a.C + c) * 2);
+    chan(cn, cm, cq, (float)(min(a.P, (s + 1) * a.rows) - s * a.rows), v.x, v.y);
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    const float nb = __shfl_xor_sync(~0u, cn, o), mb = __shfl_xor_sync(~0u, cm, o),
+                qb = __shfl_xor_sync(~0u, cq, o);
+    chan(cn, cm, cq, nb, mb, qb);
+  }
+  if (lane == 0) {
+    a.mean[w] = cm;
+    a.rstd[w] = __frsqrt_rn(cq / cn + a.eps);
+  }
+}
+
+// Backward: per image, the ranges' channel sums added up, and the groups' m1 and m2.
+__global__ void __launch_bounds__(256) gn_sums_merge_kernel(const GnArgs a) {
+  pdl_begin();
+  const int64_t n = blockIdx.x;
+  float2* sums = reinterpret_cast<float2*>(a.sums) + n * a.C;
+  for (int c = threadIdx.x; c < a.C; c += 256) {
+    float2 t = make_float2(0.f, 0.f);
+    for (int s = 0; s < a.S; ++s) {
+      const float2 v = reinterpret_cast<const float2*>(a.part)[(n * a.S + s) * a.C + c];
+      t.x += v.x;
+      t.y += v.y;
+    }
+    sums[c] = t;
+  }
+  __syncthreads();
+  const int lane = threadIdx.x & 31;
+  const float inv = 1.f / ((float)a.P * (float)a.D);
+  for (int q = threadIdx.x >> 5; q < a.groups; q += 8) {
+    float2 t = make_float2(0.f, 0.f);
+    for (int d = lane; d < a.D; d += 32) {
+      const float ga = a.gamma[(n / a.B) * a.par_gs + q * a.D + d];
+      const float2 v = sums[q * a.D + d];
+      t.x = fmaf(ga, v.x, t.x);
+      t.y = fmaf(ga, v.y, t.y);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      t.x += __shfl_xor_sync(~0u, t.x, o);
+      t.y += __shfl_xor_sync(~0u, t.y, o);
+    }
+    if (lane == 0) reinterpret_cast<float2*>(a.m12)[n * a.groups + q] = make_float2(t.x * inv, t.y * inv);
+  }
+}
+
+// The second pass: y or dx from the statistics.
+template <typename XT, typename YT, int V, bool BWD>
+__global__ void __launch_bounds__(kSplitThreads) gn_apply_kernel(const GnArgs a, int tx_n, int ty_n) {
+  pdl_begin();
+  const int tx = threadIdx.x % tx_n, ty = threadIdx.x / tx_n;
+  const int c0 = (blockIdx.y * tx_n + tx) * V;
+  if (ty >= ty_n || c0 >= a.C) return;
+  const int64_t n = blockIdx.x / a.S;
+  const int p0 = (blockIdx.x % a.S) * a.rows, p1 = min(a.P, p0 + a.rows);
+  const int64_t base = n * a.P * (int64_t)a.C + c0;
+  const XT* x = static_cast<const XT*>(a.x) + base;
+  float ga[V], be[V], mu[V], rs[V], m1[V], m2[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int64_t pc = (n / a.B) * a.par_gs + c0 + j, pg = n * a.groups + (c0 + j) / a.D;
+    ga[j] = a.gamma[pc];
+    be[j] = a.beta[pc];
+    mu[j] = a.mean[pg];
+    rs[j] = a.rstd[pg];
+    if constexpr (BWD) {
+      m1[j] = a.m12[2 * pg];
+      m2[j] = a.m12[2 * pg + 1];
+    }
+  }
+  if constexpr (!BWD) {
+    YT* out = static_cast<YT*>(a.out) + base;
+#pragma unroll
+    for (int j = 0; j < V; ++j) ga[j] *= rs[j];
+#pragma unroll 4
+    for (int p = p0 + ty; p < p1; p += ty_n) {
+      Vec<XT, V> r;
+      r.load(x + (int64_t)p * a.C);
+      float v[V];
+      r.floats(v);
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[j] = activate<sizeof(YT) == 4>(fmaf(v[j] - mu[j], ga[j], be[j]), a.act);
+      Vec<YT, V> o;
+      o.set(v);
+      o.store(out + (int64_t)p * a.C);
+    }
+  } else {
+    const YT* dy = static_cast<const YT*>(a.dy) + base;
+    const YT* y = static_cast<const YT*>(a.y) + base;
+    XT* out = static_cast<XT*>(a.out) + base;
+#pragma unroll 2
+    for (int p = p0 + ty; p < p1; p += ty_n) {
+      Vec<XT, V> rx;
+      Vec<YT, V> rd, ry;
+      rx.load(x + (int64_t)p * a.C);
+      rd.load(dy + (int64_t)p * a.C);
+      if (a.act == LSGD_ACT_RELU) ry.load(y + (int64_t)p * a.C);
+      float xv[V], dv[V], yv[V];
+      rx.floats(xv);
+      rd.floats(dv);
+      if (a.act == LSGD_ACT_RELU) ry.floats(yv);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float xh = (xv[j] - mu[j]) * rs[j];
+        float dz = dv[j];
+        if (a.act == LSGD_ACT_RELU) dz = yv[j] > 0.f ? dz : 0.f;
+        if (a.act == LSGD_ACT_SILU) {
+          const float z = fmaf(xh, ga[j], be[j]), sg = sigmoid<sizeof(XT) == 4>(z);
+          dz *= sg * fmaf(z, 1.f - sg, 1.f);
+        }
+        xv[j] = rs[j] * (fmaf(ga[j], dz, -m1[j]) - xh * m2[j]);
+      }
+      Vec<XT, V> o;
+      o.set(xv);
+      o.store(out + (int64_t)p * a.C);
+    }
+  }
+}
+
+// dgamma and dbeta of worker g: the sums of its `rows` rows of channel pairs (sum dz, sum dz xh), a fixed order.
+__global__ void __launch_bounds__(256) gn_param_grad_kernel(const float2* sums, int64_t rows, int C, int64_t par_gs,
+                                                            float* dgamma, float* dbeta) {
+  pdl_begin();
+  const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4;
+  const int c = blockIdx.x * 16 + cx;
+  const int64_t g = blockIdx.y;
+  float2 t = make_float2(0.f, 0.f);
+  if (c < C) {
+#pragma unroll 4
+    for (int64_t r = ry; r < rows; r += 16) {
+      const float2 v = sums[(g * rows + r) * C + c];
+      t.x += v.x;
+      t.y += v.y;
+    }
+  }
+  __shared__ float2 red[16][17];
+  red[ry][cx] = t;
+  __syncthreads();
+  if (ry == 0 && c < C) {
+    for (int i = 1; i < 16; ++i) {
+      t.x += red[i][cx].x;
+      t.y += red[i][cx].y;
+    }
+    dbeta[g * par_gs + c] = t.x;
+    dgamma[g * par_gs + c] = t.y;
+  }
+}
+
+// Ranges per image of the split form: enough for four CTAs per SM, of 8192 values at least.
+int gn_ranges(int64_t N, int P, int C) {
+  const int64_t by_size = ((int64_t)P * C + 8191) / 8192, by_sms = (4LL * kNumSMs + N - 1) / N;
+  const int64_t s = std::max<int64_t>(1, std::min<int64_t>({by_size, by_sms, (int64_t)P, 256}));
+  const int64_t rows = (P + s - 1) / s;
+  return (int)((P + rows - 1) / rows);
+}
+
+template <typename XT, typename YT, int V, bool BWD>
+cudaError_t gn_split(GnArgs a, cudaStream_t st) {
+  a.S = gn_ranges(a.N, a.P, a.C);
+  a.rows = (a.P + a.S - 1) / a.S;
+  const int cols = a.C / V, tx = std::min(cols, kSplitThreads), ty = kSplitThreads / tx;
+  const dim3 grid((unsigned)(a.N * a.S), (cols + tx - 1) / tx);
+  cudaError_t e = launch_pdl(gn_partial_kernel<XT, YT, V, BWD>, grid, dim3(kSplitThreads), 0, st, a, tx, ty);
+  if (e != cudaSuccess) return e;
+  if constexpr (BWD) {
+    e = launch_pdl(gn_sums_merge_kernel, dim3((unsigned)a.N), dim3(256), 0, st, a);
+  } else {
+    e = launch_pdl(gn_stats_merge_kernel, dim3((unsigned)((a.N * a.groups + 3) / 4)), dim3(128), 0, st, a);
+  }
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(gn_apply_kernel<XT, YT, V, BWD>, grid, dim3(kSplitThreads), 0, st, a, tx, ty);
+  if (e != cudaSuccess || !BWD) return e;
+  return launch_pdl(gn_param_grad_kernel, dim3((a.C + 15) / 16, (unsigned)(a.N / a.B)), dim3(256), 0, st,
+                    (const float2*)a.sums, (int64_t)a.B, a.C, a.par_gs, a.dgamma, a.dbeta);
+}
+
+template <typename XT, typename YT, bool BWD>
+cudaError_t gn_run(const GnArgs& a, int vmax, cudaStream_t st) {
+  if constexpr (sizeof(XT) == 2) {
+    if (vmax >= 8) return gn_split<XT, YT, 8, BWD>(a, st);
+  }
+  if (vmax >= 4) return gn_split<XT, YT, 4, BWD>(a, st);
+  if (vmax >= 2) return gn_split<XT, YT, 2, BWD>(a, st);
+  return gn_split<XT, YT, 1, BWD>(a, st);
+}
+
+template <bool BWD>
+cudaError_t gn_typed(const GnArgs& a, bool xb, bool yb, int vmax, cudaStream_t st) {
+  if (xb) return yb ? gn_run<uint16_t, uint16_t, BWD>(a, vmax, st) : gn_run<uint16_t, float, BWD>(a, vmax, st);
+  return yb ? gn_run<float, uint16_t, BWD>(a, vmax, st) : gn_run<float, float, BWD>(a, vmax, st);
+}
+
+// The widest vector (a power of two of values) that divides C and whose accesses to p (size z each) are aligned.
+int gn_vec(int v, int C, const void* p, int z) {
+  while (v > 1 && (C % v || reinterpret_cast<uintptr_t>(p) % std::min(16, v * z))) v >>= 1;
+  return v;
+}
+
+size_t gn_workspace(int64_t N, int P, int C, int groups, bool backward) {
+  const size_t split = (size_t)N * gn_ranges(N, P, C) * C * 2;
+  return 4 * (split + (backward ? (size_t)N * C * 2 + (size_t)N * groups * 2 : 0));
+}
+
+lsgd_status gn_error(lsgd_status s, const char* fn, const char* what) {
+  set_last_error(std::string(fn) + ": " + what);
+  return s;
+}
+
+const char* gn_shape_error(int G, int B, int64_t P, int C, int groups) {
+  if (G < 1 || B < 1 || P < 1 || C < 1 || groups < 1) return "G, B, P, C and groups must be at least 1";
+  if (C % groups) return "C must be a multiple of groups";
+  if (G > 65535 || (int64_t)G * B > (1 << 24) || C > 65536 || P > (1 << 24))
+    return "at most 65535 workers, 2^24 images (G B), 65536 channels and 2^24 positions";
+  return nullptr;
+}
+
+bool gn_overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + nb && y < x + na;
+}
+
+bool gn_bad_align(const void* p, int z) { return reinterpret_cast<uintptr_t>(p) % z != 0; }
+
+}  // namespace
+}  // namespace lsgd
+
+extern "C" {
+
+lsgd_status lsgd_groupnorm_workspace(int G, int B, int64_t P, int C, int groups, int backward, size_t* bytes) {
+  using namespace lsgd;
+  const char* bad = gn_shape_error(G, B, P, C, groups);
+  if (!bad && !bytes) bad = "bytes is NULL";
+  if (bad) return gn_error(LSGD_EINVAL, "lsgd_groupnorm_workspace", bad);
+  *bytes = gn_workspace((int64_t)G * B, (int)P, C, groups, backward != 0);
+  return LSGD_OK;
+}
+
+lsgd_status lsgd_groupnorm_forward(const void* x, int x_type, const float* gamma, const float* beta,
+                                   int64_t par_gs, void* y, int y_type, float* mean, float* rstd, int G, int B,
+                                   int64_t P, int C, int groups, float eps, int act, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+  using namespace lsgd;
+  const char* fn = "lsgd_groupnorm_forward";
+  const char* bad = gn_shape_error(G, B, P, C, groups);
+  const bool xb = x_type == LSGD_BF16, yb = y_type == LSGD_BF16;
+  const int xz = xb ? 2 : 4, yz = yb ? 2 : 4;
+  if (bad) return gn_error(LSGD_EINVAL, fn, bad);
+  const int64_t N = (int64_t)G * B;
+  const size_t n = (size_t)N * P * C, ns = (size_t)N * groups * 4, need = gn_workspace(N, (int)P, C, groups, false);
+  if (!x || !gamma || !beta || !y || !mean || !rstd) bad = "a pointer is NULL";
+  else if ((!xb && x_type != LSGD_FP32) || (!yb && y_type != LSGD_FP32)) bad = "types are LSGD_FP32 or LSGD_BF16";
+  else if (act != LSGD_ACT_NONE && act != LSGD_ACT_RELU && act != LSGD_ACT_SILU) bad = "unknown activation";
+  else if (!(eps > 0.f) || !(eps < 1e30f)) bad = "eps must be positive and finite";
+  else if (par_gs < C) bad = "par_gs must be at least C";
+  else if (gn_bad_align(x, xz) || gn_bad_align(y, yz) || gn_bad_align(gamma, 4) || gn_bad_align(beta, 4) ||
+           gn_bad_align(mean, 4) || gn_bad_align(rstd, 4))
+    bad = "a pointer is not aligned to its element";
+  else if (!workspace || workspace_bytes < need || gn_bad_align(workspace, 16))
+    bad = "workspace NULL, not 16-byte aligned or smaller than lsgd_groupnorm_workspace says";
+  else if (gn_overlap(x, n * xz, y, n * yz) || gn_overlap(mean, ns, rstd, ns) || gn_overlap(x, n * xz, workspace, need) ||
+           gn_overlap(y, n * yz, workspace, need) || gn_overlap(y, n * yz, mean, ns) || gn_overlap(y, n * yz, rstd, ns))
+    bad = "tensors overlap";
+  if (bad) return gn_error(LSGD_EINVAL, fn, bad);
+  GnArgs a{};
+  a.x = x, a.out = y, a.gamma = gamma, a.beta = beta, a.par_gs = par_gs, a.mean = mean, a.rstd = rstd;
+  a.part = static_cast<float*>(workspace);
+  a.B = B, a.P = (int)P, a.C = C, a.groups = groups, a.D = C / groups, a.act = act, a.N = N, a.eps = eps;
+  const int v = gn_vec(gn_vec(xb ? 8 : 4, C, x, xz), C, y, yz);
+  const cudaError_t e = gn_typed<false>(a, xb, yb, v, (cudaStream_t)stream);
+  return e == cudaSuccess ? LSGD_OK : gn_error(LSGD_ECUDA, fn, cudaGetErrorString(e));
+}
+
+lsgd_status lsgd_groupnorm_backward(const void* x, int x_type, const void* y, const void* dy, int y_type,
+                                    const float* gamma, const float* beta, int64_t par_gs, const float* mean,
+                                    const float* rstd, void* dx, float* dgamma, float* dbeta, int G, int B,
+                                    int64_t P, int C, int groups, int act, void* workspace,
+                                    size_t workspace_bytes, void* stream) {
+  using namespace lsgd;
+  const char* fn = "lsgd_groupnorm_backward";
+  const char* bad = gn_shape_error(G, B, P, C, groups);
+  const bool xb = x_type == LSGD_BF16, yb = y_type == LSGD_BF16;
+  const int xz = xb ? 2 : 4, yz = yb ? 2 : 4;
+  if (bad) return gn_error(LSGD_EINVAL, fn, bad);
+  const int64_t N = (int64_t)G * B;
+  const size_t n = (size_t)N * P * C, need = gn_workspace(N, (int)P, C, groups, true);
+  const bool relu = act == LSGD_ACT_RELU;
+  if (!x || !dy || !gamma || !beta || !mean || !rstd || !dx || !dgamma || !dbeta || (relu && !y))
+    bad = "a pointer is NULL (y may be only where the activation is not ReLU)";
+  else if ((!xb && x_type != LSGD_FP32) || (!yb && y_type != LSGD_FP32)) bad = "types are LSGD_FP32 or LSGD_BF16";
+  else if (act != LSGD_ACT_NONE && !relu && act != LSGD_ACT_SILU) bad = "unknown activation";
+  else if (par_gs < C) bad = "par_gs must be at least C";
+  else if (gn_bad_align(x, xz) || gn_bad_align(dx, xz) || gn_bad_align(dy, yz) || (relu && gn_bad_align(y, yz)) ||
+           gn_bad_align(gamma, 4) || gn_bad_align(beta, 4) || gn_bad_align(mean, 4) || gn_bad_align(rstd, 4) ||
+           gn_bad_align(dgamma, 4) || gn_bad_align(dbeta, 4))
+    bad = "a pointer is not aligned to its element";
+  else if (!workspace || workspace_bytes < need || gn_bad_align(workspace, 16))
+    bad = "workspace NULL, not 16-byte aligned or smaller than lsgd_groupnorm_workspace says";
+  else if (gn_overlap(x, n * xz, dx, n * xz) || gn_overlap(dy, n * yz, dx, n * xz) ||
+           (relu && gn_overlap(y, n * yz, dx, n * xz)) || gn_overlap(dgamma, 4 * (size_t)C, dbeta, 4 * (size_t)C) ||
+           gn_overlap(dx, n * xz, workspace, need) || gn_overlap(x, n * xz, workspace, need) ||
+           gn_overlap(dy, n * yz, workspace, need))
+    bad = "tensors overlap";
+  if (bad) return gn_error(LSGD_EINVAL, fn, bad);
+  GnArgs a{};
+  a.x = x, a.y = y, a.dy = dy, a.out = dx, a.gamma = gamma, a.beta = beta, a.par_gs = par_gs;
+  a.mean = const_cast<float*>(mean), a.rstd = const_cast<float*>(rstd), a.dgamma = dgamma, a.dbeta = dbeta;
+  a.B = B, a.P = (int)P, a.C = C, a.groups = groups, a.D = C / groups, a.act = act, a.N = N;
+  a.part = static_cast<float*>(workspace);
+  a.sums = a.part + (size_t)N * gn_ranges(N, a.P, C) * C * 2;
+  a.m12 = a.sums + (size_t)N * C * 2;
+  int v = gn_vec(gn_vec(gn_vec(xb ? 8 : 4, C, x, xz), C, dx, xz), C, dy, yz);
+  if (relu) v = gn_vec(v, C, y, yz);
+  const cudaError_t e = gn_typed<true>(a, xb, yb, v, (cudaStream_t)stream);
+  return e == cudaSuccess ? LSGD_OK : gn_error(LSGD_ECUDA, fn, cudaGetErrorString(e));
+}
+
+}  // extern "C"
