@@ -440,8 +440,8 @@ lsgd_status lsgd_batchnorm_stats_noalloc(const float* y, int64_t P, int C, int G
  * mean far above the deviation loses nothing more than x itself has); a bf16 y is rounded once.
  * Deterministic.  Non-finite values of x make their own image's group NaN and no other.
  *
- * `workspace` is device memory of at least the bytes that lsgd_groupnorm_workspace reports, 16-byte
- * aligned, whose contents do not matter before or after; calls (or captured graphs) that may run at
+ * `workspace` is device memory of at least the bytes that lsgd_groupnorm_workspace reports (0: it is
+ * not used and may be NULL), 16-byte aligned, whose contents do not matter before or after; calls (or captured graphs) that may run at
  * the same time need one each.  No allocation: the calls may be captured into a CUDA graph.
  * G <= 65535, G B <= 2^24, P <= 2^24, C <= 65536, sizes >= 1, C a multiple of groups, eps > 0.  Any C
  * and any alignment of at least the element's are taken; vectors of up to 16 bytes are used where C

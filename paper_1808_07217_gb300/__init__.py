@@ -9,6 +9,7 @@ raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -564,55 +565,70 @@ def lsgd_batchnorm_stats_noalloc(y, P: int, C: int, G: int, mean, rstd, stream=N
                                               _ptr(rstd), ctypes.c_void_p(stream)))
 
 
+_TYPES = {}
+
+
 def _type_of(t):
     """FP32 or BF16: how a tensor's values are held."""
-    name = str(t.dtype)
-    if name == "torch.float32":
-        return FP32
-    if name == "torch.bfloat16":
-        return BF16
-    raise LsgdError(EINVAL, f"a float32 or bfloat16 tensor is wanted, got {name}")
+    if not _TYPES:
+        import torch
+
+        _TYPES.update({torch.float32: FP32, torch.bfloat16: BF16})
+    ty = _TYPES.get(t.dtype)
+    if ty is None:
+        raise LsgdError(EINVAL, f"a float32 or bfloat16 tensor is wanted, got {t.dtype}")
+    return ty
 
 
-def _checked(tensors):
-    """Checks (name, tensor or None, number of elements, types) rows: CUDA tensors of one device, contiguous
-    and large enough, so that no kernel leaves them.  Returns the device."""
+def _checked(*tensors):
+    """Checks (name, tensor or None, number of elements, type or None for either) rows: CUDA tensors of one
+    device, contiguous and large enough, so that no kernel leaves them.  Returns the device's index."""
     dev = None
-    for name, t, n, types in tensors:
+    for name, t, n, ty in tensors:
         if t is None:
             continue
-        if not t.is_cuda:
+        at = t.get_device()
+        if at < 0:
             raise LsgdError(EINVAL, f"{name}: a CUDA tensor is wanted")
-        if _type_of(t) not in types:
+        if _type_of(t) != ty and ty is not None:
             raise LsgdError(EINVAL, f"{name}: type {t.dtype} is not taken here")
-        if not t.is_contiguous() or t.numel() < n:
+        if t.numel() < n or not t.is_contiguous():
             raise LsgdError(EINVAL, f"{name}: a contiguous tensor of at least {n} elements is wanted")
         if dev is None:
-            dev = t.device
-        elif t.device != dev:
-            raise LsgdError(EINVAL, f"{name}: on {t.device}, others on {dev}")
+            dev = at
+        elif at != dev:
+            raise LsgdError(EINVAL, f"{name}: on device {at}, others on {dev}")
     return dev
 
 
-def _on_device(dev, stream, workspace, nbytes, call):
-    """call(workspace pointer, its bytes, stream) with `dev` current.  Without a workspace one comes from
-    PyTorch's allocator for this call; on a stream other than the current one its memory is kept until
-    that stream has passed the call."""
+def _launch(dev, stream, workspace, nbytes, fn, head, tail=()):
+    """fn(*head, workspace, its bytes, *tail, stream) with device `dev` current, on `stream` or that device's
+    current one.  Without a workspace one of nbytes comes from PyTorch's allocator for this call; on a
+    stream other than the current one its memory is kept until that stream has passed the call."""
     import torch
 
-    with torch.cuda.device(dev):
-        cur = torch.cuda.current_stream()
-        st = cur.cuda_stream if stream is None else int(stream)
-        ws = workspace
-        if ws is None:
-            ws = torch.empty(max(1, nbytes), dtype=torch.uint8, device=dev)
-            if st != cur.cuda_stream:
+    if torch.cuda.current_device() != dev:
+        with torch.cuda.device(dev):
+            return _launch(dev, stream, workspace, nbytes, fn, head, tail)
+    cur = torch.cuda.current_stream().cuda_stream
+    st = cur if stream is None else int(stream)
+    ws, wp, wn = workspace, None, 0
+    if ws is None:
+        if nbytes:
+            ws = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+            wp, wn = ws.data_ptr(), nbytes
+            if st != cur:
                 ws.record_stream(torch.cuda.ExternalStream(st))
-        elif not ws.is_cuda or ws.device != dev or not ws.is_contiguous():
-            raise LsgdError(EINVAL, f"workspace: a contiguous CUDA tensor on {dev} is wanted")
-        _check(call(ctypes.c_void_p(ws.data_ptr()), ws.numel() * ws.element_size(), ctypes.c_void_p(st)))
+    elif ws.get_device() != dev or not ws.is_contiguous():
+        raise LsgdError(EINVAL, f"workspace: a contiguous tensor on CUDA device {dev} is wanted")
+    else:
+        wp, wn = ws.data_ptr(), ws.numel() * ws.element_size()
+    status = fn(*head, wp, wn, *tail, st)
+    if status != OK:
+        _check(status)
 
 
+@functools.lru_cache(maxsize=256)
 def lsgd_groupnorm_workspace(G: int, B: int, P: int, C: int, groups: int, backward: bool = False) -> int:
     """Bytes of workspace that lsgd_groupnorm_forward (or _backward) needs for these sizes."""
     n = ctypes.c_size_t()
@@ -627,14 +643,13 @@ def lsgd_groupnorm_forward(x, gamma, beta, y, mean, rstd, G: int, B: int, P: int
     [G, B, P, C] float32 or bfloat16, mean and rstd [G, B, groups] float32, gamma and beta float32 at
     worker stride par_gs (0: C)."""
     nbytes = lsgd_groupnorm_workspace(G, B, P, C, groups)
-    par_gs = int(par_gs) or int(C)
+    par_gs = par_gs or C
     n, ng, npar = G * B * P * C, G * B * groups, (G - 1) * par_gs + C
-    both, f = (FP32, BF16), (FP32,)
-    dev = _checked((("x", x, n, both), ("y", y, n, both), ("gamma", gamma, npar, f), ("beta", beta, npar, f),
-                    ("mean", mean, ng, f), ("rstd", rstd, ng, f)))
-    _on_device(dev, stream, workspace, nbytes, lambda ws, wn, st: lib().lsgd_groupnorm_forward(
-        _ptr(x), _type_of(x), _ptr(gamma), _ptr(beta), par_gs, _ptr(y), _type_of(y), _ptr(mean), _ptr(rstd),
-        int(G), int(B), int(P), int(C), int(groups), float(eps), int(act), ws, wn, st))
+    dev = _checked(("x", x, n, None), ("y", y, n, None), ("gamma", gamma, npar, FP32), ("beta", beta, npar, FP32),
+                   ("mean", mean, ng, FP32), ("rstd", rstd, ng, FP32))
+    _launch(dev, stream, workspace, nbytes, lib().lsgd_groupnorm_forward,
+            (x.data_ptr(), _type_of(x), gamma.data_ptr(), beta.data_ptr(), par_gs, y.data_ptr(), _type_of(y),
+             mean.data_ptr(), rstd.data_ptr(), G, B, P, C, groups, eps, act))
 
 
 def lsgd_groupnorm_backward(x, y, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, G: int, B: int, P: int, C: int,
@@ -642,14 +657,13 @@ def lsgd_groupnorm_backward(x, y, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta
     """The gradients of lsgd_groupnorm_forward: dx (x's type) and, written at worker stride par_gs, dgamma and
     dbeta (float32), from dy (y's type).  y, the stored output, is read for ReLU only (None otherwise)."""
     nbytes = lsgd_groupnorm_workspace(G, B, P, C, groups, True)
-    par_gs = int(par_gs) or int(C)
+    par_gs = par_gs or C
     n, ng, npar = G * B * P * C, G * B * groups, (G - 1) * par_gs + C
-    both, f = (FP32, BF16), (FP32,)
-    dev = _checked((("x", x, n, both), ("dx", dx, n, (_type_of(x),)), ("dy", dy, n, both),
-                    ("y", y, n, (_type_of(dy),)), ("gamma", gamma, npar, f), ("beta", beta, npar, f),
-                    ("dgamma", dgamma, npar, f), ("dbeta", dbeta, npar, f), ("mean", mean, ng, f),
-                    ("rstd", rstd, ng, f)))
-    _on_device(dev, stream, workspace, nbytes, lambda ws, wn, st: lib().lsgd_groupnorm_backward(
-        _ptr(x), _type_of(x), _ptr(y), _ptr(dy), _type_of(dy), _ptr(gamma), _ptr(beta), par_gs, _ptr(mean),
-        _ptr(rstd), _ptr(dx), _ptr(dgamma), _ptr(dbeta), int(G), int(B), int(P), int(C), int(groups), int(act),
-        ws, wn, st))
+    xt, yt = _type_of(x), _type_of(dy)
+    dev = _checked(("x", x, n, xt), ("dx", dx, n, xt), ("dy", dy, n, yt), ("y", y, n, yt), ("gamma", gamma, npar, FP32),
+                   ("beta", beta, npar, FP32), ("dgamma", dgamma, npar, FP32), ("dbeta", dbeta, npar, FP32),
+                   ("mean", mean, ng, FP32), ("rstd", rstd, ng, FP32))
+    _launch(dev, stream, workspace, nbytes, lib().lsgd_groupnorm_backward,
+            (x.data_ptr(), xt, y.data_ptr() if y is not None else None, dy.data_ptr(), yt, gamma.data_ptr(),
+             beta.data_ptr(), par_gs, mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), dgamma.data_ptr(),
+             dbeta.data_ptr(), G, B, P, C, groups, act))

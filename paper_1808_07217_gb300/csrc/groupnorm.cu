@@ -11,6 +11,7 @@
 // Both are bound by memory.  A thread owns V neighbouring channels (a vector of up to 16 bytes) and walks down the
 // positions, so that its parameters and channel sums stay in registers whatever the group width.
 #include <algorithm>
+#include <atomic>
 #include <string>
 
 #include "../../include/lsgd.h"
@@ -65,6 +66,14 @@ struct Vec {
       }
     }
   }
+  __device__ __forceinline__ float at(int j) const {
+    if constexpr (sizeof(T) == 4) return reinterpret_cast<const float*>(r)[j];
+    else if constexpr (V == 1) return bf2f((uint16_t)r[0]);
+    else {
+      const uint32_t w = reinterpret_cast<const uint32_t*>(r)[j / 2];
+      return __uint_as_float(j & 1 ? w & 0xffff0000u : w << 16);
+    }
+  }
   __device__ __forceinline__ void set(const float (&v)[V]) {
     if constexpr (sizeof(T) == 4) {
       float* f = reinterpret_cast<float*>(r);
@@ -102,6 +111,7 @@ struct GnArgs {
   int rows;       // positions of a range
   int64_t N;
   float eps;
+  int cl, tx_n, ty_n, sub;  // resident form: CTAs per image, threads across and down, channels summed in a thread
 };
 
 // 1 / (1 + exp(-z)): the exponential's overflow gives 0.
@@ -454,14 +464,421 @@ cudaError_t gn_split(GnArgs a, cudaStream_t st) {
                     (const float2*)a.sums, (int64_t)a.B, a.C, a.par_gs, a.dgamma, a.dbeta);
 }
 
+// ---- resident form: an image (or, in a cluster, a CTA's range of its positions) stays in registers ----
+//
+// One read of x, one write: the values that a thread loads are summed, their squared deviations from the CTA's own
+// mean are summed, and they are normalised, all out of registers.  A cluster's CTAs exchange (count, mean, squared
+// deviations) through distributed shared memory and merge them in rank order (Chan et al.).  A thread holds kHold
+// values, so that 1024 threads per SM fit the register file (64 each) and keep 64 to 128 KB of loads in flight.
+
+constexpr int kFwdHold = 32, kBwdHold = 16;  // the backward also holds dz
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// The float at `p` of this CTA's shared memory, in CTA `rank` of the cluster.
+__device__ __forceinline__ float peer_float(const float* p, int rank) {
+  uint32_t at;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+
+// Adds up every thread's V channel values over the block's rows of threads: afterwards red[r][c] for r < the returned
+// number of rows holds partial sums of column c of C / sub, `sub` neighbouring channels to a column.  Where the threads
+// across are a power of two below a warp, the rows of a warp are added by shuffles first.
+template <int V>
+__device__ __forceinline__ int column_sums(float (&v)[V], float* red, int tx, int ty, int tx_n, int ty_n, int sub) {
+  int nv = V;
+#pragma unroll
+  for (int w = V / 2; w >= 1; w >>= 1) {
+    if (nv > V / sub) {
+#pragma unroll
+      for (int j = 0; j < w; ++j) v[j] = v[2 * j] + v[2 * j + 1];
+      nv >>= 1;
+    }
+  }
+  const int cols = tx_n * nv;
+  if (tx_n < 32 && (tx_n & (tx_n - 1)) == 0) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      if (j < nv)
+        for (int o = 16; o >= tx_n; o >>= 1) v[j] += __shfl_xor_sync(~0u, v[j], o);
+    }
+    if ((threadIdx.x & 31) < tx_n) {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (j < nv) red[(threadIdx.x >> 5) * cols + tx * nv + j] = v[j];
+    }
+    return blockDim.x >> 5;
+  }
+  if (ty < ty_n) {
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (j < nv) red[ty * cols + tx * nv + j] = v[j];
+  }
+  return ty_n;
+}
+
+// out[q] = the sum over red's rows and the columns of group q (dn columns each), a warp per group.
+__device__ __forceinline__ void group_sums(const float* red, int rows, int groups, int dn, float* out) {
+  const int lane = threadIdx.x & 31, cols = groups * dn;
+  for (int q = threadIdx.x >> 5; q < groups; q += blockDim.x >> 5) {
+    float t = 0.f;
+    for (int i = lane; i < rows * dn; i += 32) t += red[(i / dn) * cols + q * dn + i % dn];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) t += __shfl_xor_sync(~0u, t, o);
+    if (lane == 0) out[q] = t;
+  }
+}
+
+// The groups of a thread's V channels, from the group and the place in it of the first.
+template <int V, typename F>
+__device__ __forceinline__ void each_group(int c0, int D, F f) {
+  int q = c0 / D, r = c0 - q * D;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    f(j, q);
+    if (++r == D) r = 0, ++q;
+  }
+}
+
+template <typename XT, typename YT, int V>
+__global__ void __launch_bounds__(1024, 1) gn_fwd_resident_kernel(const GnArgs a) {
+  constexpr int R = kFwdHold / V;
+  extern __shared__ float sm[];
+  float* gmean = sm;                // [groups]: the CTA's, then the image's mean
+  float* gsq = gmean + a.groups;    // [groups]: squared deviations, then rstd
+  float* own = gsq + a.groups;      // [2 groups]: what the other CTAs of the cluster read
+  float* par = own + 2 * a.groups;  // [2][C]: gamma and beta
+  float* red = par + 2 * a.C;
+  const int tx = threadIdx.x % a.tx_n, ty = threadIdx.x / a.tx_n, c0 = tx * V;
+  const int rank = a.cl > 1 ? blockIdx.x % a.cl : 0;
+  const int64_t n = a.cl > 1 ? blockIdx.x / a.cl : blockIdx.x;
+  const int p0 = rank * a.rows, p1 = min(a.P, p0 + a.rows), cnt = max(0, p1 - p0);
+  const int first = p0 + ty, last = ty < a.ty_n ? p1 : 0;
+  pdl_begin();
+  const int64_t base = n * a.P * (int64_t)a.C + c0;
+  const XT* x = static_cast<const XT*>(a.x) + base;
+  Vec<XT, V> r[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (first + i * a.ty_n < last) r[i].load(x + (int64_t)(first + i * a.ty_n) * a.C);
+  for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
+    const int64_t pc = (n / a.B) * a.par_gs + c;
+    par[c] = a.gamma[pc], par[a.C + c] = a.beta[pc];
+  }
+  const int dn = a.D / a.sub;
+  float t[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) t[j] = 0.f;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (first + i * a.ty_n < last) {
+      float v[V];
+      r[i].floats(v);
+#pragma unroll
+      for (int j = 0; j < V; ++j) t[j] += v[j];
+    }
+  int rows = column_sums<V>(t, red, tx, ty, a.tx_n, a.ty_n, a.sub);
+  __syncthreads();
+  group_sums(red, rows, a.groups, dn, gmean);
+  __syncthreads();
+  const float inv = cnt ? 1.f / ((float)cnt * (float)a.D) : 0.f;
+  float mu[V];
+  if (ty < a.ty_n) each_group<V>(c0, a.D, [&](int j, int q) { mu[j] = gmean[q] * inv; });
+#pragma unroll
+  for (int j = 0; j < V; ++j) t[j] = 0.f;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (first + i * a.ty_n < last) {
+      float v[V];
+      r[i].floats(v);
+#pragma unroll
+      for (int j = 0; j < V; ++j) t[j] = fmaf(v[j] - mu[j], v[j] - mu[j], t[j]);
+    }
+  rows = column_sums<V>(t, red, tx, ty, a.tx_n, a.ty_n, a.sub);
+  __syncthreads();
+  group_sums(red, rows, a.groups, dn, gsq);
+  __syncthreads();
+  if (a.cl > 1) {
+    for (int q = threadIdx.x; q < a.groups; q += blockDim.x) own[2 * q] = gmean[q] * inv, own[2 * q + 1] = gsq[q];
+    cluster_arrive();
+    cluster_wait();
+  }
+  for (int q = threadIdx.x; q < a.groups; q += blockDim.x) {
+    float m = gmean[q] * inv, sq = gsq[q], k = (float)cnt * a.D;
+    if (a.cl > 1) {
+      k = m = sq = 0.f;
+      for (int c = 0; c < a.cl; ++c)
+        chan(k, m, sq, (float)max(0, min(a.P, (c + 1) * a.rows) - c * a.rows) * a.D, peer_float(own + 2 * q, c),
+             peer_float(own + 2 * q + 1, c));
+    }
+    const float rs = __frsqrt_rn(sq / k + a.eps);
+    gmean[q] = m;
+    gsq[q] = rs;
+    if (rank == 0) a.mean[n * a.groups + q] = m, a.rstd[n * a.groups + q] = rs;
+  }
+  __syncthreads();
+  if (a.cl > 1) cluster_arrive();  // this CTA has read the others' sums; the wait is at the end
+  if (ty < a.ty_n) {
+    float ga[V], be[V];
+    each_group<V>(c0, a.D, [&](int j, int q) {
+      mu[j] = gmean[q], ga[j] = par[c0 + j] * gsq[q], be[j] = par[a.C + c0 + j];
+    });
+    YT* out = static_cast<YT*>(a.out) + base;
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      if (first + i * a.ty_n < last) {
+        float v[V];
+        r[i].floats(v);
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = activate<sizeof(YT) == 4>(fmaf(v[j] - mu[j], ga[j], be[j]), a.act);
+        Vec<YT, V> o;
+        o.set(v);
+        o.store(out + (int64_t)(first + i * a.ty_n) * a.C);
+      }
+  }
+  if (a.cl > 1) cluster_wait();
+}
+
+template <typename XT, typename YT, int V>
+__global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a) {
+  constexpr int R = kBwdHold / V;
+  extern __shared__ float sm[];
+  float* gm = sm;                     // [2 groups]: m1 and m2
+  float* own = gm + 2 * a.groups;     // [2 groups]
+  float* stat = own + 2 * a.groups;   // [2 groups]: mean and rstd
+  float* par = stat + 2 * a.groups;   // [2][C]: gamma and beta
+  float* chans = par + 2 * a.C;       // [2][C]: sum dz, sum dz xh
+  float* red = chans + 2 * a.C;       // [rows][C], twice
+  const int tx = threadIdx.x % a.tx_n, ty = threadIdx.x / a.tx_n, c0 = tx * V;
+  const int rank = a.cl > 1 ? blockIdx.x % a.cl : 0;
+  const int64_t n = a.cl > 1 ? blockIdx.x / a.cl : blockIdx.x;
+  const int p0 = rank * a.rows, p1 = min(a.P, p0 + a.rows);
+  const int first = p0 + ty, last = ty < a.ty_n ? p1 : 0;
+  const bool relu = a.act == LSGD_ACT_RELU, silu = a.act == LSGD_ACT_SILU;
+  pdl_begin();
+  const int64_t base = n * a.P * (int64_t)a.C + c0;
+  const XT* x = static_cast<const XT*>(a.x) + base;
+  const YT* dy = static_cast<const YT*>(a.dy) + base;
+  const YT* y = static_cast<const YT*>(a.y) + base;
+  Vec<XT, V> r[R];
+  float dz[R][V];
+  {
+    Vec<YT, V> rd[R], ry[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      if (first + i * a.ty_n < last) {
+        const int64_t at = (int64_t)(first + i * a.ty_n) * a.C;
+        r[i].load(x + at);
+        rd[i].load(dy + at);
+        if (relu) ry[i].load(y + at);
+      }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) dz[i][j] = 0.f;
+      if (first + i * a.ty_n < last) {
+        rd[i].floats(dz[i]);
+        if (relu) {
+          float yv[V];
+          ry[i].floats(yv);
+#pragma unroll
+          for (int j = 0; j < V; ++j) dz[i][j] = yv[j] > 0.f ? dz[i][j] : 0.f;
+        }
+      }
+    }
+  }
+  for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
+    const int64_t pc = (n / a.B) * a.par_gs + c;
+    par[c] = a.gamma[pc], par[a.C + c] = a.beta[pc];
+  }
+  for (int q = threadIdx.x; q < a.groups; q += blockDim.x)
+    stat[2 * q] = a.mean[n * a.groups + q], stat[2 * q + 1] = a.rstd[n * a.groups + q];
+  __syncthreads();
+  float s0[V], s1[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) s0[j] = s1[j] = 0.f;
+  if (ty < a.ty_n) {
+    // channel by channel, so that one channel's parameters are in registers at a time
+    each_group<V>(c0, a.D, [&](int j, int q) {
+      const float mu = stat[2 * q], rs = stat[2 * q + 1], ga = par[c0 + j], be = par[a.C + c0 + j];
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (first + i * a.ty_n < last) {
+          const float xh = (r[i].at(j) - mu) * rs;
+          if (silu) {
+            const float z = fmaf(xh, ga, be), sg = sigmoid<sizeof(XT) == 4>(z);
+            dz[i][j] *= sg * fmaf(z, 1.f - sg, 1.f);
+          }
+          s0[j] += dz[i][j];
+          s1[j] = fmaf(dz[i][j], xh, s1[j]);
+        }
+    });
+  }
+  const int shuffled = a.tx_n < 32 && (a.tx_n & (a.tx_n - 1)) == 0;
+  const int rows = shuffled ? blockDim.x >> 5 : a.ty_n;
+  float* red1 = red + rows * a.C;
+  column_sums<V>(s0, red, tx, ty, a.tx_n, a.ty_n, 1);
+  column_sums<V>(s1, red1, tx, ty, a.tx_n, a.ty_n, 1);
+  __syncthreads();
+  float2* out = reinterpret_cast<float2*>(a.sums) + (int64_t)blockIdx.x * a.C;
+  if (rows <= 32) {
+    for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
+      float t0 = 0.f, t1 = 0.f;
+      for (int i = 0; i < rows; ++i) t0 += red[i * a.C + c], t1 += red1[i * a.C + c];
+      chans[c] = t0, chans[a.C + c] = t1;
+      out[c] = make_float2(t0, t1);
+    }
+  } else {  // many rows over few channels: a warp per channel
+    const int lane = threadIdx.x & 31;
+    for (int c = threadIdx.x >> 5; c < a.C; c += blockDim.x >> 5) {
+      float t0 = 0.f, t1 = 0.f;
+      for (int i = lane; i < rows; i += 32) t0 += red[i * a.C + c], t1 += red1[i * a.C + c];
+#pragma unroll
+      for (int o = 16; o; o >>= 1) t0 += __shfl_xor_sync(~0u, t0, o), t1 += __shfl_xor_sync(~0u, t1, o);
+      if (lane == 0) {
+        chans[c] = t0, chans[a.C + c] = t1;
+        out[c] = make_float2(t0, t1);
+      }
+    }
+  }
+  __syncthreads();
+  {
+    const int lane = threadIdx.x & 31;
+    const float inv = 1.f / ((float)a.P * (float)a.D);
+    for (int q = threadIdx.x >> 5; q < a.groups; q += blockDim.x >> 5) {
+      float t0 = 0.f, t1 = 0.f;
+      for (int d = lane; d < a.D; d += 32) {
+        const float g = par[q * a.D + d];
+        t0 = fmaf(g, chans[q * a.D + d], t0);
+        t1 = fmaf(g, chans[a.C + q * a.D + d], t1);
+      }
+#pragma unroll
+      for (int o = 16; o; o >>= 1) t0 += __shfl_xor_sync(~0u, t0, o), t1 += __shfl_xor_sync(~0u, t1, o);
+      if (lane == 0) {
+        float* to = a.cl > 1 ? own : gm;
+        to[2 * q] = t0 * inv, to[2 * q + 1] = t1 * inv;
+      }
+    }
+  }
+  if (a.cl > 1) {
+    cluster_arrive();
+    cluster_wait();
+    for (int q = threadIdx.x; q < 2 * a.groups; q += blockDim.x) {
+      float t = 0.f;
+      for (int c = 0; c < a.cl; ++c) t += peer_float(own + q, c);
+      gm[q] = t;
+    }
+  }
+  __syncthreads();
+  if (a.cl > 1) cluster_arrive();
+  if (ty < a.ty_n) {
+    each_group<V>(c0, a.D, [&](int j, int q) {
+      const float mu = stat[2 * q], rs = stat[2 * q + 1], k = rs * par[c0 + j], b = rs * gm[2 * q];
+      const float m = rs * rs * gm[2 * q + 1];
+#pragma unroll
+      for (int i = 0; i < R; ++i) dz[i][j] = fmaf(k, dz[i][j], -b) - (r[i].at(j) - mu) * m;
+    });
+    XT* dx = static_cast<XT*>(a.out) + base;
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      if (first + i * a.ty_n < last) {
+        Vec<XT, V> o;
+        o.set(dz[i]);
+        o.store(dx + (int64_t)(first + i * a.ty_n) * a.C);
+      }
+  }
+  if (a.cl > 1) cluster_wait();
+}
+
+// The resident form's CTAs per image (a power of two up to 8, the portable cluster size), or 0: the split form.  A
+// CTA of T threads takes `rows` positions if rows C / hold + C <= T, whatever the vector width (a row of threads is
+// C / V wide, and hold / V positions fall to each).  CTAs of 512 threads or fewer where they do; then, where the images
+// are few, more CTAs to an image down to 4096 values each.
+int gn_cluster(int64_t N, int P, int C, int hold) {
+  auto fits = [&](int cl, int T) { return (int64_t)((P + cl - 1) / cl) * C / hold + 1 + C <= T; };
+  int cl = 0;
+  for (int T = 512; T <= 1024 && !cl; T *= 2)
+    for (int c = 1; c <= 8 && !cl; c *= 2)
+      if (fits(c, T)) cl = c;
+  while (cl && cl < 8 && N * cl < kNumSMs && (int64_t)P * C / (2 * cl) >= 4096) cl *= 2;
+  return cl;
+}
+
+// The shape of a resident launch with vectors of V values: threads, and bytes of shared memory.
+void gn_resident_shape(GnArgs& a, int V, int hold, bool bwd, int* threads, size_t* smem) {
+  a.rows = (a.P + a.cl - 1) / a.cl;
+  a.tx_n = a.C / V;
+  a.ty_n = (a.rows + hold / V - 1) / (hold / V);
+  *threads = (a.tx_n * a.ty_n + 31) / 32 * 32;
+  a.sub = std::min(V, a.D & -a.D);
+  const int rows = a.tx_n < 32 && (a.tx_n & (a.tx_n - 1)) == 0 ? *threads / 32 : a.ty_n;
+  *smem = 4 * (bwd ? 6 * (size_t)a.groups + 4 * (size_t)a.C + 2 * (size_t)rows * a.C
+                   : 4 * (size_t)a.groups + 2 * (size_t)a.C + (size_t)rows * (a.C / a.sub));
+}
+
+constexpr size_t kGnMaxSmem = 160 * 1024;
+template <typename K>
+cudaError_t gn_launch_resident(K kernel, std::atomic<int>& raised, const GnArgs& a, int threads, size_t smem,
+                               cudaStream_t st) {
+  if (threads > 1024 || smem > kGnMaxSmem) return cudaErrorInvalidValue;
+  if (smem > 48 * 1024) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (raised != dev + 1) {
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGnMaxSmem);
+      if (e != cudaSuccess) return e;
+      raised = dev + 1;
+    }
+  }
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(a.N * a.cl));
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = a.cl;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = a.cl > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+template <typename XT, typename YT, int V, bool BWD>
+cudaError_t gn_resident(GnArgs a, cudaStream_t st) {
+  int threads = 0;
+  size_t smem = 0;
+  static std::atomic<int> raised{0};  // device + 1 whose limit of shared memory this kernel's has been raised
+  gn_resident_shape(a, V, BWD ? kBwdHold : kFwdHold, BWD, &threads, &smem);
+  if constexpr (!BWD) {
+    return gn_launch_resident(gn_fwd_resident_kernel<XT, YT, V>, raised, a, threads, smem, st);
+  } else {
+    const cudaError_t e = gn_launch_resident(gn_bwd_resident_kernel<XT, YT, V>, raised, a, threads, smem, st);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(gn_param_grad_kernel, dim3((a.C + 15) / 16, (unsigned)(a.N / a.B)), dim3(256), 0, st,
+                      (const float2*)a.sums, (int64_t)a.B * a.cl, a.C, a.par_gs, a.dgamma, a.dbeta);
+  }
+}
+
+template <typename XT, typename YT, int V, bool BWD>
+cudaError_t gn_form(const GnArgs& a, cudaStream_t st) {
+  return a.cl ? gn_resident<XT, YT, V, BWD>(a, st) : gn_split<XT, YT, V, BWD>(a, st);
+}
+
 template <typename XT, typename YT, bool BWD>
 cudaError_t gn_run(const GnArgs& a, int vmax, cudaStream_t st) {
   if constexpr (sizeof(XT) == 2) {
-    if (vmax >= 8) return gn_split<XT, YT, 8, BWD>(a, st);
+    if (vmax >= 8) return gn_form<XT, YT, 8, BWD>(a, st);
   }
-  if (vmax >= 4) return gn_split<XT, YT, 4, BWD>(a, st);
-  if (vmax >= 2) return gn_split<XT, YT, 2, BWD>(a, st);
-  return gn_split<XT, YT, 1, BWD>(a, st);
+  if (vmax >= 4) return gn_form<XT, YT, 4, BWD>(a, st);
+  if (vmax >= 2) return gn_form<XT, YT, 2, BWD>(a, st);
+  return gn_form<XT, YT, 1, BWD>(a, st);
 }
 
 template <bool BWD>
@@ -477,6 +894,8 @@ int gn_vec(int v, int C, const void* p, int z) {
 }
 
 size_t gn_workspace(int64_t N, int P, int C, int groups, bool backward) {
+  const int cl = gn_cluster(N, P, C, backward ? kBwdHold : kFwdHold);
+  if (cl) return backward ? 4 * (size_t)N * cl * C * 2 : 0;
   const size_t split = (size_t)N * gn_ranges(N, P, C) * C * 2;
   return 4 * (split + (backward ? (size_t)N * C * 2 + (size_t)N * groups * 2 : 0));
 }
@@ -535,7 +954,7 @@ lsgd_status lsgd_groupnorm_forward(const void* x, int x_type, const float* gamma
   else if (gn_bad_align(x, xz) || gn_bad_align(y, yz) || gn_bad_align(gamma, 4) || gn_bad_align(beta, 4) ||
            gn_bad_align(mean, 4) || gn_bad_align(rstd, 4))
     bad = "a pointer is not aligned to its element";
-  else if (!workspace || workspace_bytes < need || gn_bad_align(workspace, 16))
+  else if (need && (!workspace || workspace_bytes < need || gn_bad_align(workspace, 16)))
     bad = "workspace NULL, not 16-byte aligned or smaller than lsgd_groupnorm_workspace says";
   else if (gn_overlap(x, n * xz, y, n * yz) || gn_overlap(mean, ns, rstd, ns) || gn_overlap(x, n * xz, workspace, need) ||
            gn_overlap(y, n * yz, workspace, need) || gn_overlap(y, n * yz, mean, ns) || gn_overlap(y, n * yz, rstd, ns))
@@ -545,6 +964,7 @@ lsgd_status lsgd_groupnorm_forward(const void* x, int x_type, const float* gamma
   a.x = x, a.out = y, a.gamma = gamma, a.beta = beta, a.par_gs = par_gs, a.mean = mean, a.rstd = rstd;
   a.part = static_cast<float*>(workspace);
   a.B = B, a.P = (int)P, a.C = C, a.groups = groups, a.D = C / groups, a.act = act, a.N = N, a.eps = eps;
+  a.cl = gn_cluster(N, a.P, C, kFwdHold);
   const int v = gn_vec(gn_vec(xb ? 8 : 4, C, x, xz), C, y, yz);
   const cudaError_t e = gn_typed<false>(a, xb, yb, v, (cudaStream_t)stream);
   return e == cudaSuccess ? LSGD_OK : gn_error(LSGD_ECUDA, fn, cudaGetErrorString(e));
@@ -586,7 +1006,8 @@ lsgd_status lsgd_groupnorm_backward(const void* x, int x_type, const void* y, co
   a.mean = const_cast<float*>(mean), a.rstd = const_cast<float*>(rstd), a.dgamma = dgamma, a.dbeta = dbeta;
   a.B = B, a.P = (int)P, a.C = C, a.groups = groups, a.D = C / groups, a.act = act, a.N = N;
   a.part = static_cast<float*>(workspace);
-  a.sums = a.part + (size_t)N * gn_ranges(N, a.P, C) * C * 2;
+  a.cl = gn_cluster(N, a.P, C, kBwdHold);
+  a.sums = a.cl ? a.part : a.part + (size_t)N * gn_ranges(N, a.P, C) * C * 2;
   a.m12 = a.sums + (size_t)N * C * 2;
   int v = gn_vec(gn_vec(gn_vec(xb ? 8 : 4, C, x, xz), C, dx, xz), C, dy, yz);
   if (relu) v = gn_vec(v, C, y, yz);

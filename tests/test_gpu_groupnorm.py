@@ -311,7 +311,7 @@ def _call(fn, **kw):
 
 _BOTH = [dict(G=0), dict(B=0), dict(P=0), dict(C=0), dict(groups=0), dict(groups=7), dict(groups=-8), dict(x=None),
          dict(gamma=None), dict(beta=None), dict(mean=None), dict(rstd=None), dict(x_type=2), dict(y_type=-1), dict(act=3),
-         dict(act=-1), dict(par_gs=63), dict(ws=None), dict(wn=15), dict(ws=(11 << 20) + 8), dict(x=(1 << 20) + 1),
+         dict(act=-1), dict(par_gs=63), dict(ws=None, P=50000), dict(wn=15, P=50000), dict(ws=(11 << 20) + 8, P=50000), dict(x=(1 << 20) + 1),
          dict(gamma=(2 << 20) + 2), dict(G=70000), dict(G=5000, B=5000), dict(P=(1 << 24) + 1), dict(C=65544),
          dict(ws=(1 << 20) + 64)]
 
@@ -342,7 +342,9 @@ def test_workspace_refuses_and_grows():
         with pytest.raises(L.LsgdError) as e:
             L.lsgd_groupnorm_workspace(*bad)
         assert e.value.status == L.EINVAL
-    assert 0 < L.lsgd_groupnorm_workspace(2, 2, 64, 64, 8) < L.lsgd_groupnorm_workspace(2, 2, 64, 64, 8, backward=True)
+    for P in (64, 100000):  # few positions stay in registers, many are split over ranges
+        assert (L.lsgd_groupnorm_workspace(2, 2, P, 64, 8) > 0) == (P > 64)
+        assert L.lsgd_groupnorm_workspace(2, 2, P, 64, 8) < L.lsgd_groupnorm_workspace(2, 2, P, 64, 8, backward=True)
 
 
 def test_binding_refuses_host_and_short_tensors():
@@ -375,5 +377,6 @@ def test_binding_refuses_wrong_tensors(P):
             P.lsgd_groupnorm_forward(*{**ok, **bad}.values(), G, B, Pn, C, groups)
         assert err.value.status == P.EINVAL
     with pytest.raises(P.LsgdError) as err:
-        P.lsgd_groupnorm_forward(*ok.values(), G, B, Pn, C, groups, workspace=torch.zeros(16, **e))
+        P.lsgd_groupnorm_backward(ok["x"], None, ok["y"], ok["gamma"], ok["beta"], ok["mean"], ok["rstd"], ok["x"].clone(),
+                                  ok["gamma"].clone(), ok["beta"].clone(), G, B, Pn, C, groups, workspace=torch.zeros(16, **e))
     assert err.value.status == P.EINVAL
