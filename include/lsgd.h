@@ -426,6 +426,41 @@ lsgd_status lsgd_conv3x3_bn_bf16(const uint16_t* x, const uint16_t* W, float* y,
 lsgd_status lsgd_batchnorm_stats_noalloc(const float* y, int64_t P, int C, int G, float* mean,
                                          float* rstd, void* stream);
 
+/* The orthogonalised update direction of G weight matrices (the workers' copies of one layer, or any
+ * others of one shape): momentum, and `steps` Newton-Schulz products that bring the singular
+ * values of the normalised momentum near one (the rule of the Muon optimiser, Jordan et al. 2024;
+ * stand-alone, no counterpart in the paper).  For each matrix of rows x cols values, row-major,
+ *   u = momentum u + g,  x = nesterov ? g + momentum u : u   (momentum = 0: x = g, u untouched, may be NULL),
+ *   X = x / ||x||_F,  `steps` times X = a X + (b A + c A A) X with A = X X^T, (a, b, c) = (3.4445, -4.7750, 2.0315),
+ *   o = X in bf16.
+ * Matrix k's values are at u + k u_gs (fp32), g + k g_gs (g_type LSGD_FP32 or LSGD_BF16) and o + k
+ * o_gs (elements; replica-major buffers: the replica stride).  ||x|| is taken without overflow or
+ * underflow: a matrix of any finite size is normalised, an all-zero one gives o = 0; a NaN or infinite
+ * value makes its own matrix's direction NaN and no other.
+ * The products run on the tensor cores with fp16 operands, fp32 accumulation and X carried as a pair
+ * of fp16 values: o is within 1.5e-3 (relative 2-norm) of exact arithmetic before its rounding to bf16, for rank-
+ * deficient matrices too.  Deterministic.  Sizes up to 32768 a side, steps 1 to 100, G <= 65535.
+ *
+ * `workspace`: device memory of at least lsgd_orthogonal_workspace's bytes, 256-byte aligned, whose
+ * contents do not matter before or after; calls (or captured graphs) that may run at the same time
+ * need one each.  No allocation: the calls may be captured into a CUDA graph.  LSGD_EINVAL for bad
+ * arguments, too small a workspace and tensors that overlap.  Device pointers, asynchronous on `stream`, which
+ * belongs to the current device; lsgd_device_status reports a device-side wait that ran out. */
+lsgd_status lsgd_orthogonal_workspace(int G, int64_t rows, int64_t cols, size_t* bytes);
+lsgd_status lsgd_orthogonal_direction(float* u, int64_t u_gs, const void* g, int g_type, int64_t g_gs,
+                                      uint16_t* o, int64_t o_gs, int G, int64_t rows, int64_t cols,
+                                      float momentum, int nesterov, int steps, void* workspace,
+                                      size_t workspace_bytes, void* stream);
+
+/* Applies directions to G workers' weights: w = (1 - lr weight_decay) w - lr scale o (the decay
+ * decoupled from the direction; scale is the caller's factor for the matrix's shape, e.g.
+ * sqrt(max(1, rows / cols))), n values a worker at w + k w_gs (fp32) and o + k o_gs (bf16); Wb, if not
+ * NULL, receives bf16(w) at Wb + k w_gs, as lsgd_sgd_update writes it.  n and all strides are free
+ * (16-byte accesses where they and the pointers allow).  LSGD_EINVAL on bad arguments and overlaps. */
+lsgd_status lsgd_direction_update(float* w, int64_t w_gs, const uint16_t* o, int64_t o_gs, uint16_t* Wb,
+                                  int G, int64_t n, float lr, float scale, float weight_decay,
+                                  void* stream);
+
 /* Group normalisation with an activation, channels last: the normalisation to put in BatchNorm's
  * place where workers should keep no statistics of their own (per-worker BatchNorm, Sec. A.4,
  * keeps running ones that the model average leaves out).  Stand-alone; no counterpart in the paper.

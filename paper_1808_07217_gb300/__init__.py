@@ -46,6 +46,7 @@ EXPORTS = [
     "lsgd_bounded_wait_selftest", "lsgd_losses_async", "lsgd_synchronize", "lsgd_set_step",
     "lsgd_conv_wgrad_bf16", "lsgd_conv3x3_bf16", "lsgd_conv3x3_bn_bf16", "lsgd_run_batch",
     "lsgd_groupnorm_workspace", "lsgd_groupnorm_forward", "lsgd_groupnorm_backward",
+    "lsgd_orthogonal_workspace", "lsgd_orthogonal_direction", "lsgd_direction_update",
 ]
 PHASES = ["input", "forward", "loss", "backward", "update", "average"]
 
@@ -192,6 +193,12 @@ def lib():
             "lsgd_grouped_gemm_bf16": ([vp, ctypes.c_int, vp, ctypes.c_int, vp, ctypes.c_int,
                                         ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, vp], st),
             "lsgd_profile_read": ([vp, P(Profile)], st),
+            "lsgd_orthogonal_workspace": ([ctypes.c_int, i64, i64, P(ctypes.c_size_t)], st),
+            "lsgd_orthogonal_direction": ([vp, i64, vp, ctypes.c_int, i64, vp, i64, ctypes.c_int, i64, i64,
+                                           ctypes.c_float, ctypes.c_int, ctypes.c_int, vp, ctypes.c_size_t,
+                                           vp], st),
+            "lsgd_direction_update": ([vp, i64, vp, i64, vp, ctypes.c_int, i64, ctypes.c_float, ctypes.c_float,
+                                       ctypes.c_float, vp], st),
             "lsgd_groupnorm_workspace": ([ctypes.c_int, ctypes.c_int, i64, ctypes.c_int, ctypes.c_int,
                                           ctypes.c_int, P(ctypes.c_size_t)], st),
             "lsgd_groupnorm_forward": ([vp, ctypes.c_int, vp, vp, i64, vp, ctypes.c_int, vp, vp, ctypes.c_int,
@@ -601,29 +608,33 @@ def _checked(*tensors):
     return dev
 
 
-def _launch(dev, stream, workspace, nbytes, fn, head, tail=()):
-    """fn(*head, workspace, its bytes, *tail, stream) with device `dev` current, on `stream` or that device's
-    current one.  Without a workspace one of nbytes comes from PyTorch's allocator for this call; on a
-    stream other than the current one its memory is kept until that stream has passed the call."""
+def _launch(dev, stream, workspace, nbytes, fn, args):
+    """fn(*args, workspace, its bytes, stream) with device `dev` current, on `stream` or that device's current
+    one.  Without a workspace one of nbytes comes from PyTorch's allocator for this call; on a stream other
+    than the current one its memory is kept until that stream has passed the call.  workspace False: fn
+    takes none."""
     import torch
 
     if torch.cuda.current_device() != dev:
         with torch.cuda.device(dev):
-            return _launch(dev, stream, workspace, nbytes, fn, head, tail)
+            return _launch(dev, stream, workspace, nbytes, fn, args)
     cur = torch.cuda.current_stream().cuda_stream
     st = cur if stream is None else int(stream)
-    ws, wp, wn = workspace, None, 0
-    if ws is None:
-        if nbytes:
-            ws = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
-            wp, wn = ws.data_ptr(), nbytes
-            if st != cur:
-                ws.record_stream(torch.cuda.ExternalStream(st))
-    elif ws.get_device() != dev or not ws.is_contiguous():
-        raise LsgdError(EINVAL, f"workspace: a contiguous tensor on CUDA device {dev} is wanted")
+    if workspace is False:
+        status = fn(*args, st)
     else:
-        wp, wn = ws.data_ptr(), ws.numel() * ws.element_size()
-    status = fn(*head, wp, wn, *tail, st)
+        ws, wp, wn = workspace, None, 0
+        if ws is None:
+            if nbytes:
+                ws = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+                wp, wn = ws.data_ptr(), nbytes
+                if st != cur:
+                    ws.record_stream(torch.cuda.ExternalStream(st))
+        elif ws.get_device() != dev or not ws.is_contiguous():
+            raise LsgdError(EINVAL, f"workspace: a contiguous tensor on CUDA device {dev} is wanted")
+        else:
+            wp, wn = ws.data_ptr(), ws.numel() * ws.element_size()
+        status = fn(*args, wp, wn, st)
     if status != OK:
         _check(status)
 
@@ -667,3 +678,41 @@ def lsgd_groupnorm_backward(x, y, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta
             (x.data_ptr(), xt, y.data_ptr() if y is not None else None, dy.data_ptr(), yt, gamma.data_ptr(),
              beta.data_ptr(), par_gs, mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), dgamma.data_ptr(),
              dbeta.data_ptr(), G, B, P, C, groups, act))
+
+
+@functools.lru_cache(maxsize=256)
+def lsgd_orthogonal_workspace(G: int, rows: int, cols: int) -> int:
+    """Bytes of workspace that lsgd_orthogonal_direction needs for these sizes."""
+    n = ctypes.c_size_t()
+    _check(lib().lsgd_orthogonal_workspace(int(G), int(rows), int(cols), ctypes.byref(n)))
+    return int(n.value)
+
+
+def lsgd_orthogonal_direction(u, g, o, G: int, rows: int, cols: int, momentum: float = 0.95, nesterov: bool = True,
+                              steps: int = 5, u_gs: int = 0, g_gs: int = 0, o_gs: int = 0, workspace=None,
+                              stream=None):
+    """u = momentum u + g and o = the orthogonalised (nesterov ? g + momentum u : u) of G matrices of rows x cols:
+    u float32 (None without momentum), g float32 or bfloat16, o bfloat16, at strides of u_gs, g_gs and o_gs
+    elements (0: rows cols)."""
+    nbytes = lsgd_orthogonal_workspace(G, rows, cols)
+    n = rows * cols
+    u_gs, g_gs, o_gs = u_gs or n, g_gs or n, o_gs or n
+    if u is None and momentum:
+        raise LsgdError(EINVAL, "u: wanted with momentum")
+    dev = _checked(("g", g, (G - 1) * g_gs + n, None), ("u", u, (G - 1) * u_gs + n, FP32),
+                   ("o", o, (G - 1) * o_gs + n, BF16))
+    _launch(dev, stream, workspace, nbytes, lib().lsgd_orthogonal_direction,
+            (u.data_ptr() if u is not None else None, u_gs, g.data_ptr(), _type_of(g), g_gs, o.data_ptr(), o_gs, G,
+             rows, cols, momentum, nesterov, steps))
+
+
+def lsgd_direction_update(w, o, Wb, G: int, n: int, lr: float, scale: float = 1.0, weight_decay: float = 0.0,
+                          w_gs: int = 0, o_gs: int = 0, stream=None):
+    """w = (1 - lr weight_decay) w - lr scale o for G workers' n values (w float32, o bfloat16), and Wb (bfloat16 or
+    None) = bf16(w); w and Wb at stride w_gs, o at o_gs elements (0: n)."""
+    w_gs, o_gs = w_gs or n, o_gs or n
+    span = (G - 1) * w_gs + n
+    dev = _checked(("w", w, span, FP32), ("o", o, (G - 1) * o_gs + n, BF16), ("Wb", Wb, span, BF16))
+    _launch(dev, stream, False, 0, lib().lsgd_direction_update,
+            (w.data_ptr(), w_gs, o.data_ptr(), o_gs, Wb.data_ptr() if Wb is not None else None, G, n, lr, scale,
+             weight_decay))

@@ -32,6 +32,7 @@
 
 #include "common.cuh"
 #include "lsgd_internal.h"
+#include "tc_ptx.cuh"
 
 namespace lsgd {
 
@@ -42,35 +43,6 @@ namespace {
 constexpr int BM = 128;
 constexpr int BK = 64;
 constexpr long long kWaitCycles = 4000000000LL;  // ~2 s at 2 GHz
-
-__device__ __forceinline__ uint32_t smem_u32(const void* p) {
-  return (uint32_t)__cvta_generic_to_shared(p);
-}
-
-__device__ __forceinline__ void mbar_init(uint64_t* bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory");
-}
-
-__device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)),
-               "r"(bytes)
-               : "memory");
-}
-
-__device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
-      " selp.u32 %0, 1, 0, p;\n}\n"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-
-__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
 
 // Bounded wait on an mbarrier phase; false (and the global error flag set) on expiry.
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity,
@@ -86,37 +58,9 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity,
   return true;
 }
 
-// The TMA and MMA instructions take their operands from uniform registers.  Their issue loops are run
-// by a whole warp (the warp index broadcast, so that the compiler knows the control flow to be
-// uniform and keeps descriptors, addresses and counters in uniform registers) and one elected lane
-// issues.  A loop under "lane == 0" instead moves every operand across for every instruction: at
-// least 46 cycles per tcgen05.mma, and 90 to 150 with the descriptor arithmetic of these kernels,
-// where the tensor core takes 23 (M = 64, N = 16), 39 (M = 128, N = 16), 48 (N = 64) or 128 (N = 256).
-__device__ __forceinline__ int uniform_warp() { return __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0); }
-
-__device__ __forceinline__ bool elect_one() {
-  uint32_t ok;
-  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(ok));
-  return ok != 0;
-}
-
 // mbar_wait by every lane; true if all saw the phase (one that ran out cannot split the warp).
 __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity) {
   return __all_sync(0xffffffffu, mbar_wait(bar, parity) ? 1 : 0) != 0;
-}
-
-// A tensor map into the descriptor cache (maps are kernel parameters: no dependency on other kernels).
-__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
-  asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
-}
-
-__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, uint64_t* bar, int x,
-                                            int y, int z) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
-      : "memory");
 }
 
 __device__ __forceinline__ void tma_load_5d(void* dst, const CUtensorMap* map, uint64_t* bar, int c0,
@@ -152,16 +96,6 @@ __device__ __forceinline__ uint64_t smem_desc_swz(uint32_t addr, uint32_t lbo, u
   d |= (uint64_t)((sbo >> 4) & 0x3FFFu) << 32;
   d |= 1ull << 46;  // descriptor version (tcgen05)
   d |= layout << 61;
-  return d;
-}
-
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo, uint32_t sbo) {
-  uint64_t d = 0;
-  d |= (uint64_t)((addr >> 4) & 0x3FFFu);
-  d |= (uint64_t)((lbo >> 4) & 0x3FFFu) << 16;
-  d |= (uint64_t)((sbo >> 4) & 0x3FFFu) << 32;
-  d |= 1ull << 46;  // descriptor version (tcgen05)
-  d |= 2ull << 61;  // SWIZZLE_128B
   return d;
 }
 
