@@ -93,29 +93,73 @@ struct DirArgs {
   __half *h, *l;     // [G][rows][ld]
   float* part;       // [G][chunks][3]
   int chunks, per;   // ranges of a matrix (elements per range)
+  uint32_t* done;    // [G], set to zero for the products
 };
 
 constexpr int kMomThreads = 256;
 
-__device__ __forceinline__ float grad_at(const DirArgs& a, int64_t i) {
-  return a.g_bf16 ? bf2f(static_cast<const uint16_t*>(a.g)[i]) : static_cast<const float*>(a.g)[i];
+// V gradient or momentum values from element i of a matrix.
+template <int V>
+__device__ __forceinline__ void load_f32(const float* p, float (&v)[V]) {
+  if constexpr (V == 1) {
+    v[0] = *p;
+  } else {
+#pragma unroll
+    for (int j = 0; j < V / 4; ++j) {
+      const float4 t = reinterpret_cast<const float4*>(p)[j];
+      v[4 * j] = t.x, v[4 * j + 1] = t.y, v[4 * j + 2] = t.z, v[4 * j + 3] = t.w;
+    }
+  }
+}
+template <int V>
+__device__ __forceinline__ void load_grad(const DirArgs& a, int64_t i, float (&v)[V]) {
+  if (!a.g_bf16) {
+    load_f32<V>(static_cast<const float*>(a.g) + i, v);
+    return;
+  }
+  const uint16_t* p = static_cast<const uint16_t*>(a.g) + i;
+  if constexpr (V == 1) {
+    v[0] = bf2f(*p);
+  } else {
+#pragma unroll
+    for (int j = 0; j < V / 4; ++j) {
+      const uint2 t = reinterpret_cast<const uint2*>(p)[j];
+      v[4 * j] = __uint_as_float(t.x << 16), v[4 * j + 1] = __uint_as_float(t.x & 0xffff0000u);
+      v[4 * j + 2] = __uint_as_float(t.y << 16), v[4 * j + 3] = __uint_as_float(t.y & 0xffff0000u);
+    }
+  }
 }
 
+template <int V>
 __global__ void __launch_bounds__(kMomThreads) direction_momentum_kernel(const DirArgs a) {
   pdl_begin();
-  const int64_t n = (int64_t)a.rows * a.cols, i0 = (int64_t)blockIdx.x * a.per, i1 = min(n, i0 + a.per);
+  const int n = a.rows * a.cols, i0 = blockIdx.x * a.per, i1 = min(n, i0 + a.per);
   const int64_t k = blockIdx.y;
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.done[k] = 0;
   NormSums s{0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int64_t i = i0 + threadIdx.x; i < i1; i += kMomThreads) {
-    const float g = grad_at(a, k * a.g_gs + i);
-    float x = g;
+#pragma unroll 2
+  for (int i = i0 + threadIdx.x * V; i < i1; i += kMomThreads * V) {
+    float x[V];
+    load_grad<V>(a, k * a.g_gs + i, x);
     if (a.mom != 0.f) {
-      const float u = fmaf(a.mom, a.u[k * a.u_gs + i], g);
-      a.u[k * a.u_gs + i] = u;
-      x = a.nesterov ? fmaf(a.mom, u, g) : u;
+      float u[V];
+      float* up = a.u + k * a.u_gs + i;
+      load_f32<V>(up, u);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        u[j] = fmaf(a.mom, u[j], x[j]);
+        x[j] = a.nesterov ? fmaf(a.mom, u[j], x[j]) : u[j];
+      }
+      if constexpr (V == 1) {
+        *up = u[0];
+      } else {
+#pragma unroll
+        for (int j = 0; j < V / 4; ++j)
+          reinterpret_cast<float4*>(up)[j] = make_float4(u[4 * j], u[4 * j + 1], u[4 * j + 2], u[4 * j + 3]);
+      }
     }
-    norm_add(s, x);
+#pragma unroll
+    for (int j = 0; j < V; ++j) norm_add(s, x[j]);
   }
   __shared__ float red[3][kMomThreads / 32];
   float v[3] = {s.mid, s.big, s.small};
@@ -138,6 +182,7 @@ __device__ __forceinline__ void split_pair(float x, __half& h, __half& l) {
   l = __float2half_rn(x - __half2float(h));
 }
 
+template <int V>
 __global__ void __launch_bounds__(kMomThreads) direction_normalise_kernel(const DirArgs a) {
   pdl_begin();
   const int64_t k = blockIdx.y;
@@ -152,63 +197,82 @@ __global__ void __launch_bounds__(kMomThreads) direction_normalise_kernel(const 
   }
   __syncthreads();
   const float2 f = factors;
-  const int64_t n = (int64_t)a.rows * a.cols, i0 = (int64_t)blockIdx.x * a.per, i1 = min(n, i0 + a.per);
-#pragma unroll 4
-  for (int64_t i = i0 + threadIdx.x; i < i1; i += kMomThreads) {
-    float x;
+  const int n = a.rows * a.cols, i0 = blockIdx.x * a.per, i1 = min(n, i0 + a.per);
+#pragma unroll 2
+  for (int i = i0 + threadIdx.x * V; i < i1; i += kMomThreads * V) {
+    float x[V];
     if (a.mom == 0.f) {
-      x = grad_at(a, k * a.g_gs + i);
+      load_grad<V>(a, k * a.g_gs + i, x);
     } else {
-      x = a.u[k * a.u_gs + i];
-      if (a.nesterov) x = fmaf(a.mom, x, grad_at(a, k * a.g_gs + i));
+      load_f32<V>(a.u + k * a.u_gs + i, x);
+      if (a.nesterov) {
+        float g[V];
+        load_grad<V>(a, k * a.g_gs + i, g);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = fmaf(a.mom, x[j], g[j]);
+      }
     }
-    __half h, l;
-    split_pair(x * f.x * f.y, h, l);
-    const int64_t r = i / a.cols, at = (k * a.rows + r) * a.ld + (i - r * a.cols);
-    a.h[at] = h;
-    a.l[at] = l;
+    __align__(16) __half h[V], l[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) split_pair(x[j] * f.x * f.y, h[j], l[j]);
+    const int r = (uint32_t)i / (uint32_t)a.cols;
+    const int64_t at = (k * a.rows + r) * a.ld + (i - r * a.cols);
+    if constexpr (V == 1) {
+      a.h[at] = h[0];
+      a.l[at] = l[0];
+    } else if constexpr (V == 4) {
+      *reinterpret_cast<uint2*>(a.h + at) = *reinterpret_cast<const uint2*>(h);
+      *reinterpret_cast<uint2*>(a.l + at) = *reinterpret_cast<const uint2*>(l);
+    } else {
+      *reinterpret_cast<uint4*>(a.h + at) = *reinterpret_cast<const uint4*>(h);
+      *reinterpret_cast<uint4*>(a.l + at) = *reinterpret_cast<const uint4*>(l);
+    }
   }
 }
 
 // ------------------------------------------------------------------------------------------------
-// The products: pairs of CTAs on 256 x 256 tiles (tcgen05 cta_group::2)
+// The products: pairs of CTAs on 256 x 256 tiles (tcgen05 cta_group::2), all steps in one launch
 //
 // A cluster of two CTAs computes a 256 x 256 fp32 tile; CTA r holds rows 128 r .. of it in its tensor memory, loads rows
 // 128 r .. of the left operand and 128 r .. of the right operand's 256, and the leader (r = 0) issues the products, which
 // read both CTAs' shared memory.  Per k-block of 64 a CTA moves 32 KB for 128 x 256 x 64 products, two thirds of what
 // a 128 x 256 tile by one CTA would.
-//   warp 0    TMA producer of both operands into a ring of kStages stages (both CTAs' bytes counted on the leader's
-//             barrier)
-//   warp 1    MMA issuer (leader only)
-//   warp 2    tensor memory allocation (two accumulators of 256 columns)
-//   warps 4-7 epilogue, a warp per 32 rows
+//   warp 0      TMA producer of both operands into a ring of kStages stages (both CTAs' bytes counted on the leader's
+//               barrier)
+//   warp 1      MMA issuer (leader only)
+//   warp 2      tensor memory allocation (two accumulators of 256 columns)
+//   warp 3      TMA loads of what the epilogue reads (h and l, or A), 64 columns at a time into a ring of kEpi buffers,
+//               ahead of the accumulator
+//   warps 4-11  epilogue: a warp per 32 rows and 32 columns of a buffer, in place; TMA stores from it
+//
+// The tiles of all steps form one list: per step the tiles of A = X X^T of every matrix, then those of P, then those of
+// X.  Pair p takes tiles p, p + pairs, ...; `done[g]` counts the CTAs' finished tiles of matrix g, whose phases follow one
+// another, and a tile starts when its matrix's earlier phases are complete.  The launch is cooperative (all pairs are
+// resident) and every tile's predecessors stand before it in the list, so that every wait ends; matrices fill each
+// other's phase ends, and nothing is launched between phases.
 
-constexpr int kTile = 256, kHalf = 128, kBK = 64, kStages = 6, kThreads = 256;
-constexpr uint32_t kOpBytes = kHalf * kBK * 2;  // one operand's share of a stage in a CTA
+constexpr int kTile = 256, kHalf = 128, kBK = 64, kStages = 4, kEpi = 3, kThreads = 384, kChunk = 64;
+constexpr uint32_t kOpBytes = kHalf * kBK * 2;  // one operand's share of a stage in a CTA; half an epilogue buffer
 
 enum Role { GRAM = 0, POLY = 1, NEXT = 2, LAST = 3 };
 
 struct MmArgs {
-  CUtensorMap a, b;   // K-major: box {64 k, 128 rows}; MN-major: box {64 rows, 64 k}
-  int a_mn, b_mn;
-  int M, N, K, G, role;
-  int tall;           // NEXT and LAST: the diagonal goes by column
-  int late;           // NEXT and LAST: t is the largest of the diagonal
-  const __half* A;    // [G][n][lda], POLY's input
-  __half* out;        // GRAM: A, POLY: P (both [G][n][lda], mirrored); NEXT: h
-  __half* out_l;      // NEXT
-  const __half *h, *l;
+  // K-major operands and epilogue tiles: box {64, 128}; MN-major operands and mirrored tiles: box {64, 64}
+  CUtensorMap xk[2], xm[2], lk[2], ak, am, pk, pm, om;
+  int G, n, rows, cols, steps, tall, o_tma;
   float *diag_a, *diag;  // [G][n]: the diagonals of A and P
+  uint32_t* done;        // [G]
   uint16_t* o;
-  int64_t lda, ldx, x_gs, o_gs;  // x_gs: elements per matrix of h and l
-  int n, ldo, o_vec;  // o_vec: rows of o are 32-byte aligned
+  int64_t o_gs;
 };
 
 struct MmSmem {
   uint8_t a[kStages][kOpBytes];  // 1024-aligned
   uint8_t b[kStages][kOpBytes];
+  uint8_t e[kEpi][2][kOpBytes];  // h or A and the tile stored; l or the mirrored tile
   uint64_t full[kStages], empty[kStages];
   uint64_t acc_full[2], acc_empty[2];
+  uint64_t epi_full[kEpi], epi_empty[kEpi];
   uint32_t tmem_base;
 };
 
@@ -237,6 +301,32 @@ __device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity) {
 __device__ __forceinline__ bool wait_bar_warp(uint64_t* bar, uint32_t parity) {
   return __all_sync(0xffffffffu, wait_bar(bar, parity) ? 1 : 0) != 0;
 }
+// Until *count, counted up by other CTAs, has reached `need` (by the whole warp).  What they wrote before is then visible
+// to this warp's loads and, behind the proxy fence, to its TMA copies.
+__device__ __forceinline__ bool wait_count_warp(const uint32_t* count, uint32_t need) {
+  int ok = 1;
+  if ((threadIdx.x & 31) == 0) {
+    auto reached = [&]() -> bool {
+      uint32_t v;
+      asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(count) : "memory");
+      return v >= need;
+    };
+    if (!reached()) {
+      const long long t0 = clock64();
+      while (!reached()) {
+        if (clock64() - t0 > kWaitCycles) {
+          atomicExch(&g_direction_timeout, 1);
+          ok = 0;
+          break;
+        }
+        __nanosleep(64);
+      }
+    }
+  }
+  ok = __shfl_sync(0xffffffffu, ok, 0);
+  asm volatile("fence.proxy.async;" ::: "memory");
+  return ok != 0;
+}
 
 __device__ __forceinline__ uint32_t cta_rank() {
   uint32_t r;
@@ -259,6 +349,12 @@ __device__ __forceinline__ void tma_load_pair(void* dst, const CUtensorMap* map,
       " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "r"(z)
       : "memory");
+}
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, const void* src, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(
+                   reinterpret_cast<uint64_t>(map)),
+               "r"(smem_u32(src)), "r"(x), "r"(y), "r"(z)
+               : "memory");
 }
 __device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -295,120 +391,79 @@ __device__ __forceinline__ void tmem_ld32(uint32_t at, float (&v)[32]) {
   for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
-// fp16 rows of the workspace: 32 values from or to a 32-byte aligned place (row strides are multiples of 16 values,
-// tiles start at multiples of 32); what lies past the row's last value is padding or, past the stride, not touched.
-__device__ __forceinline__ void load_half32(const __half* p, int have, float (&v)[32]) {
+// Eight fp16 (or bf16) values in 16 bytes.
+__device__ __forceinline__ void unpack8(const uint4 w, float (&f)[8]) {
+  const uint32_t r[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    if (16 * q < have) {
-      uint32_t w[8];
-      asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
-                   : "l"(p + 16 * q)
-                   : "memory");
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-        v[16 * q + 2 * i] = f.x;
-        v[16 * q + 2 * i + 1] = f.y;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) v[16 * q + i] = 0.f;
-    }
+  for (int i = 0; i < 4; ++i) {
+    const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&r[i]));
+    f[2 * i] = t.x, f[2 * i + 1] = t.y;
   }
 }
-__device__ __forceinline__ void store_words16(void* p, const uint32_t* w) {
-  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
-               "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
-}
-__device__ __forceinline__ void store_half32(__half* p, int have, const float (&v)[32]) {
+__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
+  uint32_t r[4];
 #pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    if (16 * q >= have) break;
-    uint32_t w[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const __half2 t = __floats2half2_rn(v[16 * q + 2 * i], v[16 * q + 2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t*>(&t);
-    }
-    store_words16(p + 16 * q, w);
+  for (int i = 0; i < 4; ++i) {
+    const __half2 t = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+    r[i] = *reinterpret_cast<const uint32_t*>(&t);
   }
+  return make_uint4(r[0], r[1], r[2], r[3]);
+}
+__device__ __forceinline__ uint4 pack8_bf16(const float (&f)[8]) {
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 t = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+    r[i] = *reinterpret_cast<const uint32_t*>(&t);
+  }
+  return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
-// The epilogue of 32 columns of one row: acc holds columns c0 .. c0 + 31 of row `row` of matrix g.  Rows at or past M
-// have been skipped by the caller; `mirror`: the tile's transpose is written too.
-__device__ __forceinline__ void mm_epilogue(const MmArgs& a, int g, int row, int c0, float (&v)[32], bool mirror, float t) {
-  const int have = a.N - c0;  // > 0
-  if (a.role <= POLY) {
-    const int64_t base = (int64_t)g * a.n * a.lda;
-    float* da = a.diag_a + (int64_t)g * a.n;
-    if (a.role == GRAM) {
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        if (c0 + i == row) da[row] = v[i] * kUnscale2, v[i] = 0.f;
-        v[i] *= kUnscale;
-      }
-    } else {  // with D = diag dA and O the rest of A: A A = O O + D O + O D + D D
-      float in[32];
-      load_half32(a.A + base + (int64_t)row * a.lda + c0, have, in);
-      const float dr = da[row];
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        const float dc = i < have ? da[c0 + i] : 0.f;
-        if (c0 + i == row) {
-          a.diag[(int64_t)g * a.n + row] = fmaf(kB, dr, kC * fmaf(dr, dr, v[i] * kUnscale2));
-          v[i] = 0.f;
-        } else {
-          v[i] = fmaf(kB, in[i], kC * fmaf(dr + dc, in[i], kUnscale * v[i]));
-        }
-      }
-    }
-    store_half32(a.out + base + (int64_t)row * a.lda + c0, have, v);
-    if (mirror) {
-#pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (i < have) a.out[base + (int64_t)(c0 + i) * a.lda + row] = __float2half_rn(v[i]);
-    }
-    return;
+// One tile of the list.
+struct Item {
+  int role, step, g, m0, n0, M, N, K;
+  uint32_t need;  // of done[g], before it starts
+};
+struct Plan {
+  int ts, tm, tn, per_sym, per_x;  // tiles a side of A; of X; tiles of a symmetric product and of X
+  int64_t per_step, total;
+  __device__ __forceinline__ explicit Plan(const MmArgs& a) {
+    ts = (a.n + kTile - 1) / kTile;
+    tm = (a.rows + kTile - 1) / kTile, tn = (a.cols + kTile - 1) / kTile;
+    per_sym = ts * (ts + 1) / 2, per_x = tm * tn;
+    per_step = (int64_t)a.G * (2 * per_sym + per_x);
+    total = per_step * a.steps;
   }
-  const int64_t at = (int64_t)g * a.x_gs + (int64_t)row * a.ldx + c0;
-  float x[32], lo[32];
-  load_half32(a.h + at, have, x);
-  load_half32(a.l + at, have, lo);
-  const float* dg = a.diag + (int64_t)g * a.n;
-  const float dr = a.tall ? 0.f : dg[row];
-#pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    const float d = kA + (a.tall ? (i < have ? dg[c0 + i] : 0.f) : dr);
-    x[i] = fmaf(d, x[i], fmaf(kA + t, lo[i], kUnscale * v[i]));
-  }
-  if (a.role == NEXT) {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) lo[i] = x[i] - __half2float(__float2half_rn(x[i]));
-    store_half32(a.out + at, have, x);
-    store_half32(a.out_l + at, have, lo);
-    return;
-  }
-  uint16_t* o = a.o + (int64_t)g * a.o_gs + (int64_t)row * a.ldo + c0;
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    if (a.o_vec && 16 * q + 16 <= have) {
-      uint32_t w[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const __nv_bfloat162 t = __floats2bfloat162_rn(x[16 * q + 2 * i] * kUnscale, x[16 * q + 2 * i + 1] * kUnscale);
-        w[i] = *reinterpret_cast<const uint32_t*>(&t);
-      }
-      store_words16(o + 16 * q, w);
+  __device__ __forceinline__ Item at(const MmArgs& a, int64_t t) const {
+    Item it;
+    it.step = (int)(t / per_step);
+    int64_t r = t - it.step * per_step;
+    const int64_t syms = (int64_t)a.G * per_sym;
+    it.need = 2u * (uint32_t)it.step * (uint32_t)(2 * per_sym + per_x);
+    if (r < 2 * syms) {
+      it.role = r < syms ? GRAM : POLY;
+      if (it.role == POLY) r -= syms, it.need += 2u * per_sym;
+      it.g = (int)(r / per_sym);
+      const int q = (int)(r - (int64_t)it.g * per_sym);
+      // tiles on and below the diagonal, row by row
+      int i = (int)((sqrtf(8.f * (float)q + 1.f) - 1.f) * 0.5f);
+      while (i * (i + 1) / 2 > q) --i;
+      while ((i + 1) * (i + 2) / 2 <= q) ++i;
+      it.m0 = i * kTile, it.n0 = (q - i * (i + 1) / 2) * kTile;
+      it.M = it.N = a.n;
+      it.K = it.role == GRAM ? max(a.rows, a.cols) : a.n;
     } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (16 * q + i < have) o[16 * q + i] = f2bf(x[16 * q + i] * kUnscale);
+      r -= 2 * syms;
+      it.role = it.step + 1 < a.steps ? NEXT : LAST;
+      it.need += 4u * per_sym;
+      it.g = (int)(r / per_x);
+      const int q = (int)(r - (int64_t)it.g * per_x);
+      it.m0 = q % tm * kTile, it.n0 = q / tm * kTile;
+      it.M = a.rows, it.N = a.cols, it.K = a.n;
     }
+    return it;
   }
-}
+};
 
 __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     direction_product_kernel(const __grid_constant__ MmArgs args) {
@@ -417,25 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
   const int warp = uniform_warp(), lane = threadIdx.x & 31;
   const uint32_t rank = cta_rank();
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-  const bool sym = args.role <= POLY;
-  const int tm = (args.M + kTile - 1) / kTile, tn = (args.N + kTile - 1) / kTile;
-  const int per_matrix = sym ? tm * (tm + 1) / 2 : tm * tn;
-  const int tiles = per_matrix * args.G;
-  const int nk = (args.K + kBK - 1) / kBK;
-  // tile t: matrix by matrix; of a symmetric product the tiles on and below the diagonal, row by row
-  auto coords = [&](int t, int& g, int& m0, int& n0) {
-    g = t / per_matrix;
-    int r = t - g * per_matrix, i, j;
-    if (sym) {
-      i = (int)((sqrtf(8.f * (float)r + 1.f) - 1.f) * 0.5f);
-      while (i * (i + 1) / 2 > r) --i;
-      while ((i + 1) * (i + 2) / 2 <= r) ++i;
-      j = r - i * (i + 1) / 2;
-    } else {
-      i = r % tm, j = r / tm;
-    }
-    m0 = i * kTile, n0 = j * kTile;
-  };
+  const Plan plan(args);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -444,7 +481,11 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sm.acc_full[i], 1);
-      mbar_init(&sm.acc_empty[i], 8);  // the epilogue warps of both CTAs
+      mbar_init(&sm.acc_empty[i], 16);  // the epilogue warps of both CTAs
+    }
+    for (int i = 0; i < kEpi; ++i) {
+      mbar_init(&sm.epi_full[i], 1);
+      mbar_init(&sm.epi_empty[i], 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -460,17 +501,21 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
   pair_sync();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = sm.tmem_base;
-  pdl_begin();
 
   if (warp == 0) {
     const bool el = elect_one();
-    int it = 0, s = 0;
+    int s = 0;
+    int64_t it = 0;
     uint32_t ph = 1;
     bool ok = true;
-    for (int t = pair; t < tiles && ok; t += pairs) {
-      int g, m0, n0;
-      coords(t, g, m0, n0);
-      m0 += rank * kHalf, n0 += rank * kHalf;
+    for (int64_t t = pair; t < plan.total && ok; t += pairs) {
+      const Item q = plan.at(args, t);
+      if (!(ok = wait_count_warp(args.done + q.g, q.need))) break;
+      const int in = q.step & 1, m0 = q.m0 + rank * kHalf, n0 = q.n0 + rank * kHalf, nk = (q.K + kBK - 1) / kBK;
+      const CUtensorMap* ma = q.role == GRAM ? (args.tall ? &args.xm[in] : &args.xk[in])
+                              : q.role == POLY ? &args.ak : (args.tall ? &args.xk[in] : &args.pk);
+      const CUtensorMap* mb = q.role <= POLY ? ma : (args.tall ? &args.pk : &args.xm[in]);
+      const bool a_mn = q.role == GRAM && args.tall, b_mn = q.role <= POLY ? a_mn : !args.tall;
       for (int kb = 0; kb < nk; ++kb, ++it) {
         if (!wait_bar_warp(&sm.empty[s], ph)) {
           ok = false;
@@ -480,17 +525,17 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
           const uint32_t bar = in_cta(&sm.full[s], 0);
           if (rank == 0) mbar_expect_tx(&sm.full[s], 4 * kOpBytes);  // two operands, two CTAs
           const int k0 = kb * kBK;
-          if (!args.a_mn) {
-            tma_load_pair(sm.a[s], &args.a, bar, k0, m0, g);
+          if (!a_mn) {
+            tma_load_pair(sm.a[s], ma, bar, k0, m0, q.g);
           } else {
-            tma_load_pair(sm.a[s], &args.a, bar, m0, k0, g);
-            tma_load_pair(sm.a[s] + kOpBytes / 2, &args.a, bar, m0 + 64, k0, g);
+            tma_load_pair(sm.a[s], ma, bar, m0, k0, q.g);
+            tma_load_pair(sm.a[s] + kOpBytes / 2, ma, bar, m0 + 64, k0, q.g);
           }
-          if (!args.b_mn) {
-            tma_load_pair(sm.b[s], &args.b, bar, k0, n0, g);
+          if (!b_mn) {
+            tma_load_pair(sm.b[s], mb, bar, k0, n0, q.g);
           } else {
-            tma_load_pair(sm.b[s], &args.b, bar, n0, k0, g);
-            tma_load_pair(sm.b[s] + kOpBytes / 2, &args.b, bar, n0 + 64, k0, g);
+            tma_load_pair(sm.b[s], mb, bar, n0, k0, q.g);
+            tma_load_pair(sm.b[s] + kOpBytes / 2, mb, bar, n0 + 64, k0, q.g);
           }
         }
         if (++s == kStages) s = 0, ph ^= 1;
@@ -498,20 +543,22 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     }
     // after a wait that ran out, the copies in flight (the leader's barriers count both CTAs') are waited for
     if (!ok && rank == 0)
-      for (int j = it > kStages ? it - kStages : 0; j < it; ++j) wait_bar(&sm.full[j % kStages], (j / kStages) & 1);
+      for (int64_t j = it > kStages ? it - kStages : 0; j < it; ++j) wait_bar(&sm.full[j % kStages], (j / kStages) & 1);
   } else if (warp == 1 && rank == 0) {
     const bool el = elect_one();
-    // fp32 accumulators, fp16 operands, N = 256, M = 256
-    const uint32_t idesc = (1u << 4) | ((uint32_t)args.a_mn << 15) | ((uint32_t)args.b_mn << 16) |
-                           ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
-    const uint64_t a0 = args.a_mn ? smem_desc(smem_u32(sm.a[0]), kOpBytes / 2, 1024) : smem_desc(smem_u32(sm.a[0]), 16, 1024);
-    const uint64_t b0 = args.b_mn ? smem_desc(smem_u32(sm.b[0]), kOpBytes / 2, 1024) : smem_desc(smem_u32(sm.b[0]), 16, 1024);
-    const uint32_t a_step = args.a_mn ? 2048 >> 4 : 32 >> 4, b_step = args.b_mn ? 2048 >> 4 : 32 >> 4;
     int i = 0, s = 0;
     uint32_t ph = 0;
     bool ok = true;
-    for (int t = pair; t < tiles && ok; t += pairs, ++i) {
-      const int ab = i & 1;
+    for (int64_t t = pair; t < plan.total && ok; t += pairs, ++i) {
+      const Item q = plan.at(args, t);
+      const int nk = (q.K + kBK - 1) / kBK, ab = i & 1;
+      const bool a_mn = q.role == GRAM && args.tall, b_mn = q.role <= POLY ? a_mn : !args.tall;
+      // fp32 accumulators, fp16 operands, N = 256, M = 256
+      const uint32_t idesc = (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
+                             ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+      const uint64_t a0 = smem_desc(smem_u32(sm.a[0]), a_mn ? kOpBytes / 2 : 16, 1024);
+      const uint64_t b0 = smem_desc(smem_u32(sm.b[0]), b_mn ? kOpBytes / 2 : 16, 1024);
+      const uint32_t a_step = a_mn ? 2048 >> 4 : 32 >> 4, b_step = b_mn ? 2048 >> 4 : 32 >> 4;
       if (!wait_bar_warp(&sm.acc_empty[ab], ((i >> 1) & 1) ^ 1)) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t acc = tmem + (uint32_t)(ab * kTile);
@@ -530,36 +577,206 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
       }
       if (ok && el) commit_pair(&sm.acc_full[ab]);
     }
+  } else if (warp == 3) {
+    const bool el = elect_one();
+    int e = 0;
+    int64_t it = 0;
+    uint32_t ph = 1;
+    bool ok = true;
+    for (int64_t t = pair; t < plan.total && ok; t += pairs) {
+      const Item q = plan.at(args, t);
+      if (!(ok = wait_count_warp(args.done + q.g, q.need))) break;
+      const int in = q.step & 1, m0 = q.m0 + rank * kHalf;
+      for (int c = 0; c < kTile && q.n0 + c < q.N; c += kChunk, ++it) {
+        if (!wait_bar_warp(&sm.epi_empty[e], ph)) {
+          ok = false;
+          break;
+        }
+        if (el) {
+          if (q.role == GRAM) {
+            mbar_arrive(&sm.epi_full[e]);
+          } else if (q.role == POLY) {
+            mbar_expect_tx(&sm.epi_full[e], kOpBytes);
+            tma_load_3d(sm.e[e][0], &args.ak, &sm.epi_full[e], q.n0 + c, m0, q.g);
+          } else {
+            mbar_expect_tx(&sm.epi_full[e], 2 * kOpBytes);
+            tma_load_3d(sm.e[e][0], &args.xk[in], &sm.epi_full[e], q.n0 + c, m0, q.g);
+            tma_load_3d(sm.e[e][1], &args.lk[in], &sm.epi_full[e], q.n0 + c, m0, q.g);
+          }
+        }
+        if (++e == kEpi) e = 0, ph ^= 1;
+      }
+    }
+    if (!ok)
+      for (int64_t j = it > kEpi ? it - kEpi : 0; j < it; ++j) wait_bar(&sm.epi_full[j % kEpi], (j / kEpi) & 1);
   } else if (warp >= 4) {
-    const int quarter = warp & 3;
+    const int quarter = warp & 3, half = (warp - 4) >> 2;
+    const int r = quarter * 32 + lane;  // the row of this CTA's half tile
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    int i = 0, of = -1;
+    const bool storer = threadIdx.x == 128;
+    int i = 0, e = 0, of = -1;
+    uint32_t ph = 0;
     float top = 0.f;
-    for (int t = pair; t < tiles; t += pairs, ++i) {
-      int g, m0, n0;
-      coords(t, g, m0, n0);
-      const int ab = i & 1;
-      if (args.late && g != of) {
-        const float* d = args.diag + (int64_t)g * args.n;
+    bool ok = true;
+    for (int64_t t = pair; t < plan.total && ok; t += pairs, ++i) {
+      const Item q = plan.at(args, t);
+      const int ab = i & 1, m0 = q.m0 + rank * kHalf, row = m0 + r, in = q.step & 1;
+      const bool mirror = q.role <= POLY && q.m0 != q.n0, sym = q.role <= POLY;
+      ok = wait_count_warp(args.done + q.g, q.need);
+      float* da = args.diag_a + (int64_t)q.g * args.n;
+      float* dg = args.diag + (int64_t)q.g * args.n;
+      const bool late = !sym && q.step + 2 >= args.steps;
+      if (ok && late && of != q.step * args.G + q.g) {  // t: the largest of P's diagonal
         top = -INFINITY;
-        for (int k = lane; k < args.n; k += 32) top = fmaxf(top, d[k]);
+        for (int k = lane; k < args.n; k += 32) top = fmaxf(top, __ldcg(dg + k));
 #pragma unroll
         for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-        of = g;
+        of = q.step * args.G + q.g;
       }
-      if (!wait_bar_warp(&sm.acc_full[ab], (i >> 1) & 1)) break;
+      const bool by_row = q.role == POLY || (!sym && !args.tall);
+      const float dr = by_row && row < q.M ? __ldcg((q.role == POLY ? da : dg) + row) : 0.f;
+      const bool by_col = q.role == POLY || (!sym && args.tall);
+      float dcol[kTile / kChunk];  // the diagonal's values at this lane's column of each chunk
+#pragma unroll
+      for (int k = 0; k < kTile / kChunk; ++k) {
+        const int col = q.n0 + k * kChunk + 32 * half + lane;
+        dcol[k] = by_col && col < q.N ? __ldcg((q.role == POLY ? da : dg) + col) : 0.f;
+      }
+      ok = ok && wait_bar_warp(&sm.acc_full[ab], (i >> 1) & 1);
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const int row = m0 + (int)rank * kHalf + quarter * 32 + lane;
-      const bool mirror = sym && m0 != n0;
-      for (int c = 0; c < kTile && n0 + c < args.N; c += 32) {
+#pragma unroll
+      for (int c = 0; c < kTile; c += kChunk) {
+        if (q.n0 + c >= q.N) break;
+        const int c0 = q.n0 + c + 32 * half;  // this thread's columns
+        ok = ok && wait_bar_warp(&sm.epi_full[e], ph);
         float v[32];
-        tmem_ld32(tmem + (uint32_t)(ab * kTile + c) + lanes, v);
-        if (row < args.M) mm_epilogue(args, g, row, n0 + c, v, mirror, top);
+        tmem_ld32(tmem + (uint32_t)(ab * kTile + c + 32 * half) + lanes, v);
+        uint8_t* mine = sm.e[e][0] + r * 128;   // 16-byte piece j of the row stands at j ^ (r & 7)
+        uint8_t* other = sm.e[e][1] + r * 128;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int at = ((half * 4 + j) ^ (r & 7)) * 16;
+          float f[8], dc[8];
+          if (by_col) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) dc[k] = __shfl_sync(~0u, dcol[c / kChunk], 8 * j + k);
+          }
+          if (q.role == GRAM) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              f[k] = v[8 * j + k] * kUnscale;
+              if (c0 + 8 * j + k == row) {
+                if (row < q.M) da[row] = v[8 * j + k] * kUnscale2;
+                f[k] = 0.f;
+              }
+            }
+          } else if (q.role == POLY) {  // with D = diag dA and O the rest of A: A A = O O + D O + O D + D D
+            unpack8(*reinterpret_cast<const uint4*>(mine + at), f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const float acc = v[8 * j + k];
+              f[k] = fmaf(kB, f[k], kC * fmaf(dr + dc[k], f[k], kUnscale * acc));
+              if (c0 + 8 * j + k == row) {
+                if (row < q.M) dg[row] = fmaf(kB, dr, kC * fmaf(dr, dr, acc * kUnscale2));
+                f[k] = 0.f;
+              }
+            }
+          } else {
+            float lo[8];
+            unpack8(*reinterpret_cast<const uint4*>(mine + at), f);
+            unpack8(*reinterpret_cast<const uint4*>(other + at), lo);
+            const float tl = kA + (late ? top : 0.f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              f[k] = fmaf(kA + (by_col ? dc[k] : dr), f[k], fmaf(tl, lo[k], kUnscale * v[8 * j + k]));
+          }
+          if (q.role == LAST) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] *= kUnscale;
+            *reinterpret_cast<uint4*>(mine + at) = pack8_bf16(f);
+          } else {
+            const uint4 w = pack8(f);
+            *reinterpret_cast<uint4*>(mine + at) = w;
+            if (q.role == NEXT) {
+              float hi[8];
+              unpack8(w, hi);
+#pragma unroll
+              for (int k = 0; k < 8; ++k) hi[k] = f[k] - hi[k];
+              *reinterpret_cast<uint4*>(other + at) = pack8(hi);
+            } else if (mirror) {
+              // the transpose: row c, 64 values of r to a box of 64 rows
+              uint8_t* box = sm.e[e][1] + (r >> 6) * (kOpBytes / 2);
+              const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const int cc = 32 * half + 8 * j + k;
+                const uint16_t b = (uint16_t)(k & 1 ? words[k / 2] >> 16 : words[k / 2]);
+                *reinterpret_cast<uint16_t*>(box + cc * 128 + ((((r & 63) >> 3) ^ (cc & 7)) * 16) + (r & 7) * 2) = b;
+              }
+            }
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        const int x = q.n0 + c;
+        if (q.role == LAST && !args.o_tma) {
+          // o's rows are not on 16-byte boundaries: a warp per row, 2 bytes a lane
+          for (int rr = warp - 4; rr < kHalf && m0 + rr < q.M; rr += 8) {
+            uint16_t* to = args.o + (int64_t)q.g * args.o_gs + (int64_t)(m0 + rr) * args.cols + x;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const int cc = lane + 32 * k;
+              if (x + cc < q.N)
+                to[cc] = *reinterpret_cast<const uint16_t*>(sm.e[e][0] + rr * 128 + (((cc >> 3) ^ (rr & 7)) * 16) + (cc & 7) * 2);
+            }
+          }
+          asm volatile("bar.sync 1, 256;" ::: "memory");
+          if (storer) mbar_arrive(&sm.epi_empty[e]);
+        } else if (storer) {
+          if (m0 < q.M) {
+            if (q.role == GRAM) tma_store(&args.ak, sm.e[e][0], x, m0, q.g);
+            if (q.role == POLY) tma_store(&args.pk, sm.e[e][0], x, m0, q.g);
+            if (q.role == LAST) tma_store(&args.om, sm.e[e][0], x, m0, q.g);
+            if (q.role == NEXT) {
+              tma_store(&args.xk[in ^ 1], sm.e[e][0], x, m0, q.g);
+              tma_store(&args.lk[in ^ 1], sm.e[e][1], x, m0, q.g);
+            }
+            if (mirror) {
+              tma_store(q.role == GRAM ? &args.am : &args.pm, sm.e[e][1], m0, x, q.g);
+              if (m0 + 64 < q.M)
+                tma_store(q.role == GRAM ? &args.am : &args.pm, sm.e[e][1] + kOpBytes / 2, m0 + 64, x, q.g);
+            }
+          }
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          // the buffer before this one has been read by its stores (kEpi > 2: the ring goes on meanwhile)
+          if (c > 0) {
+            asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+            mbar_arrive(&sm.epi_empty[e == 0 ? kEpi - 1 : e - 1]);
+          }
+          if (c + kChunk >= kTile || q.n0 + c + kChunk >= q.N) {
+            // the tile is complete: its writes, and the diagonal's by the other warps, before the count
+            asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+            mbar_arrive(&sm.epi_empty[e]);
+            asm volatile("fence.proxy.async;" ::: "memory");
+            __threadfence();
+            asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(args.done + q.g) : "memory");
+          }
+        }
+        if (++e == kEpi) e = 0, ph ^= 1;
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
       if (lane == 0) arrive_at(in_cta(&sm.acc_empty[ab], 0));
+      // a wait that ran out in one warp ends the loop in all of them, so that none is left at a barrier of theirs
+      uint32_t all;
+      asm volatile(
+          "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.red.and.pred q, 1, 256, p;\n selp.u32 %0, 1, 0, q;\n}\n"
+          : "=r"(all)
+          : "r"((uint32_t)ok)
+          : "memory");
+      ok = all != 0;
     }
+    if (storer) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
@@ -625,23 +842,13 @@ void load_encode() {
     cudaGetLastError();
 }
 
-// A rank-3 map over [G][rows][ld] fp16 (cols of them in use), 128-byte swizzle, box {64, box_rows}.
-bool half_map(CUtensorMap* map, const __half* base, int64_t cols, int64_t rows, int64_t ld, int64_t gs, int G, int box_rows) {
-  cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)G};
-  cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)gs * 2};
-  cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, estr[3] = {1, 1, 1};
-  return g_encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<__half*>(base), dims, strides, box, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 int64_t pad16(int64_t v) { return (v + 15) / 16 * 16; }
 
 // The workspace: two pairs of X, A and P, P's diagonals, the norms' partial sums; each part 1024-byte aligned.
 struct DirLayout {
   int64_t ldx, lda, n;
   int chunks, per;
-  size_t h[2], l[2], A, P, diag_a, diag, part, bytes;
+  size_t h[2], l[2], A, P, diag_a, diag, part, done, bytes;
 };
 DirLayout direction_layout(int G, int64_t rows, int64_t cols) {
   DirLayout d{};
@@ -659,9 +866,10 @@ DirLayout direction_layout(int G, int64_t rows, int64_t cols) {
   d.diag_a = take(4 * (size_t)G * d.n);
   d.diag = take(4 * (size_t)G * d.n);
   const int64_t elems = rows * cols;
-  d.per = (int)std::max<int64_t>(4096, (elems + 255) / 256);
+  d.per = (int)(std::max<int64_t>(4096, (elems + 255) / 256) + 7) / 8 * 8;
   d.chunks = (int)((elems + d.per - 1) / d.per);
   d.part = take(12 * (size_t)G * d.chunks);
+  d.done = take(4 * (size_t)G);
   d.bytes = at;
   return d;
 }
@@ -686,22 +894,40 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
 
 bool off_align(const void* p, int z) { return reinterpret_cast<uintptr_t>(p) % z != 0; }
 
-cudaError_t launch_product(const MmArgs& a, cudaStream_t st) {
-  static std::atomic<int> raised{0};
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  const size_t smem = sizeof(MmSmem) + 1024;
-  if (raised != dev + 1) {
-    e = cudaFuncSetAttribute(direction_product_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-    raised = dev + 1;
-  }
-  const int64_t tm = (a.M + kTile - 1) / kTile, tn = (a.N + kTile - 1) / kTile;
-  const int64_t tiles = (a.role <= POLY ? tm * (tm + 1) / 2 : tm * tn) * a.G;
-  if (tiles > 0x7fffffff) return cudaErrorInvalidValue;
-  return launch_pdl(direction_product_kernel, dim3(2 * (unsigned)std::min<int64_t>(tiles, kNumSMs / 2)), dim3(kThreads),
-                    smem, st, a);
+// A rank-3 map over [G][rows][ld] 16-bit values (cols of them in use), 128-byte swizzle, box {64, box_rows}.
+bool half_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, int64_t cols, int64_t rows, int64_t ld, int64_t gs,
+              int G, int box_rows) {
+  cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)G};
+  cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)gs * 2};
+  cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, estr[3] = {1, 1, 1};
+  return g_encode(map, type, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The pairs of CTAs that are resident at once on device `dev` (0: an error).
+int resident_pairs(int dev, size_t smem, cudaError_t* err) {
+  static std::atomic<int> known{0};  // (device + 1) << 16 | pairs
+  const int k = known;
+  if (k >> 16 == dev + 1) return k & 0xffff;
+  *err = cudaFuncSetAttribute(direction_product_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (*err != cudaSuccess) return 0;
+  int sms = 0, clusters = 0;
+  *err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (*err != cudaSuccess) return 0;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(sms / 2 * 2);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2, attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr, cfg.numAttrs = 1;
+  *err = cudaOccupancyMaxActiveClusters(&clusters, direction_product_kernel, &cfg);
+  if (*err != cudaSuccess || clusters < 1) return 0;
+  const int pairs = std::min(clusters, sms / 2);
+  known = (dev + 1) << 16 | pairs;
+  return pairs;
 }
 
 cudaError_t run_direction(DirArgs d, const DirLayout& ly, uint8_t* ws, int steps, cudaStream_t st) {
@@ -711,44 +937,55 @@ cudaError_t run_direction(DirArgs d, const DirLayout& ly, uint8_t* ws, int steps
   for (int i = 0; i < 2; ++i) h[i] = reinterpret_cast<__half*>(ws + ly.h[i]), l[i] = reinterpret_cast<__half*>(ws + ly.l[i]);
   d.h = h[0], d.l = l[0], d.ld = ly.ldx, d.chunks = ly.chunks, d.per = ly.per;
   d.part = reinterpret_cast<float*>(ws + ly.part);
-  const dim3 grid(ly.chunks, d.G);
-  cudaError_t e = launch_pdl(direction_momentum_kernel, grid, dim3(kMomThreads), 0, st, d);
-  if (e != cudaSuccess) return e;
-  e = launch_pdl(direction_normalise_kernel, grid, dim3(kMomThreads), 0, st, d);
-  if (e != cudaSuccess) return e;
-  const int n = (int)ly.n, tall = d.rows > d.cols;
-  const int64_t x_gs = (int64_t)d.rows * ly.ldx, a_gs = (int64_t)n * ly.lda;
+  d.done = reinterpret_cast<uint32_t*>(ws + ly.done);
   MmArgs a{};
-  a.G = d.G, a.tall = tall, a.n = n, a.lda = ly.lda, a.ldx = ly.ldx, a.x_gs = x_gs;
+  const int n = (int)ly.n;
+  const int64_t x_gs = (int64_t)d.rows * ly.ldx, a_gs = (int64_t)n * ly.lda;
+  a.G = d.G, a.n = n, a.rows = d.rows, a.cols = d.cols, a.steps = steps, a.tall = d.rows > d.cols;
   a.diag_a = reinterpret_cast<float*>(ws + ly.diag_a), a.diag = reinterpret_cast<float*>(ws + ly.diag);
-  a.o = d.o, a.o_gs = d.o_gs, a.ldo = d.cols;
-  a.o_vec = !off_align(d.o, 32) && d.cols % 16 == 0 && d.o_gs % 16 == 0;
-  CUtensorMap xk[2], xm[2], ak, pk;
+  a.done = d.done, a.o = d.o, a.o_gs = d.o_gs;
+  a.o_tma = !off_align(d.o, 16) && d.cols % 8 == 0 && d.o_gs % 8 == 0;
+  const CUtensorMapDataType f16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  bool ok = true;
   for (int i = 0; i < 2; ++i)
-    if (!half_map(&xk[i], h[i], d.cols, d.rows, ly.ldx, x_gs, d.G, kHalf) ||
-        !half_map(&xm[i], h[i], d.cols, d.rows, ly.ldx, x_gs, d.G, 64))
-      return cudaErrorInvalidValue;
-  if (!half_map(&ak, A, n, n, ly.lda, a_gs, d.G, kHalf) || !half_map(&pk, P, n, n, ly.lda, a_gs, d.G, kHalf))
-    return cudaErrorInvalidValue;
-  for (int s = 0; s < steps; ++s) {
-    const int in = s & 1;
-    MmArgs q = a;
-    q.role = GRAM, q.M = q.N = n, q.K = tall ? d.rows : d.cols;
-    q.a = q.b = tall ? xm[in] : xk[in];
-    q.a_mn = q.b_mn = tall;
-    q.out = A;
-    if ((e = launch_product(q, st)) != cudaSuccess) return e;
-    q = a;
-    q.role = POLY, q.M = q.N = q.K = n, q.a = q.b = ak, q.A = A, q.out = P;
-    if ((e = launch_product(q, st)) != cudaSuccess) return e;
-    q = a;
-    q.role = s + 1 < steps ? NEXT : LAST, q.late = s + 2 >= steps, q.M = d.rows, q.N = d.cols, q.K = n;
-    if (tall) q.a = xk[in], q.b = pk;
-    else q.a = pk, q.b = xm[in], q.b_mn = 1;
-    q.h = h[in], q.l = l[in], q.out = h[in ^ 1], q.out_l = l[in ^ 1];
-    if ((e = launch_product(q, st)) != cudaSuccess) return e;
-  }
-  return cudaSuccess;
+    ok = ok && half_map(&a.xk[i], f16, h[i], d.cols, d.rows, ly.ldx, x_gs, d.G, kHalf) &&
+         half_map(&a.xm[i], f16, h[i], d.cols, d.rows, ly.ldx, x_gs, d.G, 64) &&
+         half_map(&a.lk[i], f16, l[i], d.cols, d.rows, ly.ldx, x_gs, d.G, kHalf);
+  ok = ok && half_map(&a.ak, f16, A, n, n, ly.lda, a_gs, d.G, kHalf) && half_map(&a.am, f16, A, n, n, ly.lda, a_gs, d.G, 64) &&
+       half_map(&a.pk, f16, P, n, n, ly.lda, a_gs, d.G, kHalf) && half_map(&a.pm, f16, P, n, n, ly.lda, a_gs, d.G, 64);
+  if (a.o_tma)
+    ok = ok && half_map(&a.om, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, d.o, d.cols, d.rows, d.cols, d.o_gs, d.G, kHalf);
+  if (!ok) return cudaErrorInvalidValue;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const size_t smem = sizeof(MmSmem) + 1024;
+  const int pairs = resident_pairs(dev, smem, &e);
+  if (pairs < 1) return e == cudaSuccess ? cudaErrorInvalidConfiguration : e;
+  const dim3 grid(ly.chunks, d.G);
+  // values per access: a row of h and l is 32-byte aligned, so a vector that divides the columns stays within a row
+  auto aligned = [&](int v) {
+    const bool u = d.mom == 0.f || (!off_align(d.u, 16) && (d.G == 1 || d.u_gs % 4 == 0));
+    return d.cols % v == 0 && u && !off_align(d.g, d.g_bf16 ? 8 : 16) && (d.G == 1 || d.g_gs % 4 == 0);
+  };
+  auto prepare = [&](auto momentum, auto normalise) {
+    const cudaError_t r = launch_pdl(momentum, grid, dim3(kMomThreads), 0, st, d);
+    return r == cudaSuccess ? launch_pdl(normalise, grid, dim3(kMomThreads), 0, st, d) : r;
+  };
+  e = aligned(8)   ? prepare(direction_momentum_kernel<8>, direction_normalise_kernel<8>)
+      : aligned(4) ? prepare(direction_momentum_kernel<4>, direction_normalise_kernel<4>)
+                   : prepare(direction_momentum_kernel<1>, direction_normalise_kernel<1>);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(2 * pairs);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeCooperative;
+  attr[0].val.cooperative = 1;
+  cfg.attrs = attr, cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, direction_product_kernel, a);
 }
 
 }  // namespace
