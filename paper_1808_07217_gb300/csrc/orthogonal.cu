@@ -240,10 +240,11 @@ __global__ void __launch_bounds__(kMomThreads) direction_normalise_kernel(const 
 //   warp 0      TMA producer of both operands into a ring of kStages stages (both CTAs' bytes counted on the leader's
 //               barrier)
 //   warp 1      MMA issuer (leader only)
-//   warp 2      tensor memory allocation (two accumulators of 256 columns)
+//   warp 2      tensor memory allocation (two accumulators of 256 columns); TMA stores of the epilogue's buffers, and the
+//               count of finished tiles
 //   warp 3      TMA loads of what the epilogue reads (h and l, or A), 64 columns at a time into a ring of kEpi buffers,
 //               ahead of the accumulator
-//   warps 4-11  epilogue: a warp per 32 rows and 32 columns of a buffer, in place; TMA stores from it
+//   warps 4-11  epilogue: a warp per 32 rows and 32 columns of a buffer, in place, each at its own pace
 //
 // The tiles of all steps form one list: per step the tiles of A = X X^T of every matrix, then those of P, then those of
 // X.  Pair p takes tiles p, p + pairs, ...; `done[g]` counts the CTAs' finished tiles of matrix g, whose phases follow one
@@ -272,7 +273,7 @@ struct MmSmem {
   uint8_t e[kEpi][2][kOpBytes];  // h or A and the tile stored; l or the mirrored tile
   uint64_t full[kStages], empty[kStages];
   uint64_t acc_full[2], acc_empty[2];
-  uint64_t epi_full[kEpi], epi_empty[kEpi];
+  uint64_t epi_full[kEpi], epi_ready[kEpi], epi_empty[kEpi];
   uint32_t tmem_base;
 };
 
@@ -374,21 +375,18 @@ __device__ __forceinline__ void commit_pair(uint64_t* bar) {
 __device__ __forceinline__ void arrive_at(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// 32 accumulator columns of this warp's 32 rows, one row per lane.
-__device__ __forceinline__ void tmem_ld32(uint32_t at, float (&v)[32]) {
-  uint32_t r[32];
+// 16 accumulator columns of this warp's 32 rows, one row per lane.
+__device__ __forceinline__ void tmem_ld16(uint32_t at, float (&v)[16]) {
+  uint32_t r[16];
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
-      "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
       "tcgen05.wait::ld.sync.aligned;"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(at)
       : "memory");
 #pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
 // Eight fp16 (or bf16) values in 16 bytes.
@@ -426,25 +424,25 @@ struct Item {
 };
 struct Plan {
   int ts, tm, tn, per_sym, per_x;  // tiles a side of A; of X; tiles of a symmetric product and of X
-  int64_t per_step, total;
+  int per_step, total;  // the host has checked that the list has fewer than 2^31 tiles
   __device__ __forceinline__ explicit Plan(const MmArgs& a) {
     ts = (a.n + kTile - 1) / kTile;
     tm = (a.rows + kTile - 1) / kTile, tn = (a.cols + kTile - 1) / kTile;
     per_sym = ts * (ts + 1) / 2, per_x = tm * tn;
-    per_step = (int64_t)a.G * (2 * per_sym + per_x);
+    per_step = a.G * (2 * per_sym + per_x);
     total = per_step * a.steps;
   }
-  __device__ __forceinline__ Item at(const MmArgs& a, int64_t t) const {
+  __device__ __noinline__ Item at(const MmArgs& a, int t) const {
     Item it;
-    it.step = (int)(t / per_step);
-    int64_t r = t - it.step * per_step;
-    const int64_t syms = (int64_t)a.G * per_sym;
+    it.step = t / per_step;
+    int r = t - it.step * per_step;
+    const int syms = a.G * per_sym;
     it.need = 2u * (uint32_t)it.step * (uint32_t)(2 * per_sym + per_x);
     if (r < 2 * syms) {
       it.role = r < syms ? GRAM : POLY;
       if (it.role == POLY) r -= syms, it.need += 2u * per_sym;
-      it.g = (int)(r / per_sym);
-      const int q = (int)(r - (int64_t)it.g * per_sym);
+      it.g = r / per_sym;
+      const int q = r - it.g * per_sym;
       // tiles on and below the diagonal, row by row
       int i = (int)((sqrtf(8.f * (float)q + 1.f) - 1.f) * 0.5f);
       while (i * (i + 1) / 2 > q) --i;
@@ -456,8 +454,8 @@ struct Plan {
       r -= 2 * syms;
       it.role = it.step + 1 < a.steps ? NEXT : LAST;
       it.need += 4u * per_sym;
-      it.g = (int)(r / per_x);
-      const int q = (int)(r - (int64_t)it.g * per_x);
+      it.g = r / per_x;
+      const int q = r - it.g * per_x;
       it.m0 = q % tm * kTile, it.n0 = q / tm * kTile;
       it.M = a.rows, it.N = a.cols, it.K = a.n;
     }
@@ -485,6 +483,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     }
     for (int i = 0; i < kEpi; ++i) {
       mbar_init(&sm.epi_full[i], 1);
+      mbar_init(&sm.epi_ready[i], 8);  // the epilogue warps
       mbar_init(&sm.epi_empty[i], 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -508,7 +507,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     int64_t it = 0;
     uint32_t ph = 1;
     bool ok = true;
-    for (int64_t t = pair; t < plan.total && ok; t += pairs) {
+    for (int t = pair; t < plan.total && ok; t += pairs) {
       const Item q = plan.at(args, t);
       if (!(ok = wait_count_warp(args.done + q.g, q.need))) break;
       const int in = q.step & 1, m0 = q.m0 + rank * kHalf, n0 = q.n0 + rank * kHalf, nk = (q.K + kBK - 1) / kBK;
@@ -549,7 +548,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     int i = 0, s = 0;
     uint32_t ph = 0;
     bool ok = true;
-    for (int64_t t = pair; t < plan.total && ok; t += pairs, ++i) {
+    for (int t = pair; t < plan.total && ok; t += pairs, ++i) {
       const Item q = plan.at(args, t);
       const int nk = (q.K + kBK - 1) / kBK, ab = i & 1;
       const bool a_mn = q.role == GRAM && args.tall, b_mn = q.role <= POLY ? a_mn : !args.tall;
@@ -583,7 +582,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     int64_t it = 0;
     uint32_t ph = 1;
     bool ok = true;
-    for (int64_t t = pair; t < plan.total && ok; t += pairs) {
+    for (int t = pair; t < plan.total && ok; t += pairs) {
       const Item q = plan.at(args, t);
       if (!(ok = wait_count_warp(args.done + q.g, q.need))) break;
       const int in = q.step & 1, m0 = q.m0 + rank * kHalf;
@@ -609,142 +608,27 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     }
     if (!ok)
       for (int64_t j = it > kEpi ? it - kEpi : 0; j < it; ++j) wait_bar(&sm.epi_full[j % kEpi], (j / kEpi) & 1);
-  } else if (warp >= 4) {
-    const int quarter = warp & 3, half = (warp - 4) >> 2;
-    const int r = quarter * 32 + lane;  // the row of this CTA's half tile
-    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    const bool storer = threadIdx.x == 128;
-    int i = 0, e = 0, of = -1;
+  } else if (warp == 2) {
+    const bool el = elect_one();
+    int e = 0;
     uint32_t ph = 0;
-    float top = 0.f;
     bool ok = true;
-    for (int64_t t = pair; t < plan.total && ok; t += pairs, ++i) {
+    for (int t = pair; t < plan.total && ok; t += pairs) {
       const Item q = plan.at(args, t);
-      const int ab = i & 1, m0 = q.m0 + rank * kHalf, row = m0 + r, in = q.step & 1;
-      const bool mirror = q.role <= POLY && q.m0 != q.n0, sym = q.role <= POLY;
-      ok = wait_count_warp(args.done + q.g, q.need);
-      float* da = args.diag_a + (int64_t)q.g * args.n;
-      float* dg = args.diag + (int64_t)q.g * args.n;
-      const bool late = !sym && q.step + 2 >= args.steps;
-      if (ok && late && of != q.step * args.G + q.g) {  // t: the largest of P's diagonal
-        top = -INFINITY;
-        for (int k = lane; k < args.n; k += 32) top = fmaxf(top, __ldcg(dg + k));
-#pragma unroll
-        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-        of = q.step * args.G + q.g;
-      }
-      const bool by_row = q.role == POLY || (!sym && !args.tall);
-      const float dr = by_row && row < q.M ? __ldcg((q.role == POLY ? da : dg) + row) : 0.f;
-      const bool by_col = q.role == POLY || (!sym && args.tall);
-      float dcol[kTile / kChunk];  // the diagonal's values at this lane's column of each chunk
-#pragma unroll
-      for (int k = 0; k < kTile / kChunk; ++k) {
-        const int col = q.n0 + k * kChunk + 32 * half + lane;
-        dcol[k] = by_col && col < q.N ? __ldcg((q.role == POLY ? da : dg) + col) : 0.f;
-      }
-      ok = ok && wait_bar_warp(&sm.acc_full[ab], (i >> 1) & 1);
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-#pragma unroll
-      for (int c = 0; c < kTile; c += kChunk) {
-        if (q.n0 + c >= q.N) break;
-        const int c0 = q.n0 + c + 32 * half;  // this thread's columns
-        ok = ok && wait_bar_warp(&sm.epi_full[e], ph);
-        float v[32];
-        tmem_ld32(tmem + (uint32_t)(ab * kTile + c + 32 * half) + lanes, v);
-        uint8_t* mine = sm.e[e][0] + r * 128;   // 16-byte piece j of the row stands at j ^ (r & 7)
-        uint8_t* other = sm.e[e][1] + r * 128;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int at = ((half * 4 + j) ^ (r & 7)) * 16;
-          float f[8], dc[8];
-          if (by_col) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) dc[k] = __shfl_sync(~0u, dcol[c / kChunk], 8 * j + k);
-          }
-          if (q.role == GRAM) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              f[k] = v[8 * j + k] * kUnscale;
-              if (c0 + 8 * j + k == row) {
-                if (row < q.M) da[row] = v[8 * j + k] * kUnscale2;
-                f[k] = 0.f;
-              }
-            }
-          } else if (q.role == POLY) {  // with D = diag dA and O the rest of A: A A = O O + D O + O D + D D
-            unpack8(*reinterpret_cast<const uint4*>(mine + at), f);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const float acc = v[8 * j + k];
-              f[k] = fmaf(kB, f[k], kC * fmaf(dr + dc[k], f[k], kUnscale * acc));
-              if (c0 + 8 * j + k == row) {
-                if (row < q.M) dg[row] = fmaf(kB, dr, kC * fmaf(dr, dr, acc * kUnscale2));
-                f[k] = 0.f;
-              }
-            }
-          } else {
-            float lo[8];
-            unpack8(*reinterpret_cast<const uint4*>(mine + at), f);
-            unpack8(*reinterpret_cast<const uint4*>(other + at), lo);
-            const float tl = kA + (late ? top : 0.f);
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-              f[k] = fmaf(kA + (by_col ? dc[k] : dr), f[k], fmaf(tl, lo[k], kUnscale * v[8 * j + k]));
-          }
-          if (q.role == LAST) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] *= kUnscale;
-            *reinterpret_cast<uint4*>(mine + at) = pack8_bf16(f);
-          } else {
-            const uint4 w = pack8(f);
-            *reinterpret_cast<uint4*>(mine + at) = w;
-            if (q.role == NEXT) {
-              float hi[8];
-              unpack8(w, hi);
-#pragma unroll
-              for (int k = 0; k < 8; ++k) hi[k] = f[k] - hi[k];
-              *reinterpret_cast<uint4*>(other + at) = pack8(hi);
-            } else if (mirror) {
-              // the transpose: row c, 64 values of r to a box of 64 rows
-              uint8_t* box = sm.e[e][1] + (r >> 6) * (kOpBytes / 2);
-              const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const int cc = 32 * half + 8 * j + k;
-                const uint16_t b = (uint16_t)(k & 1 ? words[k / 2] >> 16 : words[k / 2]);
-                *reinterpret_cast<uint16_t*>(box + cc * 128 + ((((r & 63) >> 3) ^ (cc & 7)) * 16) + (r & 7) * 2) = b;
-              }
-            }
-          }
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        const int x = q.n0 + c;
-        if (q.role == LAST && !args.o_tma) {
-          // o's rows are not on 16-byte boundaries: a warp per row, 2 bytes a lane
-          for (int rr = warp - 4; rr < kHalf && m0 + rr < q.M; rr += 8) {
-            uint16_t* to = args.o + (int64_t)q.g * args.o_gs + (int64_t)(m0 + rr) * args.cols + x;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const int cc = lane + 32 * k;
-              if (x + cc < q.N)
-                to[cc] = *reinterpret_cast<const uint16_t*>(sm.e[e][0] + rr * 128 + (((cc >> 3) ^ (rr & 7)) * 16) + (cc & 7) * 2);
-            }
-          }
-          asm volatile("bar.sync 1, 256;" ::: "memory");
-          if (storer) mbar_arrive(&sm.epi_empty[e]);
-        } else if (storer) {
-          if (m0 < q.M) {
-            if (q.role == GRAM) tma_store(&args.ak, sm.e[e][0], x, m0, q.g);
-            if (q.role == POLY) tma_store(&args.pk, sm.e[e][0], x, m0, q.g);
-            if (q.role == LAST) tma_store(&args.om, sm.e[e][0], x, m0, q.g);
-            if (q.role == NEXT) {
-              tma_store(&args.xk[in ^ 1], sm.e[e][0], x, m0, q.g);
-              tma_store(&args.lk[in ^ 1], sm.e[e][1], x, m0, q.g);
-            }
+      const int m0 = q.m0 + rank * kHalf, in = q.step & 1;
+      const bool mirror = q.role <= POLY && q.m0 != q.n0, by_tma = q.role != LAST || args.o_tma;
+      for (int c = 0; c < kTile && q.n0 + c < q.N; c += kChunk) {
+        if (!(ok = wait_bar_warp(&sm.epi_ready[e], ph))) break;
+        if (el) {
+          const int x = q.n0 + c;
+          if (m0 < q.M && by_tma) {
+            const CUtensorMap* to = q.role == GRAM ? &args.ak : q.role == POLY ? &args.pk : q.role == NEXT ? &args.xk[in ^ 1] : &args.om;
+            tma_store(to, sm.e[e][0], x, m0, q.g);
+            if (q.role == NEXT) tma_store(&args.lk[in ^ 1], sm.e[e][1], x, m0, q.g);
             if (mirror) {
-              tma_store(q.role == GRAM ? &args.am : &args.pm, sm.e[e][1], m0, x, q.g);
-              if (m0 + 64 < q.M)
-                tma_store(q.role == GRAM ? &args.am : &args.pm, sm.e[e][1] + kOpBytes / 2, m0 + 64, x, q.g);
+              to = q.role == GRAM ? &args.am : &args.pm;
+              tma_store(to, sm.e[e][1], m0, x, q.g);
+              if (m0 + 64 < q.M) tma_store(to, sm.e[e][1] + kOpBytes / 2, m0 + 64, x, q.g);
             }
           }
           asm volatile("cp.async.bulk.commit_group;" ::: "memory");
@@ -754,29 +638,152 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
             mbar_arrive(&sm.epi_empty[e == 0 ? kEpi - 1 : e - 1]);
           }
           if (c + kChunk >= kTile || q.n0 + c + kChunk >= q.N) {
-            // the tile is complete: its writes, and the diagonal's by the other warps, before the count
-            asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
             mbar_arrive(&sm.epi_empty[e]);
+            // the tile is complete: its writes, and the diagonal's by the epilogue warps, before the count
+            asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
             asm volatile("fence.proxy.async;" ::: "memory");
             __threadfence();
             asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(args.done + q.g) : "memory");
           }
         }
+        __syncwarp();
+        if (++e == kEpi) e = 0, ph ^= 1;
+      }
+    }
+    if (el) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    __syncwarp();
+  } else if (warp >= 4) {
+    const int quarter = warp & 3, half = (warp - 4) >> 2;
+    const int r = quarter * 32 + lane;  // the row of this CTA's half tile
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    int i = 0, e = 0, of = -1;
+    uint32_t ph = 0;
+    float top = 0.f;
+    bool ok = true;
+    for (int t = pair; t < plan.total && ok; t += pairs, ++i) {
+      const Item q = plan.at(args, t);
+      const int role = q.role;
+      const int ab = i & 1, m0 = q.m0 + rank * kHalf, row = m0 + r;
+      const bool mirror = role <= POLY && q.m0 != q.n0, sym = role <= POLY;
+      if (!(ok = wait_count_warp(args.done + q.g, q.need))) break;
+      float* da = args.diag_a + (int64_t)q.g * args.n;
+      float* dg = args.diag + (int64_t)q.g * args.n;
+      float tl = kA;
+      if (!sym && q.step + 2 >= args.steps) {  // t: the largest of P's diagonal
+        if (of != q.step * args.G + q.g) {
+          top = -INFINITY;
+          for (int k = lane; k < args.n; k += 32) top = fmaxf(top, __ldcg(dg + k));
+#pragma unroll
+          for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+          of = q.step * args.G + q.g;
+        }
+        tl += top;
+      }
+      // the diagonal's value of this row, and of this lane's column of the coming chunk
+      const bool by_row = role == POLY || (!sym && !args.tall), by_col = role == POLY || (!sym && args.tall);
+      const float* dsrc = role == POLY ? da : dg;
+      const float dr = by_row && row < q.M ? __ldcg(dsrc + row) : 0.f;
+      int col = q.n0 + 32 * half + lane;
+      float dnext = by_col && col < q.N ? __ldcg(dsrc + col) : 0.f;
+      if (!(ok = wait_bar_warp(&sm.acc_full[ab], (i >> 1) & 1))) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll 1
+      for (int c = 0; c < kTile && q.n0 + c < q.N; c += kChunk) {
+        const float dcol = dnext;
+        col += kChunk;
+        dnext = by_col && c + kChunk < kTile && col < q.N ? __ldcg(dsrc + col) : 0.f;
+        if (!(ok = wait_bar_warp(&sm.epi_full[e], ph))) break;
+        uint8_t* mine = sm.e[e][0] + r * 128;  // 16-byte piece j of the row stands at j ^ (r & 7)
+        uint8_t* other = sm.e[e][1] + r * 128;
+#pragma unroll 1
+        for (int jj = 0; jj < 2; ++jj) {
+          const int cc = 32 * half + 16 * jj;  // the columns cc .. cc + 15 of the chunk
+          float v[16];
+          tmem_ld16(tmem + (uint32_t)(ab * kTile + c + cc) + lanes, v);
+          const int dd = row - (q.n0 + c + cc);  // the diagonal's place among them
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int at = ((cc / 8 + j) ^ (r & 7)) * 16;
+            float f[8];
+            if (role == GRAM) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                f[k] = v[8 * j + k] * kUnscale;
+                if (dd == 8 * j + k) {
+                  if (row < q.M) da[row] = v[8 * j + k] * kUnscale2;
+                  f[k] = 0.f;
+                }
+              }
+            } else if (role == POLY) {  // with D = diag dA and O the rest of A: A A = O O + D O + O D + D D
+              unpack8(*reinterpret_cast<const uint4*>(mine + at), f);
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const float acc = v[8 * j + k], dc = __shfl_sync(~0u, dcol, 16 * jj + 8 * j + k);
+                f[k] = fmaf(kB, f[k], kC * fmaf(dr + dc, f[k], kUnscale * acc));
+                if (dd == 8 * j + k) {
+                  if (row < q.M) dg[row] = fmaf(kB, dr, kC * fmaf(dr, dr, acc * kUnscale2));
+                  f[k] = 0.f;
+                }
+              }
+            } else {
+              float lo[8];
+              unpack8(*reinterpret_cast<const uint4*>(mine + at), f);
+              unpack8(*reinterpret_cast<const uint4*>(other + at), lo);
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const float d = by_col ? __shfl_sync(~0u, dcol, 16 * jj + 8 * j + k) : dr;
+                f[k] = fmaf(kA + d, f[k], fmaf(tl, lo[k], kUnscale * v[8 * j + k]));
+              }
+            }
+            if (role == LAST) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k) f[k] *= kUnscale;
+              *reinterpret_cast<uint4*>(mine + at) = pack8_bf16(f);
+            } else {
+              const uint4 w = pack8(f);
+              *reinterpret_cast<uint4*>(mine + at) = w;
+              if (role == NEXT) {
+                float hi[8];
+                unpack8(w, hi);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) hi[k] = f[k] - hi[k];
+                *reinterpret_cast<uint4*>(other + at) = pack8(hi);
+              } else if (mirror) {
+                // the transpose: row cc + .. of a box of 64 values of r
+                uint8_t* box = sm.e[e][1] + (r >> 6) * (kOpBytes / 2) + (cc + 8 * j) * 128 + (r & 7) * 2;
+                const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int k = 0; k < 8; ++k)  // row 8 j + k of the box: its number's low bits are k
+                  *reinterpret_cast<uint16_t*>(box + k * 128 + ((((r & 63) >> 3) ^ k) * 16)) =
+                      (uint16_t)(k & 1 ? words[k / 2] >> 16 : words[k / 2]);
+              }
+            }
+          }
+        }
+        if (role == LAST && !args.o_tma) {
+          // o's rows are not on 16-byte boundaries: this warp's 32 rows of 32 columns, a row at a time
+          __syncwarp();
+          uint16_t* o = args.o + (int64_t)q.g * args.o_gs + q.n0 + c + 32 * half + lane;
+          const int rows = min(32, q.M - (m0 + quarter * 32));
+          const int piece = half * 4 + (lane >> 3);
+          if (q.n0 + c + 32 * half + lane < q.N)
+#pragma unroll 4
+            for (int k = 0; k < rows; ++k) {
+              const int rr = quarter * 32 + k;
+              o[(int64_t)(m0 + rr) * args.cols] =
+                  *reinterpret_cast<const uint16_t*>(sm.e[e][0] + rr * 128 + ((piece ^ (rr & 7)) * 16) + (lane & 7) * 2);
+            }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.epi_ready[e]);
         if (++e == kEpi) e = 0, ph ^= 1;
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
       if (lane == 0) arrive_at(in_cta(&sm.acc_empty[ab], 0));
-      // a wait that ran out in one warp ends the loop in all of them, so that none is left at a barrier of theirs
-      uint32_t all;
-      asm volatile(
-          "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.red.and.pred q, 1, 256, p;\n selp.u32 %0, 1, 0, q;\n}\n"
-          : "=r"(all)
-          : "r"((uint32_t)ok)
-          : "memory");
-      ok = all != 0;
     }
-    if (storer) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
@@ -956,6 +963,8 @@ cudaError_t run_direction(DirArgs d, const DirLayout& ly, uint8_t* ws, int steps
   if (a.o_tma)
     ok = ok && half_map(&a.om, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, d.o, d.cols, d.rows, d.cols, d.o_gs, d.G, kHalf);
   if (!ok) return cudaErrorInvalidValue;
+  const int64_t ts = (n + kTile - 1) / kTile, tx = (int64_t)((d.rows + kTile - 1) / kTile) * ((d.cols + kTile - 1) / kTile);
+  if (d.G * (ts * (ts + 1) + tx) * steps > 0x3fffffff) return cudaErrorInvalidValue;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
