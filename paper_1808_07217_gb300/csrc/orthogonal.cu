@@ -27,6 +27,7 @@
 #include <atomic>
 #include <mutex>
 #include <string>
+#include <type_traits>
 
 #include "../../include/lsgd.h"
 #include "common.cuh"
@@ -93,7 +94,7 @@ struct DirArgs {
   __half *h, *l;     // [G][rows][ld]
   float* part;       // [G][chunks][3]
   int chunks, per;   // ranges of a matrix (elements per range)
-  uint32_t* done;    // [G], set to zero for the products
+  uint32_t* done;    // [3][G] (done and top of the products), set to zero for them
 };
 
 constexpr int kMomThreads = 256;
@@ -135,7 +136,7 @@ __global__ void __launch_bounds__(kMomThreads) direction_momentum_kernel(const D
   pdl_begin();
   const int n = a.rows * a.cols, i0 = blockIdx.x * a.per, i1 = min(n, i0 + a.per);
   const int64_t k = blockIdx.y;
-  if (blockIdx.x == 0 && threadIdx.x == 0) a.done[k] = 0;
+  if (blockIdx.x == 0 && threadIdx.x < 3) a.done[threadIdx.x * a.G + k] = 0;
   NormSums s{0.f, 0.f, 0.f};
 #pragma unroll 2
   for (int i = i0 + threadIdx.x * V; i < i1; i += kMomThreads * V) {
@@ -244,7 +245,9 @@ __global__ void __launch_bounds__(kMomThreads) direction_normalise_kernel(const 
 //               count of finished tiles
 //   warp 3      TMA loads of what the epilogue reads (h and l, or A), 64 columns at a time into a ring of kEpi buffers,
 //               ahead of the accumulator
-//   warps 4-11  epilogue: a warp per 32 rows and 32 columns of a buffer, in place, each at its own pace
+//   warps 4-19  epilogue: a warp per 32 rows and 16 columns of a buffer, in place, each at its own pace (8 warps took 13,000
+//               cycles a tile, mostly latencies, against the products' 8,200 at k = 1024)
+//
 //
 // The tiles of all steps form one list: per step the tiles of A = X X^T of every matrix, then those of P, then those of
 // X.  Pair p takes tiles p, p + pairs, ...; `done[g]` counts the CTAs' finished tiles of matrix g, whose phases follow one
@@ -252,7 +255,7 @@ __global__ void __launch_bounds__(kMomThreads) direction_normalise_kernel(const 
 // resident) and every tile's predecessors stand before it in the list, so that every wait ends; matrices fill each
 // other's phase ends, and nothing is launched between phases.
 
-constexpr int kTile = 256, kHalf = 128, kBK = 64, kStages = 4, kEpi = 3, kThreads = 384, kChunk = 64;
+constexpr int kTile = 256, kHalf = 128, kBK = 64, kStages = 4, kEpi = 3, kEpiWarps = 16, kThreads = 128 + 32 * kEpiWarps, kChunk = 64;
 constexpr uint32_t kOpBytes = kHalf * kBK * 2;  // one operand's share of a stage in a CTA; half an epilogue buffer
 
 enum Role { GRAM = 0, POLY = 1, NEXT = 2, LAST = 3 };
@@ -263,6 +266,7 @@ struct MmArgs {
   int G, n, rows, cols, steps, tall, o_tma;
   float *diag_a, *diag;  // [G][n]: the diagonals of A and P
   uint32_t* done;        // [G]
+  uint32_t* top;         // [2][G]: the largest of P's diagonal in each of the last two steps, as an ordered integer
   uint16_t* o;
   int64_t o_gs;
 };
@@ -325,8 +329,17 @@ __device__ __forceinline__ bool wait_count_warp(const uint32_t* count, uint32_t 
     }
   }
   ok = __shfl_sync(0xffffffffu, ok, 0);
-  asm volatile("fence.proxy.async;" ::: "memory");
+  asm volatile("fence.proxy.async.global;" ::: "memory");
   return ok != 0;
+}
+
+// An order-preserving map of floats to integers above 0, and back.
+__device__ __forceinline__ uint32_t to_ordered(float f) {
+  const uint32_t b = __float_as_uint(f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float from_ordered(uint32_t k) {
+  return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
 __device__ __forceinline__ uint32_t cta_rank() {
@@ -387,6 +400,19 @@ __device__ __forceinline__ void tmem_ld16(uint32_t at, float (&v)[16]) {
       : "memory");
 #pragma unroll
   for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+// Shared memory by its 32-bit address.
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts16(uint32_t at, const uint4 v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void sts2(uint32_t at, uint32_t low_half) {
+  asm volatile("{\n .reg .b16 h, x;\n mov.b32 {h, x}, %1;\n st.shared.b16 [%0], h;\n}\n" ::"r"(at), "r"(low_half) : "memory");
 }
 
 // Eight fp16 (or bf16) values in 16 bytes.
@@ -479,11 +505,11 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sm.acc_full[i], 1);
-      mbar_init(&sm.acc_empty[i], 16);  // the epilogue warps of both CTAs
+      mbar_init(&sm.acc_empty[i], 2 * kEpiWarps);  // the epilogue warps of both CTAs
     }
     for (int i = 0; i < kEpi; ++i) {
       mbar_init(&sm.epi_full[i], 1);
-      mbar_init(&sm.epi_ready[i], 8);  // the epilogue warps
+      mbar_init(&sm.epi_ready[i], kEpiWarps);
       mbar_init(&sm.epi_empty[i], 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -503,13 +529,16 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
 
   if (warp == 0) {
     const bool el = elect_one();
-    int s = 0;
+    int s = 0, of = -1;
     int64_t it = 0;
-    uint32_t ph = 1;
+    uint32_t ph = 1, seen = 0;
     bool ok = true;
     for (int t = pair; t < plan.total && ok; t += pairs) {
       const Item q = plan.at(args, t);
-      if (!(ok = wait_count_warp(args.done + q.g, q.need))) break;
+      if (seen != q.need || of != q.g) {  // (the last tile's wait covers this one where it is of the same phase)
+        if (!(ok = wait_count_warp(args.done + q.g, q.need))) break;
+        seen = q.need, of = q.g;
+      }
       const int in = q.step & 1, m0 = q.m0 + rank * kHalf, n0 = q.n0 + rank * kHalf, nk = (q.K + kBK - 1) / kBK;
       const CUtensorMap* ma = q.role == GRAM ? (args.tall ? &args.xm[in] : &args.xk[in])
                               : q.role == POLY ? &args.ak : (args.tall ? &args.xk[in] : &args.pk);
@@ -578,13 +607,16 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     }
   } else if (warp == 3) {
     const bool el = elect_one();
-    int e = 0;
+    int e = 0, of = -1;
     int64_t it = 0;
-    uint32_t ph = 1;
+    uint32_t ph = 1, seen = 0;
     bool ok = true;
     for (int t = pair; t < plan.total && ok; t += pairs) {
       const Item q = plan.at(args, t);
-      if (!(ok = wait_count_warp(args.done + q.g, q.need))) break;
+      if (seen != q.need || of != q.g) {
+        if (!(ok = wait_count_warp(args.done + q.g, q.need))) break;
+        seen = q.need, of = q.g;
+      }
       const int in = q.step & 1, m0 = q.m0 + rank * kHalf;
       for (int c = 0; c < kTile && q.n0 + c < q.N; c += kChunk, ++it) {
         if (!wait_bar_warp(&sm.epi_empty[e], ph)) {
@@ -619,6 +651,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
       const bool mirror = q.role <= POLY && q.m0 != q.n0, by_tma = q.role != LAST || args.o_tma;
       for (int c = 0; c < kTile && q.n0 + c < q.N; c += kChunk) {
         if (!(ok = wait_bar_warp(&sm.epi_ready[e], ph))) break;
+        const bool end = c + kChunk >= kTile || q.n0 + c + kChunk >= q.N;
         if (el) {
           const int x = q.n0 + c;
           if (m0 < q.M && by_tma) {
@@ -637,13 +670,11 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
             asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
             mbar_arrive(&sm.epi_empty[e == 0 ? kEpi - 1 : e - 1]);
           }
-          if (c + kChunk >= kTile || q.n0 + c + kChunk >= q.N) {
+          if (end) {
             asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
             mbar_arrive(&sm.epi_empty[e]);
-            // the tile is complete: its writes, and the diagonal's by the epilogue warps, before the count
             asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-            asm volatile("fence.proxy.async;" ::: "memory");
-            __threadfence();
+            // the tile's writes, and the diagonal's by the epilogue warps, before the count
             asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(args.done + q.g) : "memory");
           }
         }
@@ -654,125 +685,119 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     if (el) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     __syncwarp();
   } else if (warp >= 4) {
-    const int quarter = warp & 3, half = (warp - 4) >> 2;
+    const int quarter = warp & 3, cc = ((warp - 4) >> 2) * 16;  // 32 rows; columns cc .. cc + 15 of each chunk
     const int r = quarter * 32 + lane;  // the row of this CTA's half tile
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    int i = 0, e = 0, of = -1;
+    // within a buffer: this row's two 16-byte pieces (piece p of a row stands at p ^ (r & 7)), and the place of value r in
+    // row cc of the transpose, whose 16-byte piece k of the row's number is still to be flipped by
+    const uint32_t epi_base = smem_u32(sm.e[0][0]);
+    const uint32_t piece0 = r * 128 + ((cc / 8) ^ (r & 7)) * 16, piece1 = r * 128 + ((cc / 8 + 1) ^ (r & 7)) * 16;
+    const uint32_t flip = (uint32_t)((r >> 6) * (kOpBytes / 2) + cc * 128 + ((r & 63) >> 3) * 16 + (r & 7) * 2);
+    int i = 0, e = 0;
     uint32_t ph = 0;
-    float top = 0.f;
     bool ok = true;
     for (int t = pair; t < plan.total && ok; t += pairs, ++i) {
       const Item q = plan.at(args, t);
-      const int role = q.role;
-      const int ab = i & 1, m0 = q.m0 + rank * kHalf, row = m0 + r;
-      const bool mirror = role <= POLY && q.m0 != q.n0, sym = role <= POLY;
-      if (!(ok = wait_count_warp(args.done + q.g, q.need))) break;
+      const int role = q.role, ab = i & 1, m0 = q.m0 + rank * kHalf, row = m0 + r;
+      const bool sym = role <= POLY, on_diag = sym && q.m0 == q.n0;
+      // The first chunk's loads were issued behind the wait for this matrix's earlier phases, so that what those wrote
+      // is visible once they are here: the diagonal's value of this row and, by lane, of the chunk's columns.
+      if (!(ok = wait_bar_warp(&sm.epi_full[e], ph))) break;
       float* da = args.diag_a + (int64_t)q.g * args.n;
       float* dg = args.diag + (int64_t)q.g * args.n;
-      float tl = kA;
-      if (!sym && q.step + 2 >= args.steps) {  // t: the largest of P's diagonal
-        if (of != q.step * args.G + q.g) {
-          top = -INFINITY;
-          for (int k = lane; k < args.n; k += 32) top = fmaxf(top, __ldcg(dg + k));
-#pragma unroll
-          for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-          of = q.step * args.G + q.g;
-        }
-        tl += top;
-      }
-      // the diagonal's value of this row, and of this lane's column of the coming chunk
       const bool by_row = role == POLY || (!sym && !args.tall), by_col = role == POLY || (!sym && args.tall);
       const float* dsrc = role == POLY ? da : dg;
       const float dr = by_row && row < q.M ? __ldcg(dsrc + row) : 0.f;
-      int col = q.n0 + 32 * half + lane;
+      const float drow = role == POLY ? fmaf(kC, dr, kB) : kA + dr;
+      int col = q.n0 + cc + (lane & 15);
       float dnext = by_col && col < q.N ? __ldcg(dsrc + col) : 0.f;
+      const int late = q.step + 2 - args.steps;  // 0 and 1 in the last two steps
+      uint32_t* top = args.top + (late > 0 ? args.G : 0) + q.g;
+      const float tl = !sym && late >= 0 ? kA + from_ordered(__ldcg(top)) : kA;
       if (!(ok = wait_bar_warp(&sm.acc_full[ab], (i >> 1) & 1))) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
       for (int c = 0; c < kTile && q.n0 + c < q.N; c += kChunk) {
-        const float dcol = dnext;
+        const float dcol = role == POLY ? kC * dnext : dnext;
         col += kChunk;
         dnext = by_col && c + kChunk < kTile && col < q.N ? __ldcg(dsrc + col) : 0.f;
-        if (!(ok = wait_bar_warp(&sm.epi_full[e], ph))) break;
-        uint8_t* mine = sm.e[e][0] + r * 128;  // 16-byte piece j of the row stands at j ^ (r & 7)
-        uint8_t* other = sm.e[e][1] + r * 128;
-#pragma unroll 1
-        for (int jj = 0; jj < 2; ++jj) {
-          const int cc = 32 * half + 16 * jj;  // the columns cc .. cc + 15 of the chunk
-          float v[16];
-          tmem_ld16(tmem + (uint32_t)(ab * kTile + c + cc) + lanes, v);
-          const int dd = row - (q.n0 + c + cc);  // the diagonal's place among them
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int at = ((cc / 8 + j) ^ (r & 7)) * 16;
-            float f[8];
+        if (c > 0 && !(ok = wait_bar_warp(&sm.epi_full[e], ph))) break;
+        const uint32_t mine = epi_base + (uint32_t)e * (2 * kOpBytes), other = mine + kOpBytes;
+        float v[16];
+        tmem_ld16(tmem + (uint32_t)(ab * kTile + c + cc) + lanes, v);
+        const int dd = row - (q.n0 + c + cc);  // the diagonal's place among the columns
+        auto eight = [&](auto J, uint32_t piece) {  // columns 8 J .. 8 J + 7 of the 16
+          constexpr int j = decltype(J)::value;
+          float f[8];
+          if (sym) {
             if (role == GRAM) {
 #pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                f[k] = v[8 * j + k] * kUnscale;
-                if (dd == 8 * j + k) {
-                  if (row < q.M) da[row] = v[8 * j + k] * kUnscale2;
-                  f[k] = 0.f;
-                }
-              }
-            } else if (role == POLY) {  // with D = diag dA and O the rest of A: A A = O O + D O + O D + D D
-              unpack8(*reinterpret_cast<const uint4*>(mine + at), f);
+              for (int k = 0; k < 8; ++k) f[k] = v[8 * j + k] * kUnscale;
+            } else {  // with D = diag dA and O the rest of A: A A = O O + D O + O D + D D
+              unpack8(lds16(mine + piece), f);
 #pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const float acc = v[8 * j + k], dc = __shfl_sync(~0u, dcol, 16 * jj + 8 * j + k);
-                f[k] = fmaf(kB, f[k], kC * fmaf(dr + dc, f[k], kUnscale * acc));
-                if (dd == 8 * j + k) {
-                  if (row < q.M) dg[row] = fmaf(kB, dr, kC * fmaf(dr, dr, acc * kUnscale2));
-                  f[k] = 0.f;
-                }
-              }
-            } else {
-              float lo[8];
-              unpack8(*reinterpret_cast<const uint4*>(mine + at), f);
-              unpack8(*reinterpret_cast<const uint4*>(other + at), lo);
+              for (int k = 0; k < 8; ++k)
+                f[k] = fmaf(drow + __shfl_sync(~0u, dcol, 8 * j + k), f[k], kC * kUnscale * v[8 * j + k]);
+            }
+            if (on_diag && __any_sync(~0u, (dd >> 3) == j)) {
+              float acc = 0.f;
 #pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const float d = by_col ? __shfl_sync(~0u, dcol, 16 * jj + 8 * j + k) : dr;
-                f[k] = fmaf(kA + d, f[k], fmaf(tl, lo[k], kUnscale * v[8 * j + k]));
+              for (int k = 0; k < 8; ++k) {  // (sums and selects: an index into the registers would put them in memory)
+                acc += dd == 8 * j + k ? v[8 * j + k] : 0.f;
+                f[k] = dd == 8 * j + k ? 0.f : f[k];
+              }
+              if ((dd >> 3) == j && row < q.M) {
+                const float d = role == GRAM ? acc * kUnscale2 : fmaf(kB, dr, kC * fmaf(dr, dr, acc * kUnscale2));
+                (role == GRAM ? da : dg)[row] = d;
+                if (role == POLY && late >= 0) atomicMax(top, to_ordered(d));
               }
             }
-            if (role == LAST) {
+          } else {
+            float lo[8];
+            unpack8(lds16(mine + piece), f);
+            unpack8(lds16(other + piece), lo);
 #pragma unroll
-              for (int k = 0; k < 8; ++k) f[k] *= kUnscale;
-              *reinterpret_cast<uint4*>(mine + at) = pack8_bf16(f);
-            } else {
-              const uint4 w = pack8(f);
-              *reinterpret_cast<uint4*>(mine + at) = w;
-              if (role == NEXT) {
-                float hi[8];
-                unpack8(w, hi);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) hi[k] = f[k] - hi[k];
-                *reinterpret_cast<uint4*>(other + at) = pack8(hi);
-              } else if (mirror) {
-                // the transpose: row cc + .. of a box of 64 values of r
-                uint8_t* box = sm.e[e][1] + (r >> 6) * (kOpBytes / 2) + (cc + 8 * j) * 128 + (r & 7) * 2;
-                const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int k = 0; k < 8; ++k)  // row 8 j + k of the box: its number's low bits are k
-                  *reinterpret_cast<uint16_t*>(box + k * 128 + ((((r & 63) >> 3) ^ k) * 16)) =
-                      (uint16_t)(k & 1 ? words[k / 2] >> 16 : words[k / 2]);
-              }
+            for (int k = 0; k < 8; ++k) {
+              const float d = by_col ? kA + __shfl_sync(~0u, dcol, 8 * j + k) : drow;
+              f[k] = fmaf(d, f[k], fmaf(tl, lo[k], kUnscale * v[8 * j + k]));
             }
           }
-        }
+          if (role == LAST) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] *= kUnscale;
+            sts16(mine + piece, pack8_bf16(f));
+          } else {
+            const uint4 w = pack8(f);
+            sts16(mine + piece, w);
+            if (role == NEXT) {
+              float hi[8];
+              unpack8(w, hi);
+#pragma unroll
+              for (int k = 0; k < 8; ++k) hi[k] = f[k] - hi[k];
+              sts16(other + piece, pack8(hi));
+            } else if (!on_diag) {
+              // the transpose: rows cc + .. of a box of 64 values of r; the low bits of a row's number are k
+              const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
+                sts2(other + ((flip ^ (k << 4)) + (8 * j + k) * 128), k & 1 ? words[k / 2] >> 16 : words[k / 2]);
+            }
+          }
+        };
+        eight(std::integral_constant<int, 0>{}, piece0);
+        eight(std::integral_constant<int, 1>{}, piece1);
         if (role == LAST && !args.o_tma) {
-          // o's rows are not on 16-byte boundaries: this warp's 32 rows of 32 columns, a row at a time
+          // o's rows are not on 16-byte boundaries: this warp's 32 rows of 16 columns, two rows at a time
           __syncwarp();
-          uint16_t* o = args.o + (int64_t)q.g * args.o_gs + q.n0 + c + 32 * half + lane;
-          const int rows = min(32, q.M - (m0 + quarter * 32));
-          const int piece = half * 4 + (lane >> 3);
-          if (q.n0 + c + 32 * half + lane < q.N)
+          const int oc = cc + (lane & 15), x = q.n0 + c + oc;
+          uint16_t* o = args.o + (int64_t)q.g * args.o_gs + x;
+          if (x < q.N)
 #pragma unroll 4
-            for (int k = 0; k < rows; ++k) {
+            for (int k = lane >> 4; k < 32; k += 2) {
               const int rr = quarter * 32 + k;
-              o[(int64_t)(m0 + rr) * args.cols] =
-                  *reinterpret_cast<const uint16_t*>(sm.e[e][0] + rr * 128 + ((piece ^ (rr & 7)) * 16) + (lane & 7) * 2);
+              if (m0 + rr < q.M)
+                o[(int64_t)(m0 + rr) * args.cols] =
+                    *reinterpret_cast<const uint16_t*>(sm.e[e][0] + rr * 128 + (((oc >> 3) ^ (rr & 7)) * 16) + (oc & 7) * 2);
             }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -876,7 +901,7 @@ DirLayout direction_layout(int G, int64_t rows, int64_t cols) {
   d.per = (int)(std::max<int64_t>(4096, (elems + 255) / 256) + 7) / 8 * 8;
   d.chunks = (int)((elems + d.per - 1) / d.per);
   d.part = take(12 * (size_t)G * d.chunks);
-  d.done = take(4 * (size_t)G);
+  d.done = take(12 * (size_t)G);
   d.bytes = at;
   return d;
 }
@@ -950,7 +975,7 @@ cudaError_t run_direction(DirArgs d, const DirLayout& ly, uint8_t* ws, int steps
   const int64_t x_gs = (int64_t)d.rows * ly.ldx, a_gs = (int64_t)n * ly.lda;
   a.G = d.G, a.n = n, a.rows = d.rows, a.cols = d.cols, a.steps = steps, a.tall = d.rows > d.cols;
   a.diag_a = reinterpret_cast<float*>(ws + ly.diag_a), a.diag = reinterpret_cast<float*>(ws + ly.diag);
-  a.done = d.done, a.o = d.o, a.o_gs = d.o_gs;
+  a.done = d.done, a.top = d.done + d.G, a.o = d.o, a.o_gs = d.o_gs;
   a.o_tma = !off_align(d.o, 16) && d.cols % 8 == 0 && d.o_gs % 8 == 0;
   const CUtensorMapDataType f16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
   bool ok = true;
