@@ -441,8 +441,8 @@ lsgd_status lsgd_batchnorm_stats_noalloc(const float* y, int64_t P, int C, int G
  * of fp16 values: o is within 1.5e-3 (relative 2-norm) of exact arithmetic before its rounding to bf16, for rank-
  * deficient matrices too.  Deterministic.  Sizes up to 32768 a side, steps 1 to 100, G <= 65535.
  *
- * `workspace`: device memory of at least lsgd_orthogonal_workspace's bytes, 256-byte aligned, whose
- * contents do not matter before or after; calls (or captured graphs) that may run at the same time
+ * `workspace`: device memory of at least lsgd_orthogonal_workspace's bytes (0: it is not used and may be
+ * NULL; a smaller side up to 128 with a larger one up to 4096), 256-byte aligned, whose contents do not matter before or after; calls (or captured graphs) that may run at the same time
  * need one each.  No allocation: the calls may be captured into a CUDA graph.  LSGD_EINVAL for bad
  * arguments, too small a workspace and tensors that overlap.  Device pointers, asynchronous on `stream`, which
  * belongs to the current device; lsgd_device_status reports a device-side wait that ran out. */

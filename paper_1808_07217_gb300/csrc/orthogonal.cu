@@ -819,6 +819,385 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
 }
 
 // ------------------------------------------------------------------------------------------------
+// Resident form: a matrix of a smaller side n <= 128 in the shared memory of one CTA or a cluster, all of it in one launch
+//
+// X is held with its longer side down, [m][n], a CTA of the cluster having up to 512 of the m rows and a thread one row.
+// A row is 128 fp16 values, two swizzled pieces of 64: up to n = 64 h and l, above it h alone (l in its thread's
+// registers).  A step:
+//   1. tcgen05: [h l]^T [h l] over the CTA's rows into tensor memory, 128 x 128; above 64 that is A, up to 64 A is the sum
+//      of its parts h h, h l and l h;
+//   2. the CTAs' sums are added up in rank order (each CTA a slice of A, through distributed shared memory) and the
+//      slices given to all;
+//   3. tcgen05: A A, then P in A's place;
+//   4. tcgen05: X P, 128 rows to a tile; each thread updates its row from its tile.
+// Up to n = 64 both h and l are multiplied, so that small matrices, whose roundings do not average out, are off by less
+// than 2.5e-3 too.  What a step costs is its chain of latencies (about 5 us at 100 x 4096 in eight CTAs), which the work
+// in it hardly lengthens.
+
+constexpr int kRows = 512;       // rows of a CTA
+constexpr int kResSide = 128;
+constexpr int kPiece = 128;      // bytes of a piece's row
+
+struct ResArgs {
+  DirArgs d;
+  int n, m, cl, per, steps;  // per: rows of a CTA
+};
+
+// Shared memory, from a 1024-byte boundary: X's two pieces [2][rows][64], A and P [NP / 64][128][64], the sums [128][128] in
+// fp32, then ResTail.
+struct ResTail {
+  float da[kResSide], d[kResSide];
+  double norm[3];
+  float red[3][kRows / 32];
+  uint64_t bar[5];  // the symmetric products, and each tile of X P
+  uint32_t tmem;
+};
+template <int NP>
+constexpr size_t res_smem(int rows) {
+  return 1024 + (size_t)rows * 2 * kPiece + (NP / 64) * 128 * kPiece + 128 * 128 * 4 + sizeof(ResTail);
+}
+
+__device__ __forceinline__ void mma_one(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void commit_one(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ uint4 lds16_at(uint32_t cluster_addr) {
+  uint4 v;
+  asm volatile("ld.shared::cluster.v4.b32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "r"(cluster_addr)
+               : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t at_rank(uint32_t addr, int rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+
+template <int NP>
+__global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResArgs a) {
+  constexpr bool kBoth = NP == 64;  // l is in shared memory and multiplied too
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023) & ~1023u;
+  const int rows = blockDim.x, warps = rows >> 5;
+  const uint32_t xs = base, xpiece = (uint32_t)rows * kPiece;                  // X: piece p at xs + p xpiece
+  const uint32_t as = xs + 2 * xpiece;                                         // A, P: piece p at as + p 128 kPiece
+  const uint32_t sums = as + (NP / 64) * 128 * kPiece;
+  const uint32_t tail_at = sums + 128 * 128 * 4;
+  ResTail& tail = *reinterpret_cast<ResTail*>(smem_raw + (tail_at - smem_u32(smem_raw)));
+  const int warp = uniform_warp(), lane = threadIdx.x & 31, tid = threadIdx.x;
+  const int rank = a.cl > 1 ? (int)cta_rank() : 0;
+  const int64_t k = blockIdx.x / a.cl;
+  const int n = a.n, m0 = rank * a.per, have = max(0, min(a.per, a.m - m0));  // this CTA's rows
+  const bool tall = a.d.rows > a.d.cols;
+  const int tiles = rows / 128;
+  uint32_t cols = 128;  // of tensor memory
+  while ((int)cols < tiles * NP) cols <<= 1;
+
+  if (tid == 0) {
+    for (int i = 0; i < 5; ++i) mbar_init(&tail.bar[i], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tail.tmem)), "r"(cols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  // rows and columns past the matrix are zero
+  for (uint32_t i = tid * 16; i < 2 * xpiece; i += rows * 16) sts16(xs + i, make_uint4(0, 0, 0, 0));
+  pdl_begin();
+
+  // momentum and the norm: this CTA's values, neighbouring ones by neighbouring threads
+  const DirArgs& d = a.d;
+  const int64_t gk = k * d.g_gs, uk = k * d.u_gs;
+  // the place of value (j, i), row j of this CTA's and column i of X
+  auto place = [&](int j, int i) -> int { return tall ? (m0 + j) * n + i : i * a.m + m0 + j; };
+  {
+    NormSums s{0.f, 0.f, 0.f};
+    auto one = [&](int at) {
+      float g[1];
+      load_grad<1>(d, gk + at, g);
+      float x = g[0];
+      if (d.mom != 0.f) {
+        const float u = fmaf(d.mom, d.u[uk + at], g[0]);
+        d.u[uk + at] = u;
+        x = d.nesterov ? fmaf(d.mom, u, g[0]) : u;
+      }
+      norm_add(s, x);
+    };
+    if (tall) {
+#pragma unroll 4
+      for (int i = tid; i < have * n; i += rows) one(m0 * n + i);
+    } else if (tid < have) {
+#pragma unroll 4
+      for (int i = 0; i < n; ++i) one(i * a.m + m0 + tid);
+    }
+    float v[3] = {s.mid, s.big, s.small};
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {
+#pragma unroll
+      for (int o = 16; o; o >>= 1) v[j] += __shfl_xor_sync(~0u, v[j], o);
+      if (lane == 0) tail.red[j][warp] = v[j];
+    }
+    __syncthreads();
+    if (tid < 3) {
+      double t = 0.0;
+      for (int w = 0; w < warps; ++w) t += tail.red[tid][w];
+      tail.norm[tid] = t;
+    }
+    if (a.cl > 1) pair_sync();
+    else __syncthreads();
+  }
+  const uint32_t tmem = tail.tmem;
+  const uint32_t row_at = xs + tid * kPiece, turn = (tid & 7) << 4;  // 16-byte piece p of a row stands at p ^ (row & 7)
+  uint32_t lreg[kBoth ? 1 : NP / 2];
+  {
+    double t[3];
+    for (int j = 0; j < 3; ++j) {
+      t[j] = 0.0;
+      for (int c = 0; c < a.cl; ++c) {
+        double v;
+        asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(at_rank(smem_u32(&tail.norm[j]), c)) : "memory");
+        t[j] += v;
+      }
+    }
+    const float2 f = norm_factors(t[0], t[1], t[2]);
+#pragma unroll
+    for (int q = 0; q < NP / 8; ++q) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[i] = 0.f;
+        if (tid < have && 8 * q + i < n) {
+          const int at = place(tid, 8 * q + i);
+          float g[1] = {0.f};
+          if (d.mom == 0.f) {
+            load_grad<1>(d, gk + at, g);
+            x[i] = g[0];
+          } else {
+            x[i] = d.u[uk + at];
+            if (d.nesterov) {
+              load_grad<1>(d, gk + at, g);
+              x[i] = fmaf(d.mom, x[i], g[0]);
+            }
+          }
+          x[i] = x[i] * f.x * f.y;
+        }
+      }
+      const uint4 w = pack8(x);
+      float hi[8];
+      unpack8(w, hi);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) hi[i] = x[i] - hi[i];
+      const uint4 lo = pack8(hi);
+      if constexpr (kBoth) {
+        sts16(row_at + ((q << 4) ^ turn), w);
+        sts16(row_at + xpiece + ((q << 4) ^ turn), lo);
+      } else {
+        sts16(row_at + (q >> 3) * xpiece + (((q & 7) << 4) ^ turn), w);
+        lreg[4 * q] = lo.x, lreg[4 * q + 1] = lo.y, lreg[4 * q + 2] = lo.z, lreg[4 * q + 3] = lo.w;
+      }
+    }
+  }
+
+  uint32_t ph = 0, ph2 = 0;
+  const uint32_t quarter = (uint32_t)(warp & 3) * 32, lanes = quarter << 16;
+  const int r128 = (int)quarter + lane, groups = warps / 4;  // this thread's row of the symmetric products
+  const int ks = (have + 15) / 16, kn = (n + 15) / 16;
+  for (int step = 0; step < a.steps; ++step) {
+    // 1. [h l]^T [h l]
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 0) {
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const bool el = elect_one();
+      // M = N = 128, both operands with the sum running down the rows
+      constexpr uint32_t idesc = (1u << 4) | (1u << 15) | (1u << 16) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+      const uint64_t x0 = smem_desc(xs, xpiece, 1024);
+      for (int i = 0; i < max(ks, 1); ++i)
+        if (el) mma_one(tmem, x0 + i * (2048 >> 4), x0 + i * (2048 >> 4), idesc, i > 0);
+      if (el) commit_one(&tail.bar[0]);
+    }
+    wait_bar_warp(&tail.bar[0], ph);
+    ph ^= 1;
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    // row r128 of the sums; 16-byte piece p of a row stands at p ^ (row & 31)
+    for (int c = (warp >> 2) * 16; c < 128; c += groups * 16) {
+      float v[16];
+      tmem_ld16(tmem + c + lanes, v);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        sts16(sums + r128 * 512 + (((c / 4 + j) ^ lane) << 4),
+              make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]),
+                         __float_as_uint(v[4 * j + 3])));
+    }
+    if (a.cl > 1) pair_sync();
+    else __syncthreads();
+    // 2. this CTA's slice of A: rows rank, rank + cl, ...; four columns to a thread
+    {
+      const int per_row = NP / 4, mine = (NP - rank + a.cl - 1) / a.cl;
+      for (int e = tid; e < mine * per_row; e += rows) {
+        const int i = rank + e / per_row * a.cl, j = e % per_row;
+        float f[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int c = 0; c < a.cl; ++c) {
+          const uint32_t from = a.cl > 1 ? at_rank(sums, c) : sums;
+          auto add = [&](int row, int piece) {
+            const uint4 w = lds16_at(from + row * 512 + ((piece ^ (row & 31)) << 4));
+            f[0] += __uint_as_float(w.x), f[1] += __uint_as_float(w.y);
+            f[2] += __uint_as_float(w.z), f[3] += __uint_as_float(w.w);
+          };
+          add(i, j);
+          if constexpr (kBoth) add(i, 16 + j), add(64 + i, j);
+        }
+        float diag = 0.f;
+        bool on = false;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (4 * j + q == i) diag = f[q] * kUnscale2, on = true;
+          f[q] = 4 * j + q == i ? 0.f : f[q] * kUnscale;
+        }
+        const __half2 w0 = __floats2half2_rn(f[0], f[1]), w1 = __floats2half2_rn(f[2], f[3]);
+        const uint32_t to = as + (j >> 4) * (128 * kPiece) + i * kPiece + (((j & 15) >> 1) << 4 ^ (i & 7) << 4) + (j & 1) * 8;
+        for (int c = 0; c < a.cl; ++c) {
+          const uint32_t there = a.cl > 1 ? at_rank(to, c) : to;
+          asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(there),
+                       "r"(*reinterpret_cast<const uint32_t*>(&w0)), "r"(*reinterpret_cast<const uint32_t*>(&w1))
+                       : "memory");
+          if (on) {
+            const uint32_t da = smem_u32(&tail.da[i]);
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(a.cl > 1 ? at_rank(da, c) : da), "f"(diag) : "memory");
+          }
+        }
+      }
+    }
+    if (a.cl > 1) pair_sync();
+    // 3. A A, and P in A's place
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 0) {
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const bool el = elect_one();
+      constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(NP >> 3) << 17) | ((128u >> 4) << 24);
+      const uint64_t a0 = smem_desc(as, 16, 1024);
+      for (int i = 0; i < kn; ++i) {
+        const uint64_t at = a0 + (i >> 2) * (128 * kPiece >> 4) + (i & 3) * 2;
+        if (el) mma_one(tmem, at, at, idesc, i > 0);
+      }
+      if (el) commit_one(&tail.bar[0]);
+    }
+    wait_bar_warp(&tail.bar[0], ph);
+    ph ^= 1;
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (r128 < NP || NP == 128) {
+      const float di = tail.da[r128 < NP ? r128 : 0];
+      for (int c = (warp >> 2) * 16; c < NP; c += groups * 16) {
+        float v[16];
+        tmem_ld16(tmem + c + lanes, v);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t at = as + (c >> 6) * (128 * kPiece) + r128 * kPiece + ((((c & 63) / 8 + j) << 4) ^ ((r128 & 7) << 4));
+          float f[8];
+          unpack8(lds16(at), f);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float dj = tail.da[c + 8 * j + i];
+            const bool on = c + 8 * j + i == r128;
+            const float acc = v[8 * j + i];
+            f[i] = fmaf(fmaf(kC, di + dj, kB), f[i], kC * kUnscale * acc);
+            if (on) {
+              tail.d[r128] = fmaf(kB, di, kC * fmaf(di, di, acc * kUnscale2));
+              f[i] = 0.f;
+            }
+          }
+          sts16(at, pack8(f));
+        }
+      }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    // 4. X P
+    if (warp == 0) {
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const bool el = elect_one();
+      constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(NP >> 3) << 17) | ((128u >> 4) << 24);
+      const uint64_t x0 = smem_desc(xs, 16, 1024), p0 = smem_desc(as, 16, 1024);
+      for (int t = 0; t < tiles; ++t) {
+        for (int p = 0; p < (kBoth ? 2 : 1); ++p)
+          for (int i = 0; i < kn; ++i) {
+            const int piece = kBoth ? p : i >> 2;
+            const uint64_t xa = x0 + (uint32_t)((piece * rows + t * 128) * kPiece >> 4) + (i & 3) * 2;
+            const uint64_t pb = p0 + (i >> 2) * (128 * kPiece >> 4) + (i & 3) * 2;
+            if (el) mma_one(tmem + t * NP, xa, pb, idesc, p > 0 || i > 0);
+          }
+        if (el) commit_one(&tail.bar[1 + t]);
+      }
+    }
+    float top = 0.f;  // t of the number formats above
+    if (!kBoth && step + 2 >= a.steps) {
+      top = -INFINITY;
+      for (int i = lane; i < n; i += 32) top = fmaxf(top, tail.d[i]);
+#pragma unroll
+      for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+    }
+    wait_bar_warp(&tail.bar[1 + (warp >> 2)], ph2);
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const bool last = step + 1 == a.steps;
+#pragma unroll
+    for (int c = 0; c < NP; c += 16) {
+      if (c < n) {
+        float v[16];
+        tmem_ld16(tmem + (warp >> 2) * NP + c + lanes, v);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int q = c / 8 + j;
+          const uint32_t at = row_at + (kBoth ? 0 : (q >> 3) * xpiece) + (((q & 7) << 4) ^ turn);
+          float f[8], lo[8];
+          unpack8(lds16(at), f);
+          if constexpr (kBoth) unpack8(lds16(at + xpiece), lo);
+          else unpack8(make_uint4(lreg[4 * q], lreg[4 * q + 1], lreg[4 * q + 2], lreg[4 * q + 3]), lo);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float dj = kA + tail.d[8 * q + i];
+            f[i] = fmaf(dj, f[i], fmaf(kBoth ? dj : kA + top, lo[i], kUnscale * v[8 * j + i]));
+          }
+          if (!last) {
+            const uint4 w = pack8(f);
+            sts16(at, w);
+            float hi[8];
+            unpack8(w, hi);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) hi[i] = f[i] - hi[i];
+            const uint4 l = pack8(hi);
+            if constexpr (kBoth) sts16(at + xpiece, l);
+            else lreg[4 * q] = l.x, lreg[4 * q + 1] = l.y, lreg[4 * q + 2] = l.z, lreg[4 * q + 3] = l.w;
+          } else if (tid < have) {
+            uint16_t* o = d.o + k * d.o_gs;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (8 * q + i < n) o[place(tid, 8 * q + i)] = f2bf(f[i] * kUnscale);
+          }
+        }
+      }
+    }
+    ph2 ^= 1;
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (a.cl > 1) pair_sync();  // no CTA leaves while another may read its sums
+  if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
+}
+
+// ------------------------------------------------------------------------------------------------
 // w = (1 - lr wd) w - lr scale o, and its bf16 copy
 
 constexpr int kUpdThreads = 256;
@@ -882,8 +1261,10 @@ struct DirLayout {
   int chunks, per;
   size_t h[2], l[2], A, P, diag_a, diag, part, done, bytes;
 };
+int resident_ctas(int64_t rows, int64_t cols);
 DirLayout direction_layout(int G, int64_t rows, int64_t cols) {
   DirLayout d{};
+  if (resident_ctas(rows, cols)) return d;  // no workspace
   d.n = std::min(rows, cols);
   d.ldx = pad16(cols), d.lda = pad16(d.n);
   size_t at = 0;
@@ -962,6 +1343,49 @@ int resident_pairs(int dev, size_t smem, cudaError_t* err) {
   return pairs;
 }
 
+// CTAs per matrix of the resident form (a power of two up to 8, the portable cluster size), or 0: it does not fit.
+int resident_ctas(int64_t rows, int64_t cols) {
+  const int64_t n = std::min(rows, cols), m = std::max(rows, cols);
+  if (n > kResSide) return 0;
+  for (int cl = 1; cl <= 8; cl *= 2)
+    if ((m + cl - 1) / cl <= kRows) return cl;
+  return 0;
+}
+
+template <int NP>
+cudaError_t launch_resident(const ResArgs& a, cudaStream_t st) {
+  static std::atomic<int> raised{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (raised != dev + 1) {
+    e = cudaFuncSetAttribute(direction_resident_kernel<NP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)res_smem<NP>(kRows));
+    if (e != cudaSuccess) return e;
+    raised = dev + 1;
+  }
+  const int threads = (a.per + 127) / 128 * 128;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(a.d.G * a.cl));
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = res_smem<NP>(threads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = a.cl, attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr, cfg.numAttrs = a.cl > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, direction_resident_kernel<NP>, a);
+}
+
+cudaError_t run_resident(const DirArgs& d, int cl, int steps, cudaStream_t st) {
+  ResArgs a{};
+  a.d = d, a.cl = cl, a.steps = steps;
+  a.n = std::min(d.rows, d.cols), a.m = std::max(d.rows, d.cols);
+  a.per = (a.m + cl - 1) / cl;
+  return a.n <= 64 ? launch_resident<64>(a, st) : launch_resident<128>(a, st);
+}
+
 cudaError_t run_direction(DirArgs d, const DirLayout& ly, uint8_t* ws, int steps, cudaStream_t st) {
   std::call_once(g_encode_once, load_encode);
   if (!g_encode) return cudaErrorNotSupported;
@@ -988,8 +1412,6 @@ cudaError_t run_direction(DirArgs d, const DirLayout& ly, uint8_t* ws, int steps
   if (a.o_tma)
     ok = ok && half_map(&a.om, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, d.o, d.cols, d.rows, d.cols, d.o_gs, d.G, kHalf);
   if (!ok) return cudaErrorInvalidValue;
-  const int64_t ts = (n + kTile - 1) / kTile, tx = (int64_t)((d.rows + kTile - 1) / kTile) * ((d.cols + kTile - 1) / kTile);
-  if (d.G * (ts * (ts + 1) + tx) * steps > 0x3fffffff) return cudaErrorInvalidValue;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
@@ -1069,18 +1491,22 @@ lsgd_status lsgd_orthogonal_direction(float* u, int64_t u_gs, const void* g, int
   else if (steps < 1 || steps > 100) bad = "steps must be 1 to 100";
   else if (G > 1 && (g_gs < n || o_gs < n || (momentum != 0.f && u_gs < n))) bad = "a matrix stride is below rows * cols";
   else if (off_align(u, 4) || off_align(g, gb ? 2 : 4) || off_align(o, 2)) bad = "a pointer is not aligned to its element";
-  else if (!workspace || workspace_bytes < ly.bytes || off_align(workspace, 256))
+  else if (ly.bytes && (!workspace || workspace_bytes < ly.bytes || off_align(workspace, 256)))
     bad = "workspace NULL, not 256-byte aligned or smaller than lsgd_orthogonal_workspace says";
   else if (overlap(g, span_g, o, span_o) || overlap(workspace, ly.bytes, g, span_g) || overlap(workspace, ly.bytes, o, span_o) ||
            (momentum != 0.f && (overlap(u, span_u, g, span_g) || overlap(u, span_u, o, span_o) ||
                                 overlap(workspace, ly.bytes, u, span_u))))
     bad = "tensors overlap";
+  const int64_t ts = (ly.n + kTile - 1) / kTile, tx = ((rows + kTile - 1) / kTile) * ((cols + kTile - 1) / kTile);
+  if (!bad && G * (ts * (ts + 1) + tx) * steps > 0x3fffffff) bad = "too many matrices of this size in one call";
   if (bad) return dir_error(LSGD_EINVAL, fn, bad);
   DirArgs d{};
   d.u = u, d.g = g, d.o = o, d.u_gs = u_gs, d.g_gs = g_gs, d.o_gs = o_gs;
   d.g_bf16 = gb, d.nesterov = nesterov != 0, d.mom = momentum;
   d.G = G, d.rows = (int)rows, d.cols = (int)cols;
-  const cudaError_t e = run_direction(d, ly, static_cast<uint8_t*>(workspace), steps, (cudaStream_t)stream);
+  const int cl = resident_ctas(rows, cols);
+  const cudaError_t e = cl ? run_resident(d, cl, steps, (cudaStream_t)stream)
+                           : run_direction(d, ly, static_cast<uint8_t*>(workspace), steps, (cudaStream_t)stream);
   if (e == cudaErrorNotSupported) return dir_error(LSGD_EUNSUPPORTED, fn, "no tensor maps (cuTensorMapEncodeTiled)");
   return e == cudaSuccess ? LSGD_OK : dir_error(LSGD_ECUDA, fn, cudaGetErrorString(e));
 }

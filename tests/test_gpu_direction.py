@@ -295,11 +295,12 @@ def _lib():
     return L
 
 
+_LARGE = dict(rows=200, cols=300, u_gs=60000, g_gs=60000, o_gs=60000)  # sizes that use a workspace
 _BAD = [dict(G=0), dict(rows=0), dict(cols=0), dict(G=70000), dict(rows=32769), dict(cols=40000), dict(g=None), dict(o=None), dict(u=None),
         dict(g_type=2), dict(momentum=-0.1), dict(momentum=float("nan")), dict(momentum=float("inf")), dict(steps=0), dict(steps=101),
         dict(u_gs=10), dict(g_gs=10), dict(o_gs=10), dict(u_gs=-1 << 20), dict(u=(1 << 30) + 2), dict(g=(2 << 30) + 1), dict(o=(3 << 30) + 1),
-        dict(ws=None), dict(wn=100), dict(ws=(4 << 30) + 16), dict(o=2 << 30), dict(u=2 << 30), dict(u=3 << 30), dict(ws=1 << 30),
-        dict(ws=2 << 30), dict(ws=3 << 30)]
+        dict(ws=None, **_LARGE), dict(wn=100, **_LARGE), dict(ws=(4 << 30) + 16, **_LARGE), dict(o=2 << 30), dict(u=2 << 30), dict(u=3 << 30), dict(ws=1 << 30, **_LARGE),
+        dict(ws=2 << 30, **_LARGE), dict(ws=3 << 30, **_LARGE)]
 
 
 @pytest.mark.parametrize("kw", _BAD)
@@ -329,7 +330,7 @@ def test_workspace_refuses_and_grows():
         with pytest.raises(L.LsgdError) as e:
             L.lsgd_orthogonal_workspace(*bad)
         assert e.value.status == L.EINVAL
-    assert 0 < L.lsgd_orthogonal_workspace(1, 300, 300) < L.lsgd_orthogonal_workspace(2, 300, 300)
+    assert L.lsgd_orthogonal_workspace(9, 4096, 128) == 0 < L.lsgd_orthogonal_workspace(1, 300, 300) < L.lsgd_orthogonal_workspace(2, 300, 300)
 
 
 @pytest.mark.gpu
