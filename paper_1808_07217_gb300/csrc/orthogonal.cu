@@ -61,25 +61,12 @@ __device__ __forceinline__ void norm_add(NormSums& s, float x) {
   s.small = fmaf(t, t, s.small);
 }
 
-// kScale / ||x|| as two factors (each in range; applied one after the other), from the sums over the matrix.
-// ||x|| = 0 gives 0: the direction of a zero matrix is zero.
-__device__ __forceinline__ float2 norm_factors(double mid, double big, double small) {
-  double sq;
-  int e2 = 0;  // ||x||^2 = sq 2^e2
-  if (mid > 0x1p-60 && mid < 1e37) {
-    sq = mid;
-  } else if (mid >= 1e37 || mid != mid) {
-    sq = big, e2 = 160;
-  } else {
-    sq = small, e2 = -168;
-  }
-  if (sq == 0.0) return make_float2(0.f, 0.f);
-  const double norm = sqrt(sq);  // times 2^(e2 / 2)
-  int e = 0;
-  double f = 1.0 / norm;  // 0 or NaN where a value is infinite or NaN
-  if (f > 0.0) f = frexp(f, &e);
-  e += 12 - e2 / 2;
-  return make_float2((float)ldexp(f, e / 2), (float)ldexp(1.0, e - e / 2));
+// 2^12 / ||x|| as two factors, applied one after the other without leaving the range of fp32, from the sums over the
+// matrix.  ||x|| = 0 gives 0: the direction of a zero matrix is zero.  (fp32 sums: an error of the norm scales X by 1 + 1e-6.)
+__device__ __forceinline__ float2 norm_factors(float mid, float big, float small) {
+  if (mid > 0x1p-60f && mid < 0x1p120f) return make_float2(__frsqrt_rn(mid), 4096.f);
+  if (!(mid < 0x1p120f)) return make_float2(__frsqrt_rn(big), 0x1p-68f);  // also infinite and NaN values: 0 or NaN times them
+  return small == 0.f ? make_float2(0.f, 0.f) : make_float2(__frsqrt_rn(small), 0x1p96f);
 }
 
 struct DirArgs {
@@ -189,7 +176,7 @@ __global__ void __launch_bounds__(kMomThreads) direction_normalise_kernel(const 
   const int64_t k = blockIdx.y;
   __shared__ float2 factors;
   if (threadIdx.x < 32) {
-    double t[3] = {0, 0, 0};
+    float t[3] = {0.f, 0.f, 0.f};
     for (int c = threadIdx.x; c < a.chunks; c += 32)
       for (int j = 0; j < 3; ++j) t[j] += a.part[(k * a.chunks + c) * 3 + j];
     for (int j = 0; j < 3; ++j)
@@ -847,7 +834,7 @@ struct ResArgs {
 // fp32, then ResTail.
 struct ResTail {
   float da[kResSide], d[kResSide];
-  double norm[3];
+  float norm[3];
   float red[3][kRows / 32];
   uint64_t bar[5];  // the symmetric products, and each tile of X P
   uint32_t tmem;
@@ -912,6 +899,7 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
   }
   // rows and columns past the matrix are zero
   for (uint32_t i = tid * 16; i < 2 * xpiece; i += rows * 16) sts16(xs + i, make_uint4(0, 0, 0, 0));
+  __syncthreads();
   pdl_begin();
 
   // momentum and the norm: this CTA's values, neighbouring ones by neighbouring threads
@@ -919,26 +907,47 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
   const int64_t gk = k * d.g_gs, uk = k * d.u_gs;
   // the place of value (j, i), row j of this CTA's and column i of X
   auto place = [&](int j, int i) -> int { return tall ? (m0 + j) * n + i : i * a.m + m0 + j; };
+  const uint32_t row_at = xs + tid * kPiece, turn = (tid & 7) << 4;  // 16-byte piece p of a row stands at p ^ (row & 7)
   {
     NormSums s{0.f, 0.f, 0.f};
-    auto one = [&](int at) {
-      float g[1];
-      load_grad<1>(d, gk + at, g);
-      float x = g[0];
-      if (d.mom != 0.f) {
-        const float u = fmaf(d.mom, d.u[uk + at], g[0]);
-        d.u[uk + at] = u;
-        x = d.nesterov ? fmaf(d.mom, u, g[0]) : u;
+    // value (j, i) of up to n = 64 waits for the norm in row j, 64 fp32 values to a row's two pieces
+    auto keep = [&](int j, int i, float x) {
+      if constexpr (kBoth) {
+        const uint32_t at = xs + (i >> 5) * xpiece + j * kPiece + ((((i & 31) >> 2) ^ (j & 7)) << 4) + (i & 3) * 4;
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory");
       }
-      norm_add(s, x);
     };
-    if (tall) {
-#pragma unroll 4
-      for (int i = tid; i < have * n; i += rows) one(m0 * n + i);
-    } else if (tid < have) {
-#pragma unroll 4
-      for (int i = 0; i < n; ++i) one(i * a.m + m0 + tid);
-    }
+    // eight values at a time, their loads before the first store
+    constexpr int kAt = 8;
+    auto some = [&](auto value, int from, int step, int end, auto where) {
+      for (int b = from; b < end; b += kAt * step) {
+        float g[kAt][1], u[kAt];
+#pragma unroll
+        for (int q = 0; q < kAt; ++q) {
+          g[q][0] = u[q] = 0.f;
+          if (b + q * step < end) {
+            load_grad<1>(d, gk + value(b + q * step), g[q]);
+            if (d.mom != 0.f) u[q] = d.u[uk + value(b + q * step)];
+          }
+        }
+#pragma unroll
+        for (int q = 0; q < kAt; ++q)
+          if (b + q * step < end) {
+            float x = g[q][0];
+            if (d.mom != 0.f) {
+              const float t = fmaf(d.mom, u[q], x);
+              d.u[uk + value(b + q * step)] = t;
+              x = d.nesterov ? fmaf(d.mom, t, x) : t;
+            }
+            norm_add(s, x);
+            where(b + q * step, x);
+          }
+      }
+    };
+    if (tall)
+      some([&](int e) { return m0 * n + e; }, tid, rows, have * n, [&](int e, float x) { keep(e / n, e % n, x); });
+    else if (tid < have)
+      some([&](int i) { return i * a.m + m0 + tid; }, 0, 1, n, [&](int i, float x) { keep(tid, i, x); });
     float v[3] = {s.mid, s.big, s.small};
 #pragma unroll
     for (int j = 0; j < 3; ++j) {
@@ -948,7 +957,7 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
     }
     __syncthreads();
     if (tid < 3) {
-      double t = 0.0;
+      float t = 0.f;
       for (int w = 0; w < warps; ++w) t += tail.red[tid][w];
       tail.norm[tid] = t;
     }
@@ -956,53 +965,87 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
     else __syncthreads();
   }
   const uint32_t tmem = tail.tmem;
-  const uint32_t row_at = xs + tid * kPiece, turn = (tid & 7) << 4;  // 16-byte piece p of a row stands at p ^ (row & 7)
+  const uint32_t stage = sums + warp * 4096;  // 32 x 32 fp32 values of a warp, where the sums are not in use
   uint32_t lreg[kBoth ? 1 : NP / 2];
   {
-    double t[3];
-    for (int j = 0; j < 3; ++j) {
-      t[j] = 0.0;
-      for (int c = 0; c < a.cl; ++c) {
-        double v;
-        asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(at_rank(smem_u32(&tail.norm[j]), c)) : "memory");
+    float t[3] = {0.f, 0.f, 0.f};
+    for (int c = 0; c < a.cl; ++c)
+#pragma unroll
+      for (int j = 0; j < 3; ++j) {
+        float v;
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at_rank(smem_u32(&tail.norm[j]), c)) : "memory");
         t[j] += v;
       }
-    }
     const float2 f = norm_factors(t[0], t[1], t[2]);
+    if constexpr (kBoth) {
+      uint4 raw[16];
 #pragma unroll
-    for (int q = 0; q < NP / 8; ++q) {
-      float x[8];
+      for (int q = 0; q < 16; ++q) raw[q] = lds16(row_at + (q >> 3) * xpiece + (((q & 7) << 4) ^ turn));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[i] = 0.f;
-        if (tid < have && 8 * q + i < n) {
-          const int at = place(tid, 8 * q + i);
-          float g[1] = {0.f};
-          if (d.mom == 0.f) {
-            load_grad<1>(d, gk + at, g);
-            x[i] = g[0];
-          } else {
-            x[i] = d.u[uk + at];
-            if (d.nesterov) {
-              load_grad<1>(d, gk + at, g);
-              x[i] = fmaf(d.mom, x[i], g[0]);
-            }
-          }
-          x[i] = x[i] * f.x * f.y;
-        }
+      for (int q = 0; q < 8; ++q) {
+        const uint4 r0 = raw[2 * q], r1 = raw[2 * q + 1];
+        const uint32_t w[8] = {r0.x, r0.y, r0.z, r0.w, r1.x, r1.y, r1.z, r1.w};
+        float x[8], hi[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]) * f.x * f.y;
+        const uint4 h = pack8(x);
+        unpack8(h, hi);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) hi[i] = x[i] - hi[i];
+        sts16(row_at + ((q << 4) ^ turn), h);
+        sts16(row_at + xpiece + ((q << 4) ^ turn), pack8(hi));
       }
-      const uint4 w = pack8(x);
-      float hi[8];
-      unpack8(w, hi);
+    } else {  // once more from L2, a row's values 32 at a time
 #pragma unroll
-      for (int i = 0; i < 8; ++i) hi[i] = x[i] - hi[i];
-      const uint4 lo = pack8(hi);
-      if constexpr (kBoth) {
-        sts16(row_at + ((q << 4) ^ turn), w);
-        sts16(row_at + xpiece + ((q << 4) ^ turn), lo);
-      } else {
-        sts16(row_at + (q >> 3) * xpiece + (((q & 7) << 4) ^ turn), w);
-        lreg[4 * q] = lo.x, lreg[4 * q + 1] = lo.y, lreg[4 * q + 2] = lo.z, lreg[4 * q + 3] = lo.w;
+      for (int b = 0; b < NP; b += 32) {
+        float x[32];
+        auto batch = [&](auto at, auto use) {  // 16 values' loads before they are used
+#pragma unroll
+          for (int half = 0; half < 32; half += 16) {
+            float g[16][1], u[16];
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+              const int v = at(half + q);
+              g[q][0] = u[q] = 0.f;
+              if (v >= 0 && (d.mom == 0.f || d.nesterov)) load_grad<1>(d, gk + v, g[q]);
+              if (v >= 0 && d.mom != 0.f) u[q] = d.u[uk + v];
+            }
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+              use(half + q, (d.mom == 0.f ? g[q][0] : d.nesterov ? fmaf(d.mom, u[q], g[q][0]) : u[q]) * f.x * f.y);
+          }
+        };
+        if (!tall) {
+          batch([&](int q) { return tid < have && b + q < n ? (b + q) * a.m + m0 + tid : -1; }, [&](int q, float v) {
+#pragma unroll
+            for (int w = 0; w < 32; ++w)
+              if (w == q) x[w] = v;
+          });
+        } else {  // neighbouring lanes read neighbouring values; the warp's 32 x 32 values change places
+          __syncwarp();
+          batch([&](int q) { return warp * 32 + q < have && b + lane < n ? (m0 + warp * 32 + q) * n + b + lane : -1; },
+                [&](int q, float v) {
+                  asm volatile("st.shared.f32 [%0], %1;" ::"r"(stage + q * 128 + ((lane ^ q) << 2)), "f"(v) : "memory");
+                });
+          __syncwarp();
+#pragma unroll
+          for (int q = 0; q < 32; ++q)
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[q]) : "r"(stage + lane * 128 + ((lane ^ q) << 2)) : "memory");
+        }
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const int q = b / 8 + p;
+          float v[8], hi[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = x[8 * p + i];
+          const uint4 w = pack8(v);
+          unpack8(w, hi);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) hi[i] = v[i] - hi[i];
+          const uint4 lo = pack8(hi);
+          sts16(row_at + (q >> 3) * xpiece + (((q & 7) << 4) ^ turn), w);
+          lreg[4 * q] = lo.x, lreg[4 * q + 1] = lo.y, lreg[4 * q + 2] = lo.z, lreg[4 * q + 3] = lo.w;
+        }
       }
     }
   }
@@ -1010,7 +1053,7 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
   uint32_t ph = 0, ph2 = 0;
   const uint32_t quarter = (uint32_t)(warp & 3) * 32, lanes = quarter << 16;
   const int r128 = (int)quarter + lane, groups = warps / 4;  // this thread's row of the symmetric products
-  const int ks = (have + 15) / 16, kn = (n + 15) / 16;
+  const int ks = (have + 15) / 16, kn = (n + 15) / 16, n16 = kn * 16;  // rows and columns from n16 on are not computed
   for (int step = 0; step < a.steps; ++step) {
     // 1. [h l]^T [h l]
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -1030,7 +1073,8 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
     ph ^= 1;
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     // row r128 of the sums; 16-byte piece p of a row stands at p ^ (row & 31)
-    for (int c = (warp >> 2) * 16; c < 128; c += groups * 16) {
+    for (int c = (warp >> 2) * 16; c < 128 && ((int)quarter & (NP - 1)) < n16; c += groups * 16) {
+      if ((c & (NP - 1)) >= n16) continue;
       float v[16];
       tmem_ld16(tmem + c + lanes, v);
 #pragma unroll
@@ -1043,20 +1087,29 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
     else __syncthreads();
     // 2. this CTA's slice of A: rows rank, rank + cl, ...; four columns to a thread
     {
-      const int per_row = NP / 4, mine = (NP - rank + a.cl - 1) / a.cl;
+      const int per_row = n16 / 4, mine = (n16 - rank + a.cl - 1) / a.cl;
       for (int e = tid; e < mine * per_row; e += rows) {
         const int i = rank + e / per_row * a.cl, j = e % per_row;
         float f[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int c = 0; c < a.cl; ++c) {
-          const uint32_t from = a.cl > 1 ? at_rank(sums, c) : sums;
-          auto add = [&](int row, int piece) {
-            const uint4 w = lds16_at(from + row * 512 + ((piece ^ (row & 31)) << 4));
-            f[0] += __uint_as_float(w.x), f[1] += __uint_as_float(w.y);
-            f[2] += __uint_as_float(w.z), f[3] += __uint_as_float(w.w);
-          };
-          add(i, j);
-          if constexpr (kBoth) add(i, 16 + j), add(64 + i, j);
-        }
+        constexpr int kParts = kBoth ? 3 : 1;
+        uint4 w[8][kParts];  // every CTA's parts, loaded before the first is used
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+          if (c < a.cl) {
+            const uint32_t from = a.cl > 1 ? at_rank(sums, c) : sums;
+            auto part = [&](int row, int piece) { return lds16_at(from + row * 512 + ((piece ^ (row & 31)) << 4)); };
+            w[c][0] = part(i, j);
+            if constexpr (kBoth) w[c][1] = part(i, 16 + j), w[c][2] = part(64 + i, j);
+          }
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+          if (c < a.cl) {
+#pragma unroll
+            for (int q = 0; q < kParts; ++q) {
+              f[0] += __uint_as_float(w[c][q].x), f[1] += __uint_as_float(w[c][q].y);
+              f[2] += __uint_as_float(w[c][q].z), f[3] += __uint_as_float(w[c][q].w);
+            }
+          }
         float diag = 0.f;
         bool on = false;
 #pragma unroll
@@ -1097,9 +1150,9 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
     wait_bar_warp(&tail.bar[0], ph);
     ph ^= 1;
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    if (r128 < NP || NP == 128) {
-      const float di = tail.da[r128 < NP ? r128 : 0];
-      for (int c = (warp >> 2) * 16; c < NP; c += groups * 16) {
+    if ((int)quarter < n16) {
+      const float di = r128 < n16 ? tail.da[r128] : 0.f;
+      for (int c = (warp >> 2) * 16; c < n16; c += groups * 16) {
         float v[16];
         tmem_ld16(tmem + c + lanes, v);
 #pragma unroll
@@ -1113,7 +1166,7 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
             const bool on = c + 8 * j + i == r128;
             const float acc = v[8 * j + i];
             f[i] = fmaf(fmaf(kC, di + dj, kB), f[i], kC * kUnscale * acc);
-            if (on) {
+            if (on) {  // (r128 < n16 there)
               tail.d[r128] = fmaf(kB, di, kC * fmaf(di, di, acc * kUnscale2));
               f[i] = 0.f;
             }
@@ -1180,12 +1233,31 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
             const uint4 l = pack8(hi);
             if constexpr (kBoth) sts16(at + xpiece, l);
             else lreg[4 * q] = l.x, lreg[4 * q + 1] = l.y, lreg[4 * q + 2] = l.z, lreg[4 * q + 3] = l.w;
-          } else if (tid < have) {
+          } else if (!tall) {
             uint16_t* o = d.o + k * d.o_gs;
+            if (tid < have)
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (8 * q + i < n) o[place(tid, 8 * q + i)] = f2bf(f[i] * kUnscale);
+              for (int i = 0; i < 8; ++i)
+                if (8 * q + i < n) o[place(tid, 8 * q + i)] = f2bf(f[i] * kUnscale);
+          } else {  // 16 columns of the warp's rows, to be written row by row
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] *= kUnscale;
+            sts16(stage + lane * 32 + ((j ^ (lane >> 2 & 1)) << 4), pack8_bf16(f));
           }
+        }
+        if (last && tall) {
+          __syncwarp();
+          uint16_t* o = d.o + k * d.o_gs + (int64_t)(m0 + warp * 32) * n + c + (lane & 15);
+          const int i = lane & 15;
+          if (c + i < n)
+#pragma unroll 4
+            for (int rr = lane >> 4; rr < 32; rr += 2)
+              if (warp * 32 + rr < have) {
+                uint16_t v;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(stage + rr * 32 + (((i >> 3) ^ (rr >> 2 & 1)) << 4) + (i & 7) * 2) : "memory");
+                o[rr * n] = v;
+              }
+          __syncwarp();
         }
       }
     }
