@@ -832,7 +832,7 @@ struct ResArgs {
 
 // Shared memory, from a 1024-byte boundary: X's two pieces [2][rows][64], A and P [NP / 64][128][64], the sums [128][128] in
 // fp32, then ResTail.
-struct ResTail {
+struct __align__(16) ResTail {
   float da[kResSide], d[kResSide];
   float norm[3];
   float red[3][kRows / 32];
@@ -866,6 +866,12 @@ __device__ __forceinline__ uint32_t at_rank(uint32_t addr, int rank) {
   uint32_t r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
   return r;
+}
+
+__device__ __forceinline__ void vec8(uint32_t at, float (&f)[8]) {
+  const uint4 a = lds16(at), b = lds16(at + 16);
+  f[0] = __uint_as_float(a.x), f[1] = __uint_as_float(a.y), f[2] = __uint_as_float(a.z), f[3] = __uint_as_float(a.w);
+  f[4] = __uint_as_float(b.x), f[5] = __uint_as_float(b.y), f[6] = __uint_as_float(b.z), f[7] = __uint_as_float(b.w);
 }
 
 template <int NP>
@@ -917,8 +923,8 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory");
       }
     };
-    // eight values at a time, their loads before the first store
-    constexpr int kAt = 8;
+    // 16 values at a time, their loads before the first store
+    constexpr int kAt = 16;
     auto some = [&](auto value, int from, int step, int end, auto where) {
       for (int b = from; b < end; b += kAt * step) {
         float g[kAt][1], u[kAt];
@@ -1087,49 +1093,58 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
     else __syncthreads();
     // 2. this CTA's slice of A: rows rank, rank + cl, ...; four columns to a thread
     {
-      const int per_row = n16 / 4, mine = (n16 - rank + a.cl - 1) / a.cl;
-      for (int e = tid; e < mine * per_row; e += rows) {
-        const int i = rank + e / per_row * a.cl, j = e % per_row;
-        float f[4] = {0.f, 0.f, 0.f, 0.f};
-        constexpr int kParts = kBoth ? 3 : 1;
-        uint4 w[8][kParts];  // every CTA's parts, loaded before the first is used
+      auto slice = [&](auto one) {
+        constexpr bool kOne = decltype(one)::value;
+        const int per_row = n16 / 4, mine = kOne ? n16 : (n16 - rank + a.cl - 1) / a.cl;
+        for (int e = tid; e < mine * per_row; e += rows) {
+          const int i = kOne ? e / per_row : rank + e / per_row * a.cl, j = e % per_row;
+          float f[4] = {0.f, 0.f, 0.f, 0.f};
+          constexpr int kParts = kBoth ? 3 : 1, kCtas = kOne ? 1 : 8;
+          uint4 w[kCtas][kParts];  // every CTA's parts, loaded before the first is used
 #pragma unroll
-        for (int c = 0; c < 8; ++c)
-          if (c < a.cl) {
-            const uint32_t from = a.cl > 1 ? at_rank(sums, c) : sums;
-            auto part = [&](int row, int piece) { return lds16_at(from + row * 512 + ((piece ^ (row & 31)) << 4)); };
-            w[c][0] = part(i, j);
-            if constexpr (kBoth) w[c][1] = part(i, 16 + j), w[c][2] = part(64 + i, j);
+          for (int c = 0; c < kCtas; ++c)
+            if (kOne || c < a.cl) {
+              const uint32_t from = kOne ? sums : at_rank(sums, c);
+              auto part = [&](int row, int piece) {
+                const uint32_t at = from + row * 512 + ((piece ^ (row & 31)) << 4);
+                return kOne ? lds16(at) : lds16_at(at);
+              };
+              w[c][0] = part(i, j);
+              if constexpr (kBoth) w[c][1] = part(i, 16 + j), w[c][2] = part(64 + i, j);
+            }
+#pragma unroll
+          for (int c = 0; c < kCtas; ++c)
+            if (kOne || c < a.cl) {
+#pragma unroll
+              for (int q = 0; q < kParts; ++q) {
+                f[0] += __uint_as_float(w[c][q].x), f[1] += __uint_as_float(w[c][q].y);
+                f[2] += __uint_as_float(w[c][q].z), f[3] += __uint_as_float(w[c][q].w);
+              }
+            }
+          float diag = 0.f;
+          const bool on = j == i >> 2;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            diag += 4 * j + q == i ? f[q] * kUnscale2 : 0.f;
+            f[q] = 4 * j + q == i ? 0.f : f[q] * kUnscale;
           }
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-          if (c < a.cl) {
-#pragma unroll
-            for (int q = 0; q < kParts; ++q) {
-              f[0] += __uint_as_float(w[c][q].x), f[1] += __uint_as_float(w[c][q].y);
-              f[2] += __uint_as_float(w[c][q].z), f[3] += __uint_as_float(w[c][q].w);
+          const __half2 w0 = __floats2half2_rn(f[0], f[1]), w1 = __floats2half2_rn(f[2], f[3]);
+          const uint32_t b0 = *reinterpret_cast<const uint32_t*>(&w0), b1 = *reinterpret_cast<const uint32_t*>(&w1);
+          const uint32_t to = as + (j >> 4) * (128 * kPiece) + i * kPiece + ((((j & 15) >> 1) << 4) ^ ((i & 7) << 4)) + (j & 1) * 8;
+          const uint32_t da = smem_u32(&tail.da[i]);
+          if constexpr (kOne) {
+            asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(b0), "r"(b1) : "memory");
+            if (on) tail.da[i] = diag;
+          } else {
+            for (int c = 0; c < a.cl; ++c) {
+              asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(at_rank(to, c)), "r"(b0), "r"(b1) : "memory");
+              if (on) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at_rank(da, c)), "f"(diag) : "memory");
             }
           }
-        float diag = 0.f;
-        bool on = false;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          if (4 * j + q == i) diag = f[q] * kUnscale2, on = true;
-          f[q] = 4 * j + q == i ? 0.f : f[q] * kUnscale;
         }
-        const __half2 w0 = __floats2half2_rn(f[0], f[1]), w1 = __floats2half2_rn(f[2], f[3]);
-        const uint32_t to = as + (j >> 4) * (128 * kPiece) + i * kPiece + (((j & 15) >> 1) << 4 ^ (i & 7) << 4) + (j & 1) * 8;
-        for (int c = 0; c < a.cl; ++c) {
-          const uint32_t there = a.cl > 1 ? at_rank(to, c) : to;
-          asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(there),
-                       "r"(*reinterpret_cast<const uint32_t*>(&w0)), "r"(*reinterpret_cast<const uint32_t*>(&w1))
-                       : "memory");
-          if (on) {
-            const uint32_t da = smem_u32(&tail.da[i]);
-            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(a.cl > 1 ? at_rank(da, c) : da), "f"(diag) : "memory");
-          }
-        }
-      }
+      };
+      if (a.cl == 1) slice(std::true_type{});
+      else slice(std::false_type{});
     }
     if (a.cl > 1) pair_sync();
     // 3. A A, and P in A's place
@@ -1153,26 +1168,23 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
     if ((int)quarter < n16) {
       const float di = r128 < n16 ? tail.da[r128] : 0.f;
       for (int c = (warp >> 2) * 16; c < n16; c += groups * 16) {
-        float v[16];
+        float v[16], mine = 0.f;
         tmem_ld16(tmem + c + lanes, v);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const uint32_t at = as + (c >> 6) * (128 * kPiece) + r128 * kPiece + ((((c & 63) / 8 + j) << 4) ^ ((r128 & 7) << 4));
-          float f[8];
+          float f[8], dj[8];
           unpack8(lds16(at), f);
+          vec8(smem_u32(tail.da) + (c + 8 * j) * 4, dj);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const float dj = tail.da[c + 8 * j + i];
-            const bool on = c + 8 * j + i == r128;
-            const float acc = v[8 * j + i];
-            f[i] = fmaf(fmaf(kC, di + dj, kB), f[i], kC * kUnscale * acc);
-            if (on) {  // (r128 < n16 there)
-              tail.d[r128] = fmaf(kB, di, kC * fmaf(di, di, acc * kUnscale2));
-              f[i] = 0.f;
-            }
+            f[i] = fmaf(fmaf(kC, di + dj[i], kB), f[i], kC * kUnscale * v[8 * j + i]);
+            mine += c + 8 * j + i == r128 ? v[8 * j + i] : 0.f;
+            f[i] = c + 8 * j + i == r128 ? 0.f : f[i];
           }
           sts16(at, pack8(f));
         }
+        if (c == (r128 & ~15)) tail.d[r128] = fmaf(kB, di, kC * fmaf(di, di, mine * kUnscale2));
       }
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -1185,13 +1197,14 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
       constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(NP >> 3) << 17) | ((128u >> 4) << 24);
       const uint64_t x0 = smem_desc(xs, 16, 1024), p0 = smem_desc(as, 16, 1024);
       for (int t = 0; t < tiles; ++t) {
-        for (int p = 0; p < (kBoth ? 2 : 1); ++p)
-          for (int i = 0; i < kn; ++i) {
-            const int piece = kBoth ? p : i >> 2;
-            const uint64_t xa = x0 + (uint32_t)((piece * rows + t * 128) * kPiece >> 4) + (i & 3) * 2;
-            const uint64_t pb = p0 + (i >> 2) * (128 * kPiece >> 4) + (i & 3) * 2;
-            if (el) mma_one(tmem + t * NP, xa, pb, idesc, p > 0 || i > 0);
-          }
+        const uint64_t xt = x0 + (uint32_t)(t * 128 * kPiece >> 4);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {  // up to n = 64 the h, then the l of four slices of 16 columns; else eight of h
+          const int slice = kBoth ? i & 3 : i;
+          const uint64_t xa = xt + (i >> 2) * (xpiece >> 4) + (i & 3) * 2;
+          const uint64_t pb = p0 + (kBoth ? 0 : (i >> 2) * (128 * kPiece >> 4)) + (i & 3) * 2;
+          if (el && slice < kn) mma_one(tmem + t * NP, xa, pb, idesc, i > 0);
+        }
         if (el) commit_one(&tail.bar[1 + t]);
       }
     }
@@ -1205,7 +1218,8 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
     wait_bar_warp(&tail.bar[1 + (warp >> 2)], ph2);
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const bool last = step + 1 == a.steps;
-#pragma unroll
+    // (rolled where nothing is held in registers across it: the instruction cache holds a step then)
+#pragma unroll(kBoth ? 1 : NP / 16)
     for (int c = 0; c < NP; c += 16) {
       if (c < n) {
         float v[16];
@@ -1214,14 +1228,15 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
         for (int j = 0; j < 2; ++j) {
           const int q = c / 8 + j;
           const uint32_t at = row_at + (kBoth ? 0 : (q >> 3) * xpiece) + (((q & 7) << 4) ^ turn);
-          float f[8], lo[8];
+          float f[8], lo[8], dj[8];
           unpack8(lds16(at), f);
+          vec8(smem_u32(tail.d) + 32 * q, dj);
           if constexpr (kBoth) unpack8(lds16(at + xpiece), lo);
           else unpack8(make_uint4(lreg[4 * q], lreg[4 * q + 1], lreg[4 * q + 2], lreg[4 * q + 3]), lo);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const float dj = kA + tail.d[8 * q + i];
-            f[i] = fmaf(dj, f[i], fmaf(kBoth ? dj : kA + top, lo[i], kUnscale * v[8 * j + i]));
+            const float t = kA + dj[i];
+            f[i] = kBoth ? fmaf(t, f[i] + lo[i], kUnscale * v[8 * j + i]) : fmaf(t, f[i], fmaf(kA + top, lo[i], kUnscale * v[8 * j + i]));
           }
           if (!last) {
             const uint4 w = pack8(f);
