@@ -94,6 +94,10 @@ struct Vec {
 #pragma unroll
     for (int i = 0; i < kN; ++i) reinterpret_cast<Raw*>(p)[i] = r[i];
   }
+  __device__ __forceinline__ void stream(T* p) const {  // leaves L2 to what will be read again
+#pragma unroll
+    for (int i = 0; i < kN; ++i) __stcs(reinterpret_cast<Raw*>(p) + i, r[i]);
+  }
 };
 
 struct GnArgs {
@@ -111,7 +115,7 @@ struct GnArgs {
   int rows;       // positions of a range
   int64_t N;
   float eps;
-  int cl, tx_n, ty_n, sub;  // resident form: CTAs per image, threads across and down, channels summed in a thread
+  int cl, sub;    // resident form: CTAs per image; channels summed in a thread
 };
 
 // 1 / (1 + exp(-z)): the exponential's overflow gives 0.
@@ -134,6 +138,15 @@ __device__ __forceinline__ float activate(float z, int act) {
 
 constexpr int kSplitThreads = 256;
 
+// (count, mean, M2) <- merged with (nb, mb, qb)
+__device__ __forceinline__ void chan(float& n, float& m, float& q, float nb, float mb, float qb) {
+  if (nb == 0.f) return;
+  const float t = n + nb, w = nb / t, d = mb - m;
+  m = fmaf(d, w, m);
+  q += fmaf(d * d, n * w, qb);
+  n = t;
+}
+
 // Per range and channel: forward (mean, sum of squared deviations), backward (sum dz, sum dz xh).
 template <typename XT, typename YT, int V, bool BWD>
 __global__ void __launch_bounds__(kSplitThreads) gn_partial_kernel(const GnArgs a, int tx_n, int ty_n) {
@@ -141,89 +154,119 @@ __global__ void __launch_bounds__(kSplitThreads) gn_partial_kernel(const GnArgs 
   const int tx = threadIdx.x % tx_n, ty = threadIdx.x / tx_n;
   const int c0 = (blockIdx.y * tx_n + tx) * V;
   const bool on = ty < ty_n && c0 < a.C;
-  const int64_t n = blockIdx.x / a.S;
-  const int s = blockIdx.x % a.S;
+  const int n = blockIdx.x / a.S, s = blockIdx.x % a.S;
   const int p0 = s * a.rows, p1 = min(a.P, p0 + a.rows);
-  constexpr int U = 4;
   float s0[V], s1[V];
   float cnt = 0.f;
 #pragma unroll
   for (int j = 0; j < V; ++j) s0[j] = s1[j] = 0.f;
   if (on) {
-    const int64_t base = n * a.P * (int64_t)a.C + c0;
+    const int64_t base = (int64_t)n * a.P * a.C + c0;
     const XT* x = static_cast<const XT*>(a.x) + base;
+    const int64_t step = (int64_t)ty_n * a.C;
     if constexpr (!BWD) {
-      // batches of U positions: their mean and squared deviations, merged by Chan et al.'s formula
+      // Segments of at most 64 positions: sums of the deviations from the first U values' mean, and of their squares,
+      // merged into the running moments by Chan et al.'s formula.  The pivot is far from the segment's mean only if
+      // one of its U values is, and then that value's square in the sums bounds what the difference loses.
+      constexpr int U = 8;
       int p = p0 + ty;
-      for (; p + (U - 1) * ty_n < p1; p += U * ty_n) {
-        Vec<XT, V> r[U];
+      const XT* at = x + (int64_t)p * a.C;
+      while (p < p1) {
+        const int k = min(64, (p1 - p + ty_n - 1) / ty_n);  // positions of the segment
+        float pivot[V], d0[V], d1[V];
 #pragma unroll
-        for (int i = 0; i < U; ++i) r[i].load(x + (int64_t)(p + i * ty_n) * a.C);
-        float v[U][V];
+        for (int j = 0; j < V; ++j) d0[j] = d1[j] = 0.f;
+        for (int b = 0; b < k; b += U) {
+          Vec<XT, V> r[U];
 #pragma unroll
-        for (int i = 0; i < U; ++i) r[i].floats(v[i]);
-        const float w = U / (cnt + U), cw = cnt * w;
+          for (int i = 0; i < U; ++i)
+            if (b + i < k) r[i].load(at + i * step);
+          if (b == 0) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) pivot[j] = 0.f;
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+              if (i < k) {
+                float v[V];
+                r[i].floats(v);
+#pragma unroll
+                for (int j = 0; j < V; ++j) pivot[j] += v[j];
+              }
+            const float inv = 1.f / min(k, U);
+#pragma unroll
+            for (int j = 0; j < V; ++j) pivot[j] *= inv;
+          }
+#pragma unroll
+          for (int i = 0; i < U; ++i)
+            if (b + i < k) {
+              float v[V];
+              r[i].floats(v);
+#pragma unroll
+              for (int j = 0; j < V; ++j) {
+                const float d = v[j] - pivot[j];
+                d0[j] += d;
+                d1[j] = fmaf(d, d, d1[j]);
+              }
+            }
+          at += U * step;
+        }
+        p += k * ty_n;
+        at = x + (int64_t)p * a.C;
+        const float kf = (float)k, inv = 1.f / kf, w = kf / (cnt + kf), cw = cnt * w;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          const float m = (v[0][j] + v[1][j] + v[2][j] + v[3][j]) * (1.f / U);
-          float q = 0.f;
-#pragma unroll
-          for (int i = 0; i < U; ++i) q = fmaf(v[i][j] - m, v[i][j] - m, q);
-          const float d = m - s0[j];
+          const float e = d0[j] * inv, d = pivot[j] + e - s0[j];
           s0[j] = fmaf(d, w, s0[j]);
-          s1[j] += fmaf(d * d, cw, q);
+          s1[j] += fmaf(d * d, cw, fmaxf(fmaf(-e, d0[j], d1[j]), 0.f) + (d1[j] != d1[j] ? d1[j] : 0.f));
         }
-        cnt += U;
-      }
-      for (; p < p1; p += ty_n) {
-        Vec<XT, V> r;
-        r.load(x + (int64_t)p * a.C);
-        float v[V];
-        r.floats(v);
-        const float w = 1.f / (cnt + 1.f), cw = cnt * w;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const float d = v[j] - s0[j];
-          s0[j] = fmaf(d, w, s0[j]);
-          s1[j] = fmaf(d * d, cw, s1[j]);
-        }
-        cnt += 1.f;
+        cnt += kf;
       }
     } else {
       const YT* dy = static_cast<const YT*>(a.dy) + base;
       const YT* y = static_cast<const YT*>(a.y) + base;
+      const bool relu = a.act == LSGD_ACT_RELU, silu = a.act == LSGD_ACT_SILU;
       float ga[V], be[V], mu[V], rs[V];
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const int64_t pc = (n / a.B) * a.par_gs + c0 + j;
+        const int64_t pc = (int64_t)(n / a.B) * a.par_gs + c0 + j;
+        const int64_t pg = (int64_t)n * a.groups + (c0 + j) / a.D;
         ga[j] = a.gamma[pc];
         be[j] = a.beta[pc];
-        mu[j] = a.mean[n * a.groups + (c0 + j) / a.D];
-        rs[j] = a.rstd[n * a.groups + (c0 + j) / a.D];
+        mu[j] = a.mean[pg];
+        rs[j] = a.rstd[pg];
       }
-#pragma unroll 2
-      for (int p = p0 + ty; p < p1; p += ty_n) {
-        Vec<XT, V> rx;
-        Vec<YT, V> rd, ry;
-        rx.load(x + (int64_t)p * a.C);
-        rd.load(dy + (int64_t)p * a.C);
-        if (a.act == LSGD_ACT_RELU) ry.load(y + (int64_t)p * a.C);
-        float xv[V], dv[V], yv[V];
-        rx.floats(xv);
-        rd.floats(dv);
-        if (a.act == LSGD_ACT_RELU) ry.floats(yv);
+      constexpr int U = V >= 8 ? 2 : 4;
+      for (int p = p0 + ty; p < p1; p += U * ty_n) {
+        Vec<XT, V> rx[U];
+        Vec<YT, V> rd[U], ry[U];
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const float xh = (xv[j] - mu[j]) * rs[j];
-          float dz = dv[j];
-          if (a.act == LSGD_ACT_RELU) dz = yv[j] > 0.f ? dz : 0.f;
-          if (a.act == LSGD_ACT_SILU) {
-            const float z = fmaf(xh, ga[j], be[j]), sg = sigmoid<sizeof(XT) == 4>(z);
-            dz *= sg * fmaf(z, 1.f - sg, 1.f);
+        for (int i = 0; i < U; ++i)
+          if (p + i * ty_n < p1) {
+            const int64_t at = (int64_t)(p + i * ty_n) * a.C;
+            rx[i].load(x + at);
+            rd[i].load(dy + at);
+            if (relu) ry[i].load(y + at);
           }
-          s0[j] += dz;
-          s1[j] = fmaf(dz, xh, s1[j]);
-        }
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+          if (p + i * ty_n < p1) {
+            float xv[V], dv[V], yv[V];
+            rx[i].floats(xv);
+            rd[i].floats(dv);
+            if (relu) ry[i].floats(yv);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+              const float xh = (xv[j] - mu[j]) * rs[j];
+              float dz = dv[j];
+              if (relu) dz = yv[j] > 0.f ? dz : 0.f;
+              if (silu) {
+                const float z = fmaf(xh, ga[j], be[j]), sg = sigmoid<sizeof(XT) == 4>(z);
+                dz *= sg * fmaf(z, 1.f - sg, 1.f);
+              }
+              s0[j] += dz;
+              s1[j] = fmaf(dz, xh, s1[j]);
+            }
+          }
       }
     }
   }
@@ -237,9 +280,11 @@ __global__ void __launch_bounds__(kSplitThreads) gn_partial_kernel(const GnArgs 
   }
   rc[threadIdx.x] = cnt;
   __syncthreads();
-  if (on && ty == 0) {
-    for (int t = 1; t < ty_n; ++t) {
-      const int o = threadIdx.x + t * tx_n;
+  // halves of the rows are merged until one is left
+  for (int half = 1; half < ty_n; half *= 2) {
+    const int other = ty + half;
+    if (on && ty % (2 * half) == 0 && other < ty_n) {
+      const int o = threadIdx.x + half * tx_n;
       const float oc = rc[o];
       const float w = BWD || oc == 0.f ? 0.f : oc / (cnt + oc), cw = cnt * w;
 #pragma unroll
@@ -253,10 +298,16 @@ __global__ void __launch_bounds__(kSplitThreads) gn_partial_kernel(const GnArgs 
           s0[j] = fmaf(d, w, s0[j]);
           s1[j] += fmaf(d * d, cw, b1);
         }
+        red[(threadIdx.x * V + j) * 2] = s0[j];
+        red[(threadIdx.x * V + j) * 2 + 1] = s1[j];
       }
       cnt += oc;
+      rc[threadIdx.x] = cnt;
     }
-    float* out = a.part + ((n * a.S + s) * a.C + c0) * 2;
+    __syncthreads();
+  }
+  if (on && ty == 0) {
+    float* out = a.part + (((int64_t)n * a.S + s) * a.C + c0) * 2;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       out[2 * j] = s0[j];
@@ -265,50 +316,53 @@ __global__ void __launch_bounds__(kSplitThreads) gn_partial_kernel(const GnArgs 
   }
 }
 
-// (count, mean, M2) <- merged with (nb, mb, qb)
-__device__ __forceinline__ void chan(float& n, float& m, float& q, float nb, float mb, float qb) {
-  if (nb == 0.f) return;
-  const float t = n + nb, w = nb / t, d = mb - m;
-  m = fmaf(d, w, m);
-  q += fmaf(d * d, n * w, qb);
-  n = t;
-}
-
-// Forward: a warp per (image, group) merges its ranges' channels into mean and rstd.
+// Forward: a block per (image, group) merges its ranges' channels into mean and rstd.
 __global__ void __launch_bounds__(128) gn_stats_merge_kernel(const GnArgs a) {
   pdl_begin();
-  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (w >= a.N * a.groups) return;
-  const int64_t n = w / a.groups;
-  const int q = (int)(w % a.groups);
+  const int n = blockIdx.x / a.groups, q = blockIdx.x % a.groups;
+  const float2* part = reinterpret_cast<const float2*>(a.part) + (int64_t)n * a.S * a.C + q * a.D;
   float cn = 0.f, cm = 0.f, cq = 0.f;
-  for (int i = lane; i < a.S * a.D; i += 32) {
-    const int s = i / a.D, c = q * a.D + i % a.D;
-    const float2 v = *reinterpret_cast<const float2*>(a.part + ((n * a.S + s) * a.C + c) * 2);
-    chan(cn, cm, cq, (float)(min(a.P, (s + 1) * a.rows) - s * a.rows), v.x, v.y);
+  // range by range where a group has many channels, else 128 / D ranges at a time
+  const int dw = min(a.D, 128), lanes = 128 / dw;
+  const int d0 = threadIdx.x % dw, s0 = threadIdx.x / dw;
+  if (s0 < lanes) {
+    for (int d = d0; d < a.D; d += dw)
+#pragma unroll 4
+      for (int s = s0; s < a.S; s += lanes) {
+        const float2 v = part[(int64_t)s * a.C + d];
+        chan(cn, cm, cq, (float)(min(a.P, (s + 1) * a.rows) - s * a.rows), v.x, v.y);
+      }
   }
+  __shared__ float red[3][4];
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
     const float nb = __shfl_xor_sync(~0u, cn, o), mb = __shfl_xor_sync(~0u, cm, o),
                 qb = __shfl_xor_sync(~0u, cq, o);
     chan(cn, cm, cq, nb, mb, qb);
   }
-  if (lane == 0) {
-    a.mean[w] = cm;
-    a.rstd[w] = __frsqrt_rn(cq / cn + a.eps);
+  if ((threadIdx.x & 31) == 0) {
+    const int w = threadIdx.x >> 5;
+    red[0][w] = cn, red[1][w] = cm, red[2][w] = cq;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 4; ++w) chan(cn, cm, cq, red[0][w], red[1][w], red[2][w]);
+    a.mean[blockIdx.x] = cm;
+    a.rstd[blockIdx.x] = __frsqrt_rn(cq / cn + a.eps);
   }
 }
 
-// Backward: per image, the ranges' channel sums added up, and the groups' m1 and m2.
-__global__ void __launch_bounds__(256) gn_sums_merge_kernel(const GnArgs a) {
+// Backward: per image and `per` groups of it, the ranges' channel sums added up, and the groups' m1 and m2.
+__global__ void __launch_bounds__(256) gn_sums_merge_kernel(const GnArgs a, int per) {
   pdl_begin();
-  const int64_t n = blockIdx.x;
-  float2* sums = reinterpret_cast<float2*>(a.sums) + n * a.C;
-  for (int c = threadIdx.x; c < a.C; c += 256) {
+  const int n = blockIdx.x, q0 = blockIdx.y * per, q1 = min(a.groups, q0 + per);
+  float2* sums = reinterpret_cast<float2*>(a.sums) + (int64_t)n * a.C;
+  const float2* part = reinterpret_cast<const float2*>(a.part) + (int64_t)n * a.S * a.C;
+  for (int c = q0 * a.D + threadIdx.x; c < q1 * a.D; c += 256) {
     float2 t = make_float2(0.f, 0.f);
+#pragma unroll 8
     for (int s = 0; s < a.S; ++s) {
-      const float2 v = reinterpret_cast<const float2*>(a.part)[(n * a.S + s) * a.C + c];
+      const float2 v = part[(int64_t)s * a.C + c];
       t.x += v.x;
       t.y += v.y;
     }
@@ -317,10 +371,11 @@ __global__ void __launch_bounds__(256) gn_sums_merge_kernel(const GnArgs a) {
   __syncthreads();
   const int lane = threadIdx.x & 31;
   const float inv = 1.f / ((float)a.P * (float)a.D);
-  for (int q = threadIdx.x >> 5; q < a.groups; q += 8) {
+  const float* gamma = a.gamma + (int64_t)(n / a.B) * a.par_gs;
+  for (int q = q0 + (threadIdx.x >> 5); q < q1; q += 8) {
     float2 t = make_float2(0.f, 0.f);
     for (int d = lane; d < a.D; d += 32) {
-      const float ga = a.gamma[(n / a.B) * a.par_gs + q * a.D + d];
+      const float ga = gamma[q * a.D + d];
       const float2 v = sums[q * a.D + d];
       t.x = fmaf(ga, v.x, t.x);
       t.y = fmaf(ga, v.y, t.y);
@@ -330,115 +385,141 @@ __global__ void __launch_bounds__(256) gn_sums_merge_kernel(const GnArgs a) {
       t.x += __shfl_xor_sync(~0u, t.x, o);
       t.y += __shfl_xor_sync(~0u, t.y, o);
     }
-    if (lane == 0) reinterpret_cast<float2*>(a.m12)[n * a.groups + q] = make_float2(t.x * inv, t.y * inv);
+    if (lane == 0) reinterpret_cast<float2*>(a.m12)[(int64_t)n * a.groups + q] = make_float2(t.x * inv, t.y * inv);
   }
 }
 
-// The second pass: y or dx from the statistics.
+// The second pass: y or dx from the statistics.  The ranges in the opposite order: the last that the first pass read are
+// still in L2.
 template <typename XT, typename YT, int V, bool BWD>
 __global__ void __launch_bounds__(kSplitThreads) gn_apply_kernel(const GnArgs a, int tx_n, int ty_n) {
   pdl_begin();
   const int tx = threadIdx.x % tx_n, ty = threadIdx.x / tx_n;
   const int c0 = (blockIdx.y * tx_n + tx) * V;
   if (ty >= ty_n || c0 >= a.C) return;
-  const int64_t n = blockIdx.x / a.S;
-  const int p0 = (blockIdx.x % a.S) * a.rows, p1 = min(a.P, p0 + a.rows);
-  const int64_t base = n * a.P * (int64_t)a.C + c0;
+  const int block = gridDim.x - 1 - blockIdx.x, n = block / a.S;
+  const int p0 = (block % a.S) * a.rows, p1 = min(a.P, p0 + a.rows);
+  const int64_t base = (int64_t)n * a.P * a.C + c0;
   const XT* x = static_cast<const XT*>(a.x) + base;
-  float ga[V], be[V], mu[V], rs[V], m1[V], m2[V];
+  const bool relu = a.act == LSGD_ACT_RELU, silu = a.act == LSGD_ACT_SILU;
+  float ga[V], be[V], mu[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const int64_t pc = (n / a.B) * a.par_gs + c0 + j, pg = n * a.groups + (c0 + j) / a.D;
+    const int64_t pc = (int64_t)(n / a.B) * a.par_gs + c0 + j, pg = (int64_t)n * a.groups + (c0 + j) / a.D;
     ga[j] = a.gamma[pc];
     be[j] = a.beta[pc];
     mu[j] = a.mean[pg];
-    rs[j] = a.rstd[pg];
-    if constexpr (BWD) {
-      m1[j] = a.m12[2 * pg];
-      m2[j] = a.m12[2 * pg + 1];
-    }
   }
   if constexpr (!BWD) {
     YT* out = static_cast<YT*>(a.out) + base;
 #pragma unroll
-    for (int j = 0; j < V; ++j) ga[j] *= rs[j];
-#pragma unroll 4
-    for (int p = p0 + ty; p < p1; p += ty_n) {
-      Vec<XT, V> r;
-      r.load(x + (int64_t)p * a.C);
-      float v[V];
-      r.floats(v);
+    for (int j = 0; j < V; ++j) ga[j] *= a.rstd[(int64_t)n * a.groups + (c0 + j) / a.D];
+    constexpr int U = 4;
+    for (int p = p0 + ty; p < p1; p += U * ty_n) {
+      Vec<XT, V> r[U];
 #pragma unroll
-      for (int j = 0; j < V; ++j) v[j] = activate<sizeof(YT) == 4>(fmaf(v[j] - mu[j], ga[j], be[j]), a.act);
-      Vec<YT, V> o;
-      o.set(v);
-      o.store(out + (int64_t)p * a.C);
+      for (int i = 0; i < U; ++i)
+        if (p + i * ty_n < p1) r[i].load(x + (int64_t)(p + i * ty_n) * a.C);
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (p + i * ty_n < p1) {
+          float v[V];
+          r[i].floats(v);
+#pragma unroll
+          for (int j = 0; j < V; ++j) v[j] = activate<sizeof(YT) == 4>(fmaf(v[j] - mu[j], ga[j], be[j]), a.act);
+          Vec<YT, V> o;
+          o.set(v);
+          o.stream(out + (int64_t)(p + i * ty_n) * a.C);
+        }
     }
   } else {
     const YT* dy = static_cast<const YT*>(a.dy) + base;
     const YT* y = static_cast<const YT*>(a.y) + base;
     XT* out = static_cast<XT*>(a.out) + base;
-#pragma unroll 2
-    for (int p = p0 + ty; p < p1; p += ty_n) {
-      Vec<XT, V> rx;
-      Vec<YT, V> rd, ry;
-      rx.load(x + (int64_t)p * a.C);
-      rd.load(dy + (int64_t)p * a.C);
-      if (a.act == LSGD_ACT_RELU) ry.load(y + (int64_t)p * a.C);
-      float xv[V], dv[V], yv[V];
-      rx.floats(xv);
-      rd.floats(dv);
-      if (a.act == LSGD_ACT_RELU) ry.floats(yv);
+    float rs[V], m1[V], m2[V];
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float xh = (xv[j] - mu[j]) * rs[j];
-        float dz = dv[j];
-        if (a.act == LSGD_ACT_RELU) dz = yv[j] > 0.f ? dz : 0.f;
-        if (a.act == LSGD_ACT_SILU) {
-          const float z = fmaf(xh, ga[j], be[j]), sg = sigmoid<sizeof(XT) == 4>(z);
-          dz *= sg * fmaf(z, 1.f - sg, 1.f);
+    for (int j = 0; j < V; ++j) {
+      const int64_t pg = (int64_t)n * a.groups + (c0 + j) / a.D;
+      rs[j] = a.rstd[pg];
+      m1[j] = a.m12[2 * pg] * rs[j];
+      m2[j] = a.m12[2 * pg + 1] * rs[j];
+    }
+    constexpr int U = V >= 8 ? 2 : 4;
+    for (int p = p0 + ty; p < p1; p += U * ty_n) {
+      Vec<XT, V> rx[U];
+      Vec<YT, V> rd[U], ry[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (p + i * ty_n < p1) {
+          const int64_t at = (int64_t)(p + i * ty_n) * a.C;
+          rx[i].load(x + at);
+          rd[i].load(dy + at);
+          if (relu) ry[i].load(y + at);
         }
-        xv[j] = rs[j] * (fmaf(ga[j], dz, -m1[j]) - xh * m2[j]);
-      }
-      Vec<XT, V> o;
-      o.set(xv);
-      o.store(out + (int64_t)p * a.C);
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (p + i * ty_n < p1) {
+          float xv[V], dv[V], yv[V];
+          rx[i].floats(xv);
+          rd[i].floats(dv);
+          if (relu) ry[i].floats(yv);
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            const float xh = (xv[j] - mu[j]) * rs[j];
+            float dz = dv[j];
+            if (relu) dz = yv[j] > 0.f ? dz : 0.f;
+            if (silu) {
+              const float z = fmaf(xh, ga[j], be[j]), sg = sigmoid<sizeof(XT) == 4>(z);
+              dz *= sg * fmaf(z, 1.f - sg, 1.f);
+            }
+            xv[j] = fmaf(ga[j] * rs[j], dz, -m1[j]) - xh * m2[j];
+          }
+          Vec<XT, V> o;
+          o.set(xv);
+          o.stream(out + (int64_t)(p + i * ty_n) * a.C);
+        }
     }
   }
 }
 
 // dgamma and dbeta of worker g: the sums of its `rows` rows of channel pairs (sum dz, sum dz xh), a fixed order.
-__global__ void __launch_bounds__(256) gn_param_grad_kernel(const float2* sums, int64_t rows, int C, int64_t par_gs,
-                                                            float* dgamma, float* dbeta) {
+__global__ void __launch_bounds__(1024) gn_param_grad_kernel(const float2* sums, int64_t rows, int C, int64_t par_gs,
+                                                             float* dgamma, float* dbeta) {
   pdl_begin();
   const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4;
   const int c = blockIdx.x * 16 + cx;
   const int64_t g = blockIdx.y;
   float2 t = make_float2(0.f, 0.f);
   if (c < C) {
-#pragma unroll 4
-    for (int64_t r = ry; r < rows; r += 16) {
+#pragma unroll 8
+    for (int64_t r = ry; r < rows; r += 64) {
       const float2 v = sums[(g * rows + r) * C + c];
       t.x += v.x;
       t.y += v.y;
     }
   }
-  __shared__ float2 red[16][17];
-  red[ry][cx] = t;
+  // two rows of 16 channels to a warp
+  t.x += __shfl_xor_sync(~0u, t.x, 16);
+  t.y += __shfl_xor_sync(~0u, t.y, 16);
+  __shared__ float2 red[32][17];
+  if ((threadIdx.x & 16) == 0) red[threadIdx.x >> 5][cx] = t;
   __syncthreads();
-  if (ry == 0 && c < C) {
-    for (int i = 1; i < 16; ++i) {
-      t.x += red[i][cx].x;
-      t.y += red[i][cx].y;
+  if (threadIdx.x < 512) {  // a warp per channel
+    const int ch = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float2 v = red[lane][ch];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      v.x += __shfl_xor_sync(~0u, v.x, o);
+      v.y += __shfl_xor_sync(~0u, v.y, o);
     }
-    dbeta[g * par_gs + c] = t.x;
-    dgamma[g * par_gs + c] = t.y;
+    const int cc = blockIdx.x * 16 + ch;
+    if (lane == 0 && cc < C) dbeta[g * par_gs + cc] = v.x, dgamma[g * par_gs + cc] = v.y;
   }
 }
 
-// Ranges per image of the split form: enough for four CTAs per SM, of 8192 values at least.
+// Ranges per image of the split form: enough for four CTAs per SM, of 2048 values at least.
 int gn_ranges(int64_t N, int P, int C) {
-  const int64_t by_size = ((int64_t)P * C + 8191) / 8192, by_sms = (4LL * kNumSMs + N - 1) / N;
+  const int64_t by_size = ((int64_t)P * C + 2047) / 2048, by_sms = (4LL * kNumSMs + N - 1) / N;
   const int64_t s = std::max<int64_t>(1, std::min<int64_t>({by_size, by_sms, (int64_t)P, 256}));
   const int64_t rows = (P + s - 1) / s;
   return (int)((P + rows - 1) / rows);
@@ -453,14 +534,16 @@ cudaError_t gn_split(GnArgs a, cudaStream_t st) {
   cudaError_t e = launch_pdl(gn_partial_kernel<XT, YT, V, BWD>, grid, dim3(kSplitThreads), 0, st, a, tx, ty);
   if (e != cudaSuccess) return e;
   if constexpr (BWD) {
-    e = launch_pdl(gn_sums_merge_kernel, dim3((unsigned)a.N), dim3(256), 0, st, a);
+    // about 256 channels to a block
+    const int per = std::max(1, std::min(a.groups, 256 / a.D));
+    e = launch_pdl(gn_sums_merge_kernel, dim3((unsigned)a.N, (a.groups + per - 1) / per), dim3(256), 0, st, a, per);
   } else {
-    e = launch_pdl(gn_stats_merge_kernel, dim3((unsigned)((a.N * a.groups + 3) / 4)), dim3(128), 0, st, a);
+    e = launch_pdl(gn_stats_merge_kernel, dim3((unsigned)(a.N * a.groups)), dim3(128), 0, st, a);
   }
   if (e != cudaSuccess) return e;
   e = launch_pdl(gn_apply_kernel<XT, YT, V, BWD>, grid, dim3(kSplitThreads), 0, st, a, tx, ty);
   if (e != cudaSuccess || !BWD) return e;
-  return launch_pdl(gn_param_grad_kernel, dim3((a.C + 15) / 16, (unsigned)(a.N / a.B)), dim3(256), 0, st,
+  return launch_pdl(gn_param_grad_kernel, dim3((a.C + 15) / 16, (unsigned)(a.N / a.B)), dim3(1024), 0, st,
                     (const float2*)a.sums, (int64_t)a.B, a.C, a.par_gs, a.dgamma, a.dbeta);
 }
 
@@ -484,48 +567,85 @@ __device__ __forceinline__ float peer_float(const float* p, int rank) {
   return v;
 }
 
-// Adds up every thread's V channel values over the block's rows of threads: afterwards red[r][c] for r < the returned
-// number of rows holds partial sums of column c of C / sub, `sub` neighbouring channels to a column.  Where the threads
-// across are a power of two below a warp, the rows of a warp are added by shuffles first.
-template <int V>
-__device__ __forceinline__ int column_sums(float (&v)[V], float* red, int tx, int ty, int tx_n, int ty_n, int sub) {
-  int nv = V;
+// Adds up every thread's values v[0 .. NV) over the block's rows of threads: afterwards red[r][c] for r < the number of
+// rows (a warp's, or every thread row) holds partial sums of column c = tx NV + j.  Where the threads across are a power of
+// two below a warp, the rows of a warp are added first: at each step a lane gives half of its values away and adds up the
+// other half, so that NV values cost about NV exchanges and not NV for every step.
+template <int NV>
+__device__ __forceinline__ void column_sums(float* v, float* red, int tx, int ty, int tx_n, bool shuffled) {
+  const int cols = tx_n * NV;
+  if (!shuffled) {
 #pragma unroll
-  for (int w = V / 2; w >= 1; w >>= 1) {
-    if (nv > V / sub) {
+    for (int j = 0; j < NV; ++j) red[ty * cols + tx * NV + j] = v[j];
+    return;
+  }
+  const int lane = (ty * tx_n + tx) & 31;
+  int first = 0, have = NV;  // this lane's values: first .. first + have - 1
+  bool mine = true;          // of the lanes with the same values one writes
 #pragma unroll
-      for (int j = 0; j < w; ++j) v[j] = v[2 * j] + v[2 * j + 1];
-      nv >>= 1;
+  for (int k = 0; k < 5; ++k) {
+    const int o = 16 >> k;
+    if (o >= tx_n) {
+      const bool up = lane & o;
+      constexpr int kW[5] = {NV / 2, NV / 4, NV / 8, 0, 0};
+      const int w = kW[k];
+      if (w > 0) {
+#pragma unroll
+        for (int j = 0; j < w; ++j) {
+          const float give = up ? v[j] : v[j + w], keep = up ? v[j + w] : v[j];
+          v[j] = keep + __shfl_xor_sync(~0u, give, o);
+        }
+        first += up ? w : 0;
+        have = w;
+      } else {
+        v[0] += __shfl_xor_sync(~0u, v[0], o);
+        mine = mine && !up;
+      }
     }
   }
-  const int cols = tx_n * nv;
-  if (tx_n < 32 && (tx_n & (tx_n - 1)) == 0) {
+  if (mine) {
+    float* to = red + ((ty * tx_n + tx) >> 5) * cols + tx * NV + first;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      if (j < nv)
-        for (int o = 16; o >= tx_n; o >>= 1) v[j] += __shfl_xor_sync(~0u, v[j], o);
-    }
-    if ((threadIdx.x & 31) < tx_n) {
-#pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (j < nv) red[(threadIdx.x >> 5) * cols + tx * nv + j] = v[j];
-    }
-    return blockDim.x >> 5;
+    for (int j = 0; j < NV; ++j)
+      if (j < have) to[j] = v[j];
   }
-  if (ty < ty_n) {
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (j < nv) red[ty * cols + tx * nv + j] = v[j];
-  }
-  return ty_n;
 }
 
-// out[q] = the sum over red's rows and the columns of group q (dn columns each), a warp per group.
-__device__ __forceinline__ void group_sums(const float* red, int rows, int groups, int dn, float* out) {
-  const int lane = threadIdx.x & 31, cols = groups * dn;
-  for (int q = threadIdx.x >> 5; q < groups; q += blockDim.x >> 5) {
+// The same for V channels of which `sub` neighbours are always of one group: those are added first.
+template <int V>
+__device__ __forceinline__ void channel_sums(float (&v)[V], float* red, int tx, int ty, int tx_n, bool shuffled, int sub) {
+  if (V >= 2 && sub >= 2) {
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) v[j] = v[2 * j] + v[2 * j + 1];
+  }
+  if (V >= 4 && sub >= 4) {
+#pragma unroll
+    for (int j = 0; j < V / 4; ++j) v[j] = v[2 * j] + v[2 * j + 1];
+  }
+  if (V >= 8 && sub >= 8) {
+#pragma unroll
+    for (int j = 0; j < V / 8; ++j) v[j] = v[2 * j] + v[2 * j + 1];
+  }
+  const int nv = V / sub;
+  if (nv == 1) column_sums<1>(v, red, tx, ty, tx_n, shuffled);
+  if constexpr (V >= 2)
+    if (nv == 2) column_sums<2>(v, red, tx, ty, tx_n, shuffled);
+  if constexpr (V >= 4)
+    if (nv == 4) column_sums<4>(v, red, tx, ty, tx_n, shuffled);
+  if constexpr (V >= 8)
+    if (nv == 8) column_sums<8>(v, red, tx, ty, tx_n, shuffled);
+}
+
+// out[q] = the sum over red's rows and the columns of group q (dn columns each), a warp per group, the block's full warps.
+__device__ __forceinline__ void group_sums(const float* red, int rows, int groups, int dn, float* out, int tid, int nw) {
+  const int lane = tid & 31, cols = groups * dn;
+  const int wide = min(dn, 32), r0 = lane / wide, d0 = lane - r0 * wide, down = 32 / wide;
+  if (tid >= nw * 32) return;
+  for (int q = tid >> 5; q < groups; q += nw) {
     float t = 0.f;
-    for (int i = lane; i < rows * dn; i += 32) t += red[(i / dn) * cols + q * dn + i % dn];
+    if (r0 < down)
+      for (int r = r0; r < rows; r += down)
+        for (int d = d0; d < dn; d += wide) t += red[r * cols + q * dn + d];
 #pragma unroll
     for (int o = 16; o; o >>= 1) t += __shfl_xor_sync(~0u, t, o);
     if (lane == 0) out[q] = t;
@@ -552,20 +672,22 @@ __global__ void __launch_bounds__(1024, 1) gn_fwd_resident_kernel(const GnArgs a
   float* own = gsq + a.groups;      // [2 groups]: what the other CTAs of the cluster read
   float* par = own + 2 * a.groups;  // [2][C]: gamma and beta
   float* red = par + 2 * a.C;
-  const int tx = threadIdx.x % a.tx_n, ty = threadIdx.x / a.tx_n, c0 = tx * V;
-  const int rank = a.cl > 1 ? blockIdx.x % a.cl : 0;
-  const int64_t n = a.cl > 1 ? blockIdx.x / a.cl : blockIdx.x;
+  const int tx = threadIdx.x, ty = threadIdx.y, c0 = tx * V;
+  const int tx_n = blockDim.x, ty_n = blockDim.y, threads = tx_n * ty_n, tid = ty * tx_n + tx, nw = threads >> 5;
+  const int rank = blockIdx.x & (a.cl - 1), n = blockIdx.x / a.cl;
+  const bool shuffled = tx_n < 32 && (tx_n & (tx_n - 1)) == 0;
   const int p0 = rank * a.rows, p1 = min(a.P, p0 + a.rows), cnt = max(0, p1 - p0);
-  const int first = p0 + ty, last = ty < a.ty_n ? p1 : 0;
+  const int first = p0 + ty, last = p1;
   pdl_begin();
-  const int64_t base = n * a.P * (int64_t)a.C + c0;
+  const int64_t base = (int64_t)n * a.P * a.C + (int64_t)first * a.C + c0;
   const XT* x = static_cast<const XT*>(a.x) + base;
+  const int step = ty_n * a.C;
   Vec<XT, V> r[R];
 #pragma unroll
   for (int i = 0; i < R; ++i)
-    if (first + i * a.ty_n < last) r[i].load(x + (int64_t)(first + i * a.ty_n) * a.C);
-  for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
-    const int64_t pc = (n / a.B) * a.par_gs + c;
+    if (first + i * ty_n < last) r[i].load(x + i * step);
+  for (int c = tid; c < a.C; c += threads) {
+    const int64_t pc = (int64_t)(n / a.B) * a.par_gs + c;
     par[c] = a.gamma[pc], par[a.C + c] = a.beta[pc];
   }
   const int dn = a.D / a.sub;
@@ -574,39 +696,40 @@ __global__ void __launch_bounds__(1024, 1) gn_fwd_resident_kernel(const GnArgs a
   for (int j = 0; j < V; ++j) t[j] = 0.f;
 #pragma unroll
   for (int i = 0; i < R; ++i)
-    if (first + i * a.ty_n < last) {
+    if (first + i * ty_n < last) {
       float v[V];
       r[i].floats(v);
 #pragma unroll
       for (int j = 0; j < V; ++j) t[j] += v[j];
     }
-  int rows = column_sums<V>(t, red, tx, ty, a.tx_n, a.ty_n, a.sub);
+  channel_sums<V>(t, red, tx, ty, tx_n, shuffled, a.sub);
+  const int rows = shuffled ? nw : ty_n;
   __syncthreads();
-  group_sums(red, rows, a.groups, dn, gmean);
+  group_sums(red, rows, a.groups, dn, gmean, tid, nw);
   __syncthreads();
   const float inv = cnt ? 1.f / ((float)cnt * (float)a.D) : 0.f;
   float mu[V];
-  if (ty < a.ty_n) each_group<V>(c0, a.D, [&](int j, int q) { mu[j] = gmean[q] * inv; });
+  each_group<V>(c0, a.D, [&](int j, int q) { mu[j] = gmean[q] * inv; });
 #pragma unroll
   for (int j = 0; j < V; ++j) t[j] = 0.f;
 #pragma unroll
   for (int i = 0; i < R; ++i)
-    if (first + i * a.ty_n < last) {
+    if (first + i * ty_n < last) {
       float v[V];
       r[i].floats(v);
 #pragma unroll
       for (int j = 0; j < V; ++j) t[j] = fmaf(v[j] - mu[j], v[j] - mu[j], t[j]);
     }
-  rows = column_sums<V>(t, red, tx, ty, a.tx_n, a.ty_n, a.sub);
+  channel_sums<V>(t, red, tx, ty, tx_n, shuffled, a.sub);
   __syncthreads();
-  group_sums(red, rows, a.groups, dn, gsq);
+  group_sums(red, rows, a.groups, dn, gsq, tid, nw);
   __syncthreads();
   if (a.cl > 1) {
-    for (int q = threadIdx.x; q < a.groups; q += blockDim.x) own[2 * q] = gmean[q] * inv, own[2 * q + 1] = gsq[q];
+    for (int q = tid; q < a.groups; q += threads) own[2 * q] = gmean[q] * inv, own[2 * q + 1] = gsq[q];
     cluster_arrive();
     cluster_wait();
   }
-  for (int q = threadIdx.x; q < a.groups; q += blockDim.x) {
+  for (int q = tid; q < a.groups; q += threads) {
     float m = gmean[q] * inv, sq = gsq[q], k = (float)cnt * a.D;
     if (a.cl > 1) {
       k = m = sq = 0.f;
@@ -617,11 +740,11 @@ __global__ void __launch_bounds__(1024, 1) gn_fwd_resident_kernel(const GnArgs a
     const float rs = __frsqrt_rn(sq / k + a.eps);
     gmean[q] = m;
     gsq[q] = rs;
-    if (rank == 0) a.mean[n * a.groups + q] = m, a.rstd[n * a.groups + q] = rs;
+    if (rank == 0) a.mean[(int64_t)n * a.groups + q] = m, a.rstd[(int64_t)n * a.groups + q] = rs;
   }
   __syncthreads();
   if (a.cl > 1) cluster_arrive();  // this CTA has read the others' sums; the wait is at the end
-  if (ty < a.ty_n) {
+  {
     float ga[V], be[V];
     each_group<V>(c0, a.D, [&](int j, int q) {
       mu[j] = gmean[q], ga[j] = par[c0 + j] * gsq[q], be[j] = par[a.C + c0 + j];
@@ -629,14 +752,14 @@ __global__ void __launch_bounds__(1024, 1) gn_fwd_resident_kernel(const GnArgs a
     YT* out = static_cast<YT*>(a.out) + base;
 #pragma unroll
     for (int i = 0; i < R; ++i)
-      if (first + i * a.ty_n < last) {
+      if (first + i * ty_n < last) {
         float v[V];
         r[i].floats(v);
 #pragma unroll
         for (int j = 0; j < V; ++j) v[j] = activate<sizeof(YT) == 4>(fmaf(v[j] - mu[j], ga[j], be[j]), a.act);
         Vec<YT, V> o;
         o.set(v);
-        o.store(out + (int64_t)(first + i * a.ty_n) * a.C);
+        o.store(out + i * step);
       }
   }
   if (a.cl > 1) cluster_wait();
@@ -652,14 +775,15 @@ __global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a
   float* par = stat + 2 * a.groups;   // [2][C]: gamma and beta
   float* chans = par + 2 * a.C;       // [2][C]: sum dz, sum dz xh
   float* red = chans + 2 * a.C;       // [rows][C], twice
-  const int tx = threadIdx.x % a.tx_n, ty = threadIdx.x / a.tx_n, c0 = tx * V;
-  const int rank = a.cl > 1 ? blockIdx.x % a.cl : 0;
-  const int64_t n = a.cl > 1 ? blockIdx.x / a.cl : blockIdx.x;
+  const int tx = threadIdx.x, ty = threadIdx.y, c0 = tx * V;
+  const int tx_n = blockDim.x, ty_n = blockDim.y, threads = tx_n * ty_n, tid = ty * tx_n + tx, nw = threads >> 5;
+  const int rank = blockIdx.x & (a.cl - 1), n = blockIdx.x / a.cl;
+  const bool shuffled = tx_n < 32 && (tx_n & (tx_n - 1)) == 0;
   const int p0 = rank * a.rows, p1 = min(a.P, p0 + a.rows);
-  const int first = p0 + ty, last = ty < a.ty_n ? p1 : 0;
+  const int first = p0 + ty, last = p1, step = ty_n * a.C;
   const bool relu = a.act == LSGD_ACT_RELU, silu = a.act == LSGD_ACT_SILU;
   pdl_begin();
-  const int64_t base = n * a.P * (int64_t)a.C + c0;
+  const int64_t base = (int64_t)n * a.P * a.C + (int64_t)first * a.C + c0;
   const XT* x = static_cast<const XT*>(a.x) + base;
   const YT* dy = static_cast<const YT*>(a.dy) + base;
   const YT* y = static_cast<const YT*>(a.y) + base;
@@ -669,8 +793,8 @@ __global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a
     Vec<YT, V> rd[R], ry[R];
 #pragma unroll
     for (int i = 0; i < R; ++i)
-      if (first + i * a.ty_n < last) {
-        const int64_t at = (int64_t)(first + i * a.ty_n) * a.C;
+      if (first + i * ty_n < last) {
+        const int at = i * step;
         r[i].load(x + at);
         rd[i].load(dy + at);
         if (relu) ry[i].load(y + at);
@@ -679,7 +803,7 @@ __global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a
     for (int i = 0; i < R; ++i) {
 #pragma unroll
       for (int j = 0; j < V; ++j) dz[i][j] = 0.f;
-      if (first + i * a.ty_n < last) {
+      if (first + i * ty_n < last) {
         rd[i].floats(dz[i]);
         if (relu) {
           float yv[V];
@@ -690,23 +814,23 @@ __global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a
       }
     }
   }
-  for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
-    const int64_t pc = (n / a.B) * a.par_gs + c;
+  for (int c = tid; c < a.C; c += threads) {
+    const int64_t pc = (int64_t)(n / a.B) * a.par_gs + c;
     par[c] = a.gamma[pc], par[a.C + c] = a.beta[pc];
   }
-  for (int q = threadIdx.x; q < a.groups; q += blockDim.x)
-    stat[2 * q] = a.mean[n * a.groups + q], stat[2 * q + 1] = a.rstd[n * a.groups + q];
+  for (int q = tid; q < a.groups; q += threads)
+    stat[2 * q] = a.mean[(int64_t)n * a.groups + q], stat[2 * q + 1] = a.rstd[(int64_t)n * a.groups + q];
   __syncthreads();
   float s0[V], s1[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) s0[j] = s1[j] = 0.f;
-  if (ty < a.ty_n) {
+  {
     // channel by channel, so that one channel's parameters are in registers at a time
     each_group<V>(c0, a.D, [&](int j, int q) {
       const float mu = stat[2 * q], rs = stat[2 * q + 1], ga = par[c0 + j], be = par[a.C + c0 + j];
 #pragma unroll
       for (int i = 0; i < R; ++i)
-        if (first + i * a.ty_n < last) {
+        if (first + i * ty_n < last) {
           const float xh = (r[i].at(j) - mu) * rs;
           if (silu) {
             const float z = fmaf(xh, ga, be), sg = sigmoid<sizeof(XT) == 4>(z);
@@ -717,23 +841,22 @@ __global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a
         }
     });
   }
-  const int shuffled = a.tx_n < 32 && (a.tx_n & (a.tx_n - 1)) == 0;
-  const int rows = shuffled ? blockDim.x >> 5 : a.ty_n;
+  const int rows = shuffled ? nw : ty_n;
   float* red1 = red + rows * a.C;
-  column_sums<V>(s0, red, tx, ty, a.tx_n, a.ty_n, 1);
-  column_sums<V>(s1, red1, tx, ty, a.tx_n, a.ty_n, 1);
+  column_sums<V>(s0, red, tx, ty, tx_n, shuffled);
+  column_sums<V>(s1, red1, tx, ty, tx_n, shuffled);
   __syncthreads();
   float2* out = reinterpret_cast<float2*>(a.sums) + (int64_t)blockIdx.x * a.C;
   if (rows <= 32) {
-    for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
+    for (int c = tid; c < a.C; c += threads) {
       float t0 = 0.f, t1 = 0.f;
       for (int i = 0; i < rows; ++i) t0 += red[i * a.C + c], t1 += red1[i * a.C + c];
       chans[c] = t0, chans[a.C + c] = t1;
       out[c] = make_float2(t0, t1);
     }
   } else {  // many rows over few channels: a warp per channel
-    const int lane = threadIdx.x & 31;
-    for (int c = threadIdx.x >> 5; c < a.C; c += blockDim.x >> 5) {
+    const int lane = tid & 31;
+    for (int c = tid < nw * 32 ? tid >> 5 : a.C; c < a.C; c += nw) {
       float t0 = 0.f, t1 = 0.f;
       for (int i = lane; i < rows; i += 32) t0 += red[i * a.C + c], t1 += red1[i * a.C + c];
 #pragma unroll
@@ -746,9 +869,9 @@ __global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a
   }
   __syncthreads();
   {
-    const int lane = threadIdx.x & 31;
+    const int lane = tid & 31;
     const float inv = 1.f / ((float)a.P * (float)a.D);
-    for (int q = threadIdx.x >> 5; q < a.groups; q += blockDim.x >> 5) {
+    for (int q = tid < nw * 32 ? tid >> 5 : a.groups; q < a.groups; q += nw) {
       float t0 = 0.f, t1 = 0.f;
       for (int d = lane; d < a.D; d += 32) {
         const float g = par[q * a.D + d];
@@ -766,7 +889,7 @@ __global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a
   if (a.cl > 1) {
     cluster_arrive();
     cluster_wait();
-    for (int q = threadIdx.x; q < 2 * a.groups; q += blockDim.x) {
+    for (int q = tid; q < 2 * a.groups; q += threads) {
       float t = 0.f;
       for (int c = 0; c < a.cl; ++c) t += peer_float(own + q, c);
       gm[q] = t;
@@ -774,7 +897,7 @@ __global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a
   }
   __syncthreads();
   if (a.cl > 1) cluster_arrive();
-  if (ty < a.ty_n) {
+  {
     each_group<V>(c0, a.D, [&](int j, int q) {
       const float mu = stat[2 * q], rs = stat[2 * q + 1], k = rs * par[c0 + j], b = rs * gm[2 * q];
       const float m = rs * rs * gm[2 * q + 1];
@@ -784,10 +907,10 @@ __global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a
     XT* dx = static_cast<XT*>(a.out) + base;
 #pragma unroll
     for (int i = 0; i < R; ++i)
-      if (first + i * a.ty_n < last) {
+      if (first + i * ty_n < last) {
         Vec<XT, V> o;
         o.set(dz[i]);
-        o.store(dx + (int64_t)(first + i * a.ty_n) * a.C);
+        o.store(dx + i * step);
       }
   }
   if (a.cl > 1) cluster_wait();
@@ -795,35 +918,39 @@ __global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a
 
 // The resident form's CTAs per image (a power of two up to 8, the portable cluster size), or 0: the split form.  A
 // CTA of T threads takes `rows` positions if rows C / hold + C <= T, whatever the vector width (a row of threads is
-// C / V wide, and hold / V positions fall to each).  CTAs of 512 threads or fewer where they do; then, where the images
-// are few, more CTAs to an image down to 4096 values each.
+// C / V wide, and hold / V positions fall to each).  CTAs of about 512 threads or fewer where they do; then, where the images
+// are few, more CTAs to an image down to 4096 values each.  (One row of threads more than needed covers every V; with rows
+// rounded up to full warps a CTA has at most T + 31 threads.)
 int gn_cluster(int64_t N, int P, int C, int hold) {
   auto fits = [&](int cl, int T) { return (int64_t)((P + cl - 1) / cl) * C / hold + 1 + C <= T; };
   int cl = 0;
-  for (int T = 512; T <= 1024 && !cl; T *= 2)
+  for (int T : {608, 992})
     for (int c = 1; c <= 8 && !cl; c *= 2)
       if (fits(c, T)) cl = c;
   while (cl && cl < 8 && N * cl < kNumSMs && (int64_t)P * C / (2 * cl) >= 4096) cl *= 2;
   return cl;
 }
 
-// The shape of a resident launch with vectors of V values: threads, and bytes of shared memory.
-void gn_resident_shape(GnArgs& a, int V, int hold, bool bwd, int* threads, size_t* smem) {
+// The shape of a resident launch with vectors of V values: threads across and down (full warps where the rows of a warp
+// are added by shuffles, one at least otherwise), and bytes of shared memory.
+void gn_resident_shape(GnArgs& a, int V, int hold, bool bwd, dim3* block, size_t* smem) {
   a.rows = (a.P + a.cl - 1) / a.cl;
-  a.tx_n = a.C / V;
-  a.ty_n = (a.rows + hold / V - 1) / (hold / V);
-  *threads = (a.tx_n * a.ty_n + 31) / 32 * 32;
+  const int tx = a.C / V;
+  const bool shuffled = tx < 32 && (tx & (tx - 1)) == 0;
+  int ty = std::max((a.rows + hold / V - 1) / (hold / V), (32 + tx - 1) / tx);
+  if (shuffled) ty = (ty + 32 / tx - 1) / (32 / tx) * (32 / tx);
+  *block = dim3(tx, ty);
   a.sub = std::min(V, a.D & -a.D);
-  const int rows = a.tx_n < 32 && (a.tx_n & (a.tx_n - 1)) == 0 ? *threads / 32 : a.ty_n;
+  const int rows = shuffled ? tx * ty / 32 : ty;
   *smem = 4 * (bwd ? 6 * (size_t)a.groups + 4 * (size_t)a.C + 2 * (size_t)rows * a.C
                    : 4 * (size_t)a.groups + 2 * (size_t)a.C + (size_t)rows * (a.C / a.sub));
 }
 
 constexpr size_t kGnMaxSmem = 160 * 1024;
 template <typename K>
-cudaError_t gn_launch_resident(K kernel, std::atomic<int>& raised, const GnArgs& a, int threads, size_t smem,
+cudaError_t gn_launch_resident(K kernel, std::atomic<int>& raised, const GnArgs& a, dim3 block, size_t smem,
                                cudaStream_t st) {
-  if (threads > 1024 || smem > kGnMaxSmem) return cudaErrorInvalidValue;
+  if (block.x * block.y > 1024 || smem > kGnMaxSmem) return cudaErrorInvalidValue;
   if (smem > 48 * 1024) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -836,7 +963,7 @@ cudaError_t gn_launch_resident(K kernel, std::atomic<int>& raised, const GnArgs&
   }
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(a.N * a.cl));
-  cfg.blockDim = dim3(threads);
+  cfg.blockDim = block;
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -852,16 +979,16 @@ cudaError_t gn_launch_resident(K kernel, std::atomic<int>& raised, const GnArgs&
 
 template <typename XT, typename YT, int V, bool BWD>
 cudaError_t gn_resident(GnArgs a, cudaStream_t st) {
-  int threads = 0;
+  dim3 block;
   size_t smem = 0;
   static std::atomic<int> raised{0};  // device + 1 whose limit of shared memory this kernel's has been raised
-  gn_resident_shape(a, V, BWD ? kBwdHold : kFwdHold, BWD, &threads, &smem);
+  gn_resident_shape(a, V, BWD ? kBwdHold : kFwdHold, BWD, &block, &smem);
   if constexpr (!BWD) {
-    return gn_launch_resident(gn_fwd_resident_kernel<XT, YT, V>, raised, a, threads, smem, st);
+    return gn_launch_resident(gn_fwd_resident_kernel<XT, YT, V>, raised, a, block, smem, st);
   } else {
-    const cudaError_t e = gn_launch_resident(gn_bwd_resident_kernel<XT, YT, V>, raised, a, threads, smem, st);
+    const cudaError_t e = gn_launch_resident(gn_bwd_resident_kernel<XT, YT, V>, raised, a, block, smem, st);
     if (e != cudaSuccess) return e;
-    return launch_pdl(gn_param_grad_kernel, dim3((a.C + 15) / 16, (unsigned)(a.N / a.B)), dim3(256), 0, st,
+    return launch_pdl(gn_param_grad_kernel, dim3((a.C + 15) / 16, (unsigned)(a.N / a.B)), dim3(1024), 0, st,
                       (const float2*)a.sums, (int64_t)a.B * a.cl, a.C, a.par_gs, a.dgamma, a.dbeta);
   }
 }
@@ -908,8 +1035,8 @@ lsgd_status gn_error(lsgd_status s, const char* fn, const char* what) {
 const char* gn_shape_error(int G, int B, int64_t P, int C, int groups) {
   if (G < 1 || B < 1 || P < 1 || C < 1 || groups < 1) return "G, B, P, C and groups must be at least 1";
   if (C % groups) return "C must be a multiple of groups";
-  if (G > 65535 || (int64_t)G * B > (1 << 24) || C > 65536 || P > (1 << 24))
-    return "at most 65535 workers, 2^24 images (G B), 65536 channels and 2^24 positions";
+  if (G > 65535 || (int64_t)G * B > (1 << 24) || C > 65536 || P > (1 << 24) || (int64_t)G * B * groups > 0x7fffffff)
+    return "at most 65535 workers, 2^24 images (G B), 2^31 - 1 groups in all, 65536 channels and 2^24 positions";
   return nullptr;
 }
 
