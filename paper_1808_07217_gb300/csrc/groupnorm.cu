@@ -13,12 +13,17 @@
 #include <algorithm>
 #include <atomic>
 #include <string>
+#include <type_traits>
 
 #include "../../include/lsgd.h"
 #include "common.cuh"
 #include "lsgd_internal.h"
+#include "tc_ptx.cuh"
 
 namespace lsgd {
+
+__device__ int g_norm_timeout = 0;
+
 namespace {
 
 template <int BYTES>
@@ -49,6 +54,10 @@ struct Vec {
   __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
     for (int i = 0; i < kN; ++i) r[i] = __ldg(reinterpret_cast<const Raw*>(p) + i);
+  }
+  __device__ __forceinline__ void load_shared(const void* p) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) r[i] = static_cast<const Raw*>(p)[i];
   }
   __device__ __forceinline__ void floats(float (&v)[V]) const {
     if constexpr (sizeof(T) == 4) {
@@ -116,6 +125,7 @@ struct GnArgs {
   int64_t N;
   float eps;
   int cl, sub;    // resident form: CTAs per image; channels summed in a thread
+  int stages, slab, slab_y;  // its pipeline: images ahead; bytes of an image of x and of dy (or y)
 };
 
 // 1 / (1 + exp(-z)): the exponential's overflow gives 0.
@@ -127,11 +137,22 @@ __device__ __forceinline__ float sigmoid(float z) {
 
 // act(z).  EXACT (fp32 results): the accurate exponential and division; a bf16 result's rounding hides the fast ones'.
 // __fdividef gives 0 for divisors above 2^126, which is what 1 / (1 + exp(-z)) rounds to there.
-template <bool EXACT>
-__device__ __forceinline__ float activate(float z, int act) {
-  if (act == LSGD_ACT_RELU) return z < 0.f ? 0.f : z;  // NaN stays
-  if (act == LSGD_ACT_SILU) return z * sigmoid<EXACT>(z);
+template <bool EXACT, int ACT>
+__device__ __forceinline__ float activate(float z) {
+  if constexpr (ACT == LSGD_ACT_RELU) {
+    float r;
+    asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(z));
+    return r;
+  }
+  if constexpr (ACT == LSGD_ACT_SILU) return z * sigmoid<EXACT>(z);
   return z;
+}
+// f with the activation as a constant.
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F f) {
+  if (act == LSGD_ACT_RELU) f(std::integral_constant<int, LSGD_ACT_RELU>{});
+  else if (act == LSGD_ACT_SILU) f(std::integral_constant<int, LSGD_ACT_SILU>{});
+  else f(std::integral_constant<int, LSGD_ACT_NONE>{});
 }
 
 // ---- split form: any size, three launches ----
@@ -415,23 +436,25 @@ __global__ void __launch_bounds__(kSplitThreads) gn_apply_kernel(const GnArgs a,
 #pragma unroll
     for (int j = 0; j < V; ++j) ga[j] *= a.rstd[(int64_t)n * a.groups + (c0 + j) / a.D];
     constexpr int U = 4;
-    for (int p = p0 + ty; p < p1; p += U * ty_n) {
-      Vec<XT, V> r[U];
+    with_act(a.act, [&](auto act) {
+      for (int p = p0 + ty; p < p1; p += U * ty_n) {
+        Vec<XT, V> r[U];
 #pragma unroll
-      for (int i = 0; i < U; ++i)
-        if (p + i * ty_n < p1) r[i].load(x + (int64_t)(p + i * ty_n) * a.C);
+        for (int i = 0; i < U; ++i)
+          if (p + i * ty_n < p1) r[i].load(x + (int64_t)(p + i * ty_n) * a.C);
 #pragma unroll
-      for (int i = 0; i < U; ++i)
-        if (p + i * ty_n < p1) {
-          float v[V];
-          r[i].floats(v);
+        for (int i = 0; i < U; ++i)
+          if (p + i * ty_n < p1) {
+            float v[V];
+            r[i].floats(v);
 #pragma unroll
-          for (int j = 0; j < V; ++j) v[j] = activate<sizeof(YT) == 4>(fmaf(v[j] - mu[j], ga[j], be[j]), a.act);
-          Vec<YT, V> o;
-          o.set(v);
-          o.stream(out + (int64_t)(p + i * ty_n) * a.C);
-        }
-    }
+            for (int j = 0; j < V; ++j) v[j] = activate<sizeof(YT) == 4, decltype(act)::value>(fmaf(v[j] - mu[j], ga[j], be[j]));
+            Vec<YT, V> o;
+            o.set(v);
+            o.stream(out + (int64_t)(p + i * ty_n) * a.C);
+          }
+      }
+    });
   } else {
     const YT* dy = static_cast<const YT*>(a.dy) + base;
     const YT* y = static_cast<const YT*>(a.y) + base;
@@ -558,6 +581,8 @@ constexpr int kFwdHold = 32, kBwdHold = 16;  // the backward also holds dz
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// An arrival that only says that reading is over: nothing written has to be seen.
+__device__ __forceinline__ void cluster_read() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
 // The float at `p` of this CTA's shared memory, in CTA `rank` of the cluster.
 __device__ __forceinline__ float peer_float(const float* p, int rank) {
   uint32_t at;
@@ -638,9 +663,9 @@ __device__ __forceinline__ void channel_sums(float (&v)[V], float* red, int tx, 
 
 // out[q] = the sum over red's rows and the columns of group q (dn columns each), a warp per group, the block's full warps.
 __device__ __forceinline__ void group_sums(const float* red, int rows, int groups, int dn, float* out, int tid, int nw) {
+  if (tid >= min(nw, groups) * 32) return;
   const int lane = tid & 31, cols = groups * dn;
   const int wide = min(dn, 32), r0 = lane / wide, d0 = lane - r0 * wide, down = 32 / wide;
-  if (tid >= nw * 32) return;
   for (int q = tid >> 5; q < groups; q += nw) {
     float t = 0.f;
     if (r0 < down)
@@ -663,10 +688,34 @@ __device__ __forceinline__ void each_group(int c0, int D, F f) {
   }
 }
 
-template <typename XT, typename YT, int V>
+// Pipelined (PIPE): where there are more images than CTAs on the SMs at once, a CTA takes images blockIdx.x, blockIdx.x +
+// gridDim.x, ... and bulk copies bring the next `stages` of them to shared memory while one is worked on in registers, so
+// that the loads never stop for the sums' barriers.  One CTA to an image then, and 16-byte vectors.
+constexpr long long kWaitCycles = 4000000000LL;  // ~2 s at 2 GHz
+
+__device__ __forceinline__ bool wait_full(uint64_t* bar, uint32_t parity) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity))
+    if (clock64() - t0 > kWaitCycles) {
+      atomicExch(&g_norm_timeout, 1);
+      return false;
+    }
+  return true;
+}
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, int bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+               "l"(src), "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
+constexpr int kMaxStages = 4, kPipeHead = 64;  // bytes before the first buffer: the barriers
+
+template <typename XT, typename YT, int V, bool PIPE>
 __global__ void __launch_bounds__(1024, 1) gn_fwd_resident_kernel(const GnArgs a) {
   constexpr int R = kFwdHold / V;
-  extern __shared__ float sm[];
+  extern __shared__ __align__(16) uint8_t raw[];
+  float* sm = reinterpret_cast<float*>(raw + (PIPE ? kPipeHead + a.stages * a.slab : 0));
+  uint64_t* full = reinterpret_cast<uint64_t*>(raw);
   float* gmean = sm;                // [groups]: the CTA's, then the image's mean
   float* gsq = gmean + a.groups;    // [groups]: squared deviations, then rstd
   float* own = gsq + a.groups;      // [2 groups]: what the other CTAs of the cluster read
@@ -674,101 +723,143 @@ __global__ void __launch_bounds__(1024, 1) gn_fwd_resident_kernel(const GnArgs a
   float* red = par + 2 * a.C;
   const int tx = threadIdx.x, ty = threadIdx.y, c0 = tx * V;
   const int tx_n = blockDim.x, ty_n = blockDim.y, threads = tx_n * ty_n, tid = ty * tx_n + tx, nw = threads >> 5;
-  const int rank = blockIdx.x & (a.cl - 1), n = blockIdx.x / a.cl;
+  const int rank = PIPE ? 0 : blockIdx.x & (a.cl - 1);
   const bool shuffled = tx_n < 32 && (tx_n & (tx_n - 1)) == 0;
   const int p0 = rank * a.rows, p1 = min(a.P, p0 + a.rows), cnt = max(0, p1 - p0);
   const int first = p0 + ty, last = p1;
-  pdl_begin();
-  const int64_t base = (int64_t)n * a.P * a.C + (int64_t)first * a.C + c0;
-  const XT* x = static_cast<const XT*>(a.x) + base;
-  const int step = ty_n * a.C;
-  Vec<XT, V> r[R];
-#pragma unroll
-  for (int i = 0; i < R; ++i)
-    if (first + i * ty_n < last) r[i].load(x + i * step);
-  for (int c = tid; c < a.C; c += threads) {
-    const int64_t pc = (int64_t)(n / a.B) * a.par_gs + c;
-    par[c] = a.gamma[pc], par[a.C + c] = a.beta[pc];
-  }
-  const int dn = a.D / a.sub;
-  float t[V];
-#pragma unroll
-  for (int j = 0; j < V; ++j) t[j] = 0.f;
-#pragma unroll
-  for (int i = 0; i < R; ++i)
-    if (first + i * ty_n < last) {
-      float v[V];
-      r[i].floats(v);
-#pragma unroll
-      for (int j = 0; j < V; ++j) t[j] += v[j];
-    }
-  channel_sums<V>(t, red, tx, ty, tx_n, shuffled, a.sub);
-  const int rows = shuffled ? nw : ty_n;
-  __syncthreads();
-  group_sums(red, rows, a.groups, dn, gmean, tid, nw);
-  __syncthreads();
+  const int dn = a.D / a.sub, rows = shuffled ? nw : ty_n, step = ty_n * a.C;
   const float inv = cnt ? 1.f / ((float)cnt * (float)a.D) : 0.f;
-  float mu[V];
-  each_group<V>(c0, a.D, [&](int j, int q) { mu[j] = gmean[q] * inv; });
-#pragma unroll
-  for (int j = 0; j < V; ++j) t[j] = 0.f;
-#pragma unroll
-  for (int i = 0; i < R; ++i)
-    if (first + i * ty_n < last) {
-      float v[V];
-      r[i].floats(v);
-#pragma unroll
-      for (int j = 0; j < V; ++j) t[j] = fmaf(v[j] - mu[j], v[j] - mu[j], t[j]);
+  auto fetch = [&](int m, int s) {  // image m to buffer s
+    mbar_expect_tx(&full[s], a.slab);
+    bulk_load(raw + kPipeHead + s * a.slab, static_cast<const uint8_t*>(a.x) + (int64_t)m * a.slab, a.slab, &full[s]);
+  };
+  int n = PIPE ? blockIdx.x : blockIdx.x / a.cl, stage = 0;
+  uint32_t ph = 0;
+  if constexpr (PIPE) {
+    if (tid == 0) {
+      for (int s = 0; s < a.stages; ++s) mbar_init(&full[s], 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-  channel_sums<V>(t, red, tx, ty, tx_n, shuffled, a.sub);
-  __syncthreads();
-  group_sums(red, rows, a.groups, dn, gsq, tid, nw);
-  __syncthreads();
-  if (a.cl > 1) {
-    for (int q = tid; q < a.groups; q += threads) own[2 * q] = gmean[q] * inv, own[2 * q + 1] = gsq[q];
-    cluster_arrive();
-    cluster_wait();
+    __syncthreads();
   }
-  for (int q = tid; q < a.groups; q += threads) {
-    float m = gmean[q] * inv, sq = gsq[q], k = (float)cnt * a.D;
-    if (a.cl > 1) {
-      k = m = sq = 0.f;
-      for (int c = 0; c < a.cl; ++c)
-        chan(k, m, sq, (float)max(0, min(a.P, (c + 1) * a.rows) - c * a.rows) * a.D, peer_float(own + 2 * q, c),
-             peer_float(own + 2 * q + 1, c));
+  pdl_begin();
+  if constexpr (PIPE) {
+    if (tid == 0)
+      for (int s = 0; s < a.stages; ++s)
+        if (n + s * (int)gridDim.x < a.N) fetch(n + s * gridDim.x, s);
+  }
+  do {
+    const int64_t base = (int64_t)n * a.P * a.C + (int64_t)first * a.C + c0;
+    const int64_t pc = (int64_t)(n / a.B) * a.par_gs;
+    float ga0 = 0.f, be0 = 0.f;  // the parameters of channel tid, on their way while the image is waited for
+    if (tid < a.C) ga0 = a.gamma[pc + tid], be0 = a.beta[pc + tid];
+    Vec<XT, V> r[R];
+    if constexpr (PIPE) {
+      const bool ok = wait_full(&full[stage], ph);
+      const uint8_t* from = raw + kPipeHead + stage * a.slab + (first * a.C + c0) * (int)sizeof(XT);
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (first + i * ty_n < last) r[i].load_shared(from + i * step * (int)sizeof(XT));
+      if (__syncthreads_or(!ok)) {  // a wait ran out: the copies under way first
+        if (tid == 0)
+          for (int s = 0; s < a.stages; ++s) wait_full(&full[s], ph ^ (s < stage ? 1 : 0));
+        break;
+      }
+      if (tid == 0 && n + a.stages * (int)gridDim.x < a.N) fetch(n + a.stages * gridDim.x, stage);
+      if (++stage == a.stages) stage = 0, ph ^= 1;
+    } else {
+      const XT* x = static_cast<const XT*>(a.x) + base;
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (first + i * ty_n < last) r[i].load(x + i * step);
     }
-    const float rs = __frsqrt_rn(sq / k + a.eps);
-    gmean[q] = m;
-    gsq[q] = rs;
-    if (rank == 0) a.mean[(int64_t)n * a.groups + q] = m, a.rstd[(int64_t)n * a.groups + q] = rs;
-  }
-  __syncthreads();
-  if (a.cl > 1) cluster_arrive();  // this CTA has read the others' sums; the wait is at the end
-  {
-    float ga[V], be[V];
-    each_group<V>(c0, a.D, [&](int j, int q) {
-      mu[j] = gmean[q], ga[j] = par[c0 + j] * gsq[q], be[j] = par[a.C + c0 + j];
-    });
-    YT* out = static_cast<YT*>(a.out) + base;
+    if (tid < a.C) par[tid] = ga0, par[a.C + tid] = be0;
+    for (int c = tid + threads; c < a.C; c += threads) par[c] = a.gamma[pc + c], par[a.C + c] = a.beta[pc + c];
+    float t[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) t[j] = 0.f;
 #pragma unroll
     for (int i = 0; i < R; ++i)
       if (first + i * ty_n < last) {
         float v[V];
         r[i].floats(v);
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = activate<sizeof(YT) == 4>(fmaf(v[j] - mu[j], ga[j], be[j]), a.act);
-        Vec<YT, V> o;
-        o.set(v);
-        o.store(out + i * step);
+        for (int j = 0; j < V; ++j) t[j] += v[j];
       }
-  }
-  if (a.cl > 1) cluster_wait();
+    channel_sums<V>(t, red, tx, ty, tx_n, shuffled, a.sub);
+    __syncthreads();
+    group_sums(red, rows, a.groups, dn, gmean, tid, nw);
+    __syncthreads();
+    float mu[V];
+    each_group<V>(c0, a.D, [&](int j, int q) { mu[j] = gmean[q] * inv; });
+#pragma unroll
+    for (int j = 0; j < V; ++j) t[j] = 0.f;
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      if (first + i * ty_n < last) {
+        float v[V];
+        r[i].floats(v);
+#pragma unroll
+        for (int j = 0; j < V; ++j) t[j] = fmaf(v[j] - mu[j], v[j] - mu[j], t[j]);
+      }
+    channel_sums<V>(t, red, tx, ty, tx_n, shuffled, a.sub);
+    __syncthreads();
+    group_sums(red, rows, a.groups, dn, gsq, tid, nw);
+    __syncthreads();
+    if (!PIPE && a.cl > 1) {
+      for (int q = tid; q < a.groups; q += threads) own[2 * q] = gmean[q] * inv, own[2 * q + 1] = gsq[q];
+      cluster_arrive();
+      cluster_wait();
+    }
+    for (int q = tid; q < a.groups; q += threads) {
+      float m = gmean[q] * inv, sq = gsq[q], k = (float)cnt * a.D;
+      if (!PIPE && a.cl > 1) {
+        k = m = sq = 0.f;
+        for (int c = 0; c < a.cl; ++c)
+          chan(k, m, sq, (float)max(0, min(a.P, (c + 1) * a.rows) - c * a.rows) * a.D, peer_float(own + 2 * q, c),
+               peer_float(own + 2 * q + 1, c));
+      }
+      const float rs = __frsqrt_rn(sq / k + a.eps);
+      gmean[q] = m;
+      gsq[q] = rs;
+      if (rank == 0) a.mean[(int64_t)n * a.groups + q] = m, a.rstd[(int64_t)n * a.groups + q] = rs;
+    }
+    __syncthreads();
+    if (!PIPE && a.cl > 1) cluster_read();  // this CTA has read the others' sums; the wait is at the end
+    {
+      float ga[V], be[V];
+      each_group<V>(c0, a.D, [&](int j, int q) {
+        mu[j] = gmean[q], ga[j] = par[c0 + j] * gsq[q], be[j] = par[a.C + c0 + j];
+      });
+      YT* out = static_cast<YT*>(a.out) + base;
+      with_act(a.act, [&](auto act) {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+          if (first + i * ty_n < last) {
+            float v[V];
+            r[i].floats(v);
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = activate<sizeof(YT) == 4, decltype(act)::value>(fmaf(v[j] - mu[j], ga[j], be[j]));
+            Vec<YT, V> o;
+            o.set(v);
+            o.store(out + i * step);
+          }
+      });
+    }
+    if (!PIPE && a.cl > 1) cluster_wait();
+    n += gridDim.x;
+  } while (PIPE && n < a.N);
 }
 
-template <typename XT, typename YT, int V>
+template <typename XT, typename YT, int V, bool PIPE>
 __global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a) {
   constexpr int R = kBwdHold / V;
-  extern __shared__ float sm[];
+  extern __shared__ __align__(16) uint8_t raw[];
+  const bool relu = a.act == LSGD_ACT_RELU, silu = a.act == LSGD_ACT_SILU;
+  const int slabs = a.slab + (relu ? 2 : 1) * a.slab_y;  // x, dy and, for ReLU, y
+  float* sm = reinterpret_cast<float*>(raw + (PIPE ? kPipeHead + a.stages * slabs : 0));
+  uint64_t* full = reinterpret_cast<uint64_t*>(raw);
   float* gm = sm;                     // [2 groups]: m1 and m2
   float* own = gm + 2 * a.groups;     // [2 groups]
   float* stat = own + 2 * a.groups;   // [2 groups]: mean and rstd
@@ -777,100 +868,144 @@ __global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a
   float* red = chans + 2 * a.C;       // [rows][C], twice
   const int tx = threadIdx.x, ty = threadIdx.y, c0 = tx * V;
   const int tx_n = blockDim.x, ty_n = blockDim.y, threads = tx_n * ty_n, tid = ty * tx_n + tx, nw = threads >> 5;
-  const int rank = blockIdx.x & (a.cl - 1), n = blockIdx.x / a.cl;
+  const int rank = PIPE ? 0 : blockIdx.x & (a.cl - 1);
   const bool shuffled = tx_n < 32 && (tx_n & (tx_n - 1)) == 0;
   const int p0 = rank * a.rows, p1 = min(a.P, p0 + a.rows);
-  const int first = p0 + ty, last = p1, step = ty_n * a.C;
-  const bool relu = a.act == LSGD_ACT_RELU, silu = a.act == LSGD_ACT_SILU;
+  const int first = p0 + ty, last = p1, step = ty_n * a.C, lane = tid & 31;
+  const int rows = shuffled ? nw : ty_n;
+  float* red1 = red + rows * a.C;
+  const float inv = 1.f / ((float)a.P * (float)a.D);
+  auto fetch = [&](int m, int s) {  // image m to buffer s
+    uint8_t* to = raw + kPipeHead + s * slabs;
+    mbar_expect_tx(&full[s], slabs);
+    bulk_load(to, static_cast<const uint8_t*>(a.x) + (int64_t)m * a.slab, a.slab, &full[s]);
+    bulk_load(to + a.slab, static_cast<const uint8_t*>(a.dy) + (int64_t)m * a.slab_y, a.slab_y, &full[s]);
+    if (relu) bulk_load(to + a.slab + a.slab_y, static_cast<const uint8_t*>(a.y) + (int64_t)m * a.slab_y, a.slab_y, &full[s]);
+  };
+  int n = PIPE ? blockIdx.x : blockIdx.x / a.cl, stage = 0;
+  uint32_t ph = 0;
+  if constexpr (PIPE) {
+    if (tid == 0) {
+      for (int s = 0; s < a.stages; ++s) mbar_init(&full[s], 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncthreads();
+  }
   pdl_begin();
-  const int64_t base = (int64_t)n * a.P * a.C + (int64_t)first * a.C + c0;
-  const XT* x = static_cast<const XT*>(a.x) + base;
-  const YT* dy = static_cast<const YT*>(a.dy) + base;
-  const YT* y = static_cast<const YT*>(a.y) + base;
-  Vec<XT, V> r[R];
-  float dz[R][V];
-  {
-    Vec<YT, V> rd[R], ry[R];
+  if constexpr (PIPE) {
+    if (tid == 0)
+      for (int s = 0; s < a.stages; ++s)
+        if (n + s * (int)gridDim.x < a.N) fetch(n + s * gridDim.x, s);
+  }
+  do {
+    const int64_t base = (int64_t)n * a.P * a.C + (int64_t)first * a.C + c0;
+    const int64_t pc = (int64_t)(n / a.B) * a.par_gs, pg = (int64_t)n * a.groups;
+    float ga0 = 0.f, be0 = 0.f, mu0 = 0.f, rs0 = 0.f;  // channel tid's and group tid's, while the image is waited for
+    if (tid < a.C) ga0 = a.gamma[pc + tid], be0 = a.beta[pc + tid];
+    if (tid < a.groups) mu0 = a.mean[pg + tid], rs0 = a.rstd[pg + tid];
+    Vec<XT, V> r[R];
+    float dz[R][V];
+    auto masked = [&](const Vec<YT, V>& rd, const Vec<YT, V>& ry, float (&d)[V]) {
+      rd.floats(d);
+      if (relu) {
+        float yv[V];
+        ry.floats(yv);
 #pragma unroll
-    for (int i = 0; i < R; ++i)
-      if (first + i * ty_n < last) {
-        const int at = i * step;
-        r[i].load(x + at);
-        rd[i].load(dy + at);
-        if (relu) ry[i].load(y + at);
+        for (int j = 0; j < V; ++j) d[j] = yv[j] > 0.f ? d[j] : 0.f;
       }
+    };
+    if constexpr (PIPE) {
+      const bool ok = wait_full(&full[stage], ph);
+      const uint8_t* fx = raw + kPipeHead + stage * slabs + (first * a.C + c0) * (int)sizeof(XT);
+      const uint8_t* fd = raw + kPipeHead + stage * slabs + a.slab + (first * a.C + c0) * (int)sizeof(YT);
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
+      for (int i = 0; i < R; ++i) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) dz[i][j] = 0.f;
-      if (first + i * ty_n < last) {
-        rd[i].floats(dz[i]);
-        if (relu) {
-          float yv[V];
-          ry[i].floats(yv);
-#pragma unroll
-          for (int j = 0; j < V; ++j) dz[i][j] = yv[j] > 0.f ? dz[i][j] : 0.f;
+        for (int j = 0; j < V; ++j) dz[i][j] = 0.f;
+        if (first + i * ty_n < last) {
+          Vec<YT, V> rd, ry;
+          r[i].load_shared(fx + i * step * (int)sizeof(XT));
+          rd.load_shared(fd + i * step * (int)sizeof(YT));
+          if (relu) ry.load_shared(fd + a.slab_y + i * step * (int)sizeof(YT));
+          masked(rd, ry, dz[i]);
         }
       }
-    }
-  }
-  for (int c = tid; c < a.C; c += threads) {
-    const int64_t pc = (int64_t)(n / a.B) * a.par_gs + c;
-    par[c] = a.gamma[pc], par[a.C + c] = a.beta[pc];
-  }
-  for (int q = tid; q < a.groups; q += threads)
-    stat[2 * q] = a.mean[(int64_t)n * a.groups + q], stat[2 * q + 1] = a.rstd[(int64_t)n * a.groups + q];
-  __syncthreads();
-  float s0[V], s1[V];
-#pragma unroll
-  for (int j = 0; j < V; ++j) s0[j] = s1[j] = 0.f;
-  {
-    // channel by channel, so that one channel's parameters are in registers at a time
-    each_group<V>(c0, a.D, [&](int j, int q) {
-      const float mu = stat[2 * q], rs = stat[2 * q + 1], ga = par[c0 + j], be = par[a.C + c0 + j];
+      if (__syncthreads_or(!ok)) {  // a wait ran out: the copies under way first
+        if (tid == 0)
+          for (int s = 0; s < a.stages; ++s) wait_full(&full[s], ph ^ (s < stage ? 1 : 0));
+        break;
+      }
+      if (tid == 0 && n + a.stages * (int)gridDim.x < a.N) fetch(n + a.stages * gridDim.x, stage);
+      if (++stage == a.stages) stage = 0, ph ^= 1;
+    } else {
+      const XT* x = static_cast<const XT*>(a.x) + base;
+      const YT* dy = static_cast<const YT*>(a.dy) + base;
+      const YT* y = static_cast<const YT*>(a.y) + base;
+      Vec<YT, V> rd[R], ry[R];
 #pragma unroll
       for (int i = 0; i < R; ++i)
         if (first + i * ty_n < last) {
-          const float xh = (r[i].at(j) - mu) * rs;
-          if (silu) {
-            const float z = fmaf(xh, ga, be), sg = sigmoid<sizeof(XT) == 4>(z);
-            dz[i][j] *= sg * fmaf(z, 1.f - sg, 1.f);
-          }
-          s0[j] += dz[i][j];
-          s1[j] = fmaf(dz[i][j], xh, s1[j]);
+          const int at = i * step;
+          r[i].load(x + at);
+          rd[i].load(dy + at);
+          if (relu) ry[i].load(y + at);
         }
-    });
-  }
-  const int rows = shuffled ? nw : ty_n;
-  float* red1 = red + rows * a.C;
-  column_sums<V>(s0, red, tx, ty, tx_n, shuffled);
-  column_sums<V>(s1, red1, tx, ty, tx_n, shuffled);
-  __syncthreads();
-  float2* out = reinterpret_cast<float2*>(a.sums) + (int64_t)blockIdx.x * a.C;
-  if (rows <= 32) {
-    for (int c = tid; c < a.C; c += threads) {
-      float t0 = 0.f, t1 = 0.f;
-      for (int i = 0; i < rows; ++i) t0 += red[i * a.C + c], t1 += red1[i * a.C + c];
-      chans[c] = t0, chans[a.C + c] = t1;
-      out[c] = make_float2(t0, t1);
-    }
-  } else {  // many rows over few channels: a warp per channel
-    const int lane = tid & 31;
-    for (int c = tid < nw * 32 ? tid >> 5 : a.C; c < a.C; c += nw) {
-      float t0 = 0.f, t1 = 0.f;
-      for (int i = lane; i < rows; i += 32) t0 += red[i * a.C + c], t1 += red1[i * a.C + c];
 #pragma unroll
-      for (int o = 16; o; o >>= 1) t0 += __shfl_xor_sync(~0u, t0, o), t1 += __shfl_xor_sync(~0u, t1, o);
-      if (lane == 0) {
-        chans[c] = t0, chans[a.C + c] = t1;
-        out[c] = make_float2(t0, t1);
+      for (int i = 0; i < R; ++i) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) dz[i][j] = 0.f;
+        if (first + i * ty_n < last) masked(rd[i], ry[i], dz[i]);
       }
     }
-  }
-  __syncthreads();
-  {
-    const int lane = tid & 31;
-    const float inv = 1.f / ((float)a.P * (float)a.D);
+    if (tid < a.C) par[tid] = ga0, par[a.C + tid] = be0;
+    for (int c = tid + threads; c < a.C; c += threads) par[c] = a.gamma[pc + c], par[a.C + c] = a.beta[pc + c];
+    if (tid < a.groups) stat[2 * tid] = mu0, stat[2 * tid + 1] = rs0;
+    for (int q = tid + threads; q < a.groups; q += threads) stat[2 * q] = a.mean[pg + q], stat[2 * q + 1] = a.rstd[pg + q];
+    __syncthreads();
+    float s0[V], s1[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) s0[j] = s1[j] = 0.f;
+    // channel by channel, so that one channel's parameters are in registers at a time
+    each_group<V>(c0, a.D, [&](int j, int q) {
+      const float mu = stat[2 * q], rs = stat[2 * q + 1];
+      if (silu) {
+        const float ga = par[c0 + j], be = par[a.C + c0 + j];
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+          if (first + i * ty_n < last) {
+            const float z = fmaf((r[i].at(j) - mu) * rs, ga, be), sg = sigmoid<sizeof(XT) == 4>(z);
+            dz[i][j] *= sg * fmaf(z, 1.f - sg, 1.f);
+          }
+      }
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (first + i * ty_n < last) {
+          s0[j] += dz[i][j];
+          s1[j] = fmaf(dz[i][j], (r[i].at(j) - mu) * rs, s1[j]);
+        }
+    });
+    column_sums<V>(s0, red, tx, ty, tx_n, shuffled);
+    column_sums<V>(s1, red1, tx, ty, tx_n, shuffled);
+    __syncthreads();
+    if (rows <= 32) {
+      for (int c = tid; c < 2 * a.C; c += threads) {  // first the sums of dz, then those of dz xh
+        const float* from = c < a.C ? red + c : red1 + (c - a.C);
+        float t = 0.f;
+        for (int i = 0; i < rows; ++i) t += from[i * a.C];
+        chans[c] = t;
+      }
+    } else {  // many rows over few channels: a warp per channel
+      for (int c = tid < nw * 32 ? tid >> 5 : 2 * a.C; c < 2 * a.C; c += nw) {
+        const float* from = c < a.C ? red + c : red1 + (c - a.C);
+        float t = 0.f;
+        for (int i = lane; i < rows; i += 32) t += from[i * a.C];
+#pragma unroll
+        for (int o = 16; o; o >>= 1) t += __shfl_xor_sync(~0u, t, o);
+        if (lane == 0) chans[c] = t;
+      }
+    }
+    __syncthreads();
     for (int q = tid < nw * 32 ? tid >> 5 : a.groups; q < a.groups; q += nw) {
       float t0 = 0.f, t1 = 0.f;
       for (int d = lane; d < a.D; d += 32) {
@@ -881,23 +1016,23 @@ __global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a
 #pragma unroll
       for (int o = 16; o; o >>= 1) t0 += __shfl_xor_sync(~0u, t0, o), t1 += __shfl_xor_sync(~0u, t1, o);
       if (lane == 0) {
-        float* to = a.cl > 1 ? own : gm;
+        float* to = !PIPE && a.cl > 1 ? own : gm;
         to[2 * q] = t0 * inv, to[2 * q + 1] = t1 * inv;
       }
     }
-  }
-  if (a.cl > 1) {
-    cluster_arrive();
-    cluster_wait();
-    for (int q = tid; q < 2 * a.groups; q += threads) {
-      float t = 0.f;
-      for (int c = 0; c < a.cl; ++c) t += peer_float(own + q, c);
-      gm[q] = t;
+    if (!PIPE && a.cl > 1) {
+      cluster_arrive();
+      cluster_wait();
+      for (int q = tid; q < 2 * a.groups; q += threads) {
+        float t = 0.f;
+        for (int c = 0; c < a.cl; ++c) t += peer_float(own + q, c);
+        gm[q] = t;
+      }
     }
-  }
-  __syncthreads();
-  if (a.cl > 1) cluster_arrive();
-  {
+    __syncthreads();
+    if (!PIPE && a.cl > 1) cluster_read();
+    float2* out = reinterpret_cast<float2*>(a.sums) + ((int64_t)n * a.cl + rank) * a.C;
+    for (int c = tid; c < a.C; c += threads) out[c] = make_float2(chans[c], chans[a.C + c]);
     each_group<V>(c0, a.D, [&](int j, int q) {
       const float mu = stat[2 * q], rs = stat[2 * q + 1], k = rs * par[c0 + j], b = rs * gm[2 * q];
       const float m = rs * rs * gm[2 * q + 1];
@@ -912,8 +1047,9 @@ __global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a
         o.set(dz[i]);
         o.store(dx + i * step);
       }
-  }
-  if (a.cl > 1) cluster_wait();
+    if (!PIPE && a.cl > 1) cluster_wait();
+    n += gridDim.x;
+  } while (PIPE && n < a.N);
 }
 
 // The resident form's CTAs per image (a power of two up to 8, the portable cluster size), or 0: the split form.  A
@@ -921,12 +1057,15 @@ __global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a
 // C / V wide, and hold / V positions fall to each).  CTAs of about 512 threads or fewer where they do; then, where the images
 // are few, more CTAs to an image down to 4096 values each.  (One row of threads more than needed covers every V; with rows
 // rounded up to full warps a CTA has at most T + 31 threads.)
+bool gn_fits(int P, int C, int cl, int hold, int threads) {
+  return (int64_t)((P + cl - 1) / cl) * C / hold + 1 + C <= threads;
+}
+bool gn_aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 int gn_cluster(int64_t N, int P, int C, int hold) {
-  auto fits = [&](int cl, int T) { return (int64_t)((P + cl - 1) / cl) * C / hold + 1 + C <= T; };
   int cl = 0;
   for (int T : {608, 992})
     for (int c = 1; c <= 8 && !cl; c *= 2)
-      if (fits(c, T)) cl = c;
+      if (gn_fits(P, C, c, hold, T)) cl = c;
   while (cl && cl < 8 && N * cl < kNumSMs && (int64_t)P * C / (2 * cl) >= 4096) cl *= 2;
   return cl;
 }
@@ -946,9 +1085,9 @@ void gn_resident_shape(GnArgs& a, int V, int hold, bool bwd, dim3* block, size_t
                    : 4 * (size_t)a.groups + 2 * (size_t)a.C + (size_t)rows * (a.C / a.sub));
 }
 
-constexpr size_t kGnMaxSmem = 160 * 1024;
+constexpr size_t kGnMaxSmem = 224 * 1024;
 template <typename K>
-cudaError_t gn_launch_resident(K kernel, std::atomic<int>& raised, const GnArgs& a, dim3 block, size_t smem,
+cudaError_t gn_launch_resident(K kernel, std::atomic<int>& raised, const GnArgs& a, int grid, dim3 block, size_t smem,
                                cudaStream_t st) {
   if (block.x * block.y > 1024 || smem > kGnMaxSmem) return cudaErrorInvalidValue;
   if (smem > 48 * 1024) {
@@ -962,7 +1101,7 @@ cudaError_t gn_launch_resident(K kernel, std::atomic<int>& raised, const GnArgs&
     }
   }
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(a.N * a.cl));
+  cfg.gridDim = dim3(grid);
   cfg.blockDim = block;
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
@@ -979,18 +1118,46 @@ cudaError_t gn_launch_resident(K kernel, std::atomic<int>& raised, const GnArgs&
 
 template <typename XT, typename YT, int V, bool BWD>
 cudaError_t gn_resident(GnArgs a, cudaStream_t st) {
+  static std::atomic<int> raised{0}, raised_pipe{0};  // device + 1 whose limit of shared memory this kernel's has been raised
+  constexpr int hold = BWD ? kBwdHold : kFwdHold;
   dim3 block;
   size_t smem = 0;
-  static std::atomic<int> raised{0};  // device + 1 whose limit of shared memory this kernel's has been raised
-  gn_resident_shape(a, V, BWD ? kBwdHold : kFwdHold, BWD, &block, &smem);
-  if constexpr (!BWD) {
-    return gn_launch_resident(gn_fwd_resident_kernel<XT, YT, V>, raised, a, block, smem, st);
-  } else {
-    const cudaError_t e = gn_launch_resident(gn_bwd_resident_kernel<XT, YT, V>, raised, a, block, smem, st);
-    if (e != cudaSuccess) return e;
-    return launch_pdl(gn_param_grad_kernel, dim3((a.C + 15) / 16, (unsigned)(a.N / a.B)), dim3(1024), 0, st,
-                      (const float2*)a.sums, (int64_t)a.B * a.cl, a.C, a.par_gs, a.dgamma, a.dbeta);
+  cudaError_t e = cudaErrorInvalidValue;
+  bool piped = false;
+  if constexpr (V * sizeof(XT) == 16 || V * sizeof(YT) == 16) {
+    // the pipelined form: one CTA to an image, images of whole 16-byte pieces, at least two rounds of CTAs
+    GnArgs b = a;
+    b.cl = 1;
+    const int64_t values = (int64_t)a.P * a.C;
+    if (values <= 1024 * hold && values * sizeof(XT) % 16 == 0 && values * sizeof(YT) % 16 == 0 &&
+        gn_aligned16(a.x) && gn_aligned16(BWD ? a.dy : a.x) && gn_aligned16(BWD && a.act == LSGD_ACT_RELU ? a.y : a.x)) {
+      gn_resident_shape(b, V, hold, BWD, &block, &smem);
+      const int threads = block.x * block.y;
+      b.slab = (int)(values * sizeof(XT)), b.slab_y = (int)(values * sizeof(YT));
+      const int bytes = BWD ? b.slab + (a.act == LSGD_ACT_RELU ? 2 : 1) * b.slab_y : b.slab;
+      // as many CTAs to an SM as the registers take, and the images ahead that the shared memory then holds
+      int per_sm = threads <= 1024 ? std::min(1024 / threads, 8) : 0;
+      const int64_t room = per_sm ? 222 * 1024 / per_sm - 1024 - (int64_t)smem - kPipeHead : 0;
+      b.stages = (int)std::min<int64_t>(kMaxStages, room / bytes);
+      if (per_sm && b.stages >= 1 && a.N >= 2LL * per_sm * kNumSMs) {
+        piped = true;
+        const int grid = per_sm * kNumSMs;
+        smem += kPipeHead + (size_t)b.stages * bytes;
+        if constexpr (BWD) e = gn_launch_resident(gn_bwd_resident_kernel<XT, YT, V, true>, raised_pipe, b, grid, block, smem, st);
+        else e = gn_launch_resident(gn_fwd_resident_kernel<XT, YT, V, true>, raised_pipe, b, grid, block, smem, st);
+        a.cl = 1;
+      }
+    }
   }
+  if (!piped) {
+    gn_resident_shape(a, V, hold, BWD, &block, &smem);
+    const int grid = (int)(a.N * a.cl);
+    if constexpr (BWD) e = gn_launch_resident(gn_bwd_resident_kernel<XT, YT, V, false>, raised, a, grid, block, smem, st);
+    else e = gn_launch_resident(gn_fwd_resident_kernel<XT, YT, V, false>, raised, a, grid, block, smem, st);
+  }
+  if (e != cudaSuccess || !BWD) return e;
+  return launch_pdl(gn_param_grad_kernel, dim3((a.C + 15) / 16, (unsigned)(a.N / a.B)), dim3(1024), 0, st,
+                    (const float2*)a.sums, (int64_t)a.B * a.cl, a.C, a.par_gs, a.dgamma, a.dbeta);
 }
 
 template <typename XT, typename YT, int V, bool BWD>
@@ -1048,6 +1215,20 @@ bool gn_overlap(const void* a, size_t na, const void* b, size_t nb) {
 bool gn_bad_align(const void* p, int z) { return reinterpret_cast<uintptr_t>(p) % z != 0; }
 
 }  // namespace
+
+int norm_take_timeout_flag() {
+  int h = 0;
+  if (cudaMemcpyFromSymbol(&h, g_norm_timeout, sizeof(int)) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;
+  }
+  if (h) {
+    const int zero = 0;
+    cudaMemcpyToSymbol(g_norm_timeout, &zero, sizeof(int));
+  }
+  return h;
+}
+
 }  // namespace lsgd
 
 extern "C" {

@@ -1530,7 +1530,8 @@ lsgd_status lsgd_eval_loss(lsgd_ctx* c, int k, int64_t n, double* loss) {
 lsgd_status lsgd_device_status(lsgd_ctx* c) {
   if (c) LSGD_TRY_CUDA(c, cudaStreamSynchronize(c->stream));
   const int products = lsgd::tc_take_timeout_flag(), directions = lsgd::direction_take_timeout_flag();
-  if (products || directions)
+  const int norms = lsgd::norm_take_timeout_flag();
+  if (products || directions || norms)
     return fail(c, LSGD_ETIMEOUT,
                 "a bounded wait inside a tensor-core kernel ran out; results since the last check "
                 "are not valid");

@@ -16,6 +16,10 @@ SHAPES = [(1, 1, 1, 1, 1), (2, 3, 5, 6, 3), (1, 2, 64, 64, 8), (2, 2, 49, 90, 9)
           (1, 2, 17, 1100, 11), (1, 1, 3, 4104, 2), (3, 2, 1, 24, 4), (2, 1, 333, 16, 16), (1, 3, 257, 40, 1),
           (1, 1, 5000, 72, 4), (2, 40, 30, 12, 2), (1, 2, 1025, 130, 10), (1, 1, 33, 2048, 1), (1, 1, 40000, 8, 1),
           (1, 2, 2000, 256, 16), (2, 1, 700, 512, 8), (1, 1, 311, 258, 6)]
+# more images than the SMs hold at once: a CTA takes several, with the next ones' loads under way (and where the sizes are
+# odd, one each); few and many groups, a worker's images ending between two of a CTA's
+MANY = [(5, 521, 64, 16, 4), (3, 800, 9, 24, 24), (2, 1300, 100, 8, 1), (7, 90, 1024, 16, 4), (2, 611, 1, 64, 8), (1, 2500, 16, 6, 3),
+        (11, 60, 260, 64, 16)]
 
 
 @pytest.fixture(scope="module")
@@ -183,6 +187,24 @@ def _run_backward(P, torch, shape, x, y, dy, gamma, beta, mean, rstd, act, par_g
     rest[pick.reshape(-1)] = False
     assert (dgamma[rest] == 77).all() and (dbeta[rest] == 77).all()  # what lies between the workers' parameters
     return dx, dgamma[pick], dbeta[pick]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ["relu", "silu"])
+@pytest.mark.parametrize("x_type,y_type", [("bf16", "bf16"), ("fp32", "bf16"), ("fp32", "fp32"), ("bf16", "fp32")])
+@pytest.mark.parametrize("shape", MANY)
+def test_many_images(P, shape, x_type, y_type, act):
+    import torch
+
+    par_gs = shape[3] + 3
+    x, dy, gamma, beta, xt, yt = _inputs(shape, par_gs, x_type, y_type, seed=9)
+    gg, bg = gamma.cuda(), beta.cuda()
+    y, mean, rstd = _run_forward(P, torch, shape, x.cuda(), gg, bg, yt, act, par_gs)
+    _check_forward(shape, x, gamma, beta, y, mean, rstd, act, U16 if y_type == "bf16" else U32)
+    dx, dgamma, dbeta = _run_backward(P, torch, shape, x.cuda(), y if act == "relu" else None, dy.cuda(), gg, bg, mean,
+                                      rstd, act, par_gs)
+    _check_backward(shape, x, dy, gamma, beta, y, mean, rstd, dx, dgamma, dbeta, act, x_type)
+    assert P.lsgd_device_status() == P.OK
 
 
 @pytest.mark.gpu
