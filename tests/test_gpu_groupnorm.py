@@ -19,7 +19,7 @@ SHAPES = [(1, 1, 1, 1, 1), (2, 3, 5, 6, 3), (1, 2, 64, 64, 8), (2, 2, 49, 90, 9)
 # more images than the SMs hold at once: a CTA takes several, with the next ones' loads under way (and where the sizes are
 # odd, one each); few and many groups, a worker's images ending between two of a CTA's
 MANY = [(5, 521, 64, 16, 4), (3, 800, 9, 24, 24), (2, 1300, 100, 8, 1), (7, 90, 1024, 16, 4), (2, 611, 1, 64, 8), (1, 2500, 16, 6, 3),
-        (11, 60, 260, 64, 16)]
+        (11, 60, 260, 64, 16), (1, 3, 40000, 96, 6), (2, 1, 60001, 40, 8), (1, 12, 5003, 256, 1), (1, 2, 9001, 1536, 8)]
 
 
 @pytest.fixture(scope="module")
@@ -190,11 +190,12 @@ def _run_backward(P, torch, shape, x, y, dy, gamma, beta, mean, rstd, act, par_g
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("act", ["relu", "silu"])
 @pytest.mark.parametrize("x_type,y_type", [("bf16", "bf16"), ("fp32", "bf16"), ("fp32", "fp32"), ("bf16", "fp32")])
 @pytest.mark.parametrize("shape", MANY)
-def test_many_images(P, shape, x_type, y_type, act):
+def test_many_images(P, shape, x_type, y_type):
     import torch
+
+    act = "silu" if (x_type == y_type) == bool(shape[0] % 2) else "relu"
 
     par_gs = shape[3] + 3
     x, dy, gamma, beta, xt, yt = _inputs(shape, par_gs, x_type, y_type, seed=9)
