@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(kMomThreads) direction_normalise_kernel(const 
 //   warp 0      TMA producer of both operands into a ring of kStages stages (both CTAs' bytes counted on the leader's
 //               barrier)
 //   warp 1      MMA issuer (leader only)
-//   warp 2      tensor memory allocation (two accumulators of 256 columns); TMA stores of the epilogue's buffers, and the
+//   warp 2      tensor memory allocation (two accumulators of a tile's columns); TMA stores of the epilogue's buffers, and the
 //               count of finished tiles
 //   warp 3      TMA loads of what the epilogue reads (h and l, or A), 64 columns at a time into a ring of kEpi buffers,
 //               ahead of the accumulator
@@ -236,13 +236,16 @@ __global__ void __launch_bounds__(kMomThreads) direction_normalise_kernel(const 
 //               cycles a tile, mostly latencies, against the products' 8,200 at k = 1024)
 //
 //
+// Where the tiles are few (PAIR false) each CTA works for itself on 128 x 128 tiles: half the products and half the epilogue
+// between a tile's start and its count, for twice the operand bytes per product (direction_tile chooses).
+//
 // The tiles of all steps form one list: per step the tiles of A = X X^T of every matrix, then those of P, then those of
 // X.  Pair p takes tiles p, p + pairs, ...; `done[g]` counts the CTAs' finished tiles of matrix g, whose phases follow one
 // another, and a tile starts when its matrix's earlier phases are complete.  The launch is cooperative (all pairs are
 // resident) and every tile's predecessors stand before it in the list, so that every wait ends; matrices fill each
 // other's phase ends, and nothing is launched between phases.
 
-constexpr int kTile = 256, kHalf = 128, kBK = 64, kStages = 4, kEpi = 3, kEpiWarps = 16, kThreads = 128 + 32 * kEpiWarps, kChunk = 64;
+constexpr int kHalf = 128, kBK = 64, kStages = 4, kEpi = 3, kEpiWarps = 16, kThreads = 128 + 32 * kEpiWarps, kChunk = 64;
 constexpr uint32_t kOpBytes = kHalf * kBK * 2;  // one operand's share of a stage in a CTA; half an epilogue buffer
 
 enum Role { GRAM = 0, POLY = 1, NEXT = 2, LAST = 3 };
@@ -372,6 +375,26 @@ __device__ __forceinline__ void commit_pair(uint64_t* bar) {
       "h"((uint16_t)3)
       : "memory");
 }
+__device__ __forceinline__ void mma_one(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void commit_one(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+template <bool PAIR>
+__device__ __forceinline__ void mma_of(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (PAIR) mma_pair(d, a, b, idesc, accumulate);
+  else mma_one(d, a, b, idesc, accumulate);
+}
+template <bool PAIR>
+__device__ __forceinline__ void commit_of(uint64_t* bar) {
+  if constexpr (PAIR) commit_pair(bar);
+  else commit_one(bar);
+}
 __device__ __forceinline__ void arrive_at(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
@@ -435,7 +458,10 @@ struct Item {
   int role, step, g, m0, n0, M, N, K;
   uint32_t need;  // of done[g], before it starts
 };
+template <bool PAIR>
 struct Plan {
+  static constexpr int kTile = PAIR ? 256 : 128;
+  static constexpr uint32_t kCtas = PAIR ? 2 : 1;  // counts of a finished tile
   int ts, tm, tn, per_sym, per_x;  // tiles a side of A; of X; tiles of a symmetric product and of X
   int per_step, total;  // the host has checked that the list has fewer than 2^31 tiles
   __device__ __forceinline__ explicit Plan(const MmArgs& a) {
@@ -450,10 +476,10 @@ struct Plan {
     it.step = t / per_step;
     int r = t - it.step * per_step;
     const int syms = a.G * per_sym;
-    it.need = 2u * (uint32_t)it.step * (uint32_t)(2 * per_sym + per_x);
+    it.need = kCtas * (uint32_t)it.step * (uint32_t)(2 * per_sym + per_x);
     if (r < 2 * syms) {
       it.role = r < syms ? GRAM : POLY;
-      if (it.role == POLY) r -= syms, it.need += 2u * per_sym;
+      if (it.role == POLY) r -= syms, it.need += kCtas * per_sym;
       it.g = r / per_sym;
       const int q = r - it.g * per_sym;
       // tiles on and below the diagonal, row by row
@@ -466,7 +492,7 @@ struct Plan {
     } else {
       r -= 2 * syms;
       it.role = it.step + 1 < a.steps ? NEXT : LAST;
-      it.need += 4u * per_sym;
+      it.need += 2u * kCtas * per_sym;
       it.g = r / per_x;
       const int q = r - it.g * per_x;
       it.m0 = q % tm * kTile, it.n0 = q / tm * kTile;
@@ -476,14 +502,16 @@ struct Plan {
   }
 };
 
-__global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
-    direction_product_kernel(const __grid_constant__ MmArgs args) {
+template <bool PAIR>
+__global__ void __launch_bounds__(kThreads, 1) direction_product_kernel(const __grid_constant__ MmArgs args) {
+  constexpr int kTile = Plan<PAIR>::kTile;
+  constexpr uint32_t kCols = 2 * kTile;  // of tensor memory
   extern __shared__ uint8_t smem_raw[];
   MmSmem& sm = *reinterpret_cast<MmSmem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const int warp = uniform_warp(), lane = threadIdx.x & 31;
-  const uint32_t rank = cta_rank();
-  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-  const Plan plan(args);
+  const uint32_t rank = PAIR ? cta_rank() : 0;
+  const int pair = PAIR ? blockIdx.x >> 1 : blockIdx.x, pairs = PAIR ? gridDim.x >> 1 : gridDim.x;
+  const Plan<PAIR> plan(args);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -492,7 +520,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sm.acc_full[i], 1);
-      mbar_init(&sm.acc_empty[i], 2 * kEpiWarps);  // the epilogue warps of both CTAs
+      mbar_init(&sm.acc_empty[i], (PAIR ? 2 : 1) * kEpiWarps);  // the epilogue warps of all its CTAs
     }
     for (int i = 0; i < kEpi; ++i) {
       mbar_init(&sm.epi_full[i], 1);
@@ -503,14 +531,19 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   if (warp == 2) {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem_base)),
-                 "r"(512u)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    if constexpr (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem_base)), "r"(kCols)
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem_base)), "r"(kCols)
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
-  pair_sync();
+  if constexpr (PAIR) pair_sync();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = sm.tmem_base;
 
@@ -537,20 +570,24 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
           break;
         }
         if (el) {
-          const uint32_t bar = in_cta(&sm.full[s], 0);
-          if (rank == 0) mbar_expect_tx(&sm.full[s], 4 * kOpBytes);  // two operands, two CTAs
+          const uint32_t bar = PAIR ? in_cta(&sm.full[s], 0) : 0;
+          if (rank == 0) mbar_expect_tx(&sm.full[s], (PAIR ? 4 : 2) * kOpBytes);  // two operands of every CTA
           const int k0 = kb * kBK;
+          auto load = [&](void* to, const CUtensorMap* map, int x, int y) {
+            if constexpr (PAIR) tma_load_pair(to, map, bar, x, y, q.g);
+            else tma_load_3d(to, map, &sm.full[s], x, y, q.g);
+          };
           if (!a_mn) {
-            tma_load_pair(sm.a[s], ma, bar, k0, m0, q.g);
+            load(sm.a[s], ma, k0, m0);
           } else {
-            tma_load_pair(sm.a[s], ma, bar, m0, k0, q.g);
-            tma_load_pair(sm.a[s] + kOpBytes / 2, ma, bar, m0 + 64, k0, q.g);
+            load(sm.a[s], ma, m0, k0);
+            load(sm.a[s] + kOpBytes / 2, ma, m0 + 64, k0);
           }
           if (!b_mn) {
-            tma_load_pair(sm.b[s], mb, bar, k0, n0, q.g);
+            load(sm.b[s], mb, k0, n0);
           } else {
-            tma_load_pair(sm.b[s], mb, bar, n0, k0, q.g);
-            tma_load_pair(sm.b[s] + kOpBytes / 2, mb, bar, n0 + 64, k0, q.g);
+            load(sm.b[s], mb, n0, k0);
+            load(sm.b[s] + kOpBytes / 2, mb, n0 + 64, k0);
           }
         }
         if (++s == kStages) s = 0, ph ^= 1;
@@ -568,7 +605,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
       const Item q = plan.at(args, t);
       const int nk = (q.K + kBK - 1) / kBK, ab = i & 1;
       const bool a_mn = q.role == GRAM && args.tall, b_mn = q.role <= POLY ? a_mn : !args.tall;
-      // fp32 accumulators, fp16 operands, N = 256, M = 256
+      // fp32 accumulators, fp16 operands, M = N = kTile
       const uint32_t idesc = (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
                              ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
       const uint64_t a0 = smem_desc(smem_u32(sm.a[0]), a_mn ? kOpBytes / 2 : 16, 1024);
@@ -586,11 +623,11 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
         const uint64_t ad = a0 + (uint32_t)s * (kOpBytes >> 4), bd = b0 + (uint32_t)s * (kOpBytes >> 4);
 #pragma unroll
         for (int kk = 0; kk < kBK / 16; ++kk)
-          if (el) mma_pair(acc, ad + kk * a_step, bd + kk * b_step, idesc, (kb > 0 || kk > 0) ? 1u : 0u);
-        if (el) commit_pair(&sm.empty[s]);
+          if (el) mma_of<PAIR>(acc, ad + kk * a_step, bd + kk * b_step, idesc, (kb > 0 || kk > 0) ? 1u : 0u);
+        if (el) commit_of<PAIR>(&sm.empty[s]);
         if (++s == kStages) s = 0, ph ^= 1;
       }
-      if (ok && el) commit_pair(&sm.acc_full[ab]);
+      if (ok && el) commit_of<PAIR>(&sm.acc_full[ab]);
     }
   } else if (warp == 3) {
     const bool el = elect_one();
@@ -794,15 +831,20 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
-      if (lane == 0) arrive_at(in_cta(&sm.acc_empty[ab], 0));
+      if (lane == 0) {
+        if constexpr (PAIR) arrive_at(in_cta(&sm.acc_empty[ab], 0));
+        else mbar_arrive(&sm.acc_empty[ab]);
+      }
     }
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
-  pair_sync();  // no CTA leaves while the other may still signal its barriers or read its operands
+  if constexpr (PAIR) pair_sync();  // no CTA leaves while the other may still signal its barriers or read its operands
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  if (warp == 2)
-    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  if (warp == 2) {
+    if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols) : "memory");
+  }
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -844,16 +886,6 @@ constexpr size_t res_smem(int rows) {
   return 1024 + (size_t)rows * 2 * kPiece + (NP / 64) * 128 * kPiece + 128 * 128 * 4 + sizeof(ResTail);
 }
 
-__device__ __forceinline__ void mma_one(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-__device__ __forceinline__ void commit_one(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
 __device__ __forceinline__ uint4 lds16_at(uint32_t cluster_addr) {
   uint4 v;
   asm volatile("ld.shared::cluster.v4.b32 {%0,%1,%2,%3}, [%4];"
@@ -1405,29 +1437,74 @@ bool half_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, int6
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The pairs of CTAs that are resident at once on device `dev` (0: an error).
-int resident_pairs(int dev, size_t smem, cudaError_t* err) {
-  static std::atomic<int> known{0};  // (device + 1) << 16 | pairs
+// The CTAs (PAIR: in pairs) that are resident at once on device `dev` (0: an error), and the kernel's shared-memory limit raised.
+template <bool PAIR>
+int resident_product_ctas(int dev, size_t smem, cudaError_t* err) {
+  static std::atomic<int> known{0};  // (device + 1) << 16 | CTAs
   const int k = known;
   if (k >> 16 == dev + 1) return k & 0xffff;
-  *err = cudaFuncSetAttribute(direction_product_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  *err = cudaFuncSetAttribute(direction_product_kernel<PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (*err != cudaSuccess) return 0;
-  int sms = 0, clusters = 0;
+  int sms = 0, n = 0;
   *err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (*err != cudaSuccess) return 0;
+  if (PAIR) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(sms / 2 * 2);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2, attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr, cfg.numAttrs = 1;
+    *err = cudaOccupancyMaxActiveClusters(&n, direction_product_kernel<PAIR>, &cfg);
+    n = 2 * std::min(n, sms / 2);
+  } else {
+    *err = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, direction_product_kernel<PAIR>, kThreads, smem);
+    n = std::min(n, 1) * sms;
+  }
+  if (*err != cudaSuccess || n < 1) return 0;
+  known = (dev + 1) << 16 | n;
+  return n;
+}
+
+// Whether pairs of CTAs on 256 x 256 tiles are the faster, by a model of a step's three phases: rounds of tiles, each the longer
+// of the products' time per k-block of 64 (600 cycles for a pair; 450 for a CTA alone, whose tile a quarter the size needs
+// half the operand bytes) and what a tile costs beside them (from the wait for its matrix's last phase to its count: 11,000
+// and 7,000 cycles).
+bool direction_pairs(int G, int64_t rows, int64_t cols) {
+  const int64_t n = std::min(rows, cols), m = std::max(rows, cols);
+  auto cost = [&](int tile, int workers, int per_block, int beside) {
+    const int64_t ts = (n + tile - 1) / tile, sym = ts * (ts + 1) / 2 * G;
+    const int64_t x = ((rows + tile - 1) / tile) * ((cols + tile - 1) / tile) * G;
+    auto phase = [&](int64_t tiles, int64_t k) {
+      return (tiles + workers - 1) / workers * ((k + kBK - 1) / kBK) * per_block + beside;
+    };
+    return phase(sym, m) + phase(sym, n) + phase(x, n);
+  };
+  return cost(256, kNumSMs / 2, 600, 11000) <= cost(128, kNumSMs, 450, 7000);
+}
+
+template <bool PAIR>
+cudaError_t launch_products(const MmArgs& a, cudaStream_t st) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const size_t smem = sizeof(MmSmem) + 1024;
+  const int ctas = resident_product_ctas<PAIR>(dev, smem, &e);
+  if (ctas < 1) return e == cudaSuccess ? cudaErrorInvalidConfiguration : e;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(sms / 2 * 2);
+  cfg.gridDim = dim3(ctas);
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 2, attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr, cfg.numAttrs = 1;
-  *err = cudaOccupancyMaxActiveClusters(&clusters, direction_product_kernel, &cfg);
-  if (*err != cudaSuccess || clusters < 1) return 0;
-  const int pairs = std::min(clusters, sms / 2);
-  known = (dev + 1) << 16 | pairs;
-  return pairs;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeCooperative;
+  attr[0].val.cooperative = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = PAIR ? 2 : 1, attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr, cfg.numAttrs = PAIR ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, direction_product_kernel<PAIR>, a);
 }
 
 // CTAs per matrix of the resident form (a power of two up to 8, the portable cluster size), or 0: it does not fit.
@@ -1499,12 +1576,6 @@ cudaError_t run_direction(DirArgs d, const DirLayout& ly, uint8_t* ws, int steps
   if (a.o_tma)
     ok = ok && half_map(&a.om, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, d.o, d.cols, d.rows, d.cols, d.o_gs, d.G, kHalf);
   if (!ok) return cudaErrorInvalidValue;
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  const size_t smem = sizeof(MmSmem) + 1024;
-  const int pairs = resident_pairs(dev, smem, &e);
-  if (pairs < 1) return e == cudaSuccess ? cudaErrorInvalidConfiguration : e;
   const dim3 grid(ly.chunks, d.G);
   // values per access: a row of h and l is 32-byte aligned, so a vector that divides the columns stays within a row
   auto aligned = [&](int v) {
@@ -1515,20 +1586,11 @@ cudaError_t run_direction(DirArgs d, const DirLayout& ly, uint8_t* ws, int steps
     const cudaError_t r = launch_pdl(momentum, grid, dim3(kMomThreads), 0, st, d);
     return r == cudaSuccess ? launch_pdl(normalise, grid, dim3(kMomThreads), 0, st, d) : r;
   };
-  e = aligned(8)   ? prepare(direction_momentum_kernel<8>, direction_normalise_kernel<8>)
-      : aligned(4) ? prepare(direction_momentum_kernel<4>, direction_normalise_kernel<4>)
-                   : prepare(direction_momentum_kernel<1>, direction_normalise_kernel<1>);
+  cudaError_t e = aligned(8) ? prepare(direction_momentum_kernel<8>, direction_normalise_kernel<8>)
+                  : aligned(4) ? prepare(direction_momentum_kernel<4>, direction_normalise_kernel<4>)
+                               : prepare(direction_momentum_kernel<1>, direction_normalise_kernel<1>);
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(2 * pairs);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeCooperative;
-  attr[0].val.cooperative = 1;
-  cfg.attrs = attr, cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, direction_product_kernel, a);
+  return direction_pairs(d.G, d.rows, d.cols) ? launch_products<true>(a, st) : launch_products<false>(a, st);
 }
 
 }  // namespace
@@ -1584,7 +1646,7 @@ lsgd_status lsgd_orthogonal_direction(float* u, int64_t u_gs, const void* g, int
            (momentum != 0.f && (overlap(u, span_u, g, span_g) || overlap(u, span_u, o, span_o) ||
                                 overlap(workspace, ly.bytes, u, span_u))))
     bad = "tensors overlap";
-  const int64_t ts = (ly.n + kTile - 1) / kTile, tx = ((rows + kTile - 1) / kTile) * ((cols + kTile - 1) / kTile);
+  const int64_t ts = (ly.n + 127) / 128, tx = ((rows + 127) / 128) * ((cols + 127) / 128);
   if (!bad && G * (ts * (ts + 1) + tx) * steps > 0x3fffffff) bad = "too many matrices of this size in one call";
   if (bad) return dir_error(LSGD_EINVAL, fn, bad);
   DirArgs d{};
