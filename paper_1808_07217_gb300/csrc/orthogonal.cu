@@ -99,6 +99,11 @@ __device__ __forceinline__ void load_f32(const float* p, float (&v)[V]) {
     }
   }
 }
+// One gradient value whose type is known.
+template <bool BF16>
+__device__ __forceinline__ float grad_value(const void* g, int64_t i) {
+  return BF16 ? bf2f(static_cast<const uint16_t*>(g)[i]) : static_cast<const float*>(g)[i];
+}
 template <int V>
 __device__ __forceinline__ void load_grad(const DirArgs& a, int64_t i, float (&v)[V]) {
   if (!a.g_bf16) {
@@ -851,14 +856,14 @@ __global__ void __launch_bounds__(kThreads, 1) direction_product_kernel(const __
 // Resident form: a matrix of a smaller side n <= 128 in the shared memory of one CTA or a cluster, all of it in one launch
 //
 // X is held with its longer side down, [m][n], a CTA of the cluster having up to 512 of the m rows and a thread one row.
-// A row is 128 fp16 values, two swizzled pieces of 64: up to n = 64 h and l, above it h alone (l in its thread's
-// registers).  A step:
+// A row is 128 fp16 values, two swizzled pieces of 64: up to n = 64 h and l, above it h alone (l in tensor memory, 64 columns
+// beside the two accumulators).  A step:
 //   1. tcgen05: [h l]^T [h l] over the CTA's rows into tensor memory, 128 x 128; above 64 that is A, up to 64 A is the sum
 //      of its parts h h, h l and l h;
 //   2. the CTAs' sums are added up in rank order (each CTA a slice of A, through distributed shared memory) and the
 //      slices given to all;
 //   3. tcgen05: A A, then P in A's place;
-//   4. tcgen05: X P, 128 rows to a tile; each thread updates its row from its tile.
+//   4. tcgen05: X P, 128 rows to a tile (above n = 64 two tiles at a time); each thread updates its row from its tile.
 // Up to n = 64 both h and l are multiplied, so that small matrices, whose roundings do not average out, are off by less
 // than 2.5e-3 too.  What a step costs is its chain of latencies (about 5 us at 100 x 4096 in eight CTAs), which the work
 // in it hardly lengthens.
@@ -906,6 +911,27 @@ __device__ __forceinline__ void vec8(uint32_t at, float (&f)[8]) {
   f[4] = __uint_as_float(b.x), f[5] = __uint_as_float(b.y), f[6] = __uint_as_float(b.z), f[7] = __uint_as_float(b.w);
 }
 
+// Eight accumulator columns of this warp's 32 rows, and the same stored.
+__device__ __forceinline__ void tmem_ld16_8(uint32_t at16, float (&v)[16], uint32_t at8, uint32_t (&w)[8]) {
+  uint32_t r[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%24];\n"
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%16,%17,%18,%19,%20,%21,%22,%23}, [%25];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(w[0]), "=r"(w[1]),
+        "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+      : "r"(at16), "r"(at8)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_st8(uint32_t at, const uint32_t (&w)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+               "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+
 template <int NP>
 __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResArgs a) {
   constexpr bool kBoth = NP == 64;  // l is in shared memory and multiplied too
@@ -923,8 +949,10 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
   const int n = a.n, m0 = rank * a.per, have = max(0, min(a.per, a.m - m0));  // this CTA's rows
   const bool tall = a.d.rows > a.d.cols;
   const int tiles = rows / 128;
-  uint32_t cols = 128;  // of tensor memory
-  while ((int)cols < tiles * NP) cols <<= 1;
+  // tensor memory: the symmetric products' 128 columns and the tiles' NP each, in the same place; above n = 64 two tiles'
+  // accumulators at a time and 64 columns of l for every tile behind them
+  const uint32_t low = kBoth || tiles > 1 ? 256 : 128;  // l's first column
+  const uint32_t cols = kBoth ? (tiles > 2 ? 256 : 128) : 2 * low;
 
   if (tid == 0) {
     for (int i = 0; i < 5; ++i) mbar_init(&tail.bar[i], 1);
@@ -937,7 +965,9 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
   }
   // rows and columns past the matrix are zero
   for (uint32_t i = tid * 16; i < 2 * xpiece; i += rows * 16) sts16(xs + i, make_uint4(0, 0, 0, 0));
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   pdl_begin();
 
   // momentum and the norm: this CTA's values, neighbouring ones by neighbouring threads
@@ -957,24 +987,24 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
     };
     // 16 values at a time, their loads before the first store
     constexpr int kAt = 16;
-    auto some = [&](auto value, int from, int step, int end, auto where) {
-      for (int b = from; b < end; b += kAt * step) {
-        float g[kAt][1], u[kAt];
+    auto some = [&](auto bf16, int64_t at, int64_t stride, int from, int step, int end, auto where) {
+      constexpr bool kBf16 = decltype(bf16)::value;
+      for (int b = from; b < end; b += kAt * step, at += kAt * stride) {
+        float g[kAt], u[kAt];
+        const float* up = d.u + uk + at;
 #pragma unroll
         for (int q = 0; q < kAt; ++q) {
-          g[q][0] = u[q] = 0.f;
-          if (b + q * step < end) {
-            load_grad<1>(d, gk + value(b + q * step), g[q]);
-            if (d.mom != 0.f) u[q] = d.u[uk + value(b + q * step)];
-          }
+          const bool in = b + q * step < end;
+          g[q] = in ? grad_value<kBf16>(d.g, gk + at + q * stride) : 0.f;
+          u[q] = in && d.mom != 0.f ? up[q * stride] : 0.f;
         }
 #pragma unroll
         for (int q = 0; q < kAt; ++q)
           if (b + q * step < end) {
-            float x = g[q][0];
+            float x = g[q];
             if (d.mom != 0.f) {
               const float t = fmaf(d.mom, u[q], x);
-              d.u[uk + value(b + q * step)] = t;
+              d.u[uk + at + q * stride] = t;
               x = d.nesterov ? fmaf(d.mom, t, x) : t;
             }
             norm_add(s, x);
@@ -982,10 +1012,12 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
           }
       }
     };
-    if (tall)
-      some([&](int e) { return m0 * n + e; }, tid, rows, have * n, [&](int e, float x) { keep(e / n, e % n, x); });
-    else if (tid < have)
-      some([&](int i) { return i * a.m + m0 + tid; }, 0, 1, n, [&](int i, float x) { keep(tid, i, x); });
+    auto all = [&](auto bf16) {
+      if (tall) some(bf16, (int64_t)m0 * n + tid, rows, tid, rows, have * n, [&](int e, float x) { keep(e / n, e % n, x); });
+      else if (tid < have) some(bf16, m0 + tid, a.m, 0, 1, n, [&](int i, float x) { keep(tid, i, x); });
+    };
+    if (d.g_bf16) all(std::true_type{});
+    else all(std::false_type{});
     float v[3] = {s.mid, s.big, s.small};
 #pragma unroll
     for (int j = 0; j < 3; ++j) {
@@ -1004,7 +1036,6 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
   }
   const uint32_t tmem = tail.tmem;
   const uint32_t stage = sums + warp * 4096;  // 32 x 32 fp32 values of a warp, where the sums are not in use
-  uint32_t lreg[kBoth ? 1 : NP / 2];
   {
     float t[3] = {0.f, 0.f, 0.f};
     for (int c = 0; c < a.cl; ++c)
@@ -1033,45 +1064,49 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
         sts16(row_at + ((q << 4) ^ turn), h);
         sts16(row_at + xpiece + ((q << 4) ^ turn), pack8(hi));
       }
-    } else {  // once more from L2, a row's values 32 at a time
+    } else {  // once more from L2, a row's values 16 at a time (rolled: code that runs once is fetched at its size)
+      const uint32_t ltile = tmem + low + (warp >> 2) * 64 + ((uint32_t)(warp & 3) << 21);
+      // 16 values' loads before they are used: value q at at + q stride where in(q)
+      auto batch = [&](auto bf16, int64_t at, int64_t stride, auto in, auto use) {
+        constexpr bool kBf16 = decltype(bf16)::value;
+        const bool want_g = d.mom == 0.f || d.nesterov, want_u = d.mom != 0.f;
+        const float* up = d.u + uk + at;
+        float g[16], u[16];
 #pragma unroll
-      for (int b = 0; b < NP; b += 32) {
-        float x[32];
-        auto batch = [&](auto at, auto use) {  // 16 values' loads before they are used
+        for (int q = 0; q < 16; ++q) {
+          g[q] = want_g && in(q) ? grad_value<kBf16>(d.g, gk + at + q * stride) : 0.f;
+          u[q] = want_u && in(q) ? up[q * stride] : 0.f;
+        }
+        const float mg = want_g ? 1.f : 0.f, mu = !want_u ? 0.f : d.nesterov ? d.mom : 1.f;
 #pragma unroll
-          for (int half = 0; half < 32; half += 16) {
-            float g[16][1], u[16];
-#pragma unroll
-            for (int q = 0; q < 16; ++q) {
-              const int v = at(half + q);
-              g[q][0] = u[q] = 0.f;
-              if (v >= 0 && (d.mom == 0.f || d.nesterov)) load_grad<1>(d, gk + v, g[q]);
-              if (v >= 0 && d.mom != 0.f) u[q] = d.u[uk + v];
-            }
+        for (int q = 0; q < 16; ++q) use(q, fmaf(mu, u[q], mg * g[q]) * f.x * f.y);
+      };
+#pragma unroll 1
+      for (int b = 0; b < n; b += 16) {
+        float x[16];
+        auto all = [&](auto bf16) {
+          if (!tall) {
+            batch(bf16, (int64_t)b * a.m + m0 + tid, a.m, [&](int q) { return tid < have && b + q < n; },
+                  [&](int q, float v) { x[q] = v; });
+          } else {  // neighbouring lanes read neighbouring values; the warp's 32 x 16 values change places
+            const int row = lane >> 4, col = lane & 15;
+            batch(bf16, (int64_t)(m0 + warp * 32 + row) * n + b + col, 2 * n,
+                  [&](int q) { return warp * 32 + 2 * q + row < have && b + col < n; },
+                  [&](int q, float v) {
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(stage + (2 * q + row) * 64 + ((col ^ (q & 15)) << 2)), "f"(v) : "memory");
+                  });
+            __syncwarp();
 #pragma unroll
             for (int q = 0; q < 16; ++q)
-              use(half + q, (d.mom == 0.f ? g[q][0] : d.nesterov ? fmaf(d.mom, u[q], g[q][0]) : u[q]) * f.x * f.y);
+              asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[q]) : "r"(stage + lane * 64 + ((q ^ (lane >> 1 & 15)) << 2)) : "memory");
+            __syncwarp();
           }
         };
-        if (!tall) {
-          batch([&](int q) { return tid < have && b + q < n ? (b + q) * a.m + m0 + tid : -1; }, [&](int q, float v) {
+        if (d.g_bf16) all(std::true_type{});
+        else all(std::false_type{});
+        uint32_t low8[8];
 #pragma unroll
-            for (int w = 0; w < 32; ++w)
-              if (w == q) x[w] = v;
-          });
-        } else {  // neighbouring lanes read neighbouring values; the warp's 32 x 32 values change places
-          __syncwarp();
-          batch([&](int q) { return warp * 32 + q < have && b + lane < n ? (m0 + warp * 32 + q) * n + b + lane : -1; },
-                [&](int q, float v) {
-                  asm volatile("st.shared.f32 [%0], %1;" ::"r"(stage + q * 128 + ((lane ^ q) << 2)), "f"(v) : "memory");
-                });
-          __syncwarp();
-#pragma unroll
-          for (int q = 0; q < 32; ++q)
-            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[q]) : "r"(stage + lane * 128 + ((lane ^ q) << 2)) : "memory");
-        }
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
+        for (int p = 0; p < 2; ++p) {
           const int q = b / 8 + p;
           float v[8], hi[8];
 #pragma unroll
@@ -1082,9 +1117,11 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
           for (int i = 0; i < 8; ++i) hi[i] = v[i] - hi[i];
           const uint4 lo = pack8(hi);
           sts16(row_at + (q >> 3) * xpiece + (((q & 7) << 4) ^ turn), w);
-          lreg[4 * q] = lo.x, lreg[4 * q + 1] = lo.y, lreg[4 * q + 2] = lo.z, lreg[4 * q + 3] = lo.w;
+          low8[4 * p] = lo.x, low8[4 * p + 1] = lo.y, low8[4 * p + 2] = lo.z, low8[4 * p + 3] = lo.w;
         }
+        tmem_st8(ltile + b / 2, low8);
       }
+      asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
     }
   }
 
@@ -1223,23 +1260,6 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     // 4. X P
-    if (warp == 0) {
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const bool el = elect_one();
-      constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(NP >> 3) << 17) | ((128u >> 4) << 24);
-      const uint64_t x0 = smem_desc(xs, 16, 1024), p0 = smem_desc(as, 16, 1024);
-      for (int t = 0; t < tiles; ++t) {
-        const uint64_t xt = x0 + (uint32_t)(t * 128 * kPiece >> 4);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {  // up to n = 64 the h, then the l of four slices of 16 columns; else eight of h
-          const int slice = kBoth ? i & 3 : i;
-          const uint64_t xa = xt + (i >> 2) * (xpiece >> 4) + (i & 3) * 2;
-          const uint64_t pb = p0 + (kBoth ? 0 : (i >> 2) * (128 * kPiece >> 4)) + (i & 3) * 2;
-          if (el && slice < kn) mma_one(tmem + t * NP, xa, pb, idesc, i > 0);
-        }
-        if (el) commit_one(&tail.bar[1 + t]);
-      }
-    }
     float top = 0.f;  // t of the number formats above
     if (!kBoth && step + 2 >= a.steps) {
       top = -INFINITY;
@@ -1247,15 +1267,42 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
 #pragma unroll
       for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
     }
-    wait_bar_warp(&tail.bar[1 + (warp >> 2)], ph2);
-    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const bool last = step + 1 == a.steps;
-    // (rolled where nothing is held in registers across it: the instruction cache holds a step then)
-#pragma unroll(kBoth ? 1 : NP / 16)
-    for (int c = 0; c < NP; c += 16) {
-      if (c < n) {
+    const int tile = warp >> 2, at_once = kBoth ? tiles : 2;
+#pragma unroll 1
+    for (int t0 = 0; t0 < tiles; t0 += at_once) {
+      if (t0 > 0) {  // the accumulators have been read
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncthreads();
+      }
+      if (warp == 0) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const bool el = elect_one();
+        constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(NP >> 3) << 17) | ((128u >> 4) << 24);
+        const uint64_t x0 = smem_desc(xs, 16, 1024), p0 = smem_desc(as, 16, 1024);
+        for (int t = t0; t < min(tiles, t0 + at_once); ++t) {
+          const uint64_t xt = x0 + (uint32_t)(t * 128 * kPiece >> 4);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {  // up to n = 64 the h, then the l of four slices of 16 columns; else eight of h
+            const int slice = kBoth ? i & 3 : i;
+            const uint64_t xa = xt + (i >> 2) * (xpiece >> 4) + (i & 3) * 2;
+            const uint64_t pb = p0 + (kBoth ? 0 : (i >> 2) * (128 * kPiece >> 4)) + (i & 3) * 2;
+            if (el && slice < kn) mma_one(tmem + (t - t0) * NP, xa, pb, idesc, i > 0);
+          }
+          if (el) commit_one(&tail.bar[1 + t]);
+        }
+        __syncwarp();
+      }
+      if (tile < t0 || tile >= t0 + at_once) continue;
+      wait_bar_warp(&tail.bar[1 + tile], ph2);
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const uint32_t dtile = tmem + (tile - t0) * NP + lanes, ltile = tmem + low + tile * 64 + lanes;
+#pragma unroll 1
+      for (int c = 0; c < n; c += 16) {  // (rolled: the instruction cache holds a step then)
         float v[16];
-        tmem_ld16(tmem + (warp >> 2) * NP + c + lanes, v);
+        uint32_t low8[8];
+        if constexpr (kBoth) tmem_ld16(dtile + c, v);
+        else tmem_ld16_8(dtile + c, v, ltile + c / 2, low8);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const int q = c / 8 + j;
@@ -1264,7 +1311,7 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
           unpack8(lds16(at), f);
           vec8(smem_u32(tail.d) + 32 * q, dj);
           if constexpr (kBoth) unpack8(lds16(at + xpiece), lo);
-          else unpack8(make_uint4(lreg[4 * q], lreg[4 * q + 1], lreg[4 * q + 2], lreg[4 * q + 3]), lo);
+          else unpack8(make_uint4(low8[4 * j], low8[4 * j + 1], low8[4 * j + 2], low8[4 * j + 3]), lo);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const float t = kA + dj[i];
@@ -1279,7 +1326,7 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
             for (int i = 0; i < 8; ++i) hi[i] = f[i] - hi[i];
             const uint4 l = pack8(hi);
             if constexpr (kBoth) sts16(at + xpiece, l);
-            else lreg[4 * q] = l.x, lreg[4 * q + 1] = l.y, lreg[4 * q + 2] = l.z, lreg[4 * q + 3] = l.w;
+            else low8[4 * j] = l.x, low8[4 * j + 1] = l.y, low8[4 * j + 2] = l.z, low8[4 * j + 3] = l.w;
           } else if (!tall) {
             uint16_t* o = d.o + k * d.o_gs;
             if (tid < have)
@@ -1292,6 +1339,7 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
             sts16(stage + lane * 32 + ((j ^ (lane >> 2 & 1)) << 4), pack8_bf16(f));
           }
         }
+        if (!kBoth && !last) tmem_st8(ltile + c / 2, low8);
         if (last && tall) {
           __syncwarp();
           uint16_t* o = d.o + k * d.o_gs + (int64_t)(m0 + warp * 32) * n + c + (lane & 15);
@@ -1307,6 +1355,7 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
           __syncwarp();
         }
       }
+      if constexpr (!kBoth) asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
     }
     ph2 ^= 1;
   }
