@@ -1162,34 +1162,33 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
     else __syncthreads();
     // 2. this CTA's slice of A: rows rank, rank + cl, ...; four columns to a thread
     {
-      auto slice = [&](auto one) {
-        constexpr bool kOne = decltype(one)::value;
-        const int per_row = n16 / 4, mine = kOne ? n16 : (n16 - rank + a.cl - 1) / a.cl;
+      auto slice = [&](auto ctas) {
+        constexpr int kCtas = decltype(ctas)::value;
+        constexpr bool kOne = kCtas == 1;
+        const int per_row = n16 / 4, mine = (n16 - rank + kCtas - 1) / kCtas;
         for (int e = tid; e < mine * per_row; e += rows) {
-          const int i = kOne ? e / per_row : rank + e / per_row * a.cl, j = e % per_row;
+          const int i = rank + e / per_row * kCtas, j = e % per_row;
           float f[4] = {0.f, 0.f, 0.f, 0.f};
-          constexpr int kParts = kBoth ? 3 : 1, kCtas = kOne ? 1 : 8;
+          constexpr int kParts = kBoth ? 3 : 1;
           uint4 w[kCtas][kParts];  // every CTA's parts, loaded before the first is used
 #pragma unroll
-          for (int c = 0; c < kCtas; ++c)
-            if (kOne || c < a.cl) {
-              const uint32_t from = kOne ? sums : at_rank(sums, c);
-              auto part = [&](int row, int piece) {
-                const uint32_t at = from + row * 512 + ((piece ^ (row & 31)) << 4);
-                return kOne ? lds16(at) : lds16_at(at);
-              };
-              w[c][0] = part(i, j);
-              if constexpr (kBoth) w[c][1] = part(i, 16 + j), w[c][2] = part(64 + i, j);
-            }
+          for (int c = 0; c < kCtas; ++c) {
+            const uint32_t from = kOne ? sums : at_rank(sums, c);
+            auto part = [&](int row, int piece) {
+              const uint32_t at = from + row * 512 + ((piece ^ (row & 31)) << 4);
+              return kOne ? lds16(at) : lds16_at(at);
+            };
+            w[c][0] = part(i, j);
+            if constexpr (kBoth) w[c][1] = part(i, 16 + j), w[c][2] = part(64 + i, j);
+          }
 #pragma unroll
-          for (int c = 0; c < kCtas; ++c)
-            if (kOne || c < a.cl) {
+          for (int c = 0; c < kCtas; ++c) {
 #pragma unroll
-              for (int q = 0; q < kParts; ++q) {
-                f[0] += __uint_as_float(w[c][q].x), f[1] += __uint_as_float(w[c][q].y);
-                f[2] += __uint_as_float(w[c][q].z), f[3] += __uint_as_float(w[c][q].w);
-              }
+            for (int q = 0; q < kParts; ++q) {
+              f[0] += __uint_as_float(w[c][q].x), f[1] += __uint_as_float(w[c][q].y);
+              f[2] += __uint_as_float(w[c][q].z), f[3] += __uint_as_float(w[c][q].w);
             }
+          }
           float diag = 0.f;
           const bool on = j == i >> 2;
 #pragma unroll
@@ -1205,15 +1204,18 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
             asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(b0), "r"(b1) : "memory");
             if (on) tail.da[i] = diag;
           } else {
-            for (int c = 0; c < a.cl; ++c) {
+#pragma unroll
+            for (int c = 0; c < kCtas; ++c) {
               asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(at_rank(to, c)), "r"(b0), "r"(b1) : "memory");
               if (on) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at_rank(da, c)), "f"(diag) : "memory");
             }
           }
         }
       };
-      if (a.cl == 1) slice(std::true_type{});
-      else slice(std::false_type{});
+      if (a.cl == 1) slice(std::integral_constant<int, 1>{});
+      else if (a.cl == 2) slice(std::integral_constant<int, 2>{});
+      else if (a.cl == 4) slice(std::integral_constant<int, 4>{});
+      else slice(std::integral_constant<int, 8>{});
     }
     if (a.cl > 1) pair_sync();
     // 3. A A, and P in A's place
