@@ -508,7 +508,8 @@ struct Plan {
 };
 
 template <bool PAIR>
-__global__ void __launch_bounds__(kThreads, 1) direction_product_kernel(const __grid_constant__ MmArgs args) {
+__global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(PAIR ? 2 : 1, 1, 1)
+    direction_product_kernel(const __grid_constant__ MmArgs args) {
   constexpr int kTile = Plan<PAIR>::kTile;
   constexpr uint32_t kCols = 2 * kTile;  // of tensor memory
   extern __shared__ uint8_t smem_raw[];
@@ -1549,12 +1550,10 @@ cudaError_t launch_products(const MmArgs& a, cudaStream_t st) {
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr[2];
+  cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeCooperative;
   attr[0].val.cooperative = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = PAIR ? 2 : 1, attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr, cfg.numAttrs = PAIR ? 2 : 1;
+  cfg.attrs = attr, cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, direction_product_kernel<PAIR>, a);
 }
 
