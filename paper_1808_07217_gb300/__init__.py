@@ -572,7 +572,8 @@ def lsgd_batchnorm_stats_noalloc(y, P: int, C: int, G: int, mean, rstd, stream=N
                                               _ptr(rstd), ctypes.c_void_p(stream)))
 
 
-_TYPES = {}
+_TYPES = {}    # torch dtype -> FP32 or BF16, filled by the first call
+_WANTED = {}   # FP32, BF16 -> torch dtype
 
 
 def _type_of(t):
@@ -580,32 +581,39 @@ def _type_of(t):
     if not _TYPES:
         import torch
 
-        _TYPES.update({torch.float32: FP32, torch.bfloat16: BF16})
+        _WANTED.update({FP32: torch.float32, BF16: torch.bfloat16})
+        _TYPES.update({v: k for k, v in _WANTED.items()})
     ty = _TYPES.get(t.dtype)
     if ty is None:
         raise LsgdError(EINVAL, f"a float32 or bfloat16 tensor is wanted, got {t.dtype}")
     return ty
 
 
-def _checked(*tensors):
-    """Checks (name, tensor or None, number of elements, type or None for either) rows: CUDA tensors of one
-    device, contiguous and large enough, so that no kernel leaves them.  Returns the device's index."""
-    dev = None
-    for name, t, n, ty in tensors:
+def _checked(first, *others):
+    """Checks rows of (name, tensor or None, number of elements, FP32 or BF16): CUDA tensors of one device, contiguous
+    and large enough, so that no kernel leaves them.  Returns the device's index.  (The calls below are of a few
+    microseconds, so each row costs as few calls as it can.)"""
+    dev = first[1].get_device()
+    if dev < 0:
+        raise LsgdError(EINVAL, f"{first[0]}: a CUDA tensor is wanted")
+    for name, t, n, ty in (first, *others):
         if t is None:
             continue
-        at = t.get_device()
-        if at < 0:
-            raise LsgdError(EINVAL, f"{name}: a CUDA tensor is wanted")
-        if _type_of(t) != ty and ty is not None:
+        if t.dtype is not _WANTED[ty]:
             raise LsgdError(EINVAL, f"{name}: type {t.dtype} is not taken here")
+        if t.get_device() != dev:
+            raise LsgdError(EINVAL, f"{name}: a CUDA tensor on device {dev} is wanted")
         if t.numel() < n or not t.is_contiguous():
             raise LsgdError(EINVAL, f"{name}: a contiguous tensor of at least {n} elements is wanted")
-        if dev is None:
-            dev = at
-        elif at != dev:
-            raise LsgdError(EINVAL, f"{name}: on device {at}, others on {dev}")
     return dev
+
+
+def _stream_of(dev):
+    """The current stream of device `dev`, by PyTorch's cheaper query where this version has it."""
+    import torch
+
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(dev) if raw is not None else torch.cuda.current_stream(dev).cuda_stream
 
 
 def _launch(dev, stream, workspace, nbytes, fn, args):
@@ -618,8 +626,7 @@ def _launch(dev, stream, workspace, nbytes, fn, args):
     if torch.cuda.current_device() != dev:
         with torch.cuda.device(dev):
             return _launch(dev, stream, workspace, nbytes, fn, args)
-    cur = torch.cuda.current_stream().cuda_stream
-    st = cur if stream is None else int(stream)
+    st = _stream_of(dev) if stream is None else int(stream)
     if workspace is False:
         status = fn(*args, st)
     else:
@@ -628,7 +635,7 @@ def _launch(dev, stream, workspace, nbytes, fn, args):
             if nbytes:
                 ws = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
                 wp, wn = ws.data_ptr(), nbytes
-                if st != cur:
+                if stream is not None and st != _stream_of(dev):
                     ws.record_stream(torch.cuda.ExternalStream(st))
         elif ws.get_device() != dev or not ws.is_contiguous():
             raise LsgdError(EINVAL, f"workspace: a contiguous tensor on CUDA device {dev} is wanted")
@@ -656,10 +663,11 @@ def lsgd_groupnorm_forward(x, gamma, beta, y, mean, rstd, G: int, B: int, P: int
     nbytes = lsgd_groupnorm_workspace(G, B, P, C, groups)
     par_gs = par_gs or C
     n, ng, npar = G * B * P * C, G * B * groups, (G - 1) * par_gs + C
-    dev = _checked(("x", x, n, None), ("y", y, n, None), ("gamma", gamma, npar, FP32), ("beta", beta, npar, FP32),
+    xt, yt = _type_of(x), _type_of(y)
+    dev = _checked(("x", x, n, xt), ("y", y, n, yt), ("gamma", gamma, npar, FP32), ("beta", beta, npar, FP32),
                    ("mean", mean, ng, FP32), ("rstd", rstd, ng, FP32))
     _launch(dev, stream, workspace, nbytes, lib().lsgd_groupnorm_forward,
-            (x.data_ptr(), _type_of(x), gamma.data_ptr(), beta.data_ptr(), par_gs, y.data_ptr(), _type_of(y),
+            (x.data_ptr(), xt, gamma.data_ptr(), beta.data_ptr(), par_gs, y.data_ptr(), yt,
              mean.data_ptr(), rstd.data_ptr(), G, B, P, C, groups, eps, act))
 
 
@@ -699,10 +707,11 @@ def lsgd_orthogonal_direction(u, g, o, G: int, rows: int, cols: int, momentum: f
     u_gs, g_gs, o_gs = u_gs or n, g_gs or n, o_gs or n
     if u is None and momentum:
         raise LsgdError(EINVAL, "u: wanted with momentum")
-    dev = _checked(("g", g, (G - 1) * g_gs + n, None), ("u", u, (G - 1) * u_gs + n, FP32),
+    gt = _type_of(g)
+    dev = _checked(("g", g, (G - 1) * g_gs + n, gt), ("u", u, (G - 1) * u_gs + n, FP32),
                    ("o", o, (G - 1) * o_gs + n, BF16))
     _launch(dev, stream, workspace, nbytes, lib().lsgd_orthogonal_direction,
-            (u.data_ptr() if u is not None else None, u_gs, g.data_ptr(), _type_of(g), g_gs, o.data_ptr(), o_gs, G,
+            (u.data_ptr() if u is not None else None, u_gs, g.data_ptr(), gt, g_gs, o.data_ptr(), o_gs, G,
              rows, cols, momentum, nesterov, steps))
 
 
@@ -712,6 +721,7 @@ def lsgd_direction_update(w, o, Wb, G: int, n: int, lr: float, scale: float = 1.
     None) = bf16(w); w and Wb at stride w_gs, o at o_gs elements (0: n)."""
     w_gs, o_gs = w_gs or n, o_gs or n
     span = (G - 1) * w_gs + n
+    _type_of(w)
     dev = _checked(("w", w, span, FP32), ("o", o, (G - 1) * o_gs + n, BF16), ("Wb", Wb, span, BF16))
     _launch(dev, stream, False, 0, lib().lsgd_direction_update,
             (w.data_ptr(), w_gs, o.data_ptr(), o_gs, Wb.data_ptr() if Wb is not None else None, G, n, lr, scale,
