@@ -854,15 +854,17 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(PAIR ? 2 : 1, 1,
 }
 
 // ------------------------------------------------------------------------------------------------
-// Resident form: a matrix of a smaller side n <= 128 in the shared memory of one CTA or a cluster, all of it in one launch
+// Resident form: a matrix of a smaller side n <= 128 in the shared memory of one CTA or several, all of it in one launch
 //
-// X is held with its longer side down, [m][n], a CTA of the cluster having up to 512 of the m rows and a thread one row.
+// X is held with its longer side down, [m][n], a CTA having up to 512 of the m rows and a thread one row.  The CTAs of a
+// matrix are a cluster; or (GLOBAL) any CTAs of a cooperative launch, in groups that take one matrix after another and exchange
+// through global memory, where a cluster would be too small or leave SMs idle.
 // A row is 128 fp16 values, two swizzled pieces of 64: up to n = 64 h and l, above it h alone (l in tensor memory, 64 columns
 // beside the two accumulators).  A step:
 //   1. tcgen05: [h l]^T [h l] over the CTA's rows into tensor memory, 128 x 128; above 64 that is A, up to 64 A is the sum
 //      of its parts h h, h l and l h;
 //   2. the CTAs' sums are added up in rank order (each CTA a slice of A, through distributed shared memory) and the
-//      slices given to all;
+//      slices given to all;  (GLOBAL: the same through L2, two counted barriers)
 //   3. tcgen05: A A, then P in A's place;
 //   4. tcgen05: X P, 128 rows to a tile (above n = 64 two tiles at a time); each thread updates its row from its tile.
 // Up to n = 64 both h and l are multiplied, so that small matrices, whose roundings do not average out, are off by less
@@ -876,6 +878,13 @@ constexpr int kPiece = 128;      // bytes of a piece's row
 struct ResArgs {
   DirArgs d;
   int n, m, cl, per, steps;  // per: rows of a CTA
+  // GLOBAL: groups of cl CTAs, and per group the CTAs' sums [cl][n16][n16], A [n16][n16] without its diagonal, the diagonal
+  // [n16], the CTAs' norm sums [cl][3] and the count of barrier arrivals
+  int groups;
+  float* part;
+  uint2* full;
+  float *diag, *norms;
+  uint32_t* count;
 };
 
 // Shared memory, from a 1024-byte boundary: X's two pieces [2][rows][64], A and P [NP / 64][128][64], the sums [128][128] in
@@ -933,7 +942,7 @@ __device__ __forceinline__ void tmem_st8(uint32_t at, const uint32_t (&w)[8]) {
                : "memory");
 }
 
-template <int NP>
+template <int NP, bool GLOBAL>
 __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResArgs a) {
   constexpr bool kBoth = NP == 64;  // l is in shared memory and multiplied too
   extern __shared__ uint8_t smem_raw[];
@@ -945,8 +954,7 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
   const uint32_t tail_at = sums + 128 * 128 * 4;
   ResTail& tail = *reinterpret_cast<ResTail*>(smem_raw + (tail_at - smem_u32(smem_raw)));
   const int warp = uniform_warp(), lane = threadIdx.x & 31, tid = threadIdx.x;
-  const int rank = a.cl > 1 ? (int)cta_rank() : 0;
-  const int64_t k = blockIdx.x / a.cl;
+  const int rank = GLOBAL ? blockIdx.x % a.cl : a.cl > 1 ? (int)cta_rank() : 0, group = blockIdx.x / a.cl;
   const int n = a.n, m0 = rank * a.per, have = max(0, min(a.per, a.m - m0));  // this CTA's rows
   const bool tall = a.d.rows > a.d.cols;
   const int tiles = rows / 128;
@@ -964,408 +972,477 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  // rows and columns past the matrix are zero
-  for (uint32_t i = tid * 16; i < 2 * xpiece; i += rows * 16) sts16(xs + i, make_uint4(0, 0, 0, 0));
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   pdl_begin();
 
-  // momentum and the norm: this CTA's values, neighbouring ones by neighbouring threads
-  const DirArgs& d = a.d;
-  const int64_t gk = k * d.g_gs, uk = k * d.u_gs;
-  // the place of value (j, i), row j of this CTA's and column i of X
-  auto place = [&](int j, int i) -> int { return tall ? (m0 + j) * n + i : i * a.m + m0 + j; };
-  const uint32_t row_at = xs + tid * kPiece, turn = (tid & 7) << 4;  // 16-byte piece p of a row stands at p ^ (row & 7)
-  {
-    NormSums s{0.f, 0.f, 0.f};
-    // value (j, i) of up to n = 64 waits for the norm in row j, 64 fp32 values to a row's two pieces
-    auto keep = [&](int j, int i, float x) {
-      if constexpr (kBoth) {
-        const uint32_t at = xs + (i >> 5) * xpiece + j * kPiece + ((((i & 31) >> 2) ^ (j & 7)) << 4) + (i & 3) * 4;
-        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory");
-      }
-    };
-    // 16 values at a time, their loads before the first store
-    constexpr int kAt = 16;
-    auto some = [&](auto bf16, int64_t at, int64_t stride, int from, int step, int end, auto where) {
-      constexpr bool kBf16 = decltype(bf16)::value;
-      for (int b = from; b < end; b += kAt * step, at += kAt * stride) {
-        float g[kAt], u[kAt];
-        const float* up = d.u + uk + at;
-#pragma unroll
-        for (int q = 0; q < kAt; ++q) {
-          const bool in = b + q * step < end;
-          g[q] = in ? grad_value<kBf16>(d.g, gk + at + q * stride) : 0.f;
-          u[q] = in && d.mom != 0.f ? up[q * stride] : 0.f;
-        }
-#pragma unroll
-        for (int q = 0; q < kAt; ++q)
-          if (b + q * step < end) {
-            float x = g[q];
-            if (d.mom != 0.f) {
-              const float t = fmaf(d.mom, u[q], x);
-              d.u[uk + at + q * stride] = t;
-              x = d.nesterov ? fmaf(d.mom, t, x) : t;
-            }
-            norm_add(s, x);
-            where(b + q * step, x);
-          }
-      }
-    };
-    auto all = [&](auto bf16) {
-      if (tall) some(bf16, (int64_t)m0 * n + tid, rows, tid, rows, have * n, [&](int e, float x) { keep(e / n, e % n, x); });
-      else if (tid < have) some(bf16, m0 + tid, a.m, 0, 1, n, [&](int i, float x) { keep(tid, i, x); });
-    };
-    if (d.g_bf16) all(std::true_type{});
-    else all(std::false_type{});
-    float v[3] = {s.mid, s.big, s.small};
-#pragma unroll
-    for (int j = 0; j < 3; ++j) {
-#pragma unroll
-      for (int o = 16; o; o >>= 1) v[j] += __shfl_xor_sync(~0u, v[j], o);
-      if (lane == 0) tail.red[j][warp] = v[j];
+  // a barrier of the CTAs of this matrix; what they wrote before is visible behind it
+  uint32_t epoch = 0;
+  bool dead = false;
+  auto sync = [&]() {
+    if constexpr (GLOBAL) {
+      __syncthreads();
+      if (tid == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(a.count + group) : "memory");
+      epoch += a.cl;
+      // (after a wait that ran out the flag is set and the results do not count: no more waits)
+      dead = __syncthreads_or(dead || (warp == 0 && !wait_count_warp(a.count + group, epoch)));
+    } else if (a.cl > 1) {
+      pair_sync();
+    } else {
+      __syncthreads();
     }
+  };
+  uint32_t ph = 0, ph2 = 0;
+  for (int64_t k = group; k < a.d.G; k += GLOBAL ? a.groups : a.d.G) {
+    // rows and columns past the matrix are zero
+    for (uint32_t i = tid * 16; i < 2 * xpiece; i += rows * 16) sts16(xs + i, make_uint4(0, 0, 0, 0));
     __syncthreads();
-    if (tid < 3) {
-      float t = 0.f;
-      for (int w = 0; w < warps; ++w) t += tail.red[tid][w];
-      tail.norm[tid] = t;
-    }
-    if (a.cl > 1) pair_sync();
-    else __syncthreads();
-  }
-  const uint32_t tmem = tail.tmem;
-  const uint32_t stage = sums + warp * 4096;  // 32 x 32 fp32 values of a warp, where the sums are not in use
-  {
-    float t[3] = {0.f, 0.f, 0.f};
-    for (int c = 0; c < a.cl; ++c)
+    // momentum and the norm: this CTA's values, neighbouring ones by neighbouring threads
+    const DirArgs& d = a.d;
+    const int64_t gk = k * d.g_gs, uk = k * d.u_gs;
+    // the place of value (j, i), row j of this CTA's and column i of X
+    auto place = [&](int j, int i) -> int { return tall ? (m0 + j) * n + i : i * a.m + m0 + j; };
+    const uint32_t row_at = xs + tid * kPiece, turn = (tid & 7) << 4;  // 16-byte piece p of a row stands at p ^ (row & 7)
+    {
+      NormSums s{0.f, 0.f, 0.f};
+      // value (j, i) of up to n = 64 waits for the norm in row j, 64 fp32 values to a row's two pieces
+      auto keep = [&](int j, int i, float x) {
+        if constexpr (kBoth) {
+          const uint32_t at = xs + (i >> 5) * xpiece + j * kPiece + ((((i & 31) >> 2) ^ (j & 7)) << 4) + (i & 3) * 4;
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory");
+        }
+      };
+      // 16 values at a time, their loads before the first store
+      constexpr int kAt = 16;
+      auto some = [&](auto bf16, int64_t at, int64_t stride, int from, int step, int end, auto where) {
+        constexpr bool kBf16 = decltype(bf16)::value;
+        for (int b = from; b < end; b += kAt * step, at += kAt * stride) {
+          float g[kAt], u[kAt];
+          const float* up = d.u + uk + at;
+#pragma unroll
+          for (int q = 0; q < kAt; ++q) {
+            const bool in = b + q * step < end;
+            g[q] = in ? grad_value<kBf16>(d.g, gk + at + q * stride) : 0.f;
+            u[q] = in && d.mom != 0.f ? up[q * stride] : 0.f;
+          }
+#pragma unroll
+          for (int q = 0; q < kAt; ++q)
+            if (b + q * step < end) {
+              float x = g[q];
+              if (d.mom != 0.f) {
+                const float t = fmaf(d.mom, u[q], x);
+                d.u[uk + at + q * stride] = t;
+                x = d.nesterov ? fmaf(d.mom, t, x) : t;
+              }
+              norm_add(s, x);
+              where(b + q * step, x);
+            }
+        }
+      };
+      auto all = [&](auto bf16) {
+        if (tall) some(bf16, (int64_t)m0 * n + tid, rows, tid, rows, have * n, [&](int e, float x) { keep(e / n, e % n, x); });
+        else if (tid < have) some(bf16, m0 + tid, a.m, 0, 1, n, [&](int i, float x) { keep(tid, i, x); });
+      };
+      if (d.g_bf16) all(std::true_type{});
+      else all(std::false_type{});
+      float v[3] = {s.mid, s.big, s.small};
 #pragma unroll
       for (int j = 0; j < 3; ++j) {
-        float v;
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at_rank(smem_u32(&tail.norm[j]), c)) : "memory");
-        t[j] += v;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) v[j] += __shfl_xor_sync(~0u, v[j], o);
+        if (lane == 0) tail.red[j][warp] = v[j];
       }
-    const float2 f = norm_factors(t[0], t[1], t[2]);
-    if constexpr (kBoth) {
-      uint4 raw[16];
-#pragma unroll
-      for (int q = 0; q < 16; ++q) raw[q] = lds16(row_at + (q >> 3) * xpiece + (((q & 7) << 4) ^ turn));
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const uint4 r0 = raw[2 * q], r1 = raw[2 * q + 1];
-        const uint32_t w[8] = {r0.x, r0.y, r0.z, r0.w, r1.x, r1.y, r1.z, r1.w};
-        float x[8], hi[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]) * f.x * f.y;
-        const uint4 h = pack8(x);
-        unpack8(h, hi);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) hi[i] = x[i] - hi[i];
-        sts16(row_at + ((q << 4) ^ turn), h);
-        sts16(row_at + xpiece + ((q << 4) ^ turn), pack8(hi));
+      __syncthreads();
+      if (tid < 3) {
+        float t = 0.f;
+        for (int w = 0; w < warps; ++w) t += tail.red[tid][w];
+        if constexpr (GLOBAL) __stcg(a.norms + (group * a.cl + rank) * 3 + tid, t);
+        else tail.norm[tid] = t;
       }
-    } else {  // once more from L2, a row's values 16 at a time (rolled: code that runs once is fetched at its size)
-      const uint32_t ltile = tmem + low + (warp >> 2) * 64 + ((uint32_t)(warp & 3) << 21);
-      // 16 values' loads before they are used: value q at at + q stride where in(q)
-      auto batch = [&](auto bf16, int64_t at, int64_t stride, auto in, auto use) {
-        constexpr bool kBf16 = decltype(bf16)::value;
-        const bool want_g = d.mom == 0.f || d.nesterov, want_u = d.mom != 0.f;
-        const float* up = d.u + uk + at;
-        float g[16], u[16];
-#pragma unroll
-        for (int q = 0; q < 16; ++q) {
-          g[q] = want_g && in(q) ? grad_value<kBf16>(d.g, gk + at + q * stride) : 0.f;
-          u[q] = want_u && in(q) ? up[q * stride] : 0.f;
-        }
-        const float mg = want_g ? 1.f : 0.f, mu = !want_u ? 0.f : d.nesterov ? d.mom : 1.f;
-#pragma unroll
-        for (int q = 0; q < 16; ++q) use(q, fmaf(mu, u[q], mg * g[q]) * f.x * f.y);
-      };
-#pragma unroll 1
-      for (int b = 0; b < n; b += 16) {
-        float x[16];
-        auto all = [&](auto bf16) {
-          if (!tall) {
-            batch(bf16, (int64_t)b * a.m + m0 + tid, a.m, [&](int q) { return tid < have && b + q < n; },
-                  [&](int q, float v) { x[q] = v; });
-          } else {  // neighbouring lanes read neighbouring values; the warp's 32 x 16 values change places
-            const int row = lane >> 4, col = lane & 15;
-            batch(bf16, (int64_t)(m0 + warp * 32 + row) * n + b + col, 2 * n,
-                  [&](int q) { return warp * 32 + 2 * q + row < have && b + col < n; },
-                  [&](int q, float v) {
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(stage + (2 * q + row) * 64 + ((col ^ (q & 15)) << 2)), "f"(v) : "memory");
-                  });
-            __syncwarp();
-#pragma unroll
-            for (int q = 0; q < 16; ++q)
-              asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[q]) : "r"(stage + lane * 64 + ((q ^ (lane >> 1 & 15)) << 2)) : "memory");
-            __syncwarp();
-          }
-        };
-        if (d.g_bf16) all(std::true_type{});
-        else all(std::false_type{});
-        uint32_t low8[8];
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          const int q = b / 8 + p;
-          float v[8], hi[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = x[8 * p + i];
-          const uint4 w = pack8(v);
-          unpack8(w, hi);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) hi[i] = v[i] - hi[i];
-          const uint4 lo = pack8(hi);
-          sts16(row_at + (q >> 3) * xpiece + (((q & 7) << 4) ^ turn), w);
-          low8[4 * p] = lo.x, low8[4 * p + 1] = lo.y, low8[4 * p + 2] = lo.z, low8[4 * p + 3] = lo.w;
-        }
-        tmem_st8(ltile + b / 2, low8);
-      }
-      asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+      sync();
     }
-  }
-
-  uint32_t ph = 0, ph2 = 0;
-  const uint32_t quarter = (uint32_t)(warp & 3) * 32, lanes = quarter << 16;
-  const int r128 = (int)quarter + lane, groups = warps / 4;  // this thread's row of the symmetric products
-  const int ks = (have + 15) / 16, kn = (n + 15) / 16, n16 = kn * 16;  // rows and columns from n16 on are not computed
-  for (int step = 0; step < a.steps; ++step) {
-    // 1. [h l]^T [h l]
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
-    if (warp == 0) {
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const bool el = elect_one();
-      // M = N = 128, both operands with the sum running down the rows
-      constexpr uint32_t idesc = (1u << 4) | (1u << 15) | (1u << 16) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
-      const uint64_t x0 = smem_desc(xs, xpiece, 1024);
-      for (int i = 0; i < max(ks, 1); ++i)
-        if (el) mma_one(tmem, x0 + i * (2048 >> 4), x0 + i * (2048 >> 4), idesc, i > 0);
-      if (el) commit_one(&tail.bar[0]);
-    }
-    wait_bar_warp(&tail.bar[0], ph);
-    ph ^= 1;
-    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    // row r128 of the sums; 16-byte piece p of a row stands at p ^ (row & 31)
-    for (int c = (warp >> 2) * 16; c < 128 && ((int)quarter & (NP - 1)) < n16; c += groups * 16) {
-      if ((c & (NP - 1)) >= n16) continue;
-      float v[16];
-      tmem_ld16(tmem + c + lanes, v);
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        sts16(sums + r128 * 512 + (((c / 4 + j) ^ lane) << 4),
-              make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]),
-                         __float_as_uint(v[4 * j + 3])));
-    }
-    if (a.cl > 1) pair_sync();
-    else __syncthreads();
-    // 2. this CTA's slice of A: rows rank, rank + cl, ...; four columns to a thread
+    const uint32_t tmem = tail.tmem;
+    const uint32_t stage = sums + warp * 4096;  // 32 x 32 fp32 values of a warp, where the sums are not in use
     {
-      auto slice = [&](auto ctas) {
-        constexpr int kCtas = decltype(ctas)::value;
-        constexpr bool kOne = kCtas == 1;
-        const int per_row = n16 / 4, mine = (n16 - rank + kCtas - 1) / kCtas;
-        for (int e = tid; e < mine * per_row; e += rows) {
-          const int i = rank + e / per_row * kCtas, j = e % per_row;
-          float f[4] = {0.f, 0.f, 0.f, 0.f};
-          constexpr int kParts = kBoth ? 3 : 1;
-          uint4 w[kCtas][kParts];  // every CTA's parts, loaded before the first is used
+      float t[3] = {0.f, 0.f, 0.f};
+      for (int c = 0; c < a.cl; ++c)
 #pragma unroll
-          for (int c = 0; c < kCtas; ++c) {
-            const uint32_t from = kOne ? sums : at_rank(sums, c);
-            auto part = [&](int row, int piece) {
-              const uint32_t at = from + row * 512 + ((piece ^ (row & 31)) << 4);
-              return kOne ? lds16(at) : lds16_at(at);
-            };
-            w[c][0] = part(i, j);
-            if constexpr (kBoth) w[c][1] = part(i, 16 + j), w[c][2] = part(64 + i, j);
-          }
-#pragma unroll
-          for (int c = 0; c < kCtas; ++c) {
-#pragma unroll
-            for (int q = 0; q < kParts; ++q) {
-              f[0] += __uint_as_float(w[c][q].x), f[1] += __uint_as_float(w[c][q].y);
-              f[2] += __uint_as_float(w[c][q].z), f[3] += __uint_as_float(w[c][q].w);
-            }
-          }
-          float diag = 0.f;
-          const bool on = j == i >> 2;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            diag += 4 * j + q == i ? f[q] * kUnscale2 : 0.f;
-            f[q] = 4 * j + q == i ? 0.f : f[q] * kUnscale;
-          }
-          const __half2 w0 = __floats2half2_rn(f[0], f[1]), w1 = __floats2half2_rn(f[2], f[3]);
-          const uint32_t b0 = *reinterpret_cast<const uint32_t*>(&w0), b1 = *reinterpret_cast<const uint32_t*>(&w1);
-          const uint32_t to = as + (j >> 4) * (128 * kPiece) + i * kPiece + ((((j & 15) >> 1) << 4) ^ ((i & 7) << 4)) + (j & 1) * 8;
-          const uint32_t da = smem_u32(&tail.da[i]);
-          if constexpr (kOne) {
-            asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(b0), "r"(b1) : "memory");
-            if (on) tail.da[i] = diag;
-          } else {
-#pragma unroll
-            for (int c = 0; c < kCtas; ++c) {
-              asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(at_rank(to, c)), "r"(b0), "r"(b1) : "memory");
-              if (on) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at_rank(da, c)), "f"(diag) : "memory");
-            }
-          }
+        for (int j = 0; j < 3; ++j) {
+          float v;
+          if constexpr (GLOBAL) v = __ldcg(a.norms + (group * a.cl + c) * 3 + j);
+          else asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at_rank(smem_u32(&tail.norm[j]), c)) : "memory");
+          t[j] += v;
         }
-      };
-      if (a.cl == 1) slice(std::integral_constant<int, 1>{});
-      else if (a.cl == 2) slice(std::integral_constant<int, 2>{});
-      else if (a.cl == 4) slice(std::integral_constant<int, 4>{});
-      else slice(std::integral_constant<int, 8>{});
-    }
-    if (a.cl > 1) pair_sync();
-    // 3. A A, and P in A's place
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
-    if (warp == 0) {
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const bool el = elect_one();
-      constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(NP >> 3) << 17) | ((128u >> 4) << 24);
-      const uint64_t a0 = smem_desc(as, 16, 1024);
-      for (int i = 0; i < kn; ++i) {
-        const uint64_t at = a0 + (i >> 2) * (128 * kPiece >> 4) + (i & 3) * 2;
-        if (el) mma_one(tmem, at, at, idesc, i > 0);
+      const float2 f = norm_factors(t[0], t[1], t[2]);
+      if constexpr (kBoth) {
+        uint4 raw[16];
+#pragma unroll
+        for (int q = 0; q < 16; ++q) raw[q] = lds16(row_at + (q >> 3) * xpiece + (((q & 7) << 4) ^ turn));
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const uint4 r0 = raw[2 * q], r1 = raw[2 * q + 1];
+          const uint32_t w[8] = {r0.x, r0.y, r0.z, r0.w, r1.x, r1.y, r1.z, r1.w};
+          float x[8], hi[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]) * f.x * f.y;
+          const uint4 h = pack8(x);
+          unpack8(h, hi);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) hi[i] = x[i] - hi[i];
+          sts16(row_at + ((q << 4) ^ turn), h);
+          sts16(row_at + xpiece + ((q << 4) ^ turn), pack8(hi));
+        }
+      } else {  // once more from L2, a row's values 16 at a time (rolled: code that runs once is fetched at its size)
+        const uint32_t ltile = tmem + low + (warp >> 2) * 64 + ((uint32_t)(warp & 3) << 21);
+        // 16 values' loads before they are used: value q at at + q stride where in(q)
+        auto batch = [&](auto bf16, int64_t at, int64_t stride, auto in, auto use) {
+          constexpr bool kBf16 = decltype(bf16)::value;
+          const bool want_g = d.mom == 0.f || d.nesterov, want_u = d.mom != 0.f;
+          const float* up = d.u + uk + at;
+          float g[16], u[16];
+#pragma unroll
+          for (int q = 0; q < 16; ++q) {
+            g[q] = want_g && in(q) ? grad_value<kBf16>(d.g, gk + at + q * stride) : 0.f;
+            u[q] = want_u && in(q) ? up[q * stride] : 0.f;
+          }
+          const float mg = want_g ? 1.f : 0.f, mu = !want_u ? 0.f : d.nesterov ? d.mom : 1.f;
+#pragma unroll
+          for (int q = 0; q < 16; ++q) use(q, fmaf(mu, u[q], mg * g[q]) * f.x * f.y);
+        };
+#pragma unroll 1
+        for (int b = 0; b < n; b += 16) {
+          float x[16];
+          auto all = [&](auto bf16) {
+            if (!tall) {
+              batch(bf16, (int64_t)b * a.m + m0 + tid, a.m, [&](int q) { return tid < have && b + q < n; },
+                    [&](int q, float v) { x[q] = v; });
+            } else {  // neighbouring lanes read neighbouring values; the warp's 32 x 16 values change places
+              const int row = lane >> 4, col = lane & 15;
+              batch(bf16, (int64_t)(m0 + warp * 32 + row) * n + b + col, 2 * n,
+                    [&](int q) { return warp * 32 + 2 * q + row < have && b + col < n; },
+                    [&](int q, float v) {
+                      asm volatile("st.shared.f32 [%0], %1;" ::"r"(stage + (2 * q + row) * 64 + ((col ^ (q & 15)) << 2)), "f"(v) : "memory");
+                    });
+              __syncwarp();
+#pragma unroll
+              for (int q = 0; q < 16; ++q)
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[q]) : "r"(stage + lane * 64 + ((q ^ (lane >> 1 & 15)) << 2)) : "memory");
+              __syncwarp();
+            }
+          };
+          if (d.g_bf16) all(std::true_type{});
+          else all(std::false_type{});
+          uint32_t low8[8];
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            const int q = b / 8 + p;
+            float v[8], hi[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = x[8 * p + i];
+            const uint4 w = pack8(v);
+            unpack8(w, hi);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) hi[i] = v[i] - hi[i];
+            const uint4 lo = pack8(hi);
+            sts16(row_at + (q >> 3) * xpiece + (((q & 7) << 4) ^ turn), w);
+            low8[4 * p] = lo.x, low8[4 * p + 1] = lo.y, low8[4 * p + 2] = lo.z, low8[4 * p + 3] = lo.w;
+          }
+          tmem_st8(ltile + b / 2, low8);
+        }
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
       }
-      if (el) commit_one(&tail.bar[0]);
     }
-    wait_bar_warp(&tail.bar[0], ph);
-    ph ^= 1;
-    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    if ((int)quarter < n16) {
-      const float di = r128 < n16 ? tail.da[r128] : 0.f;
-      for (int c = (warp >> 2) * 16; c < n16; c += groups * 16) {
-        float v[16], mine = 0.f;
+
+    const uint32_t quarter = (uint32_t)(warp & 3) * 32, lanes = quarter << 16;
+    const int r128 = (int)quarter + lane, groups = warps / 4;  // this thread's row of the symmetric products
+    const int ks = (have + 15) / 16, kn = (n + 15) / 16, n16 = kn * 16;  // rows and columns from n16 on are not computed
+    for (int step = 0; step < a.steps; ++step) {
+      // 1. [h l]^T [h l]
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncthreads();
+      if (warp == 0) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const bool el = elect_one();
+        // M = N = 128, both operands with the sum running down the rows
+        constexpr uint32_t idesc = (1u << 4) | (1u << 15) | (1u << 16) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+        const uint64_t x0 = smem_desc(xs, xpiece, 1024);
+        for (int i = 0; i < max(ks, 1); ++i)
+          if (el) mma_one(tmem, x0 + i * (2048 >> 4), x0 + i * (2048 >> 4), idesc, i > 0);
+        if (el) commit_one(&tail.bar[0]);
+      }
+      wait_bar_warp(&tail.bar[0], ph);
+      ph ^= 1;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      // row r128 of the sums; 16-byte piece p of a row stands at p ^ (row & 31)
+      for (int c = (warp >> 2) * 16; c < 128 && ((int)quarter & (NP - 1)) < n16; c += groups * 16) {
+        if ((c & (NP - 1)) >= n16) continue;
+        float v[16];
         tmem_ld16(tmem + c + lanes, v);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const uint32_t at = as + (c >> 6) * (128 * kPiece) + r128 * kPiece + ((((c & 63) / 8 + j) << 4) ^ ((r128 & 7) << 4));
-          float f[8], dj[8];
-          unpack8(lds16(at), f);
-          vec8(smem_u32(tail.da) + (c + 8 * j) * 4, dj);
+        for (int j = 0; j < 4; ++j)
+          sts16(sums + r128 * 512 + (((c / 4 + j) ^ lane) << 4),
+                make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]),
+                           __float_as_uint(v[4 * j + 3])));
+      }
+      if constexpr (GLOBAL) __syncthreads();
+      else sync();
+      // 2. this CTA's slice of A: rows rank, rank + cl, ...; four columns to a thread
+      {
+        auto slice = [&](auto ctas) {
+          constexpr int kCtas = decltype(ctas)::value;
+          constexpr bool kOne = kCtas == 1;
+          const int per_row = n16 / 4, mine = (n16 - rank + kCtas - 1) / kCtas;
+          for (int e = tid; e < mine * per_row; e += rows) {
+            const int i = rank + e / per_row * kCtas, j = e % per_row;
+            float f[4] = {0.f, 0.f, 0.f, 0.f};
+            constexpr int kParts = kBoth ? 3 : 1;
+            uint4 w[kCtas][kParts];  // every CTA's parts, loaded before the first is used
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            f[i] = fmaf(fmaf(kC, di + dj[i], kB), f[i], kC * kUnscale * v[8 * j + i]);
-            mine += c + 8 * j + i == r128 ? v[8 * j + i] : 0.f;
-            f[i] = c + 8 * j + i == r128 ? 0.f : f[i];
+            for (int c = 0; c < kCtas; ++c) {
+              const uint32_t from = kOne ? sums : at_rank(sums, c);
+              auto part = [&](int row, int piece) {
+                const uint32_t at = from + row * 512 + ((piece ^ (row & 31)) << 4);
+                return kOne ? lds16(at) : lds16_at(at);
+              };
+              w[c][0] = part(i, j);
+              if constexpr (kBoth) w[c][1] = part(i, 16 + j), w[c][2] = part(64 + i, j);
+            }
+#pragma unroll
+            for (int c = 0; c < kCtas; ++c) {
+#pragma unroll
+              for (int q = 0; q < kParts; ++q) {
+                f[0] += __uint_as_float(w[c][q].x), f[1] += __uint_as_float(w[c][q].y);
+                f[2] += __uint_as_float(w[c][q].z), f[3] += __uint_as_float(w[c][q].w);
+              }
+            }
+            float diag = 0.f;
+            const bool on = j == i >> 2;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              diag += 4 * j + q == i ? f[q] * kUnscale2 : 0.f;
+              f[q] = 4 * j + q == i ? 0.f : f[q] * kUnscale;
+            }
+            const __half2 w0 = __floats2half2_rn(f[0], f[1]), w1 = __floats2half2_rn(f[2], f[3]);
+            const uint32_t b0 = *reinterpret_cast<const uint32_t*>(&w0), b1 = *reinterpret_cast<const uint32_t*>(&w1);
+            const uint32_t to = as + (j >> 4) * (128 * kPiece) + i * kPiece + ((((j & 15) >> 1) << 4) ^ ((i & 7) << 4)) + (j & 1) * 8;
+            const uint32_t da = smem_u32(&tail.da[i]);
+            if constexpr (kOne) {
+              asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(b0), "r"(b1) : "memory");
+              if (on) tail.da[i] = diag;
+            } else {
+#pragma unroll
+              for (int c = 0; c < kCtas; ++c) {
+                asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(at_rank(to, c)), "r"(b0), "r"(b1) : "memory");
+                if (on) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at_rank(da, c)), "f"(diag) : "memory");
+              }
+            }
           }
-          sts16(at, pack8(f));
-        }
-        if (c == (r128 & ~15)) tail.d[r128] = fmaf(kB, di, kC * fmaf(di, di, mine * kUnscale2));
-      }
-    }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
-    // 4. X P
-    float top = 0.f;  // t of the number formats above
-    if (!kBoth && step + 2 >= a.steps) {
-      top = -INFINITY;
-      for (int i = lane; i < n; i += 32) top = fmaxf(top, tail.d[i]);
+        };
+        if constexpr (GLOBAL) {
+          const int per_row = n16 / 4, all = n16 * per_row;
+          float4* part = reinterpret_cast<float4*>(a.part) + (int64_t)group * a.cl * all;
+          uint2* full = a.full + (int64_t)group * all;
+          float* diag = a.diag + group * n16;
+          auto word = [](float x, float y) {
+            const __half2 w = __floats2half2_rn(x, y);
+            return *reinterpret_cast<const uint32_t*>(&w);
+          };
+          for (int e = tid; e < all; e += rows) {
+            const int i = e / per_row, j = e % per_row;
+            float f[4] = {0.f, 0.f, 0.f, 0.f};
+            auto add = [&](int row, int piece) {
+              const uint4 w = lds16(sums + row * 512 + ((piece ^ (row & 31)) << 4));
+              f[0] += __uint_as_float(w.x), f[1] += __uint_as_float(w.y);
+              f[2] += __uint_as_float(w.z), f[3] += __uint_as_float(w.w);
+            };
+            add(i, j);
+            if constexpr (kBoth) add(i, 16 + j), add(64 + i, j);
+            __stcg(part + (int64_t)rank * all + e, make_float4(f[0], f[1], f[2], f[3]));
+          }
+          sync();
+          const int mine = (n16 - rank + a.cl - 1) / a.cl;
+          for (int e = tid; e < mine * per_row; e += rows) {
+            const int i = rank + e / per_row * a.cl, j = e % per_row;
+            float f[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+            for (int c = 0; c < a.cl; ++c) {
+              const float4 w = __ldcg(part + (int64_t)c * all + i * per_row + j);
+              f[0] += w.x, f[1] += w.y, f[2] += w.z, f[3] += w.w;
+            }
+            float on_diag = 0.f;
 #pragma unroll
-      for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-    }
-    const bool last = step + 1 == a.steps;
-    const int tile = warp >> 2, at_once = kBoth ? tiles : 2;
-#pragma unroll 1
-    for (int t0 = 0; t0 < tiles; t0 += at_once) {
-      if (t0 > 0) {  // the accumulators have been read
-        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        __syncthreads();
+            for (int q = 0; q < 4; ++q) {
+              on_diag += 4 * j + q == i ? f[q] * kUnscale2 : 0.f;
+              f[q] = 4 * j + q == i ? 0.f : f[q] * kUnscale;
+            }
+            __stcg(full + i * per_row + j, make_uint2(word(f[0], f[1]), word(f[2], f[3])));
+            if (j == i >> 2) __stcg(diag + i, on_diag);
+          }
+          sync();
+          for (int e = tid; e < all; e += rows) {
+            const int i = e / per_row, j = e % per_row;
+            const uint2 w = __ldcg(full + e);
+            const uint32_t to = as + (j >> 4) * (128 * kPiece) + i * kPiece + ((((j & 15) >> 1) << 4) ^ ((i & 7) << 4)) + (j & 1) * 8;
+            asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(w.x), "r"(w.y) : "memory");
+          }
+          for (int i = tid; i < n16; i += rows) tail.da[i] = __ldcg(diag + i);
+        } else if (a.cl == 1) slice(std::integral_constant<int, 1>{});
+        else if (a.cl == 2) slice(std::integral_constant<int, 2>{});
+        else if (a.cl == 4) slice(std::integral_constant<int, 4>{});
+        else slice(std::integral_constant<int, 8>{});
       }
+      if (!GLOBAL && a.cl > 1) pair_sync();
+      // 3. A A, and P in A's place
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncthreads();
       if (warp == 0) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const bool el = elect_one();
         constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(NP >> 3) << 17) | ((128u >> 4) << 24);
-        const uint64_t x0 = smem_desc(xs, 16, 1024), p0 = smem_desc(as, 16, 1024);
-        for (int t = t0; t < min(tiles, t0 + at_once); ++t) {
-          const uint64_t xt = x0 + (uint32_t)(t * 128 * kPiece >> 4);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {  // up to n = 64 the h, then the l of four slices of 16 columns; else eight of h
-            const int slice = kBoth ? i & 3 : i;
-            const uint64_t xa = xt + (i >> 2) * (xpiece >> 4) + (i & 3) * 2;
-            const uint64_t pb = p0 + (kBoth ? 0 : (i >> 2) * (128 * kPiece >> 4)) + (i & 3) * 2;
-            if (el && slice < kn) mma_one(tmem + (t - t0) * NP, xa, pb, idesc, i > 0);
-          }
-          if (el) commit_one(&tail.bar[1 + t]);
+        const uint64_t a0 = smem_desc(as, 16, 1024);
+        for (int i = 0; i < kn; ++i) {
+          const uint64_t at = a0 + (i >> 2) * (128 * kPiece >> 4) + (i & 3) * 2;
+          if (el) mma_one(tmem, at, at, idesc, i > 0);
         }
-        __syncwarp();
+        if (el) commit_one(&tail.bar[0]);
       }
-      if (tile < t0 || tile >= t0 + at_once) continue;
-      wait_bar_warp(&tail.bar[1 + tile], ph2);
+      wait_bar_warp(&tail.bar[0], ph);
+      ph ^= 1;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const uint32_t dtile = tmem + (tile - t0) * NP + lanes, ltile = tmem + low + tile * 64 + lanes;
-#pragma unroll 1
-      for (int c = 0; c < n; c += 16) {  // (rolled: the instruction cache holds a step then)
-        float v[16];
-        uint32_t low8[8];
-        if constexpr (kBoth) tmem_ld16(dtile + c, v);
-        else tmem_ld16_8(dtile + c, v, ltile + c / 2, low8);
+      if ((int)quarter < n16) {
+        const float di = r128 < n16 ? tail.da[r128] : 0.f;
+        for (int c = (warp >> 2) * 16; c < n16; c += groups * 16) {
+          float v[16], mine = 0.f;
+          tmem_ld16(tmem + c + lanes, v);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int q = c / 8 + j;
-          const uint32_t at = row_at + (kBoth ? 0 : (q >> 3) * xpiece) + (((q & 7) << 4) ^ turn);
-          float f[8], lo[8], dj[8];
-          unpack8(lds16(at), f);
-          vec8(smem_u32(tail.d) + 32 * q, dj);
-          if constexpr (kBoth) unpack8(lds16(at + xpiece), lo);
-          else unpack8(make_uint4(low8[4 * j], low8[4 * j + 1], low8[4 * j + 2], low8[4 * j + 3]), lo);
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t at = as + (c >> 6) * (128 * kPiece) + r128 * kPiece + ((((c & 63) / 8 + j) << 4) ^ ((r128 & 7) << 4));
+            float f[8], dj[8];
+            unpack8(lds16(at), f);
+            vec8(smem_u32(tail.da) + (c + 8 * j) * 4, dj);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float t = kA + dj[i];
-            f[i] = kBoth ? fmaf(t, f[i] + lo[i], kUnscale * v[8 * j + i]) : fmaf(t, f[i], fmaf(kA + top, lo[i], kUnscale * v[8 * j + i]));
+            for (int i = 0; i < 8; ++i) {
+              f[i] = fmaf(fmaf(kC, di + dj[i], kB), f[i], kC * kUnscale * v[8 * j + i]);
+              mine += c + 8 * j + i == r128 ? v[8 * j + i] : 0.f;
+              f[i] = c + 8 * j + i == r128 ? 0.f : f[i];
+            }
+            sts16(at, pack8(f));
           }
-          if (!last) {
-            const uint4 w = pack8(f);
-            sts16(at, w);
-            float hi[8];
-            unpack8(w, hi);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) hi[i] = f[i] - hi[i];
-            const uint4 l = pack8(hi);
-            if constexpr (kBoth) sts16(at + xpiece, l);
-            else low8[4 * j] = l.x, low8[4 * j + 1] = l.y, low8[4 * j + 2] = l.z, low8[4 * j + 3] = l.w;
-          } else if (!tall) {
-            uint16_t* o = d.o + k * d.o_gs;
-            if (tid < have)
-#pragma unroll
-              for (int i = 0; i < 8; ++i)
-                if (8 * q + i < n) o[place(tid, 8 * q + i)] = f2bf(f[i] * kUnscale);
-          } else {  // 16 columns of the warp's rows, to be written row by row
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] *= kUnscale;
-            sts16(stage + lane * 32 + ((j ^ (lane >> 2 & 1)) << 4), pack8_bf16(f));
-          }
-        }
-        if (!kBoth && !last) tmem_st8(ltile + c / 2, low8);
-        if (last && tall) {
-          __syncwarp();
-          uint16_t* o = d.o + k * d.o_gs + (int64_t)(m0 + warp * 32) * n + c + (lane & 15);
-          const int i = lane & 15;
-          if (c + i < n)
-#pragma unroll 4
-            for (int rr = lane >> 4; rr < 32; rr += 2)
-              if (warp * 32 + rr < have) {
-                uint16_t v;
-                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(stage + rr * 32 + (((i >> 3) ^ (rr >> 2 & 1)) << 4) + (i & 7) * 2) : "memory");
-                o[rr * n] = v;
-              }
-          __syncwarp();
+          if (c == (r128 & ~15)) tail.d[r128] = fmaf(kB, di, kC * fmaf(di, di, mine * kUnscale2));
         }
       }
-      if constexpr (!kBoth) asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncthreads();
+      // 4. X P
+      float top = 0.f;  // t of the number formats above
+      if (!kBoth && step + 2 >= a.steps) {
+        top = -INFINITY;
+        for (int i = lane; i < n; i += 32) top = fmaxf(top, tail.d[i]);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+      }
+      const bool last = step + 1 == a.steps;
+      const int tile = warp >> 2, at_once = kBoth ? tiles : 2;
+#pragma unroll 1
+      for (int t0 = 0; t0 < tiles; t0 += at_once) {
+        if (t0 > 0) {  // the accumulators have been read
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncthreads();
+        }
+        if (warp == 0) {
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const bool el = elect_one();
+          constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(NP >> 3) << 17) | ((128u >> 4) << 24);
+          const uint64_t x0 = smem_desc(xs, 16, 1024), p0 = smem_desc(as, 16, 1024);
+          for (int t = t0; t < min(tiles, t0 + at_once); ++t) {
+            const uint64_t xt = x0 + (uint32_t)(t * 128 * kPiece >> 4);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {  // up to n = 64 the h, then the l of four slices of 16 columns; else eight of h
+              const int slice = kBoth ? i & 3 : i;
+              const uint64_t xa = xt + (i >> 2) * (xpiece >> 4) + (i & 3) * 2;
+              const uint64_t pb = p0 + (kBoth ? 0 : (i >> 2) * (128 * kPiece >> 4)) + (i & 3) * 2;
+              if (el && slice < kn) mma_one(tmem + (t - t0) * NP, xa, pb, idesc, i > 0);
+            }
+            if (el) commit_one(&tail.bar[1 + t]);
+          }
+          __syncwarp();
+        }
+        if (tile < t0 || tile >= t0 + at_once) continue;
+        wait_bar_warp(&tail.bar[1 + tile], ph2);
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t dtile = tmem + (tile - t0) * NP + lanes, ltile = tmem + low + tile * 64 + lanes;
+#pragma unroll 1
+        for (int c = 0; c < n; c += 16) {  // (rolled: the instruction cache holds a step then)
+          float v[16];
+          uint32_t low8[8];
+          if constexpr (kBoth) tmem_ld16(dtile + c, v);
+          else tmem_ld16_8(dtile + c, v, ltile + c / 2, low8);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int q = c / 8 + j;
+            const uint32_t at = row_at + (kBoth ? 0 : (q >> 3) * xpiece) + (((q & 7) << 4) ^ turn);
+            float f[8], lo[8], dj[8];
+            unpack8(lds16(at), f);
+            vec8(smem_u32(tail.d) + 32 * q, dj);
+            if constexpr (kBoth) unpack8(lds16(at + xpiece), lo);
+            else unpack8(make_uint4(low8[4 * j], low8[4 * j + 1], low8[4 * j + 2], low8[4 * j + 3]), lo);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float t = kA + dj[i];
+              f[i] = kBoth ? fmaf(t, f[i] + lo[i], kUnscale * v[8 * j + i]) : fmaf(t, f[i], fmaf(kA + top, lo[i], kUnscale * v[8 * j + i]));
+            }
+            if (!last) {
+              const uint4 w = pack8(f);
+              sts16(at, w);
+              float hi[8];
+              unpack8(w, hi);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) hi[i] = f[i] - hi[i];
+              const uint4 l = pack8(hi);
+              if constexpr (kBoth) sts16(at + xpiece, l);
+              else low8[4 * j] = l.x, low8[4 * j + 1] = l.y, low8[4 * j + 2] = l.z, low8[4 * j + 3] = l.w;
+            } else if (!tall) {
+              uint16_t* o = d.o + k * d.o_gs;
+              if (tid < have)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                  if (8 * q + i < n) o[place(tid, 8 * q + i)] = f2bf(f[i] * kUnscale);
+            } else {  // 16 columns of the warp's rows, to be written row by row
+#pragma unroll
+              for (int i = 0; i < 8; ++i) f[i] *= kUnscale;
+              sts16(stage + lane * 32 + ((j ^ (lane >> 2 & 1)) << 4), pack8_bf16(f));
+            }
+          }
+          if (!kBoth && !last) tmem_st8(ltile + c / 2, low8);
+          if (last && tall) {
+            __syncwarp();
+            uint16_t* o = d.o + k * d.o_gs + (int64_t)(m0 + warp * 32) * n + c + (lane & 15);
+            const int i = lane & 15;
+            if (c + i < n)
+#pragma unroll 4
+              for (int rr = lane >> 4; rr < 32; rr += 2)
+                if (warp * 32 + rr < have) {
+                  uint16_t v;
+                  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(stage + rr * 32 + (((i >> 3) ^ (rr >> 2 & 1)) << 4) + (i & 7) * 2) : "memory");
+                  o[rr * n] = v;
+                }
+            __syncwarp();
+          }
+        }
+        if constexpr (!kBoth) asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+      }
+      ph2 ^= 1;
     }
-    ph2 ^= 1;
+    __syncthreads();  // the next matrix is written where this one was read
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
-  if (a.cl > 1) pair_sync();  // no CTA leaves while another may read its sums
-  if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
+  if (!GLOBAL && a.cl > 1) pair_sync();  // no CTA leaves while another may read its sums
+  if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tail.tmem), "r"(cols) : "memory");
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -1432,10 +1509,15 @@ struct DirLayout {
   int chunks, per;
   size_t h[2], l[2], A, P, diag_a, diag, part, done, bytes;
 };
-int resident_ctas(int64_t rows, int64_t cols);
+struct ResPlan;
+ResPlan resident_plan(int G, int64_t rows, int64_t cols);
+size_t resident_bytes(int G, int64_t rows, int64_t cols);
 DirLayout direction_layout(int G, int64_t rows, int64_t cols) {
   DirLayout d{};
-  if (resident_ctas(rows, cols)) return d;  // no workspace
+  if (std::min(rows, cols) <= kResSide) {
+    d.bytes = resident_bytes(G, rows, cols);
+    return d;
+  }
   d.n = std::min(rows, cols);
   d.ldx = pad16(cols), d.lda = pad16(d.n);
   size_t at = 0;
@@ -1557,47 +1639,88 @@ cudaError_t launch_products(const MmArgs& a, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, direction_product_kernel<PAIR>, a);
 }
 
-// CTAs per matrix of the resident form (a power of two up to 8, the portable cluster size), or 0: it does not fit.
-int resident_ctas(int64_t rows, int64_t cols) {
+// The resident form's CTAs per matrix: a cluster (a power of two up to 8, the portable size), or `groups` groups of `cl` that
+// exchange through global memory where the m rows are too many for a cluster, or where clusters of 8, of which the SMs hold 15 at
+// once, take more rounds than the groups, of which they hold 152 / cl.  cl = 0: the smaller side is too large.
+struct ResPlan {
+  int cl, groups;  // groups = 0: clusters
+};
+ResPlan resident_plan(int G, int64_t rows, int64_t cols) {
   const int64_t n = std::min(rows, cols), m = std::max(rows, cols);
-  if (n > kResSide) return 0;
-  for (int cl = 1; cl <= 8; cl *= 2)
-    if ((m + cl - 1) / cl <= kRows) return cl;
-  return 0;
+  if (n > kResSide) return ResPlan{0, 0};
+  int cl = 1;
+  while (cl < 8 && (m + cl - 1) / cl > kRows) cl *= 2;
+  const int need = (int)((m + kRows - 1) / kRows), at_once = kNumSMs / need;
+  const bool fits = (m + cl - 1) / cl <= kRows;
+  if (fits && (cl < 8 || (G + 14) / 15 <= (G + at_once - 1) / at_once)) return ResPlan{cl, 0};
+  return ResPlan{need, std::min(G, at_once)};
 }
 
-template <int NP>
+// The workspace of the groups: their sums, A, diagonals, norms and counts.
+struct ResLayout {
+  size_t full, diag, norms, count, bytes;
+};
+ResLayout resident_layout(const ResPlan& p, int64_t n) {
+  ResLayout l{};
+  if (!p.groups) return l;
+  const size_t n16 = pad16(n), a = n16 * n16;
+  l.full = (size_t)p.groups * p.cl * a * 4;
+  l.diag = l.full + (size_t)p.groups * a * 2;
+  l.norms = l.diag + (size_t)p.groups * n16 * 4;
+  l.count = l.norms + (size_t)p.groups * p.cl * 12;
+  l.bytes = l.count + (size_t)p.groups * 4;
+  return l;
+}
+
+size_t resident_bytes(int G, int64_t rows, int64_t cols) {
+  return resident_layout(resident_plan(G, rows, cols), std::min(rows, cols)).bytes;
+}
+
+template <int NP, bool GLOBAL>
 cudaError_t launch_resident(const ResArgs& a, cudaStream_t st) {
   static std::atomic<int> raised{0};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (raised != dev + 1) {
-    e = cudaFuncSetAttribute(direction_resident_kernel<NP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)res_smem<NP>(kRows));
+    e = cudaFuncSetAttribute(direction_resident_kernel<NP, GLOBAL>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)res_smem<NP>(kRows));
     if (e != cudaSuccess) return e;
     raised = dev + 1;
   }
   const int threads = (a.per + 127) / 128 * 128;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(a.d.G * a.cl));
+  cfg.gridDim = dim3((unsigned)((GLOBAL ? a.groups : a.d.G) * a.cl));
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = res_smem<NP>(threads);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  if (GLOBAL) {  // all CTAs are resident, so that every barrier ends
+    attr[0].id = cudaLaunchAttributeCooperative;
+    attr[0].val.cooperative = 1;
+  } else {
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+  }
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = a.cl, attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr, cfg.numAttrs = a.cl > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, direction_resident_kernel<NP>, a);
+  cfg.attrs = attr, cfg.numAttrs = !GLOBAL && a.cl > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, direction_resident_kernel<NP, GLOBAL>, a);
 }
 
-cudaError_t run_resident(const DirArgs& d, int cl, int steps, cudaStream_t st) {
+cudaError_t run_resident(const DirArgs& d, const ResPlan& p, uint8_t* ws, int steps, cudaStream_t st) {
   ResArgs a{};
-  a.d = d, a.cl = cl, a.steps = steps;
+  a.d = d, a.cl = p.cl, a.groups = p.groups, a.steps = steps;
   a.n = std::min(d.rows, d.cols), a.m = std::max(d.rows, d.cols);
-  a.per = (a.m + cl - 1) / cl;
-  return a.n <= 64 ? launch_resident<64>(a, st) : launch_resident<128>(a, st);
+  a.per = (a.m + p.cl - 1) / p.cl;
+  if (!p.groups) return a.n <= 64 ? launch_resident<64, false>(a, st) : launch_resident<128, false>(a, st);
+  const ResLayout l = resident_layout(p, a.n);
+  a.part = reinterpret_cast<float*>(ws), a.full = reinterpret_cast<uint2*>(ws + l.full);
+  a.diag = reinterpret_cast<float*>(ws + l.diag), a.norms = reinterpret_cast<float*>(ws + l.norms);
+  a.count = reinterpret_cast<uint32_t*>(ws + l.count);
+  const cudaError_t e = cudaMemsetAsync(a.count, 0, (size_t)p.groups * 4, st);
+  if (e != cudaSuccess) return e;
+  return a.n <= 64 ? launch_resident<64, true>(a, st) : launch_resident<128, true>(a, st);
 }
 
 cudaError_t run_direction(DirArgs d, const DirLayout& ly, uint8_t* ws, int steps, cudaStream_t st) {
@@ -1703,9 +1826,9 @@ lsgd_status lsgd_orthogonal_direction(float* u, int64_t u_gs, const void* g, int
   d.u = u, d.g = g, d.o = o, d.u_gs = u_gs, d.g_gs = g_gs, d.o_gs = o_gs;
   d.g_bf16 = gb, d.nesterov = nesterov != 0, d.mom = momentum;
   d.G = G, d.rows = (int)rows, d.cols = (int)cols;
-  const int cl = resident_ctas(rows, cols);
-  const cudaError_t e = cl ? run_resident(d, cl, steps, (cudaStream_t)stream)
-                           : run_direction(d, ly, static_cast<uint8_t*>(workspace), steps, (cudaStream_t)stream);
+  const ResPlan plan = resident_plan(G, rows, cols);
+  const cudaError_t e = plan.cl ? run_resident(d, plan, static_cast<uint8_t*>(workspace), steps, (cudaStream_t)stream)
+                                : run_direction(d, ly, static_cast<uint8_t*>(workspace), steps, (cudaStream_t)stream);
   if (e == cudaErrorNotSupported) return dir_error(LSGD_EUNSUPPORTED, fn, "no tensor maps (cuTensorMapEncodeTiled)");
   return e == cudaSuccess ? LSGD_OK : dir_error(LSGD_ECUDA, fn, cudaGetErrorString(e));
 }
