@@ -438,11 +438,13 @@ lsgd_status lsgd_batchnorm_stats_noalloc(const float* y, int64_t P, int C, int G
  * underflow: a matrix of any finite size is normalised, an all-zero one gives o = 0; a NaN or infinite
  * value makes its own matrix's direction NaN and no other.
  * The products run on the tensor cores with fp16 operands, fp32 accumulation and X carried as a pair
- * of fp16 values: o is within 1.5e-3 (relative 2-norm) of exact arithmetic before its rounding to bf16, for rank-
- * deficient matrices too.  Deterministic.  Sizes up to 32768 a side, steps 1 to 100, G <= 65535.
+ * of fp16 values: before its rounding to bf16 o is off by about 1e-3 of its 2-norm (at most 1.5e-3, and
+ * 2.5e-3 where the smaller side is 64 or less) from exact arithmetic after five steps, for rank-deficient and
+ * badly scaled matrices too.  Deterministic.  Sizes up to 32768 a side, steps 1 to 100, G <= 65535.
  *
- * `workspace`: device memory of at least lsgd_orthogonal_workspace's bytes (0: it is not used and may be
- * NULL; a smaller side up to 128 with a larger one up to 4096), 256-byte aligned, whose contents do not matter before or after; calls (or captured graphs) that may run at the same time
+ * `workspace`: device memory of at least lsgd_orthogonal_workspace's bytes (0 for most matrices with a
+ * side of at most 128: it is not used then and may be NULL), 256-byte aligned, whose contents do
+ * not matter before or after; calls (or captured graphs) that may run at the same time
  * need one each.  No allocation: the calls may be captured into a CUDA graph.  LSGD_EINVAL for bad
  * arguments, too small a workspace and tensors that overlap.  Device pointers, asynchronous on `stream`, which
  * belongs to the current device; lsgd_device_status reports a device-side wait that ran out. */

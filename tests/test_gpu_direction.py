@@ -7,12 +7,14 @@ import _operator_refs as R
 from _gpu_common import built_package
 
 U32, U16 = 2.0 ** -24, 2.0 ** -8
-# How far a direction may be off before its bf16 rounding, of its 2-norm.  A step rounds its operands (X, A, P) to fp16, 2^-11
-# of each value at most; a singular value then changes by up to 4 such roundings (X enters A twice), 2e-3, in each of five
-# steps, and by what the later steps make of it: the quintic's relative slope is 1 for small values and between -3 and 1
-# around one.  Roundings of a matrix of more than a few values are of random sign and average out: models of the same
-# roundings on the CPU give 1e-3 for large matrices and at most 1e-2 over thousands of tiny and degenerate ones.
-OFF = 1e-2
+# How far a direction may be off before its bf16 rounding, of its 2-norm.  A step rounds A and P (and above a smaller side of
+# 64 X as an operand) to fp16, 2^-11 of each value at most and 2^-11 / sqrt(3) = 2.8e-4 in the mean; |P| < 2.9, so a step's
+# rounding of P alone moves X by up to 8e-4, and the steps after it multiply what lies in X's space by a slope that is
+# below one near the plateau: the last two or three steps count, 1.5e-3 in all.  Matrices of a few values do not average:
+# CPU models of the same roundings gave at most 2.4e-3 over thousands of tiny and degenerate ones.
+def _off(shape):
+    return 2.5e-3 if min(shape[1:]) <= 64 else 1.5e-3
+
 
 # (G, rows, cols): single values, vectors, odd sizes, both orientations, sizes on, below and above every tile (64, 128,
 # 256), more matrices than CTA pairs, a long row
@@ -78,16 +80,21 @@ def _run(P, torch, shape, u, g, momentum=0.95, nesterov=True, steps=5, gs=0, lea
 
 
 def _check(o, x, steps=5):
-    """o against the definition for x (64 bits): bf16's rounding, at most 2^-8 of each value, and before it OFF of the 2-norm."""
+    """o against the definition for x (64 bits): what it may be off, and its rounding to bf16 (that of the exact values where
+    they are many, which is the same to a tenth; at most 2^-8 of each otherwise)."""
+    import torch
+
     want = R.direction(x, steps)
     got = o.float().cpu().numpy().astype(np.float64)
     for k in range(len(want)):
         norm = np.linalg.norm(want[k])
         off = np.linalg.norm(got[k] - want[k])
-        assert off <= norm * (OFF + 2.0 ** -8) and np.isfinite(got[k]).all(), (k, off / norm)
+        rounded = np.linalg.norm(torch.tensor(want[k]).bfloat16().double().numpy() - want[k])
+        rounding = 1.1 * rounded if want[k].size >= 256 else U16 * norm
+        assert off <= norm * _off(x.shape) + rounding and np.isfinite(got[k]).all(), (k, off / norm)
         # no single value is far off either: the error is spread over the matrix, not in one tile
-        rms = norm / np.sqrt(want[k].size)
-        assert np.abs(got[k] - want[k]).max() <= 2.0 ** -8 * np.abs(want[k]).max() + 8 * OFF * max(rms, np.abs(want[k]).max() / 8)
+        rms, big = norm / np.sqrt(want[k].size), np.abs(want[k]).max()
+        assert np.abs(got[k] - want[k]).max() <= U16 * big + 1e-2 * 8 * max(rms, big / 8)
 
 
 @pytest.mark.gpu
@@ -273,8 +280,8 @@ def test_a_layer_inside_a_replica_major_buffer(P):
         w = (1 - lr * wd) * w - lr * R.direction((gr + m * u).reshape(K, rows, cols), 5).reshape(K, -1)
     torch.cuda.synchronize()
     got = W.double().cpu().numpy()
-    # three directions of at most 1.21 in every singular value, each off by OFF + 2^-8 of its norm, times lr
-    tol = 3 * lr * (OFF + 2.0 ** -8) * 1.21 * np.sqrt(rows) + 8 * U32 * np.linalg.norm(w[0])
+    # three directions of at most 1.21 in every singular value, each off by 1.5e-3 + 2^-8 of its norm, times lr
+    tol = 3 * lr * (1.5e-3 + 2.0 ** -8) * 1.21 * np.sqrt(rows) + 8 * U32 * np.linalg.norm(w[0])
     for k in range(K):
         assert np.linalg.norm(got[k, before:before + rows * cols] - w[k]) <= tol
     assert torch.equal(W[:, :before], W0[:, :before]) and torch.equal(W[:, before + rows * cols:], W0[:, before + rows * cols:])
