@@ -260,6 +260,69 @@ def _check_backward(shape, x, dy, gamma, beta, y, mean, rstd, dx, dgamma, dbeta,
     assert worst.max() <= 1.0, worst.max()
 
 
+# images that no cluster holds: ranges of a few positions and of many; one group, groups within and across vectors; one
+# position's channels wider than the threads; many images
+LARGE = [(1, 1, 60007, 24, 1), (1, 2, 13001, 168, 42), (2, 3, 20011, 104, 13), (1, 1, 701, 2048, 64), (1, 1, 301, 4096, 2),
+         (2, 88, 1101, 480, 4)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("x_type,y_type", [("bf16", "bf16"), ("fp32", "bf16")])
+@pytest.mark.parametrize("shape", LARGE)
+def test_forward_of_large_images(P, shape, x_type, y_type):
+    import torch
+
+    if shape[0] * shape[1] > 100 and x_type == "fp32":
+        pytest.skip("the same path as bf16, twice the oracle's time")
+    par_gs = shape[3] + 1
+    x, _, gamma, beta, xt, yt = _inputs(shape, par_gs, x_type, y_type, seed=3)
+    y, mean, rstd = _run_forward(P, torch, shape, x.cuda(), gamma.cuda(), beta.cuda(), yt, "silu", par_gs)
+    _check_forward(shape, x, gamma, beta, y, mean, rstd, "silu", U16)
+    assert P.lsgd_device_status() == P.OK
+
+
+@pytest.mark.gpu
+def test_large_images_twice_at_once_captured_and_with_values_that_are_not_finite(P):
+    import torch
+
+    shape = G, B, Pn, C, groups = (1, 2, 13001, 168, 42)
+    x, _, gamma, beta, xt, yt = _inputs(shape, C, "bf16", "bf16")
+    clean = _run_forward(P, torch, shape, x.cuda(), gamma.cuda(), beta.cuda(), yt, "relu", C)
+    # a NaN in one image's group reaches the image's CTAs and no other group
+    x[0, 1, Pn // 3, 9] = float("nan")
+    xg, gg, bg, e = x.cuda(), gamma.cuda(), beta.cuda(), dict(device="cuda")
+    y, mean, rstd = _run_forward(P, torch, shape, xg, gg, bg, yt, "relu", C)
+    hit = torch.zeros(G, B, Pn, C, dtype=torch.bool, device="cuda")
+    hit[0, 1, :, 8:12] = True
+    hit = hit.reshape(-1)
+    assert torch.isnan(y[hit].float()).all() and torch.equal(y[~hit], clean[0][~hit])
+    # two streams' calls at once, a graph replayed, workspaces full of anything: the same bits
+    need = P.lsgd_groupnorm_workspace(G, B, Pn, C, groups, False)
+    outs = [(torch.empty_like(xg), torch.empty(B * groups, **e), torch.empty(B * groups, **e),
+             torch.full((need,), 255 * (i % 2), dtype=torch.uint8, **e)) for i in range(3)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+
+    def call(o, **kw):
+        P.lsgd_groupnorm_forward(xg, gg, bg, o[0], o[1], o[2], G, B, Pn, C, groups, act=P.ACT_RELU, workspace=o[3], **kw)
+
+    for _ in range(5):
+        for st, o in zip(streams, outs):
+            call(o, stream=st.cuda_stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(outs[2])
+    for _ in range(3):
+        outs[2][3].random_()
+        graph.replay()
+    torch.cuda.synchronize()
+    for o in outs:
+        assert torch.equal(o[0].reshape(-1).view(torch.int16), y.view(torch.int16))
+        assert torch.equal(o[1].view(torch.int32), mean.view(torch.int32))
+        assert torch.equal(o[2].view(torch.int32), rstd.view(torch.int32))
+    assert P.lsgd_device_status() == P.OK
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("shape", [(2, 3, 65, 64, 8), (1, 1, 5000, 72, 4), (2, 2, 49, 90, 9)])
 def test_same_bits_every_time_captured_and_on_another_stream(P, shape):
