@@ -889,7 +889,7 @@ __global__ void __launch_bounds__(1024, 1) gn_fwd_resident_kernel(const GnArgs a
   float* red = par + 2 * a.C;
   const int tx = threadIdx.x, ty = threadIdx.y, c0 = tx * V;
   const int tx_n = blockDim.x, ty_n = blockDim.y, threads = tx_n * ty_n, tid = ty * tx_n + tx, nw = threads >> 5;
-  const int rank = PIPE ? 0 : blockIdx.x & (a.cl - 1);
+  const int rank = PIPE ? 0 : blockIdx.x % a.cl;
   const bool shuffled = tx_n < 32 && (tx_n & (tx_n - 1)) == 0;
   const int p0 = rank * a.rows, p1 = min(a.P, p0 + a.rows), cnt = max(0, p1 - p0);
   const int first = p0 + ty, last = p1;
@@ -1034,7 +1034,7 @@ __global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a
   float* red = chans + 2 * a.C;       // [rows][C], twice
   const int tx = threadIdx.x, ty = threadIdx.y, c0 = tx * V;
   const int tx_n = blockDim.x, ty_n = blockDim.y, threads = tx_n * ty_n, tid = ty * tx_n + tx, nw = threads >> 5;
-  const int rank = PIPE ? 0 : blockIdx.x & (a.cl - 1);
+  const int rank = PIPE ? 0 : blockIdx.x % a.cl;
   const bool shuffled = tx_n < 32 && (tx_n & (tx_n - 1)) == 0;
   const int p0 = rank * a.rows, p1 = min(a.P, p0 + a.rows);
   const int first = p0 + ty, last = p1, step = ty_n * a.C, lane = tid & 31;
@@ -1218,13 +1218,34 @@ __global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a
   } while (PIPE && n < a.N);
 }
 
-// The resident form's CTAs per image (a power of two up to 16, the largest cluster), or 0: the split form.  A
+// The resident form's CTAs per image (up to 16, the largest cluster), or 0: the split form.  A
 // CTA of T threads takes `rows` positions if rows C / hold + C <= T, whatever the vector width (a row of threads is
-// C / V wide, and hold / V positions fall to each).  CTAs of about 512 threads or fewer where they do; then, where the images
-// are few, more CTAs to an image down to 4096 values each.  (One row of threads more than needed covers every V; with rows
-// rounded up to full warps a CTA has at most T + 31 threads.)
+// C / V wide, and hold / V positions fall to each).  A power of two: CTAs of about 512 threads or fewer where they do; then,
+// where the images are few, more CTAs to an image down to 4096 values each.  (One row of threads more than needed covers every
+// V; with rows rounded up to full warps a CTA has at most T + 31 threads.)  A cluster lies in one GPC: of 9 CTAs, 15 run at
+// once, of 10, 13, but of 16, 7.  Images that these fewer CTAs hold, and that would take another round in clusters of 16,
+// take one (backward of 15 images of 1517 x 90 in fp32: 31 us in clusters of 16, 19 in clusters of 9).
 bool gn_fits(int P, int C, int cl, int hold, int threads) {
   return (int64_t)((P + cl - 1) / cl) * C / hold + 1 + C <= threads;
+}
+// The threads across and down of a CTA of `rows` positions with vectors of V values: full warps where the rows of a warp are
+// added by shuffles, one at least otherwise.
+dim3 gn_block(int rows, int C, int V, int hold, bool* shuffled) {
+  const int tx = C / V;
+  *shuffled = tx < 32 && (tx & (tx - 1)) == 0;
+  int ty = std::max((rows + hold / V - 1) / (hold / V), (32 + tx - 1) / tx);
+  if (*shuffled) ty = (ty + 32 / tx - 1) / (32 / tx) * (32 / tx);
+  return dim3(tx, ty);
+}
+// The most threads that a CTA of a cluster of cl has, over the vectors that may be used.
+int64_t gn_threads(int P, int C, int cl, int hold) {
+  int64_t most = 0;
+  bool shuffled;
+  for (int V = 1; V <= 8 && C % V == 0; V *= 2) {
+    const dim3 b = gn_block((P + cl - 1) / cl, C, V, hold, &shuffled);
+    most = std::max(most, (int64_t)b.x * b.y);
+  }
+  return most;
 }
 constexpr int kMaxCluster = 16;
 int gn_cluster(int64_t N, int P, int C, int hold) {
@@ -1233,20 +1254,20 @@ int gn_cluster(int64_t N, int P, int C, int hold) {
     for (int c = 1; c <= kMaxCluster && !cl; c *= 2)
       if (gn_fits(P, C, c, hold, T)) cl = c;
   while (cl && cl < 8 && N * cl < kNumSMs && (int64_t)P * C / (2 * cl) >= 4096) cl *= 2;
+  if (cl == kMaxCluster && N > 7) {
+    if (N <= 13 && gn_threads(P, C, 10, hold) <= 1024) return 10;
+    if (N <= 15 && gn_threads(P, C, 9, hold) <= 1024) return 9;
+  }
   return cl;
 }
 
-// The shape of a resident launch with vectors of V values: threads across and down (full warps where the rows of a warp
-// are added by shuffles, one at least otherwise), and bytes of shared memory.
+// The shape of a resident launch with vectors of V values, and its bytes of shared memory.
 void gn_resident_shape(GnArgs& a, int V, int hold, bool bwd, dim3* block, size_t* smem) {
   a.rows = (a.P + a.cl - 1) / a.cl;
-  const int tx = a.C / V;
-  const bool shuffled = tx < 32 && (tx & (tx - 1)) == 0;
-  int ty = std::max((a.rows + hold / V - 1) / (hold / V), (32 + tx - 1) / tx);
-  if (shuffled) ty = (ty + 32 / tx - 1) / (32 / tx) * (32 / tx);
-  *block = dim3(tx, ty);
+  bool shuffled;
+  *block = gn_block(a.rows, a.C, V, hold, &shuffled);
   a.sub = std::min(V, a.D & -a.D);
-  const int rows = shuffled ? tx * ty / 32 : ty;
+  const int rows = shuffled ? block->x * block->y / 32 : block->y;
   *smem = 4 * (bwd ? 6 * (size_t)a.groups + 4 * (size_t)a.C + 2 * (size_t)rows * a.C
                    : 4 * (size_t)a.groups + 2 * (size_t)a.C + (size_t)rows * (a.C / a.sub));
 }

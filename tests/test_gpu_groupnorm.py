@@ -260,6 +260,23 @@ def _check_backward(shape, x, dy, gamma, beta, y, mean, rstd, dx, dgamma, dbeta,
     assert worst.max() <= 1.0, worst.max()
 
 
+# images that clusters of nine and of ten CTAs hold, in one of the directions or both, and one image more than run at once
+@pytest.mark.gpu
+@pytest.mark.parametrize("x_type,y_type", [("bf16", "bf16"), ("fp32", "fp32")])
+@pytest.mark.parametrize("shape", [(3, 5, 1517, 90, 9), (3, 3, 1517, 90, 9), (2, 5, 3001, 90, 9), (1, 13, 1040, 128, 16),
+                                   (2, 8, 1517, 90, 9), (1, 9, 2401, 64, 1), (1, 15, 130, 1024, 32)])
+def test_clusters_of_nine_and_ten(P, shape, x_type, y_type):
+    import torch
+
+    par_gs = shape[3] + 2
+    x, dy, gamma, beta, xt, yt = _inputs(shape, par_gs, x_type, y_type, seed=13)
+    gg, bg = gamma.cuda(), beta.cuda()
+    y, mean, rstd = _run_forward(P, torch, shape, x.cuda(), gg, bg, yt, "relu", par_gs)
+    _check_forward(shape, x, gamma, beta, y, mean, rstd, "relu", U16 if y_type == "bf16" else U32)
+    dx, dgamma, dbeta = _run_backward(P, torch, shape, x.cuda(), y, dy.cuda(), gg, bg, mean, rstd, "relu", par_gs)
+    _check_backward(shape, x, dy, gamma, beta, y, mean, rstd, dx, dgamma, dbeta, "relu", x_type)
+
+
 # images that no cluster holds: ranges of a few positions and of many; one group, groups within and across vectors; one
 # position's channels wider than the threads; many images
 LARGE = [(1, 1, 60007, 24, 1), (1, 2, 13001, 168, 42), (2, 3, 20011, 104, 13), (1, 1, 701, 2048, 64), (1, 1, 301, 4096, 2),
