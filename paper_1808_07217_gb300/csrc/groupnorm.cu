@@ -8,7 +8,8 @@
 //   dgamma = sum dz xh,  dbeta = sum dz (over the worker's images and positions),
 //   dx = rstd (gamma dz - m1 - xh m2).
 //
-// Both are bound by memory.  A thread owns V neighbouring channels (a vector of up to 16 bytes) and walks down the
+// Both are bound by memory: x read and y written once, and x, dy (for ReLU y) read and dx written once, where an image stays on
+// chip (the resident form below), one more read of the inputs where it does not (the split form).  A thread owns V neighbouring channels (a vector of up to 16 bytes) and walks down the
 // positions, so that its parameters and channel sums stay in registers whatever the group width.
 #include <algorithm>
 #include <atomic>
@@ -178,6 +179,11 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, int bytes,
 }
 
 // ---- split form: any size, three launches ----
+//
+// The sums over ranges of an image's positions, their merge, and a second pass from the statistics.  Forward of 8 images of 127 x
+// 129 x 320 in bf16 with SiLU: 55 us (about 20, 6 and 29; 168 MB at least, 3.1 TB/s): the merge's latency, the second read of x,
+// most of which L2 no longer holds, and SiLU's two special functions a value.  One cooperative launch that keeps a third of x
+// in shared memory between the passes took 57.6: its two ends and the wait between them cost what the kept third saves.
 
 constexpr int kSplitThreads = 256;
 
@@ -361,7 +367,8 @@ __global__ void __launch_bounds__(kSplitThreads) gn_partial_kernel(const GnArgs 
 
 // The forward's first pass where the vectors are of 16 bytes: a range's positions lie one behind another in memory, and bulk
 // copies bring kRingRows of them to every row of threads at a time, two to four such chunks ahead, so that the loads do not wait
-// for the sums.  (84 MB of 8 images: 26 us with the kernel above, whose loads stop while a batch is added up.)
+// for the sums.  (84 MB of 8 images: 20 us, 26 with the kernel above, whose loads stop while a batch is added up; the whole call
+// 57 and 62.5.)  Other vectors take that kernel: bulk copies need 16-byte rows.
 constexpr int kRingRows = 4;
 constexpr size_t kRingSmem = 112 * 1024;  // two CTAs to an SM
 
@@ -873,7 +880,10 @@ __device__ __forceinline__ void each_group(int c0, int D, F f) {
 
 // Pipelined (PIPE): where there are more images than CTAs on the SMs at once, a CTA takes images blockIdx.x, blockIdx.x +
 // gridDim.x, ... and bulk copies bring the next `stages` of them to shared memory while one is worked on in registers, so
-// that the loads never stop for the sums' barriers.  One CTA to an image then, and 16-byte vectors.
+// that the loads never stop for the sums' barriers.  One CTA to an image then, and 16-byte vectors.  2048 images of 1024 x 16, fp32
+// to bf16 with ReLU: forward 37 us (5.4 TB/s), 55 without; backward 78 us (5.2 TB/s), 102 without; what is left is the
+// sums' latency at the start and the end, and the copies' and stores' turns on the memory.  With fewer than two rounds of
+// CTAs there is nothing to bring ahead.
 constexpr int kMaxStages = 4, kPipeHead = 64;  // bytes before the first buffer: the barriers
 
 template <typename XT, typename YT, int V, bool PIPE>
@@ -1261,6 +1271,26 @@ int gn_cluster(int64_t N, int P, int C, int hold) {
   return cl;
 }
 
+// Whether the split form, which reads its inputs twice but fills all SMs, takes less time than many rounds of clusters, whose
+// CTAs load, wait for one another and store in turn.  A model in us, fitted to 120 pairs of measurements (4 to 512 images of
+// 32,000 to 400,000 values): a round costs 6 us of bf16 images, 9 of fp32 ones, more in clusters of 16 and with one CTA to
+// an SM; the split form its launches and 6 TB/s.  (Of another 100 pairs it takes the slower form, by 3 us or more, in 17.)
+// Forward of 128 images of 3100 x 64 in bf16: 74 us in clusters, 47 split, of 32 images: 25 and 26; backward of 128 images of
+// 1550 x 64: 69 and 59, of 32: 25 and 30.
+bool gn_split_faster(int cl, int64_t N, int P, int C, bool bwd, int xz, int yz, bool relu) {
+  if (cl < 4) return false;  // such images mostly fit one CTA, whose pipelined form overlaps its rounds
+  const int per_sm = (int64_t)((P + cl - 1) / cl) * C / (bwd ? kBwdHold : kFwdHold) + C / 8 <= 512 ? 2 : 1;
+  const int at_once = (cl == 4 ? 36 : cl <= 9 ? 15 : cl == 10 ? 13 : 7) * per_sm;
+  const double round = (3 + 0.75 * (xz + yz)) * (per_sm == 2 ? 1.0 : 1.2) * (cl > 10 ? 1.15 : 1.0);
+  const int bytes = bwd ? 3 * xz + (relu ? 4 : 2) * yz : 2 * xz + yz;
+  return (bwd ? 20 : 18) + (double)N * P * C * bytes / 6e6 < 5 + round * ((N + at_once - 1) / at_once);
+}
+// The form of a call: CTAs per image, or 0.
+int gn_plan(int64_t N, int P, int C, bool bwd, int xz, int yz, bool relu) {
+  const int cl = gn_cluster(N, P, C, bwd ? kBwdHold : kFwdHold);
+  return gn_split_faster(cl, N, P, C, bwd, xz, yz, relu) ? 0 : cl;
+}
+
 // The shape of a resident launch with vectors of V values, and its bytes of shared memory.
 void gn_resident_shape(GnArgs& a, int V, int hold, bool bwd, dim3* block, size_t* smem) {
   a.rows = (a.P + a.cl - 1) / a.cl;
@@ -1375,11 +1405,14 @@ int gn_vec(int v, int C, const void* p, int z) {
   return v;
 }
 
+// Enough for the form that any types and activation take.
 size_t gn_workspace(int64_t N, int P, int C, int groups, bool backward) {
   const int cl = gn_cluster(N, P, C, backward ? kBwdHold : kFwdHold);
-  if (cl) return backward ? 4 * (size_t)N * cl * C * 2 : 0;
-  const size_t split = (size_t)N * gn_ranges(N, P, C) * C * 2;
-  return 4 * (split + (backward ? (size_t)N * C * 2 + (size_t)N * groups * 2 : 0));
+  bool split = cl == 0;
+  for (int t = 0; t < 8 && !split; ++t) split = gn_split_faster(cl, N, P, C, backward, t & 1 ? 4 : 2, t & 2 ? 4 : 2, t & 4);
+  const size_t resident = backward ? (size_t)N * cl * C * 2 : 0;
+  const size_t ranges = (size_t)N * gn_ranges(N, P, C) * C * 2 + (backward ? (size_t)N * C * 2 + (size_t)N * groups * 2 : 0);
+  return 4 * (split ? std::max(resident, ranges) : resident);
 }
 
 lsgd_status gn_error(lsgd_status s, const char* fn, const char* what) {
@@ -1460,7 +1493,7 @@ lsgd_status lsgd_groupnorm_forward(const void* x, int x_type, const float* gamma
   a.x = x, a.out = y, a.gamma = gamma, a.beta = beta, a.par_gs = par_gs, a.mean = mean, a.rstd = rstd;
   a.part = static_cast<float*>(workspace);
   a.B = B, a.P = (int)P, a.C = C, a.groups = groups, a.D = C / groups, a.act = act, a.N = N, a.eps = eps;
-  a.cl = gn_cluster(N, a.P, C, kFwdHold);
+  a.cl = gn_plan(N, a.P, C, false, xz, yz, false);
   const int v = gn_vec(gn_vec(xb ? 8 : 4, C, x, xz), C, y, yz);
   const cudaError_t e = gn_typed<false>(a, xb, yb, v, (cudaStream_t)stream);
   return e == cudaSuccess ? LSGD_OK : gn_error(LSGD_ECUDA, fn, cudaGetErrorString(e));
@@ -1502,7 +1535,7 @@ lsgd_status lsgd_groupnorm_backward(const void* x, int x_type, const void* y, co
   a.mean = const_cast<float*>(mean), a.rstd = const_cast<float*>(rstd), a.dgamma = dgamma, a.dbeta = dbeta;
   a.B = B, a.P = (int)P, a.C = C, a.groups = groups, a.D = C / groups, a.act = act, a.N = N;
   a.part = static_cast<float*>(workspace);
-  a.cl = gn_cluster(N, a.P, C, kBwdHold);
+  a.cl = gn_plan(N, a.P, C, true, xz, yz, relu);
   a.sums = a.cl ? a.part : a.part + (size_t)N * gn_ranges(N, a.P, C) * C * 2;
   a.m12 = a.sums + (size_t)N * C * 2;
   int v = gn_vec(gn_vec(gn_vec(xb ? 8 : 4, C, x, xz), C, dx, xz), C, dy, yz);

@@ -19,7 +19,8 @@ SHAPES = [(1, 1, 1, 1, 1), (2, 3, 5, 6, 3), (1, 2, 64, 64, 8), (2, 2, 49, 90, 9)
 # more images than the SMs hold at once: a CTA takes several, with the next ones' loads under way (and where the sizes are
 # odd, one each); few and many groups, a worker's images ending between two of a CTA's
 MANY = [(5, 521, 64, 16, 4), (3, 800, 9, 24, 24), (2, 1300, 100, 8, 1), (7, 90, 1024, 16, 4), (2, 611, 1, 64, 8), (1, 2500, 16, 6, 3),
-        (11, 60, 260, 64, 16), (1, 3, 40000, 96, 6), (2, 1, 60001, 40, 8), (1, 12, 5003, 256, 1), (1, 2, 9001, 1536, 8)]
+        (11, 60, 260, 64, 16), (1, 3, 40000, 96, 6), (2, 1, 60001, 40, 8), (1, 12, 5003, 256, 1), (1, 2, 9001, 1536, 8),
+        (2, 16, 5000, 48, 4), (4, 16, 2500, 48, 4)]
 
 
 @pytest.fixture(scope="module")
