@@ -478,12 +478,13 @@ lsgd_status lsgd_direction_update(float* w, int64_t w_gs, const uint16_t* o, int
  * Deterministic.  Non-finite values of x make their own image's group NaN and no other.
  *
  * `workspace` is device memory of at least the bytes that lsgd_groupnorm_workspace reports (0: it is
- * not used and may be NULL), 16-byte aligned, whose contents do not matter before or after; calls (or captured graphs) that may run at
- * the same time need one each.  No allocation: the calls may be captured into a CUDA graph.
- * G <= 65535, G B <= 2^24, P <= 2^24, C <= 65536, sizes >= 1, C a multiple of groups, eps > 0.  Any C
- * and any alignment of at least the element's are taken; vectors of up to 16 bytes are used where C
- * and the pointers allow.  LSGD_EINVAL on anything else and for tensors that overlap.  Device pointers,
- * asynchronous on `stream`, which belongs to the current device. */
+ * not used and may be NULL), 16-byte aligned, whose contents do not matter before or after; calls (or
+ * captured graphs) that may run at the same time need one each.  No allocation: the calls may be
+ * captured into a CUDA graph.  G <= 65535, G B <= 2^24, P <= 2^24, C <= 65536, sizes >= 1, C a multiple of
+ * groups, eps > 0.  Any C and any alignment of at least the element's are taken; vectors of up to 16 bytes
+ * are used where C and the pointers allow.  LSGD_EINVAL on anything else and for tensors that overlap.
+ * Device pointers, asynchronous on `stream`, which belongs to the current device; lsgd_device_status
+ * reports a device-side wait that ran out. */
 typedef enum { LSGD_ACT_NONE = 0, LSGD_ACT_RELU = 1, LSGD_ACT_SILU = 2 } lsgd_activation;
 lsgd_status lsgd_groupnorm_workspace(int G, int B, int64_t P, int C, int groups, int backward,
                                      size_t* bytes);

@@ -18,8 +18,9 @@
 // t stands in for the part of P l that is a multiple of l: 0, but in the last two steps the largest d_i.  (A t that is not
 // an eigenvalue of P puts (P - t) l where X has nothing, which later steps would amplify.)  fp16 rather than bf16: the
 // same rate, 3 more bits; its range is enough because every value is stored times 2^12 and bounded: singular values of X
-// are at most 1.21, so |A| < 1.47 and |P| < 2.9 at all steps.  Measured and modelled: 6e-4 to 1e-3 off (relative 2-norm,
-// before the bf16 rounding of 1.7e-3) for random, rank-deficient and ill-conditioned matrices.
+// are at most 1.21, so |A| < 1.47 and |P| < 2.9 at all steps.  Measured and modelled: 6e-4 to 1.3e-3 off (relative 2-norm,
+// before the bf16 rounding of 1.7e-3) for random, rank-deficient and ill-conditioned matrices, up to 1.9e-3 for a handful of
+// values or a smaller side of at most 64.
 #include <cuda_fp16.h>
 #include <cudaTypedefs.h>
 
@@ -85,6 +86,11 @@ struct DirArgs {
 };
 
 constexpr int kMomThreads = 256;
+
+// Two passes before the products, because all of a matrix's squares come before its first quotient: u and the norm's partial
+// sums, then h and l.  Bound by memory, 12 bytes a value each (the second finds part of u and g in L2): 27 and 31 us for 16 x
+// 1024 x 1024 in fp32, 7.4 and 6.5 TB/s.  Vectors of 8 or 4 values where every matrix's rows are aligned to them, single
+// values otherwise (the whole call 401, 403 and 438 us).
 
 // V gradient or momentum values from element i of a matrix.
 template <int V>
@@ -240,15 +246,18 @@ __global__ void __launch_bounds__(kMomThreads) direction_normalise_kernel(const 
 //   warps 4-19  epilogue: a warp per 32 rows and 16 columns of a buffer, in place, each at its own pace (8 warps took 13,000
 //               cycles a tile, mostly latencies, against the products' 8,200 at k = 1024)
 //
-//
 // Where the tiles are few (PAIR false) each CTA works for itself on 128 x 128 tiles: half the products and half the epilogue
-// between a tile's start and its count, for twice the operand bytes per product (direction_tile chooses).
+// between a tile's start and its count, for twice the operand bytes per product (direction_pairs chooses).
 //
 // The tiles of all steps form one list: per step the tiles of A = X X^T of every matrix, then those of P, then those of
 // X.  Pair p takes tiles p, p + pairs, ...; `done[g]` counts the CTAs' finished tiles of matrix g, whose phases follow one
 // another, and a tile starts when its matrix's earlier phases are complete.  The launch is cooperative (all pairs are
 // resident) and every tile's predecessors stand before it in the list, so that every wait ends; matrices fill each
 // other's phase ends, and nothing is launched between phases.
+//
+// Measured, five steps: 16 x 1024 x 1024 in 329 us (1.04 PFLOP/s of the products that symmetry leaves; bound by the phases'
+// ends, where tiles wait for their matrix, and by operands from L2), 4 x 4096 x 4096 in 4.1 ms (1.34 PFLOP/s; the SM clock falls
+// to 1.4 GHz under the power limit, where a library product runs at 1.70).
 
 constexpr int kHalf = 128, kBK = 64, kStages = 4, kEpi = 3, kEpiWarps = 16, kThreads = 128 + 32 * kEpiWarps, kChunk = 64;
 constexpr uint32_t kOpBytes = kHalf * kBK * 2;  // one operand's share of a stage in a CTA; half an epilogue buffer
@@ -685,7 +694,10 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(PAIR ? 2 : 1, 1,
         if (el) {
           const int x = q.n0 + c;
           if (m0 < q.M && by_tma) {
-            const CUtensorMap* to = q.role == GRAM ? &args.ak : q.role == POLY ? &args.pk : q.role == NEXT ? &args.xk[in ^ 1] : &args.om;
+            const CUtensorMap* to = q.role == GRAM   ? &args.ak
+                                    : q.role == POLY ? &args.pk
+                                    : q.role == NEXT ? &args.xk[in ^ 1]
+                                                     : &args.om;
             tma_store(to, sm.e[e][0], x, m0, q.g);
             if (q.role == NEXT) tma_store(&args.lk[in ^ 1], sm.e[e][1], x, m0, q.g);
             if (mirror) {
@@ -868,8 +880,10 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(PAIR ? 2 : 1, 1,
 //   3. tcgen05: A A, then P in A's place;
 //   4. tcgen05: X P, 128 rows to a tile (above n = 64 two tiles at a time); each thread updates its row from its tile.
 // Up to n = 64 both h and l are multiplied, so that small matrices, whose roundings do not average out, are off by less
-// than 2.5e-3 too.  What a step costs is its chain of latencies (about 5 us at 100 x 4096 in eight CTAs), which the work
-// in it hardly lengthens.
+// than 2.5e-3 too.  What bounds it is each step's chain of latencies (products, their sums' exchange, products, products, the
+// rows' update), which the work in it hardly lengthens: 16 matrices of 16 x 144 take 15 us (launch included; their bytes
+// 0.1), 16 of 100 x 4096 take 119 (bytes 13.5).  The 128 columns that a tile of products has are its limit; there it is still the
+// faster: 16 x 128 x 1024 in 105 us (110 by the tiles of the form above), 16 x 128 x 128 in 70 (88), 16 x 100 x 4096 in 119 (197).
 
 constexpr int kRows = 512;       // rows of a CTA
 constexpr int kResSide = 128;
@@ -1122,12 +1136,16 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
               batch(bf16, (int64_t)(m0 + warp * 32 + row) * n + b + col, 2 * n,
                     [&](int q) { return warp * 32 + 2 * q + row < have && b + col < n; },
                     [&](int q, float v) {
-                      asm volatile("st.shared.f32 [%0], %1;" ::"r"(stage + (2 * q + row) * 64 + ((col ^ (q & 15)) << 2)), "f"(v) : "memory");
+                      asm volatile("st.shared.f32 [%0], %1;" ::"r"(stage + (2 * q + row) * 64 + ((col ^ (q & 15)) << 2)), "f"(v)
+                                   : "memory");
                     });
               __syncwarp();
 #pragma unroll
               for (int q = 0; q < 16; ++q)
-                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[q]) : "r"(stage + lane * 64 + ((q ^ (lane >> 1 & 15)) << 2)) : "memory");
+                asm volatile("ld.shared.f32 %0, [%1];"
+                             : "=f"(x[q])
+                             : "r"(stage + lane * 64 + ((q ^ (lane >> 1 & 15)) << 2))
+                             : "memory");
               __syncwarp();
             }
           };
@@ -1226,7 +1244,8 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
             }
             const __half2 w0 = __floats2half2_rn(f[0], f[1]), w1 = __floats2half2_rn(f[2], f[3]);
             const uint32_t b0 = *reinterpret_cast<const uint32_t*>(&w0), b1 = *reinterpret_cast<const uint32_t*>(&w1);
-            const uint32_t to = as + (j >> 4) * (128 * kPiece) + i * kPiece + ((((j & 15) >> 1) << 4) ^ ((i & 7) << 4)) + (j & 1) * 8;
+            const uint32_t to = as + (j >> 4) * (128 * kPiece) + i * kPiece +
+                                ((((j & 15) >> 1) << 4) ^ ((i & 7) << 4)) + (j & 1) * 8;
             const uint32_t da = smem_u32(&tail.da[i]);
             if constexpr (kOne) {
               asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(b0), "r"(b1) : "memory");
@@ -1284,7 +1303,8 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
           for (int e = tid; e < all; e += rows) {
             const int i = e / per_row, j = e % per_row;
             const uint2 w = __ldcg(full + e);
-            const uint32_t to = as + (j >> 4) * (128 * kPiece) + i * kPiece + ((((j & 15) >> 1) << 4) ^ ((i & 7) << 4)) + (j & 1) * 8;
+            const uint32_t to = as + (j >> 4) * (128 * kPiece) + i * kPiece +
+                                ((((j & 15) >> 1) << 4) ^ ((i & 7) << 4)) + (j & 1) * 8;
             asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(w.x), "r"(w.y) : "memory");
           }
           for (int i = tid; i < n16; i += rows) tail.da[i] = __ldcg(diag + i);
@@ -1393,7 +1413,8 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               const float t = kA + dj[i];
-              f[i] = kBoth ? fmaf(t, f[i] + lo[i], kUnscale * v[8 * j + i]) : fmaf(t, f[i], fmaf(kA + top, lo[i], kUnscale * v[8 * j + i]));
+              f[i] = kBoth ? fmaf(t, f[i] + lo[i], kUnscale * v[8 * j + i])
+                           : fmaf(t, f[i], fmaf(kA + top, lo[i], kUnscale * v[8 * j + i]));
             }
             if (!last) {
               const uint4 w = pack8(f);
@@ -1427,7 +1448,8 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
               for (int rr = lane >> 4; rr < 32; rr += 2)
                 if (warp * 32 + rr < have) {
                   uint16_t v;
-                  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(stage + rr * 32 + (((i >> 3) ^ (rr >> 2 & 1)) << 4) + (i & 7) * 2) : "memory");
+                  const uint32_t from = stage + rr * 32 + (((i >> 3) ^ (rr >> 2 & 1)) << 4) + (i & 7) * 2;
+                  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(from) : "memory");
                   o[rr * n] = v;
                 }
             __syncwarp();
@@ -1446,7 +1468,8 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
 }
 
 // ------------------------------------------------------------------------------------------------
-// w = (1 - lr wd) w - lr scale o, and its bf16 copy
+// w = (1 - lr wd) w - lr scale o, and its bf16 copy: one pass bound by memory, 12 bytes a value.  16 x 4096 x 4096 in 526 us,
+// 6.1 TB/s.  Eight values to a thread's access where addresses and strides allow, else one (746 us).
 
 constexpr int kUpdThreads = 256;
 
@@ -1605,7 +1628,8 @@ int resident_product_ctas(int dev, size_t smem, cudaError_t* err) {
 // Whether pairs of CTAs on 256 x 256 tiles are the faster, by a model of a step's three phases: rounds of tiles, each the longer
 // of the products' time per k-block of 64 (600 cycles for a pair; 450 for a CTA alone, whose tile a quarter the size needs
 // half the operand bytes) and what a tile costs beside them (from the wait for its matrix's last phase to its count: 11,000
-// and 7,000 cycles).
+// and 7,000 cycles).  Measured, pairs against single CTAs, in us: 16 x 1024 x 1024 399 and 504, 4096 x 4096 1065 and 1430, but
+// 2048 x 2048 263 and 248, 5 x 1031 x 777 222 and 188, 16 x 512 x 512 162 and 138, 512 x 512 135 and 103.
 bool direction_pairs(int G, int64_t rows, int64_t cols) {
   const int64_t n = std::min(rows, cols), m = std::max(rows, cols);
   auto cost = [&](int tile, int workers, int per_block, int beside) {
@@ -1641,7 +1665,8 @@ cudaError_t launch_products(const MmArgs& a, cudaStream_t st) {
 
 // The resident form's CTAs per matrix: a cluster (a power of two up to 8, the portable size), or `groups` groups of `cl` that
 // exchange through global memory where the m rows are too many for a cluster, or where clusters of 8, of which the SMs hold 15 at
-// once, take more rounds than the groups, of which they hold 152 / cl.  cl = 0: the smaller side is too large.
+// once, take more rounds than the groups, of which they hold 152 / cl.  (16 x 100 x 4096: 195 us in two rounds of clusters, 119 in
+// one of groups; of as many rounds the clusters' are the shorter.)  cl = 0: the smaller side is too large.
 struct ResPlan {
   int cl, groups;  // groups = 0: clusters
 };
@@ -1803,6 +1828,7 @@ lsgd_status lsgd_orthogonal_direction(float* u, int64_t u_gs, const void* g, int
   if (bad) return dir_error(LSGD_EINVAL, fn, bad);
   const DirLayout ly = direction_layout(G, rows, cols);
   const int64_t n = rows * cols;
+  if (G == 1) u_gs = g_gs = o_gs = n;  // a single matrix's strides do not matter
   const bool gb = g_type == LSGD_BF16;
   const size_t span_u = 4 * ((size_t)(G - 1) * std::max<int64_t>(u_gs, 0) + n);
   const size_t span_g = (gb ? 2 : 4) * ((size_t)(G - 1) * std::max<int64_t>(g_gs, 0) + n);
@@ -1820,7 +1846,7 @@ lsgd_status lsgd_orthogonal_direction(float* u, int64_t u_gs, const void* g, int
                                 overlap(workspace, ly.bytes, u, span_u))))
     bad = "tensors overlap";
   const int64_t ts = (ly.n + 127) / 128, tx = ((rows + 127) / 128) * ((cols + 127) / 128);
-  if (!bad && G * (ts * (ts + 1) + tx) * steps > 0x3fffffff) bad = "too many matrices of this size in one call";
+  if (!bad && ly.n && G * (ts * (ts + 1) + tx) * steps > 0x3fffffff) bad = "too many matrices of this size in one call";
   if (bad) return dir_error(LSGD_EINVAL, fn, bad);
   DirArgs d{};
   d.u = u, d.g = g, d.o = o, d.u_gs = u_gs, d.g_gs = g_gs, d.o_gs = o_gs;
@@ -1855,8 +1881,8 @@ lsgd_status lsgd_direction_update(float* w, int64_t w_gs, const uint16_t* o, int
   const dim3 grid((unsigned)std::min<int64_t>((n + per - 1) / per, most), G);
   const float keep = (float)(1.0 - (double)lr * weight_decay), step = (float)((double)lr * scale);
   const cudaStream_t st = (cudaStream_t)stream;
-  const cudaError_t e = vec ? launch_pdl(direction_update_kernel<8>, grid, dim3(kUpdThreads), 0, st, w, o, Wb, n, w_gs, o_gs, keep, step)
-                            : launch_pdl(direction_update_kernel<1>, grid, dim3(kUpdThreads), 0, st, w, o, Wb, n, w_gs, o_gs, keep, step);
+  const cudaError_t e = launch_pdl(vec ? direction_update_kernel<8> : direction_update_kernel<1>, grid, dim3(kUpdThreads), 0, st, w,
+                                   o, Wb, n, w_gs, o_gs, keep, step);
   return e == cudaSuccess ? LSGD_OK : dir_error(LSGD_ECUDA, fn, cudaGetErrorString(e));
 }
 

@@ -223,6 +223,27 @@ def test_same_bits_every_time_captured_and_on_another_stream(P, shape):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(1, 40, 72), (1, 192, 256)])
+@pytest.mark.parametrize("stride", [0, 1, -8, 1 << 60])
+def test_a_single_matrix_has_no_strides(P, shape, stride):
+    import ctypes
+
+    import torch
+
+    _, rows, cols = shape
+    x = np.random.default_rng(4).standard_normal(shape)
+    g = torch.tensor(x, dtype=torch.float32, device="cuda")
+    o = torch.empty(shape, dtype=torch.bfloat16, device="cuda")
+    need = P.lsgd_orthogonal_workspace(1, rows, cols)
+    ws = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
+    st = P.lib().lsgd_orthogonal_direction(None, stride, g.data_ptr(), P.FP32, stride, o.data_ptr(), stride, 1, rows, cols,
+                                           ctypes.c_float(0.0), 0, 5, ws.data_ptr(), need, None)
+    torch.cuda.synchronize()
+    assert st == P.OK
+    _check(o, x)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("G,n,gs,lead", [(1, 1, 0, 16), (3, 17, 0, 16), (2, 4096, 0, 16), (2, 4096, 8, 8), (4, 1000, 5, 3), (1, 999, 0, 1),
                                          (64, 640, 64, 16), (2, 300001, 0, 16), (1, 1 << 20, 0, 16)])
 @pytest.mark.parametrize("shadow", [True, False])
