@@ -1469,7 +1469,8 @@ __global__ void __launch_bounds__(kRows, 1) direction_resident_kernel(const ResA
 
 // ------------------------------------------------------------------------------------------------
 // w = (1 - lr wd) w - lr scale o, and its bf16 copy: one pass bound by memory, 12 bytes a value.  16 x 4096 x 4096 in 526 us,
-// 6.1 TB/s.  Eight values to a thread's access where addresses and strides allow, else one (746 us).
+// 6.1 TB/s.  Eight values to a thread's access where addresses and strides allow, else one (746 us).  Workers' values that
+// follow one another are one long vector, whatever n is.
 
 constexpr int kUpdThreads = 256;
 
@@ -1481,12 +1482,15 @@ __global__ void __launch_bounds__(kUpdThreads) direction_update_kernel(float* w,
   const int64_t k = blockIdx.y;
   w += k * w_gs, o += k * o_gs;
   if (wb) wb += k * w_gs;
+  auto one = [&](int64_t i) {
+    const float v = fmaf(-step, bf2f(o[i]), keep * w[i]);
+    w[i] = v;
+    if (wb) wb[i] = f2bf(v);
+  };
   const int64_t stride = (int64_t)gridDim.x * kUpdThreads * V;
-  for (int64_t i = ((int64_t)blockIdx.x * kUpdThreads + threadIdx.x) * V; i < n; i += stride) {
+  for (int64_t i = ((int64_t)blockIdx.x * kUpdThreads + threadIdx.x) * V; i + V <= n; i += stride) {
     if constexpr (V == 1) {
-      const float v = fmaf(-step, bf2f(o[i]), keep * w[i]);
-      w[i] = v;
-      if (wb) wb[i] = f2bf(v);
+      one(i);
     } else {
       const uint4 ov = *reinterpret_cast<const uint4*>(o + i);
       float4 a = *reinterpret_cast<const float4*>(w + i), b = *reinterpret_cast<const float4*>(w + i + 4);
@@ -1507,6 +1511,7 @@ __global__ void __launch_bounds__(kUpdThreads) direction_update_kernel(float* w,
       if (wb) *reinterpret_cast<uint4*>(wb + i) = make_uint4(bw[0], bw[1], bw[2], bw[3]);
     }
   }
+  if (blockIdx.x == 0 && threadIdx.x < n % V) one(n - n % V + threadIdx.x);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -1874,7 +1879,8 @@ lsgd_status lsgd_direction_update(float* w, int64_t w_gs, const uint16_t* o, int
     if (overlap(w, spw, o, spo) || overlap(w, spw, Wb, spb) || overlap(o, spo, Wb, spb)) bad = "tensors overlap";
   }
   if (bad) return dir_error(LSGD_EINVAL, fn, bad);
-  const bool vec = n % 8 == 0 && !off_align(w, 16) && !off_align(o, 16) && !off_align(Wb, 16) &&
+  if (w_gs == n && o_gs == n) n *= G, G = 1;
+  const bool vec = n >= 8 && !off_align(w, 16) && !off_align(o, 16) && !off_align(Wb, 16) &&
                    (G == 1 || (w_gs % 8 == 0 && o_gs % 8 == 0));
   const int64_t per = (int64_t)kUpdThreads * (vec ? 8 : 1);
   const int64_t most = std::max<int64_t>(1, 8LL * kNumSMs / G);

@@ -245,7 +245,8 @@ def test_a_single_matrix_has_no_strides(P, shape, stride):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("G,n,gs,lead", [(1, 1, 0, 16), (3, 17, 0, 16), (2, 4096, 0, 16), (2, 4096, 8, 8), (4, 1000, 5, 3), (1, 999, 0, 1),
-                                         (64, 640, 64, 16), (2, 300001, 0, 16), (1, 1 << 20, 0, 16)])
+                                         (64, 640, 64, 16), (2, 300001, 0, 16), (1, 1 << 20, 0, 16), (7, 4099, 0, 16),
+                                         (3, 1001, 7, 16), (5, 300007, 1, 16), (1, 9, 0, 16)])
 @pytest.mark.parametrize("shadow", [True, False])
 def test_update(P, G, n, gs, lead, shadow):
     import torch
