@@ -445,7 +445,8 @@ lsgd_status lsgd_batchnorm_stats_noalloc(const float* y, int64_t P, int C, int G
  * `workspace`: device memory of at least lsgd_orthogonal_workspace's bytes (0 for most matrices with a
  * side of at most 128: it is not used then and may be NULL), 256-byte aligned, whose contents do
  * not matter before or after; calls (or captured graphs) that may run at the same time
- * need one each.  No allocation: the calls may be captured into a CUDA graph.  LSGD_EINVAL for bad
+ * need one each, and streams of one priority: larger calls are cooperative launches, whose CTAs have to be
+ * on the GPU together.  No allocation: the calls may be captured into a CUDA graph.  LSGD_EINVAL for bad
  * arguments, too small a workspace and tensors that overlap.  Device pointers, asynchronous on `stream`, which
  * belongs to the current device; lsgd_device_status reports a device-side wait that ran out. */
 lsgd_status lsgd_orthogonal_workspace(int G, int64_t rows, int64_t cols, size_t* bytes);

@@ -180,7 +180,7 @@ def test_zero_and_not_finite_matrices_keep_to_themselves(P, shape):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("shape", [(3, 64, 576), (2, 300, 257)])
+@pytest.mark.parametrize("shape", [(3, 64, 576), (2, 300, 257), (3, 40, 5000), (1, 4600, 100)])
 def test_same_bits_every_time_captured_and_on_another_stream(P, shape):
     import torch
 
@@ -220,6 +220,40 @@ def test_same_bits_every_time_captured_and_on_another_stream(P, shape):
     for got in (other, named, played):
         for a, b in zip(got, want):
             assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+def test_calls_of_every_form_at_once(P):
+    """Clusters, groups that meet in global memory and both kinds of tiles on two streams, each call with its own workspace."""
+    import torch
+
+    shapes = [(20, 64, 576), (2, 40, 5000), (2, 300, 257), (1, 4600, 100), (4, 1024, 1024), (1, 300, 600)]
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    gs = [torch.randn(s, generator=gen, device="cuda") for s in shapes]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+
+    def buffers():
+        return [(torch.zeros_like(g), torch.empty_like(g, dtype=torch.bfloat16),
+                 torch.empty(max(P.lsgd_orthogonal_workspace(*g.shape), 1), dtype=torch.uint8, device="cuda")) for g in gs]
+
+    def call(g, b, **kw):
+        P.lsgd_orthogonal_direction(b[0], g, b[1], *g.shape, workspace=b[2], **kw)
+
+    want = buffers()
+    for _ in range(3):
+        for g, b in zip(gs, want):
+            call(g, b)
+    got = [buffers(), buffers()]
+    torch.cuda.synchronize()
+    for _ in range(3):  # one stream's calls in the other order, so that different forms meet
+        for i in range(len(gs)):
+            call(gs[i], got[0][i], stream=streams[0].cuda_stream)
+            call(gs[-1 - i], got[1][-1 - i], stream=streams[1].cuda_stream)
+    torch.cuda.synchronize()
+    assert P.lsgd_device_status() == P.OK
+    for bs in got:
+        for b, w in zip(bs, want):
+            assert torch.equal(b[0], w[0]) and torch.equal(b[1], w[1])
 
 
 @pytest.mark.gpu
