@@ -1671,7 +1671,10 @@ cudaError_t launch_products(const MmArgs& a, cudaStream_t st) {
 // The resident form's CTAs per matrix: a cluster (a power of two up to 8, the portable size), or `groups` groups of `cl` that
 // exchange through global memory where the m rows are too many for a cluster, or where clusters of 8, of which the SMs hold 15 at
 // once, take more rounds than the groups, of which they hold 152 / cl.  (16 x 100 x 4096: 195 us in two rounds of clusters, 119 in
-// one of groups; of as many rounds the clusters' are the shorter.)  cl = 0: the smaller side is too large.
+// one of groups; of as many rounds the clusters' are the shorter: 8 x 100 x 4096 91 and 113.)  CTAs of at most 256 rows where
+// that takes no second round: 16 x 100 x 512 78 us in single CTAs, 61 in clusters of two; 32 x 2048 36 and 28; in groups only above
+// n = 64: 100 x 5000 115 and 99, but 2 x 40 x 9000 71 and 73.  Below 256 rows another CTA costs more than it takes over (4 x 16 x
+// 256: 16 and 18).  cl = 0: the smaller side is too large.
 struct ResPlan {
   int cl, groups;  // groups = 0: clusters
 };
@@ -1681,8 +1684,12 @@ ResPlan resident_plan(int G, int64_t rows, int64_t cols) {
   int cl = 1;
   while (cl < 8 && (m + cl - 1) / cl > kRows) cl *= 2;
   const int need = (int)((m + kRows - 1) / kRows), at_once = kNumSMs / need;
+  // (all matrices in one round of the larger clusters, of which 76, 36 and 15 fit)
+  while (cl < 8 && (m + cl - 1) / cl > kRows / 2 && G <= (cl == 1 ? 76 : cl == 2 ? 36 : 15)) cl *= 2;
   const bool fits = (m + cl - 1) / cl <= kRows;
   if (fits && (cl < 8 || (G + 14) / 15 <= (G + at_once - 1) / at_once)) return ResPlan{cl, 0};
+  const int half = (int)((m + kRows / 2 - 1) / (kRows / 2));
+  if (n > 64 && (int64_t)G * half <= kNumSMs) return ResPlan{half, G};
   return ResPlan{need, std::min(G, at_once)};
 }
 

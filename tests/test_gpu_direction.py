@@ -21,7 +21,7 @@ def _off(shape):
 SHAPES = [(1, 1, 1), (3, 1, 7), (2, 7, 1), (4, 16, 144), (2, 10, 1024), (3, 64, 576), (2, 576, 64), (1, 100, 4096),
           (1, 130, 131), (1, 131, 130), (2, 128, 128), (1, 129, 300), (2, 256, 256), (1, 257, 257), (1, 300, 1031),
           (1, 1031, 300), (1, 512, 700), (160, 20, 36), (1, 24, 9000), (2, 9000, 24), (1, 1, 5000), (1, 640, 640),
-          (2, 127, 127), (1, 255, 900), (1, 100, 5000), (1, 2049, 130), (21, 70, 2100), (17, 2300, 30), (40, 12, 4096), (3, 128, 20000)]
+          (2, 127, 127), (1, 255, 900), (1, 100, 5000), (1, 2049, 130), (21, 70, 2100), (17, 2300, 30), (40, 12, 4096), (3, 128, 20000), (2, 100, 700), (1, 24, 2100), (3, 5100, 90), (1, 300, 40), (20, 33, 900)]
 
 
 @pytest.fixture(scope="module")
