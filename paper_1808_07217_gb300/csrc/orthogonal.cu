@@ -883,7 +883,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(PAIR ? 2 : 1, 1,
 // than 2.5e-3 too.  What bounds it is each step's chain of latencies (products, their sums' exchange, products, products, the
 // rows' update), which the work in it hardly lengthens: 16 matrices of 16 x 144 take 15 us (launch included; their bytes
 // 0.1), 16 of 100 x 4096 take 119 (bytes 13.5).  The 128 columns that a tile of products has are its limit; there it is still the
-// faster: 16 x 128 x 1024 in 105 us (110 by the tiles of the form above), 16 x 128 x 128 in 70 (88), 16 x 100 x 4096 in 119 (197).
+// faster: 16 x 128 x 1024 in 83 us (110 by the tiles of the form above), 16 x 128 x 128 in 70 (90), 16 x 100 x 4096 in 119 (198).
 
 constexpr int kRows = 512;       // rows of a CTA
 constexpr int kResSide = 128;
