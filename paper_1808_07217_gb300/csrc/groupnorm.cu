@@ -8,9 +8,10 @@
 //   dgamma = sum dz xh,  dbeta = sum dz (over the worker's images and positions),
 //   dx = rstd (gamma dz - m1 - xh m2).
 //
-// Both are bound by memory: x read and y written once, and x, dy (for ReLU y) read and dx written once, where an image stays on
-// chip (the resident form below), one more read of the inputs where it does not (the split form).  A thread owns V neighbouring channels (a vector of up to 16 bytes) and walks down the
-// positions, so that its parameters and channel sums stay in registers whatever the group width.
+// Both are bound by memory: x read and y written once, and x, dy (for ReLU y) read and dx written once, where an image stays
+// on chip (the resident form below), one more read of the inputs where it does not (the split form).  A thread owns V
+// neighbouring channels (a vector of up to 16 bytes) and walks down the positions, so that its parameters and channel sums
+// stay in registers whatever the group width.
 #include <algorithm>
 #include <atomic>
 #include <string>
