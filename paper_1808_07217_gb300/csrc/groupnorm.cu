@@ -182,7 +182,7 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, int bytes,
 // ---- split form: any size, three launches ----
 //
 // The sums over ranges of an image's positions, their merge, and a second pass from the statistics.  Forward of 8 images of 127 x
-// 129 x 320 in bf16 with SiLU: 55 us (about 20, 6 and 29; 168 MB at least, 3.1 TB/s): the merge's latency, the second read of x,
+// 129 x 320 in bf16 with SiLU: 54 us (about 20, 5 and 28; 168 MB at least, 3.1 TB/s): the merge's latency, the second read of x,
 // most of which L2 no longer holds, and SiLU's two special functions a value.  One cooperative launch that keeps a third of x
 // in shared memory between the passes took 57.6: its two ends and the wait between them cost what the kept third saves.
 
@@ -494,63 +494,90 @@ __global__ void __launch_bounds__(512, 2) gn_ring_partial_kernel(const GnArgs a)
   }
 }
 
-// Forward: a block per (image, group) merges its ranges' channels into mean and rstd.
-__global__ void __launch_bounds__(128) gn_stats_merge_kernel(const GnArgs a) {
+// Forward: a block per (image, group) merges its ranges' channels into mean and rstd, about eight to a thread where 1024 threads
+// are enough, one after another.  A chain of latencies: 4.7 us for 256 blocks of 38 x 10 values, 20.5 for 4 of 152 x 512.
+__global__ void __launch_bounds__(1024) gn_stats_merge_kernel(const GnArgs a) {
   pdl_begin();
-  const int n = blockIdx.x / a.groups, q = blockIdx.x % a.groups;
+  const int n = blockIdx.x / a.groups, q = blockIdx.x % a.groups, threads = blockDim.x;
   const float2* part = reinterpret_cast<const float2*>(a.part) + (int64_t)n * a.S * a.C + q * a.D;
   float cn = 0.f, cm = 0.f, cq = 0.f;
-  // range by range where a group has many channels, else 128 / D ranges at a time
-  const int dw = min(a.D, 128), lanes = 128 / dw;
+  // range by range where a group has many channels, else threads / D ranges at a time
+  const int dw = min(a.D, threads), lanes = threads / dw;
   const int d0 = threadIdx.x % dw, s0 = threadIdx.x / dw;
   if (s0 < lanes) {
+    constexpr int U = 8;  // loads before the first merge
     for (int d = d0; d < a.D; d += dw)
-#pragma unroll 4
-      for (int s = s0; s < a.S; s += lanes) {
-        const float2 v = part[(int64_t)s * a.C + d];
-        chan(cn, cm, cq, (float)(min(a.P, (s + 1) * a.rows) - s * a.rows), v.x, v.y);
+      for (int s = s0; s < a.S; s += U * lanes) {
+        float2 v[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+          if (s + i * lanes < a.S) v[i] = part[(int64_t)(s + i * lanes) * a.C + d];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const int r = s + i * lanes;
+          if (r < a.S) chan(cn, cm, cq, (float)(min(a.P, (r + 1) * a.rows) - r * a.rows), v[i].x, v[i].y);
+        }
       }
   }
-  __shared__ float red[3][4];
+  auto warp_merge = [&]() {
 #pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    const float nb = __shfl_xor_sync(~0u, cn, o), mb = __shfl_xor_sync(~0u, cm, o),
-                qb = __shfl_xor_sync(~0u, cq, o);
-    chan(cn, cm, cq, nb, mb, qb);
-  }
-  if ((threadIdx.x & 31) == 0) {
-    const int w = threadIdx.x >> 5;
-    red[0][w] = cn, red[1][w] = cm, red[2][w] = cq;
-  }
+    for (int o = 16; o; o >>= 1) {
+      const float nb = __shfl_xor_sync(~0u, cn, o), mb = __shfl_xor_sync(~0u, cm, o), qb = __shfl_xor_sync(~0u, cq, o);
+      chan(cn, cm, cq, nb, mb, qb);
+    }
+  };
+  __shared__ float red[3][32];
+  warp_merge();
+  const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (lane == 0) red[0][w] = cn, red[1][w] = cm, red[2][w] = cq;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < 4; ++w) chan(cn, cm, cq, red[0][w], red[1][w], red[2][w]);
-    a.mean[blockIdx.x] = cm;
-    a.rstd[blockIdx.x] = __frsqrt_rn(cq / cn + a.eps);
+  if (w == 0) {
+    const bool have = lane < threads / 32;
+    cn = have ? red[0][lane] : 0.f, cm = have ? red[1][lane] : 0.f, cq = have ? red[2][lane] : 0.f;
+    warp_merge();
+    if (lane == 0) {
+      a.mean[blockIdx.x] = cm;
+      a.rstd[blockIdx.x] = __frsqrt_rn(cq / cn + a.eps);
+    }
   }
 }
 
-// Backward: per image and `per` groups of it, the ranges' channel sums added up, and the groups' m1 and m2.
-__global__ void __launch_bounds__(256) gn_sums_merge_kernel(const GnArgs a, int per) {
+// Backward: per image and `per` groups of it, the ranges' channel sums added up (several threads to a channel where the
+// channels are fewer than the threads), and the groups' m1 and m2.  4 blocks of 152 x 512 values: 13 us, 46 with 256 threads.
+__global__ void __launch_bounds__(1024) gn_sums_merge_kernel(const GnArgs a, int per) {
   pdl_begin();
-  const int n = blockIdx.x, q0 = blockIdx.y * per, q1 = min(a.groups, q0 + per);
+  __shared__ float2 red[1024];
+  const int n = blockIdx.x, q0 = blockIdx.y * per, q1 = min(a.groups, q0 + per), threads = blockDim.x;
   float2* sums = reinterpret_cast<float2*>(a.sums) + (int64_t)n * a.C;
-  const float2* part = reinterpret_cast<const float2*>(a.part) + (int64_t)n * a.S * a.C;
-  for (int c = q0 * a.D + threadIdx.x; c < q1 * a.D; c += 256) {
+  const float2* part = reinterpret_cast<const float2*>(a.part) + (int64_t)n * a.S * a.C + q0 * a.D;
+  const int width = (q1 - q0) * a.D, dw = min(width, threads), lanes = threads / dw;
+  const int d0 = threadIdx.x % dw, s0 = threadIdx.x / dw;
+  auto sum = [&](int d, int from, int step) {
     float2 t = make_float2(0.f, 0.f);
 #pragma unroll 8
-    for (int s = 0; s < a.S; ++s) {
-      const float2 v = part[(int64_t)s * a.C + c];
+    for (int s = from; s < a.S; s += step) {
+      const float2 v = part[(int64_t)s * a.C + d];
       t.x += v.x;
       t.y += v.y;
     }
-    sums[c] = t;
+    return t;
+  };
+  if (lanes == 1) {
+    for (int d = threadIdx.x; d < width; d += threads) sums[q0 * a.D + d] = sum(d, 0, 1);
+  } else {
+    if (s0 < lanes) red[threadIdx.x] = sum(d0, s0, lanes);
+    __syncthreads();
+    if (s0 == 0) {
+      float2 t = red[d0];
+      for (int k = 1; k < lanes; ++k) t.x += red[k * dw + d0].x, t.y += red[k * dw + d0].y;
+      sums[q0 * a.D + d0] = t;
+    }
   }
   __syncthreads();
   const int lane = threadIdx.x & 31;
   const float inv = 1.f / ((float)a.P * (float)a.D);
   const float* gamma = a.gamma + (int64_t)(n / a.B) * a.par_gs;
-  for (int q = q0 + (threadIdx.x >> 5); q < q1; q += 8) {
+  for (int q = q0 + (threadIdx.x >> 5); q < q1; q += threads / 32) {
     float2 t = make_float2(0.f, 0.f);
     for (int d = lane; d < a.D; d += 32) {
       const float ga = gamma[q * a.D + d];
@@ -750,9 +777,13 @@ cudaError_t gn_split(GnArgs a, cudaStream_t st) {
   if constexpr (BWD) {
     // about 256 channels to a block
     const int per = std::max(1, std::min(a.groups, 256 / a.D));
-    e = launch_pdl(gn_sums_merge_kernel, dim3((unsigned)a.N, (a.groups + per - 1) / per), dim3(256), 0, st, a, per);
+    int threads = 256;
+    while (threads < 1024 && (int64_t)per * a.D * a.S > 8 * threads) threads *= 2;
+    e = launch_pdl(gn_sums_merge_kernel, dim3((unsigned)a.N, (a.groups + per - 1) / per), dim3(threads), 0, st, a, per);
   } else {
-    e = launch_pdl(gn_stats_merge_kernel, dim3((unsigned)(a.N * a.groups)), dim3(128), 0, st, a);
+    int threads = 128;
+    while (threads < 1024 && (int64_t)a.D * a.S > 8 * threads) threads *= 2;
+    e = launch_pdl(gn_stats_merge_kernel, dim3((unsigned)(a.N * a.groups)), dim3(threads), 0, st, a);
   }
   if (e != cudaSuccess) return e;
   e = launch_pdl(gn_apply_kernel<XT, YT, V, BWD>, grid, dim3(kSplitThreads), 0, st, ranges, tx, ty);

@@ -281,7 +281,7 @@ def test_clusters_of_nine_and_ten(P, shape, x_type, y_type):
 # images that no cluster holds: ranges of a few positions and of many; one group, groups within and across vectors; one
 # position's channels wider than the threads; many images
 LARGE = [(1, 1, 60007, 24, 1), (1, 2, 13001, 168, 42), (2, 3, 20011, 104, 13), (1, 1, 701, 2048, 64), (1, 1, 301, 4096, 2),
-         (2, 88, 1101, 480, 4)]
+         (2, 88, 1101, 480, 4), (2, 4, 940, 484, 2), (1, 3, 2000, 500, 1)]
 
 
 @pytest.mark.gpu
