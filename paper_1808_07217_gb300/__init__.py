@@ -616,10 +616,22 @@ def _stream_of(dev):
     return raw(dev) if raw is not None else torch.cuda.current_stream(dev).cuda_stream
 
 
+def _workspace_on(dev, st, nbytes):
+    """nbytes of the current device `dev` for a call on stream `st`.  The allocator orders a block's uses by the stream that
+    it was allocated on: a block of the current stream may still be in use by work queued there, which a call on another
+    stream does not wait for.  So it is allocated with `st` current."""
+    import torch
+
+    if st == _stream_of(dev):
+        return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    # (1 is the runtime's other handle of the default stream)
+    with torch.cuda.stream(torch.cuda.ExternalStream(0 if st == 1 else st, device=dev)):
+        return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+
+
 def _launch(dev, stream, workspace, nbytes, fn, args):
     """fn(*args, workspace, its bytes, stream) with device `dev` current, on `stream` or that device's current
-    one.  Without a workspace one of nbytes comes from PyTorch's allocator for this call; on a stream other
-    than the current one its memory is kept until that stream has passed the call.  workspace False: fn
+    one.  Without a workspace one of nbytes comes from PyTorch's allocator for this call.  workspace False: fn
     takes none."""
     import torch
 
@@ -633,10 +645,8 @@ def _launch(dev, stream, workspace, nbytes, fn, args):
         ws, wp, wn = workspace, None, 0
         if ws is None:
             if nbytes:
-                ws = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+                ws = _workspace_on(dev, st, nbytes)
                 wp, wn = ws.data_ptr(), nbytes
-                if stream is not None and st != _stream_of(dev):
-                    ws.record_stream(torch.cuda.ExternalStream(st))
         elif ws.get_device() != dev or not ws.is_contiguous():
             raise LsgdError(EINVAL, f"workspace: a contiguous tensor on CUDA device {dev} is wanted")
         else:
