@@ -1,0 +1,68 @@
+"""Group norm's sums where they are long: equal values, whose roundings all go one way, added up in 64 bits beside the kernels'
+sums.  A tolerance counts the additions that a value passes through, of half a unit (2^-24) each."""
+import numpy as np
+import pytest
+
+from _gpu_common import built_package
+
+U32 = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def P():
+    import torch
+
+    assert torch.cuda.is_available()
+    return built_package()
+
+
+def _backward(P, shape, x_type, additions, seed=0):
+    """dy = 0.1 everywhere, no activation.  dx, dgamma and dbeta against 64 bits on the GPU, one worker at a time."""
+    import torch
+
+    G, B, Pn, C, groups = shape
+    D = C // groups
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(G, B, Pn, C, generator=gen, device="cuda").to(x_type)
+    gamma = 1 + 0.2 * torch.rand(G, C, generator=gen, device="cuda")
+    beta = torch.zeros(G, C, device="cuda")
+    dy = torch.full((G, B, Pn, C), 0.1, device="cuda")
+    v = x.view(G, B, Pn, groups, D)
+    mean = torch.stack([v[k].double().mean((1, 3)) for k in range(G)]).float()
+    rstd = torch.stack([(v[k].double().var((1, 3), correction=0) + 1e-5).rsqrt() for k in range(G)]).float()
+    dx, dgamma, dbeta = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(gamma)
+    P.lsgd_groupnorm_backward(x, None, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, G, B, Pn, C, groups)
+    torch.cuda.synchronize()
+    assert P.lsgd_device_status() == P.OK
+    k_sum = additions * U32
+    for k in range(G):
+        xd, m, r = v[k].double(), mean[k].double().view(B, 1, groups, 1), rstd[k].double().view(B, 1, groups, 1)
+        xh = (xd - m) * r
+        ga, dz = gamma[k].double().view(groups, D), float(np.float32(0.1))
+        # dbeta: the sum's roundings alone; dgamma: each xh is off by the rounding of x - mean and of the product
+        want = dz * B * Pn
+        assert (dbeta[k].double() - want).abs().max() <= k_sum * want, float((dbeta[k].double() / want - 1).abs().max()) / U32
+        size = dz * xh.abs().sum((0, 1)).reshape(C)
+        want = dz * xh.sum((0, 1)).reshape(C)
+        assert ((dgamma[k].double() - want).abs() <= (k_sum + 3 * U32) * size).all()
+        # dx = rstd (gamma dz - m1 - xh m2): m1 and m2 from the same sums, and a handful of roundings of each term
+        m1 = dz * ga.mean(1)
+        mean_abs = (dz * ga * xh.abs()).mean((1, 3), keepdim=True)
+        m2 = (dz * ga * xh).mean((1, 3), keepdim=True)
+        tol = r * ((k_sum + 8 * U32) * (m1.view(1, 1, groups, 1) + xh.abs() * mean_abs) + 8 * U32 * dz * ga)
+        want = r * (dz * ga - m1.view(1, 1, groups, 1) - xh * m2)
+        tol += (U32 if x_type == torch.float32 else 2.0 ** -8) * want.abs()
+        off = (dx[k].double().view(B, Pn, groups, D) - want).abs() / tol
+        assert off.max() <= 1, float(off.max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape,x_bf16", [((1, 608, 2048, 257, 1), True), ((4, 152, 1100, 1040, 8), True),
+                                          ((2, 304, 1500, 1028, 2), False)])
+def test_backward_of_many_positions_to_a_thread(P, shape, x_bf16):
+    """As many images as leave one range to each, and channels that leave all of its positions to one thread."""
+    import torch
+
+    # 64 positions of a segment, its segments, the images by rows of 64, and the ends' trees
+    additions = 64 + (shape[2] + 63) // 64 + (shape[1] + 63) // 64 + 16
+    _backward(P, shape, torch.bfloat16 if x_bf16 else torch.float32, additions)
