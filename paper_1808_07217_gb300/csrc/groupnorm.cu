@@ -601,11 +601,18 @@ __global__ void __launch_bounds__(1024) gn_sums_merge_kernel(const GnArgs a, int
   const float* gamma = a.gamma + (int64_t)(n / a.B) * a.par_gs;
   for (int q = q0 + (threadIdx.x >> 5); q < q1; q += threads / 32) {
     float2 t = make_float2(0.f, 0.f);
-    for (int d = lane; d < a.D; d += 32) {
-      const float ga = gamma[q * a.D + d];
-      const float2 v = sums[q * a.D + d];
-      t.x = fmaf(ga, v.x, t.x);
-      t.y = fmaf(ga, v.y, t.y);
+    for (int from = lane; from < a.D; from += 32 * 64) {  // 64 channels of a lane at a time
+      float2 some = make_float2(0.f, 0.f);
+      const int end = min(a.D, from + 32 * 64);
+#pragma unroll 4
+      for (int d = from; d < end; d += 32) {
+        const float ga = gamma[q * a.D + d];
+        const float2 v = sums[q * a.D + d];
+        some.x = fmaf(ga, v.x, some.x);
+        some.y = fmaf(ga, v.y, some.y);
+      }
+      t.x += some.x;
+      t.y += some.y;
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
@@ -712,7 +719,7 @@ __global__ void __launch_bounds__(kSplitThreads, BWD ? 2 : 4) gn_apply_kernel(co
 }
 
 // dgamma and dbeta of worker g: the sums of its `rows` rows of channel pairs (sum dz, sum dz xh), a fixed order.
-__global__ void __launch_bounds__(1024) gn_param_grad_kernel(const float2* sums, int64_t rows, int C, int64_t par_gs,
+__global__ void __launch_bounds__(1024, 2) gn_param_grad_kernel(const float2* sums, int64_t rows, int C, int64_t par_gs,
                                                              float* dgamma, float* dbeta) {
   pdl_begin();
   const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4;
@@ -720,11 +727,19 @@ __global__ void __launch_bounds__(1024) gn_param_grad_kernel(const float2* sums,
   const int64_t g = blockIdx.y;
   float2 t = make_float2(0.f, 0.f);
   if (c < C) {
+    const int span = 64 * segment((int)((rows + 63) / 64));  // the rows of a segment of this thread's additions
+    for (int64_t from = ry; from < rows; from += span) {
+      float2 some = make_float2(0.f, 0.f);
+      const int n = (int)min((int64_t)span, rows - from);
+      const float2* at = sums + (g * rows + from) * C + c;
 #pragma unroll 8
-    for (int64_t r = ry; r < rows; r += 64) {
-      const float2 v = sums[(g * rows + r) * C + c];
-      t.x += v.x;
-      t.y += v.y;
+      for (int r = 0; r < n; r += 64) {
+        const float2 v = at[(int64_t)r * C];
+        some.x += v.x;
+        some.y += v.y;
+      }
+      t.x += some.x;
+      t.y += some.y;
     }
   }
   // two rows of 16 channels to a warp

@@ -66,3 +66,20 @@ def test_backward_of_many_positions_to_a_thread(P, shape, x_bf16):
     # 64 positions of a segment, its segments, the images by rows of 64, and the ends' trees
     additions = 64 + (shape[2] + 63) // 64 + (shape[1] + 63) // 64 + 16
     _backward(P, shape, torch.bfloat16 if x_bf16 else torch.float32, additions)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(1, 1 << 20, 1, 8, 1), (3, 300007, 2, 12, 2), (1, 1, 301, 65536, 1), (2, 1, 40, 50000, 1)])
+def test_backward_of_many_images_and_of_many_channels_to_a_group(P, shape):
+    """The parameters' sums over a worker's images, and a group's means over its channels."""
+    import torch
+
+    G, B, Pn, C, groups = shape
+    # an image's positions (at most 64 to a thread, then the ranges and the rows of threads), then the longer of: the images by
+    # rows of 64, in segments of 64 or of the root of their number (a multiple of 8); the group's channels by lanes of 32, 64 at a
+    # time; and the ends' trees
+    rows, lanes = -(-B // 64), -(-C // groups // 32)
+    seg = max(64, -(-int(rows ** 0.5) // 8) * 8)
+    images = min(rows, seg) + -(-rows // seg)
+    channels = min(lanes, 64) + -(-lanes // 64)
+    _backward(P, shape, torch.float32, min(Pn, 64) + min(Pn, 256) + 8 + max(images, channels) + 16)
