@@ -221,14 +221,15 @@ __global__ void __launch_bounds__(kSplitThreads) gn_partial_kernel(const GnArgs 
     const XT* x = static_cast<const XT*>(a.x) + base;
     const int64_t step = (int64_t)ty_n * a.C;
     if constexpr (!BWD) {
-      // Segments of at most 64 positions: sums of the deviations from the first U values' mean, and of their squares,
-      // merged into the running moments by Chan et al.'s formula.  The pivot is far from the segment's mean only if
-      // one of its U values is, and then that value's square in the sums bounds what the difference loses.
+      // Segments: sums of the deviations from the first U values' mean, and of their squares, merged into the running
+      // moments by Chan et al.'s formula.  The pivot is far from the segment's mean only if one of its U values
+      // is, and then that value's square in the sums bounds what the difference loses.
       constexpr int U = 8;
       int p = p0 + ty;
+      const int most = segment((p1 - p + ty_n - 1) / ty_n);
       const XT* at = x + (int64_t)p * a.C;
       while (p < p1) {
-        const int k = min(64, (p1 - p + ty_n - 1) / ty_n);  // positions of the segment
+        const int k = min(most, (p1 - p + ty_n - 1) / ty_n);  // positions of the segment
         float pivot[V], d0[V], d1[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) d0[j] = d1[j] = 0.f;
@@ -427,7 +428,8 @@ __global__ void __launch_bounds__(512, 2) gn_ring_partial_kernel(const GnArgs a)
 #pragma unroll
   for (int j = 0; j < 2 * V; ++j) run[j * threads] = 0.f;
   float total = 0.f, pivot[V], d0[V], d1[V];
-  // a segment of 16 chunks ends: its sums, of deviations from the pivot, into the running moments
+  const int most = segment(chunks * U) / U;  // the chunks of a segment
+  // a segment ends: its sums, of deviations from the pivot, into the running moments
   auto merge = [&](int k) {
     if (k == 0) return;
     const float kf = (float)k, inv = 1.f / kf, w = kf / (total + kf), cw = total * w;
@@ -440,7 +442,7 @@ __global__ void __launch_bounds__(512, 2) gn_ring_partial_kernel(const GnArgs a)
     }
     total += kf;
   };
-  int b = 0, k_seg = 0;
+  int b = 0, k_seg = 0, next = 0;
   uint32_t ph = 0;
   for (int k = 0; k < chunks; ++k) {
     const bool ok = wait_full(&full[b], ph);
@@ -457,9 +459,10 @@ __global__ void __launch_bounds__(512, 2) gn_ring_partial_kernel(const GnArgs a)
     }
     if (tid == 0 && k + a.stages < chunks) fetch(k + a.stages, b);
     if (++b == a.stages) b = 0, ph ^= 1;
-    if (k % 16 == 0) {
+    if (k == next) {
       merge(k_seg);
       k_seg = 0;
+      next += most;
       const float first = 1.f / max(have, 1);
 #pragma unroll
       for (int j = 0; j < V; ++j) pivot[j] = d0[j] = d1[j] = 0.f;
@@ -517,7 +520,8 @@ __global__ void __launch_bounds__(512, 2) gn_ring_partial_kernel(const GnArgs a)
 }
 
 // Forward: a block per (image, group) merges its ranges' channels into mean and rstd, about eight to a thread where 1024 threads
-// are enough, one after another.  A chain of latencies: 4.7 us for 256 blocks of 38 x 10 values, 20.5 for 4 of 152 x 512.
+// are enough, one after another, 64 of them at a time.  A chain of latencies: 4.7 us for 256 blocks of 38 x 10 values, 20.5 for 4
+// of 152 x 512.
 __global__ void __launch_bounds__(1024) gn_stats_merge_kernel(const GnArgs a) {
   pdl_begin();
   const int n = blockIdx.x / a.groups, q = blockIdx.x % a.groups, threads = blockDim.x;
@@ -528,18 +532,27 @@ __global__ void __launch_bounds__(1024) gn_stats_merge_kernel(const GnArgs a) {
   const int d0 = threadIdx.x % dw, s0 = threadIdx.x / dw;
   if (s0 < lanes) {
     constexpr int U = 8;  // loads before the first merge
+    float sn = 0.f, sm = 0.f, sq = 0.f;  // earlier segments' moments
+    const int batches = 64 / min(U, (a.S + lanes - 1) / lanes);  // of a segment
+    int left = batches;
     for (int d = d0; d < a.D; d += dw)
       for (int s = s0; s < a.S; s += U * lanes) {
         float2 v[U];
 #pragma unroll
         for (int i = 0; i < U; ++i)
           if (s + i * lanes < a.S) v[i] = part[(int64_t)(s + i * lanes) * a.C + d];
+        if (--left < 0) {
+          chan(sn, sm, sq, cn, cm, cq);
+          cn = cm = cq = 0.f;
+          left = batches - 1;
+        }
 #pragma unroll
         for (int i = 0; i < U; ++i) {
           const int r = s + i * lanes;
           if (r < a.S) chan(cn, cm, cq, (float)(min(a.P, (r + 1) * a.rows) - r * a.rows), v[i].x, v[i].y);
         }
       }
+    if (sn > 0.f) chan(cn, cm, cq, sn, sm, sq);
   }
   auto warp_merge = [&]() {
 #pragma unroll

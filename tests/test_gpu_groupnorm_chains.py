@@ -83,3 +83,43 @@ def test_backward_of_many_images_and_of_many_channels_to_a_group(P, shape):
     images = min(rows, seg) + -(-rows // seg)
     channels = min(lanes, 64) + -(-lanes // 64)
     _backward(P, shape, torch.float32, min(Pn, 64) + min(Pn, 256) + 8 + max(images, channels) + 16)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape,values", [((1, 1, 512, 65536, 1), "two"), ((1, 2, 600, 50001, 1), "two"), ((1, 1, 1200000, 257, 1), "two"),
+                                          ((1, 1, 1100000, 1028, 2), "random")])
+def test_forward_of_long_merges(P, shape, values):
+    """Two alternating values, so that every range and channel has the same moments: their merge over many channels of a
+    group, and many segments of positions."""
+    import torch
+
+    G, B, Pn, C, groups = shape
+    D = C // groups
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(G, B, Pn, C, generator=gen, device="cuda")
+    if values == "two":
+        x[:, :, 0::2], x[:, :, 1::2] = 0.7, 0.1
+    gamma, beta = torch.ones(G, C, device="cuda"), torch.zeros(G, C, device="cuda")
+    y = torch.empty_like(x)
+    mean, rstd = torch.empty(G * B, groups, device="cuda"), torch.empty(G * B, groups, device="cuda")
+    P.lsgd_groupnorm_forward(x, gamma, beta, y, mean, rstd, G, B, Pn, C, groups)
+    torch.cuda.synchronize()
+    assert P.lsgd_device_status() == P.OK
+    # a segment of a thread's positions and its segments (at most 256 ranges or 4096 positions of one), the ranges and channels
+    # 64 at a time and the segments of those, and the ends' trees; the variance's relative error is halved by the root
+    merges = -(-256 // max(1, 1024 // D)) * -(-D // 1024)
+    additions = 2 * max(64, int((Pn / 256) ** 0.5) + 8) + min(merges, 64) + -(-merges // 64) + 24
+    for k in range(G):
+        xd = x[k].view(B, Pn, groups, D).double()
+        m = xd.mean((1, 3))
+        r = (xd.var((1, 3), correction=0) + 1e-5).rsqrt()
+        big = x[k].abs().max().double()
+        dm = additions * U32 * big
+        assert ((mean.view(G, B, groups)[k] - m).abs() <= dm).all()
+        dr = r * (additions / 2 * U32 + (dm * r) ** 2 + 2 * U32)
+        off = ((rstd.view(G, B, groups)[k] - r).abs() / r).max() / U32
+        assert ((rstd.view(G, B, groups)[k] - r).abs() <= dr).all(), float(off)
+        s = (B, 1, groups, 1)
+        z = (xd - m.view(s)) * r.view(s)
+        tol = dm * r.view(s) + z.abs() * (dr / r).view(s) + 8 * U32 * (z.abs() + (xd.abs() + m.abs().view(s)) * r.view(s))
+        assert ((y[k].view(B, Pn, groups, D) - z).abs() <= tol).all()
