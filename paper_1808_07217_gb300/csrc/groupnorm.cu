@@ -1510,9 +1510,41 @@ const char* gn_shape_error(int G, int B, int64_t P, int C, int groups) {
   return nullptr;
 }
 
-bool gn_overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return a && b && x < y + nb && y < x + na;
+// `count` blocks of `bytes` from p, `stride` floats from one to the next; at NULL: nothing.  (A workspace that is not used, of no
+// bytes, counts by its address.)
+struct GnBlocks {
+  uintptr_t first, end;  // of all of them
+  size_t bytes;
+  int64_t stride;
+  int count;
+  GnBlocks(const void* p, size_t n, int64_t gs = 0, int blocks = 1)
+      : first(reinterpret_cast<uintptr_t>(p)), bytes(n), stride(gs), count(blocks) {
+    uint64_t span;  // (a stride may be any number: up to the last address then)
+    if (__builtin_mul_overflow((uint64_t)(blocks - 1), (uint64_t)gs, &span) || span > UINTPTR_MAX / 8) end = UINTPTR_MAX;
+    else end = first + 4 * span + n;
+    if (!p) end = 0;
+  }
+};
+// Whether any two blocks of a and b share a byte.  Where both are several, their strides are the same.
+bool gn_meet(const GnBlocks& a, const GnBlocks& b) {
+  if (a.first >= b.end || b.first >= a.end) return false;
+  if (a.count == 1 && b.count == 1) return true;
+  // block j of b lies d + t stride behind block i of a, t = j - i
+  using wide = __int128;
+  const wide d = (wide)b.first - (wide)a.first, stride = 4 * (wide)(a.count > 1 ? a.stride : b.stride), na = a.bytes, nb = b.bytes;
+  const wide t = std::max<wide>(1 - a.count, (-nb - d >= 0 ? (-nb - d) / stride : -((nb + d + stride - 1) / stride)) + 1);
+  return t <= b.count - 1 && d + t * stride < na;  // (t: the first that does not end before a's block)
+}
+// Whether anything written meets anything else of the call.
+template <int W, int R>
+bool gn_overlap(const GnBlocks (&written)[W], const GnBlocks (&read)[R]) {
+  for (int i = 0; i < W; ++i) {
+    for (int j = i + 1; j < W; ++j)
+      if (gn_meet(written[i], written[j])) return true;
+    for (int j = 0; j < R; ++j)
+      if (gn_meet(written[i], read[j])) return true;
+  }
+  return false;
 }
 
 bool gn_bad_align(const void* p, int z) { return reinterpret_cast<uintptr_t>(p) % z != 0; }
@@ -1557,6 +1589,7 @@ lsgd_status lsgd_groupnorm_forward(const void* x, int x_type, const float* gamma
   if (bad) return gn_error(LSGD_EINVAL, fn, bad);
   const int64_t N = (int64_t)G * B;
   const size_t n = (size_t)N * P * C, ns = (size_t)N * groups * 4, need = gn_workspace(N, (int)P, C, groups, false);
+  const auto params = [&](const float* p) { return GnBlocks(p, 4 * (size_t)C, par_gs, G); };
   if (!x || !gamma || !beta || !y || !mean || !rstd) bad = "a pointer is NULL";
   else if ((!xb && x_type != LSGD_FP32) || (!yb && y_type != LSGD_FP32)) bad = "types are LSGD_FP32 or LSGD_BF16";
   else if (act != LSGD_ACT_NONE && act != LSGD_ACT_RELU && act != LSGD_ACT_SILU) bad = "unknown activation";
@@ -1567,8 +1600,8 @@ lsgd_status lsgd_groupnorm_forward(const void* x, int x_type, const float* gamma
     bad = "a pointer is not aligned to its element";
   else if (need && (!workspace || workspace_bytes < need || gn_bad_align(workspace, 16)))
     bad = "workspace NULL, not 16-byte aligned or smaller than lsgd_groupnorm_workspace says";
-  else if (gn_overlap(x, n * xz, y, n * yz) || gn_overlap(mean, ns, rstd, ns) || gn_overlap(x, n * xz, workspace, need) ||
-           gn_overlap(y, n * yz, workspace, need) || gn_overlap(y, n * yz, mean, ns) || gn_overlap(y, n * yz, rstd, ns))
+  else if (gn_overlap({GnBlocks(y, n * yz), GnBlocks(mean, ns), GnBlocks(rstd, ns), GnBlocks(workspace, need)},
+                      {GnBlocks(x, n * xz), params(gamma), params(beta)}))
     bad = "tensors overlap";
   if (bad) return gn_error(LSGD_EINVAL, fn, bad);
   GnArgs a{};
@@ -1593,7 +1626,8 @@ lsgd_status lsgd_groupnorm_backward(const void* x, int x_type, const void* y, co
   const int xz = xb ? 2 : 4, yz = yb ? 2 : 4;
   if (bad) return gn_error(LSGD_EINVAL, fn, bad);
   const int64_t N = (int64_t)G * B;
-  const size_t n = (size_t)N * P * C, need = gn_workspace(N, (int)P, C, groups, true);
+  const size_t n = (size_t)N * P * C, ns = (size_t)N * groups * 4, need = gn_workspace(N, (int)P, C, groups, true);
+  const auto params = [&](const float* p) { return GnBlocks(p, 4 * (size_t)C, par_gs, G); };
   const bool relu = act == LSGD_ACT_RELU;
   if (!x || !dy || !gamma || !beta || !mean || !rstd || !dx || !dgamma || !dbeta || (relu && !y))
     bad = "a pointer is NULL (y may be only where the activation is not ReLU)";
@@ -1606,10 +1640,9 @@ lsgd_status lsgd_groupnorm_backward(const void* x, int x_type, const void* y, co
     bad = "a pointer is not aligned to its element";
   else if (!workspace || workspace_bytes < need || gn_bad_align(workspace, 16))
     bad = "workspace NULL, not 16-byte aligned or smaller than lsgd_groupnorm_workspace says";
-  else if (gn_overlap(x, n * xz, dx, n * xz) || gn_overlap(dy, n * yz, dx, n * xz) ||
-           (relu && gn_overlap(y, n * yz, dx, n * xz)) || gn_overlap(dgamma, 4 * (size_t)C, dbeta, 4 * (size_t)C) ||
-           gn_overlap(dx, n * xz, workspace, need) || gn_overlap(x, n * xz, workspace, need) ||
-           gn_overlap(dy, n * yz, workspace, need))
+  else if (gn_overlap({GnBlocks(dx, n * xz), params(dgamma), params(dbeta), GnBlocks(workspace, need)},
+                      {GnBlocks(x, n * xz), GnBlocks(dy, n * yz), GnBlocks(relu ? y : nullptr, n * yz), params(gamma),
+                       params(beta), GnBlocks(mean, ns), GnBlocks(rstd, ns)}))
     bad = "tensors overlap";
   if (bad) return gn_error(LSGD_EINVAL, fn, bad);
   GnArgs a{};
