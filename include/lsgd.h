@@ -475,7 +475,8 @@ lsgd_status lsgd_direction_update(float* w, int64_t w_gs, const uint16_t* o, int
  * par_gs and beta + g par_gs (par_gs >= C: they may stand in a replica-major parameter buffer).
  * x and y are each LSGD_FP32 or LSGD_BF16 (lsgd_precision); mean and rstd [G][B][groups] fp32 are
  * written too.  Statistics and arithmetic are fp32 (the deviations are taken from the mean, so a
- * mean far above the deviation loses nothing more than x itself has); a bf16 y is rounded once.
+ * mean far above the deviation loses nothing more than x itself has); a bf16 y is rounded once (SiLU's exponential is
+ * then a fast one, off by a hundredth of that rounding at most, and y is 0 where it is within 1e-36 of 0).
  * Deterministic.  Non-finite values of x make their own image's group NaN and no other.
  *
  * `workspace` is device memory of at least the bytes that lsgd_groupnorm_workspace reports (0: it is

@@ -130,27 +130,31 @@ struct GnArgs {
   int stages, slab, slab_y;  // its pipeline: images ahead; bytes of an image of x and of dy (or y)
 };
 
-// 1 / (1 + exp(-z)): the exponential's overflow gives 0.
-template <bool EXACT>
+// 1 / (1 + exp(-z)): the exponential's overflow gives 0.  kExact (fp32 tensors): the accurate exponential and division.  kSums
+// (the sums over bf16 tensors, dgamma and dbeta among them, which are fp32 results): the accurate exponential and the fast
+// reciprocal, 2^-23 off.  kFast: the fast exponential too, 2^-21 and |z| 2^-23 off, which a bf16 result's rounding of 2^-8 hides: y
+// (54.9 against 56.9 us for 8 images of 127 x 129 x 320, whose second pass the special function unit bounds) and the split form's
+// dx.  The fast reciprocal flushes what is below 2^-126: y is 0 from z = -87.3 on, where it is 1e-36 at most.
+enum { kFast, kSums, kExact };
+template <int KIND>
 __device__ __forceinline__ float sigmoid(float z) {
-  if constexpr (EXACT) return 1.f / (1.f + expf(-z));
+  if constexpr (KIND == kExact) return 1.f / (1.f + expf(-z));
   float e, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.44269504f));
+  if constexpr (KIND == kSums) e = expf(-z);
+  else asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.44269504f));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
   return r;
 }
 
-// act(z).  EXACT (fp32 results): the accurate exponential and division; a bf16 result's rounding of 2^-8 hides the fast ones',
-// 2^-21 and |z| 2^-23 of the value (54.9 against 56.9 us for 8 images of 127 x 129 x 320 with SiLU, whose second pass the
-// special function unit bounds).  Values below 2^-126 in magnitude become 0.
-template <bool EXACT, int ACT>
+// act(z).
+template <int KIND, int ACT>
 __device__ __forceinline__ float activate(float z) {
   if constexpr (ACT == LSGD_ACT_RELU) {
     float r;
     asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(z));
     return r;
   }
-  if constexpr (ACT == LSGD_ACT_SILU) return z * sigmoid<EXACT>(z);
+  if constexpr (ACT == LSGD_ACT_SILU) return z * sigmoid<KIND>(z);
   return z;
 }
 // f with the activation as a constant.
@@ -325,7 +329,7 @@ __global__ void __launch_bounds__(kSplitThreads) gn_partial_kernel(const GnArgs 
                 float dz = dv[j];
                 if (relu) dz = yv[j] > 0.f ? dz : 0.f;
                 if (silu) {
-                  const float z = fmaf(xh, ga[j], be[j]), sg = sigmoid<sizeof(XT) == 4>(z);
+                  const float z = fmaf(xh, ga[j], be[j]), sg = sigmoid<sizeof(XT) == 4 ? kExact : kSums>(z);
                   dz *= sg * fmaf(z, 1.f - sg, 1.f);
                 }
                 s0[j] += dz;
@@ -661,7 +665,7 @@ __global__ void __launch_bounds__(kSplitThreads, BWD ? 2 : 4) gn_apply_kernel(co
     YT* out = static_cast<YT*>(a.out) + base;
 #pragma unroll
     for (int j = 0; j < V; ++j) ga[j] *= a.rstd[(int64_t)n * a.groups + (c0 + j) / a.D];
-    constexpr int U = 4;
+    constexpr int U = 4, kKind = sizeof(YT) == 4 ? kExact : kFast;
     with_act(a.act, [&](auto act) {
       for (int p = p0 + ty; p < p1; p += U * ty_n) {
         Vec<XT, V> r[U];
@@ -674,7 +678,7 @@ __global__ void __launch_bounds__(kSplitThreads, BWD ? 2 : 4) gn_apply_kernel(co
             float v[V];
             r[i].floats(v);
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = activate<sizeof(YT) == 4, decltype(act)::value>(fmaf(v[j] - mu[j], ga[j], be[j]));
+            for (int j = 0; j < V; ++j) v[j] = activate<kKind, decltype(act)::value>(fmaf(v[j] - mu[j], ga[j], be[j]));
             Vec<YT, V> o;
             o.set(v);
             o.stream(out + (int64_t)(p + i * ty_n) * a.C);
@@ -718,7 +722,7 @@ __global__ void __launch_bounds__(kSplitThreads, BWD ? 2 : 4) gn_apply_kernel(co
             float dz = dv[j];
             if (relu) dz = yv[j] > 0.f ? dz : 0.f;
             if (silu) {
-              const float z = fmaf(xh, ga[j], be[j]), sg = sigmoid<sizeof(XT) == 4>(z);
+              const float z = fmaf(xh, ga[j], be[j]), sg = sigmoid<sizeof(XT) == 4 ? kExact : kFast>(z);
               dz *= sg * fmaf(z, 1.f - sg, 1.f);
             }
             xv[j] = fmaf(ga[j] * rs[j], dz, -m1[j]) - xh * m2[j];
@@ -1091,6 +1095,7 @@ __global__ void __launch_bounds__(1024, 1) gn_fwd_resident_kernel(const GnArgs a
         mu[j] = gmean[q], ga[j] = par[c0 + j] * gsq[q], be[j] = par[a.C + c0 + j];
       });
       YT* out = static_cast<YT*>(a.out) + base;
+      constexpr int kKind = sizeof(YT) == 4 ? kExact : kFast;
       with_act(a.act, [&](auto act) {
 #pragma unroll
         for (int i = 0; i < R; ++i)
@@ -1098,7 +1103,7 @@ __global__ void __launch_bounds__(1024, 1) gn_fwd_resident_kernel(const GnArgs a
             float v[V];
             r[i].floats(v);
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = activate<sizeof(YT) == 4, decltype(act)::value>(fmaf(v[j] - mu[j], ga[j], be[j]));
+            for (int j = 0; j < V; ++j) v[j] = activate<kKind, decltype(act)::value>(fmaf(v[j] - mu[j], ga[j], be[j]));
             Vec<YT, V> o;
             o.set(v);
             o.store(out + i * step);
@@ -1232,7 +1237,7 @@ __global__ void __launch_bounds__(1024, 1) gn_bwd_resident_kernel(const GnArgs a
 #pragma unroll
         for (int i = 0; i < R; ++i)
           if (first + i * ty_n < last) {
-            const float z = fmaf((r[i].at(j) - mu) * rs, ga, be), sg = sigmoid<sizeof(XT) == 4>(z);
+            const float z = fmaf((r[i].at(j) - mu) * rs, ga, be), sg = sigmoid<sizeof(XT) == 4 ? kExact : kSums>(z);
             dz[i][j] *= sg * fmaf(z, 1.f - sg, 1.f);
           }
       }
