@@ -25,6 +25,7 @@
 namespace lsgd {
 
 __device__ int g_norm_timeout = 0;
+static std::atomic<bool> g_norm_used{false};  // the flag is read only once a call has been made
 
 namespace {
 
@@ -1558,6 +1559,7 @@ bool gn_bad_align(const void* p, int z) { return reinterpret_cast<uintptr_t>(p) 
 
 int norm_take_timeout_flag() {
   int h = 0;
+  if (!g_norm_used) return 0;
   if (cudaMemcpyFromSymbol(&h, g_norm_timeout, sizeof(int)) != cudaSuccess) {
     cudaGetLastError();
     return 0;
@@ -1609,6 +1611,7 @@ lsgd_status lsgd_groupnorm_forward(const void* x, int x_type, const float* gamma
                       {GnBlocks(x, n * xz), params(gamma), params(beta)}))
     bad = "tensors overlap";
   if (bad) return gn_error(LSGD_EINVAL, fn, bad);
+  if (!g_norm_used) g_norm_used = true;
   GnArgs a{};
   a.x = x, a.out = y, a.gamma = gamma, a.beta = beta, a.par_gs = par_gs, a.mean = mean, a.rstd = rstd;
   a.part = static_cast<float*>(workspace);
@@ -1650,6 +1653,7 @@ lsgd_status lsgd_groupnorm_backward(const void* x, int x_type, const void* y, co
                        params(beta), GnBlocks(mean, ns), GnBlocks(rstd, ns)}))
     bad = "tensors overlap";
   if (bad) return gn_error(LSGD_EINVAL, fn, bad);
+  if (!g_norm_used) g_norm_used = true;
   GnArgs a{};
   a.x = x, a.y = y, a.dy = dy, a.out = dx, a.gamma = gamma, a.beta = beta, a.par_gs = par_gs;
   a.mean = const_cast<float*>(mean), a.rstd = const_cast<float*>(rstd), a.dgamma = dgamma, a.dbeta = dbeta;

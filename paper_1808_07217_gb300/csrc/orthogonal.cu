@@ -38,6 +38,7 @@
 namespace lsgd {
 
 __device__ int g_direction_timeout = 0;
+static std::atomic<bool> g_direction_used{false};  // the flag is read only once a call has been made
 
 namespace {
 
@@ -1815,6 +1816,7 @@ cudaError_t run_direction(DirArgs d, const DirLayout& ly, uint8_t* ws, int steps
 
 int direction_take_timeout_flag() {
   int h = 0;
+  if (!g_direction_used) return 0;
   if (cudaMemcpyFromSymbol(&h, g_direction_timeout, sizeof(int)) != cudaSuccess) {
     cudaGetLastError();
     return 0;
@@ -1868,6 +1870,7 @@ lsgd_status lsgd_orthogonal_direction(float* u, int64_t u_gs, const void* g, int
   const int64_t ts = (ly.n + 127) / 128, tx = ((rows + 127) / 128) * ((cols + 127) / 128);
   if (!bad && ly.n && G * (ts * (ts + 1) + tx) * steps > 0x3fffffff) bad = "too many matrices of this size in one call";
   if (bad) return dir_error(LSGD_EINVAL, fn, bad);
+  if (!g_direction_used) g_direction_used = true;
   DirArgs d{};
   d.u = u, d.g = g, d.o = o, d.u_gs = u_gs, d.g_gs = g_gs, d.o_gs = o_gs;
   d.g_bf16 = gb, d.nesterov = nesterov != 0, d.mom = momentum;
