@@ -474,9 +474,9 @@ lsgd_status lsgd_direction_update(float* w, int64_t w_gs, const uint16_t* o, int
  * act(z) = z, max(z, 0) or z / (1 + exp(-z)).  gamma and beta are worker g's C values at gamma + g
  * par_gs and beta + g par_gs (par_gs >= C: they may stand in a replica-major parameter buffer).
  * x and y are each LSGD_FP32 or LSGD_BF16 (lsgd_precision); mean and rstd [G][B][groups] fp32 are
- * written too.  Statistics and arithmetic are fp32 (the deviations are taken from the mean, so a
- * mean far above the deviation loses nothing more than x itself has); a bf16 y is rounded once (SiLU's exponential is
- * then a fast one, off by a hundredth of that rounding at most, and y is 0 where it is within 1e-36 of 0).
+ * written too.  Statistics and arithmetic are fp32; the deviations are taken from the mean, so that a mean of r
+ * deviations puts y off by about r 2^-22 of a deviation, a few times x's own rounding.  A bf16 y is rounded once (SiLU's
+ * exponential is then a fast one, off by a hundredth of that rounding at most, and y is 0 where it is within 1e-36 of 0).
  * Deterministic.  Non-finite values of x make their own image's group NaN and no other.
  *
  * `workspace` is device memory of at least the bytes that lsgd_groupnorm_workspace reports (0: it is
@@ -501,7 +501,7 @@ lsgd_status lsgd_groupnorm_forward(const void* x, int x_type, const float* gamma
  * the sums over worker g's images and positions, written (not added) at dgamma + g par_gs and dbeta
  * + g par_gs.  x, gamma, beta, mean and rstd as in the forward; dx has x's type, y and dy y's.
  * ReLU's derivative is taken from the stored output (y > 0), as in the training step; the other
- * activations do not read y (NULL is fine).  Sums are fp32 in a fixed order: deterministic.
+ * activations do not read y (NULL is fine).  Sums are fp32, in segments and in a fixed order: deterministic.
  * Workspace, limits and errors as for the forward (backward = 1). */
 lsgd_status lsgd_groupnorm_backward(const void* x, int x_type, const void* y, const void* dy,
                                     int y_type, const float* gamma, const float* beta,

@@ -187,7 +187,7 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, int bytes,
 // ---- split form: any size, three launches ----
 //
 // The sums over ranges of an image's positions, their merge, and a second pass from the statistics.  Forward of 8 images of 127 x
-// 129 x 320 in bf16 with SiLU: 54 us (about 20, 5 and 28; 168 MB at least, 3.1 TB/s): the merge's latency, the second read of x,
+// 129 x 320 in bf16 with SiLU: 55 us (about 20, 5 and 28; 168 MB at least, 3.1 TB/s): the merge's latency, the second read of x,
 // most of which L2 no longer holds, and SiLU's two special functions a value.  One cooperative launch that keeps a third of x
 // in shared memory between the passes took 57.6: its two ends and the wait between them cost what the kept third saves.
 
@@ -1363,8 +1363,8 @@ int gn_cluster(int64_t N, int P, int C, int hold) {
 // CTAs load, wait for one another and store in turn.  A model in us, fitted to 120 pairs of measurements (4 to 512 images of
 // 32,000 to 400,000 values): a round costs 6 us of bf16 images, 9 of fp32 ones, more in clusters of 16 and with one CTA to
 // an SM; the split form its launches and 6 TB/s.  (Of another 100 pairs it takes the slower form, by 3 us or more, in 17.)
-// Forward of 128 images of 3100 x 64 in bf16: 74 us in clusters, 47 split, of 32 images: 25 and 26; backward of 128 images of
-// 1550 x 64: 69 and 59, of 32: 25 and 30.
+// Forward of 128 images of 3100 x 64 in bf16: 66 us in clusters, 35 split, of 32 images: 18.4 and 17.7; backward of 128 images of
+// 1550 x 64: 66 and 43, of 32: 18.4 and 21.1.
 bool gn_split_faster(int cl, int64_t N, int P, int C, bool bwd, int xz, int yz, bool relu) {
   if (cl < 4) return false;  // such images mostly fit one CTA, whose pipelined form overlaps its rounds
   const int per_sm = (int64_t)((P + cl - 1) / cl) * C / (bwd ? kBwdHold : kFwdHold) + C / 8 <= 512 ? 2 : 1;

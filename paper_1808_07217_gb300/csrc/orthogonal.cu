@@ -264,9 +264,10 @@ __global__ void __launch_bounds__(kMomThreads) direction_normalise_kernel(const 
 // resident) and every tile's predecessors stand before it in the list, so that every wait ends; matrices fill each
 // other's phase ends, and nothing is launched between phases.
 //
-// Measured, five steps: 16 x 1024 x 1024 in 329 us (1.04 PFLOP/s of the products that symmetry leaves; bound by the phases'
-// ends, where tiles wait for their matrix, and by operands from L2), 4 x 4096 x 4096 in 4.1 ms (1.34 PFLOP/s; the SM clock falls
-// to 1.4 GHz under the power limit, where a library product runs at 1.70).
+// Measured, five steps: 16 x 1024 x 1024 in 329 us (1.04 PFLOP/s of the products that symmetry leaves; the tensor pipe is active
+// 50 % of the time and L2 at 46 % of its peak: neither is the bound.  Tiles wait for their matrix at the phases' ends; the rest is
+// latency that has not been told apart), 4 x 4096 x 4096 in 4.1 ms (1.34 PFLOP/s; the SM clock falls to 1.4 GHz under the power
+// limit, where a library product runs at 1.70).
 
 constexpr int kHalf = 128, kBK = 64, kStages = 4, kEpi = 3, kEpiWarps = 16, kThreads = 128 + 32 * kEpiWarps, kChunk = 64;
 constexpr uint32_t kOpBytes = kHalf * kBK * 2;  // one operand's share of a stage in a CTA; half an epilogue buffer
@@ -1546,8 +1547,6 @@ struct DirLayout {
   int chunks, per;
   size_t h[2], l[2], A, P, diag_a, diag, part, done, bytes;
 };
-struct ResPlan;
-ResPlan resident_plan(int G, int64_t rows, int64_t cols);
 size_t resident_bytes(int G, int64_t rows, int64_t cols);
 DirLayout direction_layout(int G, int64_t rows, int64_t cols) {
   DirLayout d{};
