@@ -510,6 +510,97 @@ lsgd_status lsgd_groupnorm_backward(const void* x, int x_type, const void* y, co
                                     int groups, int act, void* workspace, size_t workspace_bytes,
                                     void* stream);
 
+/* Layer normalisation of rows with an activation and, optionally, a residual that is added before it: the normalisation for
+ * the dense layers' activations (rows at a stride, as the products read and write them), which like group norm keeps no
+ * statistics for the model average to miss.  Stand-alone; no counterpart in the paper.
+ * Row i of worker g (G workers, R rows each) is C values at x + (g R + i) x_ld; r, s and dx, ds below have x's type and stride.
+ * y (and dy) have y's type and the stride y_ld.  With s = x + r, rounded to x's type and stored (r and s NULL: s = x),
+ *   mean = sum s / C,  rstd = 1 / sqrt(sum (s - mean)^2 / C + eps),  y = act(gamma (s - mean) rstd + beta),
+ * gamma and beta worker g's C values at gamma + g par_gs and beta + g par_gs (par_gs >= C).  mean and rstd [G][R] fp32 are
+ * written too.  What lies between the rows (columns C to the stride) is neither read nor written.
+ * Types, activations and their accuracy are group norm's (lsgd_groupnorm_forward).  Statistics are fp32, the deviations taken from
+ * the mean; a row whose squared deviations pass fp32's range (values of 1e19 and more) gets rstd = 0.  Deterministic.  A NaN or
+ * infinite value makes its own row NaN and no other.
+ *
+ * No workspace, no allocation: the call may be captured into a CUDA graph.  G <= 65535, 1 <= C <= 65536, R >= 0 (0: nothing is
+ * done), G R <= 2^40; any C, strides >= C and any alignment of at least the element's (vectors of up to 16 bytes are used where
+ * strides and pointers allow).  LSGD_EINVAL on anything else and where what is written overlaps any other tensor (rows
+ * count from the first row's first to the last row's last value).  Device pointers, asynchronous on `stream`, which belongs
+ * to the current device. */
+lsgd_status lsgd_layernorm_forward(const void* x, const void* r, int x_type, int64_t x_ld,
+                                   const float* gamma, const float* beta, int64_t par_gs, void* s,
+                                   void* y, int y_type, int64_t y_ld, float* mean, float* rstd, int G,
+                                   int64_t R, int64_t C, float eps, int act, void* stream);
+
+/* The gradients of lsgd_layernorm_forward from that of y: with x the rows that were normalised (s, where there was a residual),
+ * dz = dy act'(.), xh = (x - mean) rstd, m1 and m2 the means of gamma dz and of gamma dz xh over the row,
+ *   dx = rstd (gamma dz - m1 - xh m2) (+ ds),  dgamma = sum dz xh,  dbeta = sum dz.
+ * ds (NULL: none) is the gradient that reaches s past the normalisation; dx is then that of x and of r alike.  dgamma and
+ * dbeta are sums over worker g's rows, written (not added) at dgamma + g par_gs and dbeta + g par_gs; zeros if R = 0.  ReLU's
+ * derivative is taken from the stored output (y > 0); the other activations do not read y (NULL is fine).  Sums are fp32, in
+ * segments and in a fixed order: deterministic.
+ * `workspace`: device memory of at least lsgd_layernorm_workspace's bytes (0: it is not used and may be NULL), 16-byte
+ * aligned, whose contents do not matter before or after; calls (or captured graphs) that may run at the same time need
+ * one each.  Limits and errors as for the forward. */
+lsgd_status lsgd_layernorm_workspace(int G, int64_t R, int64_t C, size_t* bytes);
+lsgd_status lsgd_layernorm_backward(const void* x, int x_type, int64_t x_ld, const void* y,
+                                    const void* dy, int y_type, int64_t y_ld, const void* ds,
+                                    const float* gamma, const float* beta, int64_t par_gs,
+                                    const float* mean, const float* rstd, void* dx, float* dgamma,
+                                    float* dbeta, int G, int64_t R, int64_t C, int act,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* The norm of each worker's whole gradient, which stands in many tensors; the gradients clipped by it; and the local update
+ * with the clipped gradient.  For worker k of G, over the values g of all of its tensors,
+ *   norm[k] = sqrt(sum g^2),  f = min(1, max_norm / norm[k]),  out = f g.
+ * (Clipping keeps a step at a large, worker-scaled learning rate from growing without bound.)
+ *
+ * An lsgd_tensors describes the tensors once, on the host: tensor i of worker k is n values (0: it is skipped) at g + k g_gs,
+ * of type g_type (LSGD_FP32 or LSGD_BF16); clipped values go to out + k out_gs (out_type), or, where every out is NULL, back to
+ * their places.  The tensors may be of any sizes, alignments and strides >= n, e.g. the pieces of a replica-major buffer; with one
+ * worker the strides are not looked at.  It keeps the addresses, nothing of the values, is not changed by any call and
+ * may be used by several calls and threads at once; lsgd_tensors_destroy (NULL is fine) when no more calls are made with it (captured
+ * graphs keep what they need).  At most 65535 workers, 2^24 tensors times workers, 2^42 bytes a worker.
+ *
+ * lsgd_gradient_norm writes norm [G] (fp32); lsgd_gradient_clip writes norm (before clipping) and the clipped gradients.  Squares are
+ * summed in 64 bits in a fixed order: deterministic, and no finite gradient overflows or vanishes (a norm above fp32's range is
+ * infinite).  A NaN among a worker's gradients makes its norm and all of its clipped gradients NaN, an infinite value
+ * makes its norm infinite, f zero and its own product NaN; other workers' are not touched.  Workers with f = 1 are
+ * copied, or left as they are where they are clipped in place.  max_norm is positive and finite.
+ *
+ * `workspace`: device memory of at least lsgd_gradient_workspace's bytes (0: it is not used and may be NULL), 16-byte
+ * aligned, whose contents do not matter before or after; calls (or captured graphs) that may run at the same time need
+ * one each.  No device allocation: the calls may be captured into a CUDA graph.  LSGD_EINVAL on bad arguments, and where norm,
+ * the workspace or what is clipped overlap anything else (a tensor that is listed twice is summed twice, and not clipped).
+ * LSGD_ENOMEM if the description cannot be allocated.  Device pointers, asynchronous on `stream`, which belongs to the
+ * current device. */
+typedef struct {
+  const void* g; /* clipped in place where out is NULL */
+  void* out;
+  int64_t n, g_gs, out_gs;
+  int g_type, out_type;
+} lsgd_tensor;
+typedef struct lsgd_tensors lsgd_tensors;
+lsgd_status lsgd_tensors_create(const lsgd_tensor* tensors, int count, int G, lsgd_tensors** out);
+void lsgd_tensors_destroy(lsgd_tensors* list);
+lsgd_status lsgd_gradient_workspace(const lsgd_tensors* list, size_t* bytes);
+lsgd_status lsgd_gradient_norm(const lsgd_tensors* list, float* norm, void* workspace,
+                               size_t workspace_bytes, void* stream);
+lsgd_status lsgd_gradient_clip(const lsgd_tensors* list, float* norm, float max_norm, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/* lsgd_sgd_update with every worker's gradient clipped by its norm (lsgd_gradient_norm's) on the way, so that the clipped
+ * gradient is not written: with f = min(1, max_norm / norm[k]) and g' = f g + (i < decay_end ? weight_decay w : 0) for value i
+ * of worker k's n,  u = momentum u + g';  w -= lr (nesterov ? g' + momentum u : u), or w -= lr g' without momentum (u not
+ * touched, may be NULL); Wb (optional) receives bf16(w).  w, u and Wb at stride w_gs, g (fp32 or bf16) at g_gs >= n; any n and
+ * strides (vectors where they and the pointers allow).  f = 1 gives lsgd_sgd_update's bits.  A NaN norm makes its own worker's w
+ * NaN, an infinite one takes a step without the gradient (its infinite values excepted).  LSGD_EINVAL on bad arguments and
+ * where w, u or Wb overlap another tensor (tensors whose strides or sizes of values differ count as wholes). */
+lsgd_status lsgd_clipped_update(float* w, float* u, int64_t w_gs, const void* g, int g_type, int64_t g_gs,
+                                uint16_t* Wb, int G, int64_t n, const float* norm, float max_norm,
+                                float lr, float momentum, int nesterov, float weight_decay,
+                                int64_t decay_end, void* stream);
+
 /* Worker mini-batch indices for one step into dst [K][B] int32 (device), as lsgd_local_step. */
 lsgd_status lsgd_sample_indices(int32_t* dst, uint64_t seed, int64_t step, int K, int B, int64_t N,
                                 void* stream);

@@ -47,6 +47,8 @@ EXPORTS = [
     "lsgd_conv_wgrad_bf16", "lsgd_conv3x3_bf16", "lsgd_conv3x3_bn_bf16", "lsgd_run_batch",
     "lsgd_groupnorm_workspace", "lsgd_groupnorm_forward", "lsgd_groupnorm_backward",
     "lsgd_orthogonal_workspace", "lsgd_orthogonal_direction", "lsgd_direction_update",
+    "lsgd_layernorm_workspace", "lsgd_layernorm_forward", "lsgd_layernorm_backward", "lsgd_tensors_create",
+    "lsgd_tensors_destroy", "lsgd_gradient_workspace", "lsgd_gradient_norm", "lsgd_gradient_clip", "lsgd_clipped_update",
 ]
 PHASES = ["input", "forward", "loss", "backward", "update", "average"]
 
@@ -72,6 +74,11 @@ class LrSchedule(ctypes.Structure):
 
 class Profile(ctypes.Structure):
     _fields_ = [("count", ctypes.c_int64 * 6), ("ms", ctypes.c_double * 6)]
+
+
+class Tensor(ctypes.Structure):
+    _fields_ = [("g", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("g_gs", ctypes.c_int64),
+                ("out_gs", ctypes.c_int64), ("g_type", ctypes.c_int), ("out_type", ctypes.c_int)]
 
 
 ALLOC_FN = ctypes.CFUNCTYPE(ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p)
@@ -208,6 +215,19 @@ def lib():
                                          ctypes.c_int, ctypes.c_int, i64, ctypes.c_int, ctypes.c_int,
                                          ctypes.c_int, vp, ctypes.c_size_t, vp], st),
         }
+        ci, cf, sz = ctypes.c_int, ctypes.c_float, ctypes.c_size_t
+        sig.update({
+            "lsgd_layernorm_workspace": ([ci, i64, i64, P(sz)], st),
+            "lsgd_layernorm_forward": ([vp, vp, ci, i64, vp, vp, i64, vp, vp, ci, i64, vp, vp, ci, i64, i64, cf, ci, vp], st),
+            "lsgd_layernorm_backward": ([vp, ci, i64, vp, vp, ci, i64, vp, vp, vp, i64, vp, vp, vp, vp, vp, ci, i64, i64, ci,
+                                         vp, sz, vp], st),
+            "lsgd_tensors_create": ([P(Tensor), ci, ci, P(vp)], st),
+            "lsgd_tensors_destroy": ([vp], None),
+            "lsgd_gradient_workspace": ([vp, P(sz)], st),
+            "lsgd_gradient_norm": ([vp, vp, vp, sz, vp], st),
+            "lsgd_gradient_clip": ([vp, vp, cf, vp, sz, vp], st),
+            "lsgd_clipped_update": ([vp, vp, i64, vp, ci, i64, vp, ci, i64, vp, cf, cf, cf, ci, cf, i64, vp], st),
+        })
         for name, (args, res) in sig.items():
             f = getattr(L, name)
             f.argtypes = args
@@ -736,3 +756,135 @@ def lsgd_direction_update(w, o, Wb, G: int, n: int, lr: float, scale: float = 1.
     _launch(dev, stream, False, 0, lib().lsgd_direction_update,
             (w.data_ptr(), w_gs, o.data_ptr(), o_gs, Wb.data_ptr() if Wb is not None else None, G, n, lr, scale,
              weight_decay))
+
+
+@functools.lru_cache(maxsize=256)
+def lsgd_layernorm_workspace(G: int, R: int, C: int) -> int:
+    """Bytes of workspace that lsgd_layernorm_backward needs for these sizes (the forward needs none)."""
+    n = ctypes.c_size_t()
+    _check(lib().lsgd_layernorm_workspace(int(G), int(R), int(C), ctypes.byref(n)))
+    return int(n.value)
+
+
+def _row_span(N: int, ld: int, C: int) -> int:
+    return (N - 1) * ld + C if N else 0
+
+
+def lsgd_layernorm_forward(x, gamma, beta, y, mean, rstd, G: int, R: int, C: int, r=None, s=None, act: int = ACT_NONE,
+                           eps: float = 1e-5, par_gs: int = 0, x_ld: int = 0, y_ld: int = 0, stream=None):
+    """y = act(gamma (x - mean) rstd + beta) over rows of C values: x and y float32 or bfloat16, G R rows at strides x_ld and
+    y_ld (0: C), mean and rstd [G, R] float32, gamma and beta float32 at worker stride par_gs (0: C).  With r (x's type and
+    stride) s = x + r is stored in s and normalised instead of x."""
+    par_gs, x_ld, y_ld, N = par_gs or C, x_ld or C, y_ld or C, G * R
+    if (r is None) != (s is None):
+        raise LsgdError(EINVAL, "r and s come together")
+    nx, npar = _row_span(N, x_ld, C), (G - 1) * par_gs + C
+    xt, yt = _type_of(x), _type_of(y)
+    dev = _checked(("x", x, nx, xt), ("r", r, nx, xt), ("s", s, nx, xt), ("y", y, _row_span(N, y_ld, C), yt),
+                   ("gamma", gamma, npar, FP32), ("beta", beta, npar, FP32), ("mean", mean, N, FP32), ("rstd", rstd, N, FP32))
+    _launch(dev, stream, False, 0, lib().lsgd_layernorm_forward,
+            (x.data_ptr(), r.data_ptr() if r is not None else None, xt, x_ld, gamma.data_ptr(), beta.data_ptr(), par_gs,
+             s.data_ptr() if s is not None else None, y.data_ptr(), yt, y_ld, mean.data_ptr(), rstd.data_ptr(), G, R, C, eps,
+             act))
+
+
+def lsgd_layernorm_backward(x, y, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, G: int, R: int, C: int, ds=None,
+                            act: int = ACT_NONE, par_gs: int = 0, x_ld: int = 0, y_ld: int = 0, workspace=None, stream=None):
+    """The gradients of lsgd_layernorm_forward: dx (x's type) and, written at worker stride par_gs, dgamma and dbeta
+    (float32), from dy (y's type).  x is what was normalised (s where there was a residual); ds (x's type, None: none) is
+    added to dx.  y, the stored output, is read for ReLU only (None otherwise)."""
+    nbytes = lsgd_layernorm_workspace(G, R, C)
+    par_gs, x_ld, y_ld, N = par_gs or C, x_ld or C, y_ld or C, G * R
+    nx, ny, npar = _row_span(N, x_ld, C), _row_span(N, y_ld, C), (G - 1) * par_gs + C
+    xt, yt = _type_of(x), _type_of(dy)
+    dev = _checked(("x", x, nx, xt), ("dx", dx, nx, xt), ("ds", ds, nx, xt), ("dy", dy, ny, yt), ("y", y, ny, yt),
+                   ("gamma", gamma, npar, FP32), ("beta", beta, npar, FP32), ("dgamma", dgamma, npar, FP32),
+                   ("dbeta", dbeta, npar, FP32), ("mean", mean, N, FP32), ("rstd", rstd, N, FP32))
+    _launch(dev, stream, workspace, nbytes, lib().lsgd_layernorm_backward,
+            (x.data_ptr(), xt, x_ld, y.data_ptr() if y is not None else None, dy.data_ptr(), yt, y_ld,
+             ds.data_ptr() if ds is not None else None, gamma.data_ptr(), beta.data_ptr(), par_gs, mean.data_ptr(),
+             rstd.data_ptr(), dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), G, R, C, act))
+
+
+class Tensors:
+    """A list of tensors, described once (see lsgd_tensors_create); keeps them alive."""
+
+    def __init__(self, handle, tensors, device: int, G: int, workspace: int):
+        self.handle, self.tensors, self.device, self.G, self.workspace = handle, tensors, device, G, workspace
+
+    def __del__(self):
+        if getattr(self, "handle", None) and _lib is not None:
+            _lib.lsgd_tensors_destroy(self.handle)
+            self.handle = None
+
+
+def lsgd_tensors_create(tensors, out=None, workers: bool = True) -> Tensors:
+    """Describes the float32 or bfloat16 CUDA tensors whose norm lsgd_gradient_norm takes: each [G, ...], a worker's values one
+    behind another and at any stride from worker to worker (workers=False: every tensor is one worker's, contiguous).
+    lsgd_gradient_clip writes to the tensors `out` of the same sizes, or without them back to `tensors`.  The list keeps the
+    tensors and their addresses: resize none while it is in use."""
+    tensors = list(tensors)
+    out = None if out is None else list(out)
+    if not tensors:
+        raise LsgdError(EINVAL, "at least one tensor is wanted")
+    if out is not None and len(out) != len(tensors):
+        raise LsgdError(EINVAL, f"{len(tensors)} tensors, but {len(out)} to write to")
+    if workers and any(t.dim() == 0 for t in tensors + (out or [])):
+        raise LsgdError(EINVAL, "tensors of all workers have a first dimension of their number")
+    dev, G = tensors[0].get_device(), tensors[0].shape[0] if workers else 1
+
+    def place(t, n):
+        """(address, worker stride, type) of a tensor whose workers have n values each."""
+        if t.get_device() != dev or dev < 0:
+            raise LsgdError(EINVAL, "CUDA tensors on one device are wanted")
+        one = t[0] if workers and t.shape[0] else t
+        if (workers and t.shape[0] != G) or one.numel() != n or not one.is_contiguous():
+            raise LsgdError(EINVAL, f"a tensor of {G} workers' {n} values each, one behind another, is wanted")
+        return t.data_ptr() if n else None, t.stride(0) if workers else 0, _type_of(t)
+
+    table = (Tensor * len(tensors))()
+    for i, (e, t) in enumerate(zip(table, tensors)):
+        e.n = t.numel() // G if G else 0
+        e.g, e.g_gs, e.g_type = place(t, e.n)
+        if out is not None:
+            e.out, e.out_gs, e.out_type = place(out[i], e.n)
+    handle, n = ctypes.c_void_p(), ctypes.c_size_t()
+    _check(lib().lsgd_tensors_create(table, len(tensors), G, ctypes.byref(handle)))
+    _check(lib().lsgd_gradient_workspace(handle, ctypes.byref(n)))
+    return Tensors(handle, (tensors, out), dev, G, int(n.value))
+
+
+def lsgd_gradient_norm(tensors: Tensors, norm, workspace=None, stream=None):
+    """norm [G] (float32) = the norm of each worker's values in all of the list's tensors."""
+    dev = _checked(("norm", norm, tensors.G, _type_of(norm)))
+    if dev != tensors.device or norm.dtype is not _WANTED[FP32]:
+        raise LsgdError(EINVAL, f"norm: a float32 tensor on CUDA device {tensors.device} is wanted")
+    _launch(dev, stream, workspace, tensors.workspace, lib().lsgd_gradient_norm, (tensors.handle, norm.data_ptr()))
+
+
+def lsgd_gradient_clip(tensors: Tensors, norm, max_norm: float, workspace=None, stream=None):
+    """norm [G] (float32) as lsgd_gradient_norm, and every worker's values times min(1, max_norm / norm)."""
+    dev = _checked(("norm", norm, tensors.G, _type_of(norm)))
+    if dev != tensors.device or norm.dtype is not _WANTED[FP32]:
+        raise LsgdError(EINVAL, f"norm: a float32 tensor on CUDA device {tensors.device} is wanted")
+    _launch(dev, stream, workspace, tensors.workspace, lib().lsgd_gradient_clip, (tensors.handle, norm.data_ptr(), max_norm))
+
+
+def lsgd_clipped_update(w, u, g, Wb, G: int, n: int, norm, max_norm: float, lr: float, momentum: float = 0.0,
+                        nesterov: bool = False, weight_decay: float = 0.0, decay_end: int | None = None, w_gs: int = 0,
+                        g_gs: int = 0, stream=None):
+    """The local update of G workers' n values with the gradients clipped by their norms on the way: g' = f g + weight_decay w
+    (the decay for a worker's first decay_end values, None: all), f = min(1, max_norm / norm), u = momentum u + g',
+    w -= lr (nesterov ? g' + momentum u : u).  w and u float32 and Wb (bfloat16 or None, = bf16(w)) at stride w_gs, g float32 or
+    bfloat16 at g_gs (0: n), norm [G] float32; u None without momentum."""
+    w_gs, g_gs = w_gs or n, g_gs or n
+    span = (G - 1) * w_gs + n
+    if u is None and momentum:
+        raise LsgdError(EINVAL, "u: wanted with momentum")
+    gt = _type_of(g)
+    dev = _checked(("w", w, span, FP32), ("u", u, span, FP32), ("g", g, (G - 1) * g_gs + n, gt), ("Wb", Wb, span, BF16),
+                   ("norm", norm, G, FP32))
+    _launch(dev, stream, False, 0, lib().lsgd_clipped_update,
+            (w.data_ptr(), u.data_ptr() if u is not None else None, w_gs, g.data_ptr(), gt, g_gs,
+             Wb.data_ptr() if Wb is not None else None, G, n, norm.data_ptr(), max_norm, lr, momentum, int(bool(nesterov)),
+             weight_decay, n if decay_end is None else decay_end))

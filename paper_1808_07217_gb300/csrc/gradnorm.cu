@@ -1,0 +1,568 @@
+// The norm of each worker's whole gradient, which stands in many tensors, the gradients clipped by it, and the local update with
+// the clipped gradient.
+//
+// For worker k:  norm = sqrt(sum over its tensors' values g^2),  f = min(1, max_norm / norm),  out = f g,
+// and in the update  g' = f g + wd w, then the momentum step of lsgd_sgd_update.
+//
+// All are bound by memory.  The tensors are cut into pieces of one size in bytes, and every warp takes every n-th piece of one
+// worker: where the tensors begin is found in a table that comes with the launch, so that hundreds of small tensors cost one
+// launch and keep every SM busy.  A warp has a whole piece's loads under way at once.
+//
+// Sums.  A lane's squares of a piece (at most 64) are added in fp32, these sums in 64 bits and in a fixed order.  Where a
+// lane's fp32 sum is too large or too small for fp32's range its values are squared and added in 64 bits, whose range holds the
+// square of any fp32 value: no finite gradient overflows, none vanishes.
+#include <algorithm>
+#include <new>
+#include <string>
+#include <vector>
+
+#include "../../include/lsgd.h"
+#include "common.cuh"
+#include "lsgd_internal.h"
+#include "operands.h"
+
+struct lsgd_tensors {
+  std::vector<lsgd_tensor> list;     // without the empty ones
+  std::vector<uint32_t> first;       // first piece of each, and their number
+  int G = 0, piece = 0;              // workers; bytes of a piece
+  bool places = false;               // every tensor has an `out`
+  bool overlap = false;              // what a clipping would write overlaps something
+  int blocks = 0;                    // CTAs of a worker in the passes
+  uintptr_t lo = UINTPTR_MAX, hi = 0;  // all that is read or written lies between
+};
+
+namespace lsgd {
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMaxPiece = 4096, kMinPiece = 512;
+
+struct Entry {
+  const void* in;
+  void* out;
+  int64_t n, gs, out_gs;
+  uint32_t first;
+  uint16_t bf16, out_bf16;
+};
+// The tensors of a launch.  A launch's parameters hold up to 32,764 bytes: longer lists take several launches.
+template <int MAX>
+struct Table {
+  int count, shift;       // tensors; log2 of a piece's bytes
+  uint32_t begin, end;    // the launch's pieces
+  Entry e[MAX];
+};
+constexpr int kFew = 64, kMany = 640;
+
+// The piece's tensor: the last whose first piece is at most p, from tensor t on.
+template <int MAX>
+__device__ __forceinline__ int find(const Table<MAX>& tab, int t, uint32_t p) {
+  if (t + 1 >= tab.count || p < tab.e[t + 1].first) return t;
+  int lo = t + 1, hi = tab.count;  // e[lo].first <= p
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (tab.e[mid].first <= p) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+struct Range {  // a piece's values
+  const uint8_t* p;
+  int len, head, nv;  // values; those before the first 16-byte boundary; whole vectors behind them
+  __device__ __forceinline__ Range(const Entry& e, int shift, int64_t worker, uint32_t piece) {
+    const int zs = e.bf16 ? 1 : 2;  // log2 of a value's bytes
+    const int64_t at = (int64_t)(piece - e.first) << (shift - zs);
+    p = static_cast<const uint8_t*>(e.in) + ((worker * e.gs + at) << zs);
+    len = (int)min((int64_t)1 << (shift - zs), e.n - at);
+    head = min(len, (int)((0u - (uint32_t)reinterpret_cast<uintptr_t>(p)) & 15u) >> zs);
+    nv = (len - head) >> (4 - zs);
+  }
+};
+
+__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// f(value) for every value of a vector.
+template <typename F>
+__device__ __forceinline__ void each(const uint4& r, bool bf16, F f) {
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+  if (bf16) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f(bf_lo(w[i])), f(bf_hi(w[i]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f(__uint_as_float(w[i]));
+  }
+}
+
+constexpr int kVecs = kMaxPiece / 16 / 32;  // vectors of a lane
+
+// The sum of squares of this lane's values of a piece.
+__device__ __forceinline__ double piece_squares(const Range& r, bool bf16, int lane) {
+  const uint4* v = reinterpret_cast<const uint4*>(r.p + r.head * (bf16 ? 2 : 4));
+  uint4 raw[kVecs];
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i)
+    raw[i] = lane + 32 * i < r.nv ? __ldg(v + lane + 32 * i) : make_uint4(0, 0, 0, 0);
+  // the values before and behind the vectors: at most 7 each
+  const int tail = r.head + r.nv * (bf16 ? 8 : 4) + lane;
+  uint32_t h = 0, t = 0;
+  if (bf16) {
+    if (lane < r.head) h = (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(r.p) + lane) << 16;
+    if (tail < r.len) t = (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(r.p) + tail) << 16;
+  } else {
+    if (lane < r.head) h = __ldg(reinterpret_cast<const uint32_t*>(r.p) + lane);
+    if (tail < r.len) t = __ldg(reinterpret_cast<const uint32_t*>(r.p) + tail);
+  }
+  const float hf = __uint_as_float(h), tf = __uint_as_float(t);
+  float s = fmaf(hf, hf, tf * tf);
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) each(raw[i], bf16, [&](float x) { s = fmaf(x, x, s); });
+  // (a value whose square lost bits below 2^-149 is at most 2^-49 of a sum of 2^-100)
+  if (s >= 0x1p-100f && s < 0x1p126f) return s;
+  uint32_t any = (h | t) & 0x7fffffffu;
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) any |= (raw[i].x | raw[i].y | raw[i].z | raw[i].w) & (bf16 ? 0x7fff7fffu : 0x7fffffffu);
+  if (!any) return 0.0;
+  double d = (double)hf * hf + (double)tf * tf;
+#pragma unroll 1
+  for (int i = 0; i < kVecs; ++i) {
+    uint4 w = raw[0];
+#pragma unroll
+    for (int j = 1; j < kVecs; ++j)
+      if (j == i) w = raw[j];
+    each(w, bf16, [&](float x) {
+      if (x != 0.f) d += (double)x * x;
+    });
+  }
+  return d;
+}
+
+__device__ __forceinline__ double warp_sum(double v) {
+  for (int d = 16; d; d /= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
+  return v;
+}
+__device__ __forceinline__ double block_sum(double v) {  // in every thread
+  __shared__ double part[kWarps];
+  v = warp_sum(v);
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x / 32] = v;
+  __syncthreads();
+  v = 0.0;
+  for (int i = 0; i < kWarps; ++i) v += part[i];
+  return v;
+}
+
+// One sum for each CTA into part [G][slots] from slot `slot` on, or, with `norm`, the norm of its worker.
+template <int MAX>
+__global__ void __launch_bounds__(kThreads, 4) grad_squares_kernel(const __grid_constant__ Table<MAX> tab, double* part, int slot,
+                                                                   int slots, float* norm) {
+  pdl_begin();
+  const int lane = threadIdx.x & 31;
+  const uint32_t stride = gridDim.x * kWarps;
+  double s = 0.0;
+  int t = 0;
+  for (uint64_t p = tab.begin + blockIdx.x * kWarps + threadIdx.x / 32; p < tab.end; p += stride) {
+    t = find(tab, t, (uint32_t)p);
+    const Entry& e = tab.e[t];
+    s += piece_squares(Range(e, tab.shift, blockIdx.y, (uint32_t)p), e.bf16, lane);
+  }
+  s = block_sum(s);
+  if (threadIdx.x) return;
+  if (norm) norm[blockIdx.y] = (float)sqrt(s);
+  else part[(int64_t)blockIdx.y * slots + slot + blockIdx.x] = s;
+}
+
+__global__ void __launch_bounds__(kThreads) grad_norm_kernel(const double* part, int slots, float* norm) {
+  pdl_begin();
+  double s = 0.0;
+  for (int i = threadIdx.x; i < slots; i += kThreads) s += part[(int64_t)blockIdx.x * slots + i];
+  s = block_sum(s);
+  if (threadIdx.x == 0) norm[blockIdx.x] = (float)sqrt(s);
+}
+
+// min(1, max_norm / norm): NaN for a NaN norm, 0 for an infinite one.
+__device__ __forceinline__ float clip_factor(float norm, float max_norm) { return norm <= max_norm ? 1.f : __fdiv_rn(max_norm, norm); }
+
+__device__ __forceinline__ void put(void* out, int64_t i, bool bf16, float v) {
+  if (bf16) static_cast<uint16_t*>(out)[i] = f2bf(v);
+  else static_cast<float*>(out)[i] = v;
+}
+
+template <int MAX>
+__global__ void __launch_bounds__(kThreads, 4) grad_scale_kernel(const __grid_constant__ Table<MAX> tab, const float* norm,
+                                                                 float max_norm) {
+  pdl_begin();
+  const int lane = threadIdx.x & 31;
+  const uint32_t stride = gridDim.x * kWarps;
+  const float f = clip_factor(norm[blockIdx.y], max_norm);
+  int t = 0;
+  for (uint64_t p = tab.begin + blockIdx.x * kWarps + threadIdx.x / 32; p < tab.end; p += stride) {
+    t = find(tab, t, (uint32_t)p);
+    const Entry& e = tab.e[t];
+    if (f == 1.f && e.out == e.in) continue;
+    const bool bf16 = e.bf16, ob = e.out_bf16;
+    const Range r(e, tab.shift, blockIdx.y, (uint32_t)p);
+    const int64_t at = blockIdx.y * e.out_gs + ((int64_t)((uint32_t)p - e.first) << (tab.shift - (bf16 ? 1 : 2)));
+    void* out = static_cast<uint8_t*>(e.out) + at * (ob ? 2 : 4);
+    const auto value = [&](int i) {
+      return bf16 ? bf2f(reinterpret_cast<const uint16_t*>(r.p)[i]) : reinterpret_cast<const float*>(r.p)[i];
+    };
+    const int width = bf16 ? 8 : 4;                            // values of a vector
+    const int bytes = min(16, width * (ob ? 2 : 4));           // of one store
+    uint8_t* to = static_cast<uint8_t*>(out) + r.head * (ob ? 2 : 4);
+    if (reinterpret_cast<uintptr_t>(to) % bytes) {
+      // what is read and what is written are never aligned together: value by value
+#pragma unroll 4
+      for (int i = lane; i < r.len; i += 32) put(out, i, ob, value(i) * f);
+      continue;
+    }
+    const uint4* v = reinterpret_cast<const uint4*>(r.p + r.head * (bf16 ? 2 : 4));
+    uint4 raw[kVecs];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+      if (lane + 32 * i < r.nv) raw[i] = v[lane + 32 * i];
+    const int tail = r.head + r.nv * width + lane;
+    if (lane < r.head) put(out, lane, ob, value(lane) * f);
+    if (tail < r.len) put(out, tail, ob, value(tail) * f);
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+      if (lane + 32 * i < r.nv) {
+        float x[8];
+        int k = 0;
+        each(raw[i], bf16, [&](float q) { x[k++] = q * f; });
+        const int64_t j = lane + 32 * i;
+        const auto pair = [&](int q) { return (uint32_t)f2bf(x[q]) | (uint32_t)f2bf(x[q + 1]) << 16; };
+        if (ob && bf16) reinterpret_cast<uint4*>(to)[j] = make_uint4(pair(0), pair(2), pair(4), pair(6));
+        else if (ob) reinterpret_cast<uint2*>(to)[j] = make_uint2(pair(0), pair(2));
+        else {
+          float4* q = reinterpret_cast<float4*>(to) + (bf16 ? 2 * j : j);
+          q[0] = make_float4(x[0], x[1], x[2], x[3]);
+          if (bf16) q[1] = make_float4(x[4], x[5], x[6], x[7]);
+        }
+      }
+  }
+}
+
+// ---- the local update with the clipped gradient ----
+struct UpdateArgs {
+  float *w, *u;
+  const void* g;
+  uint16_t* wb;
+  int64_t w_gs, g_gs, n, decay_end;
+  const float* norm;
+  float max_norm, lr, m, wd;
+};
+
+template <bool GB, bool MOM, bool NEST, bool SHADOW, bool WIDE>
+__global__ void __launch_bounds__(256) clipped_update_kernel(const UpdateArgs a) {
+  pdl_begin();
+  const int64_t k = blockIdx.y, stride = (int64_t)gridDim.x * blockDim.x, first = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  const float f = clip_factor(a.norm[k], a.max_norm);
+  float *w = a.w + k * a.w_gs, *u = a.u + (MOM ? k * a.w_gs : 0);
+  uint16_t* wb = a.wb + (SHADOW ? k * a.w_gs : 0);
+  const float* gf = static_cast<const float*>(a.g) + (GB ? 0 : k * a.g_gs);
+  const uint16_t* gb = static_cast<const uint16_t*>(a.g) + (GB ? k * a.g_gs : 0);
+  const auto one = [&](int64_t i) {
+    float wv = w[i], uv = MOM ? u[i] : 0.f;
+    sgd_elem<MOM, NEST>(wv, uv, f * (GB ? bf2f(gb[i]) : gf[i]), a.lr, a.m, i < a.decay_end ? a.wd : 0.f);
+    w[i] = wv;
+    if (MOM) u[i] = uv;
+    if (SHADOW) wb[i] = f2bf(wv);
+  };
+  int64_t done = 0;
+  if constexpr (WIDE) {
+    const int64_t n4 = a.n / 4;
+    for (int64_t i = first; i < n4; i += stride) {
+      float gv[4], wv[4], uv[4];
+      if constexpr (GB) {
+        const uint2 r = __ldcs(reinterpret_cast<const uint2*>(gb) + i);
+        gv[0] = bf_lo(r.x), gv[1] = bf_hi(r.x), gv[2] = bf_lo(r.y), gv[3] = bf_hi(r.y);
+      } else {
+        *reinterpret_cast<float4*>(gv) = __ldcs(reinterpret_cast<const float4*>(gf) + i);
+      }
+      *reinterpret_cast<float4*>(wv) = __ldcs(reinterpret_cast<const float4*>(w) + i);
+      if (MOM) *reinterpret_cast<float4*>(uv) = __ldcs(reinterpret_cast<const float4*>(u) + i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        sgd_elem<MOM, NEST>(wv[j], uv[j], f * gv[j], a.lr, a.m, 4 * i + j < a.decay_end ? a.wd : 0.f);
+      if (MOM) __stcs(reinterpret_cast<float4*>(u) + i, *reinterpret_cast<float4*>(uv));
+      __stcs(reinterpret_cast<float4*>(w) + i, *reinterpret_cast<float4*>(wv));
+      if (SHADOW)
+        __stcs(reinterpret_cast<uint2*>(wb) + i, make_uint2((uint32_t)f2bf(wv[0]) | (uint32_t)f2bf(wv[1]) << 16,
+                                                            (uint32_t)f2bf(wv[2]) | (uint32_t)f2bf(wv[3]) << 16));
+    }
+    done = n4 * 4;
+  }
+  for (int64_t i = done + first; i < a.n; i += stride) one(i);
+}
+
+template <bool GB, bool MOM, bool NEST, bool SHADOW>
+cudaError_t launch_clipped(const UpdateArgs& a, int G, bool wide, cudaStream_t st) {
+  const int64_t items = wide ? std::max<int64_t>(a.n / 4, 1) : a.n;
+  const int64_t most = std::max<int64_t>(1, (int64_t)kNumSMs * 8 / G);
+  const dim3 grid((unsigned)std::min<int64_t>(most, (items + 255) / 256), G);
+  return wide ? launch_pdl(clipped_update_kernel<GB, MOM, NEST, SHADOW, true>, grid, dim3(256), 0, st, a)
+              : launch_pdl(clipped_update_kernel<GB, MOM, NEST, SHADOW, false>, grid, dim3(256), 0, st, a);
+}
+template <bool GB, bool MOM, bool NEST>
+cudaError_t clipped_shadow(const UpdateArgs& a, int G, bool wide, cudaStream_t st) {
+  return a.wb ? launch_clipped<GB, MOM, NEST, true>(a, G, wide, st) : launch_clipped<GB, MOM, NEST, false>(a, G, wide, st);
+}
+template <bool GB>
+cudaError_t clipped_rule(const UpdateArgs& a, int G, bool nesterov, bool wide, cudaStream_t st) {
+  if (a.m == 0.f) return clipped_shadow<GB, false, false>(a, G, wide, st);
+  return nesterov ? clipped_shadow<GB, true, true>(a, G, wide, st) : clipped_shadow<GB, true, false>(a, G, wide, st);
+}
+
+lsgd_status gr_error(lsgd_status s, const char* fn, const char* what) {
+  set_last_error(std::string(fn) + ": " + what);
+  return s;
+}
+int size_of(int type) { return type == LSGD_BF16 ? 2 : 4; }
+
+// The number of launches of a list, each of at most kMany tensors.
+int launches(const lsgd_tensors& l) { return (int)((l.list.size() + kMany - 1) / kMany); }
+int slots_of(const lsgd_tensors& l) { return l.blocks * launches(l); }
+
+template <int MAX>
+void fill(Table<MAX>& tab, const lsgd_tensors& l, size_t from, size_t to) {
+  tab.count = (int)(to - from);
+  tab.shift = __builtin_ctz(l.piece);
+  tab.begin = l.first[from], tab.end = l.first[to];
+  for (size_t i = from; i < to; ++i) {
+    const lsgd_tensor& t = l.list[i];
+    Entry& e = tab.e[i - from];
+    e.in = t.g, e.out = l.places ? t.out : const_cast<void*>(t.g);
+    e.n = t.n, e.gs = t.g_gs, e.out_gs = l.places ? t.out_gs : t.g_gs;
+    e.first = l.first[i];
+    e.bf16 = t.g_type == LSGD_BF16, e.out_bf16 = (l.places ? t.out_type : t.g_type) == LSGD_BF16;
+  }
+}
+
+template <int MAX>
+cudaError_t squares(const lsgd_tensors& l, size_t from, size_t to, double* part, int slot, int slots, float* norm, cudaStream_t st) {
+  Table<MAX> tab;
+  fill(tab, l, from, to);
+  return launch_pdl(grad_squares_kernel<MAX>, dim3(l.blocks, l.G), dim3(kThreads), 0, st, tab, part, slot, slots, norm);
+}
+template <int MAX>
+cudaError_t scale(const lsgd_tensors& l, size_t from, size_t to, const float* norm, float max_norm, cudaStream_t st) {
+  Table<MAX> tab;
+  fill(tab, l, from, to);
+  return launch_pdl(grad_scale_kernel<MAX>, dim3(l.blocks, l.G), dim3(kThreads), 0, st, tab, norm, max_norm);
+}
+
+cudaError_t norm_of(const lsgd_tensors& l, float* norm, double* part, cudaStream_t st) {
+  const size_t count = l.list.size();
+  const int slots = slots_of(l);
+  if (slots == 0) return cudaMemsetAsync(norm, 0, sizeof(float) * l.G, st);
+  cudaError_t e = cudaSuccess;
+  for (size_t i = 0, k = 0; i < count && e == cudaSuccess; i += kMany, ++k) {
+    const size_t to = std::min(count, i + kMany);
+    float* direct = slots == 1 ? norm : nullptr;
+    e = to - i <= kFew ? squares<kFew>(l, i, to, part, (int)k * l.blocks, slots, direct, st)
+                       : squares<kMany>(l, i, to, part, (int)k * l.blocks, slots, direct, st);
+  }
+  if (e != cudaSuccess || slots == 1) return e;
+  return launch_pdl(grad_norm_kernel, dim3(l.G), dim3(kThreads), 0, st, (const double*)part, slots, norm);
+}
+
+size_t gr_workspace(const lsgd_tensors& l) { return slots_of(l) > 1 ? (size_t)l.G * slots_of(l) * sizeof(double) : 0; }
+
+// The first or the last address of a tensor's blocks (gs may be any number where there is one worker).
+uintptr_t end_of(const void* p, int64_t n, int64_t gs, int type, int G) {
+  return reinterpret_cast<uintptr_t>(p) + (uintptr_t)((G - 1) * gs + n) * size_of(type);
+}
+
+// Whether what a clipping writes meets anything: every worker's every tensor, in order of address.  A tensor may be clipped in
+// place (what is written there is what is read), but not twice.
+bool clip_overlaps(const lsgd_tensors& l) {
+  struct Block {
+    uintptr_t at, end;
+    bool written;
+  };
+  std::vector<Block> b;
+  b.reserve(l.list.size() * l.G * 2);
+  for (const lsgd_tensor& t : l.list)
+    for (int k = 0; k < l.G; ++k) {
+      const uintptr_t in = reinterpret_cast<uintptr_t>(t.g) + (uintptr_t)(k * t.g_gs) * size_of(t.g_type);
+      const uintptr_t in_end = in + (uintptr_t)t.n * size_of(t.g_type);
+      const uintptr_t out = l.places ? reinterpret_cast<uintptr_t>(t.out) + (uintptr_t)(k * t.out_gs) * size_of(t.out_type) : in;
+      const uintptr_t out_end = out + (uintptr_t)t.n * size_of(l.places ? t.out_type : t.g_type);
+      b.push_back({out, out_end, true});
+      if (in != out || in_end != out_end) b.push_back({in, in_end, false});
+    }
+  std::sort(b.begin(), b.end(), [](const Block& x, const Block& y) { return x.at < y.at; });
+  uintptr_t end = 0, written_end = 0;  // of all blocks so far, of the written ones
+  for (const Block& x : b) {
+    if (x.at < (x.written ? end : written_end)) return true;
+    end = std::max(end, x.end);
+    if (x.written) written_end = std::max(written_end, x.end);
+  }
+  return false;
+}
+
+// Whether [p, p + bytes) meets a tensor of the list.
+bool meets(const lsgd_tensors& l, const void* p, size_t bytes) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  if (!bytes || at >= l.hi || at + bytes <= l.lo) return false;
+  const Blocks mine(p, bytes);
+  for (const lsgd_tensor& t : l.list)
+    if (blocks_meet(mine, Blocks(t.g, (size_t)t.n * size_of(t.g_type), t.g_gs, l.G, size_of(t.g_type))) ||
+        (l.places && blocks_meet(mine, Blocks(t.out, (size_t)t.n * size_of(t.out_type), t.out_gs, l.G, size_of(t.out_type)))))
+      return true;
+  return false;
+}
+
+const char* norm_error(const lsgd_tensors* l, const float* norm, const void* workspace, size_t bytes) {
+  if (!l) return "the list is NULL";
+  const size_t need = gr_workspace(*l);
+  if (!norm || misaligned(norm, 4)) return "norm is NULL or not aligned";
+  if (need && (!workspace || bytes < need || misaligned(workspace, 16)))
+    return "workspace NULL, not 16-byte aligned or smaller than lsgd_gradient_workspace says";
+  if (meets(*l, norm, 4 * (size_t)l->G) || meets(*l, workspace, need) ||
+      (need && blocks_meet(Blocks(norm, 4 * (size_t)l->G), Blocks(workspace, need))))
+    return "tensors overlap";
+  return nullptr;
+}
+
+}  // namespace
+}  // namespace lsgd
+
+extern "C" {
+
+lsgd_status lsgd_tensors_create(const lsgd_tensor* tensors, int count, int G, lsgd_tensors** out) {
+  using namespace lsgd;
+  const char* fn = "lsgd_tensors_create";
+  if (!tensors || !out || count < 1) return gr_error(LSGD_EINVAL, fn, "tensors or out is NULL, or count below 1");
+  if (G < 1 || G > 65535 || (int64_t)count * G > (1 << 24))
+    return gr_error(LSGD_EINVAL, fn, "at least 1 and at most 65535 workers, at most 2^24 tensors of all workers");
+  int places = 0;
+  int64_t bytes = 0;  // of a worker
+  for (int i = 0; i < count; ++i) {
+    const lsgd_tensor& t = tensors[i];
+    const auto bad_type = [](int type) { return type != LSGD_FP32 && type != LSGD_BF16; };
+    const auto bad_place = [&](const void* p, int64_t gs, int type) {
+      return (t.n && !p) || misaligned(p, size_of(type)) ||
+             (G > 1 && (gs < t.n || gs > ((int64_t)1 << 50) / G));
+    };
+    if (t.n < 0 || t.n > ((int64_t)1 << 40)) return gr_error(LSGD_EINVAL, fn, "a tensor has 0 to 2^40 values of a worker");
+    if (bad_type(t.g_type) || (t.out && bad_type(t.out_type))) return gr_error(LSGD_EINVAL, fn, "types are LSGD_FP32 or LSGD_BF16");
+    if (bad_place(t.g, t.g_gs, t.g_type) || (t.out && bad_place(t.out, t.out_gs, t.out_type)))
+      return gr_error(LSGD_EINVAL, fn, "a tensor is NULL, not aligned to its element, or its workers' strides below n or above 2^50");
+    if (t.n) places |= t.out ? 1 : 2;
+    bytes += t.n * size_of(t.g_type);
+    if (bytes > ((int64_t)1 << 42)) return gr_error(LSGD_EINVAL, fn, "at most 2^42 bytes of a worker");
+  }
+  if (places == 3) return gr_error(LSGD_EINVAL, fn, "either every tensor has an out or none has");
+  try {
+    auto* l = new lsgd_tensors;
+    try {
+      l->G = G, l->places = places == 1;
+      // Pieces small enough for every SM's warps to have some, up to 4096 bytes (8 vectors a lane), a launch's at most 2^31.
+      l->piece = kMaxPiece;
+      while (l->piece > kMinPiece && bytes / l->piece * G < (int64_t)kNumSMs * 64) l->piece /= 2;
+      uint32_t at = 0;
+      for (int i = 0; i < count; ++i)
+        if (tensors[i].n) {
+          const lsgd_tensor& t = tensors[i];
+          l->list.push_back(t);
+          l->first.push_back(at);
+          at += (uint32_t)((t.n * size_of(t.g_type) + l->piece - 1) / l->piece);
+          l->lo = std::min(l->lo, reinterpret_cast<uintptr_t>(t.g));
+          l->hi = std::max(l->hi, end_of(t.g, t.n, t.g_gs, t.g_type, G));
+          if (l->places) {
+            l->lo = std::min(l->lo, reinterpret_cast<uintptr_t>(t.out));
+            l->hi = std::max(l->hi, end_of(t.out, t.n, t.out_gs, t.out_type, G));
+          }
+        }
+      l->first.push_back(at);
+      const int64_t most = std::max<int64_t>(1, (int64_t)kNumSMs * 4 / G);
+      l->blocks = (int)std::min<int64_t>(most, ((int64_t)at + kWarps - 1) / kWarps);
+      l->overlap = clip_overlaps(*l);
+    } catch (...) {
+      delete l;
+      throw;
+    }
+    *out = l;
+  } catch (const std::bad_alloc&) {
+    return gr_error(LSGD_ENOMEM, fn, "out of host memory");
+  }
+  return LSGD_OK;
+}
+
+void lsgd_tensors_destroy(lsgd_tensors* list) { delete list; }
+
+lsgd_status lsgd_gradient_workspace(const lsgd_tensors* list, size_t* bytes) {
+  using namespace lsgd;
+  if (!list || !bytes) return gr_error(LSGD_EINVAL, "lsgd_gradient_workspace", "a pointer is NULL");
+  *bytes = gr_workspace(*list);
+  return LSGD_OK;
+}
+
+lsgd_status lsgd_gradient_norm(const lsgd_tensors* list, float* norm, void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace lsgd;
+  const char* fn = "lsgd_gradient_norm";
+  const char* bad = norm_error(list, norm, workspace, workspace_bytes);
+  if (bad) return gr_error(LSGD_EINVAL, fn, bad);
+  const cudaError_t e = norm_of(*list, norm, static_cast<double*>(workspace), (cudaStream_t)stream);
+  return e == cudaSuccess ? LSGD_OK : gr_error(LSGD_ECUDA, fn, cudaGetErrorString(e));
+}
+
+lsgd_status lsgd_gradient_clip(const lsgd_tensors* list, float* norm, float max_norm, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+  using namespace lsgd;
+  const char* fn = "lsgd_gradient_clip";
+  const char* bad = norm_error(list, norm, workspace, workspace_bytes);
+  if (!bad && !(max_norm > 0.f && max_norm < INFINITY)) bad = "max_norm must be positive and finite";
+  if (!bad && list->overlap) bad = "what would be written overlaps another tensor of the list";
+  if (bad) return gr_error(LSGD_EINVAL, fn, bad);
+  const cudaStream_t st = (cudaStream_t)stream;
+  cudaError_t e = norm_of(*list, norm, static_cast<double*>(workspace), st);
+  const size_t count = list->list.size();
+  for (size_t i = 0; i < count && e == cudaSuccess; i += kMany) {
+    const size_t to = std::min(count, i + kMany);
+    e = to - i <= kFew ? scale<kFew>(*list, i, to, norm, max_norm, st) : scale<kMany>(*list, i, to, norm, max_norm, st);
+  }
+  return e == cudaSuccess ? LSGD_OK : gr_error(LSGD_ECUDA, fn, cudaGetErrorString(e));
+}
+
+lsgd_status lsgd_clipped_update(float* w, float* u, int64_t w_gs, const void* g, int g_type, int64_t g_gs, uint16_t* Wb, int G,
+                                int64_t n, const float* norm, float max_norm, float lr, float momentum, int nesterov,
+                                float weight_decay, int64_t decay_end, void* stream) {
+  using namespace lsgd;
+  const char* fn = "lsgd_clipped_update";
+  const char* bad = nullptr;
+  const int gz = size_of(g_type);
+  if (G < 1 || G > 65535 || n < 0 || n > ((int64_t)1 << 40)) bad = "at least 1 and at most 65535 workers, 0 to 2^40 values";
+  else if (g_type != LSGD_FP32 && g_type != LSGD_BF16) bad = "types are LSGD_FP32 or LSGD_BF16";
+  else if (n && (!w || !g || !norm || (momentum != 0.f && !u))) bad = "a pointer is NULL (u may be only without momentum)";
+  else if (G > 1 && (w_gs < n || g_gs < n || w_gs > ((int64_t)1 << 50) / G || g_gs > ((int64_t)1 << 50) / G))
+    bad = "w_gs and g_gs must be at least n (and addresses fit 64 bits)";
+  else if (misaligned(w, 4) || misaligned(u, 4) || misaligned(g, gz) || misaligned(Wb, 2) || misaligned(norm, 4))
+    bad = "a pointer is not aligned to its element";
+  else if (!(max_norm > 0.f && max_norm < INFINITY)) bad = "max_norm must be positive and finite";
+  else if (decay_end < 0) bad = "decay_end must not be negative";
+  if (bad) return gr_error(LSGD_EINVAL, fn, bad);
+  if (n == 0) return LSGD_OK;
+  const float* mom = momentum != 0.f ? u : nullptr;
+  const auto values = [&](const void* p, int64_t gs, int z) { return Blocks(p, (size_t)n * z, gs, G, z); };
+  // (blocks_meet takes one block or equal strides: tensors of other strides or sizes of values count as wholes)
+  const auto whole = [&](const void* p, int64_t gs, int z) { return Blocks(p, (size_t)((G - 1) * gs + n) * z); };
+  const Blocks W = values(w, w_gs, 4), U = values(mom, w_gs, 4), S = values(Wb, w_gs, 2), N(norm, 4 * (size_t)G);
+  const bool same = g_type != LSGD_BF16 && g_gs == w_gs;
+  const Blocks mine = same ? values(g, g_gs, 4) : whole(g, g_gs, gz);
+  const auto g_meets = [&](const Blocks& exact, const Blocks& all) { return blocks_meet(same ? exact : all, mine); };
+  if (blocks_meet(W, U) || blocks_meet(N, W) || blocks_meet(N, U) || blocks_meet(N, S) || g_meets(W, whole(w, w_gs, 4)) ||
+      g_meets(U, whole(mom, w_gs, 4)) ||
+      any_overlap({whole(Wb, w_gs, 2)}, {whole(w, w_gs, 4), whole(mom, w_gs, 4), whole(g, g_gs, gz)}))
+    return gr_error(LSGD_EINVAL, fn, "tensors overlap");
+  UpdateArgs a{w, u, g, Wb, w_gs, g_gs, n, decay_end, norm, max_norm, lr, momentum, weight_decay};
+  const bool wide = !misaligned(w, 16) && !(momentum != 0.f && misaligned(u, 16)) && !misaligned(g, 4 * gz) && !misaligned(Wb, 8) &&
+                    (G == 1 || (w_gs % 4 == 0 && g_gs % 4 == 0));
+  const cudaStream_t st = (cudaStream_t)stream;
+  const cudaError_t e = g_type == LSGD_BF16 ? clipped_rule<true>(a, G, nesterov, wide, st) : clipped_rule<false>(a, G, nesterov, wide, st);
+  return e == cudaSuccess ? LSGD_OK : gr_error(LSGD_ECUDA, fn, cudaGetErrorString(e));
+}
+
+}  // extern "C"

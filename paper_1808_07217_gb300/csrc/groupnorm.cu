@@ -20,7 +20,9 @@
 #include "../../include/lsgd.h"
 #include "common.cuh"
 #include "lsgd_internal.h"
+#include "operands.h"
 #include "tc_ptx.cuh"
+#include "vectors.cuh"
 
 namespace lsgd {
 
@@ -28,89 +30,6 @@ __device__ int g_norm_timeout = 0;
 static std::atomic<bool> g_norm_used{false};  // the flag is read only once a call has been made
 
 namespace {
-
-template <int BYTES>
-struct RawOf;
-template <>
-struct RawOf<16> {
-  using type = uint4;
-};
-template <>
-struct RawOf<8> {
-  using type = uint2;
-};
-template <>
-struct RawOf<4> {
-  using type = uint32_t;
-};
-template <>
-struct RawOf<2> {
-  using type = uint16_t;
-};
-
-// V values of T as loaded, and as floats.
-template <typename T, int V>
-struct Vec {
-  using Raw = typename RawOf<V * (int)sizeof(T) <= 16 ? V * (int)sizeof(T) : 16>::type;
-  static constexpr int kN = V * (int)sizeof(T) <= 16 ? 1 : V * (int)sizeof(T) / 16;
-  Raw r[kN];
-  __device__ __forceinline__ void load(const T* p) {
-#pragma unroll
-    for (int i = 0; i < kN; ++i) r[i] = __ldg(reinterpret_cast<const Raw*>(p) + i);
-  }
-  __device__ __forceinline__ void load_shared(const void* p) {
-#pragma unroll
-    for (int i = 0; i < kN; ++i) r[i] = static_cast<const Raw*>(p)[i];
-  }
-  __device__ __forceinline__ void floats(float (&v)[V]) const {
-    if constexpr (sizeof(T) == 4) {
-      const float* f = reinterpret_cast<const float*>(r);
-#pragma unroll
-      for (int j = 0; j < V; ++j) v[j] = f[j];
-    } else if constexpr (V == 1) {
-      v[0] = bf2f((uint16_t)r[0]);
-    } else {
-      const uint32_t* w = reinterpret_cast<const uint32_t*>(r);
-#pragma unroll
-      for (int j = 0; j < V / 2; ++j) {
-        v[2 * j] = __uint_as_float(w[j] << 16);
-        v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-      }
-    }
-  }
-  __device__ __forceinline__ float at(int j) const {
-    if constexpr (sizeof(T) == 4) return reinterpret_cast<const float*>(r)[j];
-    else if constexpr (V == 1) return bf2f((uint16_t)r[0]);
-    else {
-      const uint32_t w = reinterpret_cast<const uint32_t*>(r)[j / 2];
-      return __uint_as_float(j & 1 ? w & 0xffff0000u : w << 16);
-    }
-  }
-  __device__ __forceinline__ void set(const float (&v)[V]) {
-    if constexpr (sizeof(T) == 4) {
-      float* f = reinterpret_cast<float*>(r);
-#pragma unroll
-      for (int j = 0; j < V; ++j) f[j] = v[j];
-    } else if constexpr (V == 1) {
-      r[0] = f2bf(v[0]);
-    } else {
-      uint32_t* w = reinterpret_cast<uint32_t*>(r);
-#pragma unroll
-      for (int j = 0; j < V / 2; ++j) {
-        const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
-        w[j] = *reinterpret_cast<const uint32_t*>(&b);
-      }
-    }
-  }
-  __device__ __forceinline__ void store(T* p) const {
-#pragma unroll
-    for (int i = 0; i < kN; ++i) reinterpret_cast<Raw*>(p)[i] = r[i];
-  }
-  __device__ __forceinline__ void stream(T* p) const {  // leaves L2 to what will be read again
-#pragma unroll
-    for (int i = 0; i < kN; ++i) __stcs(reinterpret_cast<Raw*>(p) + i, r[i]);
-  }
-};
 
 struct GnArgs {
   const void *x, *y, *dy;
@@ -130,41 +49,6 @@ struct GnArgs {
   int cl, sub;    // resident form: CTAs per image; channels summed in a thread
   int stages, slab, slab_y;  // its pipeline: images ahead; bytes of an image of x and of dy (or y)
 };
-
-// 1 / (1 + exp(-z)): the exponential's overflow gives 0.  kExact (fp32 tensors): the accurate exponential and division.  kSums
-// (the sums over bf16 tensors, dgamma and dbeta among them, which are fp32 results): the accurate exponential and the fast
-// reciprocal, 2^-23 off.  kFast: the fast exponential too, 2^-21 and |z| 2^-23 off, which a bf16 result's rounding of 2^-8 hides: y
-// (54.9 against 56.9 us for 8 images of 127 x 129 x 320, whose second pass the special function unit bounds) and the split form's
-// dx.  The fast reciprocal flushes what is below 2^-126: y is 0 from z = -87.3 on, where it is 1e-36 at most.
-enum { kFast, kSums, kExact };
-template <int KIND>
-__device__ __forceinline__ float sigmoid(float z) {
-  if constexpr (KIND == kExact) return 1.f / (1.f + expf(-z));
-  float e, r;
-  if constexpr (KIND == kSums) e = expf(-z);
-  else asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.44269504f));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
-  return r;
-}
-
-// act(z).
-template <int KIND, int ACT>
-__device__ __forceinline__ float activate(float z) {
-  if constexpr (ACT == LSGD_ACT_RELU) {
-    float r;
-    asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(z));
-    return r;
-  }
-  if constexpr (ACT == LSGD_ACT_SILU) return z * sigmoid<KIND>(z);
-  return z;
-}
-// f with the activation as a constant.
-template <typename F>
-__device__ __forceinline__ void with_act(int act, F f) {
-  if (act == LSGD_ACT_RELU) f(std::integral_constant<int, LSGD_ACT_RELU>{});
-  else if (act == LSGD_ACT_SILU) f(std::integral_constant<int, LSGD_ACT_SILU>{});
-  else f(std::integral_constant<int, LSGD_ACT_NONE>{});
-}
 
 constexpr long long kWaitCycles = 4000000000LL;  // ~2 s at 2 GHz
 
@@ -201,10 +85,6 @@ __device__ __forceinline__ void chan(float& n, float& m, float& q, float nb, flo
   q += fmaf(d * d, n * w, qb);
   n = t;
 }
-
-// How many of a thread's k positions are added up at a time: the sums of these segments are added in turn, so that no chain of
-// additions is longer than the root of k or 64.  (fp32 sums of 2048 equal values in a row are up to 1.7e-5 off, of 16384 1.6e-4.)
-__device__ __forceinline__ int segment(int k) { return max(64, ((int)sqrtf((float)k) + 7) / 8 * 8); }
 
 // Per range and channel: forward (mean, sum of squared deviations), backward (sum dz, sum dz xh).
 template <typename XT, typename YT, int V, bool BWD>
@@ -1516,44 +1396,6 @@ const char* gn_shape_error(int G, int B, int64_t P, int C, int groups) {
   return nullptr;
 }
 
-// `count` blocks of `bytes` from p, `stride` floats from one to the next; at NULL: nothing.  (A workspace that is not used, of no
-// bytes, counts by its address.)
-struct GnBlocks {
-  uintptr_t first, end;  // of all of them
-  size_t bytes;
-  int64_t stride;
-  int count;
-  GnBlocks(const void* p, size_t n, int64_t gs = 0, int blocks = 1)
-      : first(reinterpret_cast<uintptr_t>(p)), bytes(n), stride(gs), count(blocks) {
-    uint64_t span;  // (a stride may be any number: up to the last address then)
-    if (__builtin_mul_overflow((uint64_t)(blocks - 1), (uint64_t)gs, &span) || span > UINTPTR_MAX / 8) end = UINTPTR_MAX;
-    else end = first + 4 * span + n;
-    if (!p) end = 0;
-  }
-};
-// Whether any two blocks of a and b share a byte.  Where both are several, their strides are the same.
-bool gn_meet(const GnBlocks& a, const GnBlocks& b) {
-  if (a.first >= b.end || b.first >= a.end) return false;
-  if (a.count == 1 && b.count == 1) return true;
-  // block j of b lies d + t stride behind block i of a, t = j - i
-  using wide = __int128;
-  const wide d = (wide)b.first - (wide)a.first, stride = 4 * (wide)(a.count > 1 ? a.stride : b.stride), na = a.bytes, nb = b.bytes;
-  const wide t = std::max<wide>(1 - a.count, (-nb - d >= 0 ? (-nb - d) / stride : -((nb + d + stride - 1) / stride)) + 1);
-  return t <= b.count - 1 && d + t * stride < na;  // (t: the first that does not end before a's block)
-}
-// Whether anything written meets anything else of the call.
-template <int W, int R>
-bool gn_overlap(const GnBlocks (&written)[W], const GnBlocks (&read)[R]) {
-  for (int i = 0; i < W; ++i) {
-    for (int j = i + 1; j < W; ++j)
-      if (gn_meet(written[i], written[j])) return true;
-    for (int j = 0; j < R; ++j)
-      if (gn_meet(written[i], read[j])) return true;
-  }
-  return false;
-}
-
-bool gn_bad_align(const void* p, int z) { return reinterpret_cast<uintptr_t>(p) % z != 0; }
 
 }  // namespace
 
@@ -1596,19 +1438,19 @@ lsgd_status lsgd_groupnorm_forward(const void* x, int x_type, const float* gamma
   if (bad) return gn_error(LSGD_EINVAL, fn, bad);
   const int64_t N = (int64_t)G * B;
   const size_t n = (size_t)N * P * C, ns = (size_t)N * groups * 4, need = gn_workspace(N, (int)P, C, groups, false);
-  const auto params = [&](const float* p) { return GnBlocks(p, 4 * (size_t)C, par_gs, G); };
+  const auto params = [&](const float* p) { return Blocks(p, 4 * (size_t)C, par_gs, G); };
   if (!x || !gamma || !beta || !y || !mean || !rstd) bad = "a pointer is NULL";
   else if ((!xb && x_type != LSGD_FP32) || (!yb && y_type != LSGD_FP32)) bad = "types are LSGD_FP32 or LSGD_BF16";
   else if (act != LSGD_ACT_NONE && act != LSGD_ACT_RELU && act != LSGD_ACT_SILU) bad = "unknown activation";
   else if (!(eps > 0.f) || !(eps < 1e30f)) bad = "eps must be positive and finite";
   else if (par_gs < C) bad = "par_gs must be at least C";
-  else if (gn_bad_align(x, xz) || gn_bad_align(y, yz) || gn_bad_align(gamma, 4) || gn_bad_align(beta, 4) ||
-           gn_bad_align(mean, 4) || gn_bad_align(rstd, 4))
+  else if (misaligned(x, xz) || misaligned(y, yz) || misaligned(gamma, 4) || misaligned(beta, 4) ||
+           misaligned(mean, 4) || misaligned(rstd, 4))
     bad = "a pointer is not aligned to its element";
-  else if (need && (!workspace || workspace_bytes < need || gn_bad_align(workspace, 16)))
+  else if (need && (!workspace || workspace_bytes < need || misaligned(workspace, 16)))
     bad = "workspace NULL, not 16-byte aligned or smaller than lsgd_groupnorm_workspace says";
-  else if (gn_overlap({GnBlocks(y, n * yz), GnBlocks(mean, ns), GnBlocks(rstd, ns), GnBlocks(workspace, need)},
-                      {GnBlocks(x, n * xz), params(gamma), params(beta)}))
+  else if (any_overlap({Blocks(y, n * yz), Blocks(mean, ns), Blocks(rstd, ns), Blocks(workspace, need)},
+                      {Blocks(x, n * xz), params(gamma), params(beta)}))
     bad = "tensors overlap";
   if (bad) return gn_error(LSGD_EINVAL, fn, bad);
   if (!g_norm_used) g_norm_used = true;
@@ -1635,22 +1477,22 @@ lsgd_status lsgd_groupnorm_backward(const void* x, int x_type, const void* y, co
   if (bad) return gn_error(LSGD_EINVAL, fn, bad);
   const int64_t N = (int64_t)G * B;
   const size_t n = (size_t)N * P * C, ns = (size_t)N * groups * 4, need = gn_workspace(N, (int)P, C, groups, true);
-  const auto params = [&](const float* p) { return GnBlocks(p, 4 * (size_t)C, par_gs, G); };
+  const auto params = [&](const float* p) { return Blocks(p, 4 * (size_t)C, par_gs, G); };
   const bool relu = act == LSGD_ACT_RELU;
   if (!x || !dy || !gamma || !beta || !mean || !rstd || !dx || !dgamma || !dbeta || (relu && !y))
     bad = "a pointer is NULL (y may be only where the activation is not ReLU)";
   else if ((!xb && x_type != LSGD_FP32) || (!yb && y_type != LSGD_FP32)) bad = "types are LSGD_FP32 or LSGD_BF16";
   else if (act != LSGD_ACT_NONE && !relu && act != LSGD_ACT_SILU) bad = "unknown activation";
   else if (par_gs < C) bad = "par_gs must be at least C";
-  else if (gn_bad_align(x, xz) || gn_bad_align(dx, xz) || gn_bad_align(dy, yz) || (relu && gn_bad_align(y, yz)) ||
-           gn_bad_align(gamma, 4) || gn_bad_align(beta, 4) || gn_bad_align(mean, 4) || gn_bad_align(rstd, 4) ||
-           gn_bad_align(dgamma, 4) || gn_bad_align(dbeta, 4))
+  else if (misaligned(x, xz) || misaligned(dx, xz) || misaligned(dy, yz) || (relu && misaligned(y, yz)) ||
+           misaligned(gamma, 4) || misaligned(beta, 4) || misaligned(mean, 4) || misaligned(rstd, 4) ||
+           misaligned(dgamma, 4) || misaligned(dbeta, 4))
     bad = "a pointer is not aligned to its element";
-  else if (!workspace || workspace_bytes < need || gn_bad_align(workspace, 16))
+  else if (!workspace || workspace_bytes < need || misaligned(workspace, 16))
     bad = "workspace NULL, not 16-byte aligned or smaller than lsgd_groupnorm_workspace says";
-  else if (gn_overlap({GnBlocks(dx, n * xz), params(dgamma), params(dbeta), GnBlocks(workspace, need)},
-                      {GnBlocks(x, n * xz), GnBlocks(dy, n * yz), GnBlocks(relu ? y : nullptr, n * yz), params(gamma),
-                       params(beta), GnBlocks(mean, ns), GnBlocks(rstd, ns)}))
+  else if (any_overlap({Blocks(dx, n * xz), params(dgamma), params(dbeta), Blocks(workspace, need)},
+                      {Blocks(x, n * xz), Blocks(dy, n * yz), Blocks(relu ? y : nullptr, n * yz), params(gamma),
+                       params(beta), Blocks(mean, ns), Blocks(rstd, ns)}))
     bad = "tensors overlap";
   if (bad) return gn_error(LSGD_EINVAL, fn, bad);
   if (!g_norm_used) g_norm_used = true;
