@@ -522,8 +522,8 @@ lsgd_status lsgd_groupnorm_backward(const void* x, int x_type, const void* y, co
  * the mean; a row whose squared deviations pass fp32's range (values of 1e19 and more) gets rstd = 0.  Deterministic.  A NaN or
  * infinite value makes its own row NaN and no other.
  *
- * No workspace, no allocation: the call may be captured into a CUDA graph.  G <= 65535, 1 <= C <= 65536, R >= 0 (0: nothing is
- * done), G R <= 2^40; any C, strides >= C and any alignment of at least the element's (vectors of up to 16 bytes are used where
+ * No workspace, no allocation: the call may be captured into a CUDA graph.  G <= 65535, 1 <= C <= 32768, R >= 0 (0: nothing is
+ * done), G R <= 2^36; any C, strides >= C and any alignment of at least the element's (vectors of up to 16 bytes are used where
  * strides and pointers allow).  LSGD_EINVAL on anything else and where what is written overlaps any other tensor (rows
  * count from the first row's first to the last row's last value).  Device pointers, asynchronous on `stream`, which belongs
  * to the current device. */

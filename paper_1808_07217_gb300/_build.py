@@ -14,7 +14,7 @@ LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "liblsgd.so")
 SOURCES = ["kernels.cu", "gemm_simt.cu", "conv_simt.cu", "gemm_tc.cu", "head.cu", "resnet.cu", "runtime.cu",
            "bn_noalloc.cu", "groupnorm.cu", "orthogonal.cu", "layernorm.cu",
-           "gradnorm.cu"]
+           "layernorm_backward_none.cu", "layernorm_backward_relu.cu", "layernorm_backward_silu.cu", "gradnorm.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2"]
 

@@ -1,0 +1,7 @@
+#include "layernorm_backward.cuh"
+
+namespace lsgd {
+cudaError_t launch_ln_backward_none(const LnArgs& a, int G, bool xb, bool yb, int vmax, cudaStream_t st) {
+  return ln_backward_any<LSGD_ACT_NONE>(a, G, xb, yb, vmax, st);
+}
+}  // namespace lsgd

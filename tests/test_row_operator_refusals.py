@@ -47,7 +47,7 @@ def _rows(L, fn, G=3, R=50, C=40, x_ld=48, y_ld=44, par_gs=64, x_type=1, y_type=
 
 
 @pytest.mark.parametrize("fn", ["forward", "backward"])
-@pytest.mark.parametrize("bad", [dict(G=0), dict(G=65536), dict(R=-1), dict(C=0), dict(C=65537, x_ld=65537, y_ld=65537, par_gs=65537),
+@pytest.mark.parametrize("bad", [dict(G=0), dict(G=65536), dict(R=-1), dict(C=0), dict(C=32769, x_ld=32769, y_ld=32769, par_gs=32769),
                                  dict(x_ld=39), dict(y_ld=39), dict(par_gs=39), dict(x_type=2), dict(y_type=-1), dict(act=3),
                                  dict(x=1), dict(x=0), dict(gamma=0), dict(beta=2), dict(mean=0), dict(rstd=6), dict(y=0), dict(y=2),
                                  dict(x_ld=1 << 59), dict(R=1 << 40)])
