@@ -8,12 +8,15 @@
 // worker: where the tensors begin is found in a table that comes with the launch, so that hundreds of small tensors cost one
 // launch and keep every SM busy.  A warp has a whole piece's loads under way at once.
 //
-// Sums.  A lane's squares of a piece (at most 64) are added in fp32, these sums in 64 bits and in a fixed order.  Where a
-// lane's fp32 sum is too large or too small for fp32's range its values are squared and added in 64 bits, whose range holds the
-// square of any fp32 value: no finite gradient overflows, none vanishes.
+// Sums.  A warp's squares of a piece (at most 66 to a lane, then pairs of lanes) are added in fp32, the pieces' sums in 64 bits, all in
+// a fixed order.  Where a piece's fp32 sum is too large or too small for fp32's range its values are squared and added in 64
+// bits, whose range holds the square of any fp32 value: no finite gradient overflows, none vanishes.  An SM does two 64-bit
+// operations a cycle, a warp's one in 16: they are kept to one lane of a warp and one warp of a CTA (with every thread of 32 warps
+// adding their sums up and taking the root, ResNet-20's 16 norms took 34 us).
 #include <algorithm>
 #include <new>
 #include <string>
+#include <type_traits>
 #include <vector>
 
 #include "../../include/lsgd.h"
@@ -22,12 +25,14 @@
 #include "operands.h"
 
 struct lsgd_tensors {
-  std::vector<lsgd_tensor> list;     // without the empty ones
+  std::vector<lsgd_tensor> list;     // without the empty ones, those of the same types together
   std::vector<uint32_t> first;       // first piece of each, and their number
+  std::vector<size_t> launches;      // first tensor of each launch (of tensors of the same types), and their number
   int G = 0, piece = 0;              // workers; bytes of a piece
   bool places = false;               // every tensor has an `out`
   bool overlap = false;              // what a clipping would write overlaps something
   int blocks = 0;                    // CTAs of a worker in the passes
+  int cluster = 0;                   // CTAs of a worker where one launch does all (0: two)
   uintptr_t lo = UINTPTR_MAX, hi = 0;  // all that is read or written lies between
 };
 
@@ -36,42 +41,45 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxPiece = 4096, kMinPiece = 512;
+constexpr int64_t kShare = 160 << 10, kMinShare = 32 << 10;  // bytes of a worker's gradient to a CTA of a cluster
 
 struct Entry {
   const void* in;
   void* out;
   int64_t n, gs, out_gs;
-  uint32_t first;
-  uint16_t bf16, out_bf16;
 };
-// The tensors of a launch.  A launch's parameters hold up to 32,764 bytes: longer lists take several launches.
+// The tensors of a launch, all of one type and clipped to one type.  A launch's parameters hold up to 32,764 bytes: longer lists take several launches.  (They are read through
+// the constant caches, where a miss costs as much as one of memory: the first pieces, which are searched, stand close together.)
 template <int MAX>
 struct Table {
   int count, shift;       // tensors; log2 of a piece's bytes
   uint32_t begin, end;    // the launch's pieces
+  uint32_t first[MAX];    // of each tensor
   Entry e[MAX];
 };
 constexpr int kFew = 64, kMany = 640;
+static_assert(sizeof(Table<kMany>) <= 32000, "a launch's parameters");
 
 // The piece's tensor: the last whose first piece is at most p, from tensor t on.
 template <int MAX>
 __device__ __forceinline__ int find(const Table<MAX>& tab, int t, uint32_t p) {
-  if (t + 1 >= tab.count || p < tab.e[t + 1].first) return t;
-  int lo = t + 1, hi = tab.count;  // e[lo].first <= p
+  if (t + 1 >= tab.count || p < tab.first[t + 1]) return t;
+  int lo = t + 1, hi = tab.count;  // first[lo] <= p
   while (hi - lo > 1) {
     const int mid = (lo + hi) / 2;
-    if (tab.e[mid].first <= p) lo = mid;
+    if (tab.first[mid] <= p) lo = mid;
     else hi = mid;
   }
   return lo;
 }
 
+template <bool BF16>
 struct Range {  // a piece's values
   const uint8_t* p;
   int len, head, nv;  // values; those before the first 16-byte boundary; whole vectors behind them
-  __device__ __forceinline__ Range(const Entry& e, int shift, int64_t worker, uint32_t piece) {
-    const int zs = e.bf16 ? 1 : 2;  // log2 of a value's bytes
-    const int64_t at = (int64_t)(piece - e.first) << (shift - zs);
+  __device__ __forceinline__ Range(const Entry& e, int shift, int64_t worker, uint32_t piece) {  // piece: of the tensor's
+    constexpr int zs = BF16 ? 1 : 2;  // log2 of a value's bytes
+    const int64_t at = (int64_t)piece << (shift - zs);
     p = static_cast<const uint8_t*>(e.in) + ((worker * e.gs + at) << zs);
     len = (int)min((int64_t)1 << (shift - zs), e.n - at);
     head = min(len, (int)((0u - (uint32_t)reinterpret_cast<uintptr_t>(p)) & 15u) >> zs);
@@ -83,10 +91,10 @@ __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w <<
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 // f(value) for every value of a vector.
-template <typename F>
-__device__ __forceinline__ void each(const uint4& r, bool bf16, F f) {
+template <bool BF16, typename F>
+__device__ __forceinline__ void each(const uint4& r, F f) {
   const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-  if (bf16) {
+  if constexpr (BF16) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) f(bf_lo(w[i])), f(bf_hi(w[i]));
   } else {
@@ -97,17 +105,23 @@ __device__ __forceinline__ void each(const uint4& r, bool bf16, F f) {
 
 constexpr int kVecs = kMaxPiece / 16 / 32;  // vectors of a lane
 
-// The sum of squares of this lane's values of a piece.
-__device__ __forceinline__ double piece_squares(const Range& r, bool bf16, int lane) {
-  const uint4* v = reinterpret_cast<const uint4*>(r.p + r.head * (bf16 ? 2 : 4));
+__device__ __forceinline__ double warp_sum(double v) {
+  for (int d = 16; d; d /= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
+  return v;
+}
+
+// The sum of squares of a piece, in lane 0.
+template <bool BF16>
+__device__ __forceinline__ double piece_squares(const Range<BF16>& r, int lane) {
+  const uint4* v = reinterpret_cast<const uint4*>(r.p + r.head * (BF16 ? 2 : 4));
   uint4 raw[kVecs];
 #pragma unroll
   for (int i = 0; i < kVecs; ++i)
     raw[i] = lane + 32 * i < r.nv ? __ldg(v + lane + 32 * i) : make_uint4(0, 0, 0, 0);
   // the values before and behind the vectors: at most 7 each
-  const int tail = r.head + r.nv * (bf16 ? 8 : 4) + lane;
+  const int tail = r.head + r.nv * (BF16 ? 8 : 4) + lane;
   uint32_t h = 0, t = 0;
-  if (bf16) {
+  if constexpr (BF16) {
     if (lane < r.head) h = (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(r.p) + lane) << 16;
     if (tail < r.len) t = (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(r.p) + tail) << 16;
   } else {
@@ -117,13 +131,15 @@ __device__ __forceinline__ double piece_squares(const Range& r, bool bf16, int l
   const float hf = __uint_as_float(h), tf = __uint_as_float(t);
   float s = fmaf(hf, hf, tf * tf);
 #pragma unroll
-  for (int i = 0; i < kVecs; ++i) each(raw[i], bf16, [&](float x) { s = fmaf(x, x, s); });
-  // (a value whose square lost bits below 2^-149 is at most 2^-49 of a sum of 2^-100)
+  for (int i = 0; i < kVecs; ++i) each<BF16>(raw[i], [&](float x) { s = fmaf(x, x, s); });
+#pragma unroll
+  for (int d = 16; d; d /= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
+  // (the same sum in every lane: a + b is b + a.  A value whose square lost bits below 2^-149 is at most 2^-49 of a sum of 2^-100.)
   if (s >= 0x1p-100f && s < 0x1p126f) return s;
   uint32_t any = (h | t) & 0x7fffffffu;
 #pragma unroll
-  for (int i = 0; i < kVecs; ++i) any |= (raw[i].x | raw[i].y | raw[i].z | raw[i].w) & (bf16 ? 0x7fff7fffu : 0x7fffffffu);
-  if (!any) return 0.0;
+  for (int i = 0; i < kVecs; ++i) any |= (raw[i].x | raw[i].y | raw[i].z | raw[i].w) & (BF16 ? 0x7fff7fffu : 0x7fffffffu);
+  if (!__any_sync(0xffffffffu, any)) return 0.0;
   double d = (double)hf * hf + (double)tf * tf;
 #pragma unroll 1
   for (int i = 0; i < kVecs; ++i) {
@@ -131,116 +147,225 @@ __device__ __forceinline__ double piece_squares(const Range& r, bool bf16, int l
 #pragma unroll
     for (int j = 1; j < kVecs; ++j)
       if (j == i) w = raw[j];
-    each(w, bf16, [&](float x) {
+    each<BF16>(w, [&](float x) {
       if (x != 0.f) d += (double)x * x;
     });
   }
-  return d;
+  return warp_sum(d);
 }
 
-__device__ __forceinline__ double warp_sum(double v) {
-  for (int d = 16; d; d /= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
-  return v;
-}
-__device__ __forceinline__ double block_sum(double v) {  // in every thread
-  __shared__ double part[kWarps];
-  v = warp_sum(v);
+// The warps' sums (in lane 0 of each), added by the first warp: in thread 0.
+template <int THREADS>
+__device__ __forceinline__ double block_sum(double v) {
+  __shared__ double part[THREADS / 32];
   if ((threadIdx.x & 31) == 0) part[threadIdx.x / 32] = v;
   __syncthreads();
-  v = 0.0;
-  for (int i = 0; i < kWarps; ++i) v += part[i];
-  return v;
+  if (threadIdx.x >= 32) return 0.0;
+  return warp_sum(threadIdx.x < THREADS / 32 ? part[threadIdx.x] : 0.0);
+}
+// The root of a sum of squares, to fp32: by the fp32 root where the sum is in its range.
+__device__ __forceinline__ float root(double s) {
+  if (s >= 0x1p-100 && s < 0x1p120) return __fsqrt_rn((float)s);
+  return (float)sqrt(s);
+}
+
+// The sum of squares of every `stride`-th piece of a worker from p on, in lane 0.
+template <bool BF16, int MAX>
+__device__ __forceinline__ double squares_of(const Table<MAX>& tab, int64_t worker, uint64_t p, uint32_t stride) {
+  double s = 0.0;
+  int t = 0;
+  for (; p < tab.end; p += stride) {
+    t = find(tab, t, (uint32_t)p);
+    const double q = piece_squares(Range<BF16>(tab.e[t], tab.shift, worker, (uint32_t)p - tab.first[t]), threadIdx.x & 31);
+    if ((threadIdx.x & 31) == 0) s += q;
+  }
+  return s;
 }
 
 // One sum for each CTA into part [G][slots] from slot `slot` on, or, with `norm`, the norm of its worker.
-template <int MAX>
+template <int MAX, bool BF16>
 __global__ void __launch_bounds__(kThreads, 4) grad_squares_kernel(const __grid_constant__ Table<MAX> tab, double* part, int slot,
                                                                    int slots, float* norm) {
   pdl_begin();
-  const int lane = threadIdx.x & 31;
-  const uint32_t stride = gridDim.x * kWarps;
-  double s = 0.0;
-  int t = 0;
-  for (uint64_t p = tab.begin + blockIdx.x * kWarps + threadIdx.x / 32; p < tab.end; p += stride) {
-    t = find(tab, t, (uint32_t)p);
-    const Entry& e = tab.e[t];
-    s += piece_squares(Range(e, tab.shift, blockIdx.y, (uint32_t)p), e.bf16, lane);
-  }
-  s = block_sum(s);
+  const double s = block_sum<kThreads>(squares_of<BF16>(tab, blockIdx.y, tab.begin + blockIdx.x * kWarps + threadIdx.x / 32,
+                                                  gridDim.x * kWarps));
   if (threadIdx.x) return;
-  if (norm) norm[blockIdx.y] = (float)sqrt(s);
+  if (norm) norm[blockIdx.y] = root(s);
   else part[(int64_t)blockIdx.y * slots + slot + blockIdx.x] = s;
 }
 
+// A worker's norm from its CTAs' sums, in thread 0.
+__device__ __forceinline__ float norm_of_parts(const double* part, int slots, int worker) {
+  double s = 0.0;
+  for (int i = threadIdx.x; i < slots; i += kThreads) s += part[(int64_t)worker * slots + i];
+  s = block_sum<kThreads>(warp_sum(s));
+  return threadIdx.x ? 0.f : root(s);
+}
 __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const double* part, int slots, float* norm) {
   pdl_begin();
-  double s = 0.0;
-  for (int i = threadIdx.x; i < slots; i += kThreads) s += part[(int64_t)blockIdx.x * slots + i];
-  s = block_sum(s);
-  if (threadIdx.x == 0) norm[blockIdx.x] = (float)sqrt(s);
+  const float n = norm_of_parts(part, slots, blockIdx.x);
+  if (threadIdx.x == 0) norm[blockIdx.x] = n;
 }
 
 // min(1, max_norm / norm): NaN for a NaN norm, 0 for an infinite one.
 __device__ __forceinline__ float clip_factor(float norm, float max_norm) { return norm <= max_norm ? 1.f : __fdiv_rn(max_norm, norm); }
 
-__device__ __forceinline__ void put(void* out, int64_t i, bool bf16, float v) {
-  if (bf16) static_cast<uint16_t*>(out)[i] = f2bf(v);
-  else static_cast<float*>(out)[i] = v;
+// The 16 bytes that begin `shift` (an even number, below 16) bytes behind a's first, of a and what follows it, b.
+__device__ __forceinline__ uint4 funnel(const uint4& a, const uint4& b, int shift) {
+  uint32_t w[5];
+  const int words = shift >> 2;
+  if (words == 0) w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x;
+  else if (words == 1) w[0] = a.y, w[1] = a.z, w[2] = a.w, w[3] = b.x, w[4] = b.y;
+  else if (words == 2) w[0] = a.z, w[1] = a.w, w[2] = b.x, w[3] = b.y, w[4] = b.z;
+  else w[0] = a.w, w[1] = b.x, w[2] = b.y, w[3] = b.z, w[4] = b.w;
+  if (shift & 2) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __byte_perm(w[i], w[i + 1], 0x5432);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-template <int MAX>
-__global__ void __launch_bounds__(kThreads, 4) grad_scale_kernel(const __grid_constant__ Table<MAX> tab, const float* norm,
-                                                                 float max_norm) {
-  pdl_begin();
-  const int lane = threadIdx.x & 31;
-  const uint32_t stride = gridDim.x * kWarps;
-  const float f = clip_factor(norm[blockIdx.y], max_norm);
-  int t = 0;
-  for (uint64_t p = tab.begin + blockIdx.x * kWarps + threadIdx.x / 32; p < tab.end; p += stride) {
-    t = find(tab, t, (uint32_t)p);
-    const Entry& e = tab.e[t];
-    if (f == 1.f && e.out == e.in) continue;
-    const bool bf16 = e.bf16, ob = e.out_bf16;
-    const Range r(e, tab.shift, blockIdx.y, (uint32_t)p);
-    const int64_t at = blockIdx.y * e.out_gs + ((int64_t)((uint32_t)p - e.first) << (tab.shift - (bf16 ? 1 : 2)));
-    void* out = static_cast<uint8_t*>(e.out) + at * (ob ? 2 : 4);
-    const auto value = [&](int i) {
-      return bf16 ? bf2f(reinterpret_cast<const uint16_t*>(r.p)[i]) : reinterpret_cast<const float*>(r.p)[i];
-    };
-    const int width = bf16 ? 8 : 4;                            // values of a vector
-    const int bytes = min(16, width * (ob ? 2 : 4));           // of one store
-    uint8_t* to = static_cast<uint8_t*>(out) + r.head * (ob ? 2 : 4);
-    if (reinterpret_cast<uintptr_t>(to) % bytes) {
-      // what is read and what is written are never aligned together: value by value
-#pragma unroll 4
-      for (int i = lane; i < r.len; i += 32) put(out, i, ob, value(i) * f);
-      continue;
-    }
-    const uint4* v = reinterpret_cast<const uint4*>(r.p + r.head * (bf16 ? 2 : 4));
-    uint4 raw[kVecs];
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i)
-      if (lane + 32 * i < r.nv) raw[i] = v[lane + 32 * i];
-    const int tail = r.head + r.nv * width + lane;
-    if (lane < r.head) put(out, lane, ob, value(lane) * f);
-    if (tail < r.len) put(out, tail, ob, value(tail) * f);
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i)
-      if (lane + 32 * i < r.nv) {
-        float x[8];
-        int k = 0;
-        each(raw[i], bf16, [&](float q) { x[k++] = q * f; });
-        const int64_t j = lane + 32 * i;
-        const auto pair = [&](int q) { return (uint32_t)f2bf(x[q]) | (uint32_t)f2bf(x[q + 1]) << 16; };
-        if (ob && bf16) reinterpret_cast<uint4*>(to)[j] = make_uint4(pair(0), pair(2), pair(4), pair(6));
-        else if (ob) reinterpret_cast<uint2*>(to)[j] = make_uint2(pair(0), pair(2));
-        else {
-          float4* q = reinterpret_cast<float4*>(to) + (bf16 ? 2 * j : j);
-          q[0] = make_float4(x[0], x[1], x[2], x[3]);
-          if (bf16) q[1] = make_float4(x[4], x[5], x[6], x[7]);
-        }
-      }
+// 16 bytes of values times f to `to`, in 8, 16 or 32 bytes.
+template <bool BF16, bool OB>
+__device__ __forceinline__ void scale_vector(const uint4& r, void* to, float f) {
+  float x[8];
+  int k = 0;
+  each<BF16>(r, [&](float q) { x[k++] = q * f; });
+  const auto pair = [&](int q) { return (uint32_t)f2bf(x[q]) | (uint32_t)f2bf(x[q + 1]) << 16; };
+  if constexpr (OB && BF16) {
+    __stcs(static_cast<uint4*>(to), make_uint4(pair(0), pair(2), pair(4), pair(6)));
+  } else if constexpr (OB) {
+    __stcs(static_cast<uint2*>(to), make_uint2(pair(0), pair(2)));
+  } else {
+    __stcs(static_cast<float4*>(to), make_float4(x[0], x[1], x[2], x[3]));
+    if (BF16) __stcs(static_cast<float4*>(to) + 1, make_float4(x[4], x[5], x[6], x[7]));
   }
+}
+
+// A piece's values times f to its place, by a warp.  (Stores that leave L2 to the gradients that are still to be read.)
+template <bool BF16, bool OB>
+__device__ __forceinline__ void scale_piece(const Range<BF16>& r, uint8_t* out, float f) {
+  const int lane = threadIdx.x & 31;
+  constexpr int z = BF16 ? 2 : 4, oz = OB ? 2 : 4, width = 16 / z;  // bytes of a value; values of 16 bytes
+  const auto one = [&](int i) {
+    const float v = BF16 ? bf2f(reinterpret_cast<const uint16_t*>(r.p)[i]) : reinterpret_cast<const float*>(r.p)[i];
+    if constexpr (OB) reinterpret_cast<uint16_t*>(out)[i] = f2bf(v * f);
+    else reinterpret_cast<float*>(out)[i] = v * f;
+  };
+  constexpr int align = width * oz < 16 ? width * oz : 16;  // of a store
+  if ((reinterpret_cast<uintptr_t>(out) + r.head * oz) % align == 0) {
+    const uint4* v = reinterpret_cast<const uint4*>(r.p + r.head * z);
+    const int tail = r.head + r.nv * width + lane;
+#pragma unroll 1
+    for (int i = lane; i < r.nv; i += 128) {
+      uint4 raw[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (i + 32 * j < r.nv) raw[j] = v[i + 32 * j];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (i + 32 * j < r.nv) scale_vector<BF16, OB>(raw[j], out + (r.head + (i + 32 * j) * width) * oz, f);
+    }
+    if (lane < r.head) one(lane);
+    if (tail < r.len) one(tail);
+    return;
+  }
+  // What is read and what is written are not aligned together: every store's values from two aligned loads, as far as these lie within
+  // the piece; the values before and behind them (at most 15 each) one by one.
+  int first = (int)((0u - (uint32_t)reinterpret_cast<uintptr_t>(out)) & (align - 1)) / oz;
+  const uintptr_t p = reinterpret_cast<uintptr_t>(r.p);
+  if (((p + first * z) & ~(uintptr_t)15) < p) first += width;
+  const uintptr_t base = (p + first * z) & ~(uintptr_t)15, end = p + r.len * z;
+  const int by = (int)(p + first * z - base), nv = end >= base + 16 ? (int)((end - base - 16) / 16) : 0;
+  first = min(first, r.len);
+  const int rest = nv ? first + nv * width : first;
+  const uint4* v = reinterpret_cast<const uint4*>(base);
+#pragma unroll 1
+  for (int i = lane; i < nv; i += 64) {
+    uint4 a[2], b[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (i + 32 * j < nv) a[j] = v[i + 32 * j], b[j] = v[i + 32 * j + 1];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (i + 32 * j < nv) scale_vector<BF16, OB>(funnel(a[j], b[j], by), out + (first + (i + 32 * j) * width) * oz, f);
+  }
+  if (lane < first) one(lane);
+  for (int i = rest + lane; i < r.len; i += 32) one(i);
+}
+// Every `stride`-th piece of a worker, times f, from the last to the first: L2 still holds what was read last.
+template <bool BF16, bool OB, int MAX>
+__device__ __forceinline__ void scale_pieces(const Table<MAX>& tab, int64_t worker, uint32_t p, uint32_t stride, float f) {
+  if (p >= tab.end) return;
+  for (p += (tab.end - 1 - p) / stride * stride;; p -= stride) {
+    const int t = find(tab, 0, p);
+    const Entry& e = tab.e[t];
+    if (f != 1.f || e.out != e.in) {
+      const uint32_t piece = p - tab.first[t];
+      const int64_t at = worker * e.out_gs + ((int64_t)piece << (tab.shift - (BF16 ? 1 : 2)));
+      scale_piece<BF16, OB>(Range<BF16>(e, tab.shift, worker, piece), static_cast<uint8_t*>(e.out) + at * (OB ? 2 : 4), f);
+    }
+    if (p < tab.begin + stride) return;
+  }
+}
+
+// The second of two launches: every CTA adds its worker's sums up by itself.
+template <int MAX, bool BF16, bool OB>
+__global__ void __launch_bounds__(kThreads, 4) grad_scale_kernel(const __grid_constant__ Table<MAX> tab, const double* part, int slots,
+                                                                 float* norm, float max_norm) {
+  pdl_begin();
+  __shared__ float shared;
+  float n;
+  if (slots > 1) {
+    n = norm_of_parts(part, slots, blockIdx.y);
+    if (threadIdx.x == 0) {
+      shared = n;
+      if (blockIdx.x == 0) norm[blockIdx.y] = n;
+    }
+    __syncthreads();
+    n = shared;
+  } else {
+    n = norm[blockIdx.y];  // (a worker's only CTA has written it in the first launch)
+  }
+  scale_pieces<BF16, OB>(tab, blockIdx.y, tab.begin + blockIdx.x * kWarps + threadIdx.x / 32, gridDim.x * kWarps, clip_factor(n, max_norm));
+}
+
+// Both in one launch, a worker to a cluster: the CTAs' sums meet in shared memory.
+constexpr int kClusterThreads = 1024, kMaxCluster = 8;
+
+template <int MAX, bool BF16, bool CLIP, bool OB>
+__global__ void __launch_bounds__(kClusterThreads) grad_cluster_kernel(const __grid_constant__ Table<MAX> tab, float* norm,
+                                                                          float max_norm) {
+  __shared__ double sums[kMaxCluster];
+  const uint32_t cl = gridDim.x;  // a cluster is a row of the grid
+  pdl_begin();
+  const uint32_t p = tab.begin + blockIdx.x * (kClusterThreads / 32) + threadIdx.x / 32, stride = cl * (kClusterThreads / 32);
+  double s = block_sum<kClusterThreads>(squares_of<BF16>(tab, blockIdx.y, p, stride));
+  if (cl > 1) {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // every CTA's shared memory is there
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (threadIdx.x == 0)
+      for (uint32_t i = 0; i < cl; ++i) {
+        uint32_t to;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(&sums[blockIdx.x])), "r"(i));
+        asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to), "d"(s) : "memory");
+      }
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+  __shared__ float shared;
+  if (threadIdx.x == 0) {
+    if (cl > 1) {
+      s = 0.0;
+      for (uint32_t i = 0; i < cl; ++i) s += sums[i];
+    }
+    shared = root(s);
+    if (blockIdx.x == 0) norm[blockIdx.y] = shared;
+  }
+  if constexpr (!CLIP) return;
+  __syncthreads();
+  const float n = shared;
+  if constexpr (CLIP) scale_pieces<BF16, OB>(tab, blockIdx.y, p, stride, clip_factor(n, max_norm));
 }
 
 // ---- the local update with the clipped gradient ----
@@ -272,7 +397,8 @@ __global__ void __launch_bounds__(256) clipped_update_kernel(const UpdateArgs a)
   int64_t done = 0;
   if constexpr (WIDE) {
     const int64_t n4 = a.n / 4;
-    for (int64_t i = first; i < n4; i += stride) {
+    for (int64_t j = first; j < n4; j += stride) {
+      const int64_t i = n4 - 1 - j;  // from the end on: L2 still holds what the norm read last
       float gv[4], wv[4], uv[4];
       if constexpr (GB) {
         const uint2 r = __ldcs(reinterpret_cast<const uint2*>(gb) + i);
@@ -283,8 +409,8 @@ __global__ void __launch_bounds__(256) clipped_update_kernel(const UpdateArgs a)
       *reinterpret_cast<float4*>(wv) = __ldcs(reinterpret_cast<const float4*>(w) + i);
       if (MOM) *reinterpret_cast<float4*>(uv) = __ldcs(reinterpret_cast<const float4*>(u) + i);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        sgd_elem<MOM, NEST>(wv[j], uv[j], f * gv[j], a.lr, a.m, 4 * i + j < a.decay_end ? a.wd : 0.f);
+      for (int k = 0; k < 4; ++k)
+        sgd_elem<MOM, NEST>(wv[k], uv[k], f * gv[k], a.lr, a.m, 4 * i + k < a.decay_end ? a.wd : 0.f);
       if (MOM) __stcs(reinterpret_cast<float4*>(u) + i, *reinterpret_cast<float4*>(uv));
       __stcs(reinterpret_cast<float4*>(w) + i, *reinterpret_cast<float4*>(wv));
       if (SHADOW)
@@ -320,9 +446,8 @@ lsgd_status gr_error(lsgd_status s, const char* fn, const char* what) {
 }
 int size_of(int type) { return type == LSGD_BF16 ? 2 : 4; }
 
-// The number of launches of a list, each of at most kMany tensors.
-int launches(const lsgd_tensors& l) { return (int)((l.list.size() + kMany - 1) / kMany); }
-int slots_of(const lsgd_tensors& l) { return l.blocks * launches(l); }
+int slots_of(const lsgd_tensors& l) { return l.blocks * (int)(l.launches.size() - 1); }
+int out_type(const lsgd_tensor& t, bool places) { return places ? t.out_type : t.g_type; }
 
 template <int MAX>
 void fill(Table<MAX>& tab, const lsgd_tensors& l, size_t from, size_t to) {
@@ -334,40 +459,79 @@ void fill(Table<MAX>& tab, const lsgd_tensors& l, size_t from, size_t to) {
     Entry& e = tab.e[i - from];
     e.in = t.g, e.out = l.places ? t.out : const_cast<void*>(t.g);
     e.n = t.n, e.gs = t.g_gs, e.out_gs = l.places ? t.out_gs : t.g_gs;
-    e.first = l.first[i];
-    e.bf16 = t.g_type == LSGD_BF16, e.out_bf16 = (l.places ? t.out_type : t.g_type) == LSGD_BF16;
+    tab.first[i - from] = l.first[i];
   }
 }
 
-template <int MAX>
-cudaError_t squares(const lsgd_tensors& l, size_t from, size_t to, double* part, int slot, int slots, float* norm, cudaStream_t st) {
-  Table<MAX> tab;
+// f(table, BF16, OB) for the tensors of launch i.
+template <typename F>
+cudaError_t with_table(const lsgd_tensors& l, size_t i, F f) {
+  const size_t from = l.launches[i], to = l.launches[i + 1];
+  const bool bf16 = l.list[from].g_type == LSGD_BF16, ob = out_type(l.list[from], l.places) == LSGD_BF16;
+  const auto typed = [&](const auto& tab) {
+    if (bf16) return ob ? f(tab, std::true_type{}, std::true_type{}) : f(tab, std::true_type{}, std::false_type{});
+    return ob ? f(tab, std::false_type{}, std::true_type{}) : f(tab, std::false_type{}, std::false_type{});
+  };
+  if (to - from <= kFew) {
+    Table<kFew> tab;
+    fill(tab, l, from, to);
+    return typed(tab);
+  }
+  Table<kMany> tab;
   fill(tab, l, from, to);
-  return launch_pdl(grad_squares_kernel<MAX>, dim3(l.blocks, l.G), dim3(kThreads), 0, st, tab, part, slot, slots, norm);
-}
-template <int MAX>
-cudaError_t scale(const lsgd_tensors& l, size_t from, size_t to, const float* norm, float max_norm, cudaStream_t st) {
-  Table<MAX> tab;
-  fill(tab, l, from, to);
-  return launch_pdl(grad_scale_kernel<MAX>, dim3(l.blocks, l.G), dim3(kThreads), 0, st, tab, norm, max_norm);
+  return typed(tab);
 }
 
-cudaError_t norm_of(const lsgd_tensors& l, float* norm, double* part, cudaStream_t st) {
-  const size_t count = l.list.size();
+template <typename K, typename T>
+cudaError_t launch_clusters(K kernel, const lsgd_tensors& l, const T& tab, float* norm, float max_norm, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(l.cluster, l.G);
+  cfg.blockDim = dim3(kClusterThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = l.cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = l.cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, tab, norm, max_norm);
+}
+
+// The norms and, with max_norm > 0, the clipped gradients.
+cudaError_t norm_and_clip(const lsgd_tensors& l, float* norm, float max_norm, double* part, cudaStream_t st) {
+  const size_t n = l.launches.size() - 1;
+  const bool clip = max_norm > 0.f;
+  if (n == 0) return cudaMemsetAsync(norm, 0, sizeof(float) * l.G, st);
+  if (l.cluster)
+    return with_table(l, 0, [&](const auto& tab, auto bf16, auto ob) {
+      constexpr int MAX = sizeof(tab.first) / 4;
+      constexpr bool B = decltype(bf16)::value, O = decltype(ob)::value;
+      return clip ? launch_clusters(grad_cluster_kernel<MAX, B, true, O>, l, tab, norm, max_norm, st)
+                  : launch_clusters(grad_cluster_kernel<MAX, B, false, false>, l, tab, norm, max_norm, st);
+    });
   const int slots = slots_of(l);
-  if (slots == 0) return cudaMemsetAsync(norm, 0, sizeof(float) * l.G, st);
+  const dim3 grid(l.blocks, l.G), block(kThreads);
   cudaError_t e = cudaSuccess;
-  for (size_t i = 0, k = 0; i < count && e == cudaSuccess; i += kMany, ++k) {
-    const size_t to = std::min(count, i + kMany);
-    float* direct = slots == 1 ? norm : nullptr;
-    e = to - i <= kFew ? squares<kFew>(l, i, to, part, (int)k * l.blocks, slots, direct, st)
-                       : squares<kMany>(l, i, to, part, (int)k * l.blocks, slots, direct, st);
+  for (size_t i = 0; i < n && e == cudaSuccess; ++i)
+    e = with_table(l, i, [&](const auto& tab, auto bf16, auto) {
+      return launch_pdl(grad_squares_kernel<sizeof(tab.first) / 4, decltype(bf16)::value>, grid, block, 0, st, tab, part,
+                        (int)i * l.blocks, slots, slots == 1 ? norm : nullptr);
+    });
+  if (!clip) {
+    if (e != cudaSuccess || slots == 1) return e;
+    return launch_pdl(grad_norm_kernel, dim3(l.G), block, 0, st, (const double*)part, slots, norm);
   }
-  if (e != cudaSuccess || slots == 1) return e;
-  return launch_pdl(grad_norm_kernel, dim3(l.G), dim3(kThreads), 0, st, (const double*)part, slots, norm);
+  for (size_t i = 0; i < n && e == cudaSuccess; ++i)
+    e = with_table(l, i, [&](const auto& tab, auto bf16, auto ob) {
+      return launch_pdl(grad_scale_kernel<sizeof(tab.first) / 4, decltype(bf16)::value, decltype(ob)::value>, grid, block, 0, st, tab,
+                        (const double*)part, slots, norm, max_norm);
+    });
+  return e;
 }
 
-size_t gr_workspace(const lsgd_tensors& l) { return slots_of(l) > 1 ? (size_t)l.G * slots_of(l) * sizeof(double) : 0; }
+size_t gr_workspace(const lsgd_tensors& l) { return !l.cluster && slots_of(l) > 1 ? (size_t)l.G * slots_of(l) * sizeof(double) : 0; }
 
 // The first or the last address of a tensor's blocks (gs may be any number where there is one worker).
 uintptr_t end_of(const void* p, int64_t n, int64_t gs, int type, int G) {
@@ -459,23 +623,31 @@ lsgd_status lsgd_tensors_create(const lsgd_tensor* tensors, int count, int G, ls
     auto* l = new lsgd_tensors;
     try {
       l->G = G, l->places = places == 1;
-      // Pieces small enough for every SM's warps to have some, up to 4096 bytes (8 vectors a lane), a launch's at most 2^31.
-      l->piece = kMaxPiece;
-      while (l->piece > kMinPiece && bytes / l->piece * G < (int64_t)kNumSMs * 64) l->piece /= 2;
-      uint32_t at = 0;
       for (int i = 0; i < count; ++i)
-        if (tensors[i].n) {
-          const lsgd_tensor& t = tensors[i];
-          l->list.push_back(t);
-          l->first.push_back(at);
-          at += (uint32_t)((t.n * size_of(t.g_type) + l->piece - 1) / l->piece);
-          l->lo = std::min(l->lo, reinterpret_cast<uintptr_t>(t.g));
-          l->hi = std::max(l->hi, end_of(t.g, t.n, t.g_gs, t.g_type, G));
-          if (l->places) {
-            l->lo = std::min(l->lo, reinterpret_cast<uintptr_t>(t.out));
-            l->hi = std::max(l->hi, end_of(t.out, t.n, t.out_gs, t.out_type, G));
-          }
+        if (tensors[i].n) l->list.push_back(tensors[i]);
+      const auto types = [&](const lsgd_tensor& t) { return 2 * (t.g_type == LSGD_BF16) + (out_type(t, l->places) == LSGD_BF16); };
+      std::stable_sort(l->list.begin(), l->list.end(), [&](const lsgd_tensor& x, const lsgd_tensor& y) { return types(x) < types(y); });
+      for (size_t i = 0, from = 0; i < l->list.size(); ++i)
+        if (i == 0 || i - from == kMany || types(l->list[i]) != types(l->list[i - 1])) l->launches.push_back(from = i);
+      // One launch, a worker to a cluster, where it takes one and the cluster's CTAs have little to read each.
+      if (l->launches.size() == 1 && bytes <= kShare * kMaxCluster)
+        l->cluster = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxCluster, (bytes + kMinShare - 1) / kMinShare));
+      l->launches.push_back(l->list.size());
+      // Pieces small enough for every warp to have one, up to 4096 bytes (8 vectors a lane).
+      const int64_t warps = l->cluster ? l->cluster * (kClusterThreads / 32) : std::max<int64_t>(1, (int64_t)kNumSMs * 4 * kWarps / G);
+      l->piece = kMaxPiece;
+      while (l->piece > kMinPiece && bytes / l->piece < warps) l->piece /= 2;
+      uint32_t at = 0;
+      for (const lsgd_tensor& t : l->list) {
+        l->first.push_back(at);
+        at += (uint32_t)((t.n * size_of(t.g_type) + l->piece - 1) / l->piece);
+        l->lo = std::min(l->lo, reinterpret_cast<uintptr_t>(t.g));
+        l->hi = std::max(l->hi, end_of(t.g, t.n, t.g_gs, t.g_type, G));
+        if (l->places) {
+          l->lo = std::min(l->lo, reinterpret_cast<uintptr_t>(t.out));
+          l->hi = std::max(l->hi, end_of(t.out, t.n, t.out_gs, t.out_type, G));
         }
+      }
       l->first.push_back(at);
       const int64_t most = std::max<int64_t>(1, (int64_t)kNumSMs * 4 / G);
       l->blocks = (int)std::min<int64_t>(most, ((int64_t)at + kWarps - 1) / kWarps);
@@ -505,7 +677,7 @@ lsgd_status lsgd_gradient_norm(const lsgd_tensors* list, float* norm, void* work
   const char* fn = "lsgd_gradient_norm";
   const char* bad = norm_error(list, norm, workspace, workspace_bytes);
   if (bad) return gr_error(LSGD_EINVAL, fn, bad);
-  const cudaError_t e = norm_of(*list, norm, static_cast<double*>(workspace), (cudaStream_t)stream);
+  const cudaError_t e = norm_and_clip(*list, norm, 0.f, static_cast<double*>(workspace), (cudaStream_t)stream);
   return e == cudaSuccess ? LSGD_OK : gr_error(LSGD_ECUDA, fn, cudaGetErrorString(e));
 }
 
@@ -517,13 +689,7 @@ lsgd_status lsgd_gradient_clip(const lsgd_tensors* list, float* norm, float max_
   if (!bad && !(max_norm > 0.f && max_norm < INFINITY)) bad = "max_norm must be positive and finite";
   if (!bad && list->overlap) bad = "what would be written overlaps another tensor of the list";
   if (bad) return gr_error(LSGD_EINVAL, fn, bad);
-  const cudaStream_t st = (cudaStream_t)stream;
-  cudaError_t e = norm_of(*list, norm, static_cast<double*>(workspace), st);
-  const size_t count = list->list.size();
-  for (size_t i = 0; i < count && e == cudaSuccess; i += kMany) {
-    const size_t to = std::min(count, i + kMany);
-    e = to - i <= kFew ? scale<kFew>(*list, i, to, norm, max_norm, st) : scale<kMany>(*list, i, to, norm, max_norm, st);
-  }
+  const cudaError_t e = norm_and_clip(*list, norm, max_norm, static_cast<double*>(workspace), (cudaStream_t)stream);
   return e == cudaSuccess ? LSGD_OK : gr_error(LSGD_ECUDA, fn, cudaGetErrorString(e));
 }
 

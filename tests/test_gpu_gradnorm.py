@@ -21,7 +21,7 @@ def _lists():
     rng = np.random.default_rng(7)
     odd = [int(v) for v in rng.integers(1, 5000, 90)]
     return {"one value": [1], "one": [1000], "small": [3, 1, 7, 16, 0, 64, 129], "odd": odd, "large": [300001, 5, 1 << 20],
-            "many": [int(v) for v in rng.integers(0, 60, 1500)], "huge and tiny": [4_000_003, 1, 2, 3]}
+            "many": [int(v) for v in rng.integers(0, 60, 1500)], "hundreds": [int(v) for v in rng.integers(1, 300, 400)], "huge and tiny": [4_000_003, 1, 2, 3]}
 
 
 def _make(torch, sizes, G, form, dtype, rng, scale=1.0):
