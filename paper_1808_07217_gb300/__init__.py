@@ -758,6 +758,33 @@ def lsgd_direction_update(w, o, Wb, G: int, n: int, lr: float, scale: float = 1.
              weight_decay))
 
 
+_raw = []  # PyTorch's allocation and release of bytes on a stream, filled by the first call
+
+
+def _launch_scratch(dev, stream, workspace, nbytes, fn, args):
+    """_launch for calls of a few microseconds: a workspace that the caller does not give comes from PyTorch's caching
+    allocator as bytes of the call's own stream (which orders a block's uses), not as a tensor, which takes 4 us longer."""
+    import torch
+
+    if workspace is not None or not nbytes:
+        return _launch(dev, stream, workspace, nbytes, fn, args)
+    if torch.cuda.current_device() != dev:
+        with torch.cuda.device(dev):
+            return _launch_scratch(dev, stream, workspace, nbytes, fn, args)
+    if not _raw:
+        alloc = getattr(torch._C, "_cuda_cudaCachingAllocator_raw_alloc", None)
+        _raw.append(alloc or (lambda n, st: torch.cuda.caching_allocator_alloc(n, None, st)))
+        _raw.append(getattr(torch._C, "_cuda_cudaCachingAllocator_raw_delete", torch.cuda.caching_allocator_delete))
+    st = _stream_of(dev) if stream is None else int(stream)
+    at = _raw[0](nbytes, 0 if st == 1 else st)  # (1 is the runtime's other handle of the default stream)
+    try:
+        status = fn(*args, at, nbytes, st)
+    finally:
+        _raw[1](at)
+    if status != OK:
+        _check(status)
+
+
 @functools.lru_cache(maxsize=256)
 def lsgd_layernorm_workspace(G: int, R: int, C: int) -> int:
     """Bytes of workspace that lsgd_layernorm_backward needs for these sizes (the forward needs none)."""
@@ -800,7 +827,7 @@ def lsgd_layernorm_backward(x, y, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta
     dev = _checked(("x", x, nx, xt), ("dx", dx, nx, xt), ("ds", ds, nx, xt), ("dy", dy, ny, yt), ("y", y, ny, yt),
                    ("gamma", gamma, npar, FP32), ("beta", beta, npar, FP32), ("dgamma", dgamma, npar, FP32),
                    ("dbeta", dbeta, npar, FP32), ("mean", mean, N, FP32), ("rstd", rstd, N, FP32))
-    _launch(dev, stream, workspace, nbytes, lib().lsgd_layernorm_backward,
+    _launch_scratch(dev, stream, workspace, nbytes, lib().lsgd_layernorm_backward,
             (x.data_ptr(), xt, x_ld, y.data_ptr() if y is not None else None, dy.data_ptr(), yt, y_ld,
              ds.data_ptr() if ds is not None else None, gamma.data_ptr(), beta.data_ptr(), par_gs, mean.data_ptr(),
              rstd.data_ptr(), dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), G, R, C, act))
@@ -859,7 +886,7 @@ def lsgd_gradient_norm(tensors: Tensors, norm, workspace=None, stream=None):
     dev = _checked(("norm", norm, tensors.G, _type_of(norm)))
     if dev != tensors.device or norm.dtype is not _WANTED[FP32]:
         raise LsgdError(EINVAL, f"norm: a float32 tensor on CUDA device {tensors.device} is wanted")
-    _launch(dev, stream, workspace, tensors.workspace, lib().lsgd_gradient_norm, (tensors.handle, norm.data_ptr()))
+    _launch_scratch(dev, stream, workspace, tensors.workspace, lib().lsgd_gradient_norm, (tensors.handle, norm.data_ptr()))
 
 
 def lsgd_gradient_clip(tensors: Tensors, norm, max_norm: float, workspace=None, stream=None):
@@ -867,7 +894,7 @@ def lsgd_gradient_clip(tensors: Tensors, norm, max_norm: float, workspace=None, 
     dev = _checked(("norm", norm, tensors.G, _type_of(norm)))
     if dev != tensors.device or norm.dtype is not _WANTED[FP32]:
         raise LsgdError(EINVAL, f"norm: a float32 tensor on CUDA device {tensors.device} is wanted")
-    _launch(dev, stream, workspace, tensors.workspace, lib().lsgd_gradient_clip, (tensors.handle, norm.data_ptr(), max_norm))
+    _launch_scratch(dev, stream, workspace, tensors.workspace, lib().lsgd_gradient_clip, (tensors.handle, norm.data_ptr(), max_norm))
 
 
 def lsgd_clipped_update(w, u, g, Wb, G: int, n: int, norm, max_norm: float, lr: float, momentum: float = 0.0,

@@ -27,7 +27,12 @@
 struct lsgd_tensors {
   std::vector<lsgd_tensor> list;     // without the empty ones, those of the same types together
   std::vector<uint32_t> first;       // first piece of each, and their number
-  std::vector<size_t> launches;      // first tensor of each launch (of tensors of the same types), and their number
+  struct Launch {
+    size_t from, to;                 // tensors, all of the same types
+    bool bf16, out_bf16;
+    std::vector<uint64_t> table;     // what their kernels find them in
+  };
+  std::vector<Launch> launches;
   int G = 0, piece = 0;              // workers; bytes of a piece
   bool places = false;               // every tensor has an `out`
   bool overlap = false;              // what a clipping would write overlaps something
@@ -41,7 +46,7 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxPiece = 4096, kMinPiece = 512;
-constexpr int64_t kShare = 160 << 10, kMinShare = 32 << 10;  // bytes of a worker's gradient to a CTA of a cluster
+constexpr int64_t kShare = 160 << 10, kMinShare = 16 << 10;  // bytes of a worker's gradient to a CTA of a cluster
 
 struct Entry {
   const void* in;
@@ -57,7 +62,7 @@ struct Table {
   uint32_t first[MAX];    // of each tensor
   Entry e[MAX];
 };
-constexpr int kFew = 64, kMany = 640;
+constexpr int kFew = 64, kSome = 256, kMany = 640;  // sizes of table (a smaller one is a shorter launch)
 static_assert(sizeof(Table<kMany>) <= 32000, "a launch's parameters");
 
 // The piece's tensor: the last whose first piece is at most p, from tensor t on.
@@ -173,7 +178,8 @@ __device__ __forceinline__ float root(double s) {
 template <bool BF16, int MAX>
 __device__ __forceinline__ double squares_of(const Table<MAX>& tab, int64_t worker, uint64_t p, uint32_t stride) {
   double s = 0.0;
-  int t = 0;
+  int t = find(tab, 0, (uint32_t)p);  // (the table does not depend on other kernels: it is there before they are done)
+  pdl_begin();
   for (; p < tab.end; p += stride) {
     t = find(tab, t, (uint32_t)p);
     const double q = piece_squares(Range<BF16>(tab.e[t], tab.shift, worker, (uint32_t)p - tab.first[t]), threadIdx.x & 31);
@@ -186,7 +192,6 @@ __device__ __forceinline__ double squares_of(const Table<MAX>& tab, int64_t work
 template <int MAX, bool BF16>
 __global__ void __launch_bounds__(kThreads, 4) grad_squares_kernel(const __grid_constant__ Table<MAX> tab, double* part, int slot,
                                                                    int slots, float* norm) {
-  pdl_begin();
   const double s = block_sum<kThreads>(squares_of<BF16>(tab, blockIdx.y, tab.begin + blockIdx.x * kWarps + threadIdx.x / 32,
                                                   gridDim.x * kWarps));
   if (threadIdx.x) return;
@@ -331,26 +336,26 @@ __global__ void __launch_bounds__(kThreads, 4) grad_scale_kernel(const __grid_co
 }
 
 // Both in one launch, a worker to a cluster: the CTAs' sums meet in shared memory.
-constexpr int kClusterThreads = 1024, kMaxCluster = 8;
+constexpr int kClusterThreads = 512, kMaxCluster = 8;
 
 template <int MAX, bool BF16, bool CLIP, bool OB>
 __global__ void __launch_bounds__(kClusterThreads) grad_cluster_kernel(const __grid_constant__ Table<MAX> tab, float* norm,
                                                                           float max_norm) {
   __shared__ double sums[kMaxCluster];
   const uint32_t cl = gridDim.x;  // a cluster is a row of the grid
-  pdl_begin();
+  if (cl > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   const uint32_t p = tab.begin + blockIdx.x * (kClusterThreads / 32) + threadIdx.x / 32, stride = cl * (kClusterThreads / 32);
   double s = block_sum<kClusterThreads>(squares_of<BF16>(tab, blockIdx.y, p, stride));
   if (cl > 1) {
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // every CTA's shared memory is there
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // every CTA's shared memory is there
     if (threadIdx.x == 0)
       for (uint32_t i = 0; i < cl; ++i) {
         uint32_t to;
         asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(&sums[blockIdx.x])), "r"(i));
         asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to), "d"(s) : "memory");
       }
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    if (threadIdx.x < 32) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // (only its stores count)
+    else asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   }
   __shared__ float shared;
@@ -446,87 +451,89 @@ lsgd_status gr_error(lsgd_status s, const char* fn, const char* what) {
 }
 int size_of(int type) { return type == LSGD_BF16 ? 2 : 4; }
 
-int slots_of(const lsgd_tensors& l) { return l.blocks * (int)(l.launches.size() - 1); }
+int slots_of(const lsgd_tensors& l) { return l.blocks * (int)l.launches.size(); }
 int out_type(const lsgd_tensor& t, bool places) { return places ? t.out_type : t.g_type; }
 
 template <int MAX>
-void fill(Table<MAX>& tab, const lsgd_tensors& l, size_t from, size_t to) {
-  tab.count = (int)(to - from);
+void fill(lsgd_tensors::Launch& launch, const lsgd_tensors& l) {
+  launch.table.resize((sizeof(Table<MAX>) + 7) / 8);
+  Table<MAX>& tab = *reinterpret_cast<Table<MAX>*>(launch.table.data());
+  tab.count = (int)(launch.to - launch.from);
   tab.shift = __builtin_ctz(l.piece);
-  tab.begin = l.first[from], tab.end = l.first[to];
-  for (size_t i = from; i < to; ++i) {
+  tab.begin = l.first[launch.from], tab.end = l.first[launch.to];
+  for (size_t i = launch.from; i < launch.to; ++i) {
     const lsgd_tensor& t = l.list[i];
-    Entry& e = tab.e[i - from];
+    Entry& e = tab.e[i - launch.from];
     e.in = t.g, e.out = l.places ? t.out : const_cast<void*>(t.g);
     e.n = t.n, e.gs = t.g_gs, e.out_gs = l.places ? t.out_gs : t.g_gs;
-    tab.first[i - from] = l.first[i];
+    tab.first[i - launch.from] = l.first[i];
   }
 }
-
-// f(table, BF16, OB) for the tensors of launch i.
 template <typename F>
-cudaError_t with_table(const lsgd_tensors& l, size_t i, F f) {
-  const size_t from = l.launches[i], to = l.launches[i + 1];
-  const bool bf16 = l.list[from].g_type == LSGD_BF16, ob = out_type(l.list[from], l.places) == LSGD_BF16;
-  const auto typed = [&](const auto& tab) {
-    if (bf16) return ob ? f(tab, std::true_type{}, std::true_type{}) : f(tab, std::true_type{}, std::false_type{});
-    return ob ? f(tab, std::false_type{}, std::true_type{}) : f(tab, std::false_type{}, std::false_type{});
-  };
-  if (to - from <= kFew) {
-    Table<kFew> tab;
-    fill(tab, l, from, to);
-    return typed(tab);
-  }
-  Table<kMany> tab;
-  fill(tab, l, from, to);
-  return typed(tab);
+auto with_size(size_t count, F f) {
+  if (count <= kFew) return f(std::integral_constant<int, kFew>{});
+  if (count <= kSome) return f(std::integral_constant<int, kSome>{});
+  return f(std::integral_constant<int, kMany>{});
+}
+// f(the table's size, BF16, OB) of a launch.
+template <typename F>
+cudaError_t with_kind(const lsgd_tensors::Launch& l, F f) {
+  return with_size(l.to - l.from, [&](auto max) {
+    if (l.bf16) return l.out_bf16 ? f(max, std::true_type{}, std::true_type{}) : f(max, std::true_type{}, std::false_type{});
+    return l.out_bf16 ? f(max, std::false_type{}, std::true_type{}) : f(max, std::false_type{}, std::false_type{});
+  });
 }
 
-template <typename K, typename T>
-cudaError_t launch_clusters(K kernel, const lsgd_tensors& l, const T& tab, float* norm, float max_norm, cudaStream_t st) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(l.cluster, l.G);
-  cfg.blockDim = dim3(kClusterThreads);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = l.cluster;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = l.cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, tab, norm, max_norm);
+// The launch of a kernel on its table (which is copied once, by the launch itself); cluster: CTAs of one.
+template <typename TAB, typename... T, typename... A>
+cudaError_t launch_table(void (*kernel)(TAB, T...), const lsgd_tensors::Launch& l, dim3 grid, int threads, int cluster,
+                         cudaStream_t st, A... given) {
+  return [&](T... args) {
+    void* p[] = {const_cast<uint64_t*>(l.table.data()), &args...};
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelExC(&cfg, reinterpret_cast<const void*>(kernel), p);
+  }(given...);
 }
 
 // The norms and, with max_norm > 0, the clipped gradients.
 cudaError_t norm_and_clip(const lsgd_tensors& l, float* norm, float max_norm, double* part, cudaStream_t st) {
-  const size_t n = l.launches.size() - 1;
+  const size_t n = l.launches.size();
   const bool clip = max_norm > 0.f;
   if (n == 0) return cudaMemsetAsync(norm, 0, sizeof(float) * l.G, st);
   if (l.cluster)
-    return with_table(l, 0, [&](const auto& tab, auto bf16, auto ob) {
-      constexpr int MAX = sizeof(tab.first) / 4;
+    return with_kind(l.launches[0], [&](auto max, auto bf16, auto ob) {
       constexpr bool B = decltype(bf16)::value, O = decltype(ob)::value;
-      return clip ? launch_clusters(grad_cluster_kernel<MAX, B, true, O>, l, tab, norm, max_norm, st)
-                  : launch_clusters(grad_cluster_kernel<MAX, B, false, false>, l, tab, norm, max_norm, st);
+      constexpr int MAX = decltype(max)::value;
+      return launch_table(clip ? grad_cluster_kernel<MAX, B, true, O> : grad_cluster_kernel<MAX, B, false, false>, l.launches[0],
+                          dim3(l.cluster, l.G), kClusterThreads, l.cluster, st, norm, max_norm);
     });
   const int slots = slots_of(l);
-  const dim3 grid(l.blocks, l.G), block(kThreads);
+  const dim3 grid(l.blocks, l.G);
   cudaError_t e = cudaSuccess;
   for (size_t i = 0; i < n && e == cudaSuccess; ++i)
-    e = with_table(l, i, [&](const auto& tab, auto bf16, auto) {
-      return launch_pdl(grad_squares_kernel<sizeof(tab.first) / 4, decltype(bf16)::value>, grid, block, 0, st, tab, part,
-                        (int)i * l.blocks, slots, slots == 1 ? norm : nullptr);
+    e = with_kind(l.launches[i], [&](auto max, auto bf16, auto) {
+      return launch_table(grad_squares_kernel<decltype(max)::value, decltype(bf16)::value>, l.launches[i], grid, kThreads, 1, st, part,
+                          (int)i * l.blocks, slots, slots == 1 ? norm : nullptr);
     });
   if (!clip) {
     if (e != cudaSuccess || slots == 1) return e;
-    return launch_pdl(grad_norm_kernel, dim3(l.G), block, 0, st, (const double*)part, slots, norm);
+    return launch_pdl(grad_norm_kernel, dim3(l.G), dim3(kThreads), 0, st, (const double*)part, slots, norm);
   }
   for (size_t i = 0; i < n && e == cudaSuccess; ++i)
-    e = with_table(l, i, [&](const auto& tab, auto bf16, auto ob) {
-      return launch_pdl(grad_scale_kernel<sizeof(tab.first) / 4, decltype(bf16)::value, decltype(ob)::value>, grid, block, 0, st, tab,
-                        (const double*)part, slots, norm, max_norm);
+    e = with_kind(l.launches[i], [&](auto max, auto bf16, auto ob) {
+      return launch_table(grad_scale_kernel<decltype(max)::value, decltype(bf16)::value, decltype(ob)::value>, l.launches[i], grid,
+                          kThreads, 1, st, part, slots, norm, max_norm);
     });
   return e;
 }
@@ -628,11 +635,17 @@ lsgd_status lsgd_tensors_create(const lsgd_tensor* tensors, int count, int G, ls
       const auto types = [&](const lsgd_tensor& t) { return 2 * (t.g_type == LSGD_BF16) + (out_type(t, l->places) == LSGD_BF16); };
       std::stable_sort(l->list.begin(), l->list.end(), [&](const lsgd_tensor& x, const lsgd_tensor& y) { return types(x) < types(y); });
       for (size_t i = 0, from = 0; i < l->list.size(); ++i)
-        if (i == 0 || i - from == kMany || types(l->list[i]) != types(l->list[i - 1])) l->launches.push_back(from = i);
-      // One launch, a worker to a cluster, where it takes one and the cluster's CTAs have little to read each.
-      if (l->launches.size() == 1 && bytes <= kShare * kMaxCluster)
-        l->cluster = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxCluster, (bytes + kMinShare - 1) / kMinShare));
-      l->launches.push_back(l->list.size());
+        if (i == 0 || i - from == kMany || types(l->list[i]) != types(l->list[i - 1])) {
+          l->launches.push_back({from = i, i, types(l->list[i]) >= 2, (types(l->list[i]) & 1) != 0, {}});
+        }
+      for (size_t i = 0; i < l->launches.size(); ++i)
+        l->launches[i].to = i + 1 < l->launches.size() ? l->launches[i + 1].from : l->list.size();
+      // One launch, a worker to a cluster, where it takes one and the CTAs have little to read each: as many as get 16 KB or two
+      // tensors to a warp.
+      if (l->launches.size() == 1 && bytes <= kShare * kMaxCluster) {
+        const int64_t want = std::max<int64_t>(bytes / kMinShare, (int64_t)l->list.size() / (kClusterThreads / 16)) + 1;
+        l->cluster = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxCluster, want));
+      }
       // Pieces small enough for every warp to have one, up to 4096 bytes (8 vectors a lane).
       const int64_t warps = l->cluster ? l->cluster * (kClusterThreads / 32) : std::max<int64_t>(1, (int64_t)kNumSMs * 4 * kWarps / G);
       l->piece = kMaxPiece;
@@ -651,6 +664,11 @@ lsgd_status lsgd_tensors_create(const lsgd_tensor* tensors, int count, int G, ls
       l->first.push_back(at);
       const int64_t most = std::max<int64_t>(1, (int64_t)kNumSMs * 4 / G);
       l->blocks = (int)std::min<int64_t>(most, ((int64_t)at + kWarps - 1) / kWarps);
+      for (auto& launch : l->launches)
+        with_size(launch.to - launch.from, [&](auto max) {
+          fill<decltype(max)::value>(launch, *l);
+          return 0;
+        });
       l->overlap = clip_overlaps(*l);
     } catch (...) {
       delete l;

@@ -308,3 +308,84 @@ def test_update_with_norms_that_are_not_finite(P):
     norm = torch.tensor([float("nan"), float("inf"), 2.0], device="cuda")
     P.lsgd_clipped_update(w, None, g, None, 3, 100, norm, 1.0, 0.5)
     assert torch.isnan(w[0]).all() and (w[1] == 1).all() and (w[2] == 0.75).all()
+
+
+# ---- workspaces ----
+def _calls(P):
+    """(bytes of workspace, a call on `stream`, its outputs) for the operators that use one."""
+    import torch
+
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    rand = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    G, R, C = 2, 900, 1000
+    x, dy, gamma, beta = rand(G, R, C), rand(G, R, C), rand(G, C), rand(G, C)
+    y, dx, dgamma, dbeta = torch.empty_like(x), torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(gamma)
+    mean, rstd = torch.empty(G, R, device="cuda"), torch.empty(G, R, device="cuda")
+    P.lsgd_layernorm_forward(x, gamma, beta, y, mean, rstd, G, R, C)
+    grads, norm = [rand(2, 1_000_001), rand(2, 333)], torch.empty(2, device="cuda")
+    outs = [torch.empty_like(g) for g in grads]
+    T, U = P.lsgd_tensors_create(grads), P.lsgd_tensors_create(grads, outs)
+    assert T.workspace and U.workspace and P.lsgd_layernorm_workspace(G, R, C)
+    return [(P.lsgd_layernorm_workspace(G, R, C),
+             lambda **kw: P.lsgd_layernorm_backward(x, None, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, G, R, C, **kw),
+             [dx, dgamma, dbeta]),
+            (T.workspace, lambda **kw: P.lsgd_gradient_norm(T, norm, **kw), [norm]),
+            (U.workspace, lambda **kw: P.lsgd_gradient_clip(U, norm, 1.0, **kw), [norm, *outs])]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("which", [0, 1, 2])
+def test_a_workspace_belongs_to_the_calls_stream(P, which):
+    """A tensor of the workspace's size is deleted while kernels that read and write it wait on the current stream: the call
+    on another stream neither changes what they read nor finds its sums changed by them; the same with a stream of its own."""
+    import torch
+
+    nbytes, call, outs = _calls(P)[which]
+    call()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outs]
+    for t in outs:
+        t.zero_()
+    call(workspace=torch.empty(nbytes, dtype=torch.uint8, device="cuda"))
+    assert all(torch.equal(t, w) for t, w in zip(outs, want))
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        for t in outs:
+            t.zero_()
+        tmp = torch.full((nbytes,), 3, dtype=torch.uint8, device="cuda")
+        copy = torch.empty_like(tmp)
+        torch.cuda.synchronize()
+        torch.cuda._sleep(40_000_000)  # about 20 ms
+        copy.copy_(tmp)
+        for _ in range(20):
+            tmp.add_(1)
+        del tmp
+        call(stream=side.cuda_stream)
+        torch.cuda.synchronize()
+        assert (copy == 3).all()
+        assert all(torch.equal(t, w) for t, w in zip(outs, want))
+    with pytest.raises(P.LsgdError) as e:
+        call(workspace=torch.empty(nbytes - 16, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == P.EINVAL
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("which", [0, 1, 2])
+def test_a_captured_call_keeps_its_workspace_to_itself(P, which):
+    import torch
+
+    nbytes, call, outs = _calls(P)[which]
+    call()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    later = [torch.full((nbytes,), 9, dtype=torch.uint8, device="cuda") for _ in range(8)]
+    for _ in range(2):
+        for t in outs:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all((t == 9).all() for t in later)
+        assert all(torch.equal(t, w) for t, w in zip(outs, want))
