@@ -22,22 +22,28 @@
 #include "operands.h"
 
 namespace lsgd {
+
+int rows_take_timeout_flag() {
+  return take_rows_late() | take_ln_backward_late_none() | take_ln_backward_late_relu() | take_ln_backward_late_silu();
+}
+
 namespace {
 
 // ---- forward ----
-// E: values of a row in a thread.
-template <typename XT, typename YT, int V, bool RES, int E>
+// E: values of a row in a thread.  CLUSTER: a row's CTAs exchange their sums over the cluster's network, which takes about as long as a row:
+// the sums of row k + 1 are formed and sent before those of row k are waited for, and row k is read from shared memory once more.
+// (2,000 x 17,000 in bf16 with a residual: 136 us with the cluster's barrier in every row, 111 with the exchange alone, %%% so.)
+template <typename XT, typename YT, int V, bool RES, int E, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads, 2) ln_forward_kernel(const LnArgs a) {
   constexpr int N = E / V, H = E / 2;
   using In = Feed<XT, V, N>;
+  using M = Team<CLUSTER>;
   constexpr uint32_t kSlotBytes = In::kSlot * (RES ? 2 : 1);
-  __shared__ float4 stats[2 * kSlots + kExchange];
+  __shared__ float4 stats[M::kPlaces];
   extern __shared__ __align__(16) uint8_t ring[];
-  const Team m(a, V, N);
-  if (m.cl > 1) {  // every CTA's shared memory is there from here on
-    cluster_arrive();
-    cluster_wait();
-  }
+  __shared__ uint64_t bars[M::kTurns];
+  const M m(a, V, N, bars);
+  m.begin();
   pdl_begin();
   const Rows rows(a, m, gridDim.x / m.cl, blockIdx.x / m.cl);
   const int hop = m.T * V, left = m.Cs - m.t * V;  // from a vector to the thread's next one; columns from its first one on
@@ -58,30 +64,29 @@ __global__ void __launch_bounds__(kThreads, 2) ln_forward_kernel(const LnArgs a)
     if (RES) fr.land(slot);
   };
   uint32_t slot = 0, next = 0;
-  for (int d = 0; d < a.ahead; ++d, next += kSlotBytes) {
+  const int early = a.ahead + (CLUSTER ? 1 : 0);
+  for (int d = 0; d < early; ++d, next += kSlotBytes) {
     fetch(d, next);
     land(next);
   }
   const uint32_t last = next;
+  const auto advance = [&](uint32_t& s) { s = s == last ? 0 : s + kSlotBytes; };
   u64 ga[H], be[H];
   load_params<V, N>(a.gamma + blockIdx.y * a.par_gs + m.col0, m, ga);
   load_params<V, N>(a.beta + blockIdx.y * a.par_gs + m.col0, m, be);
   XT* s_out = static_cast<XT*>(a.s) + x0;
   YT* y_out = static_cast<YT*>(a.out) + rows.row * a.y_ld + at0;
   int64_t row = rows.row;
-  float4* stat = stats + m.team * m.warps;
   const float inv_n = m.n ? 1.f / m.n : 0.f, inv_C = 1.f / a.C;
-  for (int k = 0; k < rows.turns; ++k) {
-    const bool on = k < rows.mine;
-    fetch(k + a.ahead, next);
-    copies_wait(a.ahead);
-    u64 v[H];
+
+  // A row's values v, their sum s, the mean of the thread's warp (or smaller team) and the squared deviations from it.
+  const auto sums = [&](bool on, u64 (&v)[H], float& s, float& mean, float& q) {
     fx.read(slot, v);
     if constexpr (RES) {
-      u64 q[H];
-      fr.read(slot, q);
+      u64 p[H];
+      fr.read(slot, p);
 #pragma unroll
-      for (int i = 0; i < H; ++i) add2(v[i], q[i]);
+      for (int i = 0; i < H; ++i) add2(v[i], p[i]);
       if constexpr (sizeof(XT) == 2) {
 #pragma unroll
         for (int i = 0; i < H; ++i) {
@@ -97,8 +102,8 @@ __global__ void __launch_bounds__(kThreads, 2) ln_forward_kernel(const LnArgs a)
     u64 acc = v[0];
 #pragma unroll
     for (int i = 1; i < H; ++i) add2(acc, v[i]);
-    const float s = m.sum(added(acc));
-    float mean = s * inv_n;
+    s = m.sum(added(acc));
+    mean = s * inv_n;
     acc = 0;
     if (whole) {
 #pragma unroll
@@ -114,8 +119,9 @@ __global__ void __launch_bounds__(kThreads, 2) ln_forward_kernel(const LnArgs a)
         acc = mad2(w, w, acc);
       }
     }
-    float q = m.sum(added(acc));
-    if (m.slots > 1) m.moments(s, mean, q, inv_C, stat + (k & 1) * kSlots);
+    q = m.sum(added(acc));
+  };
+  const auto finish = [&](bool on, u64 (&v)[H], float mean, float q) {
     const float rstd = rsqrtf(fmaf(q, inv_C, a.eps));
     if (on) {
       if (m.t == 0 && m.rank == 0) {
@@ -135,30 +141,70 @@ __global__ void __launch_bounds__(kThreads, 2) ln_forward_kernel(const LnArgs a)
         });
       store_row<YT, V, N>(v, y_out, whole, left, hop);
     }
-    land(next);
     y_out += y_step;
     row += rows.step;
-    slot = slot == last ? 0 : slot + kSlotBytes;
-    next = next == last ? 0 : next + kSlotBytes;
+  };
+
+  if constexpr (!CLUSTER) {
+    for (int k = 0; k < rows.turns; ++k, advance(slot), advance(next)) {
+      const bool on = k < rows.mine;
+      fetch(k + a.ahead, next);
+      copies_wait(a.ahead);
+      u64 v[H];
+      float s, mean, q;
+      sums(on, v, s, mean, q);
+      if (m.slots > 1) {
+        m.post_moments(s, mean, q, stats, k);
+        m.collect_moments(mean, q, inv_C, stats, k);
+      }
+      finish(on, v, mean, q);
+      land(next);
+    }
+  } else {
+    uint32_t before = 0, coming = 0;  // the places of row k - 1, and of the row that was fetched last
+    for (int k = 0; k <= rows.turns; ++k) {
+      u64 v[H];
+      float s, mean, q;
+      if (k < rows.turns) {
+        copies_wait(a.ahead);
+        sums(true, v, s, mean, q);
+        if constexpr (RES) fx.write(slot, v);
+        m.post_moments(s, mean, q, stats, k);
+      }
+      if (k) {
+        land(coming);
+        m.collect_moments(mean, q, inv_C, stats, k - 1);
+        fx.read(before, v);
+        finish(true, v, mean, q);
+      }
+      fetch(k + early, next);
+      before = slot, coming = next;
+      advance(slot);
+      advance(next);
+    }
+    m.end();
   }
 }
 
-template <typename XT, typename YT, int V, bool RES, int E>
-cudaError_t ln_forward_held(LnArgs a, int G, cudaStream_t st) {
+template <typename XT, typename YT, int V, bool RES, int E, bool CLUSTER>
+cudaError_t ln_forward_as(LnArgs a, int G, cudaStream_t st) {
   static std::atomic<int> raised{0};  // device + 1 whose limits this kernel's have been raised to
   using In = Feed<XT, V, E / V>;
-  constexpr int slot = In::kSlot * (RES ? 2 : 1), fit = kSmemPerSm / (2 * slot + kStaticSmem);
+  constexpr int slot = In::kSlot * (RES ? 2 : 1), more = CLUSTER ? 2 : 1, own = kStaticSmem<CLUSTER>;
+  constexpr int fit = kSmemPerSm / ((1 + more) * slot + own);
   const LnPlan p = ln_plan(G, a.R, a.C, E, fit);
   const int threads = p.T * p.teams, per_sm = std::min(std::max(1, kThreadsPerSm / threads), fit);
   a.T = p.T, a.teams = p.teams, a.cl = p.cl, a.slice = p.slice;
-  a.ahead = In::kAsync && per_sm * (3 * slot + kStaticSmem) <= kSmemPerSm ? ln_ahead(p.rows, per_sm * threads, slot / kThreads) : 1;
-  return ln_launch(ln_forward_kernel<XT, YT, V, RES, E>, raised, a, dim3((unsigned)(p.ranges * p.cl), G), (a.ahead + 1) * slot, st);
+  a.ahead = In::kAsync && per_sm * ((2 + more) * slot + own) <= kSmemPerSm ? ln_ahead(p.rows, per_sm * threads, slot / kThreads) : 1;
+  return ln_launch(ln_forward_kernel<XT, YT, V, RES, E, CLUSTER>, raised, a, dim3((unsigned)(p.ranges * p.cl), G),
+                   (a.ahead + more) * slot, st);
 }
 // 16 values to a thread; 8 where single bf16 values go through registers, 32 of which they would take with a residual (32,768 x 1531:
 // 214 and 122 us).
 template <typename XT, typename YT, int V, bool RES>
 cudaError_t ln_forward(const LnArgs& a, int G, cudaStream_t st) {
-  return ln_forward_held<XT, YT, V, RES, Feed<XT, V, 1>::kAsync ? 16 : 8>(a, G, st);
+  constexpr int E = Feed<XT, V, 1>::kAsync ? 16 : 8;
+  return a.C > E * kThreads ? ln_forward_as<XT, YT, V, RES, E, true>(a, G, st) : ln_forward_as<XT, YT, V, RES, E, false>(a, G, st);
 }
 
 // The widest vector (a power of two of values, at most v) with which rows of stride ld from p on (values of z bytes) are aligned.

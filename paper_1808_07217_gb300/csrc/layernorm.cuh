@@ -18,9 +18,11 @@ constexpr int kMaxCluster = 16;
 constexpr int kMaxC = 8 * kThreads * kMaxCluster;  // with 8 values to a thread
 constexpr int kThreadsPerSm = 512;            // at 128 registers
 constexpr int kSmemPerSm = 222 * 1024;
-constexpr int kSlots = kThreads / 32 * kMaxCluster;  // of an exchange; two take turns
+template <bool CLUSTER>
+constexpr int kSlotsOf = kThreads / 32 * (CLUSTER ? kMaxCluster : 1);  // of an exchange
 constexpr int kExchange = 8;                  // slots that are read together
-constexpr int kStaticSmem = 5376;             // of a CTA: the exchanges' at most (264 of 16 bytes), and the system's
+template <bool CLUSTER>  // of a CTA: the exchanges' at most (of 16 bytes), barriers, and the system's
+constexpr int kStaticSmem = 16 * ((CLUSTER ? 4 : 2) * kSlotsOf<CLUSTER> + kExchange) + 64 + 1024;
 
 struct LnArgs {
   const void *x, *r, *y, *dy, *ds;
@@ -39,6 +41,25 @@ struct LnArgs {
   int seg;        // rows that are added up at a time
   int sums;       // backward: where in shared memory their sums stand, in bytes
 };
+
+// Each source file that includes this has a flag of its own, which a wait that runs out sets (and which is read only once a cluster,
+// whose CTAs alone wait so, has been launched).
+namespace {
+__device__ int g_rows_late = 0;
+std::atomic<bool> g_rows_clustered{false};
+int take_rows_late() {
+  int h = 0;
+  if (!g_rows_clustered) return 0;
+  if (cudaMemcpyFromSymbol(&h, g_rows_late, sizeof(int)) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;
+  }
+  if (h) {
+    const int zero = 0;
+    cudaMemcpyToSymbol(g_rows_late, &zero, sizeof(int));
+  }
+  return h;
+}
 
 // How the rows are dealt out, whatever the types.
 struct LnPlan {
@@ -70,30 +91,71 @@ inline LnPlan ln_plan(int G, int64_t R, int C, int E, int per_sm = 0) {
 __device__ __forceinline__ void team_barrier(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ void store_peer(const float* at, int rank, float v) {
-  uint32_t p;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(p) : "r"(smem_u32(at)), "r"(rank));
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(p), "f"(v) : "memory");
+// Every CTA of the cluster is here (and its shared memory there before the first time).
+__device__ __forceinline__ void cluster_meet() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ void store_peer(const float4* at, int rank, float4 v) {
-  uint32_t p;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(p) : "r"(smem_u32(at)), "r"(rank));
-  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(p), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+// v to the place `at` of the cluster's CTA `rank`, whose barrier `bar` counts the bytes.  (No barrier of the whole cluster in every row: its
+// release would wait for the rows' stores.)
+__device__ __forceinline__ uint32_t peer_address(const void* p, int rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void send(const float* at, const uint64_t* bar, int rank, float v) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.f32 [%0], %1, [%2];" ::"r"(peer_address(at, rank)), "f"(v),
+               "r"(peer_address(bar, rank))
+               : "memory");
+}
+__device__ __forceinline__ void send(const float4* at, const uint64_t* bar, int rank, float4 v) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(
+                   peer_address(at, rank)),
+               "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "r"(peer_address(bar, rank))
+               : "memory");
+}
+// Until the bytes of the phase are there, or, after about 2 s, never: the flag is set, and what follows is wrong, but ends.
+__device__ __forceinline__ void wait_bytes(uint64_t* bar, uint32_t parity) {
+  const auto there = [&] {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+        " selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+  };
+  if (there()) return;
+  const long long t0 = clock64();
+  while (!there())
+    if (clock64() - t0 > 4000000000LL) {
+      atomicExch(&g_rows_late, 1);
+      return;
+    }
 }
 
-// A thread's place, and what its team shares.
+// A thread's place, and what its team shares.  The row's warps exchange their sums in two halves, post and collect, through one of kTurns
+// places in turn.  In a CTA a barrier lies between; whoever posts row k + 2 has passed that of row k + 1, which every warp
+// reaches when it has collected row k.  A cluster's CTAs post row k + 1 before they collect row k (below), so that whoever posts
+// row k + 4 has collected row k + 2, which every warp posted when it had collected row k: four places.
+template <bool CLUSTER>
 struct Team {
+  static constexpr int kTurns = CLUSTER ? 4 : 2, kSlots = kSlotsOf<CLUSTER>, kPlaces = kTurns * kSlots + kExchange;
   int T, t, team, lane, warps, warp, cl, rank, slots;
-  int col0, Cs;  // the CTA's columns
-  int n;         // the warp's (or smaller team's) columns
-  __device__ __forceinline__ Team(const LnArgs& a, int vec, int vecs) {
+  int col0, Cs;    // the CTA's columns
+  int n;           // the warp's (or smaller team's) columns
+  uint64_t* bars;  // a cluster's: [kTurns]
+  __device__ __forceinline__ Team(const LnArgs& a, int vec, int vecs, uint64_t* cluster_bars) {
     T = a.T, team = threadIdx.x / T, t = threadIdx.x - team * T, lane = threadIdx.x & 31;
     warps = T < 32 ? 1 : T / 32, warp = T < 32 ? 0 : t / 32;
-    cl = a.cl;
-    rank = 0;
-    if (cl > 1) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    bars = cluster_bars;
+    if constexpr (CLUSTER) {
+      cl = a.cl;
+      asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    } else {
+      cl = 1, rank = 0;
+    }
     slots = warps * cl;
     col0 = rank * a.slice, Cs = min(a.slice, a.C - col0);
     n = Cs;
@@ -112,33 +174,53 @@ struct Team {
     for (int d = 16; d; d /= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
     return v;
   }
-  __device__ __forceinline__ void meet() const {  // of the row's threads: what they wrote to `stat` is there
-    if (cl == 1) {
-      team_barrier(team + 1, T);
-    } else {
-      cluster_arrive();
-      cluster_wait();
+  // Before a cluster's first exchange, and before its CTAs leave.
+  __device__ __forceinline__ void begin() const {
+    if constexpr (CLUSTER) {
+      if (threadIdx.x == 0) {
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) mbar_init(bars + i, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      }
+      cluster_meet();
     }
   }
-  // The row's mean and sum of squared deviations from a warp's sum s, mean and sum q.  `stat` [slots]: one of two that take turns.
-  __device__ __forceinline__ void moments(float s, float& mean, float& q, float inv_C, float4* stat) const {
-    const float4 mine = make_float4(s, mean, q, (float)n);
-    if (cl == 1) {
-      if (lane == 0) stat[warp] = mine;
-    } else if (lane < cl) {
-      store_peer(stat + rank * warps + warp, lane, mine);
+  __device__ __forceinline__ void end() const {
+    if constexpr (CLUSTER) cluster_meet();
+  }
+  // What the row's warps posted (`bytes` each) is there; k counts the rows.
+  __device__ __forceinline__ void meet(int k, int bytes) const {
+    if constexpr (CLUSTER) {
+      if (threadIdx.x == 0) mbar_expect_tx(bars + k % kTurns, slots * bytes);
+      wait_bytes(bars + k % kTurns, (k / kTurns) & 1);
+    } else {
+      team_barrier(team + 1, T);
     }
-    meet();
-    s = q = 0.f;
-    if (slots <= 8) {  // (what stands behind the slots is read, and not used: `stat` has room for it)
+  }
+  // The row's mean and sum of squared deviations q from a warp's sum s, mean and sum q.  (Alone: the warp is the team.)
+  __device__ __forceinline__ void post_moments(float s, float mean, float q, float4* stats, int k) const {
+    float4* stat = stats + k % kTurns * kSlots + team * warps;
+    const float4 mine = make_float4(s, mean, q, (float)n);
+    if constexpr (CLUSTER) {
+      if (lane < cl) send(stat + rank * warps + warp, bars + k % kTurns, lane, mine);
+    } else {
+      if (lane == 0) stat[warp] = mine;
+    }
+  }
+  __device__ __forceinline__ void collect_moments(float& mean, float& q, float inv_C, const float4* stats, int k) const {
+    const float4* stat = stats + k % kTurns * kSlots + team * warps;
+    meet(k, 16);
+    float s = 0.f;
+    q = 0.f;
+    if (slots <= kExchange) {  // (what stands behind the slots is read, and not used: `stats` has room for it)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < kExchange; ++i) {
         const float f = stat[i].x;
         s += i < slots ? f : 0.f;
       }
       mean = s * inv_C;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < kExchange; ++i) {
         const float f = deviation(stat[i], mean);
         q += i < slots ? f : 0.f;
       }
@@ -154,41 +236,45 @@ struct Team {
     return fmaf(f.w * d, d, f.z);
   }
   // p and q summed over the row.  In a warp the halves sum one each: 5 exchanges instead of 10.
-  __device__ __forceinline__ void sum_both(float& p, float& q, float2* stat) const {
-    if (T < 32) {
-      for (int d = T / 2; d; d /= 2) {
-        p += __shfl_xor_sync(0xffffffffu, p, d);
-        q += __shfl_xor_sync(0xffffffffu, q, d);
-      }
-      return;
+  __device__ __forceinline__ void post_both(float p, float q, float2* stats, int k) const {
+    const float v = halves(p, q);
+    float2* stat = stats + k % kTurns * kSlots + team * warps;
+    if constexpr (CLUSTER) {
+      if ((lane & 15) < cl)
+        send(reinterpret_cast<float*>(stat + rank * warps + warp) + (lane >> 4), bars + k % kTurns, lane & 15, v);
+    } else {
+      if ((lane & 15) == 0) (lane ? stat[warp].y : stat[warp].x) = v;
     }
-    float v = halves(p, q);
-    if (slots > 1) {
-      if (cl == 1) {
-        if ((lane & 15) == 0) (lane ? stat[warp].y : stat[warp].x) = v;
-      } else if ((lane & 15) < cl) {
-        store_peer(reinterpret_cast<float*>(stat + rank * warps + warp) + (lane >> 4), lane & 15, v);
-      }
-      meet();
-      p = q = 0.f;
-      if (slots <= 8) {
+  }
+  __device__ __forceinline__ void collect_both(float& p, float& q, const float2* stats, int k) const {
+    const float2* stat = stats + k % kTurns * kSlots + team * warps;
+    meet(k, 8);
+    p = q = 0.f;
+    if (slots <= kExchange) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float2 f = stat[i];
-          p += i < slots ? f.x : 0.f;
-          q += i < slots ? f.y : 0.f;
-        }
-        return;
+      for (int i = 0; i < kExchange; ++i) {
+        const float2 f = stat[i];
+        p += i < slots ? f.x : 0.f;
+        q += i < slots ? f.y : 0.f;
       }
+    } else {
       for (int i = lane; i < slots; i += 32) {
         const float2 f = stat[i];
         p += f.x;
         q += f.y;
       }
-      v = halves(p, q);
+      spread(halves(p, q), p, q);
     }
-    p = __shfl_sync(0xffffffffu, v, 0);
-    q = __shfl_sync(0xffffffffu, v, 16);
+  }
+  __device__ __forceinline__ void sum_both(float& p, float& q) const {  // of a team that is a warp or less
+    if (T == 32) {
+      spread(halves(p, q), p, q);
+      return;
+    }
+    for (int d = T / 2; d; d /= 2) {
+      p += __shfl_xor_sync(0xffffffffu, p, d);
+      q += __shfl_xor_sync(0xffffffffu, q, d);
+    }
   }
   // The warp's sum of p in lanes 0 to 15, of q in the others.
   __device__ __forceinline__ float halves(float p, float q) const {
@@ -197,6 +283,10 @@ struct Team {
 #pragma unroll
     for (int d = 8; d; d /= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
     return v;
+  }
+  static __device__ __forceinline__ void spread(float v, float& p, float& q) {
+    p = __shfl_sync(0xffffffffu, v, 0);
+    q = __shfl_sync(0xffffffffu, v, 16);
   }
 };
 
@@ -225,8 +315,8 @@ __device__ __forceinline__ float added(u64 p) {
 }
 
 // A thread's values of the parameter at p (worker's, CTA's first column), zeros behind the row's end.
-template <int V, int N>
-__device__ __forceinline__ void load_params(const float* p, const Team& m, u64 (&out)[N * V / 2]) {
+template <int V, int N, typename M>
+__device__ __forceinline__ void load_params(const float* p, const M& m, u64 (&out)[N * V / 2]) {
   float v[N * V];
 #pragma unroll
   for (int e = 0; e < N * V; ++e) {
@@ -309,6 +399,23 @@ struct Feed {
     }
     to_pairs(r, out);
   }
+  __device__ __forceinline__ void write(uint32_t slot, const u64 (&in)[N * V / 2]) const {  // back to a row's place
+    Vec<T, V> r[N];
+    from_pairs(in, r);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const uint32_t p = at + slot + j * kThreads * kBytes;
+      if constexpr (kBytes == 16)
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(p), "r"(r[j].r[0].x), "r"(r[j].r[0].y), "r"(r[j].r[0].z),
+                     "r"(r[j].r[0].w) : "memory");
+      else if constexpr (kBytes == 8)
+        asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(p), "r"(r[j].r[0].x), "r"(r[j].r[0].y) : "memory");
+      else if constexpr (kBytes == 4)
+        asm volatile("st.shared.u32 [%0], %1;" ::"r"(p), "r"(__builtin_bit_cast(uint32_t, r[j].r[0])) : "memory");
+      else
+        asm volatile("st.shared.u16 [%0], %1;" ::"r"(p), "h"(r[j].r[0]) : "memory");
+    }
+  }
 };
 __device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void copies_wait(int newer) {  // until all but the `newer` (1 or 2) last groups are there
@@ -335,7 +442,8 @@ __device__ __forceinline__ void store_row(const u64 (&v)[N * V / 2], T* p, bool 
 struct Rows {
   int mine, turns;     // the team's rows; the turns of its warp's loop, in which teams that lie in one warp go together
   int64_t step, row;   // row: of the first one, of all workers'
-  __device__ __forceinline__ Rows(const LnArgs& a, const Team& m, int64_t ranges, int64_t range) {
+  template <typename M>
+  __device__ __forceinline__ Rows(const LnArgs& a, const M& m, int64_t ranges, int64_t range) {
     int64_t from = range * a.teams, end = a.R;
     step = ranges * a.teams;
     if (a.rows) {
@@ -357,12 +465,13 @@ inline int ln_ahead(int rows, int threads, int bytes) { return rows > 1 && threa
 
 template <typename K>
 cudaError_t ln_launch(K kernel, std::atomic<int>& raised, const LnArgs& a, dim3 grid, size_t smem, cudaStream_t st) {
+  if (a.cl > 1 && !g_rows_clustered) g_rows_clustered = true;
   if (smem > 40 * 1024 || a.cl > 8) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (raised != dev + 1) {
-      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemPerSm - kStaticSmem);
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemPerSm - kStaticSmem<true>);
       if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
       if (e != cudaSuccess) return e;
       raised = dev + 1;
@@ -401,9 +510,14 @@ cudaError_t ln_dispatch(bool xb, bool yb, int vmax, F form) {
   return yb ? vec(f, h) : vec(f, f);
 }
 
+}  // namespace
+
 // layernorm_backward_*.cu: the backward with one activation each.
 cudaError_t launch_ln_backward_none(const LnArgs& a, int G, bool xb, bool yb, int vmax, cudaStream_t st);
 cudaError_t launch_ln_backward_relu(const LnArgs& a, int G, bool xb, bool yb, int vmax, cudaStream_t st);
 cudaError_t launch_ln_backward_silu(const LnArgs& a, int G, bool xb, bool yb, int vmax, cudaStream_t st);
+int take_ln_backward_late_none();
+int take_ln_backward_late_relu();
+int take_ln_backward_late_silu();
 
 }  // namespace lsgd

@@ -17,18 +17,18 @@ struct BwdShape {
   static constexpr int kBetas = ACT == LSGD_ACT_SILU ? 4 * E * kThreads : 0, kSums = 8 * E * kThreads;
 };
 
-template <typename XT, typename YT, int V, bool RES, int ACT, int E>
+// CLUSTER: as in the forward, the sums of row k + 1 are sent before those of row k are waited for; row k is read once more.
+template <typename XT, typename YT, int V, bool RES, int ACT, int E, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads, 2) ln_backward_kernel(const LnArgs a) {
+  using M = Team<CLUSTER>;
   using S = BwdShape<XT, YT, V, RES, ACT, E>;
   constexpr int N = S::N, H = E / 2;
   constexpr bool RELU = ACT == LSGD_ACT_RELU, SILU = ACT == LSGD_ACT_SILU;
-  __shared__ float2 stats[2 * kSlots + kExchange];
+  __shared__ float2 stats[M::kPlaces];
   extern __shared__ __align__(16) uint8_t ring[];
-  const Team m(a, V, N);
-  if (m.cl > 1) {  // every CTA's shared memory is there from here on
-    cluster_arrive();
-    cluster_wait();
-  }
+  __shared__ uint64_t bars[M::kTurns];
+  const M m(a, V, N, bars);
+  m.begin();
   pdl_begin();
   const int64_t ranges = gridDim.x / m.cl, range = blockIdx.x / m.cl;
   const Rows rows(a, m, ranges, range);
@@ -70,11 +70,13 @@ __global__ void __launch_bounds__(kThreads, 2) ln_backward_kernel(const LnArgs a
     row += rows.step;
   };
   uint32_t slot = 0, next = 0;
-  for (int d = 0; d < a.ahead; ++d, next += S::kSlot) {
+  const int early = a.ahead + (CLUSTER ? 1 : 0);
+  for (int d = 0; d < early; ++d, next += S::kSlot) {
     fetch(d, next);
     land(next);
   }
   const uint32_t last = next;
+  const auto advance = [&](uint32_t& s) { s = s == last ? 0 : s + S::kSlot; };
   fetch_stats(0);
   u64 ga[H], dga[H], dbe[H];
   load_params<V, N>(a.gamma + blockIdx.y * a.par_gs + m.col0, m, ga);
@@ -105,13 +107,8 @@ __global__ void __launch_bounds__(kThreads, 2) ln_backward_kernel(const LnArgs a
   };
   const float inv = -1.f / a.C;
   XT* out = static_cast<XT*>(a.out) + x0;
-  for (int k = 0; k < rows.turns; ++k) {
-    const float mean = next_mean, rstd = next_rstd;
-    fetch(k + a.ahead, next);
-    fetch_stats(k + 1);
-    copies_wait(a.ahead);
-    // (values behind the row's end have dz = 0)
-    u64 xh[H], t[H], s1 = 0, s2 = 0;
+  // A row's xh and dz; what lies behind its end has dz = 0.
+  const auto values = [&](uint32_t slot, float mean, float rstd, u64 (&xh)[H], u64 (&t)[H]) {
     fx.read(slot, xh);
     fd.read(slot, t);
     if constexpr (RELU) {
@@ -132,14 +129,22 @@ __global__ void __launch_bounds__(kThreads, 2) ln_backward_kernel(const LnArgs a
         const float p = sigmoid<kind>(z.x), q = sigmoid<kind>(z.y);
         t[i] = pack2(d.x * p * fmaf(z.x, 1.f - p, 1.f), d.y * q * fmaf(z.y, 1.f - q, 1.f));
       }
+    }
+  };
+  // Adds a row to dgamma and dbeta; t = gamma dz and its sums s1 and, with xh, s2.
+  const auto add = [&](u64 (&xh)[H], u64 (&t)[H], float& m1, float& m2) {
+    u64 s1 = 0, s2 = 0;
+#pragma unroll
+    for (int i = 0; i < H; ++i) {
       add2(dbe[i], t[i]);
       dga[i] = mad2(t[i], xh[i], dga[i]);
       t[i] = mul2(t[i], ga[i]);
       add2(s1, t[i]);
       s2 = mad2(t[i], xh[i], s2);
     }
-    float m1 = added(s1), m2 = added(s2);
-    m.sum_both(m1, m2, stats + (k & 1) * kSlots + m.team * m.warps);
+    m1 = added(s1), m2 = added(s2);
+  };
+  const auto finish = [&](bool on, uint32_t slot, u64 (&xh)[H], u64 (&t)[H], float m1, float m2, float rstd) {
     m1 *= inv, m2 *= inv;
     u64 e[H];
     if constexpr (RES) fs.read(slot, e);
@@ -148,12 +153,59 @@ __global__ void __launch_bounds__(kThreads, 2) ln_backward_kernel(const LnArgs a
       t[i] = mad2(xh[i], both(m2), sum2(t[i], both(m1)));
       t[i] = RES ? mad2(t[i], both(rstd), e[i]) : mul2(t[i], both(rstd));
     }
-    if (k < rows.mine) store_row<XT, V, N>(t, out, whole, left, hop);
-    if (++run == a.seg) flush();
-    land(next);
+    if (on) store_row<XT, V, N>(t, out, whole, left, hop);
     out += x_step;
-    slot = slot == last ? 0 : slot + S::kSlot;
-    next = next == last ? 0 : next + S::kSlot;
+  };
+  if constexpr (!CLUSTER) {
+    for (int k = 0; k < rows.turns; ++k, advance(slot), advance(next)) {
+      const float mean = next_mean, rstd = next_rstd;
+      fetch(k + a.ahead, next);
+      fetch_stats(k + 1);
+      copies_wait(a.ahead);
+      u64 xh[H], t[H];
+      float m1, m2;
+      values(slot, mean, rstd, xh, t);
+      add(xh, t, m1, m2);
+      if (m.slots > 1) {
+        m.post_both(m1, m2, stats, k);
+        m.collect_both(m1, m2, stats, k);
+      } else {
+        m.sum_both(m1, m2);
+      }
+      finish(k < rows.mine, slot, xh, t, m1, m2, rstd);
+      if (++run == a.seg) flush();
+      land(next);
+    }
+  } else {
+    uint32_t before = 0, coming = 0;  // the places of row k - 1, and of the row that was fetched last
+    float mean = 0.f, rstd = 0.f;     // of row k - 1
+    for (int k = 0; k <= rows.turns; ++k) {
+      u64 xh[H], t[H];
+      float m1, m2;
+      const float old_mean = mean, old_rstd = rstd;
+      if (k < rows.turns) {
+        mean = next_mean, rstd = next_rstd;
+        fetch_stats(k + 1);
+        copies_wait(a.ahead);
+        values(slot, mean, rstd, xh, t);
+        add(xh, t, m1, m2);
+        m.post_both(m1, m2, stats, k);
+        if (++run == a.seg) flush();
+      }
+      if (k) {
+        land(coming);
+        values(before, old_mean, old_rstd, xh, t);
+#pragma unroll
+        for (int i = 0; i < H; ++i) t[i] = mul2(t[i], ga[i]);
+        m.collect_both(m1, m2, stats, k - 1);
+        finish(true, before, xh, t, m1, m2, old_rstd);
+      }
+      fetch(k + early, next);
+      before = slot, coming = next;
+      advance(slot);
+      advance(next);
+    }
+    m.end();
   }
   // (the sums may stand where the rows did: every thread's copies are there, and read, before any is overwritten)
   asm volatile("cp.async.wait_all;" ::: "memory");
@@ -229,44 +281,46 @@ inline cudaError_t launch_param_grads(const LnArgs& a, int G, int ranges, cudaSt
   return run(ln_param_grad_kernel<32>, 32);
 }
 
-template <typename XT, typename YT, int V, bool RES, int ACT, int E>
-cudaError_t ln_backward_held(LnArgs a, int G, cudaStream_t st) {
+template <typename XT, typename YT, int V, bool RES, int ACT, int E, bool CLUSTER>
+cudaError_t ln_backward_as(LnArgs a, int G, cudaStream_t st) {
   static std::atomic<int> raised{0};  // device + 1 whose limits this kernel's have been raised to
   using S = BwdShape<XT, YT, V, RES, ACT, E>;
+  constexpr int more = CLUSTER ? 2 : 1, own = kStaticSmem<CLUSTER>;
   // as many CTAs to an SM as the shared memory takes with a row ahead
   const auto used = [](int ahead, bool apart) {
-    const int rows = (ahead + 1) * S::kSlot + S::kBetas;
-    return kStaticSmem + (apart ? rows + S::kSums : std::max(rows, S::kSums));
+    const int rows = (ahead + more) * S::kSlot + S::kBetas;
+    return own + (apart ? rows + S::kSums : std::max(rows, S::kSums));
   };
+  static_assert(own + (1 + more) * S::kSlot + S::kBetas + S::kSums <= kSmemPerSm, "one CTA with a row ahead fits");
   a.seg = 64;
-  LnPlan p = ln_plan(G, a.R, a.C, E, kSmemPerSm / used(1, false));
+  LnPlan p = ln_plan(G, a.R, a.C, E, std::max(1, kSmemPerSm / used(1, false)));
   const bool apart = p.rows >= a.seg;  // sums that are added to while rows are under way
-  if (apart) p = ln_plan(G, a.R, a.C, E, kSmemPerSm / used(1, true));
-  const int threads = p.T * p.teams, per_sm = std::min(std::max(1, kThreadsPerSm / threads), kSmemPerSm / used(1, apart));
+  if (apart) p = ln_plan(G, a.R, a.C, E, std::max(1, kSmemPerSm / used(1, true)));
+  const int threads = p.T * p.teams;
+  const int per_sm = std::max(1, std::min(kThreadsPerSm / threads, kSmemPerSm / used(1, apart)));
   a.T = p.T, a.teams = p.teams, a.cl = p.cl, a.slice = p.slice, a.rows = (int)p.rows;
   a.ahead = S::X::kAsync && S::Y::kAsync && per_sm * used(2, apart) <= kSmemPerSm
                 ? ln_ahead(p.rows, per_sm * threads, S::kSlot / kThreads) : 1;
-  a.sums = apart ? (a.ahead + 1) * S::kSlot + S::kBetas : 0;
+  a.sums = apart ? (a.ahead + more) * S::kSlot + S::kBetas : 0;
   cudaError_t e = cudaSuccess;
   if (a.R)
-    e = ln_launch(ln_backward_kernel<XT, YT, V, RES, ACT, E>, raised, a, dim3((unsigned)(p.ranges * p.cl), G),
-                  used(a.ahead, apart) - kStaticSmem, st);
+    e = ln_launch(ln_backward_kernel<XT, YT, V, RES, ACT, E, CLUSTER>, raised, a, dim3((unsigned)(p.ranges * p.cl), G),
+                  used(a.ahead, apart) - own, st);
   if (e != cudaSuccess || p.ranges == 1) return e;
   return launch_param_grads(a, G, (int)p.ranges, st);
 }
-// 16 values to a thread; 8 where all is fp32 and a CTA holds a row so (as many bytes in shared memory), and where single bf16 values go
-// through registers.
+// 16 values to a thread; 8 where all is fp32 and a CTA holds a row so or CTAs of 16 do not (as many bytes in shared memory), and where
+// single bf16 values go through registers.
 template <typename XT, typename YT, int V, bool RES, int ACT>
 cudaError_t ln_backward(const LnArgs& a, int G, cudaStream_t st) {
   constexpr bool direct = !Feed<XT, V, 1>::kAsync || !Feed<YT, V, 1>::kAsync;
-  if constexpr (direct) {
-    return ln_backward_held<XT, YT, V, RES, ACT, 8>(a, G, st);
-  } else {
-    if constexpr (sizeof(XT) + sizeof(YT) == 8) {
-      if (a.C <= 8 * kThreads) return ln_backward_held<XT, YT, V, RES, ACT, 8>(a, G, st);
-    }
-    return ln_backward_held<XT, YT, V, RES, ACT, 16>(a, G, st);
+  constexpr bool fp32 = sizeof(XT) + sizeof(YT) == 8;
+  constexpr int E = direct ? 8 : 16;
+  if constexpr (!direct && fp32) {
+    if (a.C <= 8 * kThreads) return ln_backward_as<XT, YT, V, RES, ACT, 8, false>(a, G, st);
   }
+  return a.C > E * kThreads ? ln_backward_as<XT, YT, V, RES, ACT, fp32 ? 8 : E, true>(a, G, st)
+                            : ln_backward_as<XT, YT, V, RES, ACT, E, false>(a, G, st);
 }
 
 template <int ACT>

@@ -4,4 +4,5 @@ namespace lsgd {
 cudaError_t launch_ln_backward_relu(const LnArgs& a, int G, bool xb, bool yb, int vmax, cudaStream_t st) {
   return ln_backward_any<LSGD_ACT_RELU>(a, G, xb, yb, vmax, st);
 }
+int take_ln_backward_late_relu() { return take_rows_late(); }
 }  // namespace lsgd

@@ -468,6 +468,8 @@ int tc_take_timeout_flag();
 int direction_take_timeout_flag();
 // ... and of lsgd_groupnorm_forward and _backward (groupnorm.cu).
 int norm_take_timeout_flag();
+// ... and of lsgd_layernorm_forward and _backward (layernorm.cu).
+int rows_take_timeout_flag();
 // One bounded mbarrier wait (the GEMM's mbar_wait) with the given cycle limit (<= the GEMM's):
 // *out (device) = 1 if the phase completed (arrive != 0), 0 if the wait ran out.
 cudaError_t launch_bounded_wait_selftest(long long limit_cycles, int arrive, int* out,
