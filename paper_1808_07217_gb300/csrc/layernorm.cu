@@ -32,7 +32,7 @@ namespace {
 // ---- forward ----
 // E: values of a row in a thread.  CLUSTER: a row's CTAs exchange their sums over the cluster's network, which takes about as long as a row:
 // the sums of row k + 1 are formed and sent before those of row k are waited for, and row k is read from shared memory once more.
-// (2,000 x 17,000 in bf16 with a residual: 136 us with the cluster's barrier in every row, 111 with the exchange alone, %%% so.)
+// (4 x 2,000 x 6,000 in bf16 with a residual: 110 us with the cluster's barrier in every row, 92 with the exchange alone, 86 so.)
 template <typename XT, typename YT, int V, bool RES, int E, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads, 2) ln_forward_kernel(const LnArgs a) {
   constexpr int N = E / V, H = E / 2;
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(kThreads, 2) ln_forward_kernel(const LnArgs a)
 #pragma unroll
           for (int i = 0; i < H; ++i) {
             const float2 z = unpack2(v[i]);
-            constexpr int kind = sizeof(YT) == 2 ? kFast : kExact;
+            constexpr int kind = sizeof(YT) == 2 ? kFast : kClose;
             v[i] = pack2(activate<kind, decltype(act)::value>(z.x), activate<kind, decltype(act)::value>(z.y));
           }
         });
@@ -192,12 +192,16 @@ cudaError_t ln_forward_as(LnArgs a, int G, cudaStream_t st) {
   using In = Feed<XT, V, E / V>;
   constexpr int slot = In::kSlot * (RES ? 2 : 1), more = CLUSTER ? 2 : 1, own = kStaticSmem<CLUSTER>;
   constexpr int fit = kSmemPerSm / ((1 + more) * slot + own);
-  const LnPlan p = ln_plan(G, a.R, a.C, E, fit);
+  const auto kernel = ln_forward_kernel<XT, YT, V, RES, E, CLUSTER>;
+  LnPlan p = ln_plan(G, a.R, a.C, E, fit);
+  if constexpr (CLUSTER) {
+    static ClusterCounts counts;
+    p = ln_plan(G, a.R, a.C, E, fit, ln_clusters(kernel, raised, counts, p.T * p.teams, (1 + more) * slot, p.cl));
+  }
   const int threads = p.T * p.teams, per_sm = std::min(std::max(1, kThreadsPerSm / threads), fit);
   a.T = p.T, a.teams = p.teams, a.cl = p.cl, a.slice = p.slice;
   a.ahead = In::kAsync && per_sm * ((2 + more) * slot + own) <= kSmemPerSm ? ln_ahead(p.rows, per_sm * threads, slot / kThreads) : 1;
-  return ln_launch(ln_forward_kernel<XT, YT, V, RES, E, CLUSTER>, raised, a, dim3((unsigned)(p.ranges * p.cl), G),
-                   (a.ahead + more) * slot, st);
+  return ln_launch(kernel, raised, a, dim3((unsigned)(p.ranges * p.cl), G), (a.ahead + more) * slot, st);
 }
 // 16 values to a thread; 8 where single bf16 values go through registers, 32 of which they would take with a residual (32,768 x 1531:
 // 214 and 122 us).

@@ -68,8 +68,9 @@ struct LnPlan {
   int64_t rows;    // rows of a team at most
 };
 
-// per_sm: CTAs that an SM holds at once; 0: as many as its threads allow.
-inline LnPlan ln_plan(int G, int64_t R, int C, int E, int per_sm = 0) {
+// per_sm: CTAs that an SM holds at once (0: as many as its threads allow); clusters: of those that the GPU holds at once (0: as many as
+// the SMs' CTAs make).
+inline LnPlan ln_plan(int G, int64_t R, int C, int E, int per_sm = 0, int clusters = 0) {
   LnPlan p;
   p.cl = (C + E * kThreads - 1) / (E * kThreads);
   p.slice = ((C + p.cl - 1) / p.cl + E - 1) / E * E;
@@ -81,7 +82,8 @@ inline LnPlan ln_plan(int G, int64_t R, int C, int E, int per_sm = 0) {
   p.teams = std::max(1, kThreads / p.T);
   const int by_threads = std::max(1, kThreadsPerSm / (p.T * p.teams));
   const int64_t slots = (int64_t)kNumSMs * (per_sm ? std::min(per_sm, by_threads) : by_threads);
-  const int64_t most = std::max<int64_t>(1, slots / ((int64_t)G * p.cl));
+  const int64_t at_once = clusters ? std::min<int64_t>(clusters, slots / p.cl) : slots / p.cl;
+  const int64_t most = std::max<int64_t>(1, at_once / G);
   const int64_t turns = (R + p.teams - 1) / p.teams;  // of a CTA's teams, if there were one CTA
   p.rows = std::max<int64_t>(1, (turns + most - 1) / most);
   p.ranges = (turns + p.rows - 1) / p.rows;
@@ -463,33 +465,68 @@ struct Rows {
 // 1534 in fp32, of 24 KB, 71 with two and 74 with one.
 inline int ln_ahead(int rows, int threads, int bytes) { return rows > 1 && threads * bytes <= 28 * 1024 ? 2 : 1; }
 
+cudaLaunchConfig_t ln_config(cudaLaunchAttribute (&attr)[2], dim3 grid, int threads, size_t smem, int cl, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cl;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cl > 1 ? 2 : 1;
+  return cfg;
+}
+
+// A kernel's limits raised to what the largest call needs.
+template <typename K>
+cudaError_t ln_raise(K kernel, std::atomic<int>& raised) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || raised == dev + 1) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemPerSm - kStaticSmem<true>);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess) raised = dev + 1;
+  return e;
+}
+
+// The clusters that the GPU holds at once (a cluster lies in one GPC, whose SMs are mostly no multiple of it: 2,000 x 17,000 in bf16,
+// clusters of 5 with two CTAs to an SM, took 107 us with the 60 that the SMs' CTAs make and takes 72 with as many as are held at
+// once).  0 if unknown.  The answers are kept by the launch's shape.
+struct ClusterCounts {
+  std::atomic<uint64_t> known[16] = {};
+};
+template <typename K>
+int ln_clusters(K kernel, std::atomic<int>& raised, ClusterCounts& counts, int threads, size_t smem, int cl) {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || ln_raise(kernel, raised) != cudaSuccess) return 0;
+  const uint64_t key = ((((uint64_t)dev * 32 + cl) * 2048 + threads) * (1 << 18) + smem) + 1;
+  std::atomic<uint64_t>& at = counts.known[(key ^ (key >> 18) ^ (key >> 29)) % 16];
+  const uint64_t known = at;
+  if (known >> 12 == key) return (int)(known & 4095);
+  cudaLaunchAttribute attr[2];
+  const cudaLaunchConfig_t cfg = ln_config(attr, dim3(cl), threads, smem, cl, nullptr);
+  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;
+  }
+  n = std::min(n, 4095);
+  at = key << 12 | (uint64_t)n;
+  return n;
+}
+
 template <typename K>
 cudaError_t ln_launch(K kernel, std::atomic<int>& raised, const LnArgs& a, dim3 grid, size_t smem, cudaStream_t st) {
   if (a.cl > 1 && !g_rows_clustered) g_rows_clustered = true;
   if (smem > 40 * 1024 || a.cl > 8) {
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+    const cudaError_t e = ln_raise(kernel, raised);
     if (e != cudaSuccess) return e;
-    if (raised != dev + 1) {
-      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemPerSm - kStaticSmem<true>);
-      if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-      if (e != cudaSuccess) return e;
-      raised = dev + 1;
-    }
   }
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(a.T * a.teams);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
   cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = a.cl;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = a.cl > 1 ? 2 : 1;
+  const cudaLaunchConfig_t cfg = ln_config(attr, grid, a.T * a.teams, smem, a.cl, st);
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 

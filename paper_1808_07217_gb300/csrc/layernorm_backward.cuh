@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kThreads, 2) ln_backward_kernel(const LnArgs a
     for (int i = 0; i < H; ++i) {
       xh[i] = mul2(sum2(xh[i], both(-mean)), both(rstd));
       if constexpr (SILU) {
-        constexpr int kind = sizeof(XT) == 4 ? kExact : kSums;
+        constexpr int kind = sizeof(XT) == 4 ? kClose : kSums;
         const float2 z = unpack2(mad2(xh[i], ga[i], betas[i * kThreads])), d = unpack2(t[i]);
         const float p = sigmoid<kind>(z.x), q = sigmoid<kind>(z.y);
         t[i] = pack2(d.x * p * fmaf(z.x, 1.f - p, 1.f), d.y * q * fmaf(z.y, 1.f - q, 1.f));
@@ -293,9 +293,19 @@ cudaError_t ln_backward_as(LnArgs a, int G, cudaStream_t st) {
   };
   static_assert(own + (1 + more) * S::kSlot + S::kBetas + S::kSums <= kSmemPerSm, "one CTA with a row ahead fits");
   a.seg = 64;
-  LnPlan p = ln_plan(G, a.R, a.C, E, std::max(1, kSmemPerSm / used(1, false)));
+  const auto kernel = ln_backward_kernel<XT, YT, V, RES, ACT, E, CLUSTER>;
+  const auto plan = [&](bool apart) {
+    const int fit = std::max(1, kSmemPerSm / used(1, apart));
+    LnPlan p = ln_plan(G, a.R, a.C, E, fit);
+    if constexpr (CLUSTER) {
+      static ClusterCounts counts;
+      p = ln_plan(G, a.R, a.C, E, fit, ln_clusters(kernel, raised, counts, p.T * p.teams, used(1, apart) - own, p.cl));
+    }
+    return p;
+  };
+  LnPlan p = plan(false);
   const bool apart = p.rows >= a.seg;  // sums that are added to while rows are under way
-  if (apart) p = ln_plan(G, a.R, a.C, E, std::max(1, kSmemPerSm / used(1, true)));
+  if (apart) p = plan(true);
   const int threads = p.T * p.teams;
   const int per_sm = std::max(1, std::min(kThreadsPerSm / threads, kSmemPerSm / used(1, apart)));
   a.T = p.T, a.teams = p.teams, a.cl = p.cl, a.slice = p.slice, a.rows = (int)p.rows;
@@ -304,8 +314,7 @@ cudaError_t ln_backward_as(LnArgs a, int G, cudaStream_t st) {
   a.sums = apart ? (a.ahead + more) * S::kSlot + S::kBetas : 0;
   cudaError_t e = cudaSuccess;
   if (a.R)
-    e = ln_launch(ln_backward_kernel<XT, YT, V, RES, ACT, E, CLUSTER>, raised, a, dim3((unsigned)(p.ranges * p.cl), G),
-                  used(a.ahead, apart) - own, st);
+    e = ln_launch(kernel, raised, a, dim3((unsigned)(p.ranges * p.cl), G), used(a.ahead, apart) - own, st);
   if (e != cudaSuccess || p.ranges == 1) return e;
   return launch_param_grads(a, G, (int)p.ranges, st);
 }

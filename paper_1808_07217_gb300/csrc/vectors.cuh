@@ -125,11 +125,18 @@ struct Vec {
 // reciprocal, 2^-23 off.  kFast: the fast exponential too, 2^-21 and |z| 2^-23 off, which a bf16 result's rounding of 2^-8 hides: y
 // (54.9 against 56.9 us for 8 images of 127 x 129 x 320, whose second pass the special function unit bounds) and the split form's
 // dx.  The fast reciprocal flushes what is below 2^-126: y is 0 from z = -87.3 on, where it is 1e-36 at most.
-enum { kFast, kSums, kExact };
+// kClose (layer norm's fp32 results): the accurate exponential, and the fast reciprocal with a step of Newton's iteration, which leaves
+// half a unit in the last place (a quotient takes a dozen instructions more).
+enum { kFast, kSums, kExact, kClose };
 template <int KIND>
 __device__ __forceinline__ float sigmoid(float z) {
   if constexpr (KIND == kExact) return 1.f / (1.f + expf(-z));
   float e, r;
+  if constexpr (KIND == kClose) {
+    const float d = 1.f + expf(-z);
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(d));
+    return d < 1e30f ? fmaf(r, fmaf(-d, r, 1.f), r) : r;  // (infinity: 0)
+  }
   if constexpr (KIND == kSums) e = expf(-z);
   else asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.44269504f));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
