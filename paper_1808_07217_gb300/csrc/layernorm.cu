@@ -193,10 +193,10 @@ cudaError_t ln_forward_as(LnArgs a, int G, cudaStream_t st) {
   constexpr int slot = In::kSlot * (RES ? 2 : 1), more = CLUSTER ? 2 : 1, own = kStaticSmem<CLUSTER>;
   constexpr int fit = kSmemPerSm / ((1 + more) * slot + own);
   const auto kernel = ln_forward_kernel<XT, YT, V, RES, E, CLUSTER>;
-  LnPlan p = ln_plan(G, a.R, a.C, E, fit);
+  LnPlan p = ln_plan(G, a.R, a.C, E, 0, fit);
   if constexpr (CLUSTER) {
     static ClusterCounts counts;
-    p = ln_plan(G, a.R, a.C, E, fit, ln_clusters(kernel, raised, counts, p.T * p.teams, (1 + more) * slot, p.cl));
+    p = ln_plan(G, a.R, a.C, E, 0, fit, ln_clusters(kernel, raised, counts, p.T * p.teams, (1 + more) * slot, p.cl));
   }
   const int threads = p.T * p.teams, per_sm = std::min(std::max(1, kThreadsPerSm / threads), fit);
   a.T = p.T, a.teams = p.teams, a.cl = p.cl, a.slice = p.slice;
@@ -220,7 +220,7 @@ int ln_vec(int v, int64_t rows, int64_t ld, const void* p, int z) {
 // Enough for the backward of any types and vectors.
 size_t ln_workspace(int G, int64_t R, int C) {
   int64_t most = 1;
-  for (int E : {8, 16}) most = std::max(most, ln_plan(G, R, C, E).ranges);
+  for (int E : {8, 16}) most = std::max(most, ln_plan(G, R, C, E, kFewRows).ranges);
   return most > 1 ? (size_t)G * most * C * 8 : 0;
 }
 

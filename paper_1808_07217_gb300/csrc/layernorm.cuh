@@ -68,9 +68,9 @@ struct LnPlan {
   int64_t rows;    // rows of a team at most
 };
 
-// per_sm: CTAs that an SM holds at once (0: as many as its threads allow); clusters: of those that the GPU holds at once (0: as many as
+// few: as many rows of a team stay with one CTA; per_sm: CTAs that an SM holds at once (0: as many as its threads allow); clusters: of those that the GPU holds at once (0: as many as
 // the SMs' CTAs make).
-inline LnPlan ln_plan(int G, int64_t R, int C, int E, int per_sm = 0, int clusters = 0) {
+inline LnPlan ln_plan(int G, int64_t R, int C, int E, int few, int per_sm = 0, int clusters = 0) {
   LnPlan p;
   p.cl = (C + E * kThreads - 1) / (E * kThreads);
   p.slice = ((C + p.cl - 1) / p.cl + E - 1) / E * E;
@@ -86,6 +86,7 @@ inline LnPlan ln_plan(int G, int64_t R, int C, int E, int per_sm = 0, int cluste
   const int64_t most = std::max<int64_t>(1, at_once / G);
   const int64_t turns = (R + p.teams - 1) / p.teams;  // of a CTA's teams, if there were one CTA
   p.rows = std::max<int64_t>(1, (turns + most - 1) / most);
+  if (turns <= few) p.rows = std::max<int64_t>(1, turns);
   p.ranges = (turns + p.rows - 1) / p.rows;
   return p;
 }
@@ -439,6 +440,10 @@ __device__ __forceinline__ void store_row(const u64 (&v)[N * V / 2], T* p, bool 
       if (left > j * hop) o[j].store_first(p + j * hop, left - j * hop);
   }
 }
+// Rows of a team that one CTA of the backward takes by itself: more CTAs would need the second kernel, whose launch takes about as long
+// as four rows and a quarter of the call's host time (3 x 20 x 600: 22.9 us a call with it, 18.3 without).
+constexpr int kFewRows = 4;
+
 // The rows that fall to a team.  Forward: every step-th of the worker's, so that all CTAs together walk through memory; backward: one of
 // the CTA's `rows` x teams neighbouring ones (32,768 x 2048 in bf16: 95 us, with every step-th 108; the forward 84 and 82).
 struct Rows {

@@ -296,13 +296,13 @@ cudaError_t ln_backward_as(LnArgs a, int G, cudaStream_t st) {
   const auto kernel = ln_backward_kernel<XT, YT, V, RES, ACT, E, CLUSTER>;
   const auto plan = [&](bool apart) {
     const int fit = std::max(1, kSmemPerSm / used(1, apart));
-    LnPlan p = ln_plan(G, a.R, a.C, E, fit);
+    LnPlan p = ln_plan(G, a.R, a.C, E, kFewRows, fit);
     if constexpr (CLUSTER) {
       static ClusterCounts counts;
       // A sixteenth fewer of more than two CTAs: behind the parameters' kernel they are not placed as densely as they could be
       // (2,000 x 17,000: 104 us with 58, 84 with 55; 3,000 x 9,000: 99 with 97, 72 with 92).
       const int n = ln_clusters(kernel, raised, counts, p.T * p.teams, used(1, apart) - own, p.cl);
-      p = ln_plan(G, a.R, a.C, E, fit, p.cl > 2 ? n - n / 16 : n);
+      p = ln_plan(G, a.R, a.C, E, kFewRows, fit, p.cl > 2 ? n - n / 16 : n);
     }
     return p;
   };

@@ -111,12 +111,12 @@ def _clip(L, h, norm=C, max_norm=1.0, ws=4 * BIG, need=None):
             n.value)
 
 
-LONG = (A, None, 300_000, 300_000, 0, 0, 0)
+LONG = (A, None, 3_000_000, 3_000_000, 0, 0, 0)
 
 
 @pytest.mark.parametrize("kw", [dict(norm=0), dict(norm=C + 2), dict(max_norm=0.0), dict(max_norm=-1.0), dict(max_norm=float("nan")),
                                 dict(max_norm=float("inf")), dict(ws=0), dict(ws=4 * BIG + 8), dict(need=8),
-                                dict(norm=A), dict(norm=A + 8 * 300_000 - 4), dict(ws=A + 64), dict(norm=4 * BIG)])
+                                dict(norm=A), dict(norm=A + 8 * 3_000_000 - 4), dict(ws=A + 64), dict(norm=4 * BIG)])
 def test_clip_refused(L, kw):
     s, h = _list(L, [LONG])
     assert s == L.OK
