@@ -239,14 +239,13 @@ __global__ void __launch_bounds__(kThreads, 2) ln_backward_kernel(const LnArgs a
   }
 }
 
-// dgamma and dbeta from the ranges' sums part [G][ranges][2][C] (none: zeros).  32 columns of a worker to a block; each of its TY rows
-// of threads adds every TY-th range, and these are added in pairs.
-template <int TY>
-__global__ void __launch_bounds__(32 * TY) ln_param_grad_kernel(const float* part, int ranges, int C, int64_t par_gs, float* dgamma,
+// dgamma and dbeta from the ranges' sums part [G][ranges][2][C] (none: zeros).  TX columns of a worker to a block; each of its TY rows of
+// threads adds every TY-th range, and these are added in pairs.
+template <int TX, int TY>
+__global__ void __launch_bounds__(TX * TY) ln_param_grad_kernel(const float* part, int ranges, int C, int64_t par_gs, float* dgamma,
                                                                  float* dbeta) {
   pdl_begin();
-  __shared__ float2 red[TY][32];
-  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = blockIdx.x * 32 + tx;
+  const int tx = threadIdx.x % TX, ty = threadIdx.x / TX, c = blockIdx.x * TX + tx;
   const float* p = part + (int64_t)blockIdx.y * ranges * 2 * C + c;
   float2 v = make_float2(0.f, 0.f);
   if (c < C) {
@@ -256,29 +255,36 @@ __global__ void __launch_bounds__(32 * TY) ln_param_grad_kernel(const float* par
       v.y += __ldg(p + (int64_t)i * 2 * C + C);
     }
   }
-  for (int half = TY / 2; half; half /= 2) {
-    red[ty][tx] = v;
-    __syncthreads();
-    if (ty < half) {
-      v.x += red[ty + half][tx].x;
-      v.y += red[ty + half][tx].y;
+  if constexpr (TY > 1) {
+    __shared__ float2 red[TY][TX];
+    for (int half = TY / 2; half; half /= 2) {
+      red[ty][tx] = v;
+      __syncthreads();
+      if (ty < half) {
+        v.x += red[ty + half][tx].x;
+        v.y += red[ty + half][tx].y;
+      }
+      __syncthreads();
     }
-    __syncthreads();
   }
   if (ty == 0 && c < C) {
     dgamma[blockIdx.y * par_gs + c] = v.x;
     dbeta[blockIdx.y * par_gs + c] = v.y;
   }
 }
-// About eight ranges to a thread: with 32 rows of threads for any number, 19 ranges of 16 x 4096 columns took 20 us of idle threads.
+// As few rows of threads as keep the SMs busy and no thread's chain above 64 ranges: with 32 for any number, 19 ranges of 16 x 4096
+// columns took 20 us of idle threads, with 4, 3 ranges of 30 x 11,000 took 12 us.
 inline cudaError_t launch_param_grads(const LnArgs& a, int G, int ranges, cudaStream_t st) {
-  const auto run = [&](auto kernel, int ty) {
-    return launch_pdl(kernel, dim3((a.C + 31) / 32, G), dim3(32 * ty), 0, st, (const float*)a.part, ranges, a.C, a.par_gs, a.dgamma,
+  const auto run = [&](auto kernel, int tx, int ty) {
+    return launch_pdl(kernel, dim3((a.C + tx - 1) / tx, G), dim3(tx * ty), 0, st, (const float*)a.part, ranges, a.C, a.par_gs, a.dgamma,
                       a.dbeta);
   };
-  if (ranges <= 32) return run(ln_param_grad_kernel<4>, 4);
-  if (ranges <= 128) return run(ln_param_grad_kernel<16>, 16);
-  return run(ln_param_grad_kernel<32>, 32);
+  const int64_t columns = (int64_t)G * a.C;
+  const auto enough = [&](int ty) { return ranges <= 4 * ty || (ranges <= 64 * ty && columns * ty >= kNumSMs * 512); };
+  if (enough(1)) return run(ln_param_grad_kernel<128, 1>, 128, 1);
+  if (enough(4)) return run(ln_param_grad_kernel<64, 4>, 64, 4);
+  if (enough(16)) return run(ln_param_grad_kernel<32, 16>, 32, 16);
+  return run(ln_param_grad_kernel<32, 32>, 32, 32);
 }
 
 template <typename XT, typename YT, int V, bool RES, int ACT, int E, bool CLUSTER>
