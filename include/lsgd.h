@@ -526,7 +526,8 @@ lsgd_status lsgd_groupnorm_backward(const void* x, int x_type, const void* y, co
  * done), G R <= 2^36; any C, strides >= C and any alignment of at least the element's (vectors of up to 16 bytes are used where
  * strides and pointers allow).  LSGD_EINVAL on anything else and where what is written overlaps any other tensor (rows
  * count from the first row's first to the last row's last value).  Device pointers, asynchronous on `stream`, which belongs
- * to the current device. */
+ * to the current device; lsgd_device_status reports a device-side wait that ran out (the CTAs that share a row of more than
+ * 2048 values wait for one another). */
 lsgd_status lsgd_layernorm_forward(const void* x, const void* r, int x_type, int64_t x_ld,
                                    const float* gamma, const float* beta, int64_t par_gs, void* s,
                                    void* y, int y_type, int64_t y_ld, float* mean, float* rstd, int G,
@@ -560,7 +561,7 @@ lsgd_status lsgd_layernorm_backward(const void* x, int x_type, int64_t x_ld, con
  * their places.  The tensors may be of any sizes, alignments and strides >= n, e.g. the pieces of a replica-major buffer; with one
  * worker the strides are not looked at.  It keeps the addresses, nothing of the values, is not changed by any call and
  * may be used by several calls and threads at once; lsgd_tensors_destroy (NULL is fine) when no more calls are made with it (captured
- * graphs keep what they need).  At most 65535 workers, 2^24 tensors times workers, 2^42 bytes a worker.
+ * graphs keep what they need).  At most 65535 workers, 2^22 tensors times workers, 2^42 bytes a worker.
  *
  * lsgd_gradient_norm writes norm [G] (fp32); lsgd_gradient_clip writes norm (before clipping) and the clipped gradients.  Squares are
  * summed in 64 bits in a fixed order: deterministic, and no finite gradient overflows or vanishes (a norm above fp32's range is

@@ -611,8 +611,8 @@ lsgd_status lsgd_tensors_create(const lsgd_tensor* tensors, int count, int G, ls
   using namespace lsgd;
   const char* fn = "lsgd_tensors_create";
   if (!tensors || !out || count < 1) return gr_error(LSGD_EINVAL, fn, "tensors or out is NULL, or count below 1");
-  if (G < 1 || G > 65535 || (int64_t)count * G > (1 << 24))
-    return gr_error(LSGD_EINVAL, fn, "at least 1 and at most 65535 workers, at most 2^24 tensors of all workers");
+  if (G < 1 || G > 65535 || (int64_t)count * G > (1 << 22))
+    return gr_error(LSGD_EINVAL, fn, "at least 1 and at most 65535 workers, at most 2^22 tensors of all workers");
   int places = 0;
   int64_t bytes = 0;  // of a worker
   for (int i = 0; i < count; ++i) {
@@ -680,7 +680,7 @@ lsgd_status lsgd_tensors_create(const lsgd_tensor* tensors, int count, int G, ls
       throw;
     }
     *out = l;
-  } catch (const std::bad_alloc&) {
+  } catch (...) {  // (what the containers throw)
     return gr_error(LSGD_ENOMEM, fn, "out of host memory");
   }
   return LSGD_OK;

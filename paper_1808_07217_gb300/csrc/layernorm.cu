@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(kThreads, 2) ln_forward_kernel(const LnArgs a)
   __shared__ float4 stats[M::kPlaces];
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ uint64_t bars[M::kTurns];
-  const M m(a, V, N, bars);
+  M m(a, V, N, bars);
   m.begin();
   pdl_begin();
   const Rows rows(a, m, gridDim.x / m.cl, blockIdx.x / m.cl);

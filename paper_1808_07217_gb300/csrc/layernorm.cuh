@@ -3,6 +3,7 @@
 #pragma once
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <type_traits>
 
 #include "../../include/lsgd.h"
@@ -117,8 +118,8 @@ __device__ __forceinline__ void send(const float4* at, const uint64_t* bar, int 
                "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "r"(peer_address(bar, rank))
                : "memory");
 }
-// Until the bytes of the phase are there, or, after about 2 s, never: the flag is set, and what follows is wrong, but ends.
-__device__ __forceinline__ void wait_bytes(uint64_t* bar, uint32_t parity) {
+// Whether the bytes of the phase came; not within about 2 s: the flag is set.
+__device__ __forceinline__ bool wait_bytes(uint64_t* bar, uint32_t parity) {
   const auto there = [&] {
     uint32_t ok;
     asm volatile(
@@ -129,13 +130,14 @@ __device__ __forceinline__ void wait_bytes(uint64_t* bar, uint32_t parity) {
         : "memory");
     return ok != 0;
   };
-  if (there()) return;
+  if (there()) return true;
   const long long t0 = clock64();
   while (!there())
     if (clock64() - t0 > 4000000000LL) {
       atomicExch(&g_rows_late, 1);
-      return;
+      return false;
     }
+  return true;
 }
 
 // A thread's place, and what its team shares.  The row's warps exchange their sums in two halves, post and collect, through one of kTurns
@@ -149,6 +151,7 @@ struct Team {
   int col0, Cs;    // the CTA's columns
   int n;           // the warp's (or smaller team's) columns
   uint64_t* bars;  // a cluster's: [kTurns]
+  bool lost = false;  // a wait ran out: what follows is wrong, and waits no more
   __device__ __forceinline__ Team(const LnArgs& a, int vec, int vecs, uint64_t* cluster_bars) {
     T = a.T, team = threadIdx.x / T, t = threadIdx.x - team * T, lane = threadIdx.x & 31;
     warps = T < 32 ? 1 : T / 32, warp = T < 32 ? 0 : t / 32;
@@ -192,10 +195,10 @@ struct Team {
     if constexpr (CLUSTER) cluster_meet();
   }
   // What the row's warps posted (`bytes` each) is there; k counts the rows.
-  __device__ __forceinline__ void meet(int k, int bytes) const {
+  __device__ __forceinline__ void meet(int k, int bytes) {
     if constexpr (CLUSTER) {
       if (threadIdx.x == 0) mbar_expect_tx(bars + k % kTurns, slots * bytes);
-      wait_bytes(bars + k % kTurns, (k / kTurns) & 1);
+      if (!lost) lost = !wait_bytes(bars + k % kTurns, (k / kTurns) & 1);
     } else {
       team_barrier(team + 1, T);
     }
@@ -210,7 +213,7 @@ struct Team {
       if (lane == 0) stat[warp] = mine;
     }
   }
-  __device__ __forceinline__ void collect_moments(float& mean, float& q, float inv_C, const float4* stats, int k) const {
+  __device__ __forceinline__ void collect_moments(float& mean, float& q, float inv_C, const float4* stats, int k) {
     const float4* stat = stats + k % kTurns * kSlots + team * warps;
     meet(k, 16);
     float s = 0.f;
@@ -249,7 +252,7 @@ struct Team {
       if ((lane & 15) == 0) (lane ? stat[warp].y : stat[warp].x) = v;
     }
   }
-  __device__ __forceinline__ void collect_both(float& p, float& q, const float2* stats, int k) const {
+  __device__ __forceinline__ void collect_both(float& p, float& q, const float2* stats, int k) {
     const float2* stat = stats + k % kTurns * kSlots + team * warps;
     meet(k, 8);
     p = q = 0.f;

@@ -27,7 +27,7 @@ __global__ void __launch_bounds__(kThreads, 2) ln_backward_kernel(const LnArgs a
   __shared__ float2 stats[M::kPlaces];
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ uint64_t bars[M::kTurns];
-  const M m(a, V, N, bars);
+  M m(a, V, N, bars);
   m.begin();
   pdl_begin();
   const int64_t ranges = gridDim.x / m.cl, range = blockIdx.x / m.cl;
@@ -298,7 +298,6 @@ cudaError_t ln_backward_as(LnArgs a, int G, cudaStream_t st) {
     return own + (apart ? rows + S::kSums : std::max(rows, S::kSums));
   };
   static_assert(own + (1 + more) * S::kSlot + S::kBetas + S::kSums <= kSmemPerSm, "one CTA with a row ahead fits");
-  a.seg = 64;
   const auto kernel = ln_backward_kernel<XT, YT, V, RES, ACT, E, CLUSTER>;
   const auto plan = [&](bool apart) {
     const int fit = std::max(1, kSmemPerSm / used(1, apart));
@@ -313,8 +312,9 @@ cudaError_t ln_backward_as(LnArgs a, int G, cudaStream_t st) {
     return p;
   };
   LnPlan p = plan(false);
-  const bool apart = p.rows >= a.seg;  // sums that are added to while rows are under way
+  const bool apart = p.rows >= 64;  // sums that are added to while rows are under way
   if (apart) p = plan(true);
+  a.seg = std::max(64, (int)std::ceil(std::sqrt((double)p.rows)));  // no chain of additions is longer than this
   const int threads = p.T * p.teams;
   const int per_sm = std::max(1, std::min(kThreadsPerSm / threads, kSmemPerSm / used(1, apart)));
   a.T = p.T, a.teams = p.teams, a.cl = p.cl, a.slice = p.slice, a.rows = (int)p.rows;

@@ -389,3 +389,58 @@ def test_a_captured_call_keeps_its_workspace_to_itself(P, which):
         torch.cuda.synchronize()
         assert all((t == 9).all() for t in later)
         assert all(torch.equal(t, w) for t, w in zip(outs, want))
+
+
+@pytest.mark.gpu
+def test_tensors_beyond_32_bits(P):
+    import torch
+
+    n = (1 << 31) + 12345
+    g = torch.full((1, n), 0.5, dtype=torch.bfloat16, device="cuda")
+    g[0, -7:] = 1000.0
+    out, norm = torch.empty_like(g), torch.empty(1, device="cuda")
+    P.lsgd_gradient_clip(P.lsgd_tensors_create([g], [out]), norm, 100.0)
+    want = np.sqrt(0.25 * (n - 7) + 7e6)
+    assert abs(float(norm) - want) <= NORM * want
+    f = np.float32(100.0) / norm.cpu().numpy()[0]
+    assert torch.equal(out[0, -5000:], (g[0, -5000:].float() * float(f)).bfloat16())
+    assert int((out[0, :-7] == out[0, 0]).sum()) == n - 7
+
+
+SCRIPT = """
+import torch
+import paper_1808_07217_gb300 as P
+x = torch.randn(40, 6000, device="cuda").bfloat16()
+ga, be = torch.ones(1, 6000, device="cuda"), torch.zeros(1, 6000, device="cuda")
+y, dx, m, r = torch.empty_like(x), torch.empty_like(x), torch.empty(40, device="cuda"), torch.empty(40, device="cuda")
+dg, db, norm = torch.empty(1, 6000, device="cuda"), torch.empty(1, 6000, device="cuda"), torch.empty(1, device="cuda")
+g = torch.randn(1, 3000000, device="cuda")
+T = P.lsgd_tensors_create([g, dg, db])
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+def step():
+    P.lsgd_layernorm_forward(x, ga, be, y, m, r, 1, 40, 6000)
+    P.lsgd_layernorm_backward(x, None, y, ga, be, m, r, dx, dg, db, 1, 40, 6000)
+    P.lsgd_gradient_norm(T, norm)
+with torch.cuda.graph(graph):
+    step()
+graph.replay()
+torch.cuda.synchronize()
+got = [t.clone() for t in (y, dx, dg, db, norm)]
+step()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, (y, dx, dg, db, norm)))
+assert float(norm) > 0 and P.lsgd_device_status() == P.OK
+print("ok")
+"""
+
+
+@pytest.mark.gpu
+def test_first_calls_may_be_captured():
+    import os
+    import subprocess
+    import sys
+
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    run = subprocess.run([sys.executable, "-c", SCRIPT], cwd=root, capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0 and run.stdout.strip() == "ok", run.stderr[-2000:]

@@ -338,3 +338,57 @@ def test_repeats_streams_and_graphs_give_the_same_bits(P, shape):
     torch.cuda.synchronize()
     for (dx, dg, db), w, k in zip(outs, (want[4:], other_want), (c, other)):
         assert torch.equal(dx, w[0]) and torch.equal(dg[k.pick], w[1]) and torch.equal(db[k.pick], w[2])
+
+
+# dgamma and dbeta over many rows of equal gradients, whose roundings all go one way.  Additions that a value passes through: 64 rows of
+# a segment, the segments (or the root of the rows, twice), 8 merges of teams, 64 ranges of a thread and 5 merges.
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape,additions", [((1, 300000, 640), 64 + 16 + 8 + 69), ((2, 700000, 16), 64 + 64 + 8 + 69), ((1, 40000, 4200), 64 + 16 + 69),
+                                             ((1, 9_000_000, 24), 2 * 64 + 8 + 69)])
+def test_sums_over_many_rows(P, shape, additions):
+    import torch
+
+    G, Rn, C = shape
+    gen = torch.Generator(device="cuda").manual_seed(C)
+    x = torch.randn(G * Rn, C, generator=gen, device="cuda").bfloat16()
+    gamma = torch.ones(G, C, device="cuda")
+    dy = torch.full((G * Rn, C), 0.1, device="cuda")
+    mean, rstd = torch.zeros(G * Rn, device="cuda"), torch.ones(G * Rn, device="cuda")  # xh = x, without a rounding
+    dx, dgamma, dbeta = torch.empty_like(x), torch.empty(G, C, device="cuda"), torch.empty(G, C, device="cuda")
+    P.lsgd_layernorm_backward(x, None, dy, gamma, gamma, mean, rstd, dx, dgamma, dbeta, *shape)
+    torch.cuda.synchronize()
+    v = float(np.float32(0.1))
+    assert (dbeta.double() / (v * Rn) - 1).abs().max() <= additions * U32
+    for k in range(G):
+        rows = x[k * Rn:(k + 1) * Rn]
+        want = sum(r.double().sum(0) for r in rows.split(1 << 18)) * v
+        size = sum(r.double().abs().sum(0) for r in rows.split(1 << 18)) * v
+        assert ((dgamma[k].double() - want).abs() <= (additions + 1) * U32 * size).all()
+    assert P.lsgd_device_status() == P.OK
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("C", [32768, 4096, 1000])
+def test_offsets_beyond_32_bits(P, C):
+    import torch
+
+    Rn = (1 << 31) // C + 77
+    x = torch.empty(Rn, C, dtype=torch.bfloat16, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(C)
+    block = torch.randn(64, C, generator=gen, device="cuda").bfloat16()
+    x[:64], x[-64:] = block, block
+    x[64:-64] = 1.0
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    gamma, beta = torch.rand(1, C, generator=gen, device="cuda") + 0.5, torch.randn(1, C, generator=gen, device="cuda")
+    mean, rstd = torch.empty(Rn, device="cuda"), torch.empty(Rn, device="cuda")
+    P.lsgd_layernorm_forward(x, gamma, beta, y, mean, rstd, 1, Rn, C)
+    dg, db = torch.empty(1, C, device="cuda"), torch.empty(1, C, device="cuda")
+    P.lsgd_layernorm_backward(x, None, x, gamma, beta, mean, rstd, dx, dg, db, 1, Rn, C)
+    assert torch.equal(y[:64], y[-64:]) and torch.equal(dx[:64], dx[-64:]) and torch.equal(mean[:64], mean[-64:])
+    small = Case(P, (1, 64, C), "bf16", "bf16")
+    small.x.set(block.float())
+    small.gamma, small.beta = gamma.view(-1).clone(), beta.view(-1).clone()
+    small.forward()
+    assert torch.equal(small.y.rows(), y[:64])
+    small.check_forward()
+    assert P.lsgd_device_status() == P.OK
