@@ -758,29 +758,42 @@ def lsgd_direction_update(w, o, Wb, G: int, n: int, lr: float, scale: float = 1.
              weight_decay))
 
 
-_raw = []  # PyTorch's allocation and release of bytes on a stream, filled by the first call
+_quick = None  # PyTorch's cheapest queries, filled by the first call: current device, a device's stream, bytes on a stream, their release
 
 
-def _launch_scratch(dev, stream, workspace, nbytes, fn, args):
-    """_launch for calls of a few microseconds: a workspace that the caller does not give comes from PyTorch's caching
-    allocator as bytes of the call's own stream (which orders a block's uses), not as a tensor, which takes 4 us longer."""
+def _queries():
+    global _quick
     import torch
 
-    if workspace is not None or not nbytes:
-        return _launch(dev, stream, workspace, nbytes, fn, args)
-    if torch.cuda.current_device() != dev:
+    c = torch._C
+    _quick = (getattr(c, "_cuda_getDevice", torch.cuda.current_device), getattr(c, "_cuda_getCurrentRawStream", _stream_of),
+              getattr(c, "_cuda_cudaCachingAllocator_raw_alloc", lambda n, st: torch.cuda.caching_allocator_alloc(n, None, st)),
+              getattr(c, "_cuda_cudaCachingAllocator_raw_delete", torch.cuda.caching_allocator_delete))
+    return _quick
+
+
+def _launch_quick(dev, stream, workspace, nbytes, fn, args):
+    """_launch for calls of a few microseconds.  A workspace that the caller does not give comes from PyTorch's caching
+    allocator as bytes of the call's own stream (which orders a block's uses), not as a tensor, which takes 4 us longer."""
+    device, stream_of, alloc, release = _quick or _queries()
+    if (workspace is not None and workspace is not False) or device() != dev:
+        import torch
+
         with torch.cuda.device(dev):
-            return _launch_scratch(dev, stream, workspace, nbytes, fn, args)
-    if not _raw:
-        alloc = getattr(torch._C, "_cuda_cudaCachingAllocator_raw_alloc", None)
-        _raw.append(alloc or (lambda n, st: torch.cuda.caching_allocator_alloc(n, None, st)))
-        _raw.append(getattr(torch._C, "_cuda_cudaCachingAllocator_raw_delete", torch.cuda.caching_allocator_delete))
-    st = _stream_of(dev) if stream is None else int(stream)
-    at = _raw[0](nbytes, 0 if st == 1 else st)  # (1 is the runtime's other handle of the default stream)
-    try:
-        status = fn(*args, at, nbytes, st)
-    finally:
-        _raw[1](at)
+            if workspace is not None and workspace is not False:
+                return _launch(dev, stream, workspace, nbytes, fn, args)
+            return _launch_quick(dev, stream, workspace, nbytes, fn, args)
+    st = stream_of(dev) if stream is None else int(stream)
+    if workspace is False:
+        status = fn(*args, st)
+    elif not nbytes:
+        status = fn(*args, None, 0, st)
+    else:
+        at = alloc(nbytes, 0 if st == 1 else st)  # (1 is the runtime's other handle of the default stream)
+        try:
+            status = fn(*args, at, nbytes, st)
+        finally:
+            release(at)
     if status != OK:
         _check(status)
 
@@ -793,10 +806,6 @@ def lsgd_layernorm_workspace(G: int, R: int, C: int) -> int:
     return int(n.value)
 
 
-def _row_span(N: int, ld: int, C: int) -> int:
-    return (N - 1) * ld + C if N else 0
-
-
 def lsgd_layernorm_forward(x, gamma, beta, y, mean, rstd, G: int, R: int, C: int, r=None, s=None, act: int = ACT_NONE,
                            eps: float = 1e-5, par_gs: int = 0, x_ld: int = 0, y_ld: int = 0, stream=None):
     """y = act(gamma (x - mean) rstd + beta) over rows of C values: x and y float32 or bfloat16, G R rows at strides x_ld and
@@ -805,11 +814,11 @@ def lsgd_layernorm_forward(x, gamma, beta, y, mean, rstd, G: int, R: int, C: int
     par_gs, x_ld, y_ld, N = par_gs or C, x_ld or C, y_ld or C, G * R
     if (r is None) != (s is None):
         raise LsgdError(EINVAL, "r and s come together")
-    nx, npar = _row_span(N, x_ld, C), (G - 1) * par_gs + C
+    nx, ny, npar = ((N - 1) * x_ld + C, (N - 1) * y_ld + C, (G - 1) * par_gs + C) if N else (0, 0, (G - 1) * par_gs + C)
     xt, yt = _type_of(x), _type_of(y)
-    dev = _checked(("x", x, nx, xt), ("r", r, nx, xt), ("s", s, nx, xt), ("y", y, _row_span(N, y_ld, C), yt),
+    dev = _checked(("x", x, nx, xt), ("r", r, nx, xt), ("s", s, nx, xt), ("y", y, ny, yt),
                    ("gamma", gamma, npar, FP32), ("beta", beta, npar, FP32), ("mean", mean, N, FP32), ("rstd", rstd, N, FP32))
-    _launch(dev, stream, False, 0, lib().lsgd_layernorm_forward,
+    _launch_quick(dev, stream, False, 0, lib().lsgd_layernorm_forward,
             (x.data_ptr(), r.data_ptr() if r is not None else None, xt, x_ld, gamma.data_ptr(), beta.data_ptr(), par_gs,
              s.data_ptr() if s is not None else None, y.data_ptr(), yt, y_ld, mean.data_ptr(), rstd.data_ptr(), G, R, C, eps,
              act))
@@ -822,12 +831,12 @@ def lsgd_layernorm_backward(x, y, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta
     added to dx.  y, the stored output, is read for ReLU only (None otherwise)."""
     nbytes = lsgd_layernorm_workspace(G, R, C)
     par_gs, x_ld, y_ld, N = par_gs or C, x_ld or C, y_ld or C, G * R
-    nx, ny, npar = _row_span(N, x_ld, C), _row_span(N, y_ld, C), (G - 1) * par_gs + C
+    nx, ny, npar = ((N - 1) * x_ld + C, (N - 1) * y_ld + C, (G - 1) * par_gs + C) if N else (0, 0, (G - 1) * par_gs + C)
     xt, yt = _type_of(x), _type_of(dy)
     dev = _checked(("x", x, nx, xt), ("dx", dx, nx, xt), ("ds", ds, nx, xt), ("dy", dy, ny, yt), ("y", y, ny, yt),
                    ("gamma", gamma, npar, FP32), ("beta", beta, npar, FP32), ("dgamma", dgamma, npar, FP32),
                    ("dbeta", dbeta, npar, FP32), ("mean", mean, N, FP32), ("rstd", rstd, N, FP32))
-    _launch_scratch(dev, stream, workspace, nbytes, lib().lsgd_layernorm_backward,
+    _launch_quick(dev, stream, workspace, nbytes, lib().lsgd_layernorm_backward,
             (x.data_ptr(), xt, x_ld, y.data_ptr() if y is not None else None, dy.data_ptr(), yt, y_ld,
              ds.data_ptr() if ds is not None else None, gamma.data_ptr(), beta.data_ptr(), par_gs, mean.data_ptr(),
              rstd.data_ptr(), dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), G, R, C, act))
@@ -886,7 +895,7 @@ def lsgd_gradient_norm(tensors: Tensors, norm, workspace=None, stream=None):
     dev = _checked(("norm", norm, tensors.G, _type_of(norm)))
     if dev != tensors.device or norm.dtype is not _WANTED[FP32]:
         raise LsgdError(EINVAL, f"norm: a float32 tensor on CUDA device {tensors.device} is wanted")
-    _launch_scratch(dev, stream, workspace, tensors.workspace, lib().lsgd_gradient_norm, (tensors.handle, norm.data_ptr()))
+    _launch_quick(dev, stream, workspace, tensors.workspace, lib().lsgd_gradient_norm, (tensors.handle, norm.data_ptr()))
 
 
 def lsgd_gradient_clip(tensors: Tensors, norm, max_norm: float, workspace=None, stream=None):
@@ -894,7 +903,7 @@ def lsgd_gradient_clip(tensors: Tensors, norm, max_norm: float, workspace=None, 
     dev = _checked(("norm", norm, tensors.G, _type_of(norm)))
     if dev != tensors.device or norm.dtype is not _WANTED[FP32]:
         raise LsgdError(EINVAL, f"norm: a float32 tensor on CUDA device {tensors.device} is wanted")
-    _launch_scratch(dev, stream, workspace, tensors.workspace, lib().lsgd_gradient_clip, (tensors.handle, norm.data_ptr(), max_norm))
+    _launch_quick(dev, stream, workspace, tensors.workspace, lib().lsgd_gradient_clip, (tensors.handle, norm.data_ptr(), max_norm))
 
 
 def lsgd_clipped_update(w, u, g, Wb, G: int, n: int, norm, max_norm: float, lr: float, momentum: float = 0.0,
@@ -911,7 +920,7 @@ def lsgd_clipped_update(w, u, g, Wb, G: int, n: int, norm, max_norm: float, lr: 
     gt = _type_of(g)
     dev = _checked(("w", w, span, FP32), ("u", u, span, FP32), ("g", g, (G - 1) * g_gs + n, gt), ("Wb", Wb, span, BF16),
                    ("norm", norm, G, FP32))
-    _launch(dev, stream, False, 0, lib().lsgd_clipped_update,
+    _launch_quick(dev, stream, False, 0, lib().lsgd_clipped_update,
             (w.data_ptr(), u.data_ptr() if u is not None else None, w_gs, g.data_ptr(), gt, g_gs,
              Wb.data_ptr() if Wb is not None else None, G, n, norm.data_ptr(), max_norm, lr, momentum, int(bool(nesterov)),
              weight_decay, n if decay_end is None else decay_end))

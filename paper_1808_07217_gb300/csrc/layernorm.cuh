@@ -443,9 +443,9 @@ __device__ __forceinline__ void store_row(const u64 (&v)[N * V / 2], T* p, bool 
       if (left > j * hop) o[j].store_first(p + j * hop, left - j * hop);
   }
 }
-// Rows of a team that one CTA of the backward takes by itself: more CTAs would need the second kernel, whose launch takes about as long
-// as four rows and a quarter of the call's host time (3 x 20 x 600: 22.9 us a call with it, 18.3 without).
-constexpr int kFewRows = 4;
+// Rows of a team that one CTA of the backward takes by itself: more CTAs need the second kernel, whose launch costs as much of the host's
+// time as it saves of the GPU's (3 x 20 x 600, five rows: 17.5 us a call, 8.9 of them the GPU's; 20.1 and 6.7 with it).
+constexpr int kFewRows = 6;
 
 // The rows that fall to a team.  Forward: every step-th of the worker's, so that all CTAs together walk through memory; backward: one of
 // the CTA's `rows` x teams neighbouring ones (32,768 x 2048 in bf16: 95 us, with every step-th 108; the forward 84 and 82).
