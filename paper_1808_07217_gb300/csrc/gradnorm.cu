@@ -54,8 +54,9 @@ struct Entry {
   int64_t n, gs, out_gs;
 };
 // The tensors of a launch, all of one type and clipped to one type.  A launch's parameters hold up to 32,764 bytes: longer lists take
-// several launches.  They are read through the constant caches, where a miss costs as much as one of memory: what is searched stands
-// close together, and a piece's tensor is sought from a hint on (40 workers of 200 tensors of about 300 values: 17.5 us, 21 with a search by halves).
+// several launches.  They are read through the constant caches, where a miss costs as much as one of memory: what is searched
+// stands close together, and a piece's tensor is sought from a hint on (40 workers of 200 tensors of about 300 values: 17.5 us, 21 with
+// a search by halves).
 constexpr int kHints = 128;
 template <int MAX>
 struct Table {

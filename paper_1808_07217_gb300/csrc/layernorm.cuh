@@ -448,7 +448,7 @@ __device__ __forceinline__ void store_row(const u64 (&v)[N * V / 2], T* p, bool 
 constexpr int kFewRows = 6;
 
 // The rows that fall to a team.  Forward: every step-th of the worker's, so that all CTAs together walk through memory; backward: one of
-// the CTA's `rows` x teams neighbouring ones (32,768 x 2048 in bf16: 95 us, with every step-th 108; the forward 84 and 82).
+// the CTA's `rows` x teams neighbouring ones (32,768 x 2048 in bf16: 92 us, with every step-th 105; the forward 84 and 82).
 struct Rows {
   int mine, turns;     // the team's rows; the turns of its warp's loop, in which teams that lie in one warp go together
   int64_t step, row;   // row: of the first one, of all workers'
