@@ -36,7 +36,7 @@ namespace {
 template <typename XT, typename YT, int V, bool RES, int E, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads, 2) ln_forward_kernel(const LnArgs a) {
   constexpr int N = E / V, H = E / 2;
-  using In = Feed<XT, V, N>;
+  using In = Feed<XT, V, N, CLUSTER>;
   using M = Team<CLUSTER>;
   constexpr uint32_t kSlotBytes = In::kSlot * (RES ? 2 : 1);
   __shared__ float4 stats[M::kPlaces];
@@ -79,11 +79,11 @@ __global__ void __launch_bounds__(kThreads, 2) ln_forward_kernel(const LnArgs a)
   int64_t row = rows.row;
   const float inv_n = m.n ? 1.f / m.n : 0.f, inv_C = 1.f / a.C;
 
-  // A row's values v, their sum s, the mean of the thread's warp (or smaller team) and the squared deviations from it.
-  const auto sums = [&](bool on, u64 (&v)[H], float& s, float& mean, float& q) {
+  // A row's values v (p: the residual's), their sum s, the mean of the thread's warp (or smaller team) and the squared deviations from
+  // it.
+  const auto sums = [&](bool on, u64 (&v)[H], u64 (&p)[H], float& s, float& mean, float& q) {
     fx.read(slot, v);
     if constexpr (RES) {
-      u64 p[H];
       fr.read(slot, p);
 #pragma unroll
       for (int i = 0; i < H; ++i) add2(v[i], p[i]);
@@ -148,26 +148,27 @@ __global__ void __launch_bounds__(kThreads, 2) ln_forward_kernel(const LnArgs a)
   if constexpr (!CLUSTER) {
     for (int k = 0; k < rows.turns; ++k, advance(slot), advance(next)) {
       const bool on = k < rows.mine;
+      u64 v[H], p[H];
+      fx.take(v);
+      if (RES) fr.take(p);
       fetch(k + a.ahead, next);
       copies_wait(a.ahead);
-      u64 v[H];
       float s, mean, q;
-      sums(on, v, s, mean, q);
+      sums(on, v, p, s, mean, q);
       if (m.slots > 1) {
         m.post_moments(s, mean, q, stats, k);
         m.collect_moments(mean, q, inv_C, stats, k);
       }
       finish(on, v, mean, q);
-      land(next);
     }
   } else {
     uint32_t before = 0, coming = 0;  // the places of row k - 1, and of the row that was fetched last
     for (int k = 0; k <= rows.turns; ++k) {
-      u64 v[H];
+      u64 v[H], p[H];
       float s, mean, q;
       if (k < rows.turns) {
         copies_wait(a.ahead);
-        sums(true, v, s, mean, q);
+        sums(true, v, p, s, mean, q);
         if constexpr (RES) fx.write(slot, v);
         m.post_moments(s, mean, q, stats, k);
       }
@@ -189,7 +190,7 @@ __global__ void __launch_bounds__(kThreads, 2) ln_forward_kernel(const LnArgs a)
 template <typename XT, typename YT, int V, bool RES, int E, bool CLUSTER>
 cudaError_t ln_forward_as(LnArgs a, int G, cudaStream_t st) {
   static std::atomic<int> raised{0};  // device + 1 whose limits this kernel's have been raised to
-  using In = Feed<XT, V, E / V>;
+  using In = Feed<XT, V, E / V, CLUSTER>;
   constexpr int slot = In::kSlot * (RES ? 2 : 1), more = CLUSTER ? 2 : 1, own = kStaticSmem<CLUSTER>;
   constexpr int fit = kSmemPerSm / ((1 + more) * slot + own);
   const auto kernel = ln_forward_kernel<XT, YT, V, RES, E, CLUSTER>;
@@ -203,11 +204,11 @@ cudaError_t ln_forward_as(LnArgs a, int G, cudaStream_t st) {
   a.ahead = In::kAsync && per_sm * ((2 + more) * slot + own) <= kSmemPerSm ? ln_ahead(p.rows, per_sm * threads, slot / kThreads) : 1;
   return ln_launch(kernel, raised, a, dim3((unsigned)(p.ranges * p.cl), G), (a.ahead + more) * slot, st);
 }
-// 16 values to a thread; 8 where single bf16 values go through registers, 32 of which they would take with a residual (32,768 x 1531:
+// 16 values to a thread; 8 where single bf16 values come through registers, 32 of which they would take with a residual (32,768 x 1531:
 // 214 and 122 us).
 template <typename XT, typename YT, int V, bool RES>
 cudaError_t ln_forward(const LnArgs& a, int G, cudaStream_t st) {
-  constexpr int E = Feed<XT, V, 1>::kAsync ? 16 : 8;
+  constexpr int E = V * sizeof(XT) >= 4 ? 16 : 8;
   return a.C > E * kThreads ? ln_forward_as<XT, YT, V, RES, E, true>(a, G, st) : ln_forward_as<XT, YT, V, RES, E, false>(a, G, st);
 }
 

@@ -335,13 +335,14 @@ __device__ __forceinline__ void load_params(const float* p, const M& m, u64 (&ou
 
 // One input's rows on their way through shared memory: every thread's own N vectors of the next rows, in slots of one row each.
 // Vectors of 4 bytes and more are copied by cp.async, which writes zeros where there is nothing to read (behind the row's end, and
-// rows behind the last); single bf16 values, which it does not take, through registers, one row ahead.  The vectors of a slot lie
-// kThreads vectors from one another whatever the block's size, so that they cost no address arithmetic.
-template <typename T, int V, int N>
+// rows behind the last); single bf16 values, which it does not take, come through registers, one row ahead, and only where a row is
+// read twice (in a cluster) go on to shared memory.  The vectors of a slot lie kThreads vectors from one another whatever the block's
+// size, so that they cost no address arithmetic.
+template <typename T, int V, int N, bool CLUSTER>
 struct Feed {
   static constexpr int kBytes = V * (int)sizeof(T);  // of a vector
-  static constexpr int kSlot = N * kThreads * kBytes;
-  static constexpr bool kAsync = kBytes >= 4;
+  static constexpr bool kAsync = kBytes >= 4, kShared = kAsync || CLUSTER;
+  static constexpr int kSlot = kShared ? N * kThreads * kBytes : 0;
   const T* row;   // the thread's first value of the next row to fetch
   uint32_t at;    // the thread's first vector in slot 0
   uint16_t held[kAsync ? 1 : N];
@@ -381,14 +382,23 @@ struct Feed {
     }
     row += step;
   }
+  // The row that came through registers (before the next is fetched).
+  __device__ __forceinline__ void take(u64 (&out)[N * V / 2]) const {
+    if constexpr (!kShared) {
+#pragma unroll
+      for (int i = 0; i < N * V / 2; ++i) out[i] = pack2(bf2f(held[2 * i]), bf2f(held[2 * i + 1]));
+    }
+  }
   __device__ __forceinline__ void land(uint32_t slot) const {
-    if constexpr (!kAsync) {
+    if constexpr (!kAsync && kShared) {
 #pragma unroll
       for (int j = 0; j < N; ++j)
         asm volatile("st.shared.u16 [%0], %1;" ::"r"(at + slot + j * kThreads * kBytes), "h"(held[j]) : "memory");
     }
   }
+  // A row from shared memory (nothing to do where it has been taken).
   __device__ __forceinline__ void read(uint32_t slot, u64 (&out)[N * V / 2]) const {
+    if constexpr (!kShared) return;
     Vec<T, V> r[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) {

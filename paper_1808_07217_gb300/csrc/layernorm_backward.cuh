@@ -7,11 +7,11 @@ namespace lsgd {
 namespace {
 
 // Where a slot's inputs and what follows the slots stand in shared memory.  E: values of a row in a thread.
-template <typename XT, typename YT, int V, bool RES, int ACT, int E>
+template <typename XT, typename YT, int V, bool RES, int ACT, int E, bool CLUSTER>
 struct BwdShape {
   static constexpr int N = E / V;
-  using X = Feed<XT, V, N>;
-  using Y = Feed<YT, V, N>;
+  using X = Feed<XT, V, N, CLUSTER>;
+  using Y = Feed<YT, V, N, CLUSTER>;
   static constexpr int kDy = X::kSlot, kY = kDy + Y::kSlot, kDs = kY + (ACT == LSGD_ACT_RELU ? Y::kSlot : 0),
                        kSlot = kDs + (RES ? X::kSlot : 0);
   static constexpr int kBetas = ACT == LSGD_ACT_SILU ? 4 * E * kThreads : 0, kSums = 8 * E * kThreads;
@@ -21,7 +21,7 @@ struct BwdShape {
 template <typename XT, typename YT, int V, bool RES, int ACT, int E, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads, 2) ln_backward_kernel(const LnArgs a) {
   using M = Team<CLUSTER>;
-  using S = BwdShape<XT, YT, V, RES, ACT, E>;
+  using S = BwdShape<XT, YT, V, RES, ACT, E, CLUSTER>;
   constexpr int N = S::N, H = E / 2;
   constexpr bool RELU = ACT == LSGD_ACT_RELU, SILU = ACT == LSGD_ACT_SILU;
   __shared__ float2 stats[M::kPlaces];
@@ -108,11 +108,10 @@ __global__ void __launch_bounds__(kThreads, 2) ln_backward_kernel(const LnArgs a
   const float inv = -1.f / a.C;
   XT* out = static_cast<XT*>(a.out) + x0;
   // A row's xh and dz; what lies behind its end has dz = 0.
-  const auto values = [&](uint32_t slot, float mean, float rstd, u64 (&xh)[H], u64 (&t)[H]) {
+  const auto values = [&](uint32_t slot, float mean, float rstd, u64 (&xh)[H], u64 (&t)[H], u64 (&y)[H]) {
     fx.read(slot, xh);
     fd.read(slot, t);
     if constexpr (RELU) {
-      u64 y[H];
       fy.read(slot, y);
 #pragma unroll
       for (int i = 0; i < H; ++i) {
@@ -144,9 +143,8 @@ __global__ void __launch_bounds__(kThreads, 2) ln_backward_kernel(const LnArgs a
     }
     m1 = added(s1), m2 = added(s2);
   };
-  const auto finish = [&](bool on, uint32_t slot, u64 (&xh)[H], u64 (&t)[H], float m1, float m2, float rstd) {
+  const auto finish = [&](bool on, uint32_t slot, u64 (&xh)[H], u64 (&t)[H], u64 (&e)[H], float m1, float m2, float rstd) {
     m1 *= inv, m2 *= inv;
-    u64 e[H];
     if constexpr (RES) fs.read(slot, e);
 #pragma unroll
     for (int i = 0; i < H; ++i) {
@@ -159,12 +157,16 @@ __global__ void __launch_bounds__(kThreads, 2) ln_backward_kernel(const LnArgs a
   if constexpr (!CLUSTER) {
     for (int k = 0; k < rows.turns; ++k, advance(slot), advance(next)) {
       const float mean = next_mean, rstd = next_rstd;
+      u64 xh[H], t[H], y[H], e[H];
+      fx.take(xh);
+      fd.take(t);
+      if (RELU) fy.take(y);
+      if (RES) fs.take(e);
       fetch(k + a.ahead, next);
       fetch_stats(k + 1);
       copies_wait(a.ahead);
-      u64 xh[H], t[H];
       float m1, m2;
-      values(slot, mean, rstd, xh, t);
+      values(slot, mean, rstd, xh, t, y);
       add(xh, t, m1, m2);
       if (m.slots > 1) {
         m.post_both(m1, m2, stats, k);
@@ -172,33 +174,32 @@ __global__ void __launch_bounds__(kThreads, 2) ln_backward_kernel(const LnArgs a
       } else {
         m.sum_both(m1, m2);
       }
-      finish(k < rows.mine, slot, xh, t, m1, m2, rstd);
+      finish(k < rows.mine, slot, xh, t, e, m1, m2, rstd);
       if (++run == a.seg) flush();
-      land(next);
     }
   } else {
     uint32_t before = 0, coming = 0;  // the places of row k - 1, and of the row that was fetched last
     float mean = 0.f, rstd = 0.f;     // of row k - 1
     for (int k = 0; k <= rows.turns; ++k) {
-      u64 xh[H], t[H];
+      u64 xh[H], t[H], y[H], e[H];
       float m1, m2;
       const float old_mean = mean, old_rstd = rstd;
       if (k < rows.turns) {
         mean = next_mean, rstd = next_rstd;
         fetch_stats(k + 1);
         copies_wait(a.ahead);
-        values(slot, mean, rstd, xh, t);
+        values(slot, mean, rstd, xh, t, y);
         add(xh, t, m1, m2);
         m.post_both(m1, m2, stats, k);
         if (++run == a.seg) flush();
       }
       if (k) {
         land(coming);
-        values(before, old_mean, old_rstd, xh, t);
+        values(before, old_mean, old_rstd, xh, t, y);
 #pragma unroll
         for (int i = 0; i < H; ++i) t[i] = mul2(t[i], ga[i]);
         m.collect_both(m1, m2, stats, k - 1);
-        finish(true, before, xh, t, m1, m2, old_rstd);
+        finish(true, before, xh, t, e, m1, m2, old_rstd);
       }
       fetch(k + early, next);
       before = slot, coming = next;
@@ -290,7 +291,7 @@ inline cudaError_t launch_param_grads(const LnArgs& a, int G, int ranges, cudaSt
 template <typename XT, typename YT, int V, bool RES, int ACT, int E, bool CLUSTER>
 cudaError_t ln_backward_as(LnArgs a, int G, cudaStream_t st) {
   static std::atomic<int> raised{0};  // device + 1 whose limits this kernel's have been raised to
-  using S = BwdShape<XT, YT, V, RES, ACT, E>;
+  using S = BwdShape<XT, YT, V, RES, ACT, E, CLUSTER>;
   constexpr int more = CLUSTER ? 2 : 1, own = kStaticSmem<CLUSTER>;
   // as many CTAs to an SM as the shared memory takes with a row ahead
   const auto used = [](int ahead, bool apart) {
@@ -331,7 +332,7 @@ cudaError_t ln_backward_as(LnArgs a, int G, cudaStream_t st) {
 // single bf16 values go through registers.
 template <typename XT, typename YT, int V, bool RES, int ACT>
 cudaError_t ln_backward(const LnArgs& a, int G, cudaStream_t st) {
-  constexpr bool direct = !Feed<XT, V, 1>::kAsync || !Feed<YT, V, 1>::kAsync;
+  constexpr bool direct = V * sizeof(XT) < 4 || V * sizeof(YT) < 4;
   constexpr bool fp32 = sizeof(XT) + sizeof(YT) == 8;
   constexpr int E = direct ? 8 : 16;
   if constexpr (!direct && fp32) {
