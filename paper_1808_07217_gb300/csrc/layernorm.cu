@@ -205,11 +205,15 @@ cudaError_t ln_forward_as(LnArgs a, int G, cudaStream_t st) {
   return ln_launch(kernel, raised, a, dim3((unsigned)(p.ranges * p.cl), G), (a.ahead + more) * slot, st);
 }
 // 16 values to a thread; 8 where single bf16 values come through registers, 32 of which they would take with a residual (32,768 x 1531:
-// 214 and 122 us).
+// 214 and 122 us), but not where a cluster would then be needed for a row that one CTA of 16 holds (8,000 x 3001: 35 us, 97 in clusters).
 template <typename XT, typename YT, int V, bool RES>
 cudaError_t ln_forward(const LnArgs& a, int G, cudaStream_t st) {
   constexpr int E = V * sizeof(XT) >= 4 ? 16 : 8;
-  return a.C > E * kThreads ? ln_forward_as<XT, YT, V, RES, E, true>(a, G, st) : ln_forward_as<XT, YT, V, RES, E, false>(a, G, st);
+  if (a.C <= E * kThreads) return ln_forward_as<XT, YT, V, RES, E, false>(a, G, st);
+  if constexpr (E == 8) {
+    if (a.C <= 16 * kThreads) return ln_forward_as<XT, YT, V, RES, 16, false>(a, G, st);
+  }
+  return ln_forward_as<XT, YT, V, RES, E, true>(a, G, st);
 }
 
 // The widest vector (a power of two of values, at most v) with which rows of stride ld from p on (values of z bytes) are aligned.

@@ -15,7 +15,7 @@ ROW, COLUMN = 40 * U32, 160 * U32
 # (G, R, C): single values, parts of warps, one warp and several, odd widths, every vector, the widest rows of one CTA and
 # rows of clusters of 2, 5, 8, 10 and 16, one row and many, rows that end inside a CTA's teams
 SHAPES = [(1, 1, 1), (2, 3, 5), (1, 70, 8), (3, 33, 24), (2, 130, 77), (1, 40, 256), (1, 9, 258), (2, 21, 300), (1, 50, 777),
-          (2, 5, 1024), (1, 7, 2050), (3, 2, 4096), (1, 3, 4097), (2, 3, 8200), (1, 2, 20001), (1, 2, 32767), (1, 2, 32768), (5, 1, 513),
+          (2, 5, 1024), (1, 7, 2050), (2, 6, 2303), (2, 9, 3333), (3, 2, 4096), (1, 3, 4097), (2, 3, 8200), (1, 2, 20001), (1, 2, 32767), (1, 2, 32768), (5, 1, 513),
           (1, 3000, 16), (2, 700, 100)]
 
 
