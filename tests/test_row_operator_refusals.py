@@ -25,7 +25,7 @@ vp = ctypes.c_void_p
 NAMES = ["x", "r", "gamma", "beta", "s", "y", "mean", "rstd", "dy", "ds", "dx", "dgamma", "dbeta", "ws"]
 
 
-def _rows(L, fn, G=3, R=50, C=40, x_ld=48, y_ld=44, par_gs=64, x_type=1, y_type=0, act=1, eps=1e-5, need=None, **at):
+def _rows(L, fn, G=3, R=500, C=40, x_ld=48, y_ld=44, par_gs=64, x_type=1, y_type=0, act=1, eps=1e-5, need=None, **at):
     n = ctypes.c_size_t()
     ok = L.lib().lsgd_layernorm_workspace(G, R, C, ctypes.byref(n)) == L.OK
     need = (n.value if ok else 0) if need is None else need
