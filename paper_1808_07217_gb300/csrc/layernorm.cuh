@@ -69,8 +69,8 @@ struct LnPlan {
   int64_t rows;    // rows of a team at most
 };
 
-// few: as many rows of a team stay with one CTA; per_sm: CTAs that an SM holds at once (0: as many as its threads allow); clusters: of those that the GPU holds at once (0: as many as
-// the SMs' CTAs make).
+// few: as many rows of a team stay with one CTA; per_sm: CTAs that an SM holds at once (0: as many as its threads allow); clusters: of
+// those that the GPU holds at once (0: as many as the SMs' CTAs make).
 inline LnPlan ln_plan(int G, int64_t R, int C, int E, int few, int per_sm = 0, int clusters = 0) {
   LnPlan p;
   p.cl = (C + E * kThreads - 1) / (E * kThreads);

@@ -5,8 +5,8 @@
 
 namespace lsgd {
 
-// `count` blocks of `bytes` from p, `stride` values of `elem` bytes from one to the next; at NULL: nothing.  (A workspace that is not used, of no
-// bytes, counts by its address.)
+// `count` blocks of `bytes` from p, `stride` values of `elem` bytes from one to the next; at NULL: nothing.  (A workspace that is not
+// used, of no bytes, counts by its address.)
 struct Blocks {
   uintptr_t first, end;  // of all of them
   size_t bytes;
@@ -26,7 +26,8 @@ inline bool blocks_meet(const Blocks& a, const Blocks& b) {
   if (a.count == 1 && b.count == 1) return true;
   // block j of b lies d + t stride behind block i of a, t = j - i
   using wide = __int128;
-  const wide d = (wide)b.first - (wide)a.first, stride = a.count > 1 ? a.elem * (wide)a.stride : b.elem * (wide)b.stride, na = a.bytes, nb = b.bytes;
+  const wide d = (wide)b.first - (wide)a.first, na = a.bytes, nb = b.bytes;
+  const wide stride = a.count > 1 ? a.elem * (wide)a.stride : b.elem * (wide)b.stride;
   const wide t = std::max<wide>(1 - a.count, (-nb - d >= 0 ? (-nb - d) / stride : -((nb + d + stride - 1) / stride)) + 1);
   return t <= b.count - 1 && d + t * stride < na;  // (t: the first that does not end before a's block)
 }
