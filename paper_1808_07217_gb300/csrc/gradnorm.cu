@@ -37,7 +37,8 @@ struct lsgd_tensors {
   bool places = false;               // every tensor has an `out`
   bool overlap = false;              // what a clipping would write overlaps something
   int blocks = 0;                    // CTAs of a worker in the passes
-  int cluster = 0;                   // CTAs of a worker where one launch does all (0: two)
+  int cluster = 0;                   // CTAs of a worker where one launch takes the norm (0: two)
+  bool clip_once = false;            // and clips
   uintptr_t lo = UINTPTR_MAX, hi = 0;  // all that is read or written lies between
 };
 
@@ -47,6 +48,10 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxPiece = 4096, kMinPiece = 512;
 constexpr int64_t kShare = 160 << 10, kMinShare = 16 << 10;  // bytes of a worker's gradient to a CTA of a cluster
+// Bytes that a worker's clipping reads and writes in one launch.  Its CTAs have a pass over all of them behind the norm's; two launches
+// give that to all SMs, for 3 us more of the host's time (one worker of 0.47 MB in fp32: 5.9 us, 4.5 on the host; 1.28 MB: 9.4 and
+// 4.4 us, 5.2 and 7.7 in two launches; 1.28 MB of bf16 to fp32: 18.1 and 6.3).
+constexpr int64_t kClipOnce = 1 << 20;
 
 struct Entry {
   const void* in;
@@ -55,8 +60,8 @@ struct Entry {
 };
 // The tensors of a launch, all of one type and clipped to one type.  A launch's parameters hold up to 32,764 bytes: longer lists take
 // several launches.  They are read through the constant caches, where a miss costs as much as one of memory: what is searched
-// stands close together, and a piece's tensor is sought from a hint on (40 workers of 200 tensors of about 300 values: 17.5 us, 21 with
-// a search by halves).
+// stands close together, and a piece's tensor is sought from a hint on (40 workers of 200 tensors of about 300 values, clusters of 8:
+// 17.5 us, 21 with a search by halves).
 constexpr int kHints = 128;
 template <int MAX>
 struct Table {
@@ -517,7 +522,7 @@ cudaError_t norm_and_clip(const lsgd_tensors& l, float* norm, float max_norm, do
   const size_t n = l.launches.size();
   const bool clip = max_norm > 0.f;
   if (n == 0) return cudaMemsetAsync(norm, 0, sizeof(float) * l.G, st);
-  if (l.cluster)
+  if (clip ? l.clip_once : l.cluster > 0)
     return with_kind(l.launches[0], [&](auto max, auto bf16, auto ob) {
       constexpr bool B = decltype(bf16)::value, O = decltype(ob)::value;
       constexpr int MAX = decltype(max)::value;
@@ -544,7 +549,7 @@ cudaError_t norm_and_clip(const lsgd_tensors& l, float* norm, float max_norm, do
   return e;
 }
 
-size_t gr_workspace(const lsgd_tensors& l) { return !l.cluster && slots_of(l) > 1 ? (size_t)l.G * slots_of(l) * sizeof(double) : 0; }
+size_t gr_workspace(const lsgd_tensors& l) { return !l.clip_once && slots_of(l) > 1 ? (size_t)l.G * slots_of(l) * sizeof(double) : 0; }
 
 // The first or the last address of a tensor's blocks (gs may be any number where there is one worker).
 uintptr_t end_of(const void* p, int64_t n, int64_t gs, int type, int G) {
@@ -615,7 +620,7 @@ lsgd_status lsgd_tensors_create(const lsgd_tensor* tensors, int count, int G, ls
   if (G < 1 || G > 65535 || (int64_t)count * G > (1 << 22))
     return gr_error(LSGD_EINVAL, fn, "at least 1 and at most 65535 workers, at most 2^22 tensors of all workers");
   int places = 0;
-  int64_t bytes = 0;  // of a worker
+  int64_t bytes = 0, out_bytes = 0;  // of a worker
   for (int i = 0; i < count; ++i) {
     const lsgd_tensor& t = tensors[i];
     const auto bad_type = [](int type) { return type != LSGD_FP32 && type != LSGD_BF16; };
@@ -629,6 +634,7 @@ lsgd_status lsgd_tensors_create(const lsgd_tensor* tensors, int count, int G, ls
       return gr_error(LSGD_EINVAL, fn, "a tensor is NULL, not aligned to its element, or its workers' strides below n or above 2^50");
     if (t.n) places |= t.out ? 1 : 2;
     bytes += t.n * size_of(t.g_type);
+    out_bytes += t.n * size_of(t.out ? t.out_type : t.g_type);
     if (bytes > ((int64_t)1 << 42)) return gr_error(LSGD_EINVAL, fn, "at most 2^42 bytes of a worker");
   }
   if (places == 3) return gr_error(LSGD_EINVAL, fn, "either every tensor has an out or none has");
@@ -647,10 +653,13 @@ lsgd_status lsgd_tensors_create(const lsgd_tensor* tensors, int count, int G, ls
       for (size_t i = 0; i < l->launches.size(); ++i)
         l->launches[i].to = i + 1 < l->launches.size() ? l->launches[i + 1].from : l->list.size();
       // One launch, a worker to a cluster, where it takes one and the CTAs have little to read each: as many as get 16 KB or two
-      // tensors to a warp.
+      // tensors to a warp; not where that makes more than two to an SM (64 workers of 70 KB, 320 CTAs: norm 7.2 us, 5.1 in two
+      // launches; 300 of 16 KB, 300 CTAs: 4.3 and 8.6).
       if (l->launches.size() == 1 && bytes <= kShare * kMaxCluster) {
         const int64_t want = std::max<int64_t>(bytes / kMinShare, (int64_t)l->list.size() / (kClusterThreads / 16)) + 1;
         l->cluster = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxCluster, want));
+        if ((int64_t)l->cluster * G > 2 * kNumSMs) l->cluster = 0;
+        l->clip_once = l->cluster && bytes + out_bytes <= kClipOnce;
       }
       // Pieces small enough for every warp to have one, up to 4096 bytes (8 vectors a lane).
       const int64_t warps = l->cluster ? l->cluster * (kClusterThreads / 32) : std::max<int64_t>(1, (int64_t)kNumSMs * 4 * kWarps / G);

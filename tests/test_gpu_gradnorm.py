@@ -242,6 +242,40 @@ def test_repeats_streams_and_graphs_give_the_same_bits(P):
             assert torch.equal(o, (g.float() * f).to(o.dtype))
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("G,sizes", [(3, [4999, 3, 1024, 777] * 20), (1, [300001, 5, 99991, 2]), (1, [260000]), (1, [262148]), (64, [17000, 3]),
+                                     (301, [3500]), (305, [3500])])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_calls_one_behind_another_see_what_was_written(P, G, sizes, dtype):
+    """Norms and clippings in place, each of what the one before wrote, at sizes on both sides of what takes one launch: the bits of calls
+    that are waited for.  Tensors without any alignment share lines of 128 bytes that different SMs read and write."""
+    import torch
+
+    kind = {"fp32": torch.float32, "bf16": torch.bfloat16}[dtype]
+
+    def steps(wait):
+        grads, bufs = _make(torch, sizes, G, "arena", kind, np.random.default_rng(5))
+        T = P.lsgd_tensors_create(grads)
+        norms = torch.zeros(40, G, device="cuda")
+        for i in range(0, 40, 2):
+            P.lsgd_gradient_clip(T, norms[i], limit * 0.98 ** i)
+            if wait:
+                torch.cuda.synchronize()
+            P.lsgd_gradient_norm(T, norms[i + 1])
+            if wait:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        return bufs[0], norms
+
+    limit = float(np.sqrt(sum(sizes)) * 0.9)
+    one, other = steps(True), steps(False)
+    assert torch.equal(one[0], other[0]) and torch.equal(one[1], other[1])
+    # (the clipped gradient's norm: the limit, but for the factor's, the products' and the norm's roundings)
+    eps = 2.0 ** -24 if dtype == "fp32" else 2.0 ** -8
+    last = one[1][39].cpu().numpy()
+    assert (np.abs(last - limit * 0.98 ** 38) <= (2 * NORM + 3 * U32 + eps) * limit).all()
+
+
 # ---- the update ----
 @pytest.mark.gpu
 @pytest.mark.parametrize("momentum,nesterov", [(0.0, False), (0.9, False), (0.9, True)])
