@@ -310,7 +310,8 @@ __device__ __forceinline__ void scale_pieces(const Table<MAX>& tab, int64_t work
   for (p += (tab.end - 1 - p) / stride * stride;; p -= stride) {
     const int t = find(tab, p);
     const Entry& e = tab.e[t];
-    if (f != 1.f || e.out != e.in) {
+    // (left as it is only where this worker's place is the one that was read: the first worker's may be, and no other's)
+    if (f != 1.f || e.out != e.in || (worker && e.out_gs != e.gs)) {
       const uint32_t piece = p - tab.first[t];
       const int64_t at = worker * e.out_gs + ((int64_t)piece << (tab.shift - (BF16 ? 1 : 2)));
       scale_piece<BF16, OB>(Range<BF16>(e, tab.shift, worker, piece), static_cast<uint8_t*>(e.out) + at * (OB ? 2 : 4), f);
