@@ -217,8 +217,23 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const double* part,
   if (threadIdx.x == 0) norm[blockIdx.x] = n;
 }
 
-// min(1, max_norm / norm): NaN for a NaN norm, 0 for an infinite one.
-__device__ __forceinline__ float clip_factor(float norm, float max_norm) { return norm <= max_norm ? 1.f : __fdiv_rn(max_norm, norm); }
+// f = min(1, max_norm / norm), to be multiplied by as p and then as q: NaN for a NaN norm, 0 for an infinite one.  p is 1 but where
+// f is below 2^-100: below 2^-126 fp32 holds it with few bits or not at all, though f g may be an ordinary number.  There p is a power
+// of two and q of full precision (from f = 2^-252 on; below, no product reaches 2^-124, and q is off by 2^-150); a value that p takes
+// below fp32's normal range has a product below 2^-149.
+struct Factor {
+  float p, q;
+  __device__ __forceinline__ float operator()(float x) const { return x * p * q; }
+  __device__ __forceinline__ bool one() const { return p == 1.f && q == 1.f; }
+};
+__device__ __forceinline__ Factor clip_factor(float norm, float max_norm) {
+  if (norm <= max_norm) return {1.f, 1.f};
+  float q = __fdiv_rn(max_norm, norm);
+  if (!(q < 0x1p-100f) || norm == INFINITY) return {1.f, q};
+  q = __fdiv_rn(max_norm * 0x1p64f, norm);  // (max_norm is below 2^28)
+  if (q >= 0x1p-126f) return {0x1p-64f, q};
+  return {0x1p-126f, __fdiv_rn(max_norm * 0x1p126f, norm)};  // (below 2^-62)
+}
 
 // The 16 bytes that begin `shift` (an even number, below 16) bytes behind a's first, of a and what follows it, b.
 __device__ __forceinline__ uint4 funnel(const uint4& a, const uint4& b, int shift) {
@@ -237,10 +252,10 @@ __device__ __forceinline__ uint4 funnel(const uint4& a, const uint4& b, int shif
 
 // 16 bytes of values times f to `to`, in 8, 16 or 32 bytes.
 template <bool BF16, bool OB>
-__device__ __forceinline__ void scale_vector(const uint4& r, void* to, float f) {
+__device__ __forceinline__ void scale_vector(const uint4& r, void* to, Factor f) {
   float x[8];
   int k = 0;
-  each<BF16>(r, [&](float q) { x[k++] = q * f; });
+  each<BF16>(r, [&](float q) { x[k++] = f(q); });
   const auto pair = [&](int q) { return (uint32_t)f2bf(x[q]) | (uint32_t)f2bf(x[q + 1]) << 16; };
   if constexpr (OB && BF16) {
     __stcs(static_cast<uint4*>(to), make_uint4(pair(0), pair(2), pair(4), pair(6)));
@@ -254,13 +269,13 @@ __device__ __forceinline__ void scale_vector(const uint4& r, void* to, float f) 
 
 // A piece's values times f to its place, by a warp.  (Stores that leave L2 to the gradients that are still to be read.)
 template <bool BF16, bool OB>
-__device__ __forceinline__ void scale_piece(const Range<BF16>& r, uint8_t* out, float f) {
+__device__ __forceinline__ void scale_piece(const Range<BF16>& r, uint8_t* out, Factor f) {
   const int lane = threadIdx.x & 31;
   constexpr int z = BF16 ? 2 : 4, oz = OB ? 2 : 4, width = 16 / z;  // bytes of a value; values of 16 bytes
   const auto one = [&](int i) {
     const float v = BF16 ? bf2f(reinterpret_cast<const uint16_t*>(r.p)[i]) : reinterpret_cast<const float*>(r.p)[i];
-    if constexpr (OB) reinterpret_cast<uint16_t*>(out)[i] = f2bf(v * f);
-    else reinterpret_cast<float*>(out)[i] = v * f;
+    if constexpr (OB) reinterpret_cast<uint16_t*>(out)[i] = f2bf(f(v));
+    else reinterpret_cast<float*>(out)[i] = f(v);
   };
   constexpr int align = width * oz < 16 ? width * oz : 16;  // of a store
   if ((reinterpret_cast<uintptr_t>(out) + r.head * oz) % align == 0) {
@@ -305,13 +320,13 @@ __device__ __forceinline__ void scale_piece(const Range<BF16>& r, uint8_t* out, 
 }
 // Every `stride`-th piece of a worker, times f, from the last to the first: L2 still holds what was read last.
 template <bool BF16, bool OB, int MAX>
-__device__ __forceinline__ void scale_pieces(const Table<MAX>& tab, int64_t worker, uint32_t p, uint32_t stride, float f) {
+__device__ __forceinline__ void scale_pieces(const Table<MAX>& tab, int64_t worker, uint32_t p, uint32_t stride, Factor f) {
   if (p >= tab.end) return;
   for (p += (tab.end - 1 - p) / stride * stride;; p -= stride) {
     const int t = find(tab, p);
     const Entry& e = tab.e[t];
     // (left as it is only where this worker's place is the one that was read: the first worker's may be, and no other's)
-    if (f != 1.f || e.out != e.in || (worker && e.out_gs != e.gs)) {
+    if (!f.one() || e.out != e.in || (worker && e.out_gs != e.gs)) {
       const uint32_t piece = p - tab.first[t];
       const int64_t at = worker * e.out_gs + ((int64_t)piece << (tab.shift - (BF16 ? 1 : 2)));
       scale_piece<BF16, OB>(Range<BF16>(e, tab.shift, worker, piece), static_cast<uint8_t*>(e.out) + at * (OB ? 2 : 4), f);
@@ -393,14 +408,14 @@ template <bool GB, bool MOM, bool NEST, bool SHADOW, bool WIDE>
 __global__ void __launch_bounds__(256) clipped_update_kernel(const UpdateArgs a) {
   pdl_begin();
   const int64_t k = blockIdx.y, stride = (int64_t)gridDim.x * blockDim.x, first = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  const float f = clip_factor(a.norm[k], a.max_norm);
+  const Factor f = clip_factor(a.norm[k], a.max_norm);
   float *w = a.w + k * a.w_gs, *u = a.u + (MOM ? k * a.w_gs : 0);
   uint16_t* wb = a.wb + (SHADOW ? k * a.w_gs : 0);
   const float* gf = static_cast<const float*>(a.g) + (GB ? 0 : k * a.g_gs);
   const uint16_t* gb = static_cast<const uint16_t*>(a.g) + (GB ? k * a.g_gs : 0);
   const auto one = [&](int64_t i) {
     float wv = w[i], uv = MOM ? u[i] : 0.f;
-    sgd_elem<MOM, NEST>(wv, uv, f * (GB ? bf2f(gb[i]) : gf[i]), a.lr, a.m, i < a.decay_end ? a.wd : 0.f);
+    sgd_elem<MOM, NEST>(wv, uv, f(GB ? bf2f(gb[i]) : gf[i]), a.lr, a.m, i < a.decay_end ? a.wd : 0.f);
     w[i] = wv;
     if (MOM) u[i] = uv;
     if (SHADOW) wb[i] = f2bf(wv);
@@ -421,7 +436,7 @@ __global__ void __launch_bounds__(256) clipped_update_kernel(const UpdateArgs a)
       if (MOM) *reinterpret_cast<float4*>(uv) = __ldcs(reinterpret_cast<const float4*>(u) + i);
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        sgd_elem<MOM, NEST>(wv[k], uv[k], f * gv[k], a.lr, a.m, 4 * i + k < a.decay_end ? a.wd : 0.f);
+        sgd_elem<MOM, NEST>(wv[k], uv[k], f(gv[k]), a.lr, a.m, 4 * i + k < a.decay_end ? a.wd : 0.f);
       if (MOM) __stcs(reinterpret_cast<float4*>(u) + i, *reinterpret_cast<float4*>(uv));
       __stcs(reinterpret_cast<float4*>(w) + i, *reinterpret_cast<float4*>(wv));
       if (SHADOW)
