@@ -564,8 +564,8 @@ lsgd_status lsgd_layernorm_backward(const void* x, int x_type, int64_t x_ld, con
  * graphs keep what they need).  At most 65535 workers, 2^22 tensors times workers, 2^42 bytes a worker.
  *
  * lsgd_gradient_norm writes norm [G] (fp32); lsgd_gradient_clip writes norm (before clipping) and the clipped gradients.  Squares are
- * summed in 64 bits in a fixed order: deterministic, and no finite gradient overflows or vanishes (a norm above fp32's range is
- * infinite).  A NaN among a worker's gradients makes its norm and all of its clipped gradients NaN, an infinite value
+ * summed in 64 bits in a fixed order: deterministic, and no finite gradient overflows or vanishes: a norm above fp32's range is
+ * infinite as it is written, but f is formed from the norm that it stands for.  A NaN among a worker's gradients makes its norm and all of its clipped gradients NaN, an infinite value
  * makes its norm infinite, f zero and its own product NaN; other workers' are not touched.  Workers with f = 1 are
  * copied, or left as they are where they are clipped in place.  max_norm is positive and finite.
  *
@@ -595,7 +595,8 @@ lsgd_status lsgd_gradient_clip(const lsgd_tensors* list, float* norm, float max_
  * of worker k's n,  u = momentum u + g';  w -= lr (nesterov ? g' + momentum u : u), or w -= lr g' without momentum (u not
  * touched, may be NULL); Wb (optional) receives bf16(w).  w, u and Wb at stride w_gs, g (fp32 or bf16) at g_gs >= n; any n and
  * strides (vectors where they and the pointers allow).  f = 1 gives lsgd_sgd_update's bits.  A NaN norm makes its own worker's w
- * NaN, an infinite one takes a step without the gradient (its infinite values excepted).  LSGD_EINVAL on bad arguments and
+ * NaN, an infinite one takes a step without the gradient (its infinite values excepted), also where it is that of finite gradients
+ * beyond fp32's range, which norm [G] cannot tell apart (lsgd_gradient_clip does).  LSGD_EINVAL on bad arguments and
  * where w, u or Wb overlap another tensor (tensors whose strides or sizes of values differ count as wholes). */
 lsgd_status lsgd_clipped_update(float* w, float* u, int64_t w_gs, const void* g, int g_type, int64_t g_gs,
                                 uint16_t* Wb, int G, int64_t n, const float* norm, float max_norm,

@@ -204,35 +204,39 @@ __global__ void __launch_bounds__(kThreads, 4) grad_squares_kernel(const __grid_
   else part[(int64_t)blockIdx.y * slots + slot + blockIdx.x] = s;
 }
 
-// A worker's norm from its CTAs' sums, in thread 0.
-__device__ __forceinline__ float norm_of_parts(const double* part, int slots, int worker) {
+// A worker's sum of squares from its CTAs' sums, in thread 0.
+__device__ __forceinline__ double sum_of_parts(const double* part, int slots, int worker) {
   double s = 0.0;
   for (int i = threadIdx.x; i < slots; i += kThreads) s += part[(int64_t)worker * slots + i];
-  s = block_sum<kThreads>(warp_sum(s));
-  return threadIdx.x ? 0.f : root(s);
+  return block_sum<kThreads>(warp_sum(s));
 }
 __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const double* part, int slots, float* norm) {
   pdl_begin();
-  const float n = norm_of_parts(part, slots, blockIdx.x);
-  if (threadIdx.x == 0) norm[blockIdx.x] = n;
+  const double s = sum_of_parts(part, slots, blockIdx.x);
+  if (threadIdx.x == 0) norm[blockIdx.x] = root(s);
 }
 
-// f = min(1, max_norm / norm), to be multiplied by as p and then as q: NaN for a NaN norm, 0 for an infinite one.  p is 1 but where
-// f is below 2^-100: below 2^-126 fp32 holds it with few bits or not at all, though f g may be an ordinary number.  There p is a power
-// of two and q of full precision (from f = 2^-252 on; below, no product reaches 2^-124, and q is off by 2^-150); a value that p takes
-// below fp32's normal range has a product below 2^-149.
+// min(1, max_norm / norm): NaN for a NaN norm, 0 for an infinite one.
+__device__ __forceinline__ float clip_factor(float norm, float max_norm) { return norm <= max_norm ? 1.f : __fdiv_rn(max_norm, norm); }
+// A factor below 2^-100, which below 2^-126 fp32 holds with few bits or not at all though f g may be an ordinary number: to be multiplied
+// by as p, a power of two, and then as q, of full precision (from f = 2^-252 on; below, no product reaches 2^-124, and q is off by
+// 2^-150).  A value that p takes below fp32's normal range has a product below 2^-149.
+constexpr float kSmallFactor = 0x1p-100f;
 struct Factor {
   float p, q;
   __device__ __forceinline__ float operator()(float x) const { return x * p * q; }
-  __device__ __forceinline__ bool one() const { return p == 1.f && q == 1.f; }
 };
-__device__ __forceinline__ Factor clip_factor(float norm, float max_norm) {
-  if (norm <= max_norm) return {1.f, 1.f};
-  float q = __fdiv_rn(max_norm, norm);
-  if (!(q < 0x1p-100f) || norm == INFINITY) return {1.f, q};
-  q = __fdiv_rn(max_norm * 0x1p64f, norm);  // (max_norm is below 2^28)
+// max_norm / (norm 2^64).
+__device__ __forceinline__ Factor small_factor(float norm, float max_norm) {
+  const float q = __fdiv_rn(max_norm, norm);
+  if (q >= 0x1p-36f) return {1.f, q * 0x1p-64f};
   if (q >= 0x1p-126f) return {0x1p-64f, q};
-  return {0x1p-126f, __fdiv_rn(max_norm * 0x1p126f, norm)};  // (below 2^-62)
+  return {0x1p-126f, __fdiv_rn(max_norm * 0x1p62f, norm)};
+}
+// Any factor, of a norm that is all that is known.
+__device__ __forceinline__ Factor any_factor(float norm, float max_norm) {
+  const float f = clip_factor(norm, max_norm);
+  return f < kSmallFactor && norm < INFINITY ? small_factor(norm, max_norm * 0x1p64f) : Factor{1.f, f};
 }
 
 // The 16 bytes that begin `shift` (an even number, below 16) bytes behind a's first, of a and what follows it, b.
@@ -252,10 +256,10 @@ __device__ __forceinline__ uint4 funnel(const uint4& a, const uint4& b, int shif
 
 // 16 bytes of values times f to `to`, in 8, 16 or 32 bytes.
 template <bool BF16, bool OB>
-__device__ __forceinline__ void scale_vector(const uint4& r, void* to, Factor f) {
+__device__ __forceinline__ void scale_vector(const uint4& r, void* to, float f) {
   float x[8];
   int k = 0;
-  each<BF16>(r, [&](float q) { x[k++] = f(q); });
+  each<BF16>(r, [&](float q) { x[k++] = q * f; });
   const auto pair = [&](int q) { return (uint32_t)f2bf(x[q]) | (uint32_t)f2bf(x[q + 1]) << 16; };
   if constexpr (OB && BF16) {
     __stcs(static_cast<uint4*>(to), make_uint4(pair(0), pair(2), pair(4), pair(6)));
@@ -269,13 +273,13 @@ __device__ __forceinline__ void scale_vector(const uint4& r, void* to, Factor f)
 
 // A piece's values times f to its place, by a warp.  (Stores that leave L2 to the gradients that are still to be read.)
 template <bool BF16, bool OB>
-__device__ __forceinline__ void scale_piece(const Range<BF16>& r, uint8_t* out, Factor f) {
+__device__ __forceinline__ void scale_piece(const Range<BF16>& r, uint8_t* out, float f) {
   const int lane = threadIdx.x & 31;
   constexpr int z = BF16 ? 2 : 4, oz = OB ? 2 : 4, width = 16 / z;  // bytes of a value; values of 16 bytes
   const auto one = [&](int i) {
     const float v = BF16 ? bf2f(reinterpret_cast<const uint16_t*>(r.p)[i]) : reinterpret_cast<const float*>(r.p)[i];
-    if constexpr (OB) reinterpret_cast<uint16_t*>(out)[i] = f2bf(f(v));
-    else reinterpret_cast<float*>(out)[i] = f(v);
+    if constexpr (OB) reinterpret_cast<uint16_t*>(out)[i] = f2bf(v * f);
+    else reinterpret_cast<float*>(out)[i] = v * f;
   };
   constexpr int align = width * oz < 16 ? width * oz : 16;  // of a store
   if ((reinterpret_cast<uintptr_t>(out) + r.head * oz) % align == 0) {
@@ -320,13 +324,13 @@ __device__ __forceinline__ void scale_piece(const Range<BF16>& r, uint8_t* out, 
 }
 // Every `stride`-th piece of a worker, times f, from the last to the first: L2 still holds what was read last.
 template <bool BF16, bool OB, int MAX>
-__device__ __forceinline__ void scale_pieces(const Table<MAX>& tab, int64_t worker, uint32_t p, uint32_t stride, Factor f) {
+__device__ __forceinline__ void scale_pieces(const Table<MAX>& tab, int64_t worker, uint32_t p, uint32_t stride, float f) {
   if (p >= tab.end) return;
   for (p += (tab.end - 1 - p) / stride * stride;; p -= stride) {
     const int t = find(tab, p);
     const Entry& e = tab.e[t];
     // (left as it is only where this worker's place is the one that was read: the first worker's may be, and no other's)
-    if (!f.one() || e.out != e.in || (worker && e.out_gs != e.gs)) {
+    if (f != 1.f || e.out != e.in || (worker && e.out_gs != e.gs)) {
       const uint32_t piece = p - tab.first[t];
       const int64_t at = worker * e.out_gs + ((int64_t)piece << (tab.shift - (BF16 ? 1 : 2)));
       scale_piece<BF16, OB>(Range<BF16>(e, tab.shift, worker, piece), static_cast<uint8_t*>(e.out) + at * (OB ? 2 : 4), f);
@@ -335,25 +339,71 @@ __device__ __forceinline__ void scale_pieces(const Table<MAX>& tab, int64_t work
   }
 }
 
+// Every `stride`-th piece of a worker from p on, times its small factor; false, and nothing done, where there is none: the norm is
+// that of an infinite value.  `squares`: the norm's square, which holds what the norm does not where this passes fp32's range (and its root
+// does not times 2^-64); NULL: to be summed, by a CTA that has all of the worker's pieces.  Rare: value by value, and apart from the
+// kernels' own code (in it, factors of two parts for every value cost clip_ragged 1 to 2 %).
+template <int THREADS, bool BF16, bool OB, int MAX>
+__device__ __noinline__ bool scale_by_small(const Table<MAX>& tab, int64_t worker, uint32_t p, uint32_t stride, float norm,
+                                            const double* squares, float max_norm) {
+  Factor f;
+  if (norm < INFINITY) {
+    f = small_factor(norm, max_norm * 0x1p64f);
+  } else {
+    __shared__ double sum;
+    if (!squares) {
+      const double s = block_sum<THREADS>(squares_of<BF16>(tab, worker, p, stride));
+      if (threadIdx.x == 0) sum = s;
+      __syncthreads();
+      squares = &sum;
+    }
+    if (!(*squares < INFINITY)) return false;
+    f = small_factor(root(*squares * 0x1p-128), max_norm);
+  }
+  for (uint64_t at_piece = p; at_piece < tab.end; at_piece += stride) {
+    const int t = find(tab, (uint32_t)at_piece);
+    const Entry& e = tab.e[t];
+    const uint32_t piece = (uint32_t)at_piece - tab.first[t];
+    const Range<BF16> r(e, tab.shift, worker, piece);
+    const int64_t at = worker * e.out_gs + ((int64_t)piece << (tab.shift - (BF16 ? 1 : 2)));
+    for (int i = threadIdx.x & 31; i < r.len; i += 32) {
+      const float v = f(BF16 ? bf2f(reinterpret_cast<const uint16_t*>(r.p)[i]) : reinterpret_cast<const float*>(r.p)[i]);
+      if constexpr (OB) static_cast<uint16_t*>(e.out)[at + i] = f2bf(v);
+      else static_cast<float*>(e.out)[at + i] = v;
+    }
+  }
+  return true;
+}
+// What a worker's norm makes of its gradients.
+template <int THREADS, bool BF16, bool OB, int MAX>
+__device__ __forceinline__ void clip_pieces(const Table<MAX>& tab, int64_t worker, uint32_t p, uint32_t stride, float norm,
+                                            const double* squares, float max_norm) {
+  const float f = clip_factor(norm, max_norm);
+  if (f < kSmallFactor && scale_by_small<THREADS, BF16, OB>(tab, worker, p, stride, norm, squares, max_norm)) return;
+  scale_pieces<BF16, OB>(tab, worker, p, stride, f);
+}
+
 // The second of two launches: every CTA adds its worker's sums up by itself.
 template <int MAX, bool BF16, bool OB>
 __global__ void __launch_bounds__(kThreads, 4) grad_scale_kernel(const __grid_constant__ Table<MAX> tab, const double* part, int slots,
                                                                  float* norm, float max_norm) {
   pdl_begin();
   __shared__ float shared;
+  __shared__ double squares;
+  const uint32_t p = tab.begin + blockIdx.x * kWarps + threadIdx.x / 32, stride = gridDim.x * kWarps;
   float n;
   if (slots > 1) {
-    n = norm_of_parts(part, slots, blockIdx.y);
+    const double s = sum_of_parts(part, slots, blockIdx.y);
     if (threadIdx.x == 0) {
-      shared = n;
-      if (blockIdx.x == 0) norm[blockIdx.y] = n;
+      shared = root(s), squares = s;
+      if (blockIdx.x == 0) norm[blockIdx.y] = shared;
     }
     __syncthreads();
     n = shared;
   } else {
-    n = norm[blockIdx.y];  // (a worker's only CTA has written it in the first launch)
+    n = norm[blockIdx.y];  // (a worker's only CTA has written it in the first launch, but not the sum that it is the root of)
   }
-  scale_pieces<BF16, OB>(tab, blockIdx.y, tab.begin + blockIdx.x * kWarps + threadIdx.x / 32, gridDim.x * kWarps, clip_factor(n, max_norm));
+  clip_pieces<kThreads, BF16, OB>(tab, blockIdx.y, p, stride, n, slots > 1 ? &squares : nullptr, max_norm);
 }
 
 // Both in one launch, a worker to a cluster: the CTAs' sums meet in shared memory.
@@ -380,18 +430,20 @@ __global__ void __launch_bounds__(kClusterThreads) grad_cluster_kernel(const __g
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   }
   __shared__ float shared;
+  __shared__ double squares;
   if (threadIdx.x == 0) {
     if (cl > 1) {
       s = 0.0;
       for (uint32_t i = 0; i < cl; ++i) s += sums[i];
     }
     shared = root(s);
+    if (CLIP) squares = s;
     if (blockIdx.x == 0) norm[blockIdx.y] = shared;
   }
   if constexpr (!CLIP) return;
   __syncthreads();
   const float n = shared;
-  if constexpr (CLIP) scale_pieces<BF16, OB>(tab, blockIdx.y, p, stride, clip_factor(n, max_norm));
+  if constexpr (CLIP) clip_pieces<kClusterThreads, BF16, OB>(tab, blockIdx.y, p, stride, n, &squares, max_norm);
 }
 
 // ---- the local update with the clipped gradient ----
@@ -408,7 +460,7 @@ template <bool GB, bool MOM, bool NEST, bool SHADOW, bool WIDE>
 __global__ void __launch_bounds__(256) clipped_update_kernel(const UpdateArgs a) {
   pdl_begin();
   const int64_t k = blockIdx.y, stride = (int64_t)gridDim.x * blockDim.x, first = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  const Factor f = clip_factor(a.norm[k], a.max_norm);
+  const Factor f = any_factor(a.norm[k], a.max_norm);
   float *w = a.w + k * a.w_gs, *u = a.u + (MOM ? k * a.w_gs : 0);
   uint16_t* wb = a.wb + (SHADOW ? k * a.w_gs : 0);
   const float* gf = static_cast<const float*>(a.g) + (GB ? 0 : k * a.g_gs);

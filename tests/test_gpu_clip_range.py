@@ -77,7 +77,38 @@ def test_small_factors_keep_their_bits(P, G, n, types, scale, limit):
     assert bool(((norm.double() - want).abs() <= NORM * want).all())
 
 
-# The same of the update: w = 0, so that w = -lr g' shows the clipped gradient.  Vectors, and single values at odd strides.
+# Finite gradients whose norm passes fp32's range (and is infinite as it is given) are clipped by the norm that they have.
+@pytest.mark.gpu
+@pytest.mark.parametrize("G,n", FORMS)
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("limit", [3e38, 1.0, 1e-30])
+def test_norms_beyond_fp32(P, G, n, types, limit):
+    norm, want = _clip_both_ways(P, G, n, types, 2e37, float(np.float32(limit)), 1.0)
+    ordinary = norm[[k for k in range(G) if k != 1]].double()
+    assert bool(norm[1] == float("inf")) and float(want[1]) > 4e38
+    assert bool(((ordinary - want[[k for k in range(G) if k != 1]]).abs() <= NORM * ordinary).all())
+
+
+@pytest.mark.gpu
+def test_norms_beyond_fp32_of_several_types(P):
+    import torch
+
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    grads = [(torch.randn(3, n, generator=gen, device="cuda", dtype=torch.float64) * 3e37).to(t)
+             for n, t in ((5000, torch.float32), (777, torch.bfloat16), (3, torch.float32))]
+    grads[0][2, 4] = float("inf")
+    squares = sum(_norm64(g) ** 2 for g in grads)
+    outs, norm = [torch.empty_like(g) for g in grads], torch.empty(3, device="cuda")
+    P.lsgd_gradient_clip(P.lsgd_tensors_create(grads, outs), norm, 5.0)
+    torch.cuda.synchronize()
+    assert bool((norm == float("inf")).all())
+    for g, o in zip(grads, outs):
+        assert _close(torch, o[:2], g[:2].double() * (5.0 / squares[:2].sqrt())[:, None], FACTOR)
+    # an infinite value: zeros, and its own product NaN
+    assert bool(torch.isnan(outs[0][2, 4])) and bool((outs[1][2] == 0).all()) and bool((outs[0][2, 5:] == 0).all())
+
+
+# Small factors of the update: w = 0, so that w = -lr g' shows the clipped gradient.  Vectors, and single values at odd strides.
 @pytest.mark.gpu
 @pytest.mark.parametrize("g_type", ["fp32", "bf16"])
 @pytest.mark.parametrize("n,stride", [(1000, 1000), (1001, 1003)])
