@@ -519,15 +519,17 @@ lsgd_status lsgd_groupnorm_backward(const void* x, int x_type, const void* y, co
  * gamma and beta worker g's C values at gamma + g par_gs and beta + g par_gs (par_gs >= C).  mean and rstd [G][R] fp32 are
  * written too.  What lies between the rows (columns C to the stride) is neither read nor written.
  * Types, activations and their accuracy are group norm's (lsgd_groupnorm_forward).  Statistics are fp32, the deviations taken from
- * the mean; a row whose squared deviations pass fp32's range (values of 1e19 and more) gets rstd = 0.  Deterministic.  A NaN or
- * infinite value makes its own row NaN and no other.
+ * the mean: a row whose squared deviations pass fp32's range (values of 1e19 and more) gets rstd = 0, as long as the magnitudes of
+ * its values add up to less than 3.4e38; beyond, its mean may be infinite and the row NaN.  Deterministic.  A NaN or infinite value
+ * makes its own row NaN, and no row changes another.
  *
  * No workspace, no allocation: the call may be captured into a CUDA graph.  G <= 65535, 1 <= C <= 32768, R >= 0 (0: nothing is
  * done), G R <= 2^36; any C, strides >= C and any alignment of at least the element's (vectors of up to 16 bytes are used where
  * strides and pointers allow).  LSGD_EINVAL on anything else and where what is written overlaps any other tensor (rows
  * count from the first row's first to the last row's last value).  Device pointers, asynchronous on `stream`, which belongs
- * to the current device; lsgd_device_status reports a device-side wait that ran out (the CTAs that share a row of more than
- * 2048 values wait for one another). */
+ * to the current device; lsgd_device_status reports a device-side wait that ran out (the CTAs that share a row wait for
+ * one another: rows of more than 4096 values, in a backward that reads three or four tensors of bf16 values one by one of more than
+ * 2048). */
 lsgd_status lsgd_layernorm_forward(const void* x, const void* r, int x_type, int64_t x_ld,
                                    const float* gamma, const float* beta, int64_t par_gs, void* s,
                                    void* y, int y_type, int64_t y_ld, float* mean, float* rstd, int G,
