@@ -566,10 +566,12 @@ lsgd_status lsgd_layernorm_backward(const void* x, int x_type, int64_t x_ld, con
  * graphs keep what they need).  At most 65535 workers, 2^22 tensors times workers, 2^42 bytes a worker.
  *
  * lsgd_gradient_norm writes norm [G] (fp32); lsgd_gradient_clip writes norm (before clipping) and the clipped gradients.  Squares are
- * summed in 64 bits in a fixed order: deterministic, and no finite gradient overflows or vanishes: a norm above fp32's range is
- * infinite as it is written, but f is formed from the norm that it stands for.  A NaN among a worker's gradients makes its norm and all of its clipped gradients NaN, an infinite value
- * makes its norm infinite, f zero and its own product NaN; other workers' are not touched.  Workers with f = 1 are
- * copied, or left as they are where they are clipped in place.  max_norm is positive and finite.
+ * summed in fp32 within pieces of at most 4 KB, in 64 bits from there on (and within pieces whose fp32 sum would overflow or lose
+ * bits), in a fixed order: deterministic, and norm is off by at most 2.3e-6 of it.  No finite gradient overflows or vanishes: a
+ * norm above fp32's range is infinite as it is written, but f is formed from the norm that it stands for.  A NaN among a worker's
+ * gradients makes its norm and all of its clipped gradients NaN, an infinite value makes its norm infinite, f zero and its own
+ * product NaN; other workers' are not touched.  Workers with f = 1 are copied, or left as they are where they are clipped in
+ * place.  max_norm is positive and finite.
  *
  * `workspace`: device memory of at least lsgd_gradient_workspace's bytes (0: it is not used and may be NULL), 16-byte
  * aligned, whose contents do not matter before or after; calls (or captured graphs) that may run at the same time need
