@@ -84,20 +84,7 @@ struct Vec {
 #pragma unroll
     for (int i = 0; i < kN; ++i) reinterpret_cast<Raw*>(p)[i] = r[i];
   }
-  // The first `left` values alone (what lies behind them is not touched; zeros stand for it).
-  __device__ __forceinline__ void load_first(const T* p, int left) {
-    if (left >= V) {
-      load(p);
-      return;
-    }
-    zero();
-#pragma unroll
-    for (int j = 0; j < V - 1; ++j)
-      if (j < left) {
-        if constexpr (sizeof(T) == 4) reinterpret_cast<float*>(r)[j] = __ldg(p + j);
-        else reinterpret_cast<uint32_t*>(r)[j / 2] |= (uint32_t)__ldg(p + j) << 16 * (j & 1);
-      }
-  }
+  // The first `left` values alone (what lies behind them is not touched).
   __device__ __forceinline__ void store_first(T* p, int left) const {
     if (left >= V) {
       store(p);
@@ -109,10 +96,6 @@ struct Vec {
         if constexpr (sizeof(T) == 4) p[j] = reinterpret_cast<const float*>(r)[j];
         else p[j] = (T)(reinterpret_cast<const uint32_t*>(r)[j / 2] >> 16 * (j & 1));
       }
-  }
-  __device__ __forceinline__ void zero() {
-#pragma unroll
-    for (int i = 0; i < kN; ++i) r[i] = Raw{};
   }
   __device__ __forceinline__ void stream(T* p) const {  // leaves L2 to what will be read again
 #pragma unroll
