@@ -78,3 +78,45 @@ def test_the_first_place_in_common_as_rows_of_a_buffer(P, limit):
     P.lsgd_gradient_clip(P.lsgd_tensors_create([g], [out]), norm, limit)
     torch.cuda.synchronize()
     assert torch.equal(out, held * _factor(torch, norm, limit)) and torch.equal(buf[1], held[1])
+
+
+# Layouts that a list may have, by (first value, workers' stride) in one buffer of values of a type, where what is written meets nothing
+# else: they are taken, and every value comes out as if it stood alone.  None: clipped in place.
+LAYOUTS = {
+    "pieces of one buffer, in place": [((0, 200), None, 100), ((100, 200), None, 100)],
+    "in place by name": [((0, 200), (0, 200), 100)],
+    "in place by name, beside others": [((0, 200), (0, 200), 100), ((100, 200), (1000, 100), 100)],
+    "read twice, written apart": [((0, 100), (1000, 100), 100), ((0, 100), (2000, 100), 100)],
+    "read twice in part, written apart": [((0, 150), (1000, 150), 150), ((50, 150), (2000, 100), 100)],
+    "written between what is read": [((0, 300), (100, 300), 100), ((200, 300), (1000, 100), 100)],
+    "written into the gaps of what is written": [((1000, 100), (0, 300), 100), ((2000, 100), (100, 300), 100), ((3000, 100), (200, 300), 100)],
+    "pieces that end where the next begins, written the other way round": [((0, 64), (2031, 64), 33), ((33, 64), (2000, 64), 31)],
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", list(LAYOUTS))
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("times", [1, 1001])
+def test_layouts_that_are_taken(P, name, dtype, times):
+    import torch
+
+    G, t = 3, _types(torch, dtype)
+    layout = [(i, o, n) for i, o, n in LAYOUTS[name]]
+    buf = torch.full((4000 * times,), 77.0, device="cuda", dtype=t)
+    at = lambda place, n: buf.as_strided((G, n * times), (place[1] * times, 1), place[0] * times)  # noqa: E731
+    grads = [at(i, n) for i, _, n in layout]
+    _fill(torch, grads, times)
+    outs = None if layout[0][1] is None else [at(o, n) for _, o, n in layout]
+    held, before = [g.clone() for g in grads], buf.clone()
+    norm = torch.empty(G, device="cuda")
+    limit = float(sum((g[0].double() ** 2).sum() for g in grads) ** 0.5 * 1.01)  # workers 0 and 2 below it
+    P.lsgd_gradient_clip(P.lsgd_tensors_create(grads, outs), norm, limit)
+    torch.cuda.synchronize()
+    want_norm = sum((h.double() ** 2).sum(1) for h in held).sqrt()
+    assert ((norm.double() - want_norm).abs() <= 37 * 2.0 ** -24 * want_norm).all()
+    f, want = _factor(torch, norm, limit), before
+    assert bool(f[0] == 1) and bool(f[1] < 1)
+    for h, (i, o, n) in zip(held, layout):
+        want.as_strided((G, n * times), ((o or i)[1] * times, 1), (o or i)[0] * times).copy_((h.float() * f).to(t))
+    assert torch.equal(buf, want)
