@@ -342,7 +342,7 @@ __device__ __forceinline__ void scale_pieces(const Table<MAX>& tab, int64_t work
 // Every `stride`-th piece of a worker from p on, times its small factor; false, and nothing done, where there is none: the norm is
 // that of an infinite value.  `squares`: the norm's square, which holds what the norm does not where this passes fp32's range (and its root
 // does not times 2^-64); NULL: to be summed, by a CTA that has all of the worker's pieces.  Rare: value by value, and apart from the
-// kernels' own code (in it, factors of two parts for every value cost clip_ragged 1 to 2 %).
+// kernels' own code (with factors of two parts for every value there, 300 ragged bf16 tensors of 26 MB took 19.5 to 19.8 us, and take 19.3).
 template <int THREADS, bool BF16, bool OB, int MAX>
 __device__ __noinline__ bool scale_by_small(const Table<MAX>& tab, int64_t worker, uint32_t p, uint32_t stride, float norm,
                                             const double* squares, float max_norm) {
